@@ -1,0 +1,267 @@
+// Host side of ttc_causal_conv, ttc_causal_conv_step and ttc_causal_conv_grad.
+#include "block_host.h"
+#include "causal_conv.cuh"
+
+using namespace ttc;
+using namespace ttc::blk;
+using namespace ttc::conv;
+
+namespace {
+
+int check(const ttc_conv_args* a, bool step)
+{
+    if (!a)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "arguments are null");
+    TTC_TRY(check_dtype(a->dtype, true));
+    TTC_TRY(check_sequences(a->batch, step ? 1 : a->tokens, step ? nullptr : a->seq_offsets));
+    if (a->d < 1)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "d = %d", a->d);
+    if (a->taps < 2 || a->taps > 4)
+        return fail(TTC_STATUS_UNSUPPORTED, "%d taps: 2 to 4 are served", a->taps);
+    if (a->act != TTC_ACT_NONE && a->act != TTC_ACT_SILU)
+        return fail(TTC_STATUS_UNSUPPORTED, "activation %d of a convolution", a->act);
+    if ((a->d + kThreads - 1) / kThreads > kMaxGridY)
+        return fail(TTC_STATUS_UNSUPPORTED, "d = %d", a->d);
+    TTC_TRY(check_rows("x", a->x, a->dtype, step ? a->batch == 0 : a->tokens == 0 || a->batch == 0));
+    TTC_TRY(check_floats("w", a->w, false));
+    TTC_TRY(check_floats("bias", a->bias, true));
+    TTC_TRY(check_floats("state", a->state, true, element_size(a->dtype)));
+    return check_floats("state_out", a->state_out, true, element_size(a->dtype));
+}
+
+// Channels that a thread takes at once: 16 bytes, 4 or an element, by the alignment of every pointer and stride.
+struct Width {
+    size_t size;
+    int d, v;
+    Width(int dtype, int d_) : size(element_size(dtype)), d(d_), v(16 / (int)element_size(dtype)) {}
+    void fit(const void* p, int64_t s0, int64_t s1)
+    {
+        while (v > 1 && (reinterpret_cast<uintptr_t>(p) % (v * size) || s0 % v || s1 % v))
+            v = v * (int)size > 4 ? (int)(4 / size) : 1;
+    }
+    void rows(const ttc_rows& r, bool packed, bool step)
+    {
+        if (r.ptr)
+            fit(r.ptr, packed ? 0 : r.bstride, step ? 0 : r.tstride);
+    }
+    void window(const void* p)
+    {
+        if (p)
+            fit(p, d, d);
+    }
+};
+
+ConvDev to_dev(const ttc_conv_args* a, bool step)
+{
+    ConvDev p = {};
+    const int32_t* off = step ? nullptr : a->seq_offsets;
+    p.seqs = Seqs{off, a->batch, step ? 1 : a->tokens};
+    p.d = a->d;
+    p.act = a->act;
+    p.x = dev_rows(a->x, off);
+    p.y = dev_rows(a->y, off);
+    p.w = a->w;
+    p.bias = a->bias;
+    p.state = a->state;
+    p.state_out = a->state_out;
+    return p;
+}
+
+// Tokens of a tile: 128, or fewer (not below 16) while there are less than about eight blocks for every SM.  A tile reads
+// the W - 1 rows in front of it again.
+void set_tiles(ConvDev& p, int v, int sms)
+{
+    const int64_t cols = (p.d + (int64_t)v * kThreads - 1) / (v * kThreads);
+    const int64_t seqs = p.seqs.offsets ? 1 : p.seqs.batch;
+    p.tile = 128;
+    while (p.tile > 16 && seqs * ((p.seqs.tokens + p.tile - 1) / p.tile) * cols < 8 * (int64_t)sms)
+        p.tile /= 2;
+    p.tiles = (p.seqs.tokens + p.tile - 1) / p.tile;
+}
+
+int64_t all_tiles(const ConvDev& p) { return p.tiles * (p.seqs.offsets ? 1 : p.seqs.batch); }
+
+template <typename F> int by_shape(int dtype, int v, int taps, F&& f)
+{
+    return by_type(dtype, [&](auto t) {
+        using T = decltype(t);
+        constexpr int most = 16 / (int)sizeof(T), two = 4 / (int)sizeof(T);
+        auto with_v = [&](auto vc) {
+            constexpr int V = decltype(vc)::value;
+            switch (taps) {
+            case 2: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 2>());
+            case 3: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 3>());
+            default: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 4>());
+            }
+        };
+        if (v == most)
+            return with_v(std::integral_constant<int, most>());
+        if (two > 1 && v == two)
+            return with_v(std::integral_constant<int, two>());
+        return with_v(std::integral_constant<int, 1>());
+    });
+}
+
+struct GradPlan {
+    ConvDev p;
+    int v;
+    size_t bytes;
+    bool params;
+};
+
+int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void* ws, GradPlan& o)
+{
+    TTC_TRY(check(a, false));
+    if (!g)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "gradients are null");
+    TTC_TRY(check_rows("dy", g->dy, a->dtype, a->tokens == 0 || a->batch == 0));
+    TTC_TRY(check_rows("dx", g->dx, a->dtype, true));
+    TTC_TRY(check_floats("dw", g->dw, true));
+    TTC_TRY(check_floats("dbias", g->dbias, true));
+    TTC_TRY(check_floats("dstate", g->dstate, true, element_size(a->dtype)));
+    TTC_TRY(check_floats("dstate_out", g->dstate_out, true, element_size(a->dtype)));
+    const bool packed = a->seq_offsets;
+    const size_t size = element_size(a->dtype);
+    if (rows_overlap(g->dx, a->d, a->x, a->d, a->batch, a->tokens, packed, size) ||
+        rows_overlap(g->dx, a->d, g->dy, a->d, a->batch, a->tokens, packed, size))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "dx overlaps x or dy");
+    if (g->dstate && (g->dstate == g->dstate_out || g->dstate == a->state))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "dstate overlaps state or dstate_out");
+    ConvDev& p = o.p;
+    p = to_dev(a, false);
+    p.dy = dev_rows(g->dy, a->seq_offsets);
+    p.dx = dev_rows(g->dx, a->seq_offsets);
+    p.dstate_out = g->dstate_out;
+    p.dstate = g->dstate;
+    p.dw = g->dw;
+    p.dbias = g->dbias;
+    Width w(a->dtype, a->d);
+    w.rows(a->x, packed, false);
+    w.rows(g->dy, packed, false);
+    w.rows(g->dx, packed, false);
+    w.window(a->state);
+    w.window(g->dstate);
+    w.window(g->dstate_out);
+    // the working set of 8 channels, (3 W + 2) * 8 floats, does not fit a thread's registers beside the loads
+    if (w.v > 4 && size == 2)
+        w.v = 2;
+    w.fit(nullptr, a->d, 0);
+    o.v = w.v;
+    set_tiles(p, o.v, sm_count(device));
+    o.params = g->dw || g->dbias;
+    Scratch s(ws);
+    float* part = s.take<float>(o.params ? (size_t)all_tiles(p) * (a->taps + 1) * a->d : 0);
+    p.part = o.params ? part : nullptr;
+    o.bytes = s.used;
+    return TTC_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
+{
+    TTC_TRY(check(a, false));
+    TTC_TRY(check_rows("y", a->y, a->dtype, a->tokens == 0 || a->batch == 0));
+    const bool packed = a->seq_offsets;
+    if (rows_overlap(a->y, a->d, a->x, a->d, a->batch, a->tokens, packed, element_size(a->dtype)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "y overlaps x");
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    if (a->batch == 0)
+        return TTC_OK;
+    Width w(a->dtype, a->d);
+    w.rows(a->x, packed, false);
+    w.rows(a->y, packed, false);
+    w.window(a->state);
+    w.fit(nullptr, a->d, 0);
+    ConvDev p = to_dev(a, false);
+    set_tiles(p, w.v, sm_count(device));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return by_shape(a->dtype, w.v, a->taps, [&](auto t, auto vc, auto wc) {
+        using T = decltype(t);
+        constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        if (a->tokens) {
+            const dim3 grid((unsigned)all_tiles(p), (a->d + V * kThreads - 1) / (V * kThreads));
+            conv_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+            TTC_TRY(launched("causal convolution"));
+        }
+        if (a->state_out) {
+            const dim3 grid((unsigned)a->batch, (a->d + kThreads - 1) / kThreads);
+            conv_window_kernel<T, W><<<grid, kThreads, 0, st>>>(p);
+            TTC_TRY(launched("causal convolution, last windows"));
+        }
+        return TTC_OK;
+    });
+}
+
+int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stream)
+{
+    TTC_TRY(check(a, true));
+    TTC_TRY(check_rows("y", a->y, a->dtype, a->batch == 0));
+    if (!a->state_out && a->batch)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "state_out is null");
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    if (a->batch == 0)
+        return TTC_OK;
+    Width w(a->dtype, a->d);
+    w.rows(a->x, false, true);
+    w.rows(a->y, false, true);
+    w.window(a->state_out);
+    w.fit(nullptr, a->d, 0);
+    // few sequences: narrower loads keep more SMs at work
+    const int64_t blocks = a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads));
+    if (blocks < sm_count(device) && w.v * element_size(a->dtype) > 4)
+        w.v = (int)(4 / element_size(a->dtype));
+    const ConvDev p = to_dev(a, true);
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return by_shape(a->dtype, w.v, a->taps, [&](auto t, auto vc, auto wc) {
+        using T = decltype(t);
+        constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        const dim3 grid((unsigned)a->batch, (a->d + V * kThreads - 1) / (V * kThreads));
+        conv_step_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+        return launched("causal convolution, one token");
+    });
+}
+
+int64_t ttc_causal_conv_grad_workspace(int32_t device, const ttc_conv_args* a, const ttc_conv_grads* g)
+{
+    GradPlan o;
+    TTC_TRY(plan_grad(device, a, g, nullptr, o));
+    return (int64_t)o.bytes;
+}
+
+int ttc_causal_conv_grad(int32_t device, const ttc_conv_args* a, const ttc_conv_grads* g, void* workspace,
+                         int64_t workspace_bytes, void* cuda_stream)
+{
+    GradPlan o;
+    TTC_TRY(plan_grad(device, a, g, workspace, o));
+    TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    const ConvDev& p = o.p;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return by_shape(a->dtype, o.v, a->taps, [&](auto t, auto vc, auto wc) {
+        using T = decltype(t);
+        constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        const int64_t tiles = all_tiles(p);
+        if (tiles) {
+            const dim3 grid((unsigned)tiles, (a->d + V * kThreads - 1) / (V * kThreads));
+            conv_grad_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+            TTC_TRY(launched("gradients of the causal convolution"));
+        }
+        if (o.params) {
+            conv_param_kernel<W><<<dim3((a->d + 31) / 32, W + 1), 256, 0, st>>>(p, tiles);
+            TTC_TRY(launched("gradients of the causal convolution, parameters"));
+        }
+        if (p.dstate && a->batch && (a->seq_offsets || a->tokens == 0)) {
+            conv_empty_kernel<T, W><<<dim3((unsigned)a->batch, (a->d + kThreads - 1) / kThreads), kThreads, 0, st>>>(p);
+            TTC_TRY(launched("gradients of the causal convolution, empty sequences"));
+        }
+        return TTC_OK;
+    });
+}
+
+} // extern "C"

@@ -1,0 +1,429 @@
+// Host side of ttc_linear and ttc_linear_grad.
+#include <cuda.h>
+
+#include "block_host.h"
+#include "linear_rows.cuh"
+
+using namespace ttc;
+using namespace ttc::blk;
+using namespace ttc::lin;
+
+namespace {
+
+// Rows up to which W is streamed past all of x (few_rows_kernel) instead of going through tiles of 128 rows.
+constexpr int kFewRows = 32;
+
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+int encoder(EncodeTiled& f)
+{
+    static std::atomic<void*> known;
+    void* p = known.load(std::memory_order_relaxed);
+    if (!p) {
+        cudaDriverEntryPointQueryResult found;
+        TTC_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found));
+        if (found != cudaDriverEntryPointSuccess || !p)
+            return fail(TTC_STATUS_CUDA_ERROR, "the driver has no cuTensorMapEncodeTiled");
+        known.store(p, std::memory_order_relaxed);
+    }
+    f = reinterpret_cast<EncodeTiled>(p);
+    return TTC_OK;
+}
+
+// Matrix of `rows` rows of `cols` 16-bit elements, fetched in boxes of 64 columns (128 bytes, swizzled) by `box` rows.
+int encode(CUtensorMap& map, const void* ptr, int64_t rows, int64_t cols, int64_t ld, int box, bool is_bf16)
+{
+    EncodeTiled f;
+    TTC_TRY(encoder(f));
+    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * 2};
+    const cuuint32_t boxes[2] = {64, (cuuint32_t)box}, steps[2] = {1, 1};
+    const CUresult r = f(&map, is_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void*>(ptr), dims, strides,
+                         boxes, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? TTC_OK : fail(TTC_STATUS_CUDA_ERROR, "cuTensorMapEncodeTiled: error %d", (int)r);
+}
+
+bool aligned(const void* p, int64_t ld, size_t size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)size % 16 == 0; }
+
+// An operand of a product in memory: `rows` rows of `cols` elements.
+struct Operand {
+    const void* ptr;
+    int64_t rows, cols, ld;
+};
+
+// What TMA cannot read is copied into the workspace first.
+struct Aligned {
+    Operand from, to;
+    bool copy;
+};
+
+Aligned plan_operand(const Operand& o, Scratch& s)
+{
+    Aligned r{o, o, false};
+    if (!aligned(o.ptr, o.ld, 2)) {
+        r.copy = true;
+        r.to.ld = (o.cols + 7) / 8 * 8;
+        r.to.ptr = s.take<unsigned short>((size_t)o.rows * r.to.ld);
+    }
+    return r;
+}
+
+int copy_operand(const Aligned& a, cudaStream_t st)
+{
+    if (!a.copy || a.from.rows == 0)
+        return TTC_OK;
+    align_rows_kernel<<<(unsigned)a.from.rows, 256, 0, st>>>(static_cast<const unsigned short*>(a.from.ptr), a.from.ld, a.from.rows, (int)a.from.cols,
+                                                             static_cast<unsigned short*>(const_cast<void*>(a.to.ptr)), a.to.ld);
+    return launched("projection, rows aligned");
+}
+
+// A product of `M` x `N` results over `K`: how it is tiled, and the scratch of a split contraction.
+struct Product {
+    int64_t M, N, K;
+    int bn, splits;
+    float* part;
+};
+
+// Width of a tile and parts of the contraction.  The wide tile reads least per product (its operands are 192 bytes of shared
+// memory for every 256 of a 128 x 128 tile's); narrower ones, and then parts of the contraction (at least 512 indices
+// each, summed by a launch of its own), are for results with fewer tiles than there are SMs.
+Product plan_product(int64_t M, int64_t N, int64_t K, int sms, Scratch& s)
+{
+    Product p{M, N, K, 256, 1, nullptr};
+    const int64_t tm = (M + BM - 1) / BM;
+    while (p.bn > 64 && tm * ((N + p.bn - 1) / p.bn) < sms)
+        p.bn /= 2;
+    const int64_t tiles = tm * ((N + p.bn - 1) / p.bn);
+    if (2 * tiles <= sms) {
+        int64_t most = K / 512, want = sms / tiles;
+        p.splits = (int)(want < most ? want : most);
+        if (p.splits < 2)
+            p.splits = 1;
+    }
+    if (p.splits > 1)
+        p.part = s.take<float>((size_t)p.splits * M * N);
+    return p;
+}
+
+template <bool A_MN, bool B_MN, int BN, typename OT> int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool is_bf16, int sms, cudaStream_t st)
+{
+    using S = GemmShape<BN>;
+    auto* kernel = gemm_kernel<A_MN, B_MN, BN, OT>;
+    TTC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
+    g.tiles_m = (int)((g.M + BM - 1) / BM);
+    g.tiles_n = (int)((g.N + BN - 1) / BN);
+    g.idesc = instruction(is_bf16, A_MN, B_MN, BN);
+    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+    kernel<<<(unsigned)(tiles < sms ? tiles : sms), kGemmThreads, S::SMEM, st>>>(ma, mb, g);
+    return launched("matrix product");
+}
+
+// D = A B' with A [M][K] (or [K][M] with A_MN) and B likewise, and the epilogue on it.
+template <bool A_MN, bool B_MN> int product(const Product& q, const Operand& a, const Operand& b, bool is_bf16, int out_dtype, const Epilogue& e, int sms, cudaStream_t st)
+{
+    CUtensorMap ma, mb;
+    TTC_TRY(encode(ma, a.ptr, a.rows, a.cols, a.ld, A_MN ? BK : BM, is_bf16));
+    TTC_TRY(encode(mb, b.ptr, b.rows, b.cols, b.ld, B_MN ? BK : q.bn, is_bf16));
+    GemmDev g = {};
+    g.M = q.M;
+    g.N = q.N;
+    g.k_blocks = (int)((q.K + BK - 1) / BK);
+    g.splits = q.splits;
+    g.e = e;
+    if (q.splits > 1) {
+        g.e = Epilogue{};
+        g.e.out = q.part;
+        g.e.ldo = q.N;
+        g.e.split_stride = q.M * q.N;
+        g.e.vec_o = q.N % 4 == 0;
+    }
+    const int type = q.splits > 1 ? (int)TTC_F32 : out_dtype;
+    TTC_TRY(by_type(type, [&](auto t) {
+        using OT = decltype(t);
+        switch (q.bn) {
+        case 256: return launch_tiles<A_MN, B_MN, 256, OT>(ma, mb, g, is_bf16, sms, st);
+        case 128: return launch_tiles<A_MN, B_MN, 128, OT>(ma, mb, g, is_bf16, sms, st);
+        default: return launch_tiles<A_MN, B_MN, 64, OT>(ma, mb, g, is_bf16, sms, st);
+        }
+    }));
+    if (q.splits == 1)
+        return TTC_OK;
+    return by_type(out_dtype, [&](auto t) {
+        using OT = decltype(t);
+        const unsigned blocks = (unsigned)((q.M * q.N + 255) / 256);
+        if (is_bf16)
+            split_sum_kernel<bf16, OT><<<blocks, 256, 0, st>>>(q.part, q.M * q.N, q.splits, q.M, q.N, e);
+        else
+            split_sum_kernel<__half, OT><<<blocks, 256, 0, st>>>(q.part, q.M * q.N, q.splits, q.M, q.N, e);
+        return launched("matrix product, parts of the contraction");
+    });
+}
+
+int check(const ttc_linear_args* a)
+{
+    if (!a)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "arguments are null");
+    TTC_TRY(check_dtype(a->dtype, false));
+    if (a->out_dtype != a->dtype && a->out_dtype != TTC_F32)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "output type %d for operands of type %d", a->out_dtype, a->dtype);
+    if (a->rows < 0 || a->k < 1 || a->m < 1)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "rows = %lld, k = %d, m = %d", (long long)a->rows, a->k, a->m);
+    if (a->rows > kMaxRows || a->k > kMaxRows || a->m > kMaxRows)
+        return fail(TTC_STATUS_UNSUPPORTED, "rows = %lld, k = %d, m = %d", (long long)a->rows, a->k, a->m);
+    if (a->act < TTC_ACT_NONE || a->act > TTC_ACT_SOFTPLUS)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "activation %d", a->act);
+    TTC_TRY(check_floats("x", a->x, a->rows == 0, 2));
+    TTC_TRY(check_floats("w", a->w, false, 2));
+    TTC_TRY(check_floats("bias", a->bias, true));
+    TTC_TRY(check_floats("pre", a->pre, true, 2));
+    if ((a->rows > 1 && a->ldx < a->k) || a->ldw < (a->m > 1 ? a->k : 0) || (a->pre && a->rows > 1 && a->ldp < a->m))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
+    return TTC_OK;
+}
+
+struct LinearPlan {
+    bool few;
+    Aligned x, w;
+    Product q;
+    size_t bytes;
+};
+
+int plan_linear(int device, const ttc_linear_args* a, void* ws, LinearPlan& o)
+{
+    TTC_TRY(check(a));
+    const size_t size = element_size(a->out_dtype);
+    TTC_TRY(check_floats("y", a->y, a->rows == 0, size));
+    TTC_TRY(check_floats("residual", a->residual, true, size));
+    if (a->rows > 1 && (a->ldy < a->m || (a->residual && a->ldr < a->m)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
+    const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
+    Scratch s(ws);
+    o.few = a->rows <= kFewRows;
+    o.x = Aligned{Operand{a->x, a->rows, a->k, ldx}, Operand{a->x, a->rows, a->k, ldx}, false};
+    o.w = Aligned{Operand{a->w, a->m, a->k, ldw}, Operand{a->w, a->m, a->k, ldw}, false};
+    if (!o.few) {
+        o.x = plan_operand(o.x.from, s);
+        o.w = plan_operand(o.w.from, s);
+        o.q = plan_product(a->rows, a->m, a->k, sm_count(device), s);
+    }
+    o.bytes = s.used;
+    return TTC_OK;
+}
+
+struct GradPlan {
+    Aligned x, w, dz;            // dz: dy itself where it can be used as it is
+    SlopeDev slope;
+    int slope_v, row_blocks;
+    bool need_slope;
+    Product qx, qw;
+    size_t bytes;
+};
+
+int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, void* ws, GradPlan& o)
+{
+    TTC_TRY(check(a));
+    if (!g)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "gradients are null");
+    const size_t size = element_size(a->out_dtype);
+    TTC_TRY(check_floats("dy", g->dy, a->rows == 0, size));
+    TTC_TRY(check_floats("dx", g->dx, true, 2));
+    TTC_TRY(check_floats("dw", g->dw, true, 2));
+    TTC_TRY(check_floats("dbias", g->dbias, true));
+    if (a->act != TTC_ACT_NONE && !a->pre && a->rows)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "pre is null: the gradients of an activation need it");
+    if ((a->rows > 1 && (g->lddy < a->m || (g->dx && g->lddx < a->k))) || (g->dw && a->m > 1 && g->lddw < a->k))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
+    const int sms = sm_count(device);
+    const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
+    const int64_t lddy = a->rows > 1 ? g->lddy : (a->m + 7) / 8 * 8;
+    Scratch s(ws);
+    o = GradPlan{};
+    SlopeDev& d = o.slope;
+    d.rows = a->rows;
+    d.m = a->m;
+    d.act = a->act;
+    d.dy = g->dy;
+    d.pre = a->pre;
+    d.lddy = lddy;
+    d.ldp = a->rows > 1 ? a->ldp : 0;
+    const bool products = g->dx || g->dw;
+    o.dz.from = o.dz.to = Operand{g->dy, a->rows, a->m, lddy};
+    const bool as_it_is = a->act == TTC_ACT_NONE && a->out_dtype == a->dtype && aligned(g->dy, lddy, 2);
+    if (products && !as_it_is) {
+        d.lddz = (a->m + 7) / 8 * 8;
+        d.dz = s.take<unsigned short>((size_t)a->rows * d.lddz);
+        o.dz.to = Operand{d.dz, a->rows, a->m, d.lddz};
+    }
+    o.need_slope = (products && !as_it_is) || g->dbias;
+    // eight columns to a thread where everything allows 16-byte accesses
+    const bool wide = a->m % 8 == 0 && aligned(g->dy, lddy, size) && (a->act == TTC_ACT_NONE || aligned(a->pre, d.ldp, 2));
+    o.slope_v = wide ? 8 : 1;
+    const int64_t cols = (a->m + 32 * o.slope_v - 1) / (32 * o.slope_v);
+    int64_t per = 256;
+    while (per > 16 && cols * ((a->rows + per - 1) / per) < 4 * (int64_t)sms)
+        per /= 2;
+    while ((a->rows + per - 1) / per > kMaxGridY)
+        per *= 2;
+    d.rows_per_block = (int)per;
+    o.row_blocks = (int)((a->rows + per - 1) / per);
+    if (g->dbias)
+        d.part = s.take<float>((size_t)o.row_blocks * a->m);
+    if (g->dw)
+        o.x = plan_operand(Operand{a->x, a->rows, a->k, ldx}, s);
+    if (g->dx)
+        o.w = plan_operand(Operand{a->w, a->m, a->k, ldw}, s);
+    // the two products run one behind the other and share the room for parts
+    Scratch s1 = s, s2 = s;
+    if (g->dx)
+        o.qx = plan_product(a->rows, a->k, a->m, sms, s1);
+    if (g->dw)
+        o.qw = plan_product(a->m, a->k, a->rows, sms, s2);
+    o.bytes = s1.used > s2.used ? s1.used : s2.used;
+    return TTC_OK;
+}
+
+} // namespace
+
+extern "C" {
+
+int64_t ttc_linear_workspace(int32_t device, const ttc_linear_args* a)
+{
+    LinearPlan o;
+    TTC_TRY(plan_linear(device, a, nullptr, o));
+    return (int64_t)o.bytes;
+}
+
+int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_t workspace_bytes, void* cuda_stream)
+{
+    LinearPlan o;
+    TTC_TRY(plan_linear(device, a, workspace, o));
+    TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    if (a->rows == 0)
+        return TTC_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const bool is_bf16 = a->dtype == TTC_BF16;
+    const size_t size = element_size(a->out_dtype);
+    Epilogue e = {};
+    e.out = a->y;
+    e.ldo = a->ldy;
+    e.bias = a->bias;
+    e.residual = a->residual;
+    e.ldr = a->ldr;
+    e.pre = a->pre;
+    e.ldp = a->ldp;
+    e.act = a->act;
+    e.pre_bf16 = is_bf16;
+    e.vec_o = aligned(a->y, a->ldy, size);
+    e.vec_r = aligned(a->residual, a->ldr, size);
+    e.vec_p = aligned(a->pre, a->ldp, 2);
+    if (o.few) {
+        FewDev f = {};
+        f.x = a->x;
+        f.w = a->w;
+        f.ldx = o.x.from.ld;
+        f.ldw = o.w.from.ld;
+        f.rows = (int)a->rows;
+        f.k = a->k;
+        f.m = a->m;
+        f.vec = aligned(a->x, f.ldx, 2) && aligned(a->w, f.ldw, 2);
+        f.e = e;
+        return by_type(a->out_dtype, [&](auto t) {
+            using OT = decltype(t);
+            auto go = [&](auto tc, auto nt) {
+                using T = decltype(tc);
+                few_rows_kernel<T, OT, decltype(nt)::value><<<(a->m + 15) / 16, kFewWarps * 32, 0, st>>>(f);
+                return launched("projection of few rows");
+            };
+            auto by_rows = [&](auto tc) {
+                return a->rows <= 8 ? go(tc, std::integral_constant<int, 1>()) : a->rows <= 16 ? go(tc, std::integral_constant<int, 2>())
+                                                                                             : go(tc, std::integral_constant<int, 4>());
+            };
+            return is_bf16 ? by_rows(bf16()) : by_rows(__half());
+        });
+    }
+    TTC_TRY(copy_operand(o.x, st));
+    TTC_TRY(copy_operand(o.w, st));
+    return product<false, false>(o.q, o.x.to, o.w.to, is_bf16, a->out_dtype, e, sm_count(device), st);
+}
+
+int64_t ttc_linear_grad_workspace(int32_t device, const ttc_linear_args* a, const ttc_linear_grads* g)
+{
+    GradPlan o;
+    TTC_TRY(plan_grad(device, a, g, nullptr, o));
+    return (int64_t)o.bytes;
+}
+
+int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_grads* g, void* workspace,
+                    int64_t workspace_bytes, void* cuda_stream)
+{
+    GradPlan o;
+    TTC_TRY(plan_grad(device, a, g, workspace, o));
+    TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const bool is_bf16 = a->dtype == TTC_BF16;
+    const int sms = sm_count(device);
+    if (a->rows == 0) {                                              // sums over no rows
+        if (g->dbias)
+            TTC_CUDA(cudaMemsetAsync(g->dbias, 0, sizeof(float) * a->m, st));
+        if (g->dw) {
+            zero_rows_kernel<<<(unsigned)a->m, 256, 0, st>>>(static_cast<bf16*>(g->dw), g->lddw, a->m, a->k);    // zero has the same bits in both types
+            TTC_TRY(launched("gradients of a projection without rows"));
+        }
+        return TTC_OK;
+    }
+    if (o.need_slope) {
+        TTC_TRY(by_type(a->out_dtype, [&](auto t) {
+            using OT = decltype(t);
+            const dim3 grid((unsigned)((a->m + 32 * o.slope_v - 1) / (32 * o.slope_v)), (unsigned)o.row_blocks);
+            auto go = [&](auto tc) {
+                using T = decltype(tc);
+                if (o.slope_v == 8)
+                    slope_kernel<T, OT, 8><<<grid, 256, 0, st>>>(o.slope);
+                else
+                    slope_kernel<T, OT, 1><<<grid, 256, 0, st>>>(o.slope);
+                return launched("gradients of a projection, activation");
+            };
+            return is_bf16 ? go(bf16()) : go(__half());
+        }));
+        if (g->dbias) {
+            bias_sum_kernel<<<(a->m + 31) / 32, 256, 0, st>>>(o.slope.part, o.row_blocks, a->m, g->dbias);
+            TTC_TRY(launched("gradients of a projection, bias"));
+        }
+    }
+    if (g->dx) {
+        TTC_TRY(copy_operand(o.w, st));
+        Epilogue e = {};
+        e.out = g->dx;
+        e.ldo = a->rows > 1 ? g->lddx : 0;
+        e.vec_o = aligned(g->dx, e.ldo, 2);
+        TTC_TRY((product<false, true>(o.qx, o.dz.to, o.w.to, is_bf16, a->dtype, e, sms, st)));
+    }
+    if (g->dw) {
+        TTC_TRY(copy_operand(o.x, st));
+        Epilogue e = {};
+        e.out = g->dw;
+        e.ldo = g->lddw;
+        e.vec_o = aligned(g->dw, e.ldo, 2);
+        TTC_TRY((product<true, true>(o.qw, o.dz.to, o.x.to, is_bf16, a->dtype, e, sms, st)));
+    }
+    return TTC_OK;
+}
+
+int ttc_block_device_error(int32_t device, int32_t* value)
+{
+    if (!value)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "value is null");
+    DeviceScope scope;
+    TTC_TRY(scope.enter(device));
+    int v = 0;
+    TTC_CUDA(cudaMemcpyFromSymbol(&v, g_error, sizeof(v)));
+    *value = v;
+    return TTC_OK;
+}
+
+} // extern "C"

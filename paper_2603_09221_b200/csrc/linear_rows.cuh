@@ -1,0 +1,231 @@
+// The projections' kernels beside the large matrix products (linear_umma.cuh): few rows, sums of a split contraction, dZ and
+// the bias gradient, copies that give rows the alignment TMA asks for.
+#pragma once
+
+#include "linear_umma.cuh"
+
+namespace ttc {
+namespace lin {
+
+// ---- few rows -----------------------------------------------------------------------------------------------------------
+//
+// Up to 8 NT rows (tokens) against all of W: W is read once, which bounds it.  A block takes 16 rows of W and its eight
+// warps deal out the contraction; each lane loads 16 contiguous bytes of two rows of W and of one row of x, which are the
+// operands of two mma.sync.m16n8k16: the instruction does not mind which contraction index a slot stands for, as long as
+// both operands agree, so nothing is rearranged or staged.
+
+constexpr int kFewWarps = 8, kFewAhead = 4;
+
+struct FewDev {
+    const void *x, *w;
+    long long ldx, ldw;
+    int rows, k, m;
+    int vec;                     // rows of x and W can be read by 16 bytes
+    Epilogue e;
+};
+
+template <typename T> __device__ __forceinline__ uint4 load8(const T* row, bool row_ok, int k, int k_end, bool vec)
+{
+    uint4 r = make_uint4(0, 0, 0, 0);
+    if (!row_ok || k >= k_end)
+        return r;
+    if (vec && k + 8 <= k_end)
+        return *reinterpret_cast<const uint4*>(row + k);
+    const unsigned short* u = reinterpret_cast<const unsigned short*>(row);
+    unsigned short v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = k + i < k_end ? u[k + i] : 0;
+    r.x = v[0] | (unsigned)v[1] << 16, r.y = v[2] | (unsigned)v[3] << 16;
+    r.z = v[4] | (unsigned)v[5] << 16, r.w = v[6] | (unsigned)v[7] << 16;
+    return r;
+}
+
+template <typename T> __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma16816<bf16>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma16816<__half>(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <typename T, typename OT> __device__ __forceinline__ void finish(const Epilogue& e, long long row, long long col, float z)
+{
+    if (e.bias)
+        z += e.bias[col];
+    if (e.pre)
+        static_cast<T*>(e.pre)[row * e.ldp + col] = from_f<T>(z);
+    z = activate<sizeof(OT) == 2>(z, e.act);
+    if (e.residual)
+        z += to_f(static_cast<const OT*>(e.residual)[row * e.ldr + col]);
+    static_cast<OT*>(e.out)[row * e.ldo + col] = from_f<OT>(z);
+}
+
+template <typename T, typename OT, int NT>
+__global__ void __launch_bounds__(kFewWarps * 32) few_rows_kernel(const FewDev p)
+{
+    __shared__ float part[kFewWarps][NT * 8][17];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const int f0 = blockIdx.x * 16;
+    const T *w = static_cast<const T*>(p.w), *x = static_cast<const T*>(p.x);
+    const T *w0 = w + (long long)(f0 + g) * p.ldw, *w1 = w + (long long)(f0 + g + 8) * p.ldw;
+    const bool ok0 = f0 + g < p.m, ok1 = f0 + g + 8 < p.m;
+    float acc[NT][4] = {};
+    for (int k0 = warp * 32; k0 < p.k; k0 += kFewWarps * 32 * kFewAhead) {
+        uint4 a0[kFewAhead], a1[kFewAhead];
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) {
+            const int k = k0 + i * kFewWarps * 32 + t * 8;
+            a0[i] = load8(w0, ok0, k, p.k, p.vec);
+            a1[i] = load8(w1, ok1, k, p.k, p.vec);
+        }
+#pragma unroll
+        for (int i = 0; i < kFewAhead; ++i) {
+            const int k = k0 + i * kFewWarps * 32 + t * 8;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const uint4 b = load8(x + (long long)(n * 8 + g) * p.ldx, n * 8 + g < p.rows, k, p.k, p.vec);
+                mma16816<T>(acc[n], a0[i].x, a1[i].x, a0[i].y, a1[i].y, b.x, b.y);
+                mma16816<T>(acc[n], a0[i].z, a1[i].z, a0[i].w, a1[i].w, b.z, b.w);
+            }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        part[warp][n * 8 + 2 * t][g] = acc[n][0];
+        part[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
+        part[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
+        part[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 8 * 16; i += kFewWarps * 32) {
+        const int row = i / 16, f = i % 16;
+        if (row >= p.rows || f0 + f >= p.m)
+            continue;
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < kFewWarps; ++k)
+            z += part[k][row][f];
+        finish<T, OT>(p.e, row, f0 + f, z);
+    }
+}
+
+// ---- the parts of a split contraction ---------------------------------------------------------------------------------
+
+template <typename T, typename OT>
+__global__ void __launch_bounds__(256) split_sum_kernel(const float* part, long long split_stride, int splits, long long M, long long N, const Epilogue e)
+{
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= M * N)
+        return;
+    float z = 0.f;
+    for (int s = 0; s < splits; ++s)
+        z += part[s * split_stride + i];
+    finish<T, OT>(e, i / N, i % N, z);
+}
+
+// ---- dZ and the sums over the rows --------------------------------------------------------------------------------------
+
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    switch (act) {
+    case TTC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+    case TTC_ACT_SILU: return silu_slope(z);
+    case TTC_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
+    case TTC_ACT_SOFTPLUS: return sigmoid(z);
+    default: return 1.f;
+    }
+}
+
+struct SlopeDev {
+    long long rows;
+    int m, act, rows_per_block;
+    const void *dy, *pre;
+    long long lddy, ldp;
+    void* dz;                    // null: dy is used as it is
+    long long lddz;
+    float* part;                 // [blocks of rows][m] or null
+};
+
+// dZ = dy act'(pre) in 16 bits, and each block's sums over its rows, of the unrounded values.  V columns to a thread.
+template <typename T, typename OT, int V>
+__global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
+{
+    __shared__ float sums[8][32][V + 1];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int c = (blockIdx.x * 32 + lane) * V;
+    const long long r0 = (long long)blockIdx.y * p.rows_per_block, r1 = min(p.rows, r0 + p.rows_per_block);
+    float s[V] = {};
+    if (c < p.m) {
+        for (long long r = r0 + warp; r < r1; r += 8) {
+            const Vec<OT, V> g = *reinterpret_cast<const Vec<OT, V>*>(static_cast<const OT*>(p.dy) + r * p.lddy + c);
+            Vec<T, V> z, o;
+            if (p.act != TTC_ACT_NONE)
+                z = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.pre) + r * p.ldp + c);
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float d = to_f(g.v[i]);
+                if (p.act != TTC_ACT_NONE)
+                    d *= act_slope(to_f(z.v[i]), p.act);
+                s[i] += d;
+                o.v[i] = from_f<T>(d);
+            }
+            if (p.dz)
+                *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dz) + r * p.lddz + c) = o;
+        }
+    }
+    if (!p.part)
+        return;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        sums[warp][lane][i] = s[i];
+    __syncthreads();
+    for (int at = threadIdx.x; at < 32 * V; at += 256) {
+        const int l = at / V, i = at % V, col = (blockIdx.x * 32 + l) * V + i;
+        if (col >= p.m)
+            continue;
+        float v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w)
+            v += sums[w][l][i];
+        p.part[(long long)blockIdx.y * p.m + col] = v;
+    }
+}
+
+static __global__ void __launch_bounds__(256) bias_sum_kernel(const float* part, int blocks, int m, float* out)
+{
+    __shared__ float sum[8][33];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
+    float s = 0.f;
+    if (c < m)
+        for (int b = warp; b < blocks; b += 8)
+            s += part[(long long)b * m + c];
+    sum[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < m) {
+        for (int k = 1; k < 8; ++k)
+            s += sum[k][lane];
+        out[c] = s;
+    }
+}
+
+// Rows copied to a stride that is a multiple of 16 bytes.
+static __global__ void __launch_bounds__(256) align_rows_kernel(const unsigned short* from, long long ld, long long rows, int cols, unsigned short* to, long long ldt)
+{
+    const long long r = blockIdx.x;
+    for (int c = threadIdx.x; c < cols; c += 256)
+        to[r * ldt + c] = from[r * ld + c];
+}
+
+template <typename T> __global__ void __launch_bounds__(256) zero_rows_kernel(T* to, long long ld, long long rows, int cols)
+{
+    for (int c = threadIdx.x; c < cols; c += 256)
+        to[(long long)blockIdx.x * ld + c] = from_f<T>(0.f);
+}
+
+} // namespace lin
+} // namespace ttc

@@ -1,0 +1,384 @@
+// Matrix products of the projections on the 5th-generation tensor cores: D[i][j] = sum_k A(i, k) B(j, k), with what is to
+// be done to a product before it is written (bias, activation, residual) done on the accumulators.
+//
+// One CTA per SM works through tiles of 128 x BN.  One thread keeps a ring of stages of 64 contraction indices filled by TMA
+// (128-byte swizzle), one issues tcgen05.mma (cta_group::1, kind::f16) into one of two accumulators in tensor memory, and
+// eight warps read the other one back, so that the end of a tile runs beside the products of the next.  Operands are read as
+// they lie in memory: an operand whose contraction index is not the contiguous one (the gradients') is staged in boxes of
+// 64 contiguous rows by 64 contraction indices and described to the instruction as MN-major; nothing is transposed.
+// Rows, columns and contraction indices past the end are filled with zeros by TMA.
+#pragma once
+
+#include <cuda.h>
+
+#include "block_common.cuh"
+
+namespace ttc {
+namespace lin {
+
+using namespace blk;
+
+constexpr int BM = 128, BK = 64;
+constexpr int kEpilogueWarps = 8;
+constexpr int kGemmThreads = 32 * (2 + kEpilogueWarps);
+constexpr int kSpinLimit = 1 << 22;
+constexpr int kStageRow = 80;                    // bytes of a staged row of 64, padded against bank conflicts
+
+static __device__ int g_error;                   // set where a wait gave up
+
+struct Epilogue {
+    void* out;                   // [M][N], or [splits][M][N] floats of a split contraction
+    long long ldo, split_stride;
+    const float* bias;           // [N] or null
+    const void* residual;        // type of out, or null
+    long long ldr;
+    void* pre;                   // z in 16 bits, or null
+    long long ldp;
+    int act, pre_bf16;
+    int vec_o, vec_r, vec_p;     // rows can be accessed by 16 bytes
+};
+
+struct GemmDev {
+    long long M, N;
+    int k_blocks;                // blocks of BK contraction indices in all
+    int splits;                  // parts of the contraction, each a tile of its own
+    int tiles_m, tiles_n;
+    uint32_t idesc;
+    Epilogue e;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ bool try_wait(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// Gives up after kSpinLimit polls, or once another thread of the CTA has; then the CTA stops.
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int* dead)
+{
+    for (int i = 0; i < kSpinLimit; ++i) {
+        if (try_wait(bar, parity))
+            return true;
+        if ((i & 63) == 63 && *dead)
+            return false;
+    }
+    *dead = 1;
+    g_error = 1;
+    return false;
+}
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity)
+{
+    for (int i = 0; i < kSpinLimit && !try_wait(bar, parity); ++i) {
+    }
+}
+__device__ __forceinline__ void expect_bytes(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory"); }
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32])
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+                   "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+                   "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        v[i] = __uint_as_float(r[i]);
+}
+
+// Shared-memory descriptors (128-byte swizzle).  K-major: rows of 64 contraction indices, 128 bytes each, groups of eight
+// rows 1024 bytes apart; a step of 16 indices is 32 bytes further in.  MN-major: rows of 64 indices of the other dimension, one
+// for each contraction index, groups of eight 1024 bytes apart; the next 64 are a box (8192 bytes) further; a step of 16
+// contraction indices is 2048 bytes.
+template <bool MN> __device__ __forceinline__ uint64_t operand_desc(uint32_t at)
+{
+    const uint64_t lead = MN ? (8192 >> 4) : 1;
+    return (uint64_t)((at >> 4) & 0x3fffu) | lead << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+
+// Instruction descriptor: float32 accumulators, both operands bfloat16 or both float16.
+inline uint32_t instruction(bool is_bf16, bool a_mn, bool b_mn, int bn)
+{
+    const uint32_t f = is_bf16 ? 1 : 0;
+    return 1u << 4 | f << 7 | f << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(BM >> 4) << 24;
+}
+
+// Activations.  FAST for results that are rounded to 16 bits: errors of a few 2^-22 beside 2^-9 or 2^-12.
+template <bool FAST> __device__ __forceinline__ float activate(float z, int act)
+{
+    switch (act) {
+    case TTC_ACT_RELU: return z < 0.f ? 0.f : z;                                   // NaN stays NaN
+    case TTC_ACT_SILU: return FAST ? __fdividef(z, 1.f + __expf(-z)) : silu(z);
+    case TTC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case TTC_ACT_SOFTPLUS: return softplus(z);
+    default: return z;
+    }
+}
+
+template <typename OT> __device__ __forceinline__ void load_chunk(const OT* at, bool row_ok, long long cols, bool vec, float (&v)[32])
+{
+    constexpr int V = 16 / sizeof(OT);
+    if (!row_ok) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            v[i] = 0.f;
+    } else if (vec && cols >= 32) {
+#pragma unroll
+        for (int i = 0; i < 32; i += V) {
+            const Vec<OT, V> u = *reinterpret_cast<const Vec<OT, V>*>(at + i);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[i + j] = to_f(u.v[j]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            v[i] = i < cols ? to_f(at[i]) : 0.f;
+    }
+}
+
+// Writes 32 rows x 32 columns, a row in each lane, through the warp's staging rows: rows of 64 bytes leave in 16-byte pieces.
+template <typename OT>
+__device__ __forceinline__ void store_chunk(const float (&v)[32], OT* at, long long ld, long long rows, long long cols, bool vec, char* stage, int lane)
+{
+    constexpr int V = 16 / sizeof(OT), C = 64 / sizeof(OT);          // columns of a 64-byte row
+#pragma unroll
+    for (int c0 = 0; c0 < 32; c0 += C) {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < C; i += V) {
+            Vec<OT, V> u;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                u.v[j] = from_f<OT>(v[c0 + i + j]);
+            *reinterpret_cast<Vec<OT, V>*>(stage + lane * kStageRow + i * sizeof(OT)) = u;
+        }
+        __syncwarp();
+        if (vec && cols >= c0 + C) {
+#pragma unroll
+            for (int r0 = 0; r0 < 32; r0 += 8) {
+                const int r = r0 + lane / 4, part = lane % 4;
+                if (r < rows)
+                    *reinterpret_cast<uint4*>(at + r * ld + c0 + part * V) = *reinterpret_cast<const uint4*>(stage + r * kStageRow + part * 16);
+            }
+        } else {
+            for (int e = lane; e < 32 * C; e += 32) {
+                const int r = e / C, c = e % C;
+                if (r < rows && c0 + c < cols)
+                    at[r * ld + c0 + c] = *reinterpret_cast<const OT*>(stage + r * kStageRow + c * sizeof(OT));
+            }
+        }
+    }
+}
+
+template <int BN> struct GemmShape {
+    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : 8;
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int EPI_BYTES = kEpilogueWarps * (32 * kStageRow + 128 * 4);
+    static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + 256;
+};
+
+template <bool A_MN, bool B_MN, int BN, typename OT>
+__global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                              const GemmDev p)
+{
+    using S = GemmShape<BN>;
+    constexpr int STAGES = S::STAGES;
+    extern __shared__ char smem_raw[];
+    char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) / 1024 * 1024);
+    char* s_epi = smem + STAGES * S::STAGE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(s_epi + S::EPI_BYTES);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_full = empty + 8 * STAGES, acc_empty = acc_full + 16,
+                   drained = acc_empty + 16;
+    uint32_t* s_tmem = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+    volatile int* dead = reinterpret_cast<volatile int*>(s_tmem + 1);
+
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2 * STAGES; ++i)
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(full + 8 * i) : "memory");
+        for (int i = 0; i < 2; ++i) {
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(acc_full + 8 * i) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(acc_empty + 8 * i), "r"(kEpilogueWarps) : "memory");
+        }
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drained) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        *dead = 0;
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(s_tmem)), "r"(2 * BN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *s_tmem;
+
+    const int per_split = p.tiles_m * p.tiles_n, tiles = per_split * p.splits;
+    // Tiles of eight rows of tiles follow one another column by column, so that the CTAs at work share operands in L2.
+    auto place = [&](int tile, int& mt, int& nt, int& k0, int& k1) {
+        const int split = tile / per_split, at = tile % per_split;
+        const int band = at / (8 * p.tiles_n), height = min(8, p.tiles_m - band * 8), in = at - band * 8 * p.tiles_n;
+        mt = band * 8 + in % height;
+        nt = in / height;
+        k0 = static_cast<int>((long long)p.k_blocks * split / p.splits);
+        k1 = static_cast<int>((long long)p.k_blocks * (split + 1) / p.splits);
+        return split;
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            unsigned it = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+                int mt, nt, k0, k1;
+                place(tile, mt, nt, k0, k1);
+                for (int k = k0; k < k1; ++k, ++it) {
+                    const int s = it % STAGES;
+                    if (!(ok = wait(empty + 8 * s, (it / STAGES & 1) ^ 1, dead)))
+                        break;
+                    const uint32_t bar = full + 8 * s, a = smem_u32(smem + s * S::STAGE_BYTES), b = a + S::A_BYTES;
+                    expect_bytes(bar, S::STAGE_BYTES);
+                    if (A_MN) {
+#pragma unroll
+                        for (int i = 0; i < BM / 64; ++i)
+                            tma_load(a + i * 8192, &map_a, mt * BM + i * 64, k * BK, bar);
+                    } else {
+                        tma_load(a, &map_a, k * BK, mt * BM, bar);
+                    }
+                    if (B_MN) {
+#pragma unroll
+                        for (int i = 0; i < BN / 64; ++i)
+                            tma_load(b + i * 8192, &map_b, nt * BN + i * 64, k * BK, bar);
+                    } else {
+                        tma_load(b, &map_b, k * BK, nt * BN, bar);
+                    }
+                }
+            }
+            if (!ok)                                                 // copies under way end before the CTA does
+                for (unsigned i = it > STAGES ? it - STAGES : 0; i < it; ++i)
+                    drain(full + 8 * (i % STAGES), i / STAGES & 1);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            unsigned it = 0, done = 0;
+            bool ok = true;
+            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++done) {
+                int mt, nt, k0, k1;
+                place(tile, mt, nt, k0, k1);
+                const uint32_t d = tmem + (done & 1) * BN;
+                if (!(ok = wait(acc_empty + 8 * (done & 1), (done / 2 & 1) ^ 1, dead)))
+                    break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (int k = k0; k < k1; ++k, ++it) {
+                    const int s = it % STAGES;
+                    if (!(ok = wait(full + 8 * s, it / STAGES & 1, dead)))
+                        break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a = smem_u32(smem + s * S::STAGE_BYTES), b = a + S::A_BYTES;
+#pragma unroll
+                    for (int j = 0; j < BK / 16; ++j)
+                        mma(d, operand_desc<A_MN>(a + j * (A_MN ? 2048 : 32)), operand_desc<B_MN>(b + j * (B_MN ? 2048 : 32)), p.idesc,
+                            k > k0 || j > 0);
+                    commit(empty + 8 * s);
+                }
+                if (ok)
+                    commit(acc_full + 8 * (done & 1));
+            }
+            if (!ok) {                                               // products under way end before tensor memory is given back
+                commit(drained);
+                drain(drained, 0);
+            }
+        }
+    } else {
+        const int w = warp - 2, quarter = warp % 4, half = w / 4;    // a warp reads the lanes of its quarter of tensor memory
+        char* stage = s_epi + w * (32 * kStageRow + 128 * 4);
+        float* s_bias = reinterpret_cast<float*>(stage + 32 * kStageRow);
+        constexpr bool FAST = sizeof(OT) == 2;
+        unsigned done = 0;
+        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++done) {
+            int mt, nt, k0, k1;
+            const int split = place(tile, mt, nt, k0, k1);
+            const long long row0 = (long long)mt * BM + quarter * 32, col0 = (long long)nt * BN + half * (BN / 2);
+            __syncwarp();
+            for (int c = lane; c < BN / 2; c += 32)
+                s_bias[c] = p.e.bias && col0 + c < p.N ? p.e.bias[col0 + c] : 0.f;
+            __syncwarp();
+            if (!wait(acc_full + 8 * (done & 1), done / 2 & 1, dead))
+                break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t from = tmem + (done & 1) * BN + half * (BN / 2) + ((uint32_t)(quarter * 32) << 16);
+            OT* out = static_cast<OT*>(p.e.out) + split * p.e.split_stride;
+#pragma unroll 1
+            for (int c = 0; c < BN / 2; c += 32) {
+                float v[32];
+                tmem_ld32(from + c, v);
+                if (c + 32 == BN / 2) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0)
+                        arrive(acc_empty + 8 * (done & 1));
+                }
+                const long long rows = p.M - row0, cols = p.N - (col0 + c);
+                if (rows <= 0 || cols <= 0)
+                    continue;
+                if (p.e.bias) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] += s_bias[c + i];
+                }
+                if (p.e.pre) {
+                    if (p.e.pre_bf16)
+                        store_chunk(v, static_cast<bf16*>(p.e.pre) + row0 * p.e.ldp + col0 + c, p.e.ldp, rows, cols, p.e.vec_p, stage, lane);
+                    else
+                        store_chunk(v, static_cast<__half*>(p.e.pre) + row0 * p.e.ldp + col0 + c, p.e.ldp, rows, cols, p.e.vec_p, stage, lane);
+                }
+                if (p.e.act != TTC_ACT_NONE) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] = activate<FAST>(v[i], p.e.act);
+                }
+                if (p.e.residual) {
+                    float r[32];
+                    load_chunk(static_cast<const OT*>(p.e.residual) + (row0 + lane) * p.e.ldr + col0 + c, lane < rows, cols, p.e.vec_r, r);
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] += r[i];
+                }
+                store_chunk(v, out + row0 * p.e.ldo + col0 + c, p.e.ldo, rows, cols, p.e.vec_o, stage, lane);
+            }
+        }
+    }
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    __syncwarp();
+    if (warp == 1)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * BN) : "memory");
+}
+
+} // namespace lin
+} // namespace ttc

@@ -24,13 +24,16 @@
 #include "scan_pair.cuh"
 #include "scan_frag.cuh"
 #include "peak_probe.cuh"
+#include "status.h"
 
 using namespace ttc;
 using mem::DevBuf;
 
 namespace {
-
 thread_local char g_err[512] = "";
+}
+
+namespace ttc {
 
 int fail(int status, const char* fmt, ...)
 {
@@ -41,12 +44,9 @@ int fail(int status, const char* fmt, ...)
     return status;
 }
 
-#define TTC_CUDA(call)                                                                   \
-    do {                                                                                 \
-        cudaError_t e_ = (call);                                                         \
-        if (e_ != cudaSuccess)                                                           \
-            return fail(TTC_STATUS_CUDA_ERROR, "%s: %s", #call, cudaGetErrorString(e_)); \
-    } while (0)
+} // namespace ttc
+
+namespace {
 
 constexpr int kMaxSlices = 32;   // token slices of the pipelined host-buffer entry point
 

@@ -1,0 +1,171 @@
+"""What the operators of include/ttc_block.h refuse, checked before any device is touched (no GPU needed)."""
+import pytest
+import torch
+
+from paper_2603_09221_b200 import block, lqr
+
+P = 1 << 20                 # an address that is never read: every call here is refused or only sized
+
+
+def _conv(**kw):
+    a = dict(batch=2, tokens=8, offsets=0, d=16, taps=4, act=2, dtype=1, x=P, xb=128, xt=16, y=2 * P, yb=128, yt=16, w=P, bias=P, state=0, state_out=0)
+    a.update(kw)
+    return block._CONV_ARGS.pack(*a.values())
+
+
+def _scan(**kw):
+    a = dict(batch=2, tokens=8, offsets=0, d=16, n=16, groups=1, dtype=1, softplus=1, reserved=0)
+    for k in ("x", "delta"):
+        a.update({k: P, k + "b": 128, k + "t": 16})
+    for k in ("B", "C"):
+        a.update({k: P, k + "b": 128, k + "t": 16})
+    a.update(z=0, zb=0, zt=0, y=2 * P, yb=128, yt=16, A=P, D=0, delta_bias=0, state=0, state_out=0)
+    a.update(kw)
+    return block._SCAN_ARGS.pack(*a.values())
+
+
+def _linear(**kw):
+    a = dict(rows=64, k=32, m=48, dtype=1, out_dtype=1, act=0, reserved=0, x=P, w=P, bias=0, residual=0, y=2 * P, pre=0,
+             ldx=32, ldw=32, ldr=48, ldy=48, ldp=48)
+    a.update(kw)
+    return block._LINEAR_ARGS.pack(*a.values())
+
+
+def _status(f, *args):
+    status = f(*args)
+    return status, lqr.load_library().ttc_lqr_last_error().decode()
+
+
+INVALID, UNSUPPORTED = -1, -4
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(batch=-1), INVALID), (dict(tokens=-1), INVALID), (dict(d=0), INVALID), (dict(taps=1), UNSUPPORTED), (dict(taps=5), UNSUPPORTED),
+    (dict(act=3), UNSUPPORTED), (dict(act=9), UNSUPPORTED), (dict(dtype=7), INVALID), (dict(x=0), INVALID), (dict(y=0), INVALID), (dict(w=0), INVALID),
+    (dict(x=P + 1), INVALID), (dict(w=P + 2), INVALID), (dict(xt=-16), INVALID), (dict(y=P), INVALID), (dict(y=P + 8), INVALID),
+    (dict(tokens=1 << 31), UNSUPPORTED), (dict(batch=1 << 20, tokens=1 << 20), UNSUPPORTED), (dict(offsets=P + 2), INVALID)])
+def test_convolution(kw, status):
+    lib = block._load()
+    assert _status(lib.ttc_causal_conv, 0, _conv(**kw), None)[0] == status
+
+
+def test_convolution_step_and_gradients():
+    lib = block._load()
+    assert _status(lib.ttc_causal_conv_step, 0, _conv(), None)[0] == INVALID                     # no window
+    grads = lambda **kw: block._CONV_GRADS.pack(*{**dict(dy=3 * P, dyb=128, dyt=16, dx=4 * P, dxb=128, dxt=16, dstate_out=0, dw=P, dbias=P, dstate=0), **kw}.values())  # noqa: E731
+    assert lib.ttc_causal_conv_grad_workspace(0, _conv(), grads()) > 0
+    for kw in (dict(dy=0), dict(dx=3 * P), dict(dx=P), dict(dw=P + 1), dict(dstate=P, dstate_out=P)):
+        assert _status(lib.ttc_causal_conv_grad_workspace, 0, _conv(), grads(**kw))[0] == INVALID, kw
+    status, text = _status(lib.ttc_causal_conv_grad, 0, _conv(), grads(), None, 0, None)
+    assert status == INVALID and "workspace" in text
+    status, text = _status(lib.ttc_causal_conv_grad, 0, _conv(), grads(), P + 8, 1 << 30, None)
+    assert status == INVALID and "256" in text
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(n=0), INVALID), (dict(n=129), UNSUPPORTED), (dict(groups=3), INVALID), (dict(groups=0), INVALID), (dict(d=0), INVALID), (dict(batch=-2), INVALID),
+    (dict(dtype=3), INVALID), (dict(x=0), INVALID), (dict(delta=0), INVALID), (dict(B=0), INVALID), (dict(C=0), INVALID), (dict(A=0), INVALID),
+    (dict(D=P + 1), INVALID), (dict(y=0), INVALID), (dict(y=P), INVALID), (dict(tokens=1 << 31), UNSUPPORTED), (dict(d=1 << 20), UNSUPPORTED)])
+def test_scan(kw, status):
+    lib = block._load()
+    assert _status(lib.ttc_selective_scan, 0, _scan(**kw), None, 0, None)[0] == status
+
+
+def test_scan_step_and_gradients():
+    lib = block._load()
+    assert _status(lib.ttc_selective_scan_step, 0, _scan(), None)[0] == INVALID                  # no state
+
+    def grads(**kw):
+        a = dict(dy=3 * P, dyb=128, dyt=16)
+        for i, k in enumerate(("dx", "ddelta", "dB", "dC")):
+            a.update({k: (4 + i) * P, k + "b": 128, k + "t": 16})
+        a.update(dz=0, dzb=0, dzt=0, dstate_out=0, dA=P, dD=P, ddelta_bias=P, dstate=0)
+        a.update(kw)
+        return block._SCAN_GRADS.pack(*a.values())
+
+    need = lib.ttc_selective_scan_grad_workspace(0, _scan(), grads())
+    assert need > 0
+    for kw in (dict(dy=0), dict(dx=3 * P), dict(dB=P), dict(dz=9 * P, dzt=16), dict(dA=P + 2)):
+        assert _status(lib.ttc_selective_scan_grad_workspace, 0, _scan(), grads(**kw))[0] == INVALID, kw
+    assert _status(lib.ttc_selective_scan_grad, 0, _scan(), grads(), P, need - 1, None)[0] == INVALID
+
+
+def test_scan_of_few_channels_needs_a_workspace():
+    lib = block._load()
+    long = _scan(batch=1, tokens=4096)
+    assert lib.ttc_selective_scan_workspace(0, long) > 0
+    status, text = _status(lib.ttc_selective_scan, 0, long, None, 0, None)
+    assert status == INVALID and "workspace" in text
+
+
+@pytest.mark.parametrize("kw, status", [
+    (dict(rows=-1), INVALID), (dict(k=0), INVALID), (dict(m=0), INVALID), (dict(dtype=0), INVALID), (dict(out_dtype=2), INVALID), (dict(act=5), INVALID),
+    (dict(act=-1), INVALID), (dict(x=0), INVALID), (dict(w=0), INVALID), (dict(y=0), INVALID), (dict(x=P + 1), INVALID), (dict(bias=P + 2), INVALID),
+    (dict(ldx=31), INVALID), (dict(ldw=31), INVALID), (dict(ldy=47), INVALID), (dict(residual=P, ldr=47), INVALID), (dict(rows=1 << 32), UNSUPPORTED)])
+def test_linear(kw, status):
+    lib = block._load()
+    assert _status(lib.ttc_linear, 0, _linear(**kw), None, 0, None)[0] == status
+
+
+def test_linear_gradients():
+    lib = block._load()
+    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=P, dx=P, dw=P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
+    assert lib.ttc_linear_grad_workspace(0, _linear(), grads()) >= 0
+    for kw in (dict(dy=0), dict(lddy=47), dict(lddx=31), dict(lddw=31), dict(dbias=P + 1)):
+        assert _status(lib.ttc_linear_grad_workspace, 0, _linear(), grads(**kw))[0] == INVALID, kw
+    assert _status(lib.ttc_linear_grad_workspace, 0, _linear(act=2), grads())[0] == INVALID       # no pre
+
+
+def test_null_records():
+    lib = block._load()
+    for name in ("ttc_causal_conv", "ttc_causal_conv_step", "ttc_selective_scan_step"):
+        assert getattr(lib, name)(0, None, None) == INVALID
+    for name in ("ttc_selective_scan", "ttc_linear"):
+        assert getattr(lib, name)(0, None, None, 0, None) == INVALID
+        assert getattr(lib, name + "_workspace")(0, None) == INVALID
+
+
+def test_binding_refuses_what_does_not_fit():
+    x, w, b = torch.zeros(2, 5, 8, dtype=torch.bfloat16), torch.zeros(8, 4), torch.zeros(8)
+    for bad, error in ((dict(w=torch.zeros(7, 4)), ValueError), (dict(bias=torch.zeros(8, dtype=torch.bfloat16)), ValueError),
+                       (dict(act="tanh"), ValueError), (dict(x=x[0]), ValueError), (dict(x=x.double()), TypeError),
+                       (dict(x=x.transpose(1, 2)), ValueError), (dict(state=torch.zeros(2, 4, 8, dtype=torch.bfloat16)), ValueError),
+                       (dict(offsets=torch.zeros(3, dtype=torch.int32)), ValueError)):
+        args = {**dict(x=x, w=w, bias=b, y=torch.empty_like(bad.get("x", x))), **bad}
+        with pytest.raises(error):
+            block.causal_conv(**args)
+    r = torch.zeros(2, 5, 8)
+    s = dict(x=r, delta=r, A=torch.zeros(8, 4), B=torch.zeros(2, 5, 4), C=torch.zeros(2, 5, 4), y=torch.empty_like(r))
+    for bad in (dict(A=torch.zeros(8, 5)), dict(C=torch.zeros(2, 5, 2, 4)), dict(delta=r.bfloat16()), dict(B=torch.zeros(2, 4, 4)),
+                dict(state=torch.zeros(2, 8, 5)), dict(D=torch.zeros(9)), dict(z=r[..., :4])):
+        with pytest.raises(ValueError):
+            block.selective_scan(**{**s, **bad})
+    with pytest.raises(ValueError):                                  # nothing runs on the CPU
+        block.selective_scan(**s)
+    with pytest.raises(ValueError):
+        block.linear(torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(3, 8, dtype=torch.bfloat16))
+
+
+def test_records_are_laid_out_as_the_header_says(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "sizes.c"
+    src.write_text("""#include <stddef.h>
+#include <stdio.h>
+#include "ttc_block.h"
+#define END(t, last) (offsetof(t, last) + sizeof(((t*)0)->last))
+int main(void) { printf("%zu %zu %zu %zu %zu %zu", END(ttc_conv_args, state_out), END(ttc_conv_grads, dstate), END(ttc_scan_args, state_out),
+    END(ttc_scan_grads, dstate), END(ttc_linear_args, ldp), END(ttc_linear_grads, lddw)); return 0; }
+""")
+    subprocess.run(["gcc", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "sizes"), str(src)], check=True)
+    sizes = [int(v) for v in subprocess.run([str(tmp_path / "sizes")], check=True, capture_output=True, text=True).stdout.split()]
+    assert sizes == [s.size for s in (block._CONV_ARGS, block._CONV_GRADS, block._SCAN_ARGS, block._SCAN_GRADS, block._LINEAR_ARGS, block._LINEAR_GRADS)]
+
+
+def test_every_declared_operator_is_bound():
+    import os
+    import re
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(root, "include", "ttc_block.h")).read(), flags=re.S)
+    assert set(block.EXPORTS) == set(re.findall(r"\b(ttc_\w+)\s*\(", text))
