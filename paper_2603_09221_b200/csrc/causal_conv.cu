@@ -29,15 +29,15 @@ int check(const ttc_conv_args* a, bool step)
     return check_floats("state_out", a->state_out, true, element_size(a->dtype));
 }
 
-// Channels that a thread takes at once: 16 bytes, 4 or an element, by the alignment of every pointer and stride.
+// Channels that a thread takes at once: `most` bytes, 4, or one element, by the alignment of every pointer and stride.
 struct Width {
     size_t size;
     int d, v;
-    Width(int dtype, int d_) : size(element_size(dtype)), d(d_), v(16 / (int)element_size(dtype)) {}
+    Width(int dtype, int d_, int most) : size(element_size(dtype)), d(d_), v(most / (int)element_size(dtype)) { fit(nullptr, d, 0); }
     void fit(const void* p, int64_t s0, int64_t s1)
     {
         while (v > 1 && (reinterpret_cast<uintptr_t>(p) % (v * size) || s0 % v || s1 % v))
-            v = v * (int)size > 4 ? (int)(4 / size) : 1;
+            v /= 2;
     }
     void rows(const ttc_rows& r, bool packed, bool step)
     {
@@ -47,7 +47,7 @@ struct Width {
     void window(const void* p)
     {
         if (p)
-            fit(p, d, d);
+            fit(p, 0, 0);
     }
 };
 
@@ -62,6 +62,7 @@ ConvDev to_dev(const ttc_conv_args* a, bool step)
     p.y = dev_rows(a->y, off);
     p.w = a->w;
     p.bias = a->bias;
+    p.vec_w = reinterpret_cast<uintptr_t>(a->w) % 16 == 0;
     p.state = a->state;
     p.state_out = a->state_out;
     return p;
@@ -85,7 +86,7 @@ template <typename F> int by_shape(int dtype, int v, int taps, F&& f)
 {
     return by_type(dtype, [&](auto t) {
         using T = decltype(t);
-        constexpr int most = 16 / (int)sizeof(T), two = 4 / (int)sizeof(T);
+        constexpr int most = 8 / (int)sizeof(T), two = 4 / (int)sizeof(T);
         auto with_v = [&](auto vc) {
             constexpr int V = decltype(vc)::value;
             switch (taps) {
@@ -135,17 +136,13 @@ int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void*
     p.dstate = g->dstate;
     p.dw = g->dw;
     p.dbias = g->dbias;
-    Width w(a->dtype, a->d);
+    Width w(a->dtype, a->d, 4);
     w.rows(a->x, packed, false);
     w.rows(g->dy, packed, false);
     w.rows(g->dx, packed, false);
     w.window(a->state);
     w.window(g->dstate);
     w.window(g->dstate_out);
-    // the working set of 8 channels, (3 W + 2) * 8 floats, does not fit a thread's registers beside the loads
-    if (w.v > 4 && size == 2)
-        w.v = 2;
-    w.fit(nullptr, a->d, 0);
     o.v = w.v;
     set_tiles(p, o.v, sm_count(device));
     o.params = g->dw || g->dbias;
@@ -171,11 +168,10 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
     TTC_TRY(scope.enter(device));
     if (a->batch == 0)
         return TTC_OK;
-    Width w(a->dtype, a->d);
+    Width w(a->dtype, a->d, 8);
     w.rows(a->x, packed, false);
     w.rows(a->y, packed, false);
     w.window(a->state);
-    w.fit(nullptr, a->d, 0);
     ConvDev p = to_dev(a, false);
     set_tiles(p, w.v, sm_count(device));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -206,15 +202,13 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
     TTC_TRY(scope.enter(device));
     if (a->batch == 0)
         return TTC_OK;
-    Width w(a->dtype, a->d);
+    Width w(a->dtype, a->d, 8);
     w.rows(a->x, false, true);
     w.rows(a->y, false, true);
     w.window(a->state_out);
-    w.fit(nullptr, a->d, 0);
     // few sequences: narrower loads keep more SMs at work
-    const int64_t blocks = a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads));
-    if (blocks < sm_count(device) && w.v * element_size(a->dtype) > 4)
-        w.v = (int)(4 / element_size(a->dtype));
+    while (w.v > 1 && a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads)) < sm_count(device))
+        w.v /= 2;
     const ConvDev p = to_dev(a, true);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return by_shape(a->dtype, w.v, a->taps, [&](auto t, auto vc, auto wc) {

@@ -1,7 +1,7 @@
 // Depthwise causal convolution of token rows, z_t = bias + sum_j w_j x_{t-(W-1)+j}, y_t = act(z_t), its gradients, and the
 // step of a single token.
 //
-// A thread owns V neighbouring channels (16 bytes where rows are aligned for it) and walks over a tile of tokens with the
+// A thread owns V neighbouring channels (8 bytes, backward 4, where rows are aligned for it) and walks over a tile of tokens with the
 // last W inputs in registers, so an input is read once apart from the W - 1 rows in front of a tile.  Memory bounds all
 // three kernels: one read and one write per element forward, two and one backward.
 #pragma once
@@ -19,6 +19,7 @@ struct ConvDev {
     Seqs seqs;
     int d, act;
     int tile;                       // tokens of a tile
+    int vec_w;                      // taps can be read by 16 bytes
     long long tiles;                // tiles of a sequence (equal) or of all rows (packed)
     Rows x, y, dy, dx;
     const float *w, *bias;
@@ -65,13 +66,39 @@ template <typename T, int V, int W> struct Taps {
     float w[W][V], b[V];
     __device__ __forceinline__ void load(const ConvDev& p, int c)
     {
+        float all[V * W];
+        const float* from = p.w + (long long)c * W;
+        if (V * W % 4 == 0 && p.vec_w) {
+#pragma unroll
+            for (int i = 0; i < V * W; i += 4) {
+                const float4 u = *reinterpret_cast<const float4*>(from + i);
+                all[i] = u.x, all[i + 1] = u.y, all[i + 2] = u.z, all[i + 3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V * W; ++i)
+                all[i] = from[i];
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             b[v] = p.bias ? p.bias[c + v] : 0.f;
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                w[j][v] = p.w[(long long)(c + v) * W + j];
+                w[j][v] = all[v * W + j];
         }
+    }
+    // moves the window on by one input and returns z of channel i
+    __device__ __forceinline__ float next(float (&in)[W][V], int i, float x) const
+    {
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j)
+            in[j][i] = in[j + 1][i];
+        in[W - 1][i] = x;
+        float z = b[i];
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            z = fmaf(w[j][i], in[j][i], z);
+        return z;
     }
 };
 
@@ -90,7 +117,7 @@ __device__ __forceinline__ Vec<T, V> input_at(const ConvDev& p, const Segment& s
     return zero;
 }
 
-constexpr int kAhead = 4;           // tokens whose loads are under way together
+constexpr int kAhead = 8;           // tokens whose loads are under way together
 
 template <typename T, int V, int W>
 __global__ void __launch_bounds__(kThreads) conv_kernel(const ConvDev p)
@@ -109,32 +136,29 @@ __global__ void __launch_bounds__(kThreads) conv_kernel(const ConvDev p)
             for (int i = 0; i < V; ++i)
                 in[j][i] = to_f(v.v[i]);
         }
-        for (long long t = s.t0; t < s.t1; t += kAhead) {
+        const T* x = row_ptr<const T>(p.x, s.seq, s.row0 + s.t0) + c;
+        T* y = row_ptr<T>(p.y, s.seq, s.row0 + s.t0) + c;
+        auto give = [&](const Vec<T, V>& v, T* to) {
+            Vec<T, V> out;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const float z = k.next(in, i, to_f(v.v[i]));
+                out.v[i] = from_f<T>(p.act == TTC_ACT_SILU ? silu(z) : z);
+            }
+            *reinterpret_cast<Vec<T, V>*>(to) = out;
+        };
+        int left = static_cast<int>(s.t1 - s.t0);
+        for (; left >= kAhead; left -= kAhead, x += kAhead * p.x.ts, y += kAhead * p.y.ts) {
             Vec<T, V> next[kAhead];
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
-                if (t + a < s.t1)
-                    next[a] = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, s.seq, s.row0 + t + a) + c);
+                next[a] = *reinterpret_cast<const Vec<T, V>*>(x + a * p.x.ts);
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                if (t + a >= s.t1)
-                    break;
-                Vec<T, V> out;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-#pragma unroll
-                    for (int j = 0; j + 1 < W; ++j)
-                        in[j][i] = in[j + 1][i];
-                    in[W - 1][i] = to_f(next[a].v[i]);
-                    float z = k.b[i];
-#pragma unroll
-                    for (int j = 0; j < W; ++j)
-                        z = fmaf(k.w[j][i], in[j][i], z);
-                    out.v[i] = from_f<T>(p.act == TTC_ACT_SILU ? silu(z) : z);
-                }
-                *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.y, s.seq, s.row0 + t + a) + c) = out;
-            }
+            for (int a = 0; a < kAhead; ++a)
+                give(next[a], y + a * p.y.ts);
         }
+        for (; left > 0; --left, x += p.x.ts, y += p.y.ts)
+            give(*reinterpret_cast<const Vec<T, V>*>(x), y);
     });
 }
 
@@ -185,6 +209,8 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvDev p)
         *reinterpret_cast<Vec<T, V>*>(st + (long long)j * p.d) = in[j + 1];
 }
 
+constexpr int kGradAhead = 8;
+
 // Gradients.  With dz_t = dy_t act'(z_t):  dx_s = sum_j w_j dz_{s+W-1-j}, so a walk that has reached token t can give out
 // the gradient of input t - (W - 1); it runs W - 1 tokens past its tile (whose z it computes again) or past the
 // sequence's end (dz = 0), and in front of the sequence the inputs are the window's.
@@ -197,6 +223,18 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(const ConvDev p)
     Taps<T, V, W> k;
     k.load(p, c);
     float dw[W][V] = {}, db[V] = {};
+    auto push = [](float (&dz)[W][V], int i, float g) {
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j)
+            dz[j][i] = dz[j + 1][i];
+        dz[W - 1][i] = g;
+    };
+    auto input_grad = [&](const float (&dz)[W][V], int i, float g) {
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+            g = fmaf(k.w[j][i], dz[W - 1 - j][i], g);
+        return g;
+    };
     for_segments(p, blockIdx.x, [&](const Segment& s) {
         float in[W][V], dz[W][V] = {};                               // the last W inputs and dz, oldest first
 #pragma unroll
@@ -206,66 +244,83 @@ __global__ void __launch_bounds__(kThreads) conv_grad_kernel(const ConvDev p)
             for (int i = 0; i < V; ++i)
                 in[j][i] = to_f(v.v[i]);
         }
-        const long long stop = s.t1 + W - 1;
-        for (long long t = s.t0; t < stop; t += kAhead) {
-            Vec<T, V> nx[kAhead], ny[kAhead];
+        // one token, wherever it lies
+        auto any = [&](long long u) {
+            const bool real = u < s.len, mine = u < s.t1;
+            Vec<T, V> nx, ny, extra, out;
+            if (real) {
+                nx = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, s.seq, s.row0 + u) + c);
+                ny = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.dy, s.seq, s.row0 + u) + c);
+            }
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-                if (t + a < stop && t + a < s.len) {
-                    nx[a] = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, s.seq, s.row0 + t + a) + c);
-                    ny[a] = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.dy, s.seq, s.row0 + t + a) + c);
-                }
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const long long u = t + a;
-                if (u >= stop)
-                    break;
-                const bool real = u < s.len, mine = u < s.t1;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-#pragma unroll
-                    for (int j = 0; j + 1 < W; ++j)
-                        in[j][i] = in[j + 1][i], dz[j][i] = dz[j + 1][i];
-                    in[W - 1][i] = real ? to_f(nx[a].v[i]) : 0.f;
-                    float g = real ? to_f(ny[a].v[i]) : 0.f;
-                    if (p.act == TTC_ACT_SILU && real) {
-                        float z = k.b[i];
-#pragma unroll
-                        for (int j = 0; j < W; ++j)
-                            z = fmaf(k.w[j][i], in[j][i], z);
-                        g *= silu_slope(z);
-                    }
-                    dz[W - 1][i] = g;
-                    if (mine) {
-                        db[i] += g;
-#pragma unroll
-                        for (int j = 0; j < W; ++j)
-                            dw[j][i] = fmaf(g, in[j][i], dw[j][i]);
-                    }
-                }
-                // inputs of this tile, and of the window for the tile that begins the sequence
-                const long long at = u - (W - 1);
-                if (at < s.t0 && !(s.t0 == 0 && p.dstate))
-                    continue;
-                const long long back = at - (s.len - (W - 1));       // place in the last window
-                Vec<T, V> extra, out;
-                const bool more = back >= 0 && p.dstate_out;
-                if (more)
-                    extra = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dstate_out) + (s.seq * (W - 1) + back) * p.d + c);
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    float g = more ? to_f(extra.v[i]) : 0.f;
+            for (int i = 0; i < V; ++i) {
+                const float z = k.next(in, i, real ? to_f(nx.v[i]) : 0.f);
+                float g = real ? to_f(ny.v[i]) : 0.f;
+                if (p.act == TTC_ACT_SILU && real)
+                    g *= silu_slope(z);
+                push(dz, i, g);
+                if (mine) {
+                    db[i] += g;
 #pragma unroll
                     for (int j = 0; j < W; ++j)
-                        g = fmaf(k.w[j][i], dz[W - 1 - j][i], g);
-                    out.v[i] = from_f<T>(g);
+                        dw[j][i] = fmaf(g, in[j][i], dw[j][i]);
                 }
-                if (at < 0)
-                    *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dstate) + (s.seq * (W - 1) + (W - 1) + at) * p.d + c) = out;
-                else if (p.dx.ptr)
-                    *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.dx, s.seq, s.row0 + at) + c) = out;
+            }
+            // inputs of this tile, and of the window for the tile that begins the sequence
+            const long long at = u - (W - 1);
+            if (at < s.t0 && !(s.t0 == 0 && p.dstate))
+                return;
+            const long long back = at - (s.len - (W - 1));           // place in the last window
+            const bool more = back >= 0 && p.dstate_out;
+            if (more)
+                extra = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dstate_out) + (s.seq * (W - 1) + back) * p.d + c);
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                out.v[i] = from_f<T>(input_grad(dz, i, more ? to_f(extra.v[i]) : 0.f));
+            if (at < 0)
+                *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dstate) + (s.seq * (W - 1) + (W - 1) + at) * p.d + c) = out;
+            else if (p.dx.ptr)
+                *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.dx, s.seq, s.row0 + at) + c) = out;
+        };
+        const long long stop = s.t1 + W - 1;
+        long long t = s.t0;
+        for (; t < s.t0 + W - 1; ++t)
+            any(t);
+        // in between, a token and the input W - 1 in front of it are both of this tile, and the last window is further on
+        const T* x = row_ptr<const T>(p.x, s.seq, s.row0 + t) + c;
+        const T* dy = row_ptr<const T>(p.dy, s.seq, s.row0 + t) + c;
+        T* dx = p.dx.ptr ? row_ptr<T>(p.dx, s.seq, s.row0 + t - (W - 1)) + c : nullptr;
+        for (; t + kGradAhead <= s.t1; t += kGradAhead, x += kGradAhead * p.x.ts, dy += kGradAhead * p.dy.ts) {
+            Vec<T, V> nx[kGradAhead], ny[kGradAhead];
+#pragma unroll
+            for (int a = 0; a < kGradAhead; ++a) {
+                nx[a] = *reinterpret_cast<const Vec<T, V>*>(x + a * p.x.ts);
+                ny[a] = *reinterpret_cast<const Vec<T, V>*>(dy + a * p.dy.ts);
+            }
+#pragma unroll
+            for (int a = 0; a < kGradAhead; ++a) {
+                Vec<T, V> out;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float z = k.next(in, i, to_f(nx[a].v[i]));
+                    float g = to_f(ny[a].v[i]);
+                    if (p.act == TTC_ACT_SILU)
+                        g *= silu_slope(z);
+                    push(dz, i, g);
+                    db[i] += g;
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        dw[j][i] = fmaf(g, in[j][i], dw[j][i]);
+                    out.v[i] = from_f<T>(input_grad(dz, i, 0.f));
+                }
+                if (dx) {
+                    *reinterpret_cast<Vec<T, V>*>(dx) = out;
+                    dx += p.dx.ts;
+                }
             }
         }
+        for (; t < stop; ++t)
+            any(t);
     });
     if (p.part) {
         float* to = p.part + (long long)blockIdx.x * (W + 1) * p.d + c;

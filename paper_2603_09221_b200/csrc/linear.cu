@@ -242,7 +242,6 @@ int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, v
     SlopeDev& d = o.slope;
     d.rows = a->rows;
     d.m = a->m;
-    d.act = a->act;
     d.dy = g->dy;
     d.pre = a->pre;
     d.lddy = lddy;
@@ -382,11 +381,21 @@ int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_g
             const dim3 grid((unsigned)((a->m + 32 * o.slope_v - 1) / (32 * o.slope_v)), (unsigned)o.row_blocks);
             auto go = [&](auto tc) {
                 using T = decltype(tc);
-                if (o.slope_v == 8)
-                    slope_kernel<T, OT, 8><<<grid, 256, 0, st>>>(o.slope);
-                else
-                    slope_kernel<T, OT, 1><<<grid, 256, 0, st>>>(o.slope);
-                return launched("gradients of a projection, activation");
+                auto with = [&](auto act) {
+                    constexpr int ACT = decltype(act)::value;
+                    if (o.slope_v == 8)
+                        slope_kernel<T, OT, 8, ACT><<<grid, 256, 0, st>>>(o.slope);
+                    else
+                        slope_kernel<T, OT, 1, ACT><<<grid, 256, 0, st>>>(o.slope);
+                    return launched("gradients of a projection, activation");
+                };
+                switch (a->act) {
+                case TTC_ACT_RELU: return with(std::integral_constant<int, TTC_ACT_RELU>());
+                case TTC_ACT_SILU: return with(std::integral_constant<int, TTC_ACT_SILU>());
+                case TTC_ACT_GELU: return with(std::integral_constant<int, TTC_ACT_GELU>());
+                case TTC_ACT_SOFTPLUS: return with(std::integral_constant<int, TTC_ACT_SOFTPLUS>());
+                default: return with(std::integral_constant<int, TTC_ACT_NONE>());
+                }
             };
             return is_bf16 ? go(bf16()) : go(__half());
         }));

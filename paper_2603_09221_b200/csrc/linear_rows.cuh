@@ -59,7 +59,7 @@ template <typename T, typename OT> __device__ __forceinline__ void finish(const 
         z += e.bias[col];
     if (e.pre)
         static_cast<T*>(e.pre)[row * e.ldp + col] = from_f<T>(z);
-    z = activate<sizeof(OT) == 2>(z, e.act);
+    z = activate(z, e.act);
     if (e.residual)
         z += to_f(static_cast<const OT*>(e.residual)[row * e.ldr + col]);
     static_cast<OT*>(e.out)[row * e.ldo + col] = from_f<OT>(z);
@@ -130,20 +130,23 @@ __global__ void __launch_bounds__(256) split_sum_kernel(const float* part, long 
 
 // ---- dZ and the sums over the rows --------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float act_slope(float z, int act)
+template <int ACT> __device__ __forceinline__ float act_slope(float z)
 {
-    switch (act) {
-    case TTC_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-    case TTC_ACT_SILU: return silu_slope(z);
-    case TTC_ACT_GELU: return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * 0.39894228040143268f * expf(-0.5f * z * z);
-    case TTC_ACT_SOFTPLUS: return sigmoid(z);
-    default: return 1.f;
+    if (ACT == TTC_ACT_RELU)
+        return z > 0.f ? 1.f : 0.f;
+    if (ACT == TTC_ACT_SILU)
+        return silu_slope(z);
+    if (ACT == TTC_ACT_GELU) {
+        float bell;
+        const float cdf = normal_cdf(z, bell);
+        return fmaf(z * 0.39894228040143268f, bell, cdf);
     }
+    return ACT == TTC_ACT_SOFTPLUS ? sigmoid(z) : 1.f;
 }
 
 struct SlopeDev {
     long long rows;
-    int m, act, rows_per_block;
+    int m, rows_per_block;
     const void *dy, *pre;
     long long lddy, ldp;
     void* dz;                    // null: dy is used as it is
@@ -152,7 +155,7 @@ struct SlopeDev {
 };
 
 // dZ = dy act'(pre) in 16 bits, and each block's sums over its rows, of the unrounded values.  V columns to a thread.
-template <typename T, typename OT, int V>
+template <typename T, typename OT, int V, int ACT>
 __global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
 {
     __shared__ float sums[8][32][V + 1];
@@ -164,13 +167,13 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
         for (long long r = r0 + warp; r < r1; r += 8) {
             const Vec<OT, V> g = *reinterpret_cast<const Vec<OT, V>*>(static_cast<const OT*>(p.dy) + r * p.lddy + c);
             Vec<T, V> z, o;
-            if (p.act != TTC_ACT_NONE)
+            if (ACT != TTC_ACT_NONE)
                 z = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.pre) + r * p.ldp + c);
 #pragma unroll
             for (int i = 0; i < V; ++i) {
                 float d = to_f(g.v[i]);
-                if (p.act != TTC_ACT_NONE)
-                    d *= act_slope(to_f(z.v[i]), p.act);
+                if (ACT != TTC_ACT_NONE)
+                    d *= act_slope<ACT>(to_f(z.v[i]));
                 s[i] += d;
                 o.v[i] = from_f<T>(d);
             }

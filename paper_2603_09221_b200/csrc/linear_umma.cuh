@@ -126,15 +126,31 @@ inline uint32_t instruction(bool is_bf16, bool a_mn, bool b_mn, int bn)
     return 1u << 4 | f << 7 | f << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(BM >> 4) << 24;
 }
 
-// Activations.  FAST for results that are rounded to 16 bits: errors of a few 2^-22 beside 2^-9 or 2^-12.
-template <bool FAST> __device__ __forceinline__ float activate(float z, int act)
+// Activations of 32 results; the choice lies outside of the loop.
+template <typename F> __device__ __forceinline__ void each(float (&v)[32], F&& f)
+{
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        v[i] = f(v[i]);
+}
+__device__ __forceinline__ float activate(float z, int act)
 {
     switch (act) {
     case TTC_ACT_RELU: return z < 0.f ? 0.f : z;                                   // NaN stays NaN
-    case TTC_ACT_SILU: return FAST ? __fdividef(z, 1.f + __expf(-z)) : silu(z);
-    case TTC_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    case TTC_ACT_SILU: return silu(z);
+    case TTC_ACT_GELU: return gelu(z);
     case TTC_ACT_SOFTPLUS: return softplus(z);
     default: return z;
+    }
+}
+__device__ __forceinline__ void activate(float (&v)[32], int act)
+{
+    switch (act) {
+    case TTC_ACT_RELU: return each(v, [](float z) { return activate(z, TTC_ACT_RELU); });
+    case TTC_ACT_SILU: return each(v, [](float z) { return activate(z, TTC_ACT_SILU); });
+    case TTC_ACT_GELU: return each(v, [](float z) { return activate(z, TTC_ACT_GELU); });
+    case TTC_ACT_SOFTPLUS: return each(v, [](float z) { return activate(z, TTC_ACT_SOFTPLUS); });
+    default: return;
     }
 }
 
@@ -318,7 +334,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         const int w = warp - 2, quarter = warp % 4, half = w / 4;    // a warp reads the lanes of its quarter of tensor memory
         char* stage = s_epi + w * (32 * kStageRow + 128 * 4);
         float* s_bias = reinterpret_cast<float*>(stage + 32 * kStageRow);
-        constexpr bool FAST = sizeof(OT) == 2;
         unsigned done = 0;
         for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++done) {
             int mt, nt, k0, k1;
@@ -357,11 +372,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                     else
                         store_chunk(v, static_cast<__half*>(p.e.pre) + row0 * p.e.ldp + col0 + c, p.e.ldp, rows, cols, p.e.vec_p, stage, lane);
                 }
-                if (p.e.act != TTC_ACT_NONE) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        v[i] = activate<FAST>(v[i], p.e.act);
-                }
+                activate(v, p.e.act);
                 if (p.e.residual) {
                     float r[32];
                     load_chunk(static_cast<const OT*>(p.e.residual) + (row0 + lane) * p.e.ldr + col0 + c, lane < rows, cols, p.e.vec_r, r);

@@ -1,4 +1,6 @@
 // Host side of ttc_selective_scan, ttc_selective_scan_step and ttc_selective_scan_grad.
+#include <initializer_list>
+
 #include "block_host.h"
 #include "selective_scan_grad.cuh"
 
@@ -50,7 +52,7 @@ int check_output(const ttc_scan_args* a, bool step)
 
 int lanes_of(int n)
 {
-    int lanes = 1;
+    int lanes = 2;
     while (lanes * 4 < n)
         lanes *= 2;
     return lanes;
@@ -59,7 +61,6 @@ int lanes_of(int n)
 template <typename F> int by_lanes(int lanes, F&& f)
 {
     switch (lanes) {
-    case 1: return f(std::integral_constant<int, 1>());
     case 2: return f(std::integral_constant<int, 2>());
     case 4: return f(std::integral_constant<int, 4>());
     case 8: return f(std::integral_constant<int, 8>());
@@ -68,7 +69,7 @@ template <typename F> int by_lanes(int lanes, F&& f)
     }
 }
 
-ScanDev to_dev(const ttc_scan_args* a, bool step)
+ScanDev to_dev(const ttc_scan_args* a, bool step, bool grad = false)
 {
     ScanDev p = {};
     const int32_t* off = step ? nullptr : a->seq_offsets;
@@ -77,7 +78,7 @@ ScanDev to_dev(const ttc_scan_args* a, bool step)
     p.n = a->n;
     p.groups = a->groups;
     p.softplus = a->softplus;
-    const int ch = kThreads / lanes_of(a->n);
+    const int ch = grad ? kGradThreads / lanes_of(a->n) : channels_of(lanes_of(a->n));
     p.chan_blocks = (a->d / a->groups + ch - 1) / ch;
     p.x = dev_rows(a->x, off);
     p.delta = dev_rows(a->delta, off);
@@ -98,23 +99,41 @@ struct Plan {
     ScanDev p;
     int64_t pieces;
     size_t bytes;
+    bool pairs;
 };
 
+// Whether two neighbouring elements of every row can be accessed together: no pair may lie across two groups or past a row.
+bool in_pairs(const ttc_scan_args* a, std::initializer_list<const ttc_rows*> rows)
+{
+    const size_t size = element_size(a->dtype);
+    bool ok = a->d / a->groups % 2 == 0 && a->n % 2 == 0;
+    for (const ttc_rows* r : rows)
+        if (r->ptr)
+            ok = ok && reinterpret_cast<uintptr_t>(r->ptr) % (2 * size) == 0 && r->tstride % 2 == 0 && (a->seq_offsets || r->bstride % 2 == 0);
+    return ok;
+}
+
 // Few sequences and channels leave SMs idle: then the tokens are cut into pieces, whose own shares of the state are found
-// first (a second exponential per state and token) and handed on.
+// first (a second exponential per state and token) and handed on.  Packed sequences are cut at their mean length: a longer
+// one is worked on by several blocks, at no cost to the others, whose only piece has no share to find.
 int plan_forward(int device, const ttc_scan_args* a, void* ws, Plan& o)
 {
     TTC_TRY(check(a, false));
     ScanDev& p = o.p;
     p = to_dev(a, false);
     o.pieces = a->batch;
+    o.pairs = in_pairs(a, {&a->x, &a->delta, &a->B, &a->C, &a->z, &a->y});
     o.bytes = 0;
     const int64_t sms = sm_count(device), columns = (int64_t)p.chan_blocks * a->groups;
     if (columns > kMaxGridY)
         return fail(TTC_STATUS_UNSUPPORTED, "d = %d, n = %d, groups = %d", a->d, a->n, a->groups);
     const int64_t rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
-    if (a->batch * columns < 2 * sms && rows) {
-        const int64_t want = (4 * sms + columns - 1) / columns;
+    int64_t want = 0;                            // pieces in all
+    if (a->batch * columns < sms)
+        want = (2 * sms + columns - 1) / columns;
+    else if (a->seq_offsets)
+        want = a->batch;
+    if (want && rows) {
         int64_t piece = ((rows + want - 1) / want + 63) / 64 * 64;
         piece = piece < 128 ? 128 : piece;
         if (2 * piece <= a->tokens) {
@@ -179,7 +198,7 @@ int plan_grad(int device, const ttc_scan_args* a, const ttc_scan_grads* g, void*
     TTC_TRY(check_floats("dstate", g->dstate, true));
     GradDev& p = o.g;
     p = GradDev{};
-    p.f = to_dev(a, false);
+    p.f = to_dev(a, false, true);
     const int64_t columns = (int64_t)p.f.chan_blocks * a->groups;
     if (columns > kMaxGridY)
         return fail(TTC_STATUS_UNSUPPORTED, "d = %d, n = %d, groups = %d", a->d, a->n, a->groups);
@@ -246,16 +265,20 @@ int ttc_selective_scan(int32_t device, const ttc_scan_args* a, void* workspace, 
         return by_lanes(lanes_of(a->n), [&](auto lc) {
             constexpr int LANES = decltype(lc)::value;
             const dim3 grid((unsigned)o.pieces, (unsigned)(p.chan_blocks * p.groups));
-            if (p.piece) {
-                constexpr size_t smem = Shape<LANES>::smem(true);
-                TTC_TRY(allow_smem(scan_kernel<T, LANES, true>, smem));
-                scan_kernel<T, LANES, true><<<grid, kThreads, smem, st>>>(p);
-                TTC_TRY(launched("selective scan, shares of the pieces"));
-            }
-            constexpr size_t smem = Shape<LANES>::smem(false);
-            TTC_TRY(allow_smem(scan_kernel<T, LANES, false>, smem));
-            scan_kernel<T, LANES, false><<<grid, kThreads, smem, st>>>(p);
-            return launched("selective scan");
+            auto go = [&](auto vc) {
+                constexpr int V = decltype(vc)::value;
+                if (p.piece) {
+                    constexpr size_t smem = Shape<LANES>::smem(true);
+                    TTC_TRY(allow_smem(scan_kernel<T, LANES, true, V>, smem));
+                    scan_kernel<T, LANES, true, V><<<grid, kThreads, smem, st>>>(p);
+                    TTC_TRY(launched("selective scan, shares of the pieces"));
+                }
+                constexpr size_t smem = Shape<LANES>::smem(false);
+                TTC_TRY(allow_smem(scan_kernel<T, LANES, false, V>, smem));
+                scan_kernel<T, LANES, false, V><<<grid, kThreads, smem, st>>>(p);
+                return launched("selective scan");
+            };
+            return o.pairs ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 1>());
         });
     });
 }
@@ -276,8 +299,8 @@ int ttc_selective_scan_step(int32_t device, const ttc_scan_args* a, void* cuda_s
     return by_type(a->dtype, [&](auto t) {
         using T = decltype(t);
         return by_lanes(lanes_of(a->n), [&](auto lc) {
-            constexpr int LANES = decltype(lc)::value, CH = kThreads / LANES;
-            scan_step_kernel<T, LANES><<<dim3((unsigned)a->batch, (a->d + CH - 1) / CH), kThreads, 0, st>>>(p);
+            constexpr int LANES = decltype(lc)::value, CH = kStepThreads / LANES;
+            scan_step_kernel<T, LANES><<<dim3((unsigned)a->batch, (a->d + CH - 1) / CH), kStepThreads, 0, st>>>(p);
             return launched("selective scan, one token");
         });
     });
@@ -311,7 +334,7 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
             const dim3 grid((unsigned)p.runs, (unsigned)(p.f.chan_blocks * p.f.groups));
             if (p.runs) {
                 TTC_TRY(allow_smem(grad_local_kernel<T, LANES>, S::smem_local()));
-                grad_local_kernel<T, LANES><<<grid, kThreads, S::smem_local(), st>>>(p);
+                grad_local_kernel<T, LANES><<<grid, kGradThreads, S::smem_local(), st>>>(p);
                 TTC_TRY(launched("gradients of the selective scan, shares of the pieces"));
             }
             if (a->batch) {
@@ -320,7 +343,7 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
             }
             if (p.runs) {
                 TTC_TRY(allow_smem(grad_piece_kernel<T, LANES>, S::smem_piece()));
-                grad_piece_kernel<T, LANES><<<grid, kThreads, S::smem_piece(), st>>>(p);
+                grad_piece_kernel<T, LANES><<<grid, kGradThreads, S::smem_piece(), st>>>(p);
                 TTC_TRY(launched("gradients of the selective scan"));
             }
             auto sum = [&](const float* part, int64_t stride, int64_t size, float* out) {

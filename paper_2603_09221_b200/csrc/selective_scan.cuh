@@ -1,13 +1,17 @@
 // Selective state space scan: h_t = exp(D_t A) h_{t-1} + D_t x_t B_t, y_t = (C_t . h_t + D x_t) silu(z_t), diagonal A.
 //
-// A channel's n states are spread over LANES neighbouring lanes, four to a lane (two packed pairs), so a block of 128
-// threads owns 128 / LANES channels of one group and walks over the tokens.  Tiles of tokens are staged in shared memory:
-// the step size (after bias and softplus) and D_t x_t of every token and channel, computed once, doubled up as operands of
-// packed arithmetic, and B, C of the group in float32; the next tile's rows are loaded while this one is computed.
+// A channel's n states are spread over LANES neighbouring lanes, four to a lane; a lane holds them for two neighbouring
+// channels, as packed pairs (even channel, odd channel).  A block owns 256 / LANES channels of one group and walks over the tokens in tiles.
+// Four of its warps run the recurrence; eight load the rows, compute the step size (bias, softplus) and D_t x_t of
+// every token and channel once, leave them in shared memory with B and C in float32, and take the lanes' shares of C . h
+// from there to the output rows.  Both work at the same time, on tiles next to one another, with one barrier for each tile.
 // Padding tokens have D_t = 0 (a = 1, nothing added) and padding states A = B = C = 0, so neither needs a test.
-// Per state and token: one exponential and four multiply-adds; the special-function unit (16 exponentials per clock and
-// SM) bounds it, before memory (four elements per channel and token) and issue slots.
+// Per state and token: one exponential, four multiply-adds and six bytes from shared memory.  The special-function unit (16
+// exponentials per clock and SM) bounds it, with shared memory close behind: a 16-byte load occupies the return path for four
+// clocks, broadcast or not, and with one channel to a lane (twelve bytes) that path was the bound.
 #pragma once
+
+#include <type_traits>
 
 #include "block_common.cuh"
 
@@ -16,8 +20,10 @@ namespace sscan {
 
 using namespace blk;
 
-constexpr int kThreads = 128;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStepThreads = 128;
+constexpr int kStateThreads = 128, kRowThreads = 256, kThreads = kStateThreads + kRowThreads;   // of a block: run the recurrence; load and store
+// what a block of the scan holds
+constexpr int channels_of(int lanes) { return 2 * kStateThreads / lanes; }
 
 struct ScanDev {
     Seqs seqs;
@@ -62,209 +68,355 @@ __device__ __forceinline__ bool find_piece(const ScanDev& p, long long i, Piece&
     return true;
 }
 
-template <int LANES> struct Shape {
-    static constexpr int CH = kThreads / LANES;         // channels of a block
-    static constexpr int NP = LANES * 4;                // padded states
-    static constexpr int TB = LANES == 1 ? 16 : LANES <= 8 ? 32 : 16;
-    static constexpr int EPT = (TB * CH + kThreads - 1) / kThreads;
-    static constexpr int BPT = (TB * NP + kThreads - 1) / kThreads;
-    static constexpr size_t smem(bool local) { return sizeof(float) * (TB * CH * 4 + TB * NP * (local ? 1 : 2) + (local ? 0 : TB * CH)); }
+// Rows of a tile in the order in which a block's threads load them: V neighbouring columns to a thread, ROWS rows to a pass.
+template <int WIDTH, int TB, int V> struct Lay {
+    static constexpr int COLS = WIDTH / V, ROWS = kRowThreads / COLS, PASSES = (TB + ROWS - 1) / ROWS;
+    static_assert(WIDTH % V == 0 && kRowThreads % COLS == 0, "");
 };
 
-// LOCAL: what a piece adds to the state that enters it (from zero), and the sum of its step sizes; no output rows.
-template <typename T, int LANES, bool LOCAL>
-__global__ void __launch_bounds__(kThreads) scan_kernel(const ScanDev p)
+template <int LANES> struct Shape {
+    static constexpr int CH = channels_of(LANES);
+    static constexpr int NP = LANES * 4;                // padded states
+    static constexpr int TB = LANES == 2 ? 8 : 16;
+    static constexpr int TOK = TB * CH * 2, BC = TB * NP, Y = TB * CH * LANES;      // floats of a buffer
+    static constexpr size_t smem(bool local) { return 2 * sizeof(float) * (TOK + BC * (local ? 1 : 2) + (local ? 0 : Y)); }
+};
+
+// A row operand as a thread walks over it: its own columns, ROWS rows further at each pass.
+template <typename T, int V, int PASSES> struct Walk {
+    const T* at;
+    long long pass, tile;
+    __device__ __forceinline__ void start(const Rows& r, long long seq, long long row, int col, int rows_per_pass, int tile_rows)
+    {
+        at = row_ptr<const T>(r, seq, row) + col;
+        pass = rows_per_pass * r.ts;
+        tile = tile_rows * r.ts;
+    }
+    // rows from `row` on, ROWS apart, as long as they are below `rows`; the rest reads as zero
+    template <int ROWS> __device__ __forceinline__ void load(Vec<T, V> (&raw)[PASSES], bool mine, int row, int rows)
+    {
+        const T* from = at;
+#pragma unroll
+        for (int e = 0; e < PASSES; ++e, from += pass)
+            raw[e] = load_if(reinterpret_cast<const Vec<T, V>*>(from), mine && row + e * ROWS < rows);
+        at += tile;
+    }
+};
+
+template <int V> __device__ __forceinline__ void put(float* to, const float (&v)[V])
+{
+    if constexpr (V == 2) {
+        *reinterpret_cast<float2*>(to) = make_float2(v[0], v[1]);
+    } else {
+        to[0] = v[0];
+    }
+}
+
+__device__ __forceinline__ void meet() { asm volatile("barrier.sync 0, %0;" :: "n"(kThreads) : "memory"); }
+
+// The recurrence: four states of two channels.
+template <int LANES, bool LOCAL>
+__device__ __forceinline__ void run_states(const ScanDev& p, const Piece& q, int group, int per_group, int c0, const float4* s_tok, const float* s_B,
+                                           const float* s_C, float2* s_y, int tiles)
 {
     using S = Shape<LANES>;
-    constexpr int CH = S::CH, NP = S::NP, TB = S::TB, EPT = S::EPT, BPT = S::BPT;
+    constexpr int CH = S::CH, TB = S::TB;
+    const int tid = threadIdx.x, sub = tid % LANES, pair = tid / LANES, n0 = sub * 4;
+    f2 A2[4], h2[4], total = 0;                                      // pairs of channels
+    {
+        float a[2][4], h[2][4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const bool have = c0 + 2 * pair + c < per_group;
+            const long long my = group * per_group + c0 + 2 * pair + c;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool ok = have && n0 + i < p.n;
+                a[c][i] = ok ? p.A[my * p.n + n0 + i] * kLog2e : 0.f;
+                h[c][i] = !LOCAL && q.t0 == 0 && ok && p.state ? p.state[(q.seq * p.d + my) * p.n + n0 + i] : 0.f;
+            }
+            if (!LOCAL && q.t0 > 0 && have) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n0 + i < p.n)
+                        h[c][i] = p.local[(q.last * p.d + my) * p.n + n0 + i];
+                for (long long k = q.first; k < (long long)blockIdx.x; ++k) {
+                    const float step = p.local_step[k * p.d + my];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (n0 + i < p.n)
+                            h[c][i] = fmaf(ex2(a[c][i] * step), h[c][i], p.local[(k * p.d + my) * p.n + n0 + i]);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            A2[i] = pack2(a[0][i], a[1][i]);
+            h2[i] = pack2(h[0][i], h[1][i]);
+        }
+    }
+    meet();
+    for (int tile = 0; tile < tiles; ++tile) {
+        const ulonglong2* tok = reinterpret_cast<const ulonglong2*>(s_tok) + (tile & 1) * (S::TOK / 4) + pair;
+        const float4* Bs = reinterpret_cast<const float4*>(s_B) + (tile & 1) * (S::BC / 4) + sub;
+        const float4* Cs = reinterpret_cast<const float4*>(s_C) + (tile & 1) * (S::BC / 4) + sub;
+        float2* ys = s_y + (tile & 1) * (S::Y / 2) + tid;
+        // The exponentials of the next token are issued before the products of this one, so that the special-function unit
+        // does not wait for them.
+        f2 next[4];
+        ulonglong2 tok_next;
+        auto decays = [&](int u) {
+            tok_next = tok[u * (CH / 2)];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float e0, e1;
+                unpack2(mul2(A2[i], tok_next.x), e0, e1);
+                next[i] = pack2(ex2(e0), ex2(e1));
+            }
+            if (LOCAL)
+                total = add2(total, tok_next.x);
+        };
+        decays(0);
+#pragma unroll 8
+        for (int u = 0; u < TB; ++u) {
+            f2 a[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[i] = next[i];
+            float in0, in1, y0, y1;
+            unpack2(tok_next.y, in0, in1);
+            if (u + 1 < TB)
+                decays(u + 1);
+            const float4 b4 = Bs[u * LANES];
+            const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                h2[i] = fma2(a[i], h2[i], pack2(in0 * b[i], in1 * b[i]));
+            if (!LOCAL) {
+                const float4 c4 = Cs[u * LANES];
+                const float c[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float h0, h1;
+                    unpack2(h2[i], h0, h1);
+                    y0 = i ? fmaf(h0, c[i], y0) : h0 * c[i];
+                    y1 = i ? fmaf(h1, c[i], y1) : h1 * c[i];
+                }
+                ys[u * (CH / 2 * LANES)] = make_float2(y0, y1);
+            }
+        }
+        meet();
+    }
+    float h[2][4], steps[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        unpack2(h2[i], h[0][i], h[1][i]);
+    unpack2(total, steps[0], steps[1]);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        if (c0 + 2 * pair + c >= per_group)
+            continue;
+        const long long my = group * per_group + c0 + 2 * pair + c;
+        float* to = LOCAL ? p.local + ((long long)blockIdx.x * p.d + my) * p.n : p.state_out && q.t1 == q.len ? p.state_out + (q.seq * p.d + my) * p.n : nullptr;
+        if (to)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n0 + i < p.n)
+                    to[n0 + i] = h[c][i];
+        if (LOCAL && sub == 0)
+            p.local_step[(long long)blockIdx.x * p.d + my] = steps[c];
+    }
+}
+
+// The rows: tile i + 1 is staged and the output of tile i - 1 is written while the recurrence runs over tile i; the loads of
+// tile i + 2 (of z: i) are under way meanwhile.
+template <typename T, int LANES, bool LOCAL, int V>
+__device__ __forceinline__ void run_rows(const ScanDev& p, const Piece& q, int group, int per_group, int c0, float4* s_tok, float* s_B, float* s_C,
+                                         const float2* s_y, int tiles)
+{
+    using S = Shape<LANES>;
+    constexpr int CH = S::CH, NP = S::NP, TB = S::TB;
+    using LT = Lay<CH, TB, V>;                                       // token rows
+    using LB = Lay<NP, TB, V>;                                       // rows of B and C
+    constexpr int PASSES = LT::PASSES;
+    const int tid = threadIdx.x - kStateThreads;
+    // first of the channels, and first row of a tile, that this thread loads and stores; the same for B and C
+    const int lc = tid % LT::COLS * V, lr = tid / LT::COLS;
+    const int chan = group * per_group + c0 + lc;
+    const bool have_l = c0 + lc < per_group && lr < TB;
+    const int bc = tid % LB::COLS * V, br = tid / LB::COLS;
+    const bool have_b = bc < p.n && br < TB;
+    const bool gated = !LOCAL && p.z.ptr;
+    float bias[V], skip[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        bias[v] = p.delta_bias && have_l ? p.delta_bias[chan + v] : 0.f;
+        skip[v] = !LOCAL && p.D && have_l ? p.D[chan + v] : 0.f;
+    }
+    const int len = static_cast<int>(q.t1 - q.t0);
+    const long long row = q.row0 + q.t0;
+    Walk<T, V, PASSES> x, delta, z;
+    Walk<T, V, LB::PASSES> B, C;
+    x.start(p.x, q.seq, row + lr, chan, LT::ROWS, TB);
+    delta.start(p.delta, q.seq, row + lr, chan, LT::ROWS, TB);
+    z.start(p.z, q.seq, row + lr, chan, LT::ROWS, TB);
+    B.start(p.B, q.seq, row + br, group * p.n + bc, LB::ROWS, TB);
+    C.start(p.C, q.seq, row + br, group * p.n + bc, LB::ROWS, TB);
+    T* y = row_ptr<T>(p.y, q.seq, row + lr) + chan;
+    const long long y_pass = LT::ROWS * p.y.ts, y_tile = TB * p.y.ts;
+
+    struct Raw {
+        Vec<T, V> x[PASSES], delta[PASSES], z[PASSES], B[LB::PASSES], C[LB::PASSES];
+    };
+    auto load_rows = [&](Raw& r, int tile) {
+        const int left = len - tile * TB;
+        x.template load<LT::ROWS>(r.x, have_l, lr, left);
+        delta.template load<LT::ROWS>(r.delta, have_l, lr, left);
+        B.template load<LB::ROWS>(r.B, have_b, br, left);
+        if (!LOCAL)
+            C.template load<LB::ROWS>(r.C, have_b, br, left);
+    };
+    auto load_gate = [&](Raw& r, int tile) { z.template load<LT::ROWS>(r.z, have_l && gated, lr, len - tile * TB); };
+    auto tokens = [&](auto full, const Raw& r, int left, float4* to) {
+        constexpr bool FULL = decltype(full)::value;
+#pragma unroll
+        for (int e = 0; e < PASSES; ++e) {
+            const int u = e * LT::ROWS + lr;
+            float steps[V], ins[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                float step = to_f(r.delta[e].v[v]) + bias[v];
+                if (p.softplus)
+                    step = softplus(step);
+                float in = step * to_f(r.x[e].v[v]);
+                if (!FULL && u >= left)                              // padding: nothing decays, nothing is added
+                    step = in = 0.f;
+                steps[v] = step, ins[v] = in;
+            }
+            float4* at = to + u * (CH / 2) + lc / 2;
+            if constexpr (V == 2) {
+                *at = make_float4(steps[0], steps[1], ins[0], ins[1]);
+            } else {
+                reinterpret_cast<float*>(at)[lc % 2] = steps[0];
+                reinterpret_cast<float*>(at)[2 + lc % 2] = ins[0];
+            }
+        }
+    };
+    auto stage = [&](const Raw& r, int tile) {
+        const int left = len - tile * TB;
+        if (LT::ROWS <= TB || lr < TB) {
+            float4* to = s_tok + (tile & 1) * (S::TOK / 4);
+            if (left >= TB)
+                tokens(std::true_type(), r, left, to);
+            else
+                tokens(std::false_type(), r, left, to);
+        }
+        if (LB::ROWS <= TB || br < TB) {
+#pragma unroll
+            for (int e = 0; e < LB::PASSES; ++e) {
+                const int at = (tile & 1) * S::BC + (e * LB::ROWS + br) * NP + bc;
+                float b[V], c[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+                    b[v] = to_f(r.B[e].v[v]), c[v] = LOCAL ? 0.f : to_f(r.C[e].v[v]);
+                put<V>(s_B + at, b);
+                if (!LOCAL)
+                    put<V>(s_C + at, c);
+            }
+        }
+    };
+    Vec<T, V> x0[PASSES], x1[PASSES];                                // x of the tiles whose output is still to be written
+    auto keep = [&](const Raw& r) {
+        if (!LOCAL)
+#pragma unroll
+            for (int e = 0; e < PASSES; ++e)
+                x0[e] = x1[e], x1[e] = r.x[e];
+    };
+    auto give = [&](const Raw& of, int tile) {
+        const int left = len - tile * TB;
+        const float2* shares = s_y + (tile & 1) * (S::Y / 2);
+        const int swap = (lc / 2 ^ lc / 8) & 1;                      // neighbours begin with different banks
+        T* to = y;
+#pragma unroll
+        for (int e = 0; e < PASSES; ++e, to += y_pass) {
+            const int u = e * LT::ROWS + lr;
+            if (have_l && u < left) {
+                Vec<T, V> out;
+                float sum[2];
+                f2 s2 = 0;
+                const ulonglong2* from = reinterpret_cast<const ulonglong2*>(shares + (u * (CH / 2) + lc / 2) * LANES);
+#pragma unroll
+                for (int k = 0; k < LANES / 2; ++k) {
+                    const ulonglong2 two = from[LANES > 2 ? k ^ swap : 0];
+                    s2 = k ? add2(s2, add2(two.x, two.y)) : add2(two.x, two.y);
+                }
+                unpack2(s2, sum[0], sum[1]);
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    float r = fmaf(skip[v], to_f(x0[e].v[v]), V == 2 ? sum[v] : lc % 2 ? sum[1] : sum[0]);
+                    if (gated)
+                        r *= silu(to_f(of.z[e].v[v]));
+                    out.v[v] = from_f<T>(r);
+                }
+                *reinterpret_cast<Vec<T, V>*>(to) = out;
+            }
+        }
+        y += y_tile;
+    };
+    Raw raw;
+    if (tiles) {
+        load_rows(raw, 0);
+        stage(raw, 0);
+        keep(raw);
+        load_rows(raw, 1);
+        load_gate(raw, 0);
+    }
+    meet();
+    for (int tile = 0; tile < tiles; ++tile) {
+        if (!LOCAL && tile > 0)
+            give(raw, tile - 1);
+        if (tile + 1 < tiles)
+            stage(raw, tile + 1);
+        keep(raw);
+        // Issued when nothing is left to wait for: a warp that waits for older loads waits for younger ones with them.
+        load_rows(raw, tile + 2);
+        if (tile > 0)
+            load_gate(raw, tile);
+        meet();
+    }
+    if (!LOCAL && tiles)
+        give(raw, tiles - 1);
+}
+
+// LOCAL: what a piece adds to the state that enters it (from zero), and the sum of its step sizes; no output rows.
+template <typename T, int LANES, bool LOCAL, int V>
+__global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanDev p)
+{
+    using S = Shape<LANES>;
     extern __shared__ float4 smem[];
-    float4* s_tok = smem;                                            // [TB][CH]: D_t, D_t, D_t x_t, D_t x_t
-    float* s_B = reinterpret_cast<float*>(s_tok + TB * CH);          // [TB][NP]
-    float* s_C = s_B + TB * NP;
-    float* s_y = s_C + TB * NP;                                      // [TB][CH]
+    float4* s_tok = smem;                                            // [2][TB][CH / 2]: D_t and D_t x_t of two channels
+    float* s_B = reinterpret_cast<float*>(s_tok) + 2 * S::TOK;       // [2][TB][NP]
+    float* s_C = s_B + 2 * S::BC;
+    float2* s_y = reinterpret_cast<float2*>(s_C + 2 * S::BC);        // [2][TB][CH / 2][LANES]: each lane's share of C . h
 
     Piece q;
     if (!find_piece(p, blockIdx.x, q))
         return;
-    const int tid = threadIdx.x, sub = tid % LANES, ch = tid / LANES;
     const int group = blockIdx.y / p.chan_blocks, per_group = p.d / p.groups;
-    const int c0 = (blockIdx.y % p.chan_blocks) * CH;                // first channel, within the group
-    const int my = group * per_group + c0 + ch;                      // this thread's channel
-    const bool have = c0 + ch < per_group;
-    const int n0 = sub * 4;
-    // channel and first token of a tile that this thread loads and stores: token e * (kThreads / CH) + lt
-    const int lc = tid % CH, lt = tid / CH;
-    const int chan = group * per_group + c0 + lc;
-    const bool have_l = c0 + lc < per_group;
-
-    f2 A2[2], h2[2];
-    float h[4];
-    {
-        float a[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const bool ok = have && n0 + i < p.n;
-            a[i] = ok ? p.A[(long long)my * p.n + n0 + i] * kLog2e : 0.f;
-            h[i] = 0.f;
-            if (LOCAL ? q.last == blockIdx.x : q.t0 == 0) {
-                if (ok && p.state)
-                    h[i] = p.state[(q.seq * p.d + my) * p.n + n0 + i];
-            }
-        }
-        if (LOCAL) {
-            // The last piece's own share is not needed: its place keeps the state in front of the sequence, which the
-            // pass that follows may overwrite.
-            if (q.last == blockIdx.x) {
-                for (int i = 0; i < 4; ++i)
-                    if (have && n0 + i < p.n)
-                        p.local[((long long)blockIdx.x * p.d + my) * p.n + n0 + i] = h[i];
-                return;
-            }
-        } else if (q.t0 > 0) {
-            for (int i = 0; i < 4; ++i)
-                if (have && n0 + i < p.n)
-                    h[i] = p.local[(q.last * p.d + my) * p.n + n0 + i];
-            for (long long k = q.first; k < (long long)blockIdx.x; ++k) {
-                const float step = have ? p.local_step[k * p.d + my] : 0.f;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (have && n0 + i < p.n)
-                        h[i] = fmaf(ex2(a[i] * step), h[i], p.local[(k * p.d + my) * p.n + n0 + i]);
-            }
-        }
-        A2[0] = pack2(a[0], a[1]), A2[1] = pack2(a[2], a[3]);
-        h2[0] = pack2(h[0], h[1]), h2[1] = pack2(h[2], h[3]);
+    const int c0 = (blockIdx.y % p.chan_blocks) * S::CH;             // first channel, within the group
+    if (LOCAL && q.last == blockIdx.x) {
+        // The last piece's own share is not needed: its place keeps the state in front of the sequence, which the pass that
+        // follows may overwrite.
+        const long long first = group * per_group + c0, count = (long long)min(S::CH, per_group - c0) * p.n;
+        for (long long i = threadIdx.x; i < count; i += kThreads)
+            p.local[((long long)blockIdx.x * p.d + first) * p.n + i] = p.state ? p.state[(q.seq * p.d + first) * p.n + i] : 0.f;
+        return;
     }
-    const float bias = p.delta_bias && have_l ? p.delta_bias[chan] : 0.f;
-    const float skip = !LOCAL && p.D && have_l ? p.D[chan] : 0.f;
-    const long long seq = q.seq;
-
-    T rx[EPT], rd[EPT], rz[EPT], rB[BPT], rC[BPT];
-    auto load = [&](long long t) {
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const long long u = t + e * (kThreads / CH) + lt;
-            const bool ok = have_l && u < q.t1 && (TB * CH >= kThreads || lt < TB);
-            rx[e] = rd[e] = rz[e] = from_f<T>(0.f);
-            if (ok) {
-                rx[e] = row_ptr<const T>(p.x, seq, q.row0 + u)[chan];
-                rd[e] = row_ptr<const T>(p.delta, seq, q.row0 + u)[chan];
-                if (!LOCAL && p.z.ptr)
-                    rz[e] = row_ptr<const T>(p.z, seq, q.row0 + u)[chan];
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < BPT; ++e) {
-            const int at = e * kThreads + tid, u = at / NP, k = at % NP;
-            rB[e] = rC[e] = from_f<T>(0.f);
-            if (u < TB && t + u < q.t1 && k < p.n) {
-                rB[e] = row_ptr<const T>(p.B, seq, q.row0 + t + u)[group * p.n + k];
-                if (!LOCAL)
-                    rC[e] = row_ptr<const T>(p.C, seq, q.row0 + t + u)[group * p.n + k];
-            }
-        }
-    };
-    float xs[EPT], zs[EPT];                                          // of the tile in shared memory
-    auto stage = [&](long long t) {
-#pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kThreads / CH) + lt;
-            float step = to_f(rd[e]) + bias;
-            if (p.softplus)
-                step = softplus(step);
-            if (t + u >= q.t1 || !have_l)
-                step = 0.f;
-            xs[e] = to_f(rx[e]);
-            zs[e] = to_f(rz[e]);
-            // a padding token adds nothing, whatever step * x would be
-            const float v = t + u < q.t1 ? step * xs[e] : 0.f;
-            if (u < TB)
-                s_tok[u * CH + lc] = make_float4(step, step, v, v);
-        }
-#pragma unroll
-        for (int e = 0; e < BPT; ++e) {
-            const int at = e * kThreads + tid;
-            if (at < TB * NP) {
-                s_B[at] = to_f(rB[e]);
-                if (!LOCAL)
-                    s_C[at] = to_f(rC[e]);
-            }
-        }
-    };
-
-    float total = 0.f;
-    if (q.t0 < q.t1)
-        load(q.t0);
-    for (long long t = q.t0; t < q.t1; t += TB) {
-        stage(t);
-        __syncthreads();
-        float kx[EPT], kz[EPT];
-#pragma unroll
-        for (int e = 0; e < EPT; ++e)
-            kx[e] = xs[e], kz[e] = zs[e];
-        if (t + TB < q.t1)
-            load(t + TB);
-#pragma unroll 2
-        for (int u = 0; u < TB; u += 4) {
-            float part[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[(u + j) * CH + ch];
-                const ulonglong2 b = reinterpret_cast<const ulonglong2*>(s_B)[(u + j) * LANES + sub];
-                f2 y2 = 0;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float e0, e1;
-                    unpack2(mul2(A2[i], tok.x), e0, e1);
-                    h2[i] = fma2(pack2(ex2(e0), ex2(e1)), h2[i], mul2(tok.y, i ? b.y : b.x));
-                }
-                if (LOCAL) {
-                    float s, s1;
-                    unpack2(tok.x, s, s1);
-                    total += s;
-                } else {
-                    const ulonglong2 c = reinterpret_cast<const ulonglong2*>(s_C)[(u + j) * LANES + sub];
-                    y2 = fma2(h2[1], c.y, mul2(h2[0], c.x));
-                    part[j] = sum2(y2);
-                }
-            }
-            if (!LOCAL) {
-                group_sums<4, LANES, 1>(part, tid);
-                constexpr int left = LANES >= 4 ? 1 : 4 / LANES;
-                const int first = first_value<4, LANES>(sub);
-                if (LANES <= 4 || sub < 4)
-#pragma unroll
-                    for (int i = 0; i < left; ++i)
-                        s_y[(u + first + i) * CH + ch] = part[i];
-            }
-        }
-        __syncthreads();
-        if (!LOCAL) {
-#pragma unroll
-            for (int e = 0; e < EPT; ++e) {
-                const int u = e * (kThreads / CH) + lt;
-                if (u < TB && t + u < q.t1 && have_l) {
-                    float y = fmaf(skip, kx[e], s_y[u * CH + lc]);
-                    if (p.z.ptr)
-                        y *= silu(kz[e]);
-                    row_ptr<T>(p.y, seq, q.row0 + t + u)[chan] = from_f<T>(y);
-                }
-            }
-        }
-    }
-    unpack2(h2[0], h[0], h[1]);
-    unpack2(h2[1], h[2], h[3]);
-    if (LOCAL) {
-        for (int i = 0; i < 4; ++i)
-            if (have && n0 + i < p.n)
-                p.local[((long long)blockIdx.x * p.d + my) * p.n + n0 + i] = h[i];
-        if (have && sub == 0)
-            p.local_step[(long long)blockIdx.x * p.d + my] = total;
-    } else if (p.state_out && q.t1 == q.len) {
-        for (int i = 0; i < 4; ++i)
-            if (have && n0 + i < p.n)
-                p.state_out[(q.seq * p.d + my) * p.n + n0 + i] = h[i];
-    }
+    const int tiles = static_cast<int>((q.t1 - q.t0 + S::TB - 1) / S::TB);
+    if (threadIdx.x < kStateThreads)
+        run_states<LANES, LOCAL>(p, q, group, per_group, c0, s_tok, s_B, s_C, s_y, tiles);
+    else
+        run_rows<T, LANES, LOCAL, V>(p, q, group, per_group, c0, s_tok, s_B, s_C, s_y, tiles);
 }
 
 // Pieces of packed sequences: seq_first [batch + 1], and {sequence, first token} of each; every sequence has at least one
@@ -311,9 +463,9 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
 
 // One token of each sequence: the state is read and written once, which is what bounds it.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads) scan_step_kernel(const ScanDev p)
+__global__ void __launch_bounds__(kStepThreads) scan_step_kernel(const ScanDev p)
 {
-    constexpr int CH = kThreads / LANES;
+    constexpr int CH = kStepThreads / LANES;
     const int tid = threadIdx.x, sub = tid % LANES, ch = tid / LANES;
     const long long b = blockIdx.x;
     const int c = blockIdx.y * CH + ch;

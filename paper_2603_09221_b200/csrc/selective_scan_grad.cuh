@@ -16,6 +16,7 @@
 namespace ttc {
 namespace sscan {
 
+constexpr int kGradThreads = 128;
 constexpr int kPiece = 16;        // tokens of a piece
 constexpr int kRun = 4;           // pieces that a block works through, one behind the other
 
@@ -32,10 +33,10 @@ struct GradDev {
 };
 
 template <typename T, int LANES> struct Tile {
-    static constexpr int CH = kThreads / LANES, NP = LANES * 4, TB = kPiece;
-    static constexpr int EPT = (TB * CH + kThreads - 1) / kThreads;
-    static constexpr int BPT = (TB * NP + kThreads - 1) / kThreads;
-    static constexpr int WARPS = kThreads / 32;
+    static constexpr int CH = kGradThreads / LANES, NP = LANES * 4, TB = kPiece;
+    static constexpr int EPT = (TB * CH + kGradThreads - 1) / kGradThreads;
+    static constexpr int BPT = (TB * NP + kGradThreads - 1) / kGradThreads;
+    static constexpr int WARPS = kGradThreads / 32;
     static constexpr size_t smem_local() { return sizeof(float) * (TB * CH * 6 + TB * NP * 2); }
     // tokens (D, D, Dx, Dx | g, g), B, C, y and q . B and A . (q a h), shares of dB and dC by warp
     static constexpr size_t smem_piece() { return sizeof(float) * (TB * CH * 6 + TB * NP * 2 + TB * CH * 3 + WARPS * TB * NP * 2); }
@@ -53,7 +54,7 @@ template <typename T, int LANES> struct Loader {
         const int tid = threadIdx.x, lc = tid % CH, lt = tid / CH;
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kThreads / CH) + lt;
+            const int u = e * (kGradThreads / CH) + lt;
             const bool ok = have_l && u < TB && t + u < q.t1;
             x[e] = dy[e] = z[e] = step[e] = 0.f;
             if (ok) {
@@ -67,7 +68,7 @@ template <typename T, int LANES> struct Loader {
         }
 #pragma unroll
         for (int e = 0; e < BPT; ++e) {
-            const int at = e * kThreads + tid, u = at / NP, k = at % NP;
+            const int at = e * kGradThreads + tid, u = at / NP, k = at % NP;
             float b = 0.f, c = 0.f;
             if (u < TB && t + u < q.t1 && k < p.f.n) {
                 b = to_f(row_ptr<const T>(p.f.B, q.seq, q.row0 + t + u)[group * p.f.n + k]);
@@ -78,7 +79,7 @@ template <typename T, int LANES> struct Loader {
         }
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kThreads / CH) + lt;
+            const int u = e * (kGradThreads / CH) + lt;
             const bool ok = have_l && u < TB && t + u < q.t1;
             if (ok && p.f.softplus)
                 step[e] = softplus(step[e]);
@@ -93,7 +94,7 @@ template <typename T, int LANES> struct Loader {
 };
 
 template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads) grad_local_kernel(const GradDev p)
+__global__ void __launch_bounds__(kGradThreads) grad_local_kernel(const GradDev p)
 {
     using S = Tile<T, LANES>;
     constexpr int CH = S::CH, NP = S::NP, TB = S::TB;
@@ -218,7 +219,7 @@ static __global__ void __launch_bounds__(128) grad_join_kernel(const GradDev p)
 }
 
 template <typename T, int LANES>
-__global__ void __launch_bounds__(kThreads, 2) grad_piece_kernel(const GradDev p)
+__global__ void __launch_bounds__(kGradThreads, 2) grad_piece_kernel(const GradDev p)
 {
     using S = Tile<T, LANES>;
     constexpr int CH = S::CH, NP = S::NP, TB = S::TB, EPT = S::EPT, WARPS = S::WARPS;
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, 2) grad_piece_kernel(const GradDev p
         if (p.part_BC) {
             const long long row = slot * kPiece, rows = p.runs * kRun * kPiece;
             float* to = p.part_BC + (((long long)block * rows + row) * p.f.groups + group) * 2 * NP;
-            for (int at = tid; at < TB * 2 * NP; at += kThreads) {
+            for (int at = tid; at < TB * 2 * NP; at += kGradThreads) {
                 const int u = at / (2 * NP), v = at % (2 * NP);
                 float s = 0.f;
 #pragma unroll
@@ -364,7 +365,7 @@ __global__ void __launch_bounds__(kThreads, 2) grad_piece_kernel(const GradDev p
         // gradients of this thread's tokens
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kThreads / CH) + lt;
+            const int u = e * (kGradThreads / CH) + lt;
             if (u >= TB || t + u >= q.t1 || !have_l)
                 continue;
             const long long row = q.row0 + t + u;
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(kThreads, 2) grad_piece_kernel(const GradDev p
         __syncthreads();
         if (tid < CH && have_l) {
             float a = 0.f, b = 0.f;
-            for (int i = tid; i < kThreads; i += CH)
+            for (int i = tid; i < kGradThreads; i += CH)
                 a += sums[i].x, b += sums[i].y;
             p.part_D[((long long)blockIdx.x * 2) * p.f.d + chan] = a;
             p.part_D[((long long)blockIdx.x * 2 + 1) * p.f.d + chan] = b;
