@@ -78,7 +78,7 @@ ScanDev to_dev(const ttc_scan_args* a, bool step, bool grad = false)
     p.n = a->n;
     p.groups = a->groups;
     p.softplus = a->softplus;
-    const int ch = grad ? kGradThreads / lanes_of(a->n) : channels_of(lanes_of(a->n));
+    const int ch = grad ? 2 * kGradThreads / lanes_of(a->n) : channels_of(lanes_of(a->n));
     p.chan_blocks = (a->d / a->groups + ch - 1) / ch;
     p.x = dev_rows(a->x, off);
     p.delta = dev_rows(a->delta, off);
@@ -169,6 +169,7 @@ int map_pieces(const ScanDev& p, int64_t piece, int at_least, int64_t bound, cud
 struct GradPlan {
     GradDev g;
     size_t bytes;
+    bool pairs;
 };
 
 int plan_grad(int device, const ttc_scan_args* a, const ttc_scan_grads* g, void* ws, GradPlan& o)
@@ -213,6 +214,8 @@ int plan_grad(int device, const ttc_scan_args* a, const ttc_scan_grads* g, void*
     p.dD = g->dD;
     p.ddelta_bias = g->ddelta_bias;
     p.dstate = g->dstate;
+    o.pairs = in_pairs(a, {&a->x, &a->delta, &a->B, &a->C, &a->z, &g->dy, &g->dx, &g->ddelta, &g->dz});
+    p.f.vec4 = a->n % 4 == 0;                    // the states' scratch begins on 256 bytes
     const int64_t run = kPiece * kRun, states = (int64_t)a->d * a->n;
     p.f.piece = run;
     p.f.pieces_per_seq = (a->tokens + run - 1) / run;
@@ -330,22 +333,30 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
         using T = decltype(t);
         return by_lanes(lanes_of(a->n), [&](auto lc) {
             constexpr int LANES = decltype(lc)::value;
-            using S = Tile<T, LANES>;
+            using S = Tile<LANES>;
             const dim3 grid((unsigned)p.runs, (unsigned)(p.f.chan_blocks * p.f.groups));
-            if (p.runs) {
-                TTC_TRY(allow_smem(grad_local_kernel<T, LANES>, S::smem_local()));
-                grad_local_kernel<T, LANES><<<grid, kGradThreads, S::smem_local(), st>>>(p);
-                TTC_TRY(launched("gradients of the selective scan, shares of the pieces"));
-            }
+            auto local = [&](auto vc) {
+                constexpr int V = decltype(vc)::value;
+                TTC_TRY(allow_smem(grad_local_kernel<T, LANES, V>, S::smem_local()));
+                grad_local_kernel<T, LANES, V><<<grid, kGradThreads, S::smem_local(), st>>>(p);
+                return launched("gradients of the selective scan, shares of the pieces");
+            };
+            auto pieces = [&](auto vc) {
+                constexpr int V = decltype(vc)::value;
+                TTC_TRY(allow_smem(grad_piece_kernel<T, LANES, V>, S::smem_piece()));
+                grad_piece_kernel<T, LANES, V><<<grid, kGradThreads, S::smem_piece(), st>>>(p);
+                return launched("gradients of the selective scan");
+            };
+            constexpr std::integral_constant<int, 2> two;
+            constexpr std::integral_constant<int, 1> one;
+            if (p.runs)
+                TTC_TRY(o.pairs ? local(two) : local(one));
             if (a->batch) {
                 grad_join_kernel<<<dim3((unsigned)a->batch, (unsigned)((states + 127) / 128), 2), 128, 0, st>>>(p);
                 TTC_TRY(launched("gradients of the selective scan, states and co-states"));
             }
-            if (p.runs) {
-                TTC_TRY(allow_smem(grad_piece_kernel<T, LANES>, S::smem_piece()));
-                grad_piece_kernel<T, LANES><<<grid, kGradThreads, S::smem_piece(), st>>>(p);
-                TTC_TRY(launched("gradients of the selective scan"));
-            }
+            if (p.runs)
+                TTC_TRY(o.pairs ? pieces(two) : pieces(one));
             auto sum = [&](const float* part, int64_t stride, int64_t size, float* out) {
                 if (!out)
                     return (int)TTC_OK;

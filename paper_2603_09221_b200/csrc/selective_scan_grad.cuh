@@ -1,14 +1,16 @@
 // Gradients of the selective state space scan (selective_scan.cuh).  With g_t = dy_t silu(z_t) and the co-states
 //     q_t = C_t g_t + exp(D_{t+1} A) q_{t+1}
 // both recurrences, h forward and q backward, have the same decays, and the product of a span's decays is exp(A sum D_t).
-// Every sequence is cut into pieces of 16 tokens, as many as the registers of a thread hold states and decays for:
+// Every sequence is cut into pieces of 16 tokens:
 //   1  local_kernel    of every piece, from nothing: the state behind it, the co-state a_{t0} q_{t0} in front of it (in the
 //                      same walk: the running product of decays times C_t g_t) and the sum of its D_t
 //   2  join_kernel     along every sequence: the state that enters each piece, the co-state that comes back to it; dstate
-//   3  piece_kernel    of every piece, from those: states forward, co-states backward, every gradient
+//   3  piece_kernel    of every piece, from those, in two halves of as many tokens as registers hold states for: states
+//                      forward, co-states backward, every gradient
 //   4  reduce kernels  the blocks' shares of dA, dD, ddelta_bias and of dB, dC, in a fixed order
-// Steps 1 and 3 run over all tokens at once, whatever the number of sequences and channels.  Two exponentials per state
-// and token in all.  The layout of a block is that of the forward kernel.
+// Steps 1 and 3 run over all tokens at once, whatever the number of sequences and channels.  A lane holds four states of two
+// channels, as in the forward kernel.  Decays are computed again rather than kept: 3.5 exponentials per state and token in
+// all, against 64 more registers and half the warps.
 #pragma once
 
 #include "selective_scan.cuh"
@@ -17,7 +19,7 @@ namespace ttc {
 namespace sscan {
 
 constexpr int kGradThreads = 128;
-constexpr int kPiece = 16;        // tokens of a piece
+constexpr int kPiece = 16, kHalfPiece = 8;     // tokens of a piece, and as many as a thread's registers hold states for
 constexpr int kRun = 4;           // pieces that a block works through, one behind the other
 
 struct GradDev {
@@ -32,141 +34,250 @@ struct GradDev {
     float* part_BC;               // [chan_blocks][runs * kRun * kPiece][groups][2][NP]
 };
 
-template <typename T, int LANES> struct Tile {
-    static constexpr int CH = kGradThreads / LANES, NP = LANES * 4, TB = kPiece;
-    static constexpr int EPT = (TB * CH + kGradThreads - 1) / kGradThreads;
-    static constexpr int BPT = (TB * NP + kGradThreads - 1) / kGradThreads;
+template <int LANES> struct Tile {
+    static constexpr int CH = 2 * kGradThreads / LANES, NP = LANES * 4, TB = kPiece;
     static constexpr int WARPS = kGradThreads / 32;
-    static constexpr size_t smem_local() { return sizeof(float) * (TB * CH * 6 + TB * NP * 2); }
-    // tokens (D, D, Dx, Dx | g, g), B, C, y and q . B and A . (q a h), shares of dB and dC by warp
-    static constexpr size_t smem_piece() { return sizeof(float) * (TB * CH * 6 + TB * NP * 2 + TB * CH * 3 + WARPS * TB * NP * 2); }
+    // floats: D, Dx of a channel pair; g of it; B; C
+    static constexpr int TOK = TB * CH * 2, G = TB * CH, BC = TB * NP;
+    // of half a piece: the lanes' shares of C . h, of q . B and A . (q a h); the warps' shares of dB and dC
+    static constexpr int Y = kHalfPiece * CH * LANES, Q = 2 * Y, S = WARPS * kHalfPiece * 2 * NP;
+    static constexpr size_t smem_local() { return sizeof(float) * (TOK + G + 2 * BC); }
+    static constexpr size_t smem_piece() { return smem_local() + sizeof(float) * (Y + Q + S); }
 };
 
-// Decays and rows of a tile of kPiece tokens from token t of the run into shared memory.
-template <typename T, int LANES> struct Loader {
-    using S = Tile<T, LANES>;
-    static constexpr int CH = S::CH, NP = S::NP, TB = S::TB, EPT = S::EPT, BPT = S::BPT;
-    float x[EPT], dy[EPT], z[EPT], step[EPT];      // of this thread's tokens
+// A piece's rows: loads under way in registers, then step sizes, D_t x_t, dy_t silu(z_t), B and C in shared memory.
+template <typename T, int LANES, int V> struct Loader {
+    using S = Tile<LANES>;
+    static constexpr int CH = S::CH, NP = S::NP, TB = S::TB;
+    static constexpr int COLS = CH / V, ROWS = kGradThreads / COLS, PASSES = (TB + ROWS - 1) / ROWS;
+    static constexpr int BCOLS = NP / V, BROWS = kGradThreads / BCOLS, BPASSES = (TB + BROWS - 1) / BROWS;
+    Vec<T, V> x[PASSES], delta[PASSES], dy[PASSES], z[PASSES], B[BPASSES], C[BPASSES];
+    int lc, lr, chan, bc, br, group;
+    bool mine, mine_b;
+    float bias[V];
 
-    __device__ __forceinline__ void load(const GradDev& p, const Piece& q, long long t, int group, int chan, bool have_l, float bias,
-                                         float4* s_tok, float2* s_g, float* s_B, float* s_C)
+    __device__ __forceinline__ void start(const GradDev& p, int group_, int per_group, int c0)
     {
-        const int tid = threadIdx.x, lc = tid % CH, lt = tid / CH;
+        const int tid = threadIdx.x;
+        group = group_;
+        lc = tid % COLS * V, lr = tid / COLS;
+        chan = group * per_group + c0 + lc;
+        mine = c0 + lc < per_group && lr < TB;
+        bc = tid % BCOLS * V, br = tid / BCOLS;
+        mine_b = bc < p.f.n && br < TB;
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kGradThreads / CH) + lt;
-            const bool ok = have_l && u < TB && t + u < q.t1;
-            x[e] = dy[e] = z[e] = step[e] = 0.f;
-            if (ok) {
-                const long long row = q.row0 + t + u;
-                x[e] = to_f(row_ptr<const T>(p.f.x, q.seq, row)[chan]);
-                step[e] = to_f(row_ptr<const T>(p.f.delta, q.seq, row)[chan]) + bias;
-                dy[e] = to_f(row_ptr<const T>(p.dy, q.seq, row)[chan]);
-                if (p.f.z.ptr)
-                    z[e] = to_f(row_ptr<const T>(p.f.z, q.seq, row)[chan]);
+        for (int v = 0; v < V; ++v)
+            bias[v] = p.f.delta_bias && mine ? p.f.delta_bias[chan + v] : 0.f;
+    }
+    __device__ __forceinline__ void rows(Vec<T, V> (&to)[PASSES], const Rows& r, long long seq, long long row, bool ok, int left)
+    {
+        const T* from = row_ptr<const T>(r, seq, row + lr) + chan;
+        const long long pass = ROWS * r.ts;
+#pragma unroll
+        for (int e = 0; e < PASSES; ++e, from += pass)
+            to[e] = load_if(reinterpret_cast<const Vec<T, V>*>(from), ok && lr + e * ROWS < left);
+    }
+    __device__ __forceinline__ void shared_rows(Vec<T, V> (&to)[BPASSES], const Rows& r, const GradDev& p, long long seq, long long row, int left)
+    {
+        const T* from = row_ptr<const T>(r, seq, row + br) + group * p.f.n + bc;
+        const long long pass = BROWS * r.ts;
+#pragma unroll
+        for (int e = 0; e < BPASSES; ++e, from += pass)
+            to[e] = load_if(reinterpret_cast<const Vec<T, V>*>(from), mine_b && br + e * BROWS < left);
+    }
+    // rows row .. row + left of the sequence (at most a piece)
+    __device__ __forceinline__ void load(const GradDev& p, long long seq, long long row, int left)
+    {
+        left = left < TB ? left : TB;
+        rows(delta, p.f.delta, seq, row, mine, left);
+        rows(x, p.f.x, seq, row, mine, left);
+        rows(dy, p.dy, seq, row, mine, left);
+        rows(z, p.f.z, seq, row, mine && p.f.z.ptr, left);
+        shared_rows(B, p.f.B, p, seq, row, left);
+        shared_rows(C, p.f.C, p, seq, row, left);
+    }
+    __device__ __forceinline__ void stage(const GradDev& p, int left, float4* s_tok, float2* s_g, float* s_B, float* s_C) const
+    {
+        const bool gated = p.f.z.ptr;
+        if (ROWS <= TB || lr < TB) {
+#pragma unroll
+            for (int e = 0; e < PASSES; ++e) {
+                const int u = e * ROWS + lr;
+                float step[V], in[V], g[V];
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    step[v] = to_f(delta[e].v[v]) + bias[v];
+                    if (p.f.softplus)
+                        step[v] = softplus(step[v]);
+                    in[v] = step[v] * to_f(x[e].v[v]);
+                    g[v] = to_f(dy[e].v[v]);
+                    if (gated)
+                        g[v] *= silu(to_f(z[e].v[v]));
+                    if (u >= left)                                   // padding: nothing decays, nothing is added
+                        step[v] = in[v] = g[v] = 0.f;
+                }
+                float* tok = reinterpret_cast<float*>(s_tok + u * (CH / 2) + lc / 2) + lc % 2;
+                put<V>(tok, step);
+                put<V>(tok + 2, in);
+                put<V>(reinterpret_cast<float*>(s_g + u * (CH / 2) + lc / 2) + lc % 2, g);
             }
         }
+        if (BROWS <= TB || br < TB) {
 #pragma unroll
-        for (int e = 0; e < BPT; ++e) {
-            const int at = e * kGradThreads + tid, u = at / NP, k = at % NP;
-            float b = 0.f, c = 0.f;
-            if (u < TB && t + u < q.t1 && k < p.f.n) {
-                b = to_f(row_ptr<const T>(p.f.B, q.seq, q.row0 + t + u)[group * p.f.n + k]);
-                c = to_f(row_ptr<const T>(p.f.C, q.seq, q.row0 + t + u)[group * p.f.n + k]);
-            }
-            if (at < TB * NP)
-                s_B[at] = b, s_C[at] = c;
-        }
+            for (int e = 0; e < BPASSES; ++e) {
+                const int at = (e * BROWS + br) * NP + bc;
+                float b[V], c[V];
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kGradThreads / CH) + lt;
-            const bool ok = have_l && u < TB && t + u < q.t1;
-            if (ok && p.f.softplus)
-                step[e] = softplus(step[e]);
-            const float v = ok ? step[e] * x[e] : 0.f;
-            const float g = p.f.z.ptr && ok ? dy[e] * silu(z[e]) : dy[e];
-            if (u < TB) {
-                s_tok[u * CH + lc] = make_float4(step[e], step[e], v, v);
-                s_g[u * CH + lc] = make_float2(g, g);
+                for (int v = 0; v < V; ++v)
+                    b[v] = to_f(B[e].v[v]), c[v] = to_f(C[e].v[v]);
+                put<V>(s_B + at, b);
+                put<V>(s_C + at, c);
             }
         }
     }
 };
 
-template <typename T, int LANES>
-__global__ void __launch_bounds__(kGradThreads) grad_local_kernel(const GradDev p)
+// A thread's four states of two channels: where they lie, and A log2(e) as pairs of channels.
+struct Mine {
+    long long at[2];              // of state n0 of either channel in a [d][n] array
+    int count[2];                 // states of it that exist, 0 .. 4
+    f2 A2[4];
+    __device__ __forceinline__ void start(const GradDev& p, int group, int per_group, int c0, int pair, int n0)
+    {
+        float a[2][4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int ch = c0 + 2 * pair + c;
+            at[c] = (long long)(group * per_group + ch) * p.f.n + n0;
+            count[c] = ch < per_group ? max(0, min(4, p.f.n - n0)) : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                a[c][i] = i < count[c] ? p.f.A[at[c] + i] * kLog2e : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            A2[i] = pack2(a[0][i], a[1][i]);
+    }
+    __device__ __forceinline__ void get(const float* from, f2 (&v)[4], bool vec) const
+    {
+        float w[2][4];
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (vec) {
+                const float4 u = count[c] ? *reinterpret_cast<const float4*>(from + at[c]) : make_float4(0.f, 0.f, 0.f, 0.f);
+                w[c][0] = u.x, w[c][1] = u.y, w[c][2] = u.z, w[c][3] = u.w;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[c][i] = i < count[c] ? from[at[c] + i] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = pack2(w[0][i], w[1][i]);
+    }
+    __device__ __forceinline__ void set(float* to, const f2 (&v)[4], bool vec) const
+    {
+        float w[2][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            unpack2(v[i], w[0][i], w[1][i]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (vec) {
+                if (count[c])
+                    *reinterpret_cast<float4*>(to + at[c]) = make_float4(w[c][0], w[c][1], w[c][2], w[c][3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < count[c])
+                        to[at[c] + i] = w[c][i];
+            }
+        }
+    }
+};
+
+// exp(D A) of a token
+__device__ __forceinline__ void decays(f2 (&a)[4], const f2 (&A2)[4], f2 step)
 {
-    using S = Tile<T, LANES>;
-    constexpr int CH = S::CH, NP = S::NP, TB = S::TB;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float e0, e1;
+        unpack2(mul2(A2[i], step), e0, e1);
+        a[i] = pack2(ex2(e0), ex2(e1));
+    }
+}
+// h = a h + D x B
+__device__ __forceinline__ void advance(f2 (&h)[4], const f2 (&a)[4], f2 in, const float4& b4)
+{
+    float in0, in1;
+    unpack2(in, in0, in1);
+    const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        h[i] = fma2(a[i], h[i], pack2(in0 * b[i], in1 * b[i]));
+}
+
+template <typename T, int LANES, int V>
+__global__ void __launch_bounds__(kGradThreads, 4) grad_local_kernel(const GradDev p)
+{
+    using S = Tile<LANES>;
+    constexpr int CH = S::CH, TB = S::TB;
     extern __shared__ float4 smem[];
-    float4* s_tok = smem;
-    float* s_B = reinterpret_cast<float*>(s_tok + TB * CH);
-    float* s_C = s_B + TB * NP;
-    float2* s_g = reinterpret_cast<float2*>(s_C + TB * NP);
+    float4* s_tok = smem;                                            // [TB][CH / 2]
+    float2* s_g = reinterpret_cast<float2*>(s_tok + S::TOK / 4);     // [TB][CH / 2]
+    float* s_B = reinterpret_cast<float*>(s_g + S::G / 2);           // [TB][NP]
+    float* s_C = s_B + S::BC;
 
     Piece q;
     if (!find_piece(p.f, blockIdx.x, q))
         return;
-    const int tid = threadIdx.x, sub = tid % LANES, ch = tid / LANES;
+    const int tid = threadIdx.x, sub = tid % LANES, pair = tid / LANES;
     const int group = blockIdx.y / p.f.chan_blocks, per_group = p.f.d / p.f.groups;
     const int c0 = (blockIdx.y % p.f.chan_blocks) * CH;
-    const int my = group * per_group + c0 + ch, n0 = sub * 4;
-    const bool have = c0 + ch < per_group;
-    const int chan = group * per_group + c0 + tid % CH;
-    const bool have_l = c0 + tid % CH < per_group;
-    f2 A2[2];
-    {
-        float a[4];
+    Mine my;
+    my.start(p, group, per_group, c0, pair, sub * 4);
+    Loader<T, LANES, V> tile;
+    tile.start(p, group, per_group, c0);
+    const long long states = (long long)p.f.d * p.f.n;
+    int left = static_cast<int>(q.t1 - q.t0);
+    long long row = q.row0 + q.t0, slot = (long long)blockIdx.x * kRun;
+    tile.load(p, q.seq, row, left);
+    for (; left > 0; left -= kPiece, row += kPiece, ++slot) {
+        tile.stage(p, left, s_tok, s_g, s_B, s_C);
+        __syncthreads();
+        tile.load(p, q.seq, row + kPiece, left - kPiece);
+        f2 h[4] = {0, 0, 0, 0}, r[4] = {0, 0, 0, 0}, prod[4], total = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            a[i] = have && n0 + i < p.f.n ? p.f.A[(long long)my * p.f.n + n0 + i] * kLog2e : 0.f;
-        A2[0] = pack2(a[0], a[1]), A2[1] = pack2(a[2], a[3]);
-    }
-    const float bias = p.f.delta_bias && have_l ? p.f.delta_bias[chan] : 0.f;
-    Loader<T, LANES> tile;
-    for (int k = 0; k < kRun; ++k) {
-        const long long t = q.t0 + k * kPiece;
-        if (t >= q.t1)
-            break;
-        __syncthreads();
-        tile.load(p, q, t, group, chan, have_l, bias, s_tok, s_g, s_B, s_C);
-        __syncthreads();
-        f2 h2[2] = {0, 0}, r2[2] = {0, 0}, prod[2];
-        prod[0] = prod[1] = pack2(1.f, 1.f);
-        float total = 0.f;
+            prod[i] = pack2(1.f, 1.f);
 #pragma unroll 4
         for (int u = 0; u < TB; ++u) {
-            const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[u * CH + ch];
-            const f2 g = reinterpret_cast<const f2*>(s_g)[u * CH + ch];
-            const ulonglong2 b = reinterpret_cast<const ulonglong2*>(s_B)[u * LANES + sub];
-            const ulonglong2 c = reinterpret_cast<const ulonglong2*>(s_C)[u * LANES + sub];
+            const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[u * (CH / 2) + pair];
+            f2 a[4];
+            decays(a, my.A2, tok.x);
+            advance(h, a, tok.y, reinterpret_cast<const float4*>(s_B)[u * LANES + sub]);
+            const float2 g = s_g[u * (CH / 2) + pair];
+            const float4 c4 = reinterpret_cast<const float4*>(s_C)[u * LANES + sub];
+            const float c[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float e0, e1;
-                unpack2(mul2(A2[i], tok.x), e0, e1);
-                const f2 a = pack2(ex2(e0), ex2(e1));
-                h2[i] = fma2(a, h2[i], mul2(tok.y, i ? b.y : b.x));
-                prod[i] = mul2(prod[i], a);
-                r2[i] = fma2(prod[i], mul2(g, i ? c.y : c.x), r2[i]);
+            for (int i = 0; i < 4; ++i) {
+                prod[i] = mul2(prod[i], a[i]);
+                r[i] = fma2(prod[i], pack2(g.x * c[i], g.y * c[i]), r[i]);
             }
-            float s, s1;
-            unpack2(tok.x, s, s1);
-            total += s;
+            total = add2(total, tok.x);
         }
-        const long long slot = (long long)blockIdx.x * kRun + k;
-        float h[4], r[4];
-        unpack2(h2[0], h[0], h[1]);
-        unpack2(h2[1], h[2], h[3]);
-        unpack2(r2[0], r[0], r[1]);
-        unpack2(r2[1], r[2], r[3]);
+        my.set(p.h + slot * states, h, p.f.vec4);
+        my.set(p.r + slot * states, r, p.f.vec4);
+        if (sub == 0) {
+            float s[2];
+            unpack2(total, s[0], s[1]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (have && n0 + i < p.f.n) {
-                p.h[(slot * p.f.d + my) * p.f.n + n0 + i] = h[i];
-                p.r[(slot * p.f.d + my) * p.f.n + n0 + i] = r[i];
-            }
-        if (have && sub == 0)
-            p.step[slot * p.f.d + my] = total;
+            for (int c = 0; c < 2; ++c)
+                if (my.count[c])
+                    p.step[slot * p.f.d + group * per_group + c0 + 2 * pair + c] = s[c];
+        }
+        __syncthreads();
     }
 }
 
@@ -183,227 +294,248 @@ static __global__ void __launch_bounds__(128) grad_join_kernel(const GradDev p)
     count = count < most ? count : most;
     const float a = p.f.A[at] * kLog2e;
     constexpr int kAhead = 8;
-    if (blockIdx.z == 0) {
-        float h = p.f.state ? p.f.state[seq * size + at] : 0.f;
-        for (long long k = 0; k < count; k += kAhead) {
-            float v[kAhead], s[kAhead];
+    // states walk forward, co-states backward; what each piece adds is replaced by what enters it
+    const bool back = blockIdx.z;
+    const long long start = back ? first + count - 1 : first;
+    float* v = (back ? p.r : p.h) + start * size + at;
+    const float* s = p.step + start * p.f.d + c;
+    const long long v_next = back ? -size : size, s_next = back ? -(long long)p.f.d : p.f.d;
+    const float* from = back ? p.dstate_out : p.f.state;
+    float h = from ? from[seq * size + at] : 0.f;
+    for (; count >= kAhead; count -= kAhead) {
+        float add[kAhead], step[kAhead];
+        const float *vv = v, *ss = s;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k + i < count)
-                    v[i] = p.h[(first + k + i) * size + at], s[i] = p.step[(first + k + i) * p.f.d + c];
+        for (int i = 0; i < kAhead; ++i, vv += v_next, ss += s_next)
+            add[i] = *vv, step[i] = *ss;
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k + i < count) {
-                    p.h[(first + k + i) * size + at] = h;
-                    h = fmaf(ex2(a * s[i]), h, v[i]);
-                }
+        for (int i = 0; i < kAhead; ++i, v += v_next) {
+            *v = h;
+            h = fmaf(ex2(a * step[i]), h, add[i]);
         }
-    } else {
-        float r = p.dstate_out ? p.dstate_out[seq * size + at] : 0.f;
-        for (long long k = count - 1; k >= 0; k -= kAhead) {
-            float v[kAhead], s[kAhead];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k - i >= 0)
-                    v[i] = p.r[(first + k - i) * size + at], s[i] = p.step[(first + k - i) * p.f.d + c];
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (k - i >= 0) {
-                    p.r[(first + k - i) * size + at] = r;
-                    r = fmaf(ex2(a * s[i]), r, v[i]);
-                }
-        }
-        if (p.dstate)
-            p.dstate[seq * size + at] = r;
+        s = ss;
     }
+    for (; count > 0; --count, v += v_next, s += s_next) {
+        const float add = *v, step = *s;
+        *v = h;
+        h = fmaf(ex2(a * step), h, add);
+    }
+    if (back && p.dstate)
+        p.dstate[seq * size + at] = h;
 }
 
-template <typename T, int LANES>
-__global__ void __launch_bounds__(kGradThreads, 2) grad_piece_kernel(const GradDev p)
+template <typename T, int LANES, int V>
+__global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradDev p)
 {
-    using S = Tile<T, LANES>;
-    constexpr int CH = S::CH, NP = S::NP, TB = S::TB, EPT = S::EPT, WARPS = S::WARPS;
+    using S = Tile<LANES>;
+    using L = Loader<T, LANES, V>;
+    constexpr int CH = S::CH, NP = S::NP, WARPS = S::WARPS, HALF = kHalfPiece;
     extern __shared__ float4 smem[];
-    float4* s_tok = smem;
-    float* s_B = reinterpret_cast<float*>(s_tok + TB * CH);
-    float* s_C = s_B + TB * NP;
-    float2* s_g = reinterpret_cast<float2*>(s_C + TB * NP);
-    float* s_y = reinterpret_cast<float*>(s_g + TB * CH);            // C . h
-    float2* s_q = reinterpret_cast<float2*>(s_y + TB * CH);          // q . B and A . (q a h)
-    float* s_BC = reinterpret_cast<float*>(s_q + TB * CH);           // [WARPS][TB][2][NP]
+    float4* s_tok = smem;                                            // [TB][CH / 2]
+    float2* s_g = reinterpret_cast<float2*>(s_tok + S::TOK / 4);     // [TB][CH / 2]
+    float* s_B = reinterpret_cast<float*>(s_g + S::G / 2);           // [TB][NP]
+    float* s_C = s_B + S::BC;
+    float4* s_q = reinterpret_cast<float4*>(s_C + S::BC);            // [HALF][CH / 2][LANES]: q . B and A . (q a h), of two channels
+    float2* s_y = reinterpret_cast<float2*>(s_q + S::Q / 4);         // [HALF][CH / 2][LANES]: C . h
+    float* s_BC = reinterpret_cast<float*>(s_y + S::Y / 2);          // [WARPS][HALF][2][NP]
 
     Piece q;
     if (!find_piece(p.f, blockIdx.x, q))
         return;
-    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, sub = tid % LANES, ch = tid / LANES;
+    const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32, sub = tid % LANES, pair = tid / LANES, n0 = sub * 4;
     const int group = blockIdx.y / p.f.chan_blocks, per_group = p.f.d / p.f.groups, block = blockIdx.y % p.f.chan_blocks;
     const int c0 = block * CH;
-    const int my = group * per_group + c0 + ch, n0 = sub * 4;
-    const bool have = c0 + ch < per_group;
-    const int lc = tid % CH, lt = tid / CH, chan = group * per_group + c0 + lc;
-    const bool have_l = c0 + lc < per_group;
-    f2 A2[2], dA2[2] = {0, 0};
-    {
-        float a[4];
+    Mine my;
+    my.start(p, group, per_group, c0, pair, n0);
+    L tile;
+    tile.start(p, group, per_group, c0);
+    float skip[V], sum_D[V] = {}, sum_bias[V] = {};
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        skip[v] = p.f.D && tile.mine ? p.f.D[tile.chan + v] : 0.f;
+    f2 dA[4] = {0, 0, 0, 0};
+    const long long states = (long long)p.f.d * p.f.n;
+    const bool want_z = p.dz.ptr;
+    int left = static_cast<int>(q.t1 - q.t0);
+    long long row = q.row0 + q.t0, slot = (long long)blockIdx.x * kRun;
+    for (; left > 0; left -= kPiece, row += kPiece, ++slot) {
+        tile.load(p, q.seq, row, left);
+        f2 h0[4], h1[4], r[4];                                       // states in front of both halves, co-state behind
+        my.get(p.h + slot * states, h0, p.f.vec4);
+        my.get(p.r + slot * states, r, p.f.vec4);
+        tile.stage(p, left, s_tok, s_g, s_B, s_C);
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            a[i] = have && n0 + i < p.f.n ? p.f.A[(long long)my * p.f.n + n0 + i] * kLog2e : 0.f;
-        A2[0] = pack2(a[0], a[1]), A2[1] = pack2(a[2], a[3]);
-    }
-    const float bias = p.f.delta_bias && have_l ? p.f.delta_bias[chan] : 0.f;
-    const float skip = p.f.D && have_l ? p.f.D[chan] : 0.f;
-    float sum_D = 0.f, sum_bias = 0.f;
-    Loader<T, LANES> tile;
-    for (int k = 0; k < kRun; ++k) {
-        const long long t = q.t0 + k * kPiece;
-        if (t >= q.t1)
-            break;
-        const long long slot = (long long)blockIdx.x * kRun + k;
-        float h[4], r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            h[i] = r[i] = 0.f;
-            if (have && n0 + i < p.f.n) {
-                h[i] = p.h[(slot * p.f.d + my) * p.f.n + n0 + i];
-                r[i] = p.r[(slot * p.f.d + my) * p.f.n + n0 + i];
-            }
+            h1[i] = h0[i];
+#pragma unroll 4
+        for (int u = 0; u < HALF; ++u) {
+            const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[u * (CH / 2) + pair];
+            f2 a[4];
+            decays(a, my.A2, tok.x);
+            advance(h1, a, tok.y, reinterpret_cast<const float4*>(s_B)[u * LANES + sub]);
         }
-        __syncthreads();
-        tile.load(p, q, t, group, chan, have_l, bias, s_tok, s_g, s_B, s_C);
-        __syncthreads();
-        f2 a2[TB][2], h2[TB + 1][2], r2[2];                          // h2[u]: the state in front of token u
-        h2[0][0] = pack2(h[0], h[1]), h2[0][1] = pack2(h[2], h[3]);
-        r2[0] = pack2(r[0], r[1]), r2[1] = pack2(r[2], r[3]);
+#pragma unroll 1
+        for (int half = 1; half >= 0; --half) {                      // (one copy of the code: two overflow the instruction cache)
+            if (half * HALF < left) {
+                // states of the half, h[u] in front of token u
+                f2 h[HALF + 1][4];
 #pragma unroll
-        for (int u = 0; u < TB; u += 4) {
-            float part[4];
+                for (int i = 0; i < 4; ++i)
+                    h[0][i] = half ? h1[i] : h0[i];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[(u + j) * CH + ch];
-                const ulonglong2 b = reinterpret_cast<const ulonglong2*>(s_B)[(u + j) * LANES + sub];
-                f2 y2 = 0;
+                for (int u = 0; u < HALF; ++u) {
+                    const int at = half * HALF + u;
+                    const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[at * (CH / 2) + pair];
+                    f2 a[4];
+                    decays(a, my.A2, tok.x);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    float e0, e1;
-                    unpack2(mul2(A2[i], tok.x), e0, e1);
-                    a2[u + j][i] = pack2(ex2(e0), ex2(e1));
-                    h2[u + j + 1][i] = fma2(a2[u + j][i], h2[u + j][i], mul2(tok.y, i ? b.y : b.x));
-                }
-                if (p.dz.ptr) {
-                    const ulonglong2 c = reinterpret_cast<const ulonglong2*>(s_C)[(u + j) * LANES + sub];
-                    y2 = fma2(h2[u + j + 1][1], c.y, mul2(h2[u + j + 1][0], c.x));
-                }
-                part[j] = sum2(y2);
-            }
-            if (p.dz.ptr) {
-                group_sums<4, LANES, 1>(part, lane);
-                constexpr int left = LANES >= 4 ? 1 : 4 / LANES;
-                const int first = first_value<4, LANES>(sub);
-                if (LANES <= 4 || sub < 4)
+                    for (int i = 0; i < 4; ++i)
+                        h[u + 1][i] = h[u][i];
+                    advance(h[u + 1], a, tok.y, reinterpret_cast<const float4*>(s_B)[at * LANES + sub]);
+                    if (want_z) {
+                        const float4 c4 = reinterpret_cast<const float4*>(s_C)[at * LANES + sub];
+                        const float c[4] = {c4.x, c4.y, c4.z, c4.w};
+                        float y0 = 0.f, y1 = 0.f;
 #pragma unroll
-                    for (int i = 0; i < left; ++i)
-                        s_y[(u + first + i) * CH + ch] = part[i];
-            }
-        }
-        float pair[4];                                               // q . B and A . (q a h) of two tokens
-#pragma unroll
-        for (int u = TB - 1; u >= 0; --u) {
-            const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[u * CH + ch];
-            const f2 g = reinterpret_cast<const f2*>(s_g)[u * CH + ch];
-            const ulonglong2 b = reinterpret_cast<const ulonglong2*>(s_B)[u * LANES + sub];
-            const ulonglong2 c = reinterpret_cast<const ulonglong2*>(s_C)[u * LANES + sub];
-            float bc[8];
-            f2 qB = 0, through = 0;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const f2 co = fma2(g, i ? c.y : c.x, r2[i]);         // q_t
-                unpack2(mul2(co, tok.y), bc[2 * i], bc[2 * i + 1]);
-                unpack2(mul2(h2[u + 1][i], g), bc[4 + 2 * i], bc[5 + 2 * i]);
-                r2[i] = mul2(a2[u][i], co);
-                const f2 qah = mul2(r2[i], h2[u][i]);
-                dA2[i] = fma2(tok.x, qah, dA2[i]);
-                qB = i ? fma2(co, b.y, qB) : mul2(co, b.x);
-                through = i ? fma2(A2[i], qah, through) : mul2(A2[i], qah);
-            }
-            group_sums<8, 32 / LANES, LANES>(bc, lane);
-            {
-                constexpr int W = 32 / LANES, left = W >= 8 ? 1 : 8 / W;
-                const int j = lane / LANES, first = first_value<8, W>(j);
-                if (W <= 8 || j < 8)
-#pragma unroll
-                    for (int i = 0; i < left; ++i) {
-                        const int v = first + i;
-                        s_BC[((warp * TB + u) * 2 + v / 4) * NP + n0 + v % 4] = bc[i];
+                        for (int i = 0; i < 4; ++i) {
+                            float a0, a1;
+                            unpack2(h[u + 1][i], a0, a1);
+                            y0 = fmaf(a0, c[i], y0), y1 = fmaf(a1, c[i], y1);
+                        }
+                        s_y[u * (CH / 2 * LANES) + tid] = make_float2(y0, y1);
                     }
-            }
-            pair[(u & 1) * 2] = sum2(qB);
-            pair[(u & 1) * 2 + 1] = sum2(through);
-            if (u % 2 == 0) {
-                group_sums<4, LANES, 1>(pair, lane);
-                constexpr int left = LANES >= 4 ? 1 : 4 / LANES;
-                const int first = first_value<4, LANES>(sub);
-                if (LANES <= 4 || sub < 4)
+                }
 #pragma unroll
-                    for (int i = 0; i < left; ++i)
-                        reinterpret_cast<float*>(s_q)[((u + (first + i) / 2) * CH + ch) * 2 + (first + i) % 2] = pair[i];
-            }
-        }
-        __syncthreads();
-        // shares of dB and dC of this block's channels
-        if (p.part_BC) {
-            const long long row = slot * kPiece, rows = p.runs * kRun * kPiece;
-            float* to = p.part_BC + (((long long)block * rows + row) * p.f.groups + group) * 2 * NP;
-            for (int at = tid; at < TB * 2 * NP; at += kGradThreads) {
-                const int u = at / (2 * NP), v = at % (2 * NP);
-                float s = 0.f;
+                for (int u = HALF - 1; u >= 0; --u) {
+                    const int at = half * HALF + u;
+                    const ulonglong2 tok = reinterpret_cast<const ulonglong2*>(s_tok)[at * (CH / 2) + pair];
+                    const float2 g = s_g[at * (CH / 2) + pair];
+                    const float4 b4 = reinterpret_cast<const float4*>(s_B)[at * LANES + sub], c4 = reinterpret_cast<const float4*>(s_C)[at * LANES + sub];
+                    const float b[4] = {b4.x, b4.y, b4.z, b4.w}, c[4] = {c4.x, c4.y, c4.z, c4.w};
+                    f2 a[4], through = 0;
+                    decays(a, my.A2, tok.x);
+                    float in0, in1, bc[8], qB0 = 0.f, qB1 = 0.f;
+                    unpack2(tok.y, in0, in1);
 #pragma unroll
-                for (int w = 0; w < WARPS; ++w)
-                    s += s_BC[(w * TB + u) * 2 * NP + v];
-                to[(long long)u * p.f.groups * 2 * NP + v] = s;
-            }
-        }
-        // gradients of this thread's tokens
+                    for (int i = 0; i < 4; ++i) {
+                        const f2 co = add2(r[i], pack2(g.x * c[i], g.y * c[i]));      // q_t
+                        float q0, q1, s0, s1;
+                        unpack2(co, q0, q1);
+                        unpack2(h[u + 1][i], s0, s1);
+                        bc[i] = fmaf(q1, in1, q0 * in0);
+                        bc[4 + i] = fmaf(s1, g.y, s0 * g.x);
+                        qB0 = fmaf(q0, b[i], qB0), qB1 = fmaf(q1, b[i], qB1);
+                        r[i] = mul2(a[i], co);
+                        const f2 qah = mul2(r[i], h[u][i]);
+                        dA[i] = fma2(tok.x, qah, dA[i]);
+                        through = fma2(my.A2[i], qah, through);
+                    }
+                    float th0, th1;
+                    unpack2(through, th0, th1);
+                    s_q[u * (CH / 2 * LANES) + tid] = make_float4(qB0, qB1, th0, th1);
+                    group_sums<8, 32 / LANES, LANES>(bc, lane);
+                    constexpr int W = 32 / LANES, kept = W >= 8 ? 1 : 8 / W;
+                    const int j = lane / LANES, first = first_value<8, W>(j);
+                    if (W <= 8 || j < 8)
 #pragma unroll
-        for (int e = 0; e < EPT; ++e) {
-            const int u = e * (kGradThreads / CH) + lt;
-            if (u >= TB || t + u >= q.t1 || !have_l)
-                continue;
-            const long long row = q.row0 + t + u;
-            const float2 s = s_q[u * CH + lc];
-            const float g = s_g[u * CH + lc].x;
-            if (p.dx.ptr)
-                row_ptr<T>(p.dx, q.seq, row)[chan] = from_f<T>(fmaf(tile.step[e], s.x, skip * g));
-            float dstep = fmaf(tile.x[e], s.x, s.y * (1.f / kLog2e));
-            if (p.f.softplus)
-                dstep *= -expm1f(-tile.step[e]);                     // the logistic function of what the softplus was given
-            if (p.ddelta.ptr)
-                row_ptr<T>(p.ddelta, q.seq, row)[chan] = from_f<T>(dstep);
-            if (p.dz.ptr)
-                row_ptr<T>(p.dz, q.seq, row)[chan] = from_f<T>(tile.dy[e] * fmaf(skip, tile.x[e], s_y[u * CH + lc]) * silu_slope(tile.z[e]));
-            sum_D = fmaf(g, tile.x[e], sum_D);
-            sum_bias += dstep;
+                        for (int i = 0; i < kept; ++i) {
+                            const int v = first + i;
+                            s_BC[((warp * HALF + u) * 2 + v / 4) * NP + n0 + v % 4] = bc[i];
+                        }
+                    asm volatile("" ::: "memory");                   // keeps the loads of a token with its products
+                }
+                __syncthreads();
+                // shares of dB and dC of this block's channels
+                if (p.part_BC) {
+                    const long long at0 = slot * kPiece + half * HALF, rows = p.runs * kRun * kPiece;
+                    float* to = p.part_BC + (((long long)block * rows + at0) * p.f.groups + group) * 2 * NP;
+                    for (int at = tid; at < HALF * 2 * NP; at += kGradThreads) {
+                        const int u = at / (2 * NP), v = at % (2 * NP);
+                        float s = 0.f;
+#pragma unroll
+                        for (int w = 0; w < WARPS; ++w)
+                            s += s_BC[(w * HALF + u) * 2 * NP + v];
+                        to[(long long)u * p.f.groups * 2 * NP + v] = s;
+                    }
+                }
+                // gradients of this thread's tokens
+#pragma unroll
+                for (int e = 0; e < L::PASSES; ++e) {
+                    const int u = e * L::ROWS + tile.lr;
+                    if (u / HALF != half || u >= left || !tile.mine)
+                        continue;
+                    const int at = (u % HALF * (CH / 2) + tile.lc / 2) * LANES;
+                    float4 s = s_q[at];
+#pragma unroll
+                    for (int i = 1; i < LANES; ++i) {
+                        const float4 m = s_q[at + i];
+                        s.x += m.x, s.y += m.y, s.z += m.z, s.w += m.w;
+                    }
+                    float2 y = make_float2(0.f, 0.f);
+                    if (want_z) {
+                        y = s_y[at];
+#pragma unroll
+                        for (int i = 1; i < LANES; ++i) {
+                            const float2 m = s_y[at + i];
+                            y.x += m.x, y.y += m.y;
+                        }
+                    }
+                    const float* steps = reinterpret_cast<const float*>(s_tok + u * (CH / 2) + tile.lc / 2) + tile.lc % 2;
+                    const float* gs = reinterpret_cast<const float*>(s_g + u * (CH / 2) + tile.lc / 2) + tile.lc % 2;
+                    Vec<T, V> dx, ddelta, dz;
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
+                        const bool odd = V == 2 ? v : tile.lc % 2;
+                        const float qB = odd ? s.y : s.x, th = odd ? s.w : s.z, step = steps[v], g = gs[v], x = to_f(tile.x[e].v[v]);
+                        dx.v[v] = from_f<T>(fmaf(step, qB, skip[v] * g));
+                        float d = fmaf(x, qB, th * (1.f / kLog2e));
+                        if (p.f.softplus) {
+                            // the logistic function of what the softplus was given, 1 - exp(-D); a series where that cancels
+                            const float small = step * fmaf(step, fmaf(step, fmaf(step, -1.f / 24, 1.f / 6), -0.5f), 1.f);
+                            d *= step < 0.06f ? small : 1.f - ex2(step * -kLog2e);
+                        }
+                        ddelta.v[v] = from_f<T>(d);
+                        if (want_z) {
+                            const float z = to_f(tile.z[e].v[v]);
+                            dz.v[v] = from_f<T>(to_f(tile.dy[e].v[v]) * fmaf(skip[v], x, odd ? y.y : y.x) * silu_slope(z));
+                        }
+                        sum_D[v] = fmaf(g, x, sum_D[v]);
+                        sum_bias[v] += d;
+                    }
+                    const long long to = row + u;
+                    if (p.dx.ptr)
+                        *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.dx, q.seq, to) + tile.chan) = dx;
+                    if (p.ddelta.ptr)
+                        *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.ddelta, q.seq, to) + tile.chan) = ddelta;
+                    if (want_z)
+                        *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.dz, q.seq, to) + tile.chan) = dz;
+                }
+                __syncthreads();
+            }
         }
     }
-    if (p.part_A) {
-        float v[4];
-        unpack2(dA2[0], v[0], v[1]);
-        unpack2(dA2[1], v[2], v[3]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (have && n0 + i < p.f.n)
-                p.part_A[((long long)blockIdx.x * p.f.d + my) * p.f.n + n0 + i] = v[i];
-    }
+    if (p.part_A)
+        my.set(p.part_A + (long long)blockIdx.x * states, dA, p.f.vec4);
     if (p.part_D) {
+        // a channel's sums lie with the ROWS threads that load it
+        float* sums = reinterpret_cast<float*>(s_q);                 // [2][ROWS][CH]
+        if (tile.mine)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                sums[tile.lr * CH + tile.lc + v] = sum_D[v];
+                sums[(L::ROWS + tile.lr) * CH + tile.lc + v] = sum_bias[v];
+            }
         __syncthreads();
-        float2* sums = reinterpret_cast<float2*>(s_tok);
-        sums[tid] = make_float2(sum_D, sum_bias);
-        __syncthreads();
-        if (tid < CH && have_l) {
-            float a = 0.f, b = 0.f;
-            for (int i = tid; i < kGradThreads; i += CH)
-                a += sums[i].x, b += sums[i].y;
-            p.part_D[((long long)blockIdx.x * 2) * p.f.d + chan] = a;
-            p.part_D[((long long)blockIdx.x * 2 + 1) * p.f.d + chan] = b;
+        constexpr int held = L::ROWS < kPiece ? L::ROWS : kPiece;
+        for (int c = tid; c < 2 * CH; c += kGradThreads) {
+            const int kind = c / CH, ch = c % CH;
+            if (c0 + ch >= per_group)
+                continue;
+            float s = 0.f;
+            for (int i = 0; i < held; ++i)
+                s += sums[(kind * L::ROWS + i) * CH + ch];
+            p.part_D[((long long)blockIdx.x * 2 + kind) * p.f.d + group * per_group + c0 + ch] = s;
         }
     }
 }
