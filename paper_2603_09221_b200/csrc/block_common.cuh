@@ -29,7 +29,13 @@ template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
 template <typename P> __device__ __forceinline__ P load_if(const P* from, bool ok)
 {
     P r;
-    if constexpr (sizeof(P) == 8) {
+    if constexpr (sizeof(P) == 16) {
+        uint4 v;
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+                     "@p ld.global.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}\n"
+                     : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w) : "l"(from), "r"((int)ok));
+        r = *reinterpret_cast<P*>(&v);
+    } else if constexpr (sizeof(P) == 8) {
         uint2 v;
         asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %3, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\t@p ld.global.v2.b32 {%0, %1}, [%2];\n\t}\n"
                      : "=&r"(v.x), "=&r"(v.y) : "l"(from), "r"((int)ok));

@@ -29,15 +29,18 @@ int check(const ttc_conv_args* a, bool step)
     return check_floats("state_out", a->state_out, true, element_size(a->dtype));
 }
 
-// Channels that a thread takes at once: `most` bytes, 4, or one element, by the alignment of every pointer and stride.
+// Channels that a thread takes, and whether every pointer and stride allows one access for them: else they are two, one by one.
 struct Width {
     size_t size;
-    int d, v;
-    Width(int dtype, int d_, int most) : size(element_size(dtype)), d(d_), v(most / (int)element_size(dtype)) { fit(nullptr, d, 0); }
+    int v;
+    bool aligned;
+    Width(int dtype, int d, int most) : size(element_size(dtype)), v(most), aligned(true) { fit(nullptr, d, 0); }
     void fit(const void* p, int64_t s0, int64_t s1)
     {
-        while (v > 1 && (reinterpret_cast<uintptr_t>(p) % (v * size) || s0 % v || s1 % v))
-            v /= 2;
+        while (aligned && (reinterpret_cast<uintptr_t>(p) % (v * size) || s0 % v || s1 % v)) {
+            aligned = v > 2;
+            v = 2;
+        }
     }
     void rows(const ttc_rows& r, bool packed, bool step)
     {
@@ -68,46 +71,43 @@ ConvDev to_dev(const ttc_conv_args* a, bool step)
     return p;
 }
 
-// Tokens of a tile: 128, or fewer (not below 16) while there are less than about eight blocks for every SM.  A tile reads
+// Tokens of a tile: 128, or fewer (not below 16) while there are less than about six blocks for every SM.  A tile reads
 // the W - 1 rows in front of it again.
 void set_tiles(ConvDev& p, int v, int sms)
 {
     const int64_t cols = (p.d + (int64_t)v * kThreads - 1) / (v * kThreads);
     const int64_t seqs = p.seqs.offsets ? 1 : p.seqs.batch;
     p.tile = 128;
-    while (p.tile > 16 && seqs * ((p.seqs.tokens + p.tile - 1) / p.tile) * cols < 8 * (int64_t)sms)
+    while (p.tile > 16 && seqs * ((p.seqs.tokens + p.tile - 1) / p.tile) * cols < 6 * (int64_t)sms)
         p.tile /= 2;
     p.tiles = (p.seqs.tokens + p.tile - 1) / p.tile;
 }
 
 int64_t all_tiles(const ConvDev& p) { return p.tiles * (p.seqs.offsets ? 1 : p.seqs.batch); }
 
-template <typename F> int by_shape(int dtype, int v, int taps, F&& f)
+template <bool WIDE, typename F> int by_shape(int dtype, const Width& w, int taps, F&& f)
 {
     return by_type(dtype, [&](auto t) {
-        using T = decltype(t);
-        constexpr int most = 8 / (int)sizeof(T), two = 4 / (int)sizeof(T);
-        auto with_v = [&](auto vc) {
-            constexpr int V = decltype(vc)::value;
+        auto with = [&](auto vc, auto ac) {
             switch (taps) {
-            case 2: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 2>());
-            case 3: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 3>());
-            default: return f(t, std::integral_constant<int, V>(), std::integral_constant<int, 4>());
+            case 2: return f(t, vc, ac, std::integral_constant<int, 2>());
+            case 3: return f(t, vc, ac, std::integral_constant<int, 3>());
+            default: return f(t, vc, ac, std::integral_constant<int, 4>());
             }
         };
-        if (v == most)
-            return with_v(std::integral_constant<int, most>());
-        if (two > 1 && v == two)
-            return with_v(std::integral_constant<int, two>());
-        return with_v(std::integral_constant<int, 1>());
+        if constexpr (WIDE)
+            if (w.v == 4)
+                return with(std::integral_constant<int, 4>(), std::true_type());
+        return w.aligned ? with(std::integral_constant<int, 2>(), std::true_type()) : with(std::integral_constant<int, 2>(), std::false_type());
     });
 }
 
 struct GradPlan {
     ConvDev p;
-    int v;
+    Width w;
     size_t bytes;
     bool params;
+    explicit GradPlan(const ttc_conv_args* a) : w(a ? a->dtype : TTC_F32, a ? a->d : 2, 2) {}
 };
 
 int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void* ws, GradPlan& o)
@@ -136,15 +136,14 @@ int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void*
     p.dstate = g->dstate;
     p.dw = g->dw;
     p.dbias = g->dbias;
-    Width w(a->dtype, a->d, 4);
+    Width& w = o.w;
     w.rows(a->x, packed, false);
     w.rows(g->dy, packed, false);
     w.rows(g->dx, packed, false);
     w.window(a->state);
     w.window(g->dstate);
     w.window(g->dstate_out);
-    o.v = w.v;
-    set_tiles(p, o.v, sm_count(device));
+    set_tiles(p, w.v, sm_count(device));
     o.params = g->dw || g->dbias;
     Scratch s(ws);
     float* part = s.take<float>(o.params ? (size_t)all_tiles(p) * (a->taps + 1) * a->d : 0);
@@ -168,19 +167,20 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
     TTC_TRY(scope.enter(device));
     if (a->batch == 0)
         return TTC_OK;
-    Width w(a->dtype, a->d, 8);
+    Width w(a->dtype, a->d, 2);
     w.rows(a->x, packed, false);
     w.rows(a->y, packed, false);
     w.window(a->state);
     ConvDev p = to_dev(a, false);
     set_tiles(p, w.v, sm_count(device));
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return by_shape(a->dtype, w.v, a->taps, [&](auto t, auto vc, auto wc) {
+    return by_shape<false>(a->dtype, w, a->taps, [&](auto t, auto vc, auto ac, auto wc) {
         using T = decltype(t);
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        constexpr bool ALIGNED = decltype(ac)::value;
         if (a->tokens) {
             const dim3 grid((unsigned)all_tiles(p), (a->d + V * kThreads - 1) / (V * kThreads));
-            conv_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+            conv_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
             TTC_TRY(launched("causal convolution"));
         }
         if (a->state_out) {
@@ -202,27 +202,28 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
     TTC_TRY(scope.enter(device));
     if (a->batch == 0)
         return TTC_OK;
-    Width w(a->dtype, a->d, 8);
+    Width w(a->dtype, a->d, 4);
     w.rows(a->x, false, true);
     w.rows(a->y, false, true);
     w.window(a->state_out);
     // few sequences: narrower loads keep more SMs at work
-    while (w.v > 1 && a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads)) < sm_count(device))
-        w.v /= 2;
+    if (w.v > 2 && a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads)) < sm_count(device))
+        w.v = 2;
     const ConvDev p = to_dev(a, true);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return by_shape(a->dtype, w.v, a->taps, [&](auto t, auto vc, auto wc) {
+    return by_shape<true>(a->dtype, w, a->taps, [&](auto t, auto vc, auto ac, auto wc) {
         using T = decltype(t);
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        constexpr bool ALIGNED = decltype(ac)::value;
         const dim3 grid((unsigned)a->batch, (a->d + V * kThreads - 1) / (V * kThreads));
-        conv_step_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+        conv_step_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
         return launched("causal convolution, one token");
     });
 }
 
 int64_t ttc_causal_conv_grad_workspace(int32_t device, const ttc_conv_args* a, const ttc_conv_grads* g)
 {
-    GradPlan o;
+    GradPlan o(a);
     TTC_TRY(plan_grad(device, a, g, nullptr, o));
     return (int64_t)o.bytes;
 }
@@ -230,20 +231,21 @@ int64_t ttc_causal_conv_grad_workspace(int32_t device, const ttc_conv_args* a, c
 int ttc_causal_conv_grad(int32_t device, const ttc_conv_args* a, const ttc_conv_grads* g, void* workspace,
                          int64_t workspace_bytes, void* cuda_stream)
 {
-    GradPlan o;
+    GradPlan o(a);
     TTC_TRY(plan_grad(device, a, g, workspace, o));
     TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
     DeviceScope scope;
     TTC_TRY(scope.enter(device));
     const ConvDev& p = o.p;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return by_shape(a->dtype, o.v, a->taps, [&](auto t, auto vc, auto wc) {
+    return by_shape<false>(a->dtype, o.w, a->taps, [&](auto t, auto vc, auto ac, auto wc) {
         using T = decltype(t);
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
+        constexpr bool ALIGNED = decltype(ac)::value;
         const int64_t tiles = all_tiles(p);
         if (tiles) {
             const dim3 grid((unsigned)tiles, (a->d + V * kThreads - 1) / (V * kThreads));
-            conv_grad_kernel<T, V, W><<<grid, kThreads, 0, st>>>(p);
+            conv_grad_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
             TTC_TRY(launched("gradients of the causal convolution"));
         }
         if (o.params) {

@@ -1,10 +1,13 @@
 // Depthwise causal convolution of token rows, z_t = bias + sum_j w_j x_{t-(W-1)+j}, y_t = act(z_t), its gradients, and the
 // step of a single token.
 //
-// A thread owns V neighbouring channels (8 bytes, backward 4, where rows are aligned for it) and walks over a tile of tokens with the
+// A thread owns V = 2 neighbouring channels (four in the step), loaded and stored at once where rows are aligned for it and
+// one by one where they are not, computes on packed pairs of them, and walks over a tile of tokens with the
 // last W inputs in registers, so an input is read once apart from the W - 1 rows in front of a tile.  Memory bounds all
 // three kernels: one read and one write per element forward, two and one backward.
 #pragma once
+
+#include <type_traits>
 
 #include "block_common.cuh"
 
@@ -14,6 +17,7 @@ namespace conv {
 using namespace blk;
 
 constexpr int kThreads = 128;
+constexpr int kAhead = 8, kGradAhead = 4;      // tokens whose loads are under way together
 
 struct ConvDev {
     Seqs seqs;
@@ -35,8 +39,21 @@ struct Segment {
     long long t0, t1;               // tokens of it in the tile
 };
 
-// Calls f for every sequence that has tokens in tile `i`.
-template <typename F> __device__ __forceinline__ void for_segments(const ConvDev& p, long long i, F&& f)
+// First sequence that ends behind the first row of tile `i`: every lane of the warp looks at some of them, so that one round
+// of loads does where a search by halves would wait for several.  All lanes of the warp take part.
+__device__ __forceinline__ long long first_sequence(const ConvDev& p, long long i)
+{
+    if (!p.seqs.offsets)
+        return 0;
+    const long long r0 = i * p.tile;
+    int before = 0;
+    for (long long b = threadIdx.x % 32; b < p.seqs.batch; b += 32)
+        before += clamp_offset(p.seqs, b + 1) <= r0;
+    return __reduce_add_sync(0xffffffffu, before);
+}
+
+// Calls f for every sequence that has tokens in tile `i`, the first of which may be `from`.
+template <typename F> __device__ __forceinline__ void for_segments(const ConvDev& p, long long i, long long from, F&& f)
 {
     if (!p.seqs.offsets) {
         const long long seq = i / p.tiles, t0 = (i % p.tiles) * p.tile;
@@ -44,31 +61,87 @@ template <typename F> __device__ __forceinline__ void for_segments(const ConvDev
         return;
     }
     const long long r0 = i * p.tile, r1 = r0 + p.tile < p.seqs.tokens ? r0 + p.tile : p.seqs.tokens;
-    long long lo = 0, hi = p.seqs.batch;            // first sequence that ends behind r0
-    while (lo < hi) {
-        const long long mid = (lo + hi) / 2;
-        if (clamp_offset(p.seqs, mid + 1) > r0)
-            hi = mid;
-        else
-            lo = mid + 1;
-    }
-    for (; lo < p.seqs.batch; ++lo) {
-        const Span s = span_of(p.seqs, lo);
+    for (long long b = from; b < p.seqs.batch; ++b) {
+        const Span s = span_of(p.seqs, b);
         if (s.row0 >= r1)
             break;
         const long long t0 = r0 > s.row0 ? r0 - s.row0 : 0, t1 = r1 - s.row0 < s.len ? r1 - s.row0 : s.len;
         if (t0 < t1)
-            f(Segment{lo, s.row0, s.len, t0, t1});
+            f(Segment{b, s.row0, s.len, t0, t1});
     }
 }
 
+// V channels of a row, `count` of which exist; ALIGNED: as one access.  What does not exist reads as the channel before it.
+template <bool ALIGNED, typename T, int V> __device__ __forceinline__ Vec<T, V> fetch(const T* from, int count)
+{
+    if constexpr (ALIGNED) {
+        return *reinterpret_cast<const Vec<T, V>*>(from);
+    } else {
+        static_assert(V == 2, "");
+        Vec<T, V> r;
+        r.v[0] = from[0];
+        r.v[1] = from[count - 1];
+        return r;
+    }
+}
+template <bool ALIGNED, typename T, int V> __device__ __forceinline__ Vec<T, V> fetch_if(const T* from, bool ok, int count)
+{
+    if constexpr (ALIGNED) {
+        return load_if(reinterpret_cast<const Vec<T, V>*>(from), ok);
+    } else {
+        Vec<T, V> r;
+        r.v[0] = load_if(reinterpret_cast<const Vec<T, 1>*>(from), ok).v[0];
+        r.v[1] = load_if(reinterpret_cast<const Vec<T, 1>*>(from + (count - 1)), ok).v[0];
+        return r;
+    }
+}
+template <bool ALIGNED, typename T, int V> __device__ __forceinline__ void give(T* to, const Vec<T, V>& v, int count)
+{
+    if constexpr (ALIGNED) {
+        *reinterpret_cast<Vec<T, V>*>(to) = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < count)
+                to[i] = v.v[i];
+    }
+}
+template <typename T, int V> __device__ __forceinline__ void widen(f2 (&to)[V / 2], const Vec<T, V>& v)
+{
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i)
+        to[i] = pack2(to_f(v.v[2 * i]), to_f(v.v[2 * i + 1]));
+}
+template <typename T, int V> __device__ __forceinline__ Vec<T, V> narrow(const f2 (&from)[V / 2])
+{
+    Vec<T, V> r;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        float a, b;
+        unpack2(from[i], a, b);
+        r.v[2 * i] = from_f<T>(a), r.v[2 * i + 1] = from_f<T>(b);
+    }
+    return r;
+}
+
+// the logistic function of both
+__device__ __forceinline__ f2 sigmoid2(f2 z)
+{
+    float a, b;
+    unpack2(mul2(z, pack2(-kLog2e, -kLog2e)), a, b);
+    unpack2(add2(pack2(ex2(a), ex2(b)), pack2(1.f, 1.f)), a, b);
+    return pack2(rcp(a), rcp(b));
+}
+
 template <typename T, int V, int W> struct Taps {
-    float w[W][V], b[V];
+    f2 w[W][V / 2], b[V / 2];
+    int count;                      // channels that exist
     __device__ __forceinline__ void load(const ConvDev& p, int c)
     {
-        float all[V * W];
+        count = p.d - c < V ? p.d - c : V;
+        float all[V * W], bias[V];
         const float* from = p.w + (long long)c * W;
-        if (V * W % 4 == 0 && p.vec_w) {
+        if (V * W % 4 == 0 && p.vec_w && count == V) {
 #pragma unroll
             for (int i = 0; i < V * W; i += 4) {
                 const float4 u = *reinterpret_cast<const float4*>(from + i);
@@ -77,88 +150,81 @@ template <typename T, int V, int W> struct Taps {
         } else {
 #pragma unroll
             for (int i = 0; i < V * W; ++i)
-                all[i] = from[i];
+                all[i] = i < count * W ? from[i] : 0.f;
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            b[v] = p.bias ? p.bias[c + v] : 0.f;
+        for (int v = 0; v < V; ++v)
+            bias[v] = p.bias && v < count ? p.bias[c + v] : 0.f;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            b[i] = pack2(bias[2 * i], bias[2 * i + 1]);
 #pragma unroll
             for (int j = 0; j < W; ++j)
-                w[j][v] = all[v * W + j];
+                w[j][i] = pack2(all[2 * i * W + j], all[(2 * i + 1) * W + j]);
         }
     }
-    // moves the window on by one input and returns z of channel i
-    __device__ __forceinline__ float next(float (&in)[W][V], int i, float x) const
+    // moves the window on by one input and returns z of pair i
+    __device__ __forceinline__ f2 next(f2 (&in)[W][V / 2], int i, f2 x) const
     {
 #pragma unroll
         for (int j = 0; j + 1 < W; ++j)
             in[j][i] = in[j + 1][i];
         in[W - 1][i] = x;
-        float z = b[i];
+        f2 z = b[i];
 #pragma unroll
         for (int j = 0; j < W; ++j)
-            z = fmaf(w[j][i], in[j][i], z);
+            z = fma2(w[j][i], in[j][i], z);
         return z;
     }
 };
 
 // Input at token t of a sequence, which lies in the window in front of it where t < 0.
-template <typename T, int V, int W>
-__device__ __forceinline__ Vec<T, V> input_at(const ConvDev& p, const Segment& s, long long t, int c)
+template <bool ALIGNED, typename T, int V, int W>
+__device__ __forceinline__ Vec<T, V> input_at(const ConvDev& p, const Segment& s, long long t, int c, int count)
 {
-    if (t >= 0)
-        return *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, s.seq, s.row0 + t) + c);
-    if (p.state)
-        return *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.state) + (s.seq * (W - 1) + (W - 1) + t) * p.d + c);
-    Vec<T, V> zero;
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        zero.v[v] = from_f<T>(0.f);
-    return zero;
+    const T* from = t >= 0 ? row_ptr<const T>(p.x, s.seq, s.row0 + t) + c : static_cast<const T*>(p.state) + (s.seq * (W - 1) + (W - 1) + t) * p.d + c;
+    return fetch_if<ALIGNED, T, V>(from, t >= 0 || p.state, count);
 }
 
-constexpr int kAhead = 8;           // tokens whose loads are under way together
-
-template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads) conv_kernel(const ConvDev p)
+template <typename T, int V, bool ALIGNED, int W>
+__global__ void __launch_bounds__(kThreads, 10) conv_kernel(const ConvDev p)
 {
     const int c = (blockIdx.y * kThreads + threadIdx.x) * V;
+    const long long from = first_sequence(p, blockIdx.x);
     if (c >= p.d)
         return;
     Taps<T, V, W> k;
     k.load(p, c);
-    for_segments(p, blockIdx.x, [&](const Segment& s) {
-        float in[W][V];                                              // the last W inputs, oldest first
+    for_segments(p, blockIdx.x, from, [&](const Segment& s) {
+        f2 in[W][V / 2];                                             // the last W inputs, oldest first
 #pragma unroll
-        for (int j = 1; j < W; ++j) {
-            const Vec<T, V> v = input_at<T, V, W>(p, s, s.t0 - W + j, c);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                in[j][i] = to_f(v.v[i]);
-        }
+        for (int j = 1; j < W; ++j)
+            widen(in[j], input_at<ALIGNED, T, V, W>(p, s, s.t0 - W + j, c, k.count));
         const T* x = row_ptr<const T>(p.x, s.seq, s.row0 + s.t0) + c;
         T* y = row_ptr<T>(p.y, s.seq, s.row0 + s.t0) + c;
-        auto give = [&](const Vec<T, V>& v, T* to) {
-            Vec<T, V> out;
+        auto token = [&](const Vec<T, V>& v) {
+            f2 out[V / 2], now[V / 2];
+            widen(now, v);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float z = k.next(in, i, to_f(v.v[i]));
-                out.v[i] = from_f<T>(p.act == TTC_ACT_SILU ? silu(z) : z);
+            for (int i = 0; i < V / 2; ++i) {
+                const f2 z = k.next(in, i, now[i]);
+                out[i] = p.act == TTC_ACT_SILU ? mul2(z, sigmoid2(z)) : z;
             }
-            *reinterpret_cast<Vec<T, V>*>(to) = out;
+            give<ALIGNED>(y, narrow<T, V>(out), k.count);
+            y += p.y.ts;
         };
         int left = static_cast<int>(s.t1 - s.t0);
-        for (; left >= kAhead; left -= kAhead, x += kAhead * p.x.ts, y += kAhead * p.y.ts) {
-            Vec<T, V> next[kAhead];
+        for (; left >= kAhead; left -= kAhead) {
+            Vec<T, V> now[kAhead];
+#pragma unroll
+            for (int a = 0; a < kAhead; ++a, x += p.x.ts)
+                now[a] = fetch<ALIGNED, T, V>(x, k.count);
 #pragma unroll
             for (int a = 0; a < kAhead; ++a)
-                next[a] = *reinterpret_cast<const Vec<T, V>*>(x + a * p.x.ts);
-#pragma unroll
-            for (int a = 0; a < kAhead; ++a)
-                give(next[a], y + a * p.y.ts);
+                token(now[a]);
         }
-        for (; left > 0; --left, x += p.x.ts, y += p.y.ts)
-            give(*reinterpret_cast<const Vec<T, V>*>(x), y);
+        for (; left > 0; --left, x += p.x.ts)
+            token(fetch<ALIGNED, T, V>(x, k.count));
     });
 }
 
@@ -174,161 +240,160 @@ __global__ void __launch_bounds__(kThreads) conv_window_kernel(const ConvDev p)
     T v[W - 1];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
-        v[j] = input_at<T, 1, W>(p, g, s.len - (W - 1) + j, c).v[0];
+        v[j] = input_at<true, T, 1, W>(p, g, s.len - (W - 1) + j, c, 1).v[0];
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
         static_cast<T*>(p.state_out)[((long long)blockIdx.x * (W - 1) + j) * p.d + c] = v[j];
 }
 
-template <typename T, int V, int W>
+template <typename T, int V, bool ALIGNED, int W>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvDev p)
 {
     const int c = (blockIdx.y * kThreads + threadIdx.x) * V;
     if (c >= p.d)
         return;
     const long long b = blockIdx.x;
-    Vec<T, V> in[W], out;
+    const int count = p.d - c < V ? p.d - c : V;
+    Vec<T, V> in[W];
     T* st = static_cast<T*>(p.state_out) + b * (W - 1) * p.d + c;
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
-        in[j] = *reinterpret_cast<const Vec<T, V>*>(st + (long long)j * p.d);
-    in[W - 1] = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, b, 0) + c);
+        in[j] = fetch<ALIGNED, T, V>(st + (long long)j * p.d, count);
+    in[W - 1] = fetch<ALIGNED, T, V>(row_ptr<const T>(p.x, b, 0) + c, count);
     Taps<T, V, W> k;
     k.load(p, c);
+    f2 z[V / 2];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        float z = k.b[i];
+    for (int i = 0; i < V / 2; ++i)
+        z[i] = k.b[i];
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-            z = fmaf(k.w[j][i], to_f(in[j].v[i]), z);
-        out.v[i] = from_f<T>(p.act == TTC_ACT_SILU ? silu(z) : z);
+    for (int j = 0; j < W; ++j) {
+        f2 now[V / 2];
+        widen(now, in[j]);
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            z[i] = fma2(k.w[j][i], now[i], z[i]);
     }
-    *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.y, b, 0) + c) = out;
+    if (p.act == TTC_ACT_SILU)
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i)
+            z[i] = mul2(z[i], sigmoid2(z[i]));
+    give<ALIGNED>(row_ptr<T>(p.y, b, 0) + c, narrow<T, V>(z), count);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)
-        *reinterpret_cast<Vec<T, V>*>(st + (long long)j * p.d) = in[j + 1];
+        give<ALIGNED>(st + (long long)j * p.d, in[j + 1], count);
 }
-
-constexpr int kGradAhead = 8;
 
 // Gradients.  With dz_t = dy_t act'(z_t):  dx_s = sum_j w_j dz_{s+W-1-j}, so a walk that has reached token t can give out
 // the gradient of input t - (W - 1); it runs W - 1 tokens past its tile (whose z it computes again) or past the
 // sequence's end (dz = 0), and in front of the sequence the inputs are the window's.
-template <typename T, int V, int W>
-__global__ void __launch_bounds__(kThreads) conv_grad_kernel(const ConvDev p)
+template <typename T, int V, bool ALIGNED, int W>
+__global__ void __launch_bounds__(kThreads, 7) conv_grad_kernel(const ConvDev p)
 {
     const int c = (blockIdx.y * kThreads + threadIdx.x) * V;
+    const long long from = first_sequence(p, blockIdx.x);
     if (c >= p.d)
         return;
     Taps<T, V, W> k;
     k.load(p, c);
-    float dw[W][V] = {}, db[V] = {};
-    auto push = [](float (&dz)[W][V], int i, float g) {
+    f2 dw[W][V / 2] = {}, db[V / 2] = {};
+    for_segments(p, blockIdx.x, from, [&](const Segment& s) {
+        f2 in[W][V / 2], dz[W][V / 2] = {};                          // the last W inputs and dz, oldest first
 #pragma unroll
-        for (int j = 0; j + 1 < W; ++j)
-            dz[j][i] = dz[j + 1][i];
-        dz[W - 1][i] = g;
-    };
-    auto input_grad = [&](const float (&dz)[W][V], int i, float g) {
+        for (int j = 1; j < W; ++j)
+            widen(in[j], input_at<ALIGNED, T, V, W>(p, s, s.t0 - W + j, c, k.count));
+        const T* x = row_ptr<const T>(p.x, s.seq, s.row0 + s.t0) + c;
+        const T* dy = row_ptr<const T>(p.dy, s.seq, s.row0 + s.t0) + c;
+        T* dx = p.dx.ptr ? row_ptr<T>(p.dx, s.seq, s.row0 + s.t0) + c : nullptr;
+        // Token t: EDGE where it may lie past the tile or the sequence, or the input it leads to in front of the tile.
+        auto token = [&](auto edge, long long u, const Vec<T, V>& vx, const Vec<T, V>& vy) {
+            constexpr bool EDGE = decltype(edge)::value;
+            const bool real = !EDGE || u < s.len, mine = !EDGE || u < s.t1;
+            f2 now[V / 2], g[V / 2], out[V / 2] = {};
+            const long long at = u - (W - 1), back = at - (s.len - (W - 1));          // input, and its place in the last window
+            if (EDGE && back >= 0 && p.dstate_out)
+                widen(out, fetch<ALIGNED, T, V>(static_cast<const T*>(p.dstate_out) + (s.seq * (W - 1) + back) * p.d + c, k.count));
+            widen(now, vx);
+            widen(g, vy);                                            // zero past the sequence
 #pragma unroll
-        for (int j = 0; j < W; ++j)
-            g = fmaf(k.w[j][i], dz[W - 1 - j][i], g);
-        return g;
-    };
-    for_segments(p, blockIdx.x, [&](const Segment& s) {
-        float in[W][V], dz[W][V] = {};                               // the last W inputs and dz, oldest first
+            for (int i = 0; i < V / 2; ++i) {
+                const f2 z = k.next(in, i, now[i]);
+                if (p.act == TTC_ACT_SILU) {
+                    const f2 q = sigmoid2(z), rest = fma2(q, pack2(-1.f, -1.f), pack2(1.f, 1.f));
+                    g[i] = real ? mul2(g[i], fma2(mul2(q, z), rest, q)) : 0;
+                }
 #pragma unroll
-        for (int j = 1; j < W; ++j) {
-            const Vec<T, V> v = input_at<T, V, W>(p, s, s.t0 - W + j, c);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                in[j][i] = to_f(v.v[i]);
-        }
-        // one token, wherever it lies
-        auto any = [&](long long u) {
-            const bool real = u < s.len, mine = u < s.t1;
-            Vec<T, V> nx, ny, extra, out;
-            if (real) {
-                nx = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.x, s.seq, s.row0 + u) + c);
-                ny = *reinterpret_cast<const Vec<T, V>*>(row_ptr<const T>(p.dy, s.seq, s.row0 + u) + c);
-            }
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float z = k.next(in, i, real ? to_f(nx.v[i]) : 0.f);
-                float g = real ? to_f(ny.v[i]) : 0.f;
-                if (p.act == TTC_ACT_SILU && real)
-                    g *= silu_slope(z);
-                push(dz, i, g);
+                for (int j = 0; j + 1 < W; ++j)
+                    dz[j][i] = dz[j + 1][i];
+                dz[W - 1][i] = g[i];
                 if (mine) {
-                    db[i] += g;
+                    db[i] = add2(db[i], g[i]);
 #pragma unroll
                     for (int j = 0; j < W; ++j)
-                        dw[j][i] = fmaf(g, in[j][i], dw[j][i]);
+                        dw[j][i] = fma2(g[i], in[j][i], dw[j][i]);
                 }
+#pragma unroll
+                for (int j = 0; j < W; ++j)
+                    out[i] = fma2(k.w[j][i], dz[W - 1 - j][i], out[i]);
             }
-            // inputs of this tile, and of the window for the tile that begins the sequence
-            const long long at = u - (W - 1);
-            if (at < s.t0 && !(s.t0 == 0 && p.dstate))
-                return;
-            const long long back = at - (s.len - (W - 1));           // place in the last window
-            const bool more = back >= 0 && p.dstate_out;
-            if (more)
-                extra = *reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dstate_out) + (s.seq * (W - 1) + back) * p.d + c);
-#pragma unroll
-            for (int i = 0; i < V; ++i)
-                out.v[i] = from_f<T>(input_grad(dz, i, more ? to_f(extra.v[i]) : 0.f));
-            if (at < 0)
-                *reinterpret_cast<Vec<T, V>*>(static_cast<T*>(p.dstate) + (s.seq * (W - 1) + (W - 1) + at) * p.d + c) = out;
-            else if (p.dx.ptr)
-                *reinterpret_cast<Vec<T, V>*>(row_ptr<T>(p.dx, s.seq, s.row0 + at) + c) = out;
-        };
-        const long long stop = s.t1 + W - 1;
-        long long t = s.t0;
-        for (; t < s.t0 + W - 1; ++t)
-            any(t);
-        // in between, a token and the input W - 1 in front of it are both of this tile, and the last window is further on
-        const T* x = row_ptr<const T>(p.x, s.seq, s.row0 + t) + c;
-        const T* dy = row_ptr<const T>(p.dy, s.seq, s.row0 + t) + c;
-        T* dx = p.dx.ptr ? row_ptr<T>(p.dx, s.seq, s.row0 + t - (W - 1)) + c : nullptr;
-        for (; t + kGradAhead <= s.t1; t += kGradAhead, x += kGradAhead * p.x.ts, dy += kGradAhead * p.dy.ts) {
-            Vec<T, V> nx[kGradAhead], ny[kGradAhead];
-#pragma unroll
-            for (int a = 0; a < kGradAhead; ++a) {
-                nx[a] = *reinterpret_cast<const Vec<T, V>*>(x + a * p.x.ts);
-                ny[a] = *reinterpret_cast<const Vec<T, V>*>(dy + a * p.dy.ts);
-            }
-#pragma unroll
-            for (int a = 0; a < kGradAhead; ++a) {
-                Vec<T, V> out;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float z = k.next(in, i, to_f(nx[a].v[i]));
-                    float g = to_f(ny[a].v[i]);
-                    if (p.act == TTC_ACT_SILU)
-                        g *= silu_slope(z);
-                    push(dz, i, g);
-                    db[i] += g;
-#pragma unroll
-                    for (int j = 0; j < W; ++j)
-                        dw[j][i] = fmaf(g, in[j][i], dw[j][i]);
-                    out.v[i] = from_f<T>(input_grad(dz, i, 0.f));
-                }
+            if (!EDGE || at >= s.t0) {
                 if (dx) {
-                    *reinterpret_cast<Vec<T, V>*>(dx) = out;
+                    give<ALIGNED>(dx, narrow<T, V>(out), k.count);
                     dx += p.dx.ts;
                 }
+            } else if (s.t0 == 0 && p.dstate) {                      // of the window, by the tile that begins the sequence
+                give<ALIGNED>(static_cast<T*>(p.dstate) + (s.seq * (W - 1) + (W - 1) + at) * p.d + c, narrow<T, V>(out), k.count);
             }
+        };
+        const long long stop = s.t1 + W - 1, rows = stop < s.len ? stop : s.len;
+        // a group of W - 1 tokens, then groups that lie inside, then what is left
+        auto edge = [&](long long t, int count) {
+            Vec<T, V> vx[kGradAhead], vy[kGradAhead];
+#pragma unroll
+            for (int a = 0; a < kGradAhead; ++a) {
+                const bool ok = a < count && t + a < rows;
+                vx[a] = fetch_if<ALIGNED, T, V>(x + a * p.x.ts, ok, k.count);
+                vy[a] = fetch_if<ALIGNED, T, V>(dy + a * p.dy.ts, ok, k.count);
+            }
+#pragma unroll
+            for (int a = 0; a < kGradAhead; ++a)
+                if (a < count)
+                    token(std::true_type(), t + a, vx[a], vy[a]);
+            x += count * p.x.ts, dy += count * p.dy.ts;
+        };
+        long long t = s.t0;
+        int count = W - 1;                                           // not above kGradAhead
+        for (;;) {
+            edge(t, count);
+            t += count;
+            for (; t + kGradAhead <= s.t1; t += kGradAhead) {
+                Vec<T, V> vx[kGradAhead], vy[kGradAhead];
+#pragma unroll
+                for (int a = 0; a < kGradAhead; ++a, x += p.x.ts, dy += p.dy.ts) {
+                    vx[a] = fetch<ALIGNED, T, V>(x, k.count);
+                    vy[a] = fetch<ALIGNED, T, V>(dy, k.count);
+                }
+#pragma unroll
+                for (int a = 0; a < kGradAhead; ++a)
+                    token(std::false_type(), t + a, vx[a], vy[a]);
+            }
+            if (t >= stop)
+                break;
+            count = stop - t < kGradAhead ? static_cast<int>(stop - t) : kGradAhead;
         }
-        for (; t < stop; ++t)
-            any(t);
     });
     if (p.part) {
         float* to = p.part + (long long)blockIdx.x * (W + 1) * p.d + c;
 #pragma unroll
         for (int j = 0; j <= W; ++j)
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                to[(long long)j * p.d + i] = j < W ? dw[j][i] : db[i];
+            for (int i = 0; i < V / 2; ++i) {
+                float a, b;
+                unpack2(j < W ? dw[j][i] : db[i], a, b);
+                to[(long long)j * p.d + 2 * i] = a;
+                if (2 * i + 1 < k.count)
+                    to[(long long)j * p.d + 2 * i + 1] = b;
+            }
     }
 }
 
