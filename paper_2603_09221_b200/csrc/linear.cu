@@ -85,15 +85,23 @@ struct Product {
     float* part;
 };
 
-// Width of a tile and parts of the contraction.  The wide tile reads least per product (its operands are 192 bytes of shared
-// memory for every 256 of a 128 x 128 tile's); narrower ones, and then parts of the contraction (at least 512 indices
-// each, summed by a launch of its own), are for results with fewer tiles than there are SMs.
+// Width of a tile and parts of the contraction.  A block of 64 contraction indices takes about 400 + 1.75 BN clocks: filling
+// and reading its (128 + BN) x 128 bytes of shared memory, twice 128 + BN clocks, and what goes with it; so the width is the
+// one with the least of that times the rounds of tiles over the SMs (512 x 4096 results over 2048 indices: 64 wide 21.9 us in two
+// rounds, 128 wide in one 15).  Results with few tiles split the contraction too, in parts of at least 512 indices that a
+// launch of its own sums.
 Product plan_product(int64_t M, int64_t N, int64_t K, int sms, Scratch& s)
 {
     Product p{M, N, K, 256, 1, nullptr};
     const int64_t tm = (M + BM - 1) / BM;
-    while (p.bn > 64 && tm * ((N + p.bn - 1) / p.bn) < sms)
-        p.bn /= 2;
+    int64_t least = INT64_MAX;
+    for (int bn = 256; bn >= 64; bn /= 2) {
+        const int64_t rounds = (tm * ((N + bn - 1) / bn) + sms - 1) / sms, cost = rounds * (1600 + 7 * bn);
+        if (cost < least) {
+            least = cost;
+            p.bn = bn;
+        }
+    }
     const int64_t tiles = tm * ((N + p.bn - 1) / p.bn);
     if (2 * tiles <= sms) {
         int64_t most = K / 512, want = sms / tiles;

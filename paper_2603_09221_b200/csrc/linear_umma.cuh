@@ -1,7 +1,7 @@
 // Matrix products of the projections on the 5th-generation tensor cores: D[i][j] = sum_k A(i, k) B(j, k), with what is to
 // be done to a product before it is written (bias, activation, residual) done on the accumulators.
 //
-// One CTA per SM works through tiles of 128 x BN.  One thread keeps a ring of stages of 64 contraction indices filled by TMA
+// One CTA per SM works through tiles of 128 x BN.  One warp keeps a ring of stages of 64 contraction indices filled by TMA
 // (128-byte swizzle), one issues tcgen05.mma (cta_group::1, kind::f16) into one of two accumulators in tensor memory, and
 // eight warps read the other one back, so that the end of a tile runs beside the products of the next.  Operands are read as
 // they lie in memory: an operand whose contraction index is not the contiguous one (the gradients') is staged in boxes of
@@ -68,6 +68,13 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, volatile int
     *dead = 1;
     g_error = 1;
     return false;
+}
+// true in one lane of the (converged) warp
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t pred;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(pred));
+    return pred != 0;
 }
 __device__ __forceinline__ void drain(uint32_t bar, uint32_t parity)
 {
@@ -252,7 +259,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint32_t tmem = *s_tmem;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
 
     const int per_split = p.tiles_m * p.tiles_n, tiles = per_split * p.splits;
     // Tiles of eight rows of tiles follow one another column by column, so that the CTAs at work share operands in L2.
@@ -266,18 +273,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         return split;
     };
 
+    // Both issuing warps walk their loops as a whole and elect a lane for the instruction itself: what it is given then comes
+    // from uniform registers (from one lane's own registers the products of a stage took 500 clocks to issue).
+    const uint32_t stages = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
     if (warp == 0) {
-        if (lane == 0) {
-            unsigned it = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
-                int mt, nt, k0, k1;
-                place(tile, mt, nt, k0, k1);
-                for (int k = k0; k < k1; ++k, ++it) {
-                    const int s = it % STAGES;
-                    if (!(ok = wait(empty + 8 * s, (it / STAGES & 1) ^ 1, dead)))
-                        break;
-                    const uint32_t bar = full + 8 * s, a = smem_u32(smem + s * S::STAGE_BYTES), b = a + S::A_BYTES;
+        unsigned it = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+            int mt, nt, k0, k1;
+            place(tile, mt, nt, k0, k1);
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % STAGES;
+                if (!(ok = wait(empty + 8 * s, (it / STAGES & 1) ^ 1, dead)))
+                    break;
+                const uint32_t bar = full + 8 * s, a = stages + s * S::STAGE_BYTES, b = a + S::A_BYTES;
+                if (elect_one()) {
                     expect_bytes(bar, S::STAGE_BYTES);
                     if (A_MN) {
 #pragma unroll
@@ -294,41 +304,45 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                         tma_load(b, &map_b, k * BK, nt * BN, bar);
                     }
                 }
+                __syncwarp();
             }
-            if (!ok)                                                 // copies under way end before the CTA does
-                for (unsigned i = it > STAGES ? it - STAGES : 0; i < it; ++i)
-                    drain(full + 8 * (i % STAGES), i / STAGES & 1);
         }
+        if (!ok)                                                     // copies under way end before the CTA does
+            for (unsigned i = it > STAGES ? it - STAGES : 0; i < it; ++i)
+                drain(full + 8 * (i % STAGES), i / STAGES & 1);
     } else if (warp == 1) {
-        if (lane == 0) {
-            unsigned it = 0, done = 0;
-            bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++done) {
-                int mt, nt, k0, k1;
-                place(tile, mt, nt, k0, k1);
-                const uint32_t d = tmem + (done & 1) * BN;
-                if (!(ok = wait(acc_empty + 8 * (done & 1), (done / 2 & 1) ^ 1, dead)))
+        unsigned it = 0, done = 0;
+        bool ok = true;
+        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++done) {
+            int mt, nt, k0, k1;
+            place(tile, mt, nt, k0, k1);
+            const uint32_t d = tmem + (done & 1) * BN;
+            if (!(ok = wait(acc_empty + 8 * (done & 1), (done / 2 & 1) ^ 1, dead)))
+                break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            for (int k = k0; k < k1; ++k, ++it) {
+                const int s = it % STAGES;
+                if (!(ok = wait(full + 8 * s, it / STAGES & 1, dead)))
                     break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (int k = k0; k < k1; ++k, ++it) {
-                    const int s = it % STAGES;
-                    if (!(ok = wait(full + 8 * s, it / STAGES & 1, dead)))
-                        break;
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t a = smem_u32(smem + s * S::STAGE_BYTES), b = a + S::A_BYTES;
+                const uint32_t a = stages + s * S::STAGE_BYTES, b = a + S::A_BYTES;
+                const uint64_t da = operand_desc<A_MN>(a), db = operand_desc<B_MN>(b);
+                if (elect_one()) {
 #pragma unroll
                     for (int j = 0; j < BK / 16; ++j)
-                        mma(d, operand_desc<A_MN>(a + j * (A_MN ? 2048 : 32)), operand_desc<B_MN>(b + j * (B_MN ? 2048 : 32)), p.idesc,
-                            k > k0 || j > 0);
+                        mma(d, da + j * ((A_MN ? 2048 : 32) >> 4), db + j * ((B_MN ? 2048 : 32) >> 4), p.idesc, k > k0 || j > 0);
                     commit(empty + 8 * s);
+                    if (k + 1 == k1)
+                        commit(acc_full + 8 * (done & 1));
                 }
-                if (ok)
-                    commit(acc_full + 8 * (done & 1));
+                __syncwarp();
             }
-            if (!ok) {                                               // products under way end before tensor memory is given back
+        }
+        if (!ok) {                                                   // products under way end before tensor memory is given back
+            if (elect_one())
                 commit(drained);
-                drain(drained, 0);
-            }
+            __syncwarp();
+            drain(drained, 0);
         }
     } else {
         const int w = warp - 2, quarter = warp % 4, half = w / 4;    // a warp reads the lanes of its quarter of tensor memory
