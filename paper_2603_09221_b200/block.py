@@ -17,10 +17,14 @@ the channels have to be contiguous.
 from __future__ import annotations
 
 import ctypes
+import os
 import struct
+import subprocess
+import warnings
 
 import torch
 
+from . import build as _build
 from . import lqr as _lqr
 from .lqr import TTC_BF16, TTC_F32, TtcError, _check, _raw_stream  # noqa: F401
 
@@ -50,8 +54,11 @@ _NO_ROWS = (0, 0, 0)
 _lib = None
 
 
+_step = None                    # the compiled short way into the calls for single tokens, bound to the library when it is loaded
+
+
 def _load():
-    global _lib
+    global _lib, _step
     if _lib is None:
         lib = _lqr.load_library()
         p, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
@@ -68,8 +75,26 @@ def _load():
                 f.argtypes = [i32, p, p]
             else:
                 f.argtypes = [i32, p] + grads + [p, i64, p]
-        _lib = lib
+        _lib, _step = lib, _short_way(lib)
     return _lib
+
+
+class _LongWay:
+    """Stands in for the compiled module where it cannot be built: every call is marshalled here."""
+    conv_step = scan_step = linear = staticmethod(lambda *args: None)
+
+
+def _short_way(lib):
+    try:
+        if not os.path.exists(_build.STEP) or os.environ.get("TTC_LQR_REBUILD"):
+            _build.build_step_binding(force=True)
+        from . import _step as step
+    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        warnings.warn("single-token calls take the slower way through Python: %s" % e)
+        return _LongWay
+    step.bind(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
+                for k in ("ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_linear", "ttc_linear_workspace")))
+    return step
 
 
 def _type_of(t, f32=True):
@@ -251,6 +276,12 @@ def causal_conv(x, w, bias=None, act="none", state=None, offsets=None, y=None, s
 
 def causal_conv_step(x, w, state, bias=None, act="none", y=None, stream=None):
     """One token of each sequence, ``x [batch, channels]``: as :func:`causal_conv`; ``state`` moves on in place."""
+    if stream is None:
+        if _step is None:
+            _load()
+        got = _step.conv_step(x, w, state, bias, ACTIVATIONS.get(act, -1), y)
+        if got is not None:
+            return got
     if y is None:
         y = _like(x, stream)
     if x.dim() != 2:
@@ -339,6 +370,12 @@ def selective_scan(x, delta, A, B, C, D=None, z=None, delta_bias=None, softplus=
 
 def selective_scan_step(x, delta, A, B, C, state, D=None, z=None, delta_bias=None, softplus=False, y=None, stream=None):
     """One token of each sequence, ``x [batch, channels]``: as :func:`selective_scan`; ``state`` moves on in place."""
+    if stream is None:
+        if _step is None:
+            _load()
+        got = _step.scan_step(x, delta, A, B, C, state, D, z, delta_bias, softplus, y)
+        if got is not None:
+            return got
     if y is None:
         y = _like(x, stream)
     if x.dim() != 2:
@@ -425,6 +462,12 @@ def linear(x, w, bias=None, act="none", residual=None, y=None, pre=None, out_dty
     dtype, dev = x.dtype, x.get_device()
     if out_dtype is None:
         out_dtype = y.dtype if y is not None else dtype
+    if stream is None and pre is None and (out_dtype is dtype or out_dtype is _F32):
+        if _step is None:
+            _load()
+        got = _step.linear(x, w, bias, ACTIVATIONS.get(act, -1), residual, y, out_dtype is _F32)
+        if got is not None:
+            return got
     code, a = _type_of(x, False), ACTIVATIONS.get(act)
     if a is None:
         raise ValueError("unknown activation %r" % (act,))

@@ -9,6 +9,7 @@ import tempfile
 _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libttc_lqr.so")
+STEP = os.path.join(_HERE, "_step.so")
 NVCC_FLAGS = [
     "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
     "-Xcompiler", "-fPIC",
@@ -19,10 +20,10 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
-def _stale():
-    if not os.path.exists(LIB):
+def _stale(artefact=LIB):
+    if not os.path.exists(artefact):
         return True
-    t = os.path.getmtime(LIB)
+    t = os.path.getmtime(artefact)
     deps = glob.glob(os.path.join(CSRC, "*")) + glob.glob(os.path.join(_HERE, "..", "include", "*.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -42,3 +43,22 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
                 raise failed[0]
             subprocess.run(nvcc + ["-shared", "-o", LIB] + objects, check=True)
     return LIB
+
+
+def step_command():
+    """The compiler's call for ``_step.so`` (``csrc/step_binding.cpp``): a Python module against torch's own headers and libraries."""
+    import sysconfig
+    import torch
+    root = os.path.dirname(torch.__file__)
+    inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+           os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
+    cmd += ["-isystem" + i for i in inc] + ["-o", STEP, os.path.join(CSRC, "step_binding.cpp"), "-L" + os.path.join(root, "lib")]
+    return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
+
+
+def build_step_binding(force: bool = False) -> str:
+    """Compile ``_step.so``, the short way into the calls for single tokens."""
+    if force or _stale(STEP):
+        subprocess.run(step_command(), check=True)
+    return STEP

@@ -82,29 +82,39 @@ int copy_operand(const Aligned& a, cudaStream_t st)
 struct Product {
     int64_t M, N, K;
     int bn, splits;
+    bool pair;                   // two CTAs on tiles of 256 x 256
     float* part;
 };
+
+constexpr int64_t kPairCost = 3050, kSegment = 512, kLong = 1024;
 
 // Width of a tile and parts of the contraction.  A block of 64 contraction indices takes about 400 + 1.75 BN clocks: filling
 // and reading its (128 + BN) x 128 bytes of shared memory, twice 128 + BN clocks, and what goes with it; so the width is the
 // one with the least of that times the rounds of tiles over the SMs (512 x 4096 results over 2048 indices: 64 wide 21.9 us in two
 // rounds, 128 wide in one 15).  Results with few tiles split the contraction too, in parts of at least 512 indices that a
 // launch of its own sums.
-Product plan_product(int64_t M, int64_t N, int64_t K, int sms, Scratch& s)
+Product plan_product(int64_t M, int64_t N, int64_t K, bool f32, int sms, Scratch& s)
 {
-    Product p{M, N, K, 256, 1, nullptr};
+    Product p{M, N, K, 256, 1, false, nullptr};
     const int64_t tm = (M + BM - 1) / BM;
     int64_t least = INT64_MAX;
-    for (int bn = 256; bn >= 64; bn /= 2) {
+    const bool exact = f32 && K > kLong;      // float32 results of a long contraction: segments, which the 128 wide tile has
+    for (int bn = exact ? 128 : 256; bn >= (exact ? 128 : 64); bn /= 2) {
         const int64_t rounds = (tm * ((N + bn - 1) / bn) + sms - 1) / sms, cost = rounds * (1600 + 7 * bn);
         if (cost < least) {
             least = cost;
             p.bn = bn;
         }
     }
+    const int64_t pairs = sms / 2, rounds = ((M + 2 * BM - 1) / (2 * BM) * ((N + 255) / 256) + pairs - 1) / pairs;
+    if (!exact && rounds * kPairCost < least) {
+        p.pair = true;
+        p.bn = 256;
+        return p;
+    }
     const int64_t tiles = tm * ((N + p.bn - 1) / p.bn);
     if (2 * tiles <= sms) {
-        int64_t most = K / 512, want = sms / tiles;
+        const int64_t most = K / 512, want = sms / tiles;
         p.splits = (int)(want < most ? want : most);
         if (p.splits < 2)
             p.splits = 1;
@@ -114,17 +124,29 @@ Product plan_product(int64_t M, int64_t N, int64_t K, int sms, Scratch& s)
     return p;
 }
 
-template <bool A_MN, bool B_MN, int BN, typename OT> int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool is_bf16, int sms, cudaStream_t st)
+template <bool A_MN, bool B_MN, int BN, bool PAIR, typename OT> int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool is_bf16, int sms, cudaStream_t st)
 {
-    using S = GemmShape<BN>;
-    auto* kernel = gemm_kernel<A_MN, B_MN, BN, OT>;
+    using S = GemmShape<BN, PAIR>;
+    constexpr int CTAS = PAIR ? 2 : 1;
+    auto* kernel = gemm_kernel<A_MN, B_MN, BN, PAIR, OT>;
     TTC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
-    g.tiles_m = (int)((g.M + BM - 1) / BM);
+    g.tiles_m = (int)((g.M + CTAS * BM - 1) / (CTAS * BM));
     g.tiles_n = (int)((g.N + BN - 1) / BN);
-    g.idesc = instruction(is_bf16, A_MN, B_MN, BN);
-    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n * g.splits;
-    kernel<<<(unsigned)(tiles < sms ? tiles : sms), kGemmThreads, S::SMEM, st>>>(ma, mb, g);
-    return launched("matrix product");
+    g.idesc = instruction(is_bf16, A_MN, B_MN, CTAS * BM, BN);
+    const int64_t tiles = (int64_t)g.tiles_m * g.tiles_n * g.splits, most = sms / CTAS;
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3((unsigned)(CTAS * (tiles < most ? tiles : most)));
+    c.blockDim = dim3(kGemmThreads);
+    c.dynamicSmemBytes = S::SMEM;
+    c.stream = st;
+    cudaLaunchAttribute cluster;
+    cluster.id = cudaLaunchAttributeClusterDimension;
+    cluster.val.clusterDim.x = CTAS;
+    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
+    c.attrs = &cluster;
+    c.numAttrs = PAIR ? 1 : 0;
+    const cudaError_t e = cudaLaunchKernelEx(&c, kernel, ma, mb, g);
+    return e == cudaSuccess ? launched("matrix product") : fail(TTC_STATUS_CUDA_ERROR, "matrix product: %s", cudaGetErrorString(e));
 }
 
 // D = A B' with A [M][K] (or [K][M] with A_MN) and B likewise, and the epilogue on it.
@@ -132,12 +154,13 @@ template <bool A_MN, bool B_MN> int product(const Product& q, const Operand& a, 
 {
     CUtensorMap ma, mb;
     TTC_TRY(encode(ma, a.ptr, a.rows, a.cols, a.ld, A_MN ? BK : BM, is_bf16));
-    TTC_TRY(encode(mb, b.ptr, b.rows, b.cols, b.ld, B_MN ? BK : q.bn, is_bf16));
+    TTC_TRY(encode(mb, b.ptr, b.rows, b.cols, b.ld, B_MN ? BK : q.pair ? q.bn / 2 : q.bn, is_bf16));
     GemmDev g = {};
     g.M = q.M;
     g.N = q.N;
     g.k_blocks = (int)((q.K + BK - 1) / BK);
     g.splits = q.splits;
+    g.segment = kSegment / BK;
     g.e = e;
     if (q.splits > 1) {
         g.e = Epilogue{};
@@ -149,10 +172,12 @@ template <bool A_MN, bool B_MN> int product(const Product& q, const Operand& a, 
     const int type = q.splits > 1 ? (int)TTC_F32 : out_dtype;
     TTC_TRY(by_type(type, [&](auto t) {
         using OT = decltype(t);
+        if (q.pair)
+            return launch_tiles<A_MN, B_MN, 256, true, OT>(ma, mb, g, is_bf16, sms, st);
         switch (q.bn) {
-        case 256: return launch_tiles<A_MN, B_MN, 256, OT>(ma, mb, g, is_bf16, sms, st);
-        case 128: return launch_tiles<A_MN, B_MN, 128, OT>(ma, mb, g, is_bf16, sms, st);
-        default: return launch_tiles<A_MN, B_MN, 64, OT>(ma, mb, g, is_bf16, sms, st);
+        case 256: return launch_tiles<A_MN, B_MN, 256, false, OT>(ma, mb, g, is_bf16, sms, st);
+        case 128: return launch_tiles<A_MN, B_MN, 128, false, OT>(ma, mb, g, is_bf16, sms, st);
+        default: return launch_tiles<A_MN, B_MN, 64, false, OT>(ma, mb, g, is_bf16, sms, st);
         }
     }));
     if (q.splits == 1)
@@ -213,7 +238,7 @@ int plan_linear(int device, const ttc_linear_args* a, void* ws, LinearPlan& o)
     if (!o.few) {
         o.x = plan_operand(o.x.from, s);
         o.w = plan_operand(o.w.from, s);
-        o.q = plan_product(a->rows, a->m, a->k, sm_count(device), s);
+        o.q = plan_product(a->rows, a->m, a->k, a->out_dtype == TTC_F32, sm_count(device), s);
     }
     o.bytes = s.used;
     return TTC_OK;
@@ -283,9 +308,9 @@ int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, v
     // the two products run one behind the other and share the room for parts
     Scratch s1 = s, s2 = s;
     if (g->dx)
-        o.qx = plan_product(a->rows, a->k, a->m, sms, s1);
+        o.qx = plan_product(a->rows, a->k, a->m, false, sms, s1);
     if (g->dw)
-        o.qw = plan_product(a->m, a->k, a->rows, sms, s2);
+        o.qw = plan_product(a->m, a->k, a->rows, false, sms, s2);
     o.bytes = s1.used > s2.used ? s1.used : s2.used;
     return TTC_OK;
 }

@@ -1,8 +1,10 @@
 // Matrix products of the projections on the 5th-generation tensor cores: D[i][j] = sum_k A(i, k) B(j, k), with what is to
 // be done to a product before it is written (bias, activation, residual) done on the accumulators.
 //
-// One CTA per SM works through tiles of 128 x BN.  One warp keeps a ring of stages of 64 contraction indices filled by TMA
-// (128-byte swizzle), one issues tcgen05.mma (cta_group::1, kind::f16) into one of two accumulators in tensor memory, and
+// One CTA per SM works through tiles of 128 x BN, or, where there are enough of them, two neighbouring ones through tiles of
+// 256 x 256 (cta_group::2): each then fetches and reads 64 KB of shared memory for a block of 64 contraction indices instead
+// of 96, which is what bounds a single CTA (128 bytes per clock: 768 clocks against 512 of products).  One warp keeps a ring of stages of 64 contraction indices filled by TMA
+// (128-byte swizzle), one issues tcgen05.mma (kind::f16) into one of two accumulators in tensor memory, and
 // eight warps read the other one back, so that the end of a tile runs beside the products of the next.  Operands are read as
 // they lie in memory: an operand whose contraction index is not the contiguous one (the gradients') is staged in boxes of
 // 64 contiguous rows by 64 contraction indices and described to the instruction as MN-major; nothing is transposed.
@@ -42,6 +44,7 @@ struct GemmDev {
     long long M, N;
     int k_blocks;                // blocks of BK contraction indices in all
     int splits;                  // parts of the contraction, each a tile of its own
+    int segment;                 // float32 results: blocks of BK that the tensor cores add up before the sum goes to registers
     int tiles_m, tiles_n;
     uint32_t idesc;
     Epilogue e;
@@ -91,6 +94,37 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+// ---- two CTAs of a cluster on one tile (cta_group::2) ----
+// The same barrier of the pair's first CTA.
+__device__ __forceinline__ uint32_t in_first(uint32_t bar)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+    return r;
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" :: "r"(bar), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}\n"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
 __device__ __forceinline__ void commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
@@ -127,10 +161,10 @@ template <bool MN> __device__ __forceinline__ uint64_t operand_desc(uint32_t at)
 }
 
 // Instruction descriptor: float32 accumulators, both operands bfloat16 or both float16.
-inline uint32_t instruction(bool is_bf16, bool a_mn, bool b_mn, int bn)
+inline uint32_t instruction(bool is_bf16, bool a_mn, bool b_mn, int bm, int bn)
 {
     const uint32_t f = is_bf16 ? 1 : 0;
-    return 1u << 4 | f << 7 | f << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(BM >> 4) << 24;
+    return 1u << 4 | f << 7 | f << 10 | (uint32_t)a_mn << 15 | (uint32_t)b_mn << 16 | (uint32_t)(bn >> 3) << 17 | (uint32_t)(bm >> 4) << 24;
 }
 
 // Activations of 32 results; the choice lies outside of the loop.
@@ -217,19 +251,24 @@ __device__ __forceinline__ void store_chunk(const float (&v)[32], OT* at, long l
     }
 }
 
-template <int BN> struct GemmShape {
-    static constexpr int STAGES = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+// PAIR: two CTAs on a tile of 256 x BN, each with half of the rows of either operand and half of the results.
+template <int BN, bool PAIR> struct GemmShape {
+    static constexpr int B_ROWS = PAIR ? BN / 2 : BN;
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = B_ROWS * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+    static constexpr int STAGES = 196608 / STAGE_BYTES;
     static constexpr int EPI_BYTES = kEpilogueWarps * (32 * kStageRow + 128 * 4);
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + 256;
 };
 
-template <bool A_MN, bool B_MN, int BN, typename OT>
+template <bool A_MN, bool B_MN, int BN, bool PAIR, typename OT>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                               const GemmDev p)
 {
-    using S = GemmShape<BN>;
-    constexpr int STAGES = S::STAGES;
+    using S = GemmShape<BN, PAIR>;
+    constexpr int STAGES = S::STAGES, CTAS = PAIR ? 2 : 1;
+    // The tensor cores cut sums off instead of rounding them, an error that grows with the contraction (1.0e-6 of the result's
+    // norm at 1024 indices): float32 results of longer ones are added up in registers, segment by segment.
+    constexpr bool SEGMENTS = sizeof(OT) == 4 && BN == 128 && !PAIR;
     extern __shared__ char smem_raw[];
     char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) / 1024 * 1024);
     char* s_epi = smem + STAGES * S::STAGE_BYTES;
@@ -240,12 +279,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     volatile int* dead = reinterpret_cast<volatile int*>(s_tmem + 1);
 
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const int rank = PAIR ? blockIdx.x % 2 : 0;                      // in the cluster
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2 * STAGES; ++i)
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(full + 8 * i) : "memory");
         for (int i = 0; i < 2; ++i) {
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(acc_full + 8 * i) : "memory");
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(acc_empty + 8 * i), "r"(kEpilogueWarps) : "memory");
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(acc_empty + 8 * i), "r"(CTAS * kEpilogueWarps) : "memory");
         }
         asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(drained) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -253,11 +293,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         *dead = 0;
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(s_tmem)), "r"(2 * BN) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if (PAIR) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(s_tmem)), "r"(2 * BN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(s_tmem)), "r"(2 * BN) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
     }
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    __syncwarp();
+    if (PAIR)
+        cluster_sync();                                              // the other CTA's barriers and tensor memory are there
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
 
@@ -273,13 +321,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         return split;
     };
 
+    const int first_tile = blockIdx.x / CTAS, tile_step = gridDim.x / CTAS;
     // Both issuing warps walk their loops as a whole and elect a lane for the instruction itself: what it is given then comes
     // from uniform registers (from one lane's own registers the products of a stage took 500 clocks to issue).
     const uint32_t stages = __shfl_sync(0xffffffffu, smem_u32(smem), 0);
     if (warp == 0) {
         unsigned it = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x) {
+        for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
             int mt, nt, k0, k1;
             place(tile, mt, nt, k0, k1);
             for (int k = k0; k < k1; ++k, ++it) {
@@ -287,90 +336,157 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                 if (!(ok = wait(empty + 8 * s, (it / STAGES & 1) ^ 1, dead)))
                     break;
                 const uint32_t bar = full + 8 * s, a = stages + s * S::STAGE_BYTES, b = a + S::A_BYTES;
+                // rows of the operands that this CTA fetches; a pair's copies all count on the first CTA's barrier
+                const int ra = (mt * CTAS + rank) * BM, rb = nt * BN + rank * S::B_ROWS;
+                const uint32_t counted = PAIR ? in_first(bar) : bar;
+                auto fetch = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
+                    if (PAIR)
+                        tma_load_pair(to, map, x, y, counted);
+                    else
+                        tma_load(to, map, x, y, counted);
+                };
                 if (elect_one()) {
-                    expect_bytes(bar, S::STAGE_BYTES);
+                    if (rank == 0)
+                        expect_bytes(bar, CTAS * S::STAGE_BYTES);
                     if (A_MN) {
 #pragma unroll
                         for (int i = 0; i < BM / 64; ++i)
-                            tma_load(a + i * 8192, &map_a, mt * BM + i * 64, k * BK, bar);
+                            fetch(a + i * 8192, &map_a, ra + i * 64, k * BK);
                     } else {
-                        tma_load(a, &map_a, k * BK, mt * BM, bar);
+                        fetch(a, &map_a, k * BK, ra);
                     }
                     if (B_MN) {
 #pragma unroll
-                        for (int i = 0; i < BN / 64; ++i)
-                            tma_load(b + i * 8192, &map_b, nt * BN + i * 64, k * BK, bar);
+                        for (int i = 0; i < S::B_ROWS / 64; ++i)
+                            fetch(b + i * 8192, &map_b, rb + i * 64, k * BK);
                     } else {
-                        tma_load(b, &map_b, k * BK, nt * BN, bar);
+                        fetch(b, &map_b, k * BK, rb);
                     }
                 }
                 __syncwarp();
             }
         }
-        if (!ok)                                                     // copies under way end before the CTA does
-            for (unsigned i = it > STAGES ? it - STAGES : 0; i < it; ++i)
-                drain(full + 8 * (i % STAGES), i / STAGES & 1);
-    } else if (warp == 1) {
+        if (!ok) {                                                   // copies under way end before the CTA does
+            if (rank == 0) {
+                for (unsigned i = it > STAGES ? it - STAGES : 0; i < it; ++i)
+                    drain(full + 8 * (i % STAGES), i / STAGES & 1);
+            } else {                                                 // theirs count on a barrier that only the first CTA can look at
+                for (int i = 0; i < 1000; ++i)
+                    __nanosleep(1000);
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
         unsigned it = 0, done = 0;
         bool ok = true;
-        for (int tile = blockIdx.x; ok && tile < tiles; tile += gridDim.x, ++done) {
-            int mt, nt, k0, k1;
-            place(tile, mt, nt, k0, k1);
-            const uint32_t d = tmem + (done & 1) * BN;
-            if (!(ok = wait(acc_empty + 8 * (done & 1), (done / 2 & 1) ^ 1, dead)))
-                break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            for (int k = k0; k < k1; ++k, ++it) {
-                const int s = it % STAGES;
-                if (!(ok = wait(full + 8 * s, it / STAGES & 1, dead)))
+        for (int tile = first_tile; ok && tile < tiles; tile += tile_step) {
+            int mt, nt, begin, end;
+            place(tile, mt, nt, begin, end);
+            for (int k0 = begin; ok && k0 < end; ++done) {
+                const int k1 = SEGMENTS ? min(end, k0 + p.segment) : end;
+                const uint32_t d = tmem + (done & 1) * BN;
+                if (!(ok = wait(acc_empty + 8 * (done & 1), (done / 2 & 1) ^ 1, dead)))
                     break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                const uint32_t a = stages + s * S::STAGE_BYTES, b = a + S::A_BYTES;
-                const uint64_t da = operand_desc<A_MN>(a), db = operand_desc<B_MN>(b);
-                if (elect_one()) {
+                for (int k = k0; k < k1; ++k, ++it) {
+                    const int s = it % STAGES;
+                    if (!(ok = wait(full + 8 * s, it / STAGES & 1, dead)))
+                        break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t a = stages + s * S::STAGE_BYTES, b = a + S::A_BYTES;
+                    const uint64_t da = operand_desc<A_MN>(a), db = operand_desc<B_MN>(b);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int j = 0; j < BK / 16; ++j)
-                        mma(d, da + j * ((A_MN ? 2048 : 32) >> 4), db + j * ((B_MN ? 2048 : 32) >> 4), p.idesc, k > k0 || j > 0);
-                    commit(empty + 8 * s);
-                    if (k + 1 == k1)
-                        commit(acc_full + 8 * (done & 1));
+                        for (int j = 0; j < BK / 16; ++j)
+                            if (PAIR)
+                                mma_pair(d, da + j * ((A_MN ? 2048 : 32) >> 4), db + j * ((B_MN ? 2048 : 32) >> 4), p.idesc, k > k0 || j > 0);
+                            else
+                                mma(d, da + j * ((A_MN ? 2048 : 32) >> 4), db + j * ((B_MN ? 2048 : 32) >> 4), p.idesc, k > k0 || j > 0);
+                        if (PAIR) {
+                            commit_pair(empty + 8 * s);
+                            if (k + 1 == k1)
+                                commit_pair(acc_full + 8 * (done & 1));
+                        } else {
+                            commit(empty + 8 * s);
+                            if (k + 1 == k1)
+                                commit(acc_full + 8 * (done & 1));
+                        }
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                k0 = k1;
             }
         }
         if (!ok) {                                                   // products under way end before tensor memory is given back
-            if (elect_one())
-                commit(drained);
+            if (elect_one()) {
+                if (PAIR)
+                    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(drained) : "memory");
+                else
+                    commit(drained);
+            }
             __syncwarp();
             drain(drained, 0);
         }
-    } else {
+    } else if (warp >= 2) {
         const int w = warp - 2, quarter = warp % 4, half = w / 4;    // a warp reads the lanes of its quarter of tensor memory
         char* stage = s_epi + w * (32 * kStageRow + 128 * 4);
         float* s_bias = reinterpret_cast<float*>(stage + 32 * kStageRow);
         unsigned done = 0;
-        for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x, ++done) {
+        for (int tile = first_tile; tile < tiles; tile += tile_step, done += SEGMENTS ? 0 : 1) {
             int mt, nt, k0, k1;
             const int split = place(tile, mt, nt, k0, k1);
-            const long long row0 = (long long)mt * BM + quarter * 32, col0 = (long long)nt * BN + half * (BN / 2);
+            const long long row0 = ((long long)mt * CTAS + rank) * BM + quarter * 32, col0 = (long long)nt * BN + half * (BN / 2);
             __syncwarp();
             for (int c = lane; c < BN / 2; c += 32)
                 s_bias[c] = p.e.bias && col0 + c < p.N ? p.e.bias[col0 + c] : 0.f;
             __syncwarp();
-            if (!wait(acc_full + 8 * (done & 1), done / 2 & 1, dead))
-                break;
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t from = tmem + (done & 1) * BN + half * (BN / 2) + ((uint32_t)(quarter * 32) << 16);
-            OT* out = static_cast<OT*>(p.e.out) + split * p.e.split_stride;
-#pragma unroll 1
-            for (int c = 0; c < BN / 2; c += 32) {
-                float v[32];
-                tmem_ld32(from + c, v);
-                if (c + 32 == BN / 2) {
+            bool ok = true;
+            float sum[SEGMENTS ? BN / 64 : 1][32];
+            if (SEGMENTS) {
+                for (int k = k0; ok && k < k1; k += p.segment, ++done) {
+                    if (!(ok = wait(acc_full + 8 * (done & 1), done / 2 & 1, dead)))
+                        break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t from = tmem + (done & 1) * BN + half * (BN / 2) + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+                    for (int c = 0; c < BN / 64; ++c) {
+                        float v[32];
+                        tmem_ld32(from + 32 * c, v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            sum[SEGMENTS ? c : 0][i] = k == k0 ? v[i] : sum[SEGMENTS ? c : 0][i] + v[i];
+                    }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0)
                         arrive(acc_empty + 8 * (done & 1));
+                }
+            } else {
+                ok = wait(acc_full + 8 * (done & 1), done / 2 & 1, dead);
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            }
+            if (!ok)
+                break;
+            const uint32_t from = tmem + (done & 1) * BN + half * (BN / 2) + ((uint32_t)(quarter * 32) << 16);
+            OT* out = static_cast<OT*>(p.e.out) + split * p.e.split_stride;
+#pragma unroll(SEGMENTS ? BN / 64 : 1)
+            for (int c = 0; c < BN / 2; c += 32) {
+                float v[32];
+                if (SEGMENTS) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        v[i] = sum[SEGMENTS ? c / 32 : 0][i];
+                } else {
+                    tmem_ld32(from + c, v);
+                }
+                if (!SEGMENTS && c + 32 == BN / 2) {
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (PAIR)
+                            arrive_cluster(in_first(acc_empty + 8 * (done & 1)));
+                        else
+                            arrive(acc_empty + 8 * (done & 1));
+                    }
                 }
                 const long long rows = p.M - row0, cols = p.N - (col0 + c);
                 if (rows <= 0 || cols <= 0)
@@ -401,8 +517,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
     __syncwarp();
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * BN) : "memory");
+    if (PAIR)
+        cluster_sync();                                              // neither CTA is signalled after it has ended
+    if (warp == 1) {
+        if (PAIR)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * BN) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(2 * BN) : "memory");
+    }
 }
 
 } // namespace lin

@@ -142,3 +142,55 @@ def test_control_layer_between_projections():
     want = u1.view(tokens, heads * n).to(H).double() @ w_out.double().t() + x.double()
     e = 2 * bu.U * 12 * (u1.view(tokens, heads * n).to(H).double().abs() @ w_out.double().abs().t()) + 2 * bu.U * want.abs()
     bu.within(y, f64(want), f64(e), H, "y")
+
+
+def _both(f):
+    """The same call by the compiled short way (current stream) and by the long one (a stream is named): the same bits."""
+    a = f(None)
+    b = f(torch.cuda.current_stream())
+    torch.cuda.synchronize()
+    return a, b
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+def test_both_ways_into_the_calls_for_single_tokens(dtype):
+    g = torch.Generator(device=DEV).manual_seed(4)
+    r = lambda *s, t=dtype: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+    batch, d, n = 5, 48, 16
+    wide = r(batch, 3 * d)
+    for x in (r(batch, d), wide[:, d:2 * d], wide[:, 1:d + 1]):
+        for bias in (None, r(d, t=F)):
+            w, state = r(d, 4, t=F), r(batch, 3, d)
+            states = [state.clone(), state.clone()]
+            a, b = _both(lambda s: block.causal_conv_step(x, w, states[s is not None], bias, act="silu", stream=s))
+            assert torch.equal(a, b) and torch.equal(*states)
+        for groups in (1, 2):
+            A, B, C, st = -r(d, n, t=F).abs(), r(batch, groups, n), r(batch, groups, n), r(batch, d, n, t=F)
+            states = [st.clone(), st.clone()]
+            out = [torch.empty_like(x), torch.empty_like(x)]
+            a, b = _both(lambda s: block.selective_scan_step(x, x, A, B, C, states[s is not None], z=x, softplus=True, y=out[s is not None], stream=s))
+            assert torch.equal(a, b) and torch.equal(*states) and a is out[0] and b is out[1]
+    if dtype is not F:
+        for rows, res in ((3, True), (200, False)):
+            x, w, bias = r(rows, 2 * d)[:, 3:d + 3], r(40, d), r(40, t=F)
+            a, b = _both(lambda s: block.linear(x, w, bias, act="gelu", residual=r_ if res else None, out_dtype=F, stream=s)
+                         if (r_ := torch.ones((rows, 40), device=DEV)) is not None else None)
+            assert torch.equal(a, b) and a.dtype == F
+
+
+def test_the_short_way_refuses_what_the_long_one_refuses():
+    x, w, state = torch.zeros((2, 8), device=DEV), torch.zeros((8, 4), device=DEV), torch.zeros((2, 3, 8), device=DEV)
+    for bad in (dict(w=w[:7]), dict(w=w.cpu()), dict(state=state[:, :2]), dict(state=state.half()), dict(act="tanh"), dict(x=x[0]), dict(bias=w),
+                dict(y=x[:1]), dict(x=x.double()), dict(act="gelu"), dict(w=torch.zeros((8, 5), device=DEV), state=torch.zeros((2, 4, 8), device=DEV))):
+        with pytest.raises((ValueError, TypeError, lqr.TtcError)):
+            block.causal_conv_step(**{**dict(x=x, w=w, state=state), **bad})
+    A, B, st = torch.zeros((8, 4), device=DEV), torch.zeros((2, 4), device=DEV), torch.zeros((2, 8, 4), device=DEV)
+    ok = dict(x=x, delta=x, A=A, B=B, C=B, state=st)
+    block.selective_scan_step(**ok)
+    for bad in (dict(A=A[:, :3]), dict(B=B[:1]), dict(C=B.half()), dict(state=st[0]), dict(z=x[:, :4]), dict(D=A), dict(x=x.t()), dict(delta=x.cpu())):
+        with pytest.raises((ValueError, TypeError, lqr.TtcError)):
+            block.selective_scan_step(**{**ok, **bad})
+    h = torch.zeros((2, 8), device=DEV, dtype=H)
+    for bad in (dict(w=h[:, :7]), dict(w=h.float()), dict(bias=x), dict(residual=h), dict(act="tanh"), dict(x=x), dict(out_dtype=torch.bfloat16), dict(y=h)):
+        with pytest.raises((ValueError, TypeError, lqr.TtcError)):
+            block.linear(**{**dict(x=h, w=torch.zeros((5, 8), device=DEV, dtype=H)), **bad})
