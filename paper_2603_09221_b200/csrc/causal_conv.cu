@@ -81,9 +81,8 @@ void set_tiles(ConvDev& p, int v, int sms)
     while (p.tile > 16 && seqs * ((p.seqs.tokens + p.tile - 1) / p.tile) * cols < 6 * (int64_t)sms)
         p.tile /= 2;
     p.tiles = (p.seqs.tokens + p.tile - 1) / p.tile;
+    p.all_tiles = seqs * p.tiles;
 }
-
-int64_t all_tiles(const ConvDev& p) { return p.tiles * (p.seqs.offsets ? 1 : p.seqs.batch); }
 
 template <bool WIDE, typename F> int by_shape(int dtype, const Width& w, int taps, F&& f)
 {
@@ -145,8 +144,10 @@ int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void*
     w.window(g->dstate_out);
     set_tiles(p, w.v, sm_count(device));
     o.params = g->dw || g->dbias;
+    if (g->dstate && a->batch > 8 * (int64_t)(kMaxGridY - 8))
+        return fail(TTC_STATUS_UNSUPPORTED, "gradients of %lld sequences", (long long)a->batch);
     Scratch s(ws);
-    float* part = s.take<float>(o.params ? (size_t)all_tiles(p) * (a->taps + 1) * a->d : 0);
+    float* part = s.take<float>(o.params ? (size_t)p.all_tiles * (a->taps + 1) * a->d : 0);
     p.part = o.params ? part : nullptr;
     o.bytes = s.used;
     return TTC_OK;
@@ -173,17 +174,22 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
     w.window(a->state);
     ConvDev p = to_dev(a, false);
     set_tiles(p, w.v, sm_count(device));
+    // any overlap of the windows in front and behind
+    const size_t bytes = (size_t)a->batch * (a->taps - 1) * a->d * element_size(a->dtype);
+    const char *s0 = static_cast<const char*>(a->state), *s1 = static_cast<const char*>(a->state_out);
+    const bool in_place = s0 && s1 && s0 < s1 + bytes && s1 < s0 + bytes;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return by_shape<false>(a->dtype, w, a->taps, [&](auto t, auto vc, auto ac, auto wc) {
         using T = decltype(t);
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
         constexpr bool ALIGNED = decltype(ac)::value;
-        if (a->tokens) {
-            const dim3 grid((unsigned)all_tiles(p), (a->d + V * kThreads - 1) / (V * kThreads));
+        const int64_t windows = a->state_out && !in_place ? a->batch : 0;
+        if (p.all_tiles + windows) {
+            const dim3 grid((unsigned)(p.all_tiles + windows), (a->d + V * kThreads - 1) / (V * kThreads));
             conv_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
             TTC_TRY(launched("causal convolution"));
         }
-        if (a->state_out) {
+        if (in_place) {
             const dim3 grid((unsigned)a->batch, (a->d + kThreads - 1) / kThreads);
             conv_window_kernel<T, W><<<grid, kThreads, 0, st>>>(p);
             TTC_TRY(launched("causal convolution, last windows"));
@@ -242,19 +248,16 @@ int ttc_causal_conv_grad(int32_t device, const ttc_conv_args* a, const ttc_conv_
         using T = decltype(t);
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
         constexpr bool ALIGNED = decltype(ac)::value;
-        const int64_t tiles = all_tiles(p);
-        if (tiles) {
-            const dim3 grid((unsigned)tiles, (a->d + V * kThreads - 1) / (V * kThreads));
+        if (p.all_tiles) {
+            const dim3 grid((unsigned)p.all_tiles, (a->d + V * kThreads - 1) / (V * kThreads));
             conv_grad_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
             TTC_TRY(launched("gradients of the causal convolution"));
         }
-        if (o.params) {
-            conv_param_kernel<W><<<dim3((a->d + 31) / 32, W + 1), 256, 0, st>>>(p, tiles);
+        // eight sequences to a block
+        const int64_t empties = p.dstate && (a->seq_offsets || a->tokens == 0) ? (a->batch + 7) / 8 : 0;
+        if (o.params || empties) {
+            conv_param_kernel<T, W><<<dim3((a->d + 31) / 32, (unsigned)(W + 1 + empties)), 256, 0, st>>>(p);
             TTC_TRY(launched("gradients of the causal convolution, parameters"));
-        }
-        if (p.dstate && a->batch && (a->seq_offsets || a->tokens == 0)) {
-            conv_empty_kernel<T, W><<<dim3((unsigned)a->batch, (a->d + kThreads - 1) / kThreads), kThreads, 0, st>>>(p);
-            TTC_TRY(launched("gradients of the causal convolution, empty sequences"));
         }
         return TTC_OK;
     });

@@ -25,6 +25,7 @@ struct ConvDev {
     int tile;                       // tokens of a tile
     int vec_w;                      // taps can be read by 16 bytes
     long long tiles;                // tiles of a sequence (equal) or of all rows (packed)
+    long long all_tiles;
     Rows x, y, dy, dx;
     const float *w, *bias;
     const void *state, *dstate_out;
@@ -186,10 +187,39 @@ __device__ __forceinline__ Vec<T, V> input_at(const ConvDev& p, const Segment& s
     return fetch_if<ALIGNED, T, V>(from, t >= 0 || p.state, count);
 }
 
+// The last W - 1 inputs of sequence `seq`, channel c.
+template <typename T, int W> __device__ __forceinline__ void keep_window(const ConvDev& p, long long seq, int c)
+{
+    const Span s = span_of(p.seqs, seq);
+    const Segment g{seq, s.row0, s.len, 0, 0};
+    T v[W - 1];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+        v[j] = input_at<true, T, 1, W>(p, g, s.len - (W - 1) + j, c, 1).v[0];
+#pragma unroll
+    for (int j = 0; j < W - 1; ++j)
+        static_cast<T*>(p.state_out)[(seq * (W - 1) + j) * p.d + c] = v[j];
+}
+// In a launch of its own where state_out is state, behind the one that reads the windows in front.
+template <typename T, int W> __global__ void __launch_bounds__(kThreads) conv_window_kernel(const ConvDev p)
+{
+    const int c = blockIdx.y * kThreads + threadIdx.x;
+    if (c < p.d)
+        keep_window<T, W>(p, blockIdx.x, c);
+}
+
+// Blocks past the tiles keep the last windows, one sequence each.
 template <typename T, int V, bool ALIGNED, int W>
 __global__ void __launch_bounds__(kThreads, 10) conv_kernel(const ConvDev p)
 {
     const int c = (blockIdx.y * kThreads + threadIdx.x) * V;
+    if (blockIdx.x >= p.all_tiles) {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (c + i < p.d)
+                keep_window<T, W>(p, blockIdx.x - p.all_tiles, c + i);
+        return;
+    }
     const long long from = first_sequence(p, blockIdx.x);
     if (c >= p.d)
         return;
@@ -226,24 +256,6 @@ __global__ void __launch_bounds__(kThreads, 10) conv_kernel(const ConvDev p)
         for (; left > 0; --left, x += p.x.ts)
             token(fetch<ALIGNED, T, V>(x, k.count));
     });
-}
-
-// The last W - 1 inputs of every sequence.  A launch of its own, behind the one that reads the windows in front: state_out may be state.
-template <typename T, int W>
-__global__ void __launch_bounds__(kThreads) conv_window_kernel(const ConvDev p)
-{
-    const int c = blockIdx.y * kThreads + threadIdx.x;
-    if (c >= p.d)
-        return;
-    const Span s = span_of(p.seqs, blockIdx.x);
-    const Segment g{(long long)blockIdx.x, s.row0, s.len, 0, 0};
-    T v[W - 1];
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j)
-        v[j] = input_at<true, T, 1, W>(p, g, s.len - (W - 1) + j, c, 1).v[0];
-#pragma unroll
-    for (int j = 0; j < W - 1; ++j)
-        static_cast<T*>(p.state_out)[((long long)blockIdx.x * (W - 1) + j) * p.d + c] = v[j];
 }
 
 template <typename T, int V, bool ALIGNED, int W>
@@ -398,15 +410,27 @@ __global__ void __launch_bounds__(kThreads, 7) conv_grad_kernel(const ConvDev p)
 }
 
 // Sums the tiles' shares of dw and dbias: a block per tap and 32 channels, the tiles dealt out to its eight warps, whose
-// sums are added in a fixed order.
-template <int W> __global__ void __launch_bounds__(256) conv_param_kernel(const ConvDev p, long long tiles)
+// sums are added in a fixed order.  Blocks past the taps pass the gradient of the last window of a sequence without tokens
+// on to its first one.
+template <typename T, int W> __global__ void __launch_bounds__(256) conv_param_kernel(const ConvDev p)
 {
     __shared__ float sum[8][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int c = blockIdx.x * 32 + lane, j = blockIdx.y;
+    if (j > W) {
+        const long long seq = j - (W + 1) + (long long)warp * (gridDim.y - (W + 1));
+        if (c < p.d && seq < p.seqs.batch && span_of(p.seqs, seq).len == 0)
+            for (int k = 0; k < W - 1; ++k) {
+                const long long at = (seq * (W - 1) + k) * p.d + c;
+                static_cast<T*>(p.dstate)[at] = p.dstate_out ? static_cast<const T*>(p.dstate_out)[at] : from_f<T>(0.f);
+            }
+        return;
+    }
+    if (!p.dw && !p.dbias)
+        return;
     float s = 0.f;
     if (c < p.d)
-        for (long long i = warp; i < tiles; i += 8)
+        for (long long i = warp; i < p.all_tiles; i += 8)
             s += p.part[(i * (W + 1) + j) * p.d + c];
     sum[warp][lane] = s;
     __syncthreads();
@@ -419,18 +443,6 @@ template <int W> __global__ void __launch_bounds__(256) conv_param_kernel(const 
         } else if (p.dbias) {
             p.dbias[c] = s;
         }
-    }
-}
-
-// Sequences without tokens: what the last window gets goes to the first one.
-template <typename T, int W> __global__ void __launch_bounds__(kThreads) conv_empty_kernel(const ConvDev p)
-{
-    const int c = blockIdx.y * kThreads + threadIdx.x;
-    if (c >= p.d || span_of(p.seqs, blockIdx.x).len > 0)
-        return;
-    for (int j = 0; j < W - 1; ++j) {
-        const long long at = ((long long)blockIdx.x * (W - 1) + j) * p.d + c;
-        static_cast<T*>(p.dstate)[at] = p.dstate_out ? static_cast<const T*>(p.dstate_out)[at] : from_f<T>(0.f);
     }
 }
 

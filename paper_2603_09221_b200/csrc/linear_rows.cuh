@@ -14,7 +14,7 @@ namespace lin {
 // operands of two mma.sync.m16n8k16: the instruction does not mind which contraction index a slot stands for, as long as
 // both operands agree, so nothing is rearranged or staged.
 
-constexpr int kFewWarps = 8, kFewAhead = 4;
+constexpr int kFewWarps = 8, kFewAhead = 8;
 
 struct FewDev {
     const void *x, *w;

@@ -352,20 +352,19 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
             if (p.runs)
                 TTC_TRY(o.pairs ? local(two) : local(one));
             if (a->batch) {
-                grad_join_kernel<<<dim3((unsigned)a->batch, (unsigned)((states + 127) / 128), 2), 128, 0, st>>>(p);
+                if (a->n % 4 == 0)
+                    grad_join_kernel<4><<<dim3((unsigned)a->batch, (unsigned)((states / 4 + 127) / 128), 2), 128, 0, st>>>(p);
+                else
+                    grad_join_kernel<1><<<dim3((unsigned)a->batch, (unsigned)((states + 127) / 128), 2), 128, 0, st>>>(p);
                 TTC_TRY(launched("gradients of the selective scan, states and co-states"));
             }
             if (p.runs)
                 TTC_TRY(o.pairs ? pieces(two) : pieces(one));
-            auto sum = [&](const float* part, int64_t stride, int64_t size, float* out) {
-                if (!out)
-                    return (int)TTC_OK;
-                grad_sum_kernel<<<(unsigned)((size + 31) / 32), 256, 0, st>>>(p, part, stride, size, out);
-                return launched("gradients of the selective scan, parameters");
-            };
-            TTC_TRY(sum(p.part_A, states, states, p.dA));
-            TTC_TRY(sum(p.part_D, 2 * (int64_t)a->d, a->d, p.dD));
-            TTC_TRY(sum(p.part_D ? p.part_D + a->d : nullptr, 2 * (int64_t)a->d, a->d, p.ddelta_bias));
+            const int64_t blocks = (p.dA ? (states + 31) / 32 : 0) + (p.dD || p.ddelta_bias ? 2 * (((int64_t)a->d + 31) / 32) : 0);
+            if (blocks) {
+                grad_sum_kernel<<<(unsigned)blocks, 256, 0, st>>>(p);
+                TTC_TRY(launched("gradients of the selective scan, parameters"));
+            }
             if (p.part_BC && p.runs) {
                 grad_rows_kernel<T><<<dim3((unsigned)p.runs, 4), 256, 0, st>>>(p, LANES * 4);
                 TTC_TRY(launched("gradients of the selective scan, B and C"));

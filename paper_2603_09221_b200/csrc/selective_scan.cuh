@@ -461,43 +461,49 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
         map[i] = make_int2(-1, 0);
 }
 
-// One token of each sequence: the state is read and written once, which is what bounds it.
+// One token of each sequence: the state is read and written once, which is what bounds it; for few sequences the latency of
+// one round of loads.
 template <typename T, int LANES>
-__global__ void __launch_bounds__(kStepThreads) scan_step_kernel(const ScanDev p)
+__global__ void __launch_bounds__(kStepThreads, 12) scan_step_kernel(const ScanDev p)
 {
     constexpr int CH = kStepThreads / LANES;
     const int tid = threadIdx.x, sub = tid % LANES, ch = tid / LANES;
     const long long b = blockIdx.x;
     const int c = blockIdx.y * CH + ch;
     const bool have = c < p.d;
-    const int n0 = sub * 4, per_group = p.d / p.groups;
+    const int n0 = sub * 4;
     float y[1] = {0.f};
-    float x = 0.f;
+    float x = 0.f, gate = 1.f, skip = 0.f;
     if (have) {
-        const int group = c / per_group;
-        float* st = p.state_out + (b * p.d + c) * p.n;
-        const float* A = p.A + (long long)c * p.n;
-        const T* B = row_ptr<const T>(p.B, b, 0) + group * p.n;
-        const T* C = row_ptr<const T>(p.C, b, 0) + group * p.n;
+        const int first = c / (p.d / p.groups) * p.n + n0, count = min(4, p.n - n0);
+        float* st = p.state_out + (b * p.d + c) * p.n + n0;
+        const float* A = p.A + (long long)c * p.n + n0;
+        const T* B = row_ptr<const T>(p.B, b, 0) + first;
+        const T* C = row_ptr<const T>(p.C, b, 0) + first;
         float h[4] = {}, a[4] = {}, bb[4] = {}, cc[4] = {};
+        x = to_f(row_ptr<const T>(p.x, b, 0)[c]);
+        float step = to_f(row_ptr<const T>(p.delta, b, 0)[c]) + (p.delta_bias ? p.delta_bias[c] : 0.f);
         if (p.vec4) {
-            if (n0 < p.n) {
-                const float4 v = *reinterpret_cast<const float4*>(st + n0), w = *reinterpret_cast<const float4*>(A + n0);
+            if (count > 0) {
+                const float4 v = *reinterpret_cast<const float4*>(st), w = *reinterpret_cast<const float4*>(A);
                 h[0] = v.x, h[1] = v.y, h[2] = v.z, h[3] = v.w;
                 a[0] = w.x, a[1] = w.y, a[2] = w.z, a[3] = w.w;
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (n0 + i < p.n)
-                    h[i] = st[n0 + i], a[i] = A[n0 + i];
+                if (i < count)
+                    h[i] = st[i], a[i] = A[i];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (n0 + i < p.n)
-                bb[i] = to_f(B[n0 + i]), cc[i] = to_f(C[n0 + i]);
-        x = to_f(row_ptr<const T>(p.x, b, 0)[c]);
-        float step = to_f(row_ptr<const T>(p.delta, b, 0)[c]) + (p.delta_bias ? p.delta_bias[c] : 0.f);
+            if (i < count)
+                bb[i] = to_f(B[i]), cc[i] = to_f(C[i]);
+        if (sub == 0) {
+            skip = p.D ? p.D[c] : 0.f;
+            if (p.z.ptr)
+                gate = silu(to_f(row_ptr<const T>(p.z, b, 0)[c]));
+        }
         if (p.softplus)
             step = softplus(step);
         const float v = step * x;
@@ -507,22 +513,18 @@ __global__ void __launch_bounds__(kStepThreads) scan_step_kernel(const ScanDev p
             y[0] = fmaf(h[i], cc[i], y[0]);
         }
         if (p.vec4) {
-            if (n0 < p.n)
-                *reinterpret_cast<float4*>(st + n0) = make_float4(h[0], h[1], h[2], h[3]);
+            if (count > 0)
+                *reinterpret_cast<float4*>(st) = make_float4(h[0], h[1], h[2], h[3]);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (n0 + i < p.n)
-                    st[n0 + i] = h[i];
+                if (i < count)
+                    st[i] = h[i];
         }
     }
     group_sums<1, LANES, 1>(y, tid);
-    if (have && sub == 0) {
-        float v = fmaf(p.D ? p.D[c] : 0.f, x, y[0]);
-        if (p.z.ptr)
-            v *= silu(to_f(row_ptr<const T>(p.z, b, 0)[c]));
-        row_ptr<T>(p.y, b, 0)[c] = from_f<T>(v);
-    }
+    if (have && sub == 0)
+        row_ptr<T>(p.y, b, 0)[c] = from_f<T>(fmaf(skip, x, y[0]) * gate);
 }
 
 } // namespace sscan

@@ -281,47 +281,58 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_local_kernel(const GradD
     }
 }
 
-// blockIdx.z 0: states forward, 1: co-states backward.  In: what each piece adds; out: what enters it.
-static __global__ void __launch_bounds__(128) grad_join_kernel(const GradDev p)
+// blockIdx.z 0: states forward, 1: co-states backward.  In: what each piece adds; out: what enters it.  V states of a channel
+// to a thread (four where n is a multiple of four).
+template <int V> __global__ void __launch_bounds__(128) grad_join_kernel(const GradDev p)
 {
-    const long long at = (long long)blockIdx.y * 128 + threadIdx.x, size = (long long)p.f.d * p.f.n;
+    const long long at = ((long long)blockIdx.y * 128 + threadIdx.x) * V, size = (long long)p.f.d * p.f.n;
     if (at >= size)
         return;
+    typedef Vec<float, V> Some;
     const long long seq = blockIdx.x, c = at / p.f.n;
     const long long first = (p.f.piece_map ? p.f.seq_first[seq] : seq * p.f.pieces_per_seq) * kRun;
     const long long most = p.f.piece_map ? (p.f.seq_first[seq + 1] * (long long)kRun - first) : p.f.pieces_per_seq * kRun;
     long long count = (span_of(p.f.seqs, seq).len + kPiece - 1) / kPiece;
     count = count < most ? count : most;
-    const float a = p.f.A[at] * kLog2e;
+    float a[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        a[i] = p.f.A[at + i] * kLog2e;
     constexpr int kAhead = 8;
-    // states walk forward, co-states backward; what each piece adds is replaced by what enters it
     const bool back = blockIdx.z;
     const long long start = back ? first + count - 1 : first;
     float* v = (back ? p.r : p.h) + start * size + at;
     const float* s = p.step + start * p.f.d + c;
     const long long v_next = back ? -size : size, s_next = back ? -(long long)p.f.d : p.f.d;
     const float* from = back ? p.dstate_out : p.f.state;
-    float h = from ? from[seq * size + at] : 0.f;
+    Some h;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+        h.v[i] = from ? from[seq * size + at + i] : 0.f;
+    auto piece = [&](Some add, float step) {
+        *reinterpret_cast<Some*>(v) = h;
+        v += v_next;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            h.v[i] = fmaf(ex2(a[i] * step), h.v[i], add.v[i]);
+    };
     for (; count >= kAhead; count -= kAhead) {
-        float add[kAhead], step[kAhead];
-        const float *vv = v, *ss = s;
+        Some add[kAhead];
+        float step[kAhead];
+        const float* vv = v;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i, vv += v_next, ss += s_next)
-            add[i] = *vv, step[i] = *ss;
+        for (int i = 0; i < kAhead; ++i, vv += v_next, s += s_next)
+            add[i] = *reinterpret_cast<const Some*>(vv), step[i] = *s;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i, v += v_next) {
-            *v = h;
-            h = fmaf(ex2(a * step[i]), h, add[i]);
-        }
-        s = ss;
+        for (int i = 0; i < kAhead; ++i)
+            piece(add[i], step[i]);
     }
-    for (; count > 0; --count, v += v_next, s += s_next) {
-        const float add = *v, step = *s;
-        *v = h;
-        h = fmaf(ex2(a * step), h, add);
-    }
+    for (; count > 0; --count, s += s_next)
+        piece(*reinterpret_cast<const Some*>(v), *s);
     if (back && p.dstate)
-        p.dstate[seq * size + at] = h;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            p.dstate[seq * size + at + i] = h.v[i];
 }
 
 template <typename T, int LANES, int V>
@@ -540,12 +551,19 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
     }
 }
 
-// Sum over the runs: out[i] = sum_r part[r * stride + i], i < size; runs without a sequence were not written.
-static __global__ void __launch_bounds__(256) grad_sum_kernel(const GradDev p, const float* part, long long stride, long long size, float* out)
+// Sums over the runs, dA first, then dD and ddelta_bias: out[i] = sum_r part[r][i], 32 of them to a block.  Runs without a
+// sequence were not written.
+static __global__ void __launch_bounds__(256) grad_sum_kernel(const GradDev p)
 {
     __shared__ float sum[8][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-    const long long i = (long long)blockIdx.x * 32 + lane;
+    const long long states = (long long)p.f.d * p.f.n, a_blocks = p.dA ? (states + 31) / 32 : 0, d_blocks = (p.f.d + 31) / 32;
+    const long long b = blockIdx.x - a_blocks;
+    const bool of_A = b < 0;
+    const int kind = of_A ? 0 : static_cast<int>(b / d_blocks);      // 0: dD, 1: ddelta_bias
+    const long long i = (of_A ? blockIdx.x : b % d_blocks) * 32 + lane, size = of_A ? states : p.f.d, stride = of_A ? states : 2ll * p.f.d;
+    const float* part = of_A ? p.part_A : p.part_D + kind * p.f.d;
+    float* out = of_A ? p.dA : kind ? p.ddelta_bias : p.dD;
     const long long runs = p.f.piece_map ? p.f.seq_first[p.f.seqs.batch] : p.runs;
     float s = 0.f;
     if (i < size)
@@ -553,7 +571,7 @@ static __global__ void __launch_bounds__(256) grad_sum_kernel(const GradDev p, c
             s += part[r * stride + i];
     sum[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && i < size) {
+    if (warp == 0 && i < size && out) {
         for (int k = 1; k < 8; ++k)
             s += sum[k][lane];
         out[i] = s;
