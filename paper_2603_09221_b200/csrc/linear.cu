@@ -360,7 +360,7 @@ int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_
         f.rows = (int)a->rows;
         f.k = a->k;
         f.m = a->m;
-        f.vec = aligned(a->x, f.ldx, 2) && aligned(a->w, f.ldw, 2);
+        f.vec = a->k % 8 == 0 && aligned(a->x, f.ldx, 2) && aligned(a->w, f.ldw, 2);
         f.e = e;
         return by_type(a->out_dtype, [&](auto t) {
             using OT = decltype(t);

@@ -20,22 +20,20 @@ struct FewDev {
     const void *x, *w;
     long long ldx, ldw;
     int rows, k, m;
-    int vec;                     // rows of x and W can be read by 16 bytes
+    int vec;                     // rows of x and W can be read by 16 bytes, and end on them
     Epilogue e;
 };
 
 template <typename T> __device__ __forceinline__ uint4 load8(const T* row, bool row_ok, int k, int k_end, bool vec)
 {
-    uint4 r = make_uint4(0, 0, 0, 0);
-    if (!row_ok || k >= k_end)
-        return r;
-    if (vec && k + 8 <= k_end)
-        return *reinterpret_cast<const uint4*>(row + k);
+    if (vec)                                                         // (k_end is a multiple of 8)
+        return load_if(reinterpret_cast<const uint4*>(row + k), row_ok && k < k_end);
     const unsigned short* u = reinterpret_cast<const unsigned short*>(row);
     unsigned short v[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        v[i] = k + i < k_end ? u[k + i] : 0;
+        v[i] = row_ok && k + i < k_end ? u[k + i] : 0;
+    uint4 r;
     r.x = v[0] | (unsigned)v[1] << 16, r.y = v[2] | (unsigned)v[3] << 16;
     r.z = v[4] | (unsigned)v[5] << 16, r.w = v[6] | (unsigned)v[7] << 16;
     return r;
@@ -75,20 +73,25 @@ __global__ void __launch_bounds__(kFewWarps * 32) few_rows_kernel(const FewDev p
     const T *w0 = w + (long long)(f0 + g) * p.ldw, *w1 = w + (long long)(f0 + g + 8) * p.ldw;
     const bool ok0 = f0 + g < p.m, ok1 = f0 + g + 8 < p.m;
     float acc[NT][4] = {};
+    auto load = [&](const T* row, bool ok, int k) { return load8(row, ok, k, p.k, p.vec); };
+    // all of W's loads of a round first, and x's with them while they are few
+    constexpr bool TOGETHER = NT == 1;
     for (int k0 = warp * 32; k0 < p.k; k0 += kFewWarps * 32 * kFewAhead) {
-        uint4 a0[kFewAhead], a1[kFewAhead];
+        uint4 a0[kFewAhead], a1[kFewAhead], b0[TOGETHER ? kFewAhead : 1];
 #pragma unroll
         for (int i = 0; i < kFewAhead; ++i) {
             const int k = k0 + i * kFewWarps * 32 + t * 8;
-            a0[i] = load8(w0, ok0, k, p.k, p.vec);
-            a1[i] = load8(w1, ok1, k, p.k, p.vec);
+            a0[i] = load(w0, ok0, k);
+            a1[i] = load(w1, ok1, k);
+            if (TOGETHER)
+                b0[TOGETHER ? i : 0] = load(x + (long long)g * p.ldx, g < p.rows, k);
         }
 #pragma unroll
         for (int i = 0; i < kFewAhead; ++i) {
             const int k = k0 + i * kFewWarps * 32 + t * 8;
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                const uint4 b = load8(x + (long long)(n * 8 + g) * p.ldx, n * 8 + g < p.rows, k, p.k, p.vec);
+                const uint4 b = TOGETHER ? b0[TOGETHER ? i : 0] : load(x + (long long)(n * 8 + g) * p.ldx, n * 8 + g < p.rows, k);
                 mma16816<T>(acc[n], a0[i].x, a1[i].x, a0[i].y, a1[i].y, b.x, b.y);
                 mma16816<T>(acc[n], a0[i].z, a1[i].z, a0[i].w, a1[i].w, b.z, b.w);
             }
