@@ -128,13 +128,15 @@ int plan_forward(int device, const ttc_scan_args* a, void* ws, Plan& o)
     if (columns > kMaxGridY)
         return fail(TTC_STATUS_UNSUPPORTED, "d = %d, n = %d, groups = %d", a->d, a->n, a->groups);
     const int64_t rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
-    int64_t want = 0;                            // pieces in all
-    if (a->batch * columns < sms)
-        want = (2 * sms + columns - 1) / columns;
+    int64_t want = 0;                            // pieces in all; two blocks of each SM hold all that are not more
+    if (3 * a->batch * columns <= 2 * sms)
+        want = 2 * sms / columns;
     else if (a->seq_offsets)
         want = a->batch;
     if (want && rows) {
-        int64_t piece = ((rows + want - 1) / want + 63) / 64 * 64;
+        // (of equal sequences, as many to each)
+        const int64_t each = a->seq_offsets ? 1 : want / a->batch;
+        int64_t piece = ((a->seq_offsets ? (rows + want - 1) / want : (a->tokens + each - 1) / each) + 15) / 16 * 16;
         piece = piece < 128 ? 128 : piece;
         if (2 * piece <= a->tokens) {
             p.piece = piece;
