@@ -53,6 +53,21 @@ template <typename P> __device__ __forceinline__ P load_if(const P* from, bool o
     return r;
 }
 
+// Stores to shared memory that loads around them may pass: for areas that are only read behind a barrier.  To the compiler an
+// ordinary store may touch what the next load reads, and a loop with one in each step waits for its loads step by step.
+__device__ __forceinline__ void put_aside(float* to, float a)
+{
+    asm volatile("st.shared.f32 [%0], %1;" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "f"(a));
+}
+__device__ __forceinline__ void put_aside(float2* to, float a, float b)
+{
+    asm volatile("st.shared.v2.f32 [%0], {%1, %2};" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "f"(a), "f"(b));
+}
+__device__ __forceinline__ void put_aside(float4* to, float a, float b, float c, float d)
+{
+    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" :: "r"((uint32_t)__cvta_generic_to_shared(to)), "f"(a), "f"(b), "f"(c), "f"(d));
+}
+
 struct Rows {
     void* ptr;
     long long bs, ts;

@@ -77,7 +77,7 @@ template <int WIDTH, int TB, int V> struct Lay {
 template <int LANES> struct Shape {
     static constexpr int CH = channels_of(LANES);
     static constexpr int NP = LANES * 4;                // padded states
-    static constexpr int TB = LANES == 2 ? 8 : 16;
+    static constexpr int TB = LANES == 2 ? 8 : LANES == 4 ? 32 : 16;
     static constexpr int TOK = TB * CH * 2, BC = TB * NP, Y = TB * CH * LANES;      // floats of a buffer
     static constexpr size_t smem(bool local) { return 2 * sizeof(float) * (TOK + BC * (local ? 1 : 2) + (local ? 0 : Y)); }
 };
@@ -202,7 +202,7 @@ __device__ __forceinline__ void run_states(const ScanDev& p, const Piece& q, int
                     y0 = i ? fmaf(h0, c[i], y0) : h0 * c[i];
                     y1 = i ? fmaf(h1, c[i], y1) : h1 * c[i];
                 }
-                ys[u * (CH / 2 * LANES)] = make_float2(y0, y1);
+                put_aside(ys + u * (CH / 2 * LANES), y0, y1);
             }
         }
         meet();

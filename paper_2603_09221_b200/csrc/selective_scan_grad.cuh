@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
                             unpack2(h[u + 1][i], a0, a1);
                             y0 = fmaf(a0, c[i], y0), y1 = fmaf(a1, c[i], y1);
                         }
-                        s_y[u * (CH / 2 * LANES) + tid] = make_float2(y0, y1);
+                        put_aside(s_y + u * (CH / 2 * LANES) + tid, y0, y1);
                     }
                 }
 #pragma unroll
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
                     }
                     float th0, th1;
                     unpack2(through, th0, th1);
-                    s_q[u * (CH / 2 * LANES) + tid] = make_float4(qB0, qB1, th0, th1);
+                    put_aside(s_q + u * (CH / 2 * LANES) + tid, qB0, qB1, th0, th1);
                     group_sums<8, 32 / LANES, LANES>(bc, lane);
                     constexpr int W = 32 / LANES, kept = W >= 8 ? 1 : 8 / W;
                     const int j = lane / LANES, first = first_value<8, W>(j);
@@ -452,7 +452,7 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
 #pragma unroll
                         for (int i = 0; i < kept; ++i) {
                             const int v = first + i;
-                            s_BC[((warp * HALF + u) * 2 + v / 4) * NP + n0 + v % 4] = bc[i];
+                            put_aside(s_BC + ((warp * HALF + u) * 2 + v / 4) * NP + n0 + v % 4, bc[i]);
                         }
                     asm volatile("" ::: "memory");                   // keeps the loads of a token with its products
                 }
