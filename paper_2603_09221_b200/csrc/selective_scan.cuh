@@ -170,7 +170,7 @@ __device__ __forceinline__ void run_states(const ScanDev& p, const Piece& q, int
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 float e0, e1;
-                unpack2(mul2(A2[i], tok_next.x), e0, e1);
+                unpack2(fma2(A2[i], tok_next.x, pack2(kExBias, kExBias)), e0, e1);
                 next[i] = pack2(ex2(e0), ex2(e1));
             }
             if (LOCAL)
@@ -509,7 +509,7 @@ __global__ void __launch_bounds__(kStepThreads, 12) scan_step_kernel(const ScanD
         const float v = step * x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[i] = fmaf(ex2(step * (a[i] * kLog2e)), h[i], v * bb[i]);
+            h[i] = fmaf(ex2(fmaf(step, a[i] * kLog2e, kExBias)), h[i], v * bb[i]);
             y[0] = fmaf(h[i], cc[i], y[0]);
         }
         if (p.vec4) {

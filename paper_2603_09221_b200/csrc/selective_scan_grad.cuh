@@ -203,7 +203,7 @@ __device__ __forceinline__ void decays(f2 (&a)[4], const f2 (&A2)[4], f2 step)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         float e0, e1;
-        unpack2(mul2(A2[i], step), e0, e1);
+        unpack2(fma2(A2[i], step, pack2(kExBias, kExBias)), e0, e1);
         a[i] = pack2(ex2(e0), ex2(e1));
     }
 }
