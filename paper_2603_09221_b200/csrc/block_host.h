@@ -96,8 +96,8 @@ inline int check_sequences(int64_t batch, int64_t tokens, const int32_t* offsets
 
 inline Rows dev_rows(const ttc_rows& r, const int32_t* offsets) { return Rows{r.ptr, offsets ? 0 : r.bstride, r.tstride}; }
 
-// Rows of an output and of an input that share elements.  Columns of one wider matrix (equal strides, one a multiple of
-// the other) do not; where the strides say nothing, the caller is believed.
+// Rows of an output and of an input that share elements, or may: ranges that meet, unless they are different columns of one
+// wider matrix (equal strides, one a multiple of the other).  Equal strides of another kind say nothing; the caller is believed.
 inline bool rows_overlap(const ttc_rows& a, int64_t wa, const ttc_rows& b, int64_t wb, int64_t batch, int64_t tokens, bool packed, size_t size)
 {
     if (!a.ptr || !b.ptr || batch <= 0 || tokens <= 0)
@@ -112,7 +112,7 @@ inline bool rows_overlap(const ttc_rows& a, int64_t wa, const ttc_rows& b, int64
         return true;
     const bool by_token = tokens > 1, by_batch = nb > 0;
     if ((by_token && a.tstride != b.tstride) || (by_batch && a.bstride != b.bstride))
-        return false;
+        return true;
     int64_t period = by_token ? a.tstride : by_batch ? a.bstride : 0;
     if (by_token && by_batch) {
         const int64_t lo = a.tstride < a.bstride ? a.tstride : a.bstride, hi = a.tstride < a.bstride ? a.bstride : a.tstride;

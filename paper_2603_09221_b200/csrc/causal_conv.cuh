@@ -40,17 +40,24 @@ struct Segment {
     long long t0, t1;               // tokens of it in the tile
 };
 
-// First sequence that ends behind the first row of tile `i`: every lane of the warp looks at some of them, so that one round
-// of loads does where a search by halves would wait for several.  All lanes of the warp take part.
+// First sequence that ends behind the first row of tile `i`.  Every lane of the warp looks at a place of its own, so that a
+// round of loads narrows the search to a 32nd (up to 32 sequences: one round).  All lanes of the warp take part.
 __device__ __forceinline__ long long first_sequence(const ConvDev& p, long long i)
 {
     if (!p.seqs.offsets)
         return 0;
     const long long r0 = i * p.tile;
-    int before = 0;
-    for (long long b = threadIdx.x % 32; b < p.seqs.batch; b += 32)
-        before += clamp_offset(p.seqs, b + 1) <= r0;
-    return __reduce_add_sync(0xffffffffu, before);
+    long long lo = 0, hi = p.seqs.batch;
+    while (lo < hi) {
+        const long long step = (hi - lo + 31) / 32, b = lo + threadIdx.x % 32 * step;
+        const bool before = b < hi && clamp_offset(p.seqs, b + 1) <= r0;
+        const int count = __popc(__ballot_sync(0xffffffffu, before));
+        if (count == 0)
+            break;
+        hi = lo + count * step < hi ? lo + count * step : hi;
+        lo += (count - 1) * step + 1;
+    }
+    return lo;
 }
 
 // Calls f for every sequence that has tokens in tile `i`, the first of which may be `from`.

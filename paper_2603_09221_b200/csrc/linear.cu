@@ -230,6 +230,12 @@ int plan_linear(int device, const ttc_linear_args* a, void* ws, LinearPlan& o)
     TTC_TRY(check_floats("residual", a->residual, true, size));
     if (a->rows > 1 && (a->ldy < a->m || (a->residual && a->ldr < a->m)))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
+    auto rows = [](const void* p, int64_t ld) { return ttc_rows{const_cast<void*>(p), 0, ld}; };
+    auto clash = [&](const void* out, int64_t ld) {
+        return rows_overlap(rows(out, ld), a->m, rows(a->x, a->ldx), a->k, 1, a->rows, false, 2);
+    };
+    if ((a->out_dtype == a->dtype && clash(a->y, a->ldy)) || (a->pre && clash(a->pre, a->ldp)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "y or pre overlaps x");
     const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
     Scratch s(ws);
     o.few = a->rows <= kFewRows;
@@ -267,6 +273,8 @@ int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, v
         return fail(TTC_STATUS_INVALID_ARGUMENT, "pre is null: the gradients of an activation need it");
     if ((a->rows > 1 && (g->lddy < a->m || (g->dx && g->lddx < a->k))) || (g->dw && a->m > 1 && g->lddw < a->k))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
+    if (g->dx && rows_overlap(ttc_rows{g->dx, 0, g->lddx}, a->k, ttc_rows{const_cast<void*>(a->x), 0, a->ldx}, a->k, 1, a->rows, false, 2))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "dx overlaps x");
     const int sms = sm_count(device);
     const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
     const int64_t lddy = a->rows > 1 ? g->lddy : (a->m + 7) / 8 * 8;

@@ -40,6 +40,13 @@ struct ScanDev {
     float *local, *local_step;    // [pieces][d][n] and [pieces][d]: what a piece adds to a state, and its sum of D_t
 };
 
+// A log2(e).  Minus infinity becomes the lowest number: times the step 0 of a padding token it has to be 0.
+__device__ __forceinline__ float exponent(float A)
+{
+    const float e = A * kLog2e;
+    return e < -3.4e38f ? -3.4e38f : e;
+}
+
 struct Piece {
     long long seq, t0, t1, row0, len;
     long long first, last;        // pieces of the same sequence
@@ -132,7 +139,7 @@ __device__ __forceinline__ void run_states(const ScanDev& p, const Piece& q, int
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bool ok = have && n0 + i < p.n;
-                a[c][i] = ok ? p.A[my * p.n + n0 + i] * kLog2e : 0.f;
+                a[c][i] = ok ? exponent(p.A[my * p.n + n0 + i]) : 0.f;
                 h[c][i] = !LOCAL && q.t0 == 0 && ok && p.state ? p.state[(q.seq * p.d + my) * p.n + n0 + i] : 0.f;
             }
             if (!LOCAL && q.t0 > 0 && have) {
@@ -445,11 +452,8 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
         }
         // offsets that do decrease could ask for more pieces than there is room for: they are cut off
         const long long end = base + (long long)sum[threadIdx.x], first = end - count;
-        if (b < s.batch) {
+        if (b < s.batch)
             seq_first[b] = static_cast<int>(first < bound ? first : bound);
-            for (int i = 0; i < count && first + i < bound; ++i)
-                map[first + i] = make_int2(static_cast<int>(b), static_cast<int>(i * piece));
-        }
         __syncthreads();
         if (threadIdx.x == 1023)
             base = static_cast<int>(end < bound ? end : bound);
@@ -457,8 +461,18 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
     }
     if (threadIdx.x == 0)
         seq_first[s.batch] = base;
-    for (long long i = base + threadIdx.x; i < bound; i += 1024)
-        map[i] = make_int2(-1, 0);
+    __syncthreads();
+    for (long long i = threadIdx.x; i < bound; i += 1024) {
+        long long lo = 0, hi = s.batch;                              // the last sequence that does not begin behind piece i
+        while (hi - lo > 1) {
+            const long long mid = (lo + hi) / 2;
+            if (seq_first[mid] <= i)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        map[i] = i < base ? make_int2(static_cast<int>(lo), static_cast<int>((i - seq_first[lo]) * piece)) : make_int2(-1, 0);
+    }
 }
 
 // One token of each sequence: the state is read and written once, which is what bounds it; for few sequences the latency of

@@ -152,7 +152,7 @@ struct Mine {
             count[c] = ch < per_group ? max(0, min(4, p.f.n - n0)) : 0;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                a[c][i] = i < count[c] ? p.f.A[at[c] + i] * kLog2e : 0.f;
+                a[c][i] = i < count[c] ? exponent(p.f.A[at[c] + i]) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -297,7 +297,7 @@ template <int V> __global__ void __launch_bounds__(128) grad_join_kernel(const G
     float a[V];
 #pragma unroll
     for (int i = 0; i < V; ++i)
-        a[i] = p.f.A[at + i] * kLog2e;
+        a[i] = exponent(p.f.A[at + i]);
     constexpr int kAhead = 8;
     const bool back = blockIdx.z;
     const long long start = back ? first + count - 1 : first;

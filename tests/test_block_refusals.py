@@ -101,7 +101,8 @@ def test_scan_of_few_channels_needs_a_workspace():
 @pytest.mark.parametrize("kw, status", [
     (dict(rows=-1), INVALID), (dict(k=0), INVALID), (dict(m=0), INVALID), (dict(dtype=0), INVALID), (dict(out_dtype=2), INVALID), (dict(act=5), INVALID),
     (dict(act=-1), INVALID), (dict(x=0), INVALID), (dict(w=0), INVALID), (dict(y=0), INVALID), (dict(x=P + 1), INVALID), (dict(bias=P + 2), INVALID),
-    (dict(ldx=31), INVALID), (dict(ldw=31), INVALID), (dict(ldy=47), INVALID), (dict(residual=P, ldr=47), INVALID), (dict(rows=1 << 32), UNSUPPORTED)])
+    (dict(ldx=31), INVALID), (dict(ldw=31), INVALID), (dict(ldy=47), INVALID), (dict(residual=P, ldr=47), INVALID), (dict(rows=1 << 32), UNSUPPORTED), (dict(y=P), INVALID),
+    (dict(pre=P + 16), INVALID)])
 def test_linear(kw, status):
     lib = block._load()
     assert _status(lib.ttc_linear, 0, _linear(**kw), None, 0, None)[0] == status
@@ -109,9 +110,9 @@ def test_linear(kw, status):
 
 def test_linear_gradients():
     lib = block._load()
-    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=P, dx=P, dw=P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
+    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=3 * P, dx=4 * P, dw=P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
     assert lib.ttc_linear_grad_workspace(0, _linear(), grads()) >= 0
-    for kw in (dict(dy=0), dict(lddy=47), dict(lddx=31), dict(lddw=31), dict(dbias=P + 1)):
+    for kw in (dict(dy=0), dict(lddy=47), dict(lddx=31), dict(lddw=31), dict(dbias=P + 1), dict(dx=P)):
         assert _status(lib.ttc_linear_grad_workspace, 0, _linear(), grads(**kw))[0] == INVALID, kw
     assert _status(lib.ttc_linear_grad_workspace, 0, _linear(act=2), grads())[0] == INVALID       # no pre
 

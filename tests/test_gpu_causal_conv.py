@@ -96,6 +96,15 @@ def test_packed_sequences_and_rows_outside_of_them(cuts, rows, dtype):
     assert bool((dx[:cuts[0]] == 99).all()) and bool((dx[cuts[-1]:] == 99).all())
 
 
+def test_many_short_sequences():
+    lengths = torch.randint(0, 4, (5000,), generator=torch.Generator().manual_seed(5))
+    cuts = [0, *lengths.cumsum(0).tolist()]
+    offsets = torch.tensor(cuts, dtype=torch.int32, device=DEV)
+    v = _inputs(len(cuts) - 1, (cuts[-1],), 10, 4, F)
+    _check_forward(v, "silu", (cuts[-1],), offsets)
+    _check_grad(v, "silu", (cuts[-1],), offsets)
+
+
 def test_without_bias_and_window():
     v = _inputs(2, (2, 21), 24, 4, torch.float16, window=False)
     v["bias"] = None

@@ -189,6 +189,34 @@ def test_gradient_against_differences():
         assert loss(x, up) - loss(x, w) == float(got["dw"][i, j])
 
 
+def test_pairs_of_ctas_in_a_graph():
+    """Enough tiles of 256 x 256 for two CTAs on each, ragged in both directions; captured and replayed on new values."""
+    g = torch.Generator(device=DEV).manual_seed(10)
+    x, w, b, r = _randn(g, 9001, 72), _randn(g, 1000, 72), _randn(g, 1000, t=F), _randn(g, 9001, 1000)
+    first = _check(x, w, b, "silu", r)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y = block.linear(x, w, b, act="silu", residual=r)
+    graph.replay()
+    assert torch.equal(y, first)
+    x.copy_(_randn(g, 9001, 72))
+    graph.replay()
+    assert torch.equal(y, _check(x, w, b, "silu", r))
+    _check_grad(_randn(g, 1024, 3000), _randn(g, 9000, 3000), _randn(g, 1024, 9000), "relu", _randn(g, 1024, 9000))
+
+
+def test_long_contractions_in_float32():
+    """Added up in segments of 512 indices, 32 steps of the tensor cores, each of which cuts off u of the partial sum in the mean.  With
+    random signs a partial sum is in the mean not larger than the segment's own, so a segment is off by at most 32 u = 1.9e-6 of
+    its norm, and the segments' norms add up in squares to the result's."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    for rows, k, m in ((1500, 4096, 700), (64, 8000, 96), (20, 4096, 50), (300, 1100, 257)):
+        x, w = _randn(g, rows, k), _randn(g, m, k)
+        y = _check(x, w, out_dtype=F)
+        want = x.double() @ w.double().t()
+        assert float((y.double() - want).norm() / want.norm()) <= 32 * bu.U
+
+
 def test_graphs_and_streams():
     g = torch.Generator(device=DEV).manual_seed(9)
     x, w, b, dy = _randn(g, 70, 1033), _randn(g, 90, 1033), _randn(g, 90, t=F), _randn(g, 70, 90)

@@ -252,6 +252,29 @@ def test_offsets_that_make_no_sense_stay_in_range():
     assert bool((guard[:100] == 3).all()) and bool((guard[400:] == 3).all())
 
 
+@pytest.mark.parametrize("d, n", [(4, 4), (300, 16)])
+def test_many_short_sequences(d, n):
+    lengths = torch.randint(0, 4, (3000,), generator=torch.Generator().manual_seed(5))
+    cuts = [0, *lengths.cumsum(0).tolist()]
+    offsets = torch.tensor(cuts, dtype=torch.int32, device=DEV)
+    v = _inputs(len(cuts) - 1, (cuts[-1],), d, n, F)
+    _check_forward(v, (cuts[-1],), offsets)
+    if d == 4:
+        _check_grad(v, (cuts[-1],), offsets)
+
+
+def test_a_decay_of_minus_infinity():
+    """exp(D A) = 0: the state is the last token's share, at tokens that do not fill a tile too."""
+    v = _inputs(1, (1, 21), 6, 16, F)
+    v["A"][2] = float("-inf")
+    last = torch.empty((1, 6, 16), device=DEV)
+    y = block.selective_scan(**v, state_out=last)
+    assert torch.isfinite(y).all() and torch.isfinite(last).all()
+    step = torch.nn.functional.softplus(v["delta"][0, -1, 2].double() + v["delta_bias"][2].double())
+    want = float(step * v["x"][0, -1, 2].double()) * v["B"][0, -1, 0].double()
+    bu.within(last[0, 2], bu.f64(want), 24 * bu.U * np.abs(bu.f64(want)), F, "state")
+
+
 def test_the_same_bits_again_and_in_captured_graphs():
     v = _inputs(2, (2, 500), 24, 16, torch.bfloat16)
     dy = torch.randn((2, 500, 24), device=DEV).bfloat16()
