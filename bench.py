@@ -437,7 +437,42 @@ def run_layer(args):
         gout = torch.randn((N, n), generator=gen, device=dev)
         grads = {k: torch.empty_like(w[k]) for k in lqr.LAYER_GRAD_KEYS}
 
+    project = lambda: None  # noqa: E731
+    leave = lambda: None  # noqa: E731
+    block_launches = 0
+    if args.from_tokens > 0:               # the layer between its projections: coefficient vectors from token rows, output onto the residual stream
+        from paper_2603_09221_b200 import block
+        c["name"] += "_from_tokens%d" % args.from_tokens
+        args.no_e2e = True
+        gen = torch.Generator(device=dev)
+        gen.manual_seed(sharding.rank_seed(500, rank))
+        rows, heads, model = N // c["batch"][1], c["batch"][1], args.from_tokens
+        rand = lambda *shape: torch.randn(shape, generator=gen, device=dev)  # noqa: E731
+        x, w_out = rand(rows, model).bfloat16(), (rand(model, heads * n) * (heads * n) ** -0.5).bfloat16()
+        names = workloads.LAYER_KEYS[:9]
+        weights = {k: (rand(heads * w[k].shape[1], model) * 0.3 * model ** -0.5).bfloat16() for k in names}
+        flat = {k: torch.empty((rows, heads * w[k].shape[1]), device=dev) for k in names}
+        u_rows, y = torch.empty((rows, heads * n), device=dev, dtype=torch.bfloat16), torch.empty_like(x)
+        for k in names:
+            w[k] = flat[k].view(N, -1)
+        ins[:9] = [w[k] for k in names]
+
+        def project():
+            for k in names:                # gates, weights and diag(R^-1) are positive; the state and the mixing of A and B are not held to that
+                block.linear(x, weights[k], act="none" if k in ("s_a", "s_b", "h0") else "softplus", y=flat[k])
+
+        def leave():
+            u_rows.copy_(u1.view(rows, heads * n))
+            block.linear(u_rows, w_out, residual=x, y=y)
+
+        block_launches = len(names) + 1
+
     def step():
+        project()
+        solve()
+        leave()
+
+    def solve():
         if gradient:
             solver.layer_grad(*ins, T, gout, grads, u1=u1, info=info)
         elif baseline:
@@ -468,7 +503,7 @@ def run_layer(args):
         step()
         e1[i].record()
     barrier()
-    launches = solver.query(lqr.TTC_QUERY_TOTAL_LAUNCHES) - launches0
+    launches = solver.query(lqr.TTC_QUERY_TOTAL_LAUNCHES) - launches0 + args.steps * block_launches
     clocks = sampler.stop() if rank == 0 else None
     per_step = [e0[i].elapsed_time(e1[i]) for i in range(args.steps)]
     value, ms_per_step, _ = sharding.aggregate_throughput(N, sum(per_step) / len(per_step), device=dev)
@@ -903,6 +938,9 @@ def main():
     ap.add_argument("--lowrank-q", action="store_true", help="cfg4: hand Q over as its factors (ttc_lqr_solve_lowrank_q)")
     ap.add_argument("--grad", action="store_true", help="layer workloads: time ttc_lqr_layer_grad (every gradient requested)")
     ap.add_argument("--sweep", action="store_true", help="layer workloads: horizon x batch grid, recursion and sigma baseline")
+    ap.add_argument("--from-tokens", type=int, default=0, metavar="WIDTH",
+                    help="layer workloads: a step begins with bfloat16 token rows of this width (the coefficient vectors are projections of "
+                         "them, ttc_linear) and ends with the layer's output on the residual stream")
     ap.add_argument("--no-cpu-baseline", action="store_true")
     ap.add_argument("--no-e2e", action="store_true")
     ap.add_argument("--no-sides", action="store_true", help="default run: skip the side measurements of cfg0..cfg3")
