@@ -430,9 +430,10 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
                     unpack2(tok.y, in0, in1);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const f2 co = add2(r[i], pack2(g.x * c[i], g.y * c[i]));      // q_t
-                        float q0, q1, s0, s1;
-                        unpack2(co, q0, q1);
+                        float q0, q1, s0, s1;                        // q_t, h_t
+                        unpack2(r[i], q0, q1);
+                        q0 = fmaf(g.x, c[i], q0), q1 = fmaf(g.y, c[i], q1);
+                        const f2 co = pack2(q0, q1);
                         unpack2(h[u + 1][i], s0, s1);
                         bc[i] = fmaf(q1, in1, q0 * in0);
                         bc[4 + i] = fmaf(s1, g.y, s0 * g.x);
