@@ -24,6 +24,14 @@ template <> __device__ __forceinline__ __half from_f<__half>(float v) { return _
 // V elements that are loaded and stored together
 template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
 
+// First thing in kernels that are launched with launch_early (block_host.h): their blocks are set up while the kernel in front of
+// them in the stream ends, and go on once all of it is done and visible; the same is allowed to the kernel behind.
+__device__ __forceinline__ void wait_for_previous()
+{
+    asm volatile("griddepcontrol.launch_dependents;");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // A load under a predicate, zero without it.  Written out so that no branch is left around it: where two paths join
 // behind a load, its result is waited for.
 template <typename P> __device__ __forceinline__ P load_if(const P* from, bool ok)

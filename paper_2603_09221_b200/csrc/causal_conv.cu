@@ -222,8 +222,7 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
         constexpr bool ALIGNED = decltype(ac)::value;
         const dim3 grid((unsigned)a->batch, (a->d + V * kThreads - 1) / (V * kThreads));
-        conv_step_kernel<T, V, ALIGNED, W><<<grid, kThreads, 0, st>>>(p);
-        return launched("causal convolution, one token");
+        return launch_early("causal convolution, one token", conv_step_kernel<T, V, ALIGNED, W>, grid, kThreads, st, p);
     });
 }
 

@@ -268,6 +268,7 @@ __global__ void __launch_bounds__(kThreads, 10) conv_kernel(const ConvDev p)
 template <typename T, int V, bool ALIGNED, int W>
 __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvDev p)
 {
+    wait_for_previous();
     const int c = (blockIdx.y * kThreads + threadIdx.x) * V;
     if (c >= p.d)
         return;

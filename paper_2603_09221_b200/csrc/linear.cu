@@ -374,8 +374,7 @@ int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_
             using OT = decltype(t);
             auto go = [&](auto tc, auto nt) {
                 using T = decltype(tc);
-                few_rows_kernel<T, OT, decltype(nt)::value><<<(a->m + 15) / 16, kFewWarps * 32, 0, st>>>(f);
-                return launched("projection of few rows");
+                return launch_early("projection of few rows", few_rows_kernel<T, OT, decltype(nt)::value>, dim3((a->m + 15) / 16), kFewWarps * 32, st, f);
             };
             auto by_rows = [&](auto tc) {
                 return a->rows <= 8 ? go(tc, std::integral_constant<int, 1>()) : a->rows <= 16 ? go(tc, std::integral_constant<int, 2>())

@@ -66,6 +66,7 @@ template <typename T, typename OT> __device__ __forceinline__ void finish(const 
 template <typename T, typename OT, int NT>
 __global__ void __launch_bounds__(kFewWarps * 32) few_rows_kernel(const FewDev p)
 {
+    wait_for_previous();
     __shared__ float part[kFewWarps][NT * 8][17];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     const int f0 = blockIdx.x * 16;

@@ -480,6 +480,7 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
 template <typename T, int LANES>
 __global__ void __launch_bounds__(kStepThreads, 12) scan_step_kernel(const ScanDev p)
 {
+    wait_for_previous();
     constexpr int CH = kStepThreads / LANES;
     const int tid = threadIdx.x, sub = tid % LANES, ch = tid / LANES;
     const long long b = blockIdx.x;
