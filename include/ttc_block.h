@@ -74,7 +74,7 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream);
 
 /*
  * One token of each of `batch` sequences (tokens and seq_offsets are ignored; row b of x and y is element b * bstride):
- * y as above, and the window `state` moves on by one token in place.  state_out is not used.
+ * y as above, and the window in `state_out` moves on by one token in place.  state is not used.
  */
 int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stream);
 

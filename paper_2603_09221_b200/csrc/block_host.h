@@ -127,6 +127,12 @@ inline bool rows_overlap(const ttc_rows& a, int64_t wa, const ttc_rows& b, int64
     return shift < wa || shift + wb > period;
 }
 
+inline bool ranges_meet(const void* a, size_t bytes_a, const void* b, size_t bytes_b)
+{
+    const char *a0 = static_cast<const char*>(a), *b0 = static_cast<const char*>(b);
+    return a0 && b0 && a0 < b0 + bytes_b && b0 < a0 + bytes_a;
+}
+
 // Parts of a workspace, each aligned to 256 bytes.
 struct Scratch {
     char* base;

@@ -29,6 +29,8 @@ int check(const ttc_conv_args* a, bool step)
     return check_floats("state_out", a->state_out, true, element_size(a->dtype));
 }
 
+size_t window_bytes(const ttc_conv_args* a) { return (size_t)a->batch * (a->taps - 1) * a->d * element_size(a->dtype); }
+
 // Channels that a thread takes, and whether every pointer and stride allows one access for them: else they are two, one by one.
 struct Width {
     size_t size;
@@ -125,7 +127,8 @@ int plan_grad(int device, const ttc_conv_args* a, const ttc_conv_grads* g, void*
     if (rows_overlap(g->dx, a->d, a->x, a->d, a->batch, a->tokens, packed, size) ||
         rows_overlap(g->dx, a->d, g->dy, a->d, a->batch, a->tokens, packed, size))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "dx overlaps x or dy");
-    if (g->dstate && (g->dstate == g->dstate_out || g->dstate == a->state))
+    const size_t bytes = window_bytes(a);
+    if (ranges_meet(g->dstate, bytes, g->dstate_out, bytes) || ranges_meet(g->dstate, bytes, a->state, bytes))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "dstate overlaps state or dstate_out");
     ConvDev& p = o.p;
     p = to_dev(a, false);
@@ -164,6 +167,10 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
     const bool packed = a->seq_offsets;
     if (rows_overlap(a->y, a->d, a->x, a->d, a->batch, a->tokens, packed, element_size(a->dtype)))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "y overlaps x");
+    const size_t bytes = window_bytes(a);
+    const bool in_place = ranges_meet(a->state, bytes, a->state_out, bytes);
+    if (in_place && a->state != a->state_out)
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "state_out overlaps parts of state");
     DeviceScope scope;
     TTC_TRY(scope.enter(device));
     if (a->batch == 0)
@@ -174,10 +181,6 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
     w.window(a->state);
     ConvDev p = to_dev(a, false);
     set_tiles(p, w.v, sm_count(device));
-    // any overlap of the windows in front and behind
-    const size_t bytes = (size_t)a->batch * (a->taps - 1) * a->d * element_size(a->dtype);
-    const char *s0 = static_cast<const char*>(a->state), *s1 = static_cast<const char*>(a->state_out);
-    const bool in_place = s0 && s1 && s0 < s1 + bytes && s1 < s0 + bytes;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     return by_shape<false>(a->dtype, w, a->taps, [&](auto t, auto vc, auto ac, auto wc) {
         using T = decltype(t);

@@ -1,6 +1,8 @@
 // Host side of ttc_linear and ttc_linear_grad.
 #include <cuda.h>
 
+#include <initializer_list>
+
 #include "block_host.h"
 #include "linear_rows.cuh"
 
@@ -45,6 +47,20 @@ int encode(CUtensorMap& map, const void* ptr, int64_t rows, int64_t cols, int64_
 }
 
 bool aligned(const void* p, int64_t ld, size_t size) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld * (int64_t)size % 16 == 0; }
+
+// Matrices of a call that share elements, or may (rows_overlap); of different types or numbers of rows: ranges that meet.
+struct Matrix {
+    const void* ptr;
+    int64_t rows, cols, ld;
+    size_t size;
+    size_t bytes() const { return rows > 0 ? (size_t)((rows - 1) * ld + cols) * size : 0; }
+};
+bool meet(const Matrix& a, const Matrix& b)
+{
+    if (a.size != b.size || a.rows != b.rows)
+        return ranges_meet(a.ptr, a.bytes(), b.ptr, b.bytes());
+    return rows_overlap(ttc_rows{const_cast<void*>(a.ptr), 0, a.ld}, a.cols, ttc_rows{const_cast<void*>(b.ptr), 0, b.ld}, b.cols, 1, a.rows, false, a.size);
+}
 
 // An operand of a product in memory: `rows` rows of `cols` elements.
 struct Operand {
@@ -230,12 +246,13 @@ int plan_linear(int device, const ttc_linear_args* a, void* ws, LinearPlan& o)
     TTC_TRY(check_floats("residual", a->residual, true, size));
     if (a->rows > 1 && (a->ldy < a->m || (a->residual && a->ldr < a->m)))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
-    auto rows = [](const void* p, int64_t ld) { return ttc_rows{const_cast<void*>(p), 0, ld}; };
-    auto clash = [&](const void* out, int64_t ld) {
-        return rows_overlap(rows(out, ld), a->m, rows(a->x, a->ldx), a->k, 1, a->rows, false, 2);
-    };
-    if ((a->out_dtype == a->dtype && clash(a->y, a->ldy)) || (a->pre && clash(a->pre, a->ldp)))
-        return fail(TTC_STATUS_INVALID_ARGUMENT, "y or pre overlaps x");
+    const Matrix y{a->y, a->rows, a->m, a->ldy, size}, pre{a->pre, a->rows, a->m, a->ldp, 2}, r{a->residual, a->rows, a->m, a->ldr, size};
+    for (const Matrix& in : {Matrix{a->x, a->rows, a->k, a->ldx, 2}, Matrix{a->w, a->m, a->k, a->ldw, 2}})
+        if (meet(y, in) || meet(pre, in))
+            return fail(TTC_STATUS_INVALID_ARGUMENT, "y or pre overlaps x or w");
+    const bool in_place = a->y == a->residual && (a->rows == 1 || a->ldy == a->ldr);
+    if (meet(pre, y) || meet(pre, r) || (!in_place && meet(y, r)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "y, pre and parts of residual overlap");
     const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
     Scratch s(ws);
     o.few = a->rows <= kFewRows;
@@ -273,8 +290,13 @@ int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, v
         return fail(TTC_STATUS_INVALID_ARGUMENT, "pre is null: the gradients of an activation need it");
     if ((a->rows > 1 && (g->lddy < a->m || (g->dx && g->lddx < a->k))) || (g->dw && a->m > 1 && g->lddw < a->k))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "row strides shorter than the rows");
-    if (g->dx && rows_overlap(ttc_rows{g->dx, 0, g->lddx}, a->k, ttc_rows{const_cast<void*>(a->x), 0, a->ldx}, a->k, 1, a->rows, false, 2))
-        return fail(TTC_STATUS_INVALID_ARGUMENT, "dx overlaps x");
+    const Matrix dx{g->dx, a->rows, a->k, g->lddx, 2}, dw{g->dw, a->m, a->k, g->lddw, 2};
+    for (const Matrix& in : {Matrix{a->x, a->rows, a->k, a->ldx, 2}, Matrix{a->w, a->m, a->k, a->ldw, 2}, Matrix{g->dy, a->rows, a->m, g->lddy, size},
+                             Matrix{a->act == TTC_ACT_NONE ? nullptr : a->pre, a->rows, a->m, a->ldp, 2}})
+        if (meet(dx, in) || meet(dw, in))
+            return fail(TTC_STATUS_INVALID_ARGUMENT, "dx or dw overlaps an input");
+    if (meet(dx, dw))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "dx and dw overlap");
     const int sms = sm_count(device);
     const int64_t ldx = a->rows > 1 ? a->ldx : (a->k + 7) / 8 * 8, ldw = a->m > 1 ? a->ldw : (a->k + 7) / 8 * 8;
     const int64_t lddy = a->rows > 1 ? g->lddy : (a->m + 7) / 8 * 8;

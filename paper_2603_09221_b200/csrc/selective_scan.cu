@@ -37,8 +37,12 @@ int check(const ttc_scan_args* a, bool step)
 
 bool same_rows(const ttc_rows& a, const ttc_rows& b) { return a.ptr == b.ptr && a.tstride == b.tstride && a.bstride == b.bstride; }
 
+size_t state_bytes(const ttc_scan_args* a) { return (size_t)a->batch * a->d * a->n * sizeof(float); }
+
 int check_output(const ttc_scan_args* a, bool step)
 {
+    if (!step && a->state != a->state_out && ranges_meet(a->state, state_bytes(a), a->state_out, state_bytes(a)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "state_out overlaps parts of state");
     TTC_TRY(check_rows("y", a->y, a->dtype, a->batch == 0 || (!step && a->tokens == 0)));
     const int64_t tokens = step ? 1 : a->tokens, shared = (int64_t)a->groups * a->n;
     const bool packed = !step && a->seq_offsets;
@@ -199,6 +203,8 @@ int plan_grad(int device, const ttc_scan_args* a, const ttc_scan_grads* g, void*
     TTC_TRY(check_floats("dD", g->dD, true));
     TTC_TRY(check_floats("ddelta_bias", g->ddelta_bias, true));
     TTC_TRY(check_floats("dstate", g->dstate, true));
+    if (ranges_meet(g->dstate, state_bytes(a), a->state, state_bytes(a)) || ranges_meet(g->dstate, state_bytes(a), g->dstate_out, state_bytes(a)))
+        return fail(TTC_STATUS_INVALID_ARGUMENT, "dstate overlaps state or dstate_out");
     GradDev& p = o.g;
     p = GradDev{};
     p.f = to_dev(a, false, true);

@@ -140,9 +140,10 @@ __device__ __forceinline__ void run_states(const ScanDev& p, const Piece& q, int
             for (int i = 0; i < 4; ++i) {
                 const bool ok = have && n0 + i < p.n;
                 a[c][i] = ok ? exponent(p.A[my * p.n + n0 + i]) : 0.f;
-                h[c][i] = !LOCAL && q.t0 == 0 && ok && p.state ? p.state[(q.seq * p.d + my) * p.n + n0 + i] : 0.f;
+                h[c][i] = !LOCAL && !p.piece && ok && p.state ? p.state[(q.seq * p.d + my) * p.n + n0 + i] : 0.f;
             }
-            if (!LOCAL && q.t0 > 0 && have) {
+            // (state itself may be overwritten already by the last piece)
+            if (!LOCAL && p.piece && have) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (n0 + i < p.n)

@@ -110,11 +110,47 @@ def test_linear(kw, status):
 
 def test_linear_gradients():
     lib = block._load()
-    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=3 * P, dx=4 * P, dw=P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
+    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=3 * P, dx=4 * P, dw=5 * P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
     assert lib.ttc_linear_grad_workspace(0, _linear(), grads()) >= 0
     for kw in (dict(dy=0), dict(lddy=47), dict(lddx=31), dict(lddw=31), dict(dbias=P + 1), dict(dx=P)):
         assert _status(lib.ttc_linear_grad_workspace, 0, _linear(), grads(**kw))[0] == INVALID, kw
     assert _status(lib.ttc_linear_grad_workspace, 0, _linear(act=2), grads())[0] == INVALID       # no pre
+
+
+def test_outputs_that_overlap():
+    lib = block._load()
+    status = lambda f, *args: _status(getattr(lib, f), 0, *args)[0]  # noqa: E731
+    # windows and states: in place or apart, not in part (one sequence's window is 3 x 16 x 2 bytes, its state 16 x 16 x 4)
+    for out, want in ((6 * P + 96, INVALID), (6 * P - 2, INVALID)):
+        assert status("ttc_causal_conv", _conv(state=6 * P, state_out=out), None) == want
+    for out, want in ((6 * P + 1024, INVALID), (6 * P - 4, INVALID)):
+        assert status("ttc_selective_scan", _scan(state=6 * P, state_out=out), None, 0, None) == want
+    conv = lambda **kw: block._CONV_GRADS.pack(*{**dict(dy=3 * P, dyb=128, dyt=16, dx=4 * P, dxb=128, dxt=16, dstate_out=0, dw=P, dbias=P, dstate=0), **kw}.values())  # noqa: E731
+    for out, want in ((6 * P, INVALID), (6 * P + 96, INVALID), (7 * P + 2, INVALID), (8 * P, True)):
+        got = status("ttc_causal_conv_grad_workspace", _conv(state=6 * P), conv(dstate=out, dstate_out=7 * P))
+        assert got == want or (want is True and got >= 0)
+
+    def scan(**kw):
+        a = dict(dy=3 * P, dyb=128, dyt=16, dx=4 * P, dxb=128, dxt=16)
+        for k in ("ddelta", "dB", "dC", "dz"):
+            a.update({k: 0, k + "b": 0, k + "t": 0})
+        a.update(dstate_out=0, dA=0, dD=0, ddelta_bias=0, dstate=0)
+        a.update(kw)
+        return block._SCAN_GRADS.pack(*a.values())
+
+    for out, want in ((6 * P, INVALID), (6 * P + 1024, INVALID), (7 * P + 4, INVALID), (8 * P, True)):
+        got = status("ttc_selective_scan_grad_workspace", _scan(state=6 * P), scan(dstate=out, dstate_out=7 * P))
+        assert got == want or (want is True and got >= 0)
+    # matrices: y and pre with x, W and one another, y with parts of r; columns of one wider matrix are apart
+    for kw, want in ((dict(w=5 * P, y=5 * P + 64), INVALID), (dict(w=5 * P, pre=5 * P - 2), INVALID), (dict(pre=2 * P + 32), INVALID),
+                     (dict(residual=2 * P + 32), INVALID), (dict(residual=2 * P, ldr=64), INVALID), (dict(residual=2 * P), 0), (dict(residual=2 * P + 96, ldr=96, ldy=96), 0),
+                     (dict(out_dtype=0, y=P + 4000), INVALID), (dict(out_dtype=0, pre=P, x=5 * P, y=P + 8), INVALID)):
+        assert status("ttc_linear_workspace", _linear(**{**dict(w=9 * P), **kw})) == want, kw
+    grads = lambda **kw: block._LINEAR_GRADS.pack(*{**dict(dy=3 * P, dx=4 * P, dw=5 * P, dbias=P, lddy=48, lddx=32, lddw=32), **kw}.values())  # noqa: E731
+    for kw, want in ((dict(dx=3 * P), INVALID), (dict(dx=3 * P + 96, lddx=96, lddy=96), True), (dict(dx=9 * P), INVALID), (dict(dw=9 * P + 64), INVALID), (dict(dw=3 * P), INVALID),
+                     (dict(dw=P), INVALID), (dict(dx=5 * P + 2), INVALID), (dict(dx=7 * P + 2), INVALID), (dict(), True)):
+        got = status("ttc_linear_grad_workspace", _linear(w=9 * P, pre=7 * P, act=2), grads(**kw))
+        assert got == want or (want is True and got >= 0), kw
 
 
 def test_null_records():

@@ -194,3 +194,40 @@ def test_the_short_way_refuses_what_the_long_one_refuses():
     for bad in (dict(w=h[:, :7]), dict(w=h.float()), dict(bias=x), dict(residual=h), dict(act="tanh"), dict(x=x), dict(out_dtype=torch.bfloat16), dict(y=h)):
         with pytest.raises((ValueError, TypeError, lqr.TtcError)):
             block.linear(**{**dict(x=h, w=torch.zeros((5, 8), device=DEV, dtype=H)), **bad})
+
+
+def test_single_tokens_captured_behind_joins_copies_and_fills():
+    """The kernels of single tokens are launched while what is in front of them ends: of every kind, and from two streams at once."""
+    g = torch.Generator(device=DEV).manual_seed(21)
+    r = lambda *s, t=H: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+    w, x0, x1, taps, A = r(64, 96), r(2, 5, 96), r(2, 5, 64), r(64, 4, t=F), -torch.rand((64, 16), generator=g, device=DEV)
+    x, other, window, state = r(5, 96), r(5, 64), r(5, 3, 64), r(5, 64, 16, t=F)
+    first = window.clone(), state.clone()
+    B = r(5, 16)
+
+    def run():
+        here, aside = torch.cuda.current_stream(), torch.cuda.Stream()
+        aside.wait_stream(here)
+        with torch.cuda.stream(aside):
+            other.copy_(x1[0])                                       # one branch ends in a copy
+        x.copy_(x0[0])                                               # so does the other
+        here.wait_stream(aside)
+        u = block.linear(x, w)                                       # behind a join
+        c = block.causal_conv_step(u + other, taps, window, act="silu")              # behind a kernel of torch
+        window[0].zero_()                                            # a fill
+        y = block.selective_scan_step(c, other, A, B, B, state, softplus=True)
+        return y, block.causal_conv_step(y, taps, window)
+
+    want = [t.clone() for t in (*run(), window, state)]
+    window.copy_(first[0]), state.copy_(first[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = run()
+    for again in range(3):
+        window.copy_(first[0]), state.copy_(first[1])
+        x.zero_(), other.zero_()
+        graph.replay()
+        for a, b in zip((*got, window, state), want):
+            assert torch.equal(a, b), again
