@@ -172,17 +172,22 @@ inline int launched(const char* what)
 
 // Launch of a kernel that begins with wait_for_previous: what a launch costs behind another one (about 1 us) overlaps with that
 // one's end.  For the kernels of single tokens, which take 3 to 5 us.
-template <typename... P, typename... A> int launch_early(const char* what, void (*kernel)(P...), dim3 grid, int threads, cudaStream_t st, const A&... args)
+// `cluster`: blocks of a cluster, along y.
+template <typename... P, typename... A>
+int launch_early(const char* what, void (*kernel)(P...), dim3 grid, int threads, int cluster, cudaStream_t st, const A&... args)
 {
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
     c.blockDim = dim3(threads);
     c.stream = st;
-    cudaLaunchAttribute early;
-    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    early.val.programmaticStreamSerializationAllowed = 1;
-    c.attrs = &early;
-    c.numAttrs = 1;
+    cudaLaunchAttribute with[2];
+    with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    with[0].val.programmaticStreamSerializationAllowed = 1;
+    with[1].id = cudaLaunchAttributeClusterDimension;
+    with[1].val.clusterDim.x = with[1].val.clusterDim.z = 1;
+    with[1].val.clusterDim.y = cluster;
+    c.attrs = with;
+    c.numAttrs = cluster > 1 ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelEx(&c, kernel, P(args)...);
     return e == cudaSuccess ? launched(what) : fail(TTC_STATUS_CUDA_ERROR, "%s: %s", what, cudaGetErrorString(e));
 }

@@ -215,8 +215,9 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
     w.rows(a->x, false, true);
     w.rows(a->y, false, true);
     w.window(a->state_out);
-    // few sequences: narrower loads keep more SMs at work
-    if (w.v > 2 && a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads)) < sm_count(device))
+    // Narrower loads until every SM has many blocks (d = 4096: 64 sequences 2.7 us by four channels to a thread, 2.1 by two; 256
+    // 5.5 and 5.3; 1024 16.2 and 17.8).
+    if (w.v > 2 && a->batch * ((a->d + w.v * kThreads - 1) / (w.v * kThreads)) < 16 * (int64_t)sm_count(device))
         w.v = 2;
     const ConvDev p = to_dev(a, true);
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -225,7 +226,7 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
         constexpr bool ALIGNED = decltype(ac)::value;
         const dim3 grid((unsigned)a->batch, (a->d + V * kThreads - 1) / (V * kThreads));
-        return launch_early("causal convolution, one token", conv_step_kernel<T, V, ALIGNED, W>, grid, kThreads, st, p);
+        return launch_early("causal convolution, one token", conv_step_kernel<T, V, ALIGNED, W>, grid, kThreads, 1, st, p);
     });
 }
 

@@ -15,6 +15,15 @@ namespace {
 // Rows up to which W is streamed past all of x (few_rows_kernel) instead of going through tiles of 128 rows.
 constexpr int kFewRows = 32;
 
+// Parts of the contraction of few_rows_kernel
+int few_parts(int64_t blocks, int64_t k, int sms)
+{
+    int parts = 1;
+    while (parts < 8 && 2 * parts * blocks <= 2 * sms && k >= parts * 2 * 1024)
+        parts *= 2;
+    return parts;
+}
+
 typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
@@ -99,23 +108,29 @@ struct Product {
     int64_t M, N, K;
     int bn, splits;
     bool pair;                   // two CTAs on tiles of 256 x 256
+    bool segments;               // added up in registers, every kSegment contraction indices
     float* part;
 };
-
-constexpr int64_t kPairCost = 3050, kSegment = 512, kLong = 1024;
 
 // Width of a tile and parts of the contraction.  A block of 64 contraction indices takes about 400 + 1.75 BN clocks: filling
 // and reading its (128 + BN) x 128 bytes of shared memory, twice 128 + BN clocks, and what goes with it; so the width is the
 // one with the least of that times the rounds of tiles over the SMs (512 x 4096 results over 2048 indices: 64 wide 21.9 us in two
-// rounds, 128 wide in one 15).  Results with few tiles split the contraction too, in parts of at least 512 indices that a
-// launch of its own sums.
+// rounds, 128 wide in one 15).  In the same unit (a quarter of a clock) a pair's block costs kPairCost: 8192 x 2048 over 4096 99 us
+// in pairs and 105 without, 4096 x 2048 over 2048 28.9 and 30.4, but 512 x 4096 over 2048 18.0 and 14.7, 1024 x 2304 over 1024 13.4 and 10.4.
+constexpr int64_t kPairCost = 3050;
+// Results with few tiles split the contraction too, in parts of at least 512 indices that a launch of its own sums.  That
+// costs about 4 us, a block of 64 about 0.2: 64 x 2048 over 4096 (four parts) 19.6 -> 11.8 us, 256 x 2048 over 4096 (two) 20.1 -> 17.5, but
+// 128 x 4096 over 2048 (two) 12.5 -> 13.9 and 64 x 1024 over 1024 7.6 -> 8.4; so as many blocks have to be saved:
+constexpr int64_t kWorthSplit = 24;
+// float32 results: contractions longer than kLong are added up in registers every kSegment indices.
+constexpr int64_t kSegment = 512, kLong = 1024;
+
 Product plan_product(int64_t M, int64_t N, int64_t K, bool f32, int sms, Scratch& s)
 {
-    Product p{M, N, K, 256, 1, false, nullptr};
+    Product p{M, N, K, 256, 1, false, f32 && K > kLong, nullptr};
     const int64_t tm = (M + BM - 1) / BM;
     int64_t least = INT64_MAX;
-    const bool exact = f32 && K > kLong;      // float32 results of a long contraction: segments, which the 128 wide tile has
-    for (int bn = exact ? 128 : 256; bn >= (exact ? 128 : 64); bn /= 2) {
+    for (int bn = p.segments ? 128 : 256; bn >= (p.segments ? 128 : 64); bn /= 2) {
         const int64_t rounds = (tm * ((N + bn - 1) / bn) + sms - 1) / sms, cost = rounds * (1600 + 7 * bn);
         if (cost < least) {
             least = cost;
@@ -123,28 +138,26 @@ Product plan_product(int64_t M, int64_t N, int64_t K, bool f32, int sms, Scratch
         }
     }
     const int64_t pairs = sms / 2, rounds = ((M + 2 * BM - 1) / (2 * BM) * ((N + 255) / 256) + pairs - 1) / pairs;
-    if (!exact && rounds * kPairCost < least) {
+    if (rounds * kPairCost < least) {
         p.pair = true;
         p.bn = 256;
         return p;
     }
-    const int64_t tiles = tm * ((N + p.bn - 1) / p.bn);
-    if (2 * tiles <= sms) {
-        const int64_t most = K / 512, want = sms / tiles;
-        p.splits = (int)(want < most ? want : most);
-        if (p.splits < 2)
-            p.splits = 1;
-    }
-    if (p.splits > 1)
+    const int64_t tiles = tm * ((N + p.bn - 1) / p.bn), blocks = (K + BK - 1) / BK;
+    int64_t splits = sms / tiles < K / 512 ? sms / tiles : K / 512;
+    if (splits > 1 && blocks - blocks / splits >= kWorthSplit) {
+        p.splits = (int)splits;
         p.part = s.take<float>((size_t)p.splits * M * N);
+    }
     return p;
 }
 
-template <bool A_MN, bool B_MN, int BN, bool PAIR, typename OT> int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool is_bf16, int sms, cudaStream_t st)
+template <bool A_MN, bool B_MN, int BN, bool PAIR, bool SEGMENTS, typename OT>
+int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool is_bf16, int sms, cudaStream_t st)
 {
     using S = GemmShape<BN, PAIR>;
     constexpr int CTAS = PAIR ? 2 : 1;
-    auto* kernel = gemm_kernel<A_MN, B_MN, BN, PAIR, OT>;
+    auto* kernel = gemm_kernel<A_MN, B_MN, BN, PAIR, OT, SEGMENTS>;
     TTC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
     g.tiles_m = (int)((g.M + CTAS * BM - 1) / (CTAS * BM));
     g.tiles_n = (int)((g.N + BN - 1) / BN);
@@ -188,12 +201,16 @@ template <bool A_MN, bool B_MN> int product(const Product& q, const Operand& a, 
     const int type = q.splits > 1 ? (int)TTC_F32 : out_dtype;
     TTC_TRY(by_type(type, [&](auto t) {
         using OT = decltype(t);
+        if constexpr (!A_MN && !B_MN && sizeof(OT) == 4)             // (only the forward product has float32 results)
+            if (q.segments)
+                return q.pair ? launch_tiles<A_MN, B_MN, 256, true, true, OT>(ma, mb, g, is_bf16, sms, st)
+                              : launch_tiles<A_MN, B_MN, 128, false, true, OT>(ma, mb, g, is_bf16, sms, st);
         if (q.pair)
-            return launch_tiles<A_MN, B_MN, 256, true, OT>(ma, mb, g, is_bf16, sms, st);
+            return launch_tiles<A_MN, B_MN, 256, true, false, OT>(ma, mb, g, is_bf16, sms, st);
         switch (q.bn) {
-        case 256: return launch_tiles<A_MN, B_MN, 256, false, OT>(ma, mb, g, is_bf16, sms, st);
-        case 128: return launch_tiles<A_MN, B_MN, 128, false, OT>(ma, mb, g, is_bf16, sms, st);
-        default: return launch_tiles<A_MN, B_MN, 64, false, OT>(ma, mb, g, is_bf16, sms, st);
+        case 256: return launch_tiles<A_MN, B_MN, 256, false, false, OT>(ma, mb, g, is_bf16, sms, st);
+        case 128: return launch_tiles<A_MN, B_MN, 128, false, false, OT>(ma, mb, g, is_bf16, sms, st);
+        default: return launch_tiles<A_MN, B_MN, 64, false, false, OT>(ma, mb, g, is_bf16, sms, st);
         }
     }));
     if (q.splits == 1)
@@ -396,7 +413,11 @@ int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_
             using OT = decltype(t);
             auto go = [&](auto tc, auto nt) {
                 using T = decltype(tc);
-                return launch_early("projection of few rows", few_rows_kernel<T, OT, decltype(nt)::value>, dim3((a->m + 15) / 16), kFewWarps * 32, st, f);
+                constexpr int NT = decltype(nt)::value, COLS = FewShape<NT>::COLS;
+                const int blocks = (a->m + COLS - 1) / COLS;
+                const int parts = few_parts(blocks, a->k, sm_count(device));
+                f.part = (a->k + 256 * parts - 1) / (256 * parts) * 256;
+                return launch_early("projection of few rows", few_rows_kernel<T, OT, NT>, dim3(blocks, parts), kFewWarps * 32, parts, st, f);
             };
             auto by_rows = [&](auto tc) {
                 return a->rows <= 8 ? go(tc, std::integral_constant<int, 1>()) : a->rows <= 16 ? go(tc, std::integral_constant<int, 2>())

@@ -9,17 +9,24 @@ namespace lin {
 
 // ---- few rows -----------------------------------------------------------------------------------------------------------
 //
-// Up to 8 NT rows (tokens) against all of W: W is read once, which bounds it.  A block takes 16 rows of W and its eight
-// warps deal out the contraction; each lane loads 16 contiguous bytes of two rows of W and of one row of x, which are the
+// Up to 8 NT rows (tokens) against all of W: W is read once, which bounds it.  A block takes 16 MT rows of W and a part of
+// the contraction (a cluster shares the parts out and adds them up over shared memory of its blocks); its eight
+// warps deal that out again.  Each lane loads 16 contiguous bytes of two rows of W for every 16, and of one row of x for every 8, which are the
 // operands of two mma.sync.m16n8k16: the instruction does not mind which contraction index a slot stands for, as long as
 // both operands agree, so nothing is rearranged or staged.
 
-constexpr int kFewWarps = 8, kFewAhead = 8;
+constexpr int kFewWarps = 8;
+
+// Rows of x (8 NT) and of W (16 MT) of a block, and as many steps of 32 contraction indices as have their loads under way together.
+template <int NT> struct FewShape {
+    static constexpr int MT = NT == 4 ? 2 : 1, AHEAD = NT == 1 ? 8 : NT == 2 ? 4 : 2, COLS = 16 * MT;
+};
 
 struct FewDev {
     const void *x, *w;
     long long ldx, ldw;
     int rows, k, m;
+    int part;                    // contraction indices of a block, a multiple of 8 where there is more than one part
     int vec;                     // rows of x and W can be read by 16 bytes, and end on them
     Epilogue e;
 };
@@ -64,58 +71,83 @@ template <typename T, typename OT> __device__ __forceinline__ void finish(const 
 }
 
 template <typename T, typename OT, int NT>
-__global__ void __launch_bounds__(kFewWarps * 32) few_rows_kernel(const FewDev p)
+__global__ void __launch_bounds__(kFewWarps * 32, 2) few_rows_kernel(const FewDev p)
 {
     wait_for_previous();
-    __shared__ float part[kFewWarps][NT * 8][17];
+    using S = FewShape<NT>;
+    constexpr int MT = S::MT, AHEAD = S::AHEAD, COLS = S::COLS;
+    __shared__ float part[kFewWarps][NT * 8][COLS + 1];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
-    const int f0 = blockIdx.x * 16;
-    const T *w = static_cast<const T*>(p.w), *x = static_cast<const T*>(p.x);
-    const T *w0 = w + (long long)(f0 + g) * p.ldw, *w1 = w + (long long)(f0 + g + 8) * p.ldw;
-    const bool ok0 = f0 + g < p.m, ok1 = f0 + g + 8 < p.m;
-    float acc[NT][4] = {};
-    auto load = [&](const T* row, bool ok, int k) { return load8(row, ok, k, p.k, p.vec); };
-    // all of W's loads of a round first, and x's with them while they are few
-    constexpr bool TOGETHER = NT == 1;
-    for (int k0 = warp * 32; k0 < p.k; k0 += kFewWarps * 32 * kFewAhead) {
-        uint4 a0[kFewAhead], a1[kFewAhead], b0[TOGETHER ? kFewAhead : 1];
+    const int f0 = blockIdx.x * COLS, parts = gridDim.y;
+    const int begin = blockIdx.y * p.part, end = min(p.k, begin + p.part);
+    const T *w = static_cast<const T*>(p.w) + (long long)(f0 + g) * p.ldw, *x = static_cast<const T*>(p.x) + (long long)g * p.ldx;
+    const long long w8 = 8 * p.ldw, x8 = 8 * p.ldx;
+    float acc[MT][NT][4] = {};
+    for (int k0 = begin + warp * 32; k0 < end; k0 += kFewWarps * 32 * AHEAD) {       // (the same for all lanes: mma.sync is theirs together)
+        uint4 a[AHEAD][2 * MT], b[AHEAD][NT];
 #pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) {
-            const int k = k0 + i * kFewWarps * 32 + t * 8;
-            a0[i] = load(w0, ok0, k);
-            a1[i] = load(w1, ok1, k);
-            if (TOGETHER)
-                b0[TOGETHER ? i : 0] = load(x + (long long)g * p.ldx, g < p.rows, k);
-        }
-#pragma unroll
-        for (int i = 0; i < kFewAhead; ++i) {
+        for (int i = 0; i < AHEAD; ++i) {
             const int k = k0 + i * kFewWarps * 32 + t * 8;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 b = TOGETHER ? b0[TOGETHER ? i : 0] : load(x + (long long)(n * 8 + g) * p.ldx, n * 8 + g < p.rows, k);
-                mma16816<T>(acc[n], a0[i].x, a1[i].x, a0[i].y, a1[i].y, b.x, b.y);
-                mma16816<T>(acc[n], a0[i].z, a1[i].z, a0[i].w, a1[i].w, b.z, b.w);
-            }
+            for (int j = 0; j < 2 * MT; ++j)
+                a[i][j] = load8(w + j * w8, f0 + g + 8 * j < p.m, k, end, p.vec);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                b[i][n] = load8(x + n * x8, n * 8 + g < p.rows, k, end, p.vec);
         }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+            for (int j = 0; j < MT; ++j)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const uint4 &a0 = a[i][2 * j], &a1 = a[i][2 * j + 1];
+                    mma16816<T>(acc[j][n], a0.x, a1.x, a0.y, a1.y, b[i][n].x, b[i][n].y);
+                    mma16816<T>(acc[j][n], a0.z, a1.z, a0.w, a1.w, b[i][n].z, b[i][n].w);
+                }
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        part[warp][n * 8 + 2 * t][g] = acc[n][0];
-        part[warp][n * 8 + 2 * t + 1][g] = acc[n][1];
-        part[warp][n * 8 + 2 * t][g + 8] = acc[n][2];
-        part[warp][n * 8 + 2 * t + 1][g + 8] = acc[n][3];
-    }
+    for (int j = 0; j < MT; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            part[warp][n * 8 + 2 * t][16 * j + g] = acc[j][n][0];
+            part[warp][n * 8 + 2 * t + 1][16 * j + g] = acc[j][n][1];
+            part[warp][n * 8 + 2 * t][16 * j + g + 8] = acc[j][n][2];
+            part[warp][n * 8 + 2 * t + 1][16 * j + g + 8] = acc[j][n][3];
+        }
     __syncthreads();
-    for (int i = threadIdx.x; i < NT * 8 * 16; i += kFewWarps * 32) {
-        const int row = i / 16, f = i % 16;
-        if (row >= p.rows || f0 + f >= p.m)
-            continue;
+    for (int i = threadIdx.x; i < NT * 8 * COLS; i += kFewWarps * 32) {
+        const int row = i / COLS, f = i % COLS;
         float z = 0.f;
 #pragma unroll
         for (int k = 0; k < kFewWarps; ++k)
             z += part[k][row][f];
+        if (parts > 1)
+            part[0][row][f] = z;                                     // for the cluster
+        else if (row < p.rows && f0 + f < p.m)
+            finish<T, OT>(p.e, row, f0 + f, z);
+    }
+    if (parts == 1)
+        return;
+    __syncwarp();
+    cluster_sync();
+    for (int i = blockIdx.y * (kFewWarps * 32) + threadIdx.x; i < NT * 8 * COLS; i += parts * (kFewWarps * 32)) {
+        const int row = i / COLS, f = i % COLS;
+        if (row >= p.rows || f0 + f >= p.m)
+            continue;
+        const uint32_t at = smem_u32(&part[0][row][f]);
+        float z = 0.f;
+        for (int s = 0; s < parts; ++s) {
+            uint32_t there;
+            float v;
+            asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(s));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+            z += v;
+        }
         finish<T, OT>(p.e, row, f0 + f, z);
     }
+    __syncwarp();
+    cluster_sync();                                                  // no block ends while another one reads its sums
 }
 
 // ---- the parts of a split contraction ---------------------------------------------------------------------------------

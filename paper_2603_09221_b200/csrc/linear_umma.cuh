@@ -149,6 +149,17 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, float (&v)[32])
     for (int i = 0; i < 32; ++i)
         v[i] = __uint_as_float(r[i]);
 }
+// eight columns added to v
+__device__ __forceinline__ void tmem_add8(uint32_t at, float* v)
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] += __uint_as_float(r[i]);
+}
 
 // Shared-memory descriptors (128-byte swizzle).  K-major: rows of 64 contraction indices, 128 bytes each, groups of eight
 // rows 1024 bytes apart; a step of 16 indices is 32 bytes further in.  MN-major: rows of 64 indices of the other dimension, one
@@ -260,15 +271,14 @@ template <int BN, bool PAIR> struct GemmShape {
     static constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + EPI_BYTES + 256;
 };
 
-template <bool A_MN, bool B_MN, int BN, bool PAIR, typename OT>
+// SEGMENTS: the tensor cores cut sums off instead of rounding them, an error that grows with the contraction (1.0e-6 of the
+// result's norm at 1024 indices); the results of longer ones are then added up in registers, segment by segment.
+template <bool A_MN, bool B_MN, int BN, bool PAIR, typename OT, bool SEGMENTS>
 __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                               const GemmDev p)
 {
     using S = GemmShape<BN, PAIR>;
     constexpr int STAGES = S::STAGES, CTAS = PAIR ? 2 : 1;
-    // The tensor cores cut sums off instead of rounding them, an error that grows with the contraction (1.0e-6 of the result's
-    // norm at 1024 indices): float32 results of longer ones are added up in registers, segment by segment.
-    constexpr bool SEGMENTS = sizeof(OT) == 4 && BN == 128 && !PAIR;
     extern __shared__ char smem_raw[];
     char* smem = reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) / 1024 * 1024);
     char* s_epi = smem + STAGES * S::STAGE_BYTES;
@@ -440,7 +450,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                 s_bias[c] = p.e.bias && col0 + c < p.N ? p.e.bias[col0 + c] : 0.f;
             __syncwarp();
             bool ok = true;
-            float sum[SEGMENTS ? BN / 64 : 1][32];
+            float sum[SEGMENTS ? BN / 64 : 1][32] = {};
             if (SEGMENTS) {
                 for (int k = k0; ok && k < k1; k += p.segment, ++done) {
                     if (!(ok = wait(acc_full + 8 * (done & 1), done / 2 & 1, dead)))
@@ -448,17 +458,16 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t from = tmem + (done & 1) * BN + half * (BN / 2) + ((uint32_t)(quarter * 32) << 16);
 #pragma unroll
-                    for (int c = 0; c < BN / 64; ++c) {
-                        float v[32];
-                        tmem_ld32(from + 32 * c, v);
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            sum[SEGMENTS ? c : 0][i] = k == k0 ? v[i] : sum[SEGMENTS ? c : 0][i] + v[i];
-                    }
+                    for (int c = 0; c < BN / 2; c += 8)
+                        tmem_add8(from + c, &sum[SEGMENTS ? c / 32 : 0][c % 32]);
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
-                    if (lane == 0)
-                        arrive(acc_empty + 8 * (done & 1));
+                    if (lane == 0) {
+                        if (PAIR)
+                            arrive_cluster(in_first(acc_empty + 8 * (done & 1)));
+                        else
+                            arrive(acc_empty + 8 * (done & 1));
+                    }
                 }
             } else {
                 ok = wait(acc_full + 8 * (done & 1), done / 2 & 1, dead);
