@@ -174,11 +174,12 @@ inline int launched(const char* what)
 // one's end.  For the kernels of single tokens, which take 3 to 5 us.
 // `cluster`: blocks of a cluster, along y.
 template <typename... P, typename... A>
-int launch_early(const char* what, void (*kernel)(P...), dim3 grid, int threads, int cluster, cudaStream_t st, const A&... args)
+int launch_early(const char* what, void (*kernel)(P...), dim3 grid, int threads, int smem, int cluster, cudaStream_t st, const A&... args)
 {
     cudaLaunchConfig_t c = {};
     c.gridDim = grid;
     c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
     c.stream = st;
     cudaLaunchAttribute with[2];
     with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

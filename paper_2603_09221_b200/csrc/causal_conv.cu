@@ -226,7 +226,7 @@ int ttc_causal_conv_step(int32_t device, const ttc_conv_args* a, void* cuda_stre
         constexpr int V = decltype(vc)::value, W = decltype(wc)::value;
         constexpr bool ALIGNED = decltype(ac)::value;
         const dim3 grid((unsigned)a->batch, (a->d + V * kThreads - 1) / (V * kThreads));
-        return launch_early("causal convolution, one token", conv_step_kernel<T, V, ALIGNED, W>, grid, kThreads, 1, st, p);
+        return launch_early("causal convolution, one token", conv_step_kernel<T, V, ALIGNED, W>, grid, kThreads, 0, 1, st, p);
     });
 }
 

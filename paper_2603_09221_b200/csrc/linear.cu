@@ -12,10 +12,14 @@ using namespace ttc::lin;
 
 namespace {
 
-// Rows up to which W is streamed past all of x (few_rows_kernel) instead of going through tiles of 128 rows.
+// Rows up to which W is streamed past all of x (few_rows_kernel) instead of going through tiles of 128 rows.  2048 -> 4096,
+// 1024 -> 1024 and 8192 -> 8192: 32 rows 9.3, 4.8 and 33.8 us, by tiles 11.9, 7.5 and 36.4; 64 rows 14.3, 8.2 and 58.6 (by a form for as
+// many), by tiles 12.3, 7.5 and 36.5.
 constexpr int kFewRows = 32;
 
-// Parts of the contraction of few_rows_kernel
+// Parts of the contraction of few_rows_kernel, the blocks of a cluster: while all blocks are at work at once, two to an SM, and a part has 1024
+// indices.  What a cluster costs is about 1.2 us: 8 rows, 4096 -> 2048 7.5 -> 6.4 us and 16 rows 16.9 -> 8.3 in 2 and 4 parts, but 1024 -> 1024
+// 2.7 -> 3.9; twice as many blocks 8 rows, 2048 -> 4096 5.7 -> 9.3.
 int few_parts(int64_t blocks, int64_t k, int sms)
 {
     int parts = 1;
@@ -417,7 +421,13 @@ int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_
                 const int blocks = (a->m + COLS - 1) / COLS;
                 const int parts = few_parts(blocks, a->k, sm_count(device));
                 f.part = (a->k + 256 * parts - 1) / (256 * parts) * 256;
-                return launch_early("projection of few rows", few_rows_kernel<T, OT, NT>, dim3(blocks, parts), kFewWarps * 32, parts, st, f);
+                static std::atomic<uint64_t> allowed;                // devices, a bit each, that know of its shared memory
+                const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+                if (FewShape<NT>::RING && !(allowed.load(std::memory_order_relaxed) & bit)) {
+                    TTC_CUDA(cudaFuncSetAttribute(few_rows_kernel<T, OT, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewShape<NT>::SMEM));
+                    allowed.fetch_or(bit, std::memory_order_relaxed);
+                }
+                return launch_early("projection of few rows", few_rows_kernel<T, OT, NT>, dim3(blocks, parts), kFewWarps * 32, FewShape<NT>::SMEM, parts, st, f);
             };
             auto by_rows = [&](auto tc) {
                 return a->rows <= 8 ? go(tc, std::integral_constant<int, 1>()) : a->rows <= 16 ? go(tc, std::integral_constant<int, 2>())

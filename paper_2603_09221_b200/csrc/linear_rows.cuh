@@ -17,9 +17,15 @@ namespace lin {
 
 constexpr int kFewWarps = 8;
 
-// Rows of x (8 NT) and of W (16 MT) of a block, and as many steps of 32 contraction indices as have their loads under way together.
+// Rows of W of a block (16 MT), loads of a lane for 32 contraction indices, and as many such steps as are under way together:
+// in registers, or, where those hold too few of them, in shared memory (2048 -> 4096 and 8192 -> 8192: 8 rows 5.7 and 28.9 us by
+// registers, 6.1 and 28.0 by shared memory; 16 rows 6.6 and 34.8, 7.0 and 32.0; 32 rows 9.9 and 40.1, 9.3 and 33.8).
 template <int NT> struct FewShape {
-    static constexpr int MT = NT == 4 ? 2 : 1, AHEAD = NT == 1 ? 8 : NT == 2 ? 4 : 2, COLS = 16 * MT;
+    static constexpr int MT = NT <= 2 ? 1 : 2, COLS = 16 * MT, LOADS = 2 * MT + NT;
+    static constexpr bool RING = NT > 2;
+    static constexpr int DEPTH = RING ? 24 / LOADS : NT == 1 ? 8 : 4;
+    static constexpr int SUMS = kFewWarps * NT * 8 * (COLS + 1) * 4, HELD = RING ? DEPTH * kFewWarps * LOADS * 32 * 16 : 0;
+    static constexpr int SMEM = HELD > SUMS ? HELD : SUMS;
 };
 
 struct FewDev {
@@ -75,37 +81,82 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) few_rows_kernel(const FewDe
 {
     wait_for_previous();
     using S = FewShape<NT>;
-    constexpr int MT = S::MT, AHEAD = S::AHEAD, COLS = S::COLS;
-    __shared__ float part[kFewWarps][NT * 8][COLS + 1];
+    constexpr int MT = S::MT, COLS = S::COLS, LOADS = S::LOADS, DEPTH = S::DEPTH;
+    extern __shared__ uint4 s_few[];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
     const int f0 = blockIdx.x * COLS, parts = gridDim.y;
     const int begin = blockIdx.y * p.part, end = min(p.k, begin + p.part);
     const T *w = static_cast<const T*>(p.w) + (long long)(f0 + g) * p.ldw, *x = static_cast<const T*>(p.x) + (long long)g * p.ldx;
     const long long w8 = 8 * p.ldw, x8 = 8 * p.ldx;
+    const int steps = (end - begin - warp * 32 + kFewWarps * 32 - 1) / (kFewWarps * 32);           // (the same for all lanes: mma.sync is theirs together)
+    auto index = [&](int step) { return begin + (step * kFewWarps + warp) * 32 + t * 8; };
     float acc[MT][NT][4] = {};
-    for (int k0 = begin + warp * 32; k0 < end; k0 += kFewWarps * 32 * AHEAD) {       // (the same for all lanes: mma.sync is theirs together)
-        uint4 a[AHEAD][2 * MT], b[AHEAD][NT];
+    auto multiply = [&](const uint4 (&a)[2 * MT], const uint4& b, int n) {
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int k = k0 + i * kFewWarps * 32 + t * 8;
+        for (int j = 0; j < MT; ++j) {
+            mma16816<T>(acc[j][n], a[2 * j].x, a[2 * j + 1].x, a[2 * j].y, a[2 * j + 1].y, b.x, b.y);
+            mma16816<T>(acc[j][n], a[2 * j].z, a[2 * j + 1].z, a[2 * j].w, a[2 * j + 1].w, b.z, b.w);
+        }
+    };
+    if constexpr (!S::RING) {
+        for (int i0 = 0; i0 < steps; i0 += DEPTH) {
+            uint4 a[DEPTH][2 * MT], b[DEPTH][NT];
+#pragma unroll
+            for (int i = 0; i < DEPTH; ++i) {
+                const int k = index(i0 + i);
+#pragma unroll
+                for (int j = 0; j < 2 * MT; ++j)
+                    a[i][j] = load8(w + j * w8, f0 + g + 8 * j < p.m, k, end, p.vec);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    b[i][n] = load8(x + n * x8, n * 8 + g < p.rows, k, end, p.vec);
+            }
+#pragma unroll
+            for (int i = 0; i < DEPTH; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    multiply(a[i], b[i][n], n);
+        }
+    } else {
+        // places in shared memory that only this lane writes and reads
+        uint4* ring = s_few + warp * (LOADS * 32) + lane;
+        auto copy = [&](uint4* to, const T* row, bool ok, int k) {
+            if (p.vec) {
+                const bool in = ok && k < end;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(smem_u32(to)), "l"(in ? row + k : static_cast<const T*>(p.w)), "r"(in ? 16 : 0) : "memory");
+            } else {
+                *to = load8(row, ok, k, end, false);
+            }
+        };
+        auto fetch = [&](int step) {
+            if (step < steps) {
+                uint4* to = ring + step % DEPTH * (kFewWarps * LOADS * 32);
+#pragma unroll
+                for (int j = 0; j < 2 * MT; ++j)
+                    copy(to + j * 32, w + j * w8, f0 + g + 8 * j < p.m, index(step));
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    copy(to + (2 * MT + n) * 32, x + n * x8, n * 8 + g < p.rows, index(step));
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int i = 0; i < DEPTH; ++i)
+            fetch(i);
+        for (int i = 0; i < steps; ++i) {
+            asm volatile("cp.async.wait_group %0;" :: "n"(DEPTH - 1) : "memory");
+            const uint4* from = ring + i % DEPTH * (kFewWarps * LOADS * 32);
+            uint4 a[2 * MT];
 #pragma unroll
             for (int j = 0; j < 2 * MT; ++j)
-                a[i][j] = load8(w + j * w8, f0 + g + 8 * j < p.m, k, end, p.vec);
+                a[j] = from[j * 32];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-                b[i][n] = load8(x + n * x8, n * 8 + g < p.rows, k, end, p.vec);
+                multiply(a, from[(2 * MT + n) * 32], n);
+            fetch(i + DEPTH);                                        // behind the products: what they read is overwritten
         }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-            for (int j = 0; j < MT; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const uint4 &a0 = a[i][2 * j], &a1 = a[i][2 * j + 1];
-                    mma16816<T>(acc[j][n], a0.x, a1.x, a0.y, a1.y, b[i][n].x, b[i][n].y);
-                    mma16816<T>(acc[j][n], a0.z, a1.z, a0.w, a1.w, b[i][n].z, b[i][n].w);
-                }
     }
+    __syncthreads();                                                 // (no copy is under way: the last groups are empty)
+    float (*part)[NT * 8][COLS + 1] = reinterpret_cast<float (*)[NT * 8][COLS + 1]>(s_few);
 #pragma unroll
     for (int j = 0; j < MT; ++j)
 #pragma unroll

@@ -311,7 +311,7 @@ int ttc_selective_scan_step(int32_t device, const ttc_scan_args* a, void* cuda_s
         using T = decltype(t);
         return by_lanes(lanes_of(a->n), [&](auto lc) {
             constexpr int LANES = decltype(lc)::value, CH = kStepThreads / LANES;
-            return launch_early("selective scan, one token", scan_step_kernel<T, LANES>, dim3((unsigned)a->batch, (a->d + CH - 1) / CH), kStepThreads, 1, st, p);
+            return launch_early("selective scan, one token", scan_step_kernel<T, LANES>, dim3((unsigned)a->batch, (a->d + CH - 1) / CH), kStepThreads, 0, 1, st, p);
         });
     });
 }

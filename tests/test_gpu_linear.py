@@ -68,7 +68,7 @@ def test_shapes(shape, out, dtype):
     _check(_randn(g, rows, k, t=dtype), _randn(g, m, k, t=dtype), _randn(g, m, t=F), out_dtype=F if out == "f32" else dtype)
 
 
-@pytest.mark.parametrize("rows", [1, 8, 9, 16, 17, 32, 33])
+@pytest.mark.parametrize("rows", [1, 8, 9, 16, 17, 32, 33, 57, 64, 65])
 @pytest.mark.parametrize("k, m", [(1024, 33), (2064, 50), (4100, 30), (5003, 17), (9000, 1000)])
 def test_few_rows_over_long_contractions(rows, k, m):
     """The contraction shared out between the blocks of a cluster, in parts that end anywhere."""
