@@ -212,12 +212,6 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-__device__ __forceinline__ float sum2(f2 v)
-{
-    float a, b;
-    unpack2(v, a, b);
-    return a + b;
-}
 
 // Sums over the W lanes of a group (lanes that differ in the bits STRIDE, 2 STRIDE, .. of the lane index).  In: NV values
 // of every lane.  While a lane holds more than one value, a round sends half of them to the partner and keeps the sums of

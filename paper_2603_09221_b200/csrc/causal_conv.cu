@@ -74,7 +74,8 @@ ConvDev to_dev(const ttc_conv_args* a, bool step)
 }
 
 // Tokens of a tile: 128, or fewer (not below 16) while there are less than about six blocks for every SM.  A tile reads
-// the W - 1 rows in front of it again.
+// the W - 1 rows in front of it again.  (2 x 2048 x 4096: 19.3 us; with two blocks for every SM 25.6, with twelve 20.1.
+// Gradients of 4 x 2048 x 4096: 62.8, 63.0 and 70.3.)
 void set_tiles(ConvDev& p, int v, int sms)
 {
     const int64_t cols = (p.d + (int64_t)v * kThreads - 1) / (v * kThreads);

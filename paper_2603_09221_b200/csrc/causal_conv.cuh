@@ -5,6 +5,12 @@
 // one by one where they are not, computes on packed pairs of them, and walks over a tile of tokens with the
 // last W inputs in registers, so an input is read once apart from the W - 1 rows in front of a tile.  Memory bounds all
 // three kernels: one read and one write per element forward, two and one backward.
+//
+// Forward, 4 x 2048 tokens of 4096 channels, bfloat16, four taps, SiLU: 34.8 us, 3.9 TB/s (a copy of the same arrays by torch: 24.7);
+// at four times the tokens 110 us, 4.9 TB/s.  Issue slots (62 %) are close behind; four channels to a thread 36.0, the next tokens'
+// loads under way beside the arithmetic 38 (registers).  Backward, 8191 packed rows of 2047 channels, which allow accesses of
+// two bytes only: 46 us, 50 instructions per element in 61 % of the issue slots; aligned, 4 x 2048 of 4096: 62.8 us, 3.2 TB/s.
+// A step, 64 sequences of 4096 channels: 2.3 us.
 #pragma once
 
 #include <type_traits>

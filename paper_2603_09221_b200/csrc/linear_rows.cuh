@@ -10,10 +10,11 @@ namespace lin {
 // ---- few rows -----------------------------------------------------------------------------------------------------------
 //
 // Up to 8 NT rows (tokens) against all of W: W is read once, which bounds it.  A block takes 16 MT rows of W and a part of
-// the contraction (a cluster shares the parts out and adds them up over shared memory of its blocks); its eight
-// warps deal that out again.  Each lane loads 16 contiguous bytes of two rows of W for every 16, and of one row of x for every 8, which are the
-// operands of two mma.sync.m16n8k16: the instruction does not mind which contraction index a slot stands for, as long as
-// both operands agree, so nothing is rearranged or staged.
+// the contraction (a cluster shares the parts out and adds them up over the shared memory of its blocks); its eight warps deal
+// that out again.  Each lane loads 16 contiguous bytes of two rows of W for every 16, and of one row of x for every 8, which are
+// the operands of two mma.sync.m16n8k16: the instruction does not mind which contraction index a slot stands for, as long as
+// both operands agree, so nothing is rearranged.  8 rows, 2048 -> 4096: 4.6 us for 16.8 MB of W (one round of loads); 8192 -> 8192
+// 28.9 us, 4.6 TB/s; 32 rows 9.3 and 33.7, of which L2 gives the blocks as many bytes of x as of W.
 
 constexpr int kFewWarps = 8;
 
@@ -241,7 +242,8 @@ struct SlopeDev {
     float* part;                 // [blocks of rows][m] or null
 };
 
-// dZ = dy act'(pre) in 16 bits, and each block's sums over its rows, of the unrounded values.  V columns to a thread.
+// dZ = dy act'(pre) in 16 bits, and each block's sums over its rows, of the unrounded values.  V columns to a thread.  Bound by
+// memory: 8192 x 8192 in bfloat16 with GELU 78 us for 403 MB, 5.2 TB/s.
 template <typename T, typename OT, int V, int ACT>
 __global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
 {

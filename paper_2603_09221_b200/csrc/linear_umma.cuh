@@ -3,12 +3,17 @@
 //
 // One CTA per SM works through tiles of 128 x BN, or, where there are enough of them, two neighbouring ones through tiles of
 // 256 x 256 (cta_group::2): each then fetches and reads 64 KB of shared memory for a block of 64 contraction indices instead
-// of 96, which is what bounds a single CTA (128 bytes per clock: 768 clocks against 512 of products).  One warp keeps a ring of stages of 64 contraction indices filled by TMA
-// (128-byte swizzle), one issues tcgen05.mma (kind::f16) into one of two accumulators in tensor memory, and
-// eight warps read the other one back, so that the end of a tile runs beside the products of the next.  Operands are read as
-// they lie in memory: an operand whose contraction index is not the contiguous one (the gradients') is staged in boxes of
-// 64 contiguous rows by 64 contraction indices and described to the instruction as MN-major; nothing is transposed.
-// Rows, columns and contraction indices past the end are filled with zeros by TMA.
+// of 96, which is what bounds a single CTA (128 bytes per clock: 768 clocks against 512 of products).  One warp keeps a ring of
+// stages of 64 contraction indices filled by TMA (128-byte swizzle), one issues tcgen05.mma (kind::f16) into one of two
+// accumulators in tensor memory, and eight warps read the other one back, so that the end of a tile runs beside the products
+// of the next.  Operands are read as they lie in memory: an operand whose contraction index is not the contiguous one (the
+// gradients') is staged in boxes of 64 contiguous rows by 64 contraction indices and described to the instruction as MN-major;
+// nothing is transposed.  Rows, columns and contraction indices past the end are filled with zeros by TMA.
+//
+// bfloat16, 8192 x 8192 over 8192: 692 us, 1589 TFLOP/s (torch.mm in the same loop 682 to 728); 8192 x 2048 over 4096 93 us alone and 97
+// back to back (92, 93), where power bounds both.  512 x 4096 over 2048 15.0 us (9.1): one round of tiles, whose start and end
+// nothing hides.  Float32 results with softplus, 4096 x 2304 over 1024: 28 us, of which the end of a tile, 9 us, comes twice.
+// Sums in segments: 4096 x 2048 over 2048 41 us (31 without).
 #pragma once
 
 #include <cuda.h>

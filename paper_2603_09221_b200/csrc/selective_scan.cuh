@@ -1,7 +1,8 @@
 // Selective state space scan: h_t = exp(D_t A) h_{t-1} + D_t x_t B_t, y_t = (C_t . h_t + D x_t) silu(z_t), diagonal A.
 //
 // A channel's n states are spread over LANES neighbouring lanes, four to a lane; a lane holds them for two neighbouring
-// channels, as packed pairs (even channel, odd channel).  A block owns 256 / LANES channels of one group and walks over the tokens in tiles.
+// channels, as packed pairs (even channel, odd channel).  A block owns 256 / LANES channels of one group and walks over the
+// tokens in tiles.
 // Four of its warps run the recurrence; eight load the rows, compute the step size (bias, softplus) and D_t x_t of
 // every token and channel once, leave them in shared memory with B and C in float32, and take the lanes' shares of C . h
 // from there to the output rows.  Both work at the same time, on tiles next to one another, with one barrier for each tile.
@@ -9,6 +10,16 @@
 // Per state and token: one exponential, four multiply-adds and six bytes from shared memory.  The special-function unit (16
 // exponentials per clock and SM) bounds it, with shared memory close behind: a 16-byte load occupies the return path for four
 // clocks, broadcast or not, and with one channel to a lane (twelve bytes) that path was the bound.
+//
+// 4 sequences of 2048 tokens, 4096 channels, 16 states, bfloat16: 250 us, 2.15e12 states a second, the unit at 60 % (137 us would
+// be all of it with what softplus and gate ask for), issue slots 59 %; 256 blocks on 148 SMs leave some with one.  On the way:
+// every warp loading and stepping, one channel to a lane 338 us, two channels 532 (too few warps), warps with roles 324 with
+// four for the rows and 283 with eight, loads without branches 256, tiles of 32 tokens 250 (at 16 states; 8 and 16 where
+// other widths are fastest).
+//
+// Few channels: the tokens are cut into pieces.  A first pass (LOCAL: recurrence without outputs) finds what each piece adds to
+// the state, from zero, and the sum of its steps; the second takes the state in front of its piece from those, since a
+// piece's decay is exp(A sum D_t).  16381 tokens, 1024 channels, 16 states: 87 + 121 us, twice the exponentials.
 #pragma once
 
 #include <type_traits>
@@ -477,7 +488,7 @@ static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long lon
 }
 
 // One token of each sequence: the state is read and written once, which is what bounds it; for few sequences the latency of
-// one round of loads.
+// one round of loads (16 sequences, 4096 channels, 16 states: 4.3 us for 8.9 MB).
 template <typename T, int LANES>
 __global__ void __launch_bounds__(kStepThreads, 12) scan_step_kernel(const ScanDev p)
 {
