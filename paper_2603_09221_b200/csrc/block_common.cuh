@@ -144,19 +144,15 @@ __device__ __forceinline__ float silu_slope(float z)
 }
 // log(1 + exp(z)) = max(z, 0) + log1p(exp(-|z|)), log1p(e) = e P(e) on [0, 1]: P of degree 9, fitted for the relative
 // error (5e-9; 1.5e-7 as evaluated)
+__device__ constexpr float kLog1p[10] = {1.f, -0.4999990165233612f, 0.3332996368408203f, -0.24954132735729218f, 0.19675931334495544f,
+                                         -0.15305569767951965f, 0.10603617131710052f, -0.056959159672260284f, 0.019851263612508774f, -0.0032439809292554855f};
 __device__ __forceinline__ float softplus(float z)
 {
     const float e = ex2(fabsf(z) * -kLog2e);
-    float p = -0.0032439809292554855f;
-    p = fmaf(p, e, 0.019851263612508774f);
-    p = fmaf(p, e, -0.056959159672260284f);
-    p = fmaf(p, e, 0.10603617131710052f);
-    p = fmaf(p, e, -0.15305569767951965f);
-    p = fmaf(p, e, 0.19675931334495544f);
-    p = fmaf(p, e, -0.24954132735729218f);
-    p = fmaf(p, e, 0.3332996368408203f);
-    p = fmaf(p, e, -0.4999990165233612f);
-    p = fmaf(p, e, 1.f);
+    float p = kLog1p[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i)
+        p = fmaf(p, e, kLog1p[i]);
     return fmaf(p, e, fmaxf(z, 0.f));
 }
 // Phi(z) and exp(-z^2 / 2): Phi(-|z|) = 1/2 erfcx(|z| / sqrt 2) exp(-z^2 / 2), erfcx as t Q(t), t = 1 / (1 + 0.4 |z| / sqrt 2),
@@ -211,6 +207,27 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
     f2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
+}
+
+// sigmoid, silu and softplus of both: the same operations
+__device__ __forceinline__ f2 sigmoid2(f2 z)
+{
+    float a, b;
+    unpack2(mul2(z, pack2(-kLog2e, -kLog2e)), a, b);
+    unpack2(add2(pack2(ex2(a), ex2(b)), pack2(1.f, 1.f)), a, b);
+    return pack2(rcp(a), rcp(b));
+}
+__device__ __forceinline__ f2 silu2(f2 z) { return mul2(z, sigmoid2(z)); }
+__device__ __forceinline__ f2 softplus2(f2 z)
+{
+    float a, b;
+    unpack2(z, a, b);
+    const f2 e = pack2(ex2(fabsf(a) * -kLog2e), ex2(fabsf(b) * -kLog2e));
+    f2 p = pack2(kLog1p[9], kLog1p[9]);
+#pragma unroll
+    for (int i = 8; i >= 0; --i)
+        p = fma2(p, e, pack2(kLog1p[i], kLog1p[i]));
+    return fma2(p, e, pack2(fmaxf(a, 0.f), fmaxf(b, 0.f)));
 }
 
 // Sums over the W lanes of a group (lanes that differ in the bits STRIDE, 2 STRIDE, .. of the lane index).  In: NV values

@@ -138,15 +138,6 @@ template <typename T, int V> __device__ __forceinline__ Vec<T, V> narrow(const f
     return r;
 }
 
-// the logistic function of both
-__device__ __forceinline__ f2 sigmoid2(f2 z)
-{
-    float a, b;
-    unpack2(mul2(z, pack2(-kLog2e, -kLog2e)), a, b);
-    unpack2(add2(pack2(ex2(a), ex2(b)), pack2(1.f, 1.f)), a, b);
-    return pack2(rcp(a), rcp(b));
-}
-
 template <typename T, int V, int W> struct Taps {
     f2 w[W][V / 2], b[V / 2];
     int count;                      // channels that exist
@@ -251,7 +242,7 @@ __global__ void __launch_bounds__(kThreads, 10) conv_kernel(const ConvDev p)
 #pragma unroll
             for (int i = 0; i < V / 2; ++i) {
                 const f2 z = k.next(in, i, now[i]);
-                out[i] = p.act == TTC_ACT_SILU ? mul2(z, sigmoid2(z)) : z;
+                out[i] = p.act == TTC_ACT_SILU ? silu2(z) : z;
             }
             give<ALIGNED>(y, narrow<T, V>(out), k.count);
             y += p.y.ts;
@@ -303,7 +294,7 @@ __global__ void __launch_bounds__(kThreads) conv_step_kernel(const ConvDev p)
     if (p.act == TTC_ACT_SILU)
 #pragma unroll
         for (int i = 0; i < V / 2; ++i)
-            z[i] = mul2(z[i], sigmoid2(z[i]));
+            z[i] = silu2(z[i]);
     give<ALIGNED>(row_ptr<T>(p.y, b, 0) + c, narrow<T, V>(z), count);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j)

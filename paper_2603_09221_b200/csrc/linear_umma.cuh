@@ -190,6 +190,12 @@ template <typename F> __device__ __forceinline__ void each(float (&v)[32], F&& f
     for (int i = 0; i < 32; ++i)
         v[i] = f(v[i]);
 }
+template <typename F> __device__ __forceinline__ void each_pair(float (&v)[32], F&& f)
+{
+#pragma unroll
+    for (int i = 0; i < 32; i += 2)
+        unpack2(f(pack2(v[i], v[i + 1])), v[i], v[i + 1]);
+}
 __device__ __forceinline__ float activate(float z, int act)
 {
     switch (act) {
@@ -204,9 +210,9 @@ __device__ __forceinline__ void activate(float (&v)[32], int act)
 {
     switch (act) {
     case TTC_ACT_RELU: return each(v, [](float z) { return activate(z, TTC_ACT_RELU); });
-    case TTC_ACT_SILU: return each(v, [](float z) { return activate(z, TTC_ACT_SILU); });
+    case TTC_ACT_SILU: return each_pair(v, [](f2 z) { return silu2(z); });
     case TTC_ACT_GELU: return each(v, [](float z) { return activate(z, TTC_ACT_GELU); });
-    case TTC_ACT_SOFTPLUS: return each(v, [](float z) { return activate(z, TTC_ACT_SOFTPLUS); });
+    case TTC_ACT_SOFTPLUS: return each_pair(v, [](f2 z) { return softplus2(z); });
     default: return;
     }
 }
@@ -507,8 +513,10 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
                     continue;
                 if (p.e.bias) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        v[i] += s_bias[c + i];
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 b = *reinterpret_cast<const float4*>(s_bias + c + i);
+                        v[i] += b.x, v[i + 1] += b.y, v[i + 2] += b.z, v[i + 3] += b.w;
+                    }
                 }
                 if (p.e.pre) {
                     if (p.e.pre_bf16)

@@ -301,23 +301,20 @@ __device__ __forceinline__ void run_rows(const ScanDev& p, const Piece& q, int g
 #pragma unroll
         for (int e = 0; e < PASSES; ++e) {
             const int u = e * LT::ROWS + lr;
-            float steps[V], ins[V];
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                float step = to_f(r.delta[e].v[v]) + bias[v];
-                if (p.softplus)
-                    step = softplus(step);
-                float in = step * to_f(r.x[e].v[v]);
-                if (!FULL && u >= left)                              // padding: nothing decays, nothing is added
-                    step = in = 0.f;
-                steps[v] = step, ins[v] = in;
-            }
+            const bool none = !FULL && u >= left;                    // padding: nothing decays, nothing is added
             float4* at = to + u * (CH / 2) + lc / 2;
             if constexpr (V == 2) {
-                *at = make_float4(steps[0], steps[1], ins[0], ins[1]);
+                f2 step = add2(pack2(to_f(r.delta[e].v[0]), to_f(r.delta[e].v[1])), pack2(bias[0], bias[1]));
+                if (p.softplus)
+                    step = softplus2(step);
+                const f2 in = mul2(step, pack2(to_f(r.x[e].v[0]), to_f(r.x[e].v[1])));
+                *reinterpret_cast<ulonglong2*>(at) = none ? make_ulonglong2(0, 0) : make_ulonglong2(step, in);
             } else {
-                reinterpret_cast<float*>(at)[lc % 2] = steps[0];
-                reinterpret_cast<float*>(at)[2 + lc % 2] = ins[0];
+                float step = to_f(r.delta[e].v[0]) + bias[0];
+                if (p.softplus)
+                    step = softplus(step);
+                reinterpret_cast<float*>(at)[lc % 2] = none ? 0.f : step;
+                reinterpret_cast<float*>(at)[2 + lc % 2] = none ? 0.f : step * to_f(r.x[e].v[0]);
             }
         }
     };
@@ -361,7 +358,6 @@ __device__ __forceinline__ void run_rows(const ScanDev& p, const Piece& q, int g
             const int u = e * LT::ROWS + lr;
             if (have_l && u < left) {
                 Vec<T, V> out;
-                float sum[2];
                 f2 s2 = 0;
                 const ulonglong2* from = reinterpret_cast<const ulonglong2*>(shares + (u * (CH / 2) + lc / 2) * LANES);
 #pragma unroll
@@ -369,13 +365,19 @@ __device__ __forceinline__ void run_rows(const ScanDev& p, const Piece& q, int g
                     const ulonglong2 two = from[LANES > 2 ? k ^ swap : 0];
                     s2 = k ? add2(s2, add2(two.x, two.y)) : add2(two.x, two.y);
                 }
-                unpack2(s2, sum[0], sum[1]);
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    float r = fmaf(skip[v], to_f(x0[e].v[v]), V == 2 ? sum[v] : lc % 2 ? sum[1] : sum[0]);
+                float r0, r1;
+                if constexpr (V == 2) {
+                    s2 = fma2(pack2(skip[0], skip[1]), pack2(to_f(x0[e].v[0]), to_f(x0[e].v[1])), s2);
                     if (gated)
-                        r *= silu(to_f(of.z[e].v[v]));
-                    out.v[v] = from_f<T>(r);
+                        s2 = mul2(s2, silu2(pack2(to_f(of.z[e].v[0]), to_f(of.z[e].v[1]))));
+                    unpack2(s2, r0, r1);
+                    out.v[0] = from_f<T>(r0), out.v[1] = from_f<T>(r1);
+                } else {
+                    unpack2(s2, r0, r1);
+                    float r = fmaf(skip[0], to_f(x0[e].v[0]), lc % 2 ? r1 : r0);
+                    if (gated)
+                        r *= silu(to_f(of.z[e].v[0]));
+                    out.v[0] = from_f<T>(r);
                 }
                 *reinterpret_cast<Vec<T, V>*>(to) = out;
             }

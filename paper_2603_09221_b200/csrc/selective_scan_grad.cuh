@@ -109,23 +109,29 @@ template <typename T, int LANES, int V> struct Loader {
 #pragma unroll
             for (int e = 0; e < PASSES; ++e) {
                 const int u = e * ROWS + lr;
-                float step[V], in[V], g[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    step[v] = to_f(delta[e].v[v]) + bias[v];
+                const bool none = u >= left;                         // padding: nothing decays, nothing is added
+                float4* tok = s_tok + u * (CH / 2) + lc / 2;
+                float2* to_g = s_g + u * (CH / 2) + lc / 2;
+                if constexpr (V == 2) {
+                    f2 step = add2(pack2(to_f(delta[e].v[0]), to_f(delta[e].v[1])), pack2(bias[0], bias[1]));
                     if (p.f.softplus)
-                        step[v] = softplus(step[v]);
-                    in[v] = step[v] * to_f(x[e].v[v]);
-                    g[v] = to_f(dy[e].v[v]);
+                        step = softplus2(step);
+                    f2 g = pack2(to_f(dy[e].v[0]), to_f(dy[e].v[1]));
                     if (gated)
-                        g[v] *= silu(to_f(z[e].v[v]));
-                    if (u >= left)                                   // padding: nothing decays, nothing is added
-                        step[v] = in[v] = g[v] = 0.f;
+                        g = mul2(g, silu2(pack2(to_f(z[e].v[0]), to_f(z[e].v[1]))));
+                    const f2 in = mul2(step, pack2(to_f(x[e].v[0]), to_f(x[e].v[1])));
+                    *reinterpret_cast<ulonglong2*>(tok) = none ? make_ulonglong2(0, 0) : make_ulonglong2(step, in);
+                    *reinterpret_cast<f2*>(to_g) = none ? 0 : g;
+                } else {
+                    float step = to_f(delta[e].v[0]) + bias[0], g = to_f(dy[e].v[0]);
+                    if (p.f.softplus)
+                        step = softplus(step);
+                    if (gated)
+                        g *= silu(to_f(z[e].v[0]));
+                    reinterpret_cast<float*>(tok)[lc % 2] = none ? 0.f : step;
+                    reinterpret_cast<float*>(tok)[2 + lc % 2] = none ? 0.f : step * to_f(x[e].v[0]);
+                    reinterpret_cast<float*>(to_g)[lc % 2] = none ? 0.f : g;
                 }
-                float* tok = reinterpret_cast<float*>(s_tok + u * (CH / 2) + lc / 2) + lc % 2;
-                put<V>(tok, step);
-                put<V>(tok + 2, in);
-                put<V>(reinterpret_cast<float*>(s_g + u * (CH / 2) + lc / 2) + lc % 2, g);
             }
         }
         if (BROWS <= TB || br < TB) {
