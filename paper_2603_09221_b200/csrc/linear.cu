@@ -172,12 +172,14 @@ int launch_tiles(const CUtensorMap& ma, const CUtensorMap& mb, GemmDev& g, bool 
     c.blockDim = dim3(kGemmThreads);
     c.dynamicSmemBytes = S::SMEM;
     c.stream = st;
-    cudaLaunchAttribute cluster;
-    cluster.id = cudaLaunchAttributeClusterDimension;
-    cluster.val.clusterDim.x = CTAS;
-    cluster.val.clusterDim.y = cluster.val.clusterDim.z = 1;
-    c.attrs = &cluster;
-    c.numAttrs = PAIR ? 1 : 0;
+    cudaLaunchAttribute with[2];
+    with[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;     // (as launch_early)
+    with[0].val.programmaticStreamSerializationAllowed = 1;
+    with[1].id = cudaLaunchAttributeClusterDimension;
+    with[1].val.clusterDim.x = CTAS;
+    with[1].val.clusterDim.y = with[1].val.clusterDim.z = 1;
+    c.attrs = with;
+    c.numAttrs = PAIR ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelEx(&c, kernel, ma, mb, g);
     return e == cudaSuccess ? launched("matrix product") : fail(TTC_STATUS_CUDA_ERROR, "matrix product: %s", cudaGetErrorString(e));
 }
@@ -222,11 +224,8 @@ template <bool A_MN, bool B_MN> int product(const Product& q, const Operand& a, 
     return by_type(out_dtype, [&](auto t) {
         using OT = decltype(t);
         const unsigned blocks = (unsigned)((q.M * q.N + 255) / 256);
-        if (is_bf16)
-            split_sum_kernel<bf16, OT><<<blocks, 256, 0, st>>>(q.part, q.M * q.N, q.splits, q.M, q.N, e);
-        else
-            split_sum_kernel<__half, OT><<<blocks, 256, 0, st>>>(q.part, q.M * q.N, q.splits, q.M, q.N, e);
-        return launched("matrix product, parts of the contraction");
+        auto* kernel = is_bf16 ? split_sum_kernel<bf16, OT> : split_sum_kernel<__half, OT>;
+        return launch_early("matrix product, parts of the contraction", kernel, dim3(blocks), 256, 0, 1, st, q.part, q.M * q.N, q.splits, q.M, q.N, e);
     });
 }
 

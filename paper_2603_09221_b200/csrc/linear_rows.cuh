@@ -207,6 +207,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, 2) few_rows_kernel(const FewDe
 template <typename T, typename OT>
 __global__ void __launch_bounds__(256) split_sum_kernel(const float* part, long long split_stride, int splits, long long M, long long N, const Epilogue e)
 {
+    wait_for_previous();
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
     if (i >= M * N)
         return;

@@ -329,6 +329,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) gemm_kernel(const __grid_cons
         cluster_sync();                                              // the other CTA's barriers and tensor memory are there
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
+    wait_for_previous();                                             // what stands above needs nothing of it
 
     const int per_split = p.tiles_m * p.tiles_n, tiles = per_split * p.splits;
     // Tiles of eight rows of tiles follow one another column by column, so that the CTAs at work share operands in L2.
