@@ -195,8 +195,7 @@ int ttc_causal_conv(int32_t device, const ttc_conv_args* a, void* cuda_stream)
         }
         if (in_place) {
             const dim3 grid((unsigned)a->batch, (a->d + kThreads - 1) / kThreads);
-            conv_window_kernel<T, W><<<grid, kThreads, 0, st>>>(p);
-            TTC_TRY(launched("causal convolution, last windows"));
+            TTC_TRY((launch_early("causal convolution, last windows", conv_window_kernel<T, W>, grid, kThreads, 0, 1, st, p)));
         }
         return TTC_OK;
     });
@@ -260,8 +259,8 @@ int ttc_causal_conv_grad(int32_t device, const ttc_conv_args* a, const ttc_conv_
         // eight sequences to a block
         const int64_t empties = p.dstate && (a->seq_offsets || a->tokens == 0) ? (a->batch + 7) / 8 : 0;
         if (o.params || empties) {
-            conv_param_kernel<T, W><<<dim3((a->d + 31) / 32, (unsigned)(W + 1 + empties)), 256, 0, st>>>(p);
-            TTC_TRY(launched("gradients of the causal convolution, parameters"));
+            TTC_TRY((launch_early("gradients of the causal convolution, parameters", conv_param_kernel<T, W>,
+                                  dim3((a->d + 31) / 32, (unsigned)(W + 1 + empties)), 256, 0, 1, st, p)));
         }
         return TTC_OK;
     });

@@ -207,6 +207,7 @@ template <typename T, int W> __device__ __forceinline__ void keep_window(const C
 // In a launch of its own where state_out is state, behind the one that reads the windows in front.
 template <typename T, int W> __global__ void __launch_bounds__(kThreads) conv_window_kernel(const ConvDev p)
 {
+    wait_for_previous();
     const int c = blockIdx.y * kThreads + threadIdx.x;
     if (c < p.d)
         keep_window<T, W>(p, blockIdx.x, c);
@@ -419,6 +420,7 @@ __global__ void __launch_bounds__(kThreads, 7) conv_grad_kernel(const ConvDev p)
 // on to its first one.
 template <typename T, int W> __global__ void __launch_bounds__(256) conv_param_kernel(const ConvDev p)
 {
+    wait_for_previous();
     __shared__ float sum[8][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int c = blockIdx.x * 32 + lane, j = blockIdx.y;

@@ -102,9 +102,9 @@ int copy_operand(const Aligned& a, cudaStream_t st)
 {
     if (!a.copy || a.from.rows == 0)
         return TTC_OK;
-    align_rows_kernel<<<(unsigned)a.from.rows, 256, 0, st>>>(static_cast<const unsigned short*>(a.from.ptr), a.from.ld, a.from.rows, (int)a.from.cols,
-                                                             static_cast<unsigned short*>(const_cast<void*>(a.to.ptr)), a.to.ld);
-    return launched("projection, rows aligned");
+    return launch_early("projection, rows aligned", align_rows_kernel, dim3((unsigned)a.from.rows), 256, 0, 1, st,
+                        static_cast<const unsigned short*>(a.from.ptr), a.from.ld, a.from.rows, (int)a.from.cols,
+                        static_cast<unsigned short*>(const_cast<void*>(a.to.ptr)), a.to.ld);
 }
 
 // A product of `M` x `N` results over `K`: how it is tiled, and the scratch of a split contraction.
@@ -462,8 +462,8 @@ int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_g
         if (g->dbias)
             TTC_CUDA(cudaMemsetAsync(g->dbias, 0, sizeof(float) * a->m, st));
         if (g->dw) {
-            zero_rows_kernel<<<(unsigned)a->m, 256, 0, st>>>(static_cast<bf16*>(g->dw), g->lddw, a->m, a->k);    // zero has the same bits in both types
-            TTC_TRY(launched("gradients of a projection without rows"));
+            TTC_TRY((launch_early("gradients of a projection without rows", zero_rows_kernel<bf16>, dim3((unsigned)a->m), 256, 0, 1, st, static_cast<bf16*>(g->dw),
+                                  g->lddw, a->m, a->k)));            // zero has the same bits in both types
         }
         return TTC_OK;
     }
@@ -475,10 +475,8 @@ int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_g
                 using T = decltype(tc);
                 auto with = [&](auto act) {
                     constexpr int ACT = decltype(act)::value;
-                    if (o.slope_v == 8)
-                        slope_kernel<T, OT, 8, ACT><<<grid, 256, 0, st>>>(o.slope);
-                    else
-                        slope_kernel<T, OT, 1, ACT><<<grid, 256, 0, st>>>(o.slope);
+                    auto* kernel = o.slope_v == 8 ? slope_kernel<T, OT, 8, ACT> : slope_kernel<T, OT, 1, ACT>;
+                    kernel<<<grid, 256, 0, st>>>(o.slope);
                     return launched("gradients of a projection, activation");
                 };
                 switch (a->act) {
@@ -492,8 +490,7 @@ int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_g
             return is_bf16 ? go(bf16()) : go(__half());
         }));
         if (g->dbias) {
-            bias_sum_kernel<<<(a->m + 31) / 32, 256, 0, st>>>(o.slope.part, o.row_blocks, a->m, g->dbias);
-            TTC_TRY(launched("gradients of a projection, bias"));
+            TTC_TRY((launch_early("gradients of a projection, bias", bias_sum_kernel, dim3((a->m + 31) / 32), 256, 0, 1, st, o.slope.part, o.row_blocks, a->m, g->dbias)));
         }
     }
     if (g->dx) {

@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
 
 static __global__ void __launch_bounds__(256) bias_sum_kernel(const float* part, int blocks, int m, float* out)
 {
+    wait_for_previous();
     __shared__ float sum[8][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, c = blockIdx.x * 32 + lane;
     float s = 0.f;
@@ -309,6 +310,7 @@ static __global__ void __launch_bounds__(256) bias_sum_kernel(const float* part,
 // Rows copied to a stride that is a multiple of 16 bytes.
 static __global__ void __launch_bounds__(256) align_rows_kernel(const unsigned short* from, long long ld, long long rows, int cols, unsigned short* to, long long ldt)
 {
+    wait_for_previous();
     const long long r = blockIdx.x;
     for (int c = threadIdx.x; c < cols; c += 256)
         to[r * ldt + c] = from[r * ld + c];
@@ -316,6 +318,7 @@ static __global__ void __launch_bounds__(256) align_rows_kernel(const unsigned s
 
 template <typename T> __global__ void __launch_bounds__(256) zero_rows_kernel(T* to, long long ld, long long rows, int cols)
 {
+    wait_for_previous();
     for (int c = threadIdx.x; c < cols; c += 256)
         to[(long long)blockIdx.x * ld + c] = from_f<T>(0.f);
 }

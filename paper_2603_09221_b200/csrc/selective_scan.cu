@@ -172,8 +172,8 @@ template <typename K> int allow_smem(K* kernel, size_t bytes)
 
 int map_pieces(const ScanDev& p, int64_t piece, int at_least, int64_t bound, cudaStream_t st)
 {
-    piece_map_kernel<<<1, 1024, 0, st>>>(p.seqs, piece, at_least, bound, const_cast<int2*>(p.piece_map), const_cast<int*>(p.seq_first));
-    return launched("selective scan, pieces");
+    return launch_early("selective scan, pieces", piece_map_kernel, dim3(1), 1024, 0, 1, st, p.seqs, piece, at_least, bound,
+                        const_cast<int2*>(p.piece_map), const_cast<int*>(p.seq_first));
 }
 
 struct GradPlan {
@@ -363,22 +363,18 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
             if (p.runs)
                 TTC_TRY(o.pairs ? local(two) : local(one));
             if (a->batch) {
-                if (a->n % 4 == 0)
-                    grad_join_kernel<4><<<dim3((unsigned)a->batch, (unsigned)((states / 4 + 127) / 128), 2), 128, 0, st>>>(p);
-                else
-                    grad_join_kernel<1><<<dim3((unsigned)a->batch, (unsigned)((states + 127) / 128), 2), 128, 0, st>>>(p);
-                TTC_TRY(launched("gradients of the selective scan, states and co-states"));
+                const int v = a->n % 4 == 0 ? 4 : 1;
+                TTC_TRY(launch_early("gradients of the selective scan, states and co-states", v == 4 ? grad_join_kernel<4> : grad_join_kernel<1>,
+                                     dim3((unsigned)a->batch, (unsigned)((states / v + 127) / 128), 2), 128, 0, 1, st, p));
             }
             if (p.runs)
                 TTC_TRY(o.pairs ? pieces(two) : pieces(one));
             const int64_t blocks = (p.dA ? (states + 31) / 32 : 0) + (p.dD || p.ddelta_bias ? 2 * (((int64_t)a->d + 31) / 32) : 0);
             if (blocks) {
-                grad_sum_kernel<<<(unsigned)blocks, 256, 0, st>>>(p);
-                TTC_TRY(launched("gradients of the selective scan, parameters"));
+                TTC_TRY((launch_early("gradients of the selective scan, parameters", grad_sum_kernel, dim3((unsigned)blocks), 256, 0, 1, st, p)));
             }
             if (p.part_BC && p.runs) {
-                grad_rows_kernel<T><<<dim3((unsigned)p.runs, 4), 256, 0, st>>>(p, LANES * 4);
-                TTC_TRY(launched("gradients of the selective scan, B and C"));
+                TTC_TRY((launch_early("gradients of the selective scan, B and C", grad_rows_kernel<T>, dim3((unsigned)p.runs, 4), 256, 0, 1, st, p, LANES * 4)));
             }
             return (int)TTC_OK;
         });

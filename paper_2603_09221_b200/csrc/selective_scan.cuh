@@ -19,7 +19,7 @@
 //
 // Few channels: the tokens are cut into pieces.  A first pass (LOCAL: recurrence without outputs) finds what each piece adds to
 // the state, from zero, and the sum of its steps; the second takes the state in front of its piece from those, since a
-// piece's decay is exp(A sum D_t).  16381 tokens, 1024 channels, 16 states: 87 + 121 us, twice the exponentials.
+// piece's decay is exp(A sum D_t).  16381 tokens, 1024 channels, 16 states: 84 + 115 us, twice the exponentials.
 #pragma once
 
 #include <type_traits>
@@ -444,6 +444,7 @@ __global__ void __launch_bounds__(kThreads, 2) scan_kernel(const ScanDev p)
 // piece, so that its last state is written.  One block.
 static __global__ void __launch_bounds__(1024) piece_map_kernel(Seqs s, long long piece, int at_least, long long bound, int2* map, int* seq_first)
 {
+    wait_for_previous();
     __shared__ int sum[1024];
     __shared__ int base;
     if (threadIdx.x == 0)

@@ -13,9 +13,9 @@
 // 3.5 exponentials per state and token in all (one in step 1; in step 3 one for the states, a half for the first half's,
 // which are walked twice, and one for the co-states).
 //
-// 4 sequences of 1024 tokens, 2048 channels, 16 states, bfloat16: 68 + 19 + 237 + 13 us; step 3 is bound by issue slots (49 %) and
+// 4 sequences of 1024 tokens, 2048 channels, 16 states, bfloat16: 70 + 19 + 228 + 13 us; step 3 is bound by issue slots (49 %) and
 // by the 11 warps of an SM (168 registers) that wait for one another's values.  Step 3 with decays kept, one channel to a lane:
-// 555 us; computed again, two channels: 258; one copy of the code for both halves, which then fits the instruction cache: 239;
+// 555 us; computed again, two channels: 258; one copy of the code for both halves, which then fits the instruction cache: 239, now 228;
 // with 128 registers (spills) 259; runs of eight pieces to a block instead of four 261 (fewer blocks in the last round).
 #pragma once
 
@@ -297,6 +297,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) grad_local_kernel(const GradD
 // to a thread (four where n is a multiple of four).
 template <int V> __global__ void __launch_bounds__(128) grad_join_kernel(const GradDev p)
 {
+    wait_for_previous();
     const long long at = ((long long)blockIdx.y * 128 + threadIdx.x) * V, size = (long long)p.f.d * p.f.n;
     if (at >= size)
         return;
@@ -568,6 +569,7 @@ __global__ void __launch_bounds__(kGradThreads, 3) grad_piece_kernel(const GradD
 // sequence were not written.
 static __global__ void __launch_bounds__(256) grad_sum_kernel(const GradDev p)
 {
+    wait_for_previous();
     __shared__ float sum[8][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const long long states = (long long)p.f.d * p.f.n, a_blocks = p.dA ? (states + 31) / 32 : 0, d_blocks = (p.f.d + 31) / 32;
@@ -594,6 +596,7 @@ static __global__ void __launch_bounds__(256) grad_sum_kernel(const GradDev p)
 // dB and dC of every token: the channel blocks of its group added up.
 template <typename T> __global__ void __launch_bounds__(256) grad_rows_kernel(const GradDev p, int NP)
 {
+    wait_for_previous();
     Piece q;
     if (!find_piece(p.f, blockIdx.x, q))
         return;
