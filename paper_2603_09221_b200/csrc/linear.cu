@@ -357,9 +357,9 @@ int plan_grad(int device, const ttc_linear_args* a, const ttc_linear_grads* g, v
         o.w = plan_operand(Operand{a->w, a->m, a->k, ldw}, s);
     // the two products run one behind the other and share the room for parts
     Scratch s1 = s, s2 = s;
-    if (g->dx)
+    if (g->dx && a->rows)                        // (no rows: no products, and no tiles to share the SMs out to)
         o.qx = plan_product(a->rows, a->k, a->m, false, sms, s1);
-    if (g->dw)
+    if (g->dw && a->rows)
         o.qw = plan_product(a->m, a->k, a->rows, false, sms, s2);
     o.bytes = s1.used > s2.used ? s1.used : s2.used;
     return TTC_OK;

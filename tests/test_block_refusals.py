@@ -117,6 +117,24 @@ def test_linear_gradients():
     assert _status(lib.ttc_linear_grad_workspace, 0, _linear(act=2), grads())[0] == INVALID       # no pre
 
 
+def test_linear_gradients_of_no_rows():
+    """Every output there, by its address, and no rows: sums over nothing, and no product to plan (in a process of its own: a
+    signal ends the process)."""
+    import subprocess
+    import sys
+    code = """
+from paper_2603_09221_b200 import block
+from tests.test_block_refusals import P, _linear
+lib = block._load()
+for act, pre in ((0, 0), (2, 7 * P)):
+    for out in (dict(dx=4 * P), dict(dw=5 * P), dict(dbias=6 * P), dict(dx=4 * P, dw=5 * P, dbias=6 * P)):
+        g = dict(dy=3 * P, dx=0, dw=0, dbias=0, lddy=48, lddx=32, lddw=32)
+        need = lib.ttc_linear_grad_workspace(0, _linear(rows=0, act=act, pre=pre), block._LINEAR_GRADS.pack(*{**g, **out}.values()))
+        assert need >= 0, (out, need)
+"""
+    subprocess.run([sys.executable, "-c", code], check=True)
+
+
 def test_outputs_that_overlap():
     lib = block._load()
     status = lambda f, *args: _status(getattr(lib, f), 0, *args)[0]  # noqa: E731
