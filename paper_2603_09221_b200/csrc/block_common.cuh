@@ -21,8 +21,8 @@ template <> __device__ __forceinline__ float from_f<float>(float v) { return v; 
 template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
 template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
-// V elements that are loaded and stored together
-template <typename T, int V> struct alignas(sizeof(T) * V) Vec { T v[V]; };
+// V elements that are loaded and stored together, by 16 bytes where they are more: the alignment that the host sides ask for
+template <typename T, int V> struct alignas(sizeof(T) * V < 16 ? sizeof(T) * V : 16) Vec { T v[V]; };
 
 // First thing in kernels that are launched with launch_early (block_host.h): their blocks are set up while the kernel in front of
 // them in the stream ends, and go on once all of it is done and visible; the same is allowed to the kernel behind.

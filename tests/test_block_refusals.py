@@ -224,3 +224,20 @@ def test_every_declared_operator_is_bound():
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     text = re.sub(r"/\*.*?\*/", "", open(os.path.join(root, "include", "ttc_block.h")).read(), flags=re.S)
     assert set(block.EXPORTS) == set(re.findall(r"\b(ttc_\w+)\s*\(", text))
+
+
+def test_accesses_ask_for_no_more_than_sixteen_bytes(tmp_path):
+    """The host sides let kernels read several elements at once where rows lie on 16 bytes; no such access may assume more."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "alignment.cu"
+    src.write_text("""#include "block_common.cuh"
+using namespace ttc::blk;
+template <typename T> constexpr bool fits() {
+    return alignof(Vec<T, 1>) == sizeof(T) && alignof(Vec<T, 2>) == 2 * sizeof(T) && alignof(Vec<T, 4>) <= 16 && alignof(Vec<T, 8>) <= 16 && sizeof(Vec<T, 8>) == 8 * sizeof(T);
+}
+static_assert(fits<float>() && fits<bf16>() && fits<__half>(), "");
+""")
+    subprocess.run(["nvcc", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(root, "paper_2603_09221_b200", "csrc"), "-c",
+                    "-o", str(tmp_path / "alignment.o"), str(src)], check=True)

@@ -1,8 +1,9 @@
-"""Calls at the edges of what include/ttc_block.h allows: no rows with outputs in place."""
+"""Calls at the edges of what include/ttc_block.h allows: no rows with every output there, rows that lie on 16 bytes and no more."""
 import pytest
 import torch
 
 from paper_2603_09221_b200 import block
+from tests import block_util as bu
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -25,3 +26,25 @@ def test_gradients_of_no_rows_with_every_output_there(act):
     assert lib.ttc_linear_grad(0, record, grads, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
     torch.cuda.synchronize()
     assert bool((dx == 5).all()) and not dw.any() and not dbias.any()
+
+
+@pytest.mark.parametrize("act", ["none", "gelu"])
+@pytest.mark.parametrize("at, width", [(4, 72), (4, 76), (0, 68), (12, 80), (1, 65)])
+def test_gradients_of_float32_slices(act, at, width):
+    """dy in float32 that begins 16 bytes into a wider row, or whose rows lie 16 bytes off 32: the same bits as from dense rows.  Rows
+    off 16 bytes are read column by column and added up in another order: rows + 8 roundings on either side, slopes below 1.13."""
+    g = torch.Generator(device=DEV).manual_seed(12)
+    rows, k, m = 77, 40, 64
+    r = lambda *s, t=torch.bfloat16: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+    x, w, pre = r(rows, k), r(m, k), None if act == "none" else r(rows, m)
+    wide = r(rows, width, t=F)
+    dy = wide[:, at:at + m]
+    for keys in (("dx", "dw", "dbias"), ("dbias",)):
+        want = block.linear_grad(dy.contiguous(), x, w, act=act, pre=pre, want=keys)
+        got = block.linear_grad(dy, x, w, act=act, pre=pre, want=keys)
+        for key in keys:
+            if key == "dbias" and (at % 4 or width % 4):
+                assert bool(((got[key] - want[key]).abs() <= 2 * (rows + 8) * bu.U * 1.13 * dy.abs().sum(0)).all())
+            else:
+                assert torch.equal(got[key], want[key]), key
+    assert block.device_error(0) == 0
