@@ -117,6 +117,12 @@ bool in_pairs(const ttc_scan_args* a, std::initializer_list<const ttc_rows*> row
     return ok;
 }
 
+// Pieces are counted in 32 bits, and are as many blocks.
+int check_pieces(int64_t pieces)
+{
+    return pieces <= INT32_MAX ? (int)TTC_OK : fail(TTC_STATUS_UNSUPPORTED, "%lld pieces of sequences", (long long)pieces);
+}
+
 // Few sequences and channels leave SMs idle: then the tokens are cut into pieces, whose own shares of the state are found
 // first (a second exponential per state and token) and handed on.  That pays where a sequence's work can be cut by three or more
 // (2048 tokens, 1024 channels, 16 states, which are 16 blocks a sequence; in pieces and without: one sequence 39.9 and 148.7 us,
@@ -150,6 +156,7 @@ int plan_forward(int device, const ttc_scan_args* a, void* ws, Plan& o)
             p.piece = piece;
             p.pieces_per_seq = (a->tokens + piece - 1) / piece;
             o.pieces = a->seq_offsets ? a->tokens / piece + a->batch : a->batch * p.pieces_per_seq;
+            TTC_TRY(check_pieces(o.pieces));
             Scratch s(ws);
             if (a->seq_offsets) {
                 p.piece_map = s.take<int2>(o.pieces);
@@ -232,6 +239,7 @@ int plan_grad(int device, const ttc_scan_args* a, const ttc_scan_grads* g, void*
     p.f.piece = run;
     p.f.pieces_per_seq = (a->tokens + run - 1) / run;
     p.runs = a->seq_offsets ? a->tokens / run + a->batch : a->batch * p.f.pieces_per_seq;
+    TTC_TRY(check_pieces(p.runs));
     Scratch s(ws);
     if (a->seq_offsets) {
         p.f.piece_map = s.take<int2>(p.runs);

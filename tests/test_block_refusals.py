@@ -241,3 +241,10 @@ static_assert(fits<float>() && fits<bf16>() && fits<__half>(), "");
 """)
     subprocess.run(["nvcc", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(root, "paper_2603_09221_b200", "csrc"), "-c",
                     "-o", str(tmp_path / "alignment.o"), str(src)], check=True)
+
+
+def test_pieces_that_no_32_bits_count_are_refused():
+    lib = block._load()
+    a = block._SCAN_ARGS.pack((1 << 31) - (1 << 16), (1 << 31) - (1 << 16), P, 1, 1, 1, 0, 0, 0, *(P, 1, 1) * 4, *(0, 0, 0) * 2, P, 0, 0, 0, 0)
+    g = block._SCAN_GRADS.pack(2 * P, 1, 1, *(0, 0, 0) * 5, 0, 0, 0, 0, 0)
+    assert lib.ttc_selective_scan_grad_workspace(0, a, g) == UNSUPPORTED

@@ -48,3 +48,28 @@ def test_gradients_of_float32_slices(act, at, width):
             else:
                 assert torch.equal(got[key], want[key]), key
     assert block.device_error(0) == 0
+
+
+def test_wrong_offsets_that_ask_for_more_pieces_than_32_bits_count(monkeypatch):
+    """1024 offsets that jump back and forth over 2^28 rows: 512 sequences of all the rows, 2^31 pieces of 64.  The first one has
+    its pieces, the others what is left of the room; scratch and outputs stay within their bounds."""
+    T, batch = (1 << 28) + 64, 1023
+    bf = torch.bfloat16
+    one, none = torch.ones((T, 1), device=DEV, dtype=bf), torch.zeros((T, 1), device=DEV, dtype=bf)
+    offsets = torch.zeros(batch + 1, device=DEV, dtype=torch.int32)
+    offsets[1::2] = T
+    kept = []
+
+    def guarded(need, x, stream):
+        block._check(min(need, 0))
+        kept.append((torch.full((need + 512,), 0x5a, dtype=torch.uint8, device=DEV), need))
+        return kept[-1][0], kept[-1][0].data_ptr() + 256
+
+    monkeypatch.setattr(block, "_workspace", guarded)
+    A, last = torch.full((1, 1), -0.5, device=DEV), torch.ones((batch, 1, 1), device=DEV)
+    got = block.selective_scan_grad(none, one, none, A, one, one, offsets=offsets, dstate_out=last, want=("dA", "dstate", "ddelta_bias"))
+    torch.cuda.synchronize()
+    for ws, need in kept:
+        assert bool((ws[:256] == 0x5a).all()) and bool((ws[256 + need:] == 0x5a).all())
+    assert float(got["dstate"][0]) == 1.0                            # steps of zero: nothing decays, and dy is zero
+    assert torch.isfinite(got["dA"]).all() and not got["dA"].any()   # no step, no share
