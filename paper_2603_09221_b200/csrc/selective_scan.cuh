@@ -51,7 +51,7 @@ struct ScanDev {
     float *local, *local_step;    // [pieces][d][n] and [pieces][d]: what a piece adds to a state, and its sum of D_t
 };
 
-// A log2(e).  Minus infinity becomes the lowest number: times the step 0 of a padding token it has to be 0.
+// A log2(e).  Minus infinity becomes the lowest number: times a step of 0 (of a padding token, or a softplus that underflows) it has to be 0.
 __device__ __forceinline__ float exponent(float A)
 {
     const float e = A * kLog2e;
@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(kStepThreads, 12) scan_step_kernel(const ScanD
         const float v = step * x;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            h[i] = fmaf(ex2(fmaf(step, a[i] * kLog2e, kExBias)), h[i], v * bb[i]);
+            h[i] = fmaf(ex2(fmaf(step, exponent(a[i]), kExBias)), h[i], v * bb[i]);
             y[0] = fmaf(h[i], cc[i], y[0]);
         }
         if (p.vec4) {

@@ -73,3 +73,34 @@ def test_wrong_offsets_that_ask_for_more_pieces_than_32_bits_count(monkeypatch):
         assert bool((ws[:256] == 0x5a).all()) and bool((ws[256 + need:] == 0x5a).all())
     assert float(got["dstate"][0]) == 1.0                            # steps of zero: nothing decays, and dy is zero
     assert torch.isfinite(got["dA"]).all() and not got["dA"].any()   # no step, no share
+
+
+@pytest.mark.parametrize("softplus", [True, False])
+@pytest.mark.parametrize("n", [16, 6])
+def test_a_decay_of_minus_infinity_in_single_tokens(n, softplus):
+    """What the prompt gives: a step of nothing (of zero, or a softplus below the numbers there are) keeps the state, any other
+    leaves the token's share.  Either side is off by at most 24 operations a token, of the magnitudes that were ever added."""
+    g = torch.Generator(device=DEV).manual_seed(14)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    batch, d = 3, 10
+    x, B, C, D, delta = r(batch, 4, d), r(batch, 4, n), r(batch, 4, n), r(d), r(batch, 4, d).abs()
+    delta[:, 1::2] = -200.0 if softplus else 0.0
+    A = -torch.rand((d, n), generator=g, device=DEV)
+    A[4], A[7, 1] = float("-inf"), float("-inf")
+    state = r(batch, d, n)
+    last, mag = torch.empty_like(state), state.abs()
+    y = block.selective_scan(x, delta, A, B, C, D=D, softplus=softplus, state=state, state_out=last)
+    steps = torch.nn.functional.softplus(delta) if softplus else delta
+    assert torch.isfinite(y).all() and torch.isfinite(last).all()
+    for t in range(4):
+        before = state.clone()
+        got = block.selective_scan_step(x[:, t], delta[:, t], A, B[:, t], C[:, t], state, D=D, softplus=softplus)
+        if t % 2:
+            assert torch.equal(state, before)
+        mag = mag + (steps[:, t] * x[:, t]).abs()[..., None] * B[:, t, None].abs()
+        room = 2 * (n + 24 * (t + 1)) * bu.U * ((mag * C[:, t, None].abs()).sum(-1) + (D * x[:, t]).abs())
+        assert bool(((got - y[:, t]).abs() <= room).all()), t
+    assert bool(((state - last).abs() <= 2 * 24 * 4 * bu.U * mag).all())
+    share = (torch.nn.functional.softplus(delta[:, 2, 4].double()) if softplus else delta[:, 2, 4].double()) * x[:, 2, 4].double()
+    want = share[:, None] * B[:, 2].double()
+    assert bool(((state[:, 4].double() - want).abs() <= 24 * bu.U * want.abs()).all())
