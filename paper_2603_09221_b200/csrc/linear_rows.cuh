@@ -263,7 +263,7 @@ __global__ void __launch_bounds__(256) slope_kernel(const SlopeDev p)
             for (int i = 0; i < V; ++i) {
                 float d = to_f(g.v[i]);
                 if (ACT != TTC_ACT_NONE)
-                    d *= act_slope<ACT>(to_f(z.v[i]));
+                    d = __fmul_rn(d, act_slope<ACT>(to_f(z.v[i])));  // (never one operation with the sum: dbias has the same bits with and without dZ)
                 s[i] += d;
                 o.v[i] = from_f<T>(d);
             }

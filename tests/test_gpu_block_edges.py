@@ -104,3 +104,15 @@ def test_a_decay_of_minus_infinity_in_single_tokens(n, softplus):
     share = (torch.nn.functional.softplus(delta[:, 2, 4].double()) if softplus else delta[:, 2, 4].double()) * x[:, 2, 4].double()
     want = share[:, None] * B[:, 2].double()
     assert bool(((state[:, 4].double() - want).abs() <= 24 * bu.U * want.abs()).all())
+
+
+@pytest.mark.parametrize("dtype", [F, torch.bfloat16])
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "softplus"])
+def test_each_gradient_of_an_activation_alone_has_the_same_bits(act, dtype):
+    g = torch.Generator(device=DEV).manual_seed(15)
+    r = lambda *s, t=torch.bfloat16: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+    for rows, k, m in ((77, 40, 64), (301, 33, 45)):
+        x, w, pre, dy = r(rows, k), r(m, k), r(rows, m), r(rows, m, t=dtype)
+        whole = block.linear_grad(dy, x, w, act=act, pre=pre)
+        for key in whole:
+            assert torch.equal(block.linear_grad(dy, x, w, act=act, pre=pre, want=(key,))[key], whole[key]), key
