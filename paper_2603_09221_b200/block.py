@@ -89,11 +89,13 @@ def _short_way(lib):
         if not os.path.exists(_build.STEP) or os.environ.get("TTC_LQR_REBUILD"):
             _build.build_step_binding(force=True)
         from . import _step as step
-    except (ImportError, OSError, subprocess.CalledProcessError) as e:
+        # with the records' sizes: one that was compiled with another header is refused
+        step.bind(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
+                    for k in ("ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_linear", "ttc_linear_workspace")),
+                  _CONV_ARGS.size, _SCAN_ARGS.size, _LINEAR_ARGS.size)
+    except (ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:
         warnings.warn("single-token calls take the slower way through Python: %s" % e)
         return _LongWay
-    step.bind(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
-                for k in ("ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_linear", "ttc_linear_workspace")))
     return step
 
 

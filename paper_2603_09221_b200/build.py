@@ -1,6 +1,7 @@
 """Build step of the CUDA library: nvcc, sm_100a only, in-tree output next to this file."""
 from __future__ import annotations
 
+import contextlib
 import glob
 import os
 import subprocess
@@ -28,6 +29,21 @@ def _stale(artefact=LIB):
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+@contextlib.contextmanager
+def _in_place(artefact):
+    """A path beside `artefact` to write to, which takes its place once it is whole: another process may load it meanwhile."""
+    stem, end = os.path.splitext(os.path.basename(artefact))
+    fd, path = tempfile.mkstemp(prefix=stem + ".", suffix=end, dir=os.path.dirname(artefact))
+    os.close(fd)
+    try:
+        yield path
+        os.chmod(path, 0o755)
+        os.replace(path, artefact)
+    except BaseException:
+        os.unlink(path)
+        raise
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     """Compile every ``csrc/*.cu`` (side by side) into ``libttc_lqr.so``; rebuilds when a source is newer."""
     if force or _stale():
@@ -41,11 +57,12 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
             failed = [subprocess.CalledProcessError(job.returncode, cmd) for cmd, job in jobs if job.wait()]
             if failed:
                 raise failed[0]
-            subprocess.run(nvcc + ["-shared", "-o", LIB] + objects, check=True)
+            with _in_place(LIB) as path:
+                subprocess.run(nvcc + ["-shared", "-o", path] + objects, check=True)
     return LIB
 
 
-def step_command():
+def step_command(output):
     """The compiler's call for ``_step.so`` (``csrc/step_binding.cpp``): a Python module against torch's own headers and libraries."""
     import sysconfig
     import torch
@@ -53,12 +70,13 @@ def step_command():
     inc = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
            os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include")]
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI]
-    cmd += ["-isystem" + i for i in inc] + ["-o", STEP, os.path.join(CSRC, "step_binding.cpp"), "-L" + os.path.join(root, "lib")]
+    cmd += ["-isystem" + i for i in inc] + ["-o", output, os.path.join(CSRC, "step_binding.cpp"), "-L" + os.path.join(root, "lib")]
     return cmd + ["-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch", "-ltorch_python"]
 
 
 def build_step_binding(force: bool = False) -> str:
     """Compile ``_step.so``, the short way into the calls for single tokens."""
     if force or _stale(STEP):
-        subprocess.run(step_command(), check=True)
+        with _in_place(STEP) as path:
+            subprocess.run(step_command(path), check=True)
     return STEP

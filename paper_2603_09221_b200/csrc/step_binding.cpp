@@ -232,11 +232,12 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t count)
     }
 }
 
-// Addresses of the library's functions, in the order of the declarations above.
+// Addresses of the library's functions, in the order of the declarations above, and the sizes of the records that they take (a module
+// that was compiled with another header than the library must not fill them).
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
 {
-    if (count != 4) {
-        PyErr_SetString(PyExc_TypeError, "bind takes four addresses");
+    if (count != 7) {
+        PyErr_SetString(PyExc_TypeError, "bind takes four addresses and three sizes");
         return nullptr;
     }
     void* at[4];
@@ -244,6 +245,16 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
         at[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred())
             return nullptr;
+    }
+    const long sizes[3] = {(long)sizeof(ttc_conv_args), (long)sizeof(ttc_scan_args), (long)sizeof(ttc_linear_args)};
+    for (int i = 0; i < 3; ++i) {
+        const long size = PyLong_AsLong(args[4 + i]);
+        if (PyErr_Occurred())
+            return nullptr;
+        if (size != sizes[i]) {
+            PyErr_Format(PyExc_ImportError, "_step.so was built for records of %ld bytes, not %ld: build it again", sizes[i], size);
+            return nullptr;
+        }
     }
     conv_step_call = reinterpret_cast<decltype(conv_step_call)>(at[0]);
     scan_step_call = reinterpret_cast<decltype(scan_step_call)>(at[1]);
