@@ -362,6 +362,15 @@ def layer_oracle(w, idx, T):
     return ref, time.perf_counter() - t0
 
 
+def projection_scratch(x, w, y):
+    """Bytes of scratch that ttc_linear asks for: none where the projection is one launch."""
+    from paper_2603_09221_b200 import block
+    types = [block._DTYPES[t.dtype] for t in (x, y)]
+    record = block._LINEAR_ARGS.pack(x.shape[0], x.shape[1], w.shape[0], *types, 0, 0, x.data_ptr(), w.data_ptr(), 0, 0, y.data_ptr(), 0,
+                                     x.stride(0), w.stride(0), 0, y.stride(0), 0)
+    return block._load().ttc_linear_workspace(x.get_device(), record)
+
+
 def run_layer(args):
     """--workload layer16 / layer32: one step = one ttc_lqr_solve_layer over the whole workload."""
     key = args.workload
@@ -456,16 +465,20 @@ def run_layer(args):
         for k in names:
             w[k] = flat[k].view(N, -1)
         ins[:9] = [w[k] for k in names]
+        # gates, weights and diag(R^-1) are positive; the state and the mixing of A and B are not held to that
+        acts = {k: "none" if k in ("s_a", "s_b", "h0") else "softplus" for k in names}
 
         def project():
-            for k in names:                # gates, weights and diag(R^-1) are positive; the state and the mixing of A and B are not held to that
-                block.linear(x, weights[k], act="none" if k in ("s_a", "s_b", "h0") else "softplus", y=flat[k])
+            for k in names:
+                block.linear(x, weights[k], act=acts[k], y=flat[k])
 
         def leave():
             u_rows.copy_(u1.view(rows, heads * n))
             block.linear(u_rows, w_out, residual=x, y=y)
 
-        block_launches = len(names) + 1
+        # a projection without scratch is one launch (neither parts of its contraction nor rows to be copied); else it is not known here
+        projections = [(x, weights[k], flat[k]) for k in names] + [(u_rows, w_out, y)]
+        block_launches = None if any(projection_scratch(*p) for p in projections) else len(projections)
 
     def step():
         project()
@@ -503,7 +516,8 @@ def run_layer(args):
         step()
         e1[i].record()
     barrier()
-    launches = solver.query(lqr.TTC_QUERY_TOTAL_LAUNCHES) - launches0 + args.steps * block_launches
+    launches = solver.query(lqr.TTC_QUERY_TOTAL_LAUNCHES) - launches0
+    launches = None if block_launches is None else launches + args.steps * block_launches
     clocks = sampler.stop() if rank == 0 else None
     per_step = [e0[i].elapsed_time(e1[i]) for i in range(args.steps)]
     value, ms_per_step, _ = sharding.aggregate_throughput(N, sum(per_step) / len(per_step), device=dev)
@@ -544,7 +558,23 @@ def run_layer(args):
                              % peaks["sm_max_mhz"],
                 "algorithmic_flops_per_launch": N * flops_i, "algorithmic_bytes_per_launch": N * (bin_i + bout_i),
                 "hbm_frac": (N * (bin_i + bout_i) / (kernel_ms * 1e-3) / 1e9) / peaks["hbm_gbs"]}
+    kernel = "sigma_product (baseline)" if baseline else "ttc_layer"
+    outputs, row_errs = ["u1", "P0", "info"], {}
+    if args.from_tokens > 0:
+        # the time is that of several kernels with bounds of their own: no fraction of one
+        roofline, kernel, outputs = None, "%d x ttc_linear, %s" % (len(projections), kernel), outputs + ["y"]
     cpu = None
+    if args.from_tokens > 0 and not args.no_cpu_baseline:
+        # sampled token rows of every projection in 64 bits, from what it was handed: float32 results are off by 32 u of a segment's norm
+        # (u = 2^-24), the activation and the sums by less; the output row is rounded to bfloat16, half a step 2^-8
+        at = torch.unique(torch.linspace(0, rows - 1, 64, device=dev).long())
+        rel = lambda got, want: float((got.double() - want).norm() / want.norm())  # noqa: E731
+        for k in names:
+            z = x[at].double() @ weights[k].double().t()
+            row_errs[k] = rel(flat[k][at], torch.nn.functional.softplus(z) if acts[k] == "softplus" else z)
+        row_errs["u_rows"] = rel(u_rows[at], u1.view(rows, -1)[at].double())
+        row_errs["y"] = rel(y[at], u_rows[at].double() @ w_out.double().t() + x[at].double())
+        assert all(v <= (2.0 ** -8 + 1e-5 if k in ("u_rows", "y") else 1e-5) for k, v in row_errs.items()), row_errs
     if not args.no_cpu_baseline and world == 1:
         idx = np.unique(np.linspace(0, N - 1, args.cpu_sample if not gradient else max(8, args.cpu_sample // 64)).astype(np.int64))
         from tests import parity_util as pu
@@ -581,14 +611,16 @@ def run_layer(args):
         cpu = {"value": len(idx) / dt, "unit": "instances/s", "cores": int(ref["threads"]), "kind": "oracle",
                "sample": "%d instances spread over the workload (parameter synthesis in numpy + C recursion)" % len(idx),
                "seconds": dt, "parity_max_rel_err": errs, "speedup_gpu_over_cpu": value / (len(idx) / dt)}
+        if row_errs:
+            cpu["parity_rows_rel_norm"] = row_errs
     print(json.dumps({"metric": "lqr_instances_per_sec", "value": value, "unit": "instances/s", "n_gpus": world,
                       "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms_per_step, "higher_is_better": True,
                       "scaling": "weak", "vs_baseline": None, "dtype": "f32", "data": "synthetic",
                       "config": {"workload": c["name"], "n": n, "r": r, "T": T, "instances": N, "batch": list(c["batch"]),
-                                 "outputs": ["u1", "P0", "info"], "kernel": "sigma_product (baseline)" if baseline else "ttc_layer",
+                                 "outputs": outputs, "kernel": kernel,
                                  "l2": "working set fits L2: a 192 MB buffer is written between timed steps"},
-                      "roofline": roofline, "cpu_baseline": cpu, "e2e": e2e, "gpu_launches": int(launches),
-                      "launches_per_step": launches / args.steps, "clocks": clocks}))
+                      "roofline": roofline, "cpu_baseline": cpu, "e2e": e2e, "gpu_launches": launches and int(launches),
+                      "launches_per_step": launches and launches / args.steps, "clocks": clocks}))
     solver.close()
     if dist:
         td.destroy_process_group()
