@@ -156,7 +156,7 @@ int64_t ttc_linear_workspace(int32_t device, const ttc_linear_args* a);
 int ttc_linear(int32_t device, const ttc_linear_args* a, void* workspace, int64_t workspace_bytes, void* cuda_stream);
 
 /*
- * Gradients of ttc_linear given dy [rows][m] (type `out_dtype`, row stride ldy; the gradient of the residual is dy itself):
+ * Gradients of ttc_linear given dy [rows][m] (type `out_dtype`, row stride lddy; the gradient of the residual is dy itself):
  *     dZ = dy act'(pre);   dx = dZ W [rows][k],   dw = dZ' x [m][k],   dbias = sum over the rows of dZ [m] (float32).
  * pre is what the forward call wrote (needed unless act is TTC_ACT_NONE).  dZ is rounded to `dtype` for the products
  * (their operands; a relative 2^-9 for bfloat16, as the rounding of dx and dw themselves), not for dbias.  dx and dw are of
