@@ -96,35 +96,46 @@ inline int check_sequences(int64_t batch, int64_t tokens, const int32_t* offsets
 
 inline Rows dev_rows(const ttc_rows& r, const int32_t* offsets) { return Rows{r.ptr, offsets ? 0 : r.bstride, r.tstride}; }
 
-// Rows of an output and of an input that share elements, or may: ranges that meet, unless they are different columns of one
-// wider matrix (equal strides, one a multiple of the other).  Equal strides of another kind say nothing; the caller is believed.
+inline int64_t floor_div(int64_t a, int64_t b) { return a / b - (a % b != 0 && (a < 0) != (b < 0)); }
+
+// Rows of an output and of an input that share elements, or may.  Where the strides are the same, they share one if the distance
+// of their first elements is i S + j s + c for differences i, j of sequences and tokens and c of columns: for each i (S the larger
+// stride: few come into question) the j that leaves the least c is looked at.  Other strides, or rows that overlap one another
+// so often that i is not soon found: ranges that meet.
 inline bool rows_overlap(const ttc_rows& a, int64_t wa, const ttc_rows& b, int64_t wb, int64_t batch, int64_t tokens, bool packed, size_t size)
 {
     if (!a.ptr || !b.ptr || batch <= 0 || tokens <= 0)
         return false;
-    const int64_t nb = packed ? 0 : batch - 1;
+    const int64_t nb = packed ? 0 : batch - 1, nt = tokens - 1;
     const char *a0 = static_cast<const char*>(a.ptr), *b0 = static_cast<const char*>(b.ptr);
-    const char* a1 = a0 + (nb * a.bstride + (tokens - 1) * a.tstride + wa) * (int64_t)size;
-    const char* b1 = b0 + (nb * b.bstride + (tokens - 1) * b.tstride + wb) * (int64_t)size;
+    const char* a1 = a0 + (nb * a.bstride + nt * a.tstride + wa) * (int64_t)size;
+    const char* b1 = b0 + (nb * b.bstride + nt * b.tstride + wb) * (int64_t)size;
     if (a1 <= b0 || b1 <= a0)
         return false;
-    if (a0 == b0)
+    if ((nt > 0 && a.tstride != b.tstride) || (nb > 0 && a.bstride != b.bstride))
         return true;
-    const bool by_token = tokens > 1, by_batch = nb > 0;
-    if ((by_token && a.tstride != b.tstride) || (by_batch && a.bstride != b.bstride))
-        return true;
-    int64_t period = by_token ? a.tstride : by_batch ? a.bstride : 0;
-    if (by_token && by_batch) {
-        const int64_t lo = a.tstride < a.bstride ? a.tstride : a.bstride, hi = a.tstride < a.bstride ? a.bstride : a.tstride;
-        if (lo == 0 || hi % lo)
-            return false;
-        period = lo;
+    int64_t S = nt > 0 ? a.tstride : 0, nS = nt, s = nb > 0 ? a.bstride : 0, ns = nb;
+    if (S < s) {
+        const int64_t t = S, n = nS;
+        S = s, nS = ns, s = t, ns = n;
     }
-    if (period == 0)
+    const int64_t far = (b0 - a0) / (int64_t)size, least = 1 - wb, most = wa - 1;               // c in least .. most
+    int64_t i0 = 0, i1 = 0;
+    if (S > 0) {
+        i0 = -floor_div(most + ns * s - far, S), i1 = floor_div(far - least + ns * s, S);
+        i0 = i0 < -nS ? -nS : i0, i1 = i1 > nS ? nS : i1;
+    }
+    if (i1 - i0 > 64)
         return true;
-    int64_t shift = (b0 - a0) / (int64_t)size % period;
-    shift = shift < 0 ? shift + period : shift;
-    return shift < wa || shift + wb > period;
+    for (int64_t i = i0; i <= i1; ++i) {
+        const int64_t left = far - i * S;
+        int64_t j = s > 0 ? floor_div(left - least, s) : 0;
+        j = j > ns ? ns : j;
+        const int64_t c = left - j * s;
+        if (j >= -ns && c >= least && c <= most)
+            return true;
+    }
+    return false;
 }
 
 inline bool ranges_meet(const void* a, size_t bytes_a, const void* b, size_t bytes_b)

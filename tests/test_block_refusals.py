@@ -248,3 +248,34 @@ def test_pieces_that_no_32_bits_count_are_refused():
     a = block._SCAN_ARGS.pack((1 << 31) - (1 << 16), (1 << 31) - (1 << 16), P, 1, 1, 1, 0, 0, 0, *(P, 1, 1) * 4, *(0, 0, 0) * 2, P, 0, 0, 0, 0)
     g = block._SCAN_GRADS.pack(2 * P, 1, 1, *(0, 0, 0) * 5, 0, 0, 0, 0, 0)
     assert lib.ttc_selective_scan_grad_workspace(0, a, g) == UNSUPPORTED
+
+
+def test_which_rows_overlap():
+    """Outputs may lie in the same storage as inputs, in other columns, tokens or sequences; what is refused is rows that share an
+    element (or rows of other strides whose ranges meet).  Against a count of the elements."""
+    import random
+    lib = block._load()
+    rng = random.Random(3)
+
+    def elements(at, batch, tokens, bs, ts, d):
+        return {at + b * bs + t * ts + c for b in range(batch) for t in range(tokens) for c in range(d)}
+
+    def refused(batch, tokens, d, x, xb, xt, y, yb, yt):
+        a = _conv(batch=batch, tokens=tokens, d=d, dtype=0, x=P + 4 * x, xb=xb, xt=xt)
+        g = block._CONV_GRADS.pack(64 * P, xb, xt, P + 4 * y, yb, yt, 0, 0, 0, 0)
+        need = lib.ttc_causal_conv_grad_workspace(0, a, g)
+        assert need == INVALID or need >= 0
+        return need == INVALID
+
+    assert not refused(2, 64, 16, 0, 128 * 16, 16, 64 * 16, 128 * 16, 16)           # the first tokens and the last ones of a batch
+    assert refused(2, 65, 16, 0, 128 * 16, 16, 64 * 16, 128 * 16, 16)
+    assert refused(2, 64, 16, 0, 128 * 16, 16, 16, 128 * 16, 16)                    # one token on
+    assert not refused(1, 8, 16, 0, 0, 32, 16, 0, 32)                               # beside one another
+    assert refused(4, 3, 16, 0, 64, 16, 48, 64, 16)                                 # three tokens of four, and on from the fourth into the next
+    assert not refused(3, 8, 16, 0, 16, 96, 48, 16, 96)                             # [tokens, batch, channels], batches beside one another
+    for _ in range(4000):
+        batch, tokens, d = rng.randint(1, 4), rng.randint(1, 6), rng.randint(1, 5)
+        strides = [rng.choice((0, 1, 2, 3, 5, 7, 10, 30, 31)) + rng.choice((0, 0, d, d * tokens)) for _ in range(2)]
+        x, y = rng.randint(0, 60), rng.randint(0, 60)
+        same = bool(elements(x, batch, tokens, *strides, d) & elements(y, batch, tokens, *strides, d))
+        assert refused(batch, tokens, d, x, *strides, y, *strides) == same, (batch, tokens, d, x, y, strides)

@@ -116,3 +116,21 @@ def test_each_gradient_of_an_activation_alone_has_the_same_bits(act, dtype):
         whole = block.linear_grad(dy, x, w, act=act, pre=pre)
         for key in whole:
             assert torch.equal(block.linear_grad(dy, x, w, act=act, pre=pre, want=(key,))[key], whole[key]), key
+
+
+def test_outputs_in_other_tokens_of_the_inputs_storage():
+    g = torch.Generator(device=DEV).manual_seed(16)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV)  # noqa: E731
+    for batch in (1, 3):
+        room, d, n = r(batch, 130, 24), 24, 8
+        x, y = room[:, :65], room[:, 65:]
+        taps, A, B = r(d, 4), -r(d, n).abs(), r(batch, 65, n)
+        want = block.causal_conv(x.clone(), taps, act="silu")
+        assert torch.equal(block.causal_conv(x, taps, act="silu", y=y), want)
+        want = block.selective_scan(x.clone(), x.clone(), A, B, B, softplus=True)
+        assert torch.equal(block.selective_scan(x, x, A, B, B, softplus=True, y=y), want)
+        dy = r(batch, 65, d)
+        want = block.causal_conv_grad(dy, x.clone(), taps, want=("dx",))["dx"]
+        assert torch.equal(block.causal_conv_grad(dy, x, taps, want=("dx",), out={"dx": y})["dx"], want)
+        with pytest.raises(Exception, match="overlap"):
+            block.causal_conv(x, taps, y=room[:, 64:129])
