@@ -432,26 +432,31 @@ def selective_scan_grad(dy, x, delta, A, B, C, D=None, z=None, delta_bias=None, 
 
 # ---- projections --------------------------------------------------------------------------------------------------------
 
+def _on(stream, f):
+    """f() with `stream` as the current one."""
+    if stream is None:
+        return f()
+    with torch.cuda.stream(stream):
+        return f()
+
+
 def _matrix(t, name, cols, dtype, device, rows=None, stream=None, output=False):
     """``t`` as ``[rows, cols]``, its address, rows and row stride.  Leading dimensions are taken together; inputs whose rows
-    no single stride describes are copied."""
+    no single stride describes, or lie over one another (a row for all tokens, by ``expand``), are copied."""
     if t is None:
         return None, 0, 0, 0
     shape = t.shape
     if len(shape) < 1 or shape[-1] != cols or t.dtype is not dtype or t.get_device() != device:
         _explain(t, name, (*shape[:-1], cols), dtype, device)
     if len(shape) != 2:
-        if output:
-            t = t.view(-1, cols) if t.numel() else t.reshape(0, cols)
-        elif stream is None:
-            t = t.reshape(-1, cols) if t.numel() else t.reshape(0, cols)
-        else:
-            with torch.cuda.stream(stream):
-                t = t.reshape(-1, cols) if t.numel() else t.reshape(0, cols)
+        lead = (-1, cols) if t.numel() else (0, cols)
+        t = t.view(lead) if output else _on(stream, lambda: t.reshape(lead))
         shape = t.shape
     ld, one = t.stride()
     if (one != 1 and cols > 1 and shape[0]) or (rows is not None and shape[0] != rows):
         raise ValueError("%s must be %s rows of contiguous elements, got %s with strides %s" % (name, rows, tuple(shape), t.stride()))
+    if ld < cols and shape[0] > 1 and not output:
+        t, ld = _on(stream, t.contiguous), cols
     return t, t.data_ptr(), shape[0], ld
 
 
@@ -479,7 +484,7 @@ def linear(x, w, bias=None, act="none", residual=None, y=None, pre=None, out_dty
         raise TypeError("outputs are of x's type or float32, not %s" % out_dtype)
     m, k = w.shape
     x2, px, rows, ldx = _matrix(x, "x", k, dtype, dev, None, stream)
-    _, pw, _, ldw = _matrix(w, "w", k, dtype, dev)
+    w2, pw, _, ldw = _matrix(w, "w", k, dtype, dev, None, stream)
     if residual is not None and residual.shape[:-1] != x.shape[:-1]:
         raise ValueError("residual must be %s, got %s" % ((*x.shape[:-1], m), tuple(residual.shape)))
     r2, pr, _, ldr = _matrix(residual, "residual", m, out_dtype, dev, rows, stream)
@@ -519,7 +524,7 @@ def linear_grad(dy, x, w, act="none", pre=None, want=LINEAR_GRAD_KEYS, out=None,
     if dy.shape != (*x.shape[:-1], m):
         raise ValueError("dy must be %s, got %s" % ((*x.shape[:-1], m), tuple(dy.shape)))
     x2, px, rows, ldx = _matrix(x, "x", k, dtype, dev, None, stream)
-    _, pw, _, ldw = _matrix(w, "w", k, dtype, dev)
+    w2, pw, _, ldw = _matrix(w, "w", k, dtype, dev, None, stream)
     p2, pp, _, ldp = _matrix(pre, "pre", m, dtype, dev, rows, stream)
     d2, pdy, _, lddy = _matrix(dy, "dy", m, dy.dtype, dev, rows, stream)
     _device_of(x)

@@ -134,3 +134,34 @@ def test_outputs_in_other_tokens_of_the_inputs_storage():
         assert torch.equal(block.causal_conv_grad(dy, x, taps, want=("dx",), out={"dx": y})["dx"], want)
         with pytest.raises(Exception, match="overlap"):
             block.causal_conv(x, taps, y=room[:, 64:129])
+
+
+@pytest.mark.parametrize("rows", [5, 70])
+def test_one_row_for_all_tokens(rows):
+    """Operands of projections that are the same row again and again (expand), or rows that lie over one another, as the others:
+    the same bits as from copies, on the current stream and on a named one."""
+    g = torch.Generator(device=DEV).manual_seed(17)
+    r = lambda *s, t=torch.bfloat16: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+    k, m = 40, 24
+    x, w, res, dy, pre = r(rows, k), r(m, k), r(rows, m), r(rows, m), r(rows, m)
+    line = r(16 * max(rows, m) + k)
+    again = dict(x=x[:1].expand(rows, k), w=w[:1].expand(m, k), residual=res[:1].expand(rows, m), dy=dy[:1].expand(rows, m), pre=pre[:1].expand(rows, m))
+    over = dict(x=line.as_strided((rows, k), (8, 1)), w=line.as_strided((m, k), (8, 1)), residual=line.as_strided((rows, m), (1, 1)),
+                dy=line.as_strided((rows, m), (16, 1)), pre=line.as_strided((rows, m), (8, 1)))
+    batched = dict(x=x[None, :1].expand(rows, 2, k)[:, 0], residual=res[None].expand(2, rows, m)[1])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for some in (again, over, batched):
+        for name, t in some.items():
+            a = {**dict(x=x, w=w, residual=res, dy=dy, pre=pre), name: t}
+            b = {**a, name: t.contiguous()}
+            for stream in (None, side):
+                forward = lambda v: block.linear(v["x"], v["w"], residual=v["residual"], act="silu", stream=stream)  # noqa: E731
+                back = lambda v: block.linear_grad(v["dy"], v["x"], v["w"], act="silu", pre=v["pre"], stream=stream)  # noqa: E731
+                torch.cuda.synchronize()
+                assert torch.equal(forward(a), forward(b)), name
+                one, two = back(a), back(b)
+                side.synchronize()
+                assert all(torch.equal(one[q], two[q]) for q in one), name
+    with pytest.raises(Exception):                                   # but no output
+        block.linear(x, w, y=res[:1].expand(rows, m))
