@@ -165,3 +165,78 @@ def test_one_row_for_all_tokens(rows):
                 assert all(torch.equal(one[q], two[q]) for q in one), name
     with pytest.raises(Exception):                                   # but no output
         block.linear(x, w, y=res[:1].expand(rows, m))
+
+
+def test_rows_past_32_bits():
+    """Rows whose elements lie more than 2^31 behind the first: the last tokens are what a call on them alone gives, from the window and
+    state in front of them.  (A state that begins 4000 tokens earlier has forgotten, at decays below exp(-0.2 D), what was before.)"""
+    g = torch.Generator(device=DEV).manual_seed(18)
+    r = lambda *s, t=torch.bfloat16: torch.randn(s, generator=g, device=DEV, dtype=t)  # noqa: E731
+    T, d, n = 530000, 4096, 4
+    assert (T - 1000) * d > 2 ** 31
+    x, taps, A, B = r(1, T, d), r(d, 4, t=F), -torch.rand((d, n), generator=g, device=DEV) - 0.2, r(1, T, n)
+    y = block.causal_conv(x, taps, act="silu")
+    tail, before = (lambda t: t[:, T - 1000:].contiguous()), (lambda t: t[:, T - 5000:T - 1000].contiguous())  # noqa: E731
+    window = x[:, T - 1003:T - 1000].contiguous()
+    assert torch.equal(tail(y), block.causal_conv(tail(x), taps, act="silu", state=window))
+    dx = block.causal_conv_grad(y, x, taps, act="silu", want=("dx",))["dx"]
+    assert torch.equal(tail(dx), block.causal_conv_grad(tail(y), tail(x), taps, act="silu", state=window, want=("dx",))["dx"])
+    state, last, end = (torch.empty((1, d, n), device=DEV) for _ in range(3))
+    block.selective_scan(before(x), before(y), A, before(B), before(B), softplus=True, state_out=state)
+    want = block.selective_scan(tail(x), tail(y), A, tail(B), tail(B), softplus=True, state=state, state_out=last)
+    out = block.selective_scan(x, y, A, B, B, softplus=True, state_out=end, y=dx)
+    close = lambda a, b, limit: float((a.double() - b.double()).norm() / b.double().norm()) <= limit  # noqa: E731
+    assert close(tail(out), want, 1e-4) and close(end, last, 1e-6)   # (a rounding to bfloat16 that falls the other way now and then)
+    del out, dx
+    got = block.selective_scan_grad(y, x, y, A, B, B, softplus=True, want=("ddelta", "dB"))
+    want = block.selective_scan_grad(tail(y), tail(x), tail(y), A, tail(B), tail(B), softplus=True, state=state, want=("ddelta", "dB"))
+    for key in want:
+        assert close(tail(got[key]), want[key], 1e-4), key
+
+
+def test_projections_past_32_bits():
+    g = torch.Generator(device=DEV).manual_seed(19)
+    r = lambda *s: torch.randn(s, generator=g, device=DEV, dtype=torch.bfloat16)  # noqa: E731
+    rows, k, m = 70001, 64, 32776
+    x, w, res = r(rows, k), r(m, k), r(rows, m)
+    end = slice(rows - 300, rows)
+    assert end.start * m > 2 ** 31
+    assert torch.equal(block.linear(x, w, residual=res, act="silu")[end], block.linear(x[end], w, residual=res[end], act="silu"))
+    dx, want = block.linear_grad(res, x, w, want=("dx",))["dx"][end].double(), res[end].double() @ w.double()
+    # half a step of bfloat16, and 2 u of the magnitudes for each 16 of the products
+    room = 2.0 ** -8 * want.abs() + 2 * bu.U * (m / 16 + 8) * (res[end].double().abs() @ w.double().abs())
+    assert bool(((dx - want).abs() <= room).all()) and block.device_error(0) == 0
+
+
+def test_calls_from_several_threads():
+    """Each thread on a stream of its own, with its own states: single tokens, projections and gradients at once."""
+    import threading
+    bf = torch.bfloat16
+
+    def work(seed, out):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        r = lambda *s, t=bf: torch.randn(s, generator=g, device=DEV).to(t)  # noqa: E731
+        x, w, taps, A, B = r(6, 64), r(64, 64) * 0.125, r(64, 4, t=F) * 0.5, -r(64, 16, t=F).abs(), r(6, 16) * 0.25
+        window, state = torch.zeros((6, 3, 64), device=DEV, dtype=bf), torch.zeros((6, 64, 16), device=DEV)
+        got = []
+        for _ in range(40):
+            c = block.causal_conv_step(block.linear(x, w), taps, window, act="silu")
+            x = block.linear(block.selective_scan_step(c, c, A, B, B, state, softplus=True), w, residual=x) * 0.1
+            got += [x, block.linear_grad(x, c, w)["dw"], block.selective_scan_grad(x[None], c[None], c[None], A, B[None], B[None], softplus=True)["dA"]]
+        torch.cuda.current_stream().synchronize()
+        out[seed] = [*got, window, state]
+
+    def on_a_stream(seed, out):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            work(seed, out)
+
+    alone, together = {}, {}
+    for seed in range(4):
+        work(seed, alone)
+    threads = [threading.Thread(target=on_a_stream, args=(seed, together)) for seed in range(4)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    torch.cuda.synchronize()
+    assert sorted(together) == sorted(alone)
+    for seed in alone:
+        assert all(torch.isfinite(a).all() and torch.equal(a, b) for a, b in zip(alone[seed], together[seed])), seed
