@@ -13,8 +13,9 @@ using namespace ttc::lin;
 namespace {
 
 // Rows up to which W is streamed past all of x (few_rows_kernel) instead of going through tiles of 128 rows.  2048 -> 4096,
-// 1024 -> 1024 and 8192 -> 8192: 32 rows 9.3, 4.8 and 33.8 us, by tiles 11.9, 7.5 and 36.4; 64 rows 14.3, 8.2 and 58.6 (by a form for as
-// many), by tiles 12.3, 7.5 and 36.5.
+// 1024 -> 1024 and 8192 -> 8192: 32 rows 9.3, 4.9 and 33.7 us, by tiles 11.2, 6.6 and 35.6; 64 rows 14.3, 8.2 and 58.6 (by a form for as
+// many), by tiles 11.3, 6.7 and 35.5.  Rows that cannot be read by 16 bytes: 2047 -> 4095, 8 rows 15.8 us and 32 rows 39.5, against 34.5 for
+// 64 rows by tiles, most of it the copies of W and x.
 constexpr int kFewRows = 32;
 
 // Parts of the contraction of few_rows_kernel, the blocks of a cluster: while all blocks are at work at once, two to an SM, and a part has 1024
@@ -118,13 +119,13 @@ struct Product {
 
 // Width of a tile and parts of the contraction.  A block of 64 contraction indices takes about 400 + 1.75 BN clocks: filling
 // and reading its (128 + BN) x 128 bytes of shared memory, twice 128 + BN clocks, and what goes with it; so the width is the
-// one with the least of that times the rounds of tiles over the SMs (512 x 4096 results over 2048 indices: 64 wide 21.9 us in two
-// rounds, 128 wide in one 15).  In the same unit (a quarter of a clock) a pair's block costs kPairCost: 8192 x 2048 over 4096 99 us
-// in pairs and 105 without, 4096 x 2048 over 2048 28.9 and 30.4, but 512 x 4096 over 2048 18.0 and 14.7, 1024 x 2304 over 1024 13.4 and 10.4.
+// one with the least of that times the rounds of tiles over the SMs (512 x 4096 results over 2048 indices: 64 wide 19.7 us in two
+// rounds, 128 wide in one 13.7).  In the same unit (a quarter of a clock) a pair's block costs kPairCost: 8192 x 2048 over 4096 97 us
+// in pairs and 104 without, 4096 x 2048 over 2048 28.2 and 29.9, but 512 x 4096 over 2048 16.7 and 13.6, 1024 x 2304 over 1024 11.9 and 9.2.
 constexpr int64_t kPairCost = 3050;
 // Results with few tiles split the contraction too, in parts of at least 512 indices that a launch of its own sums.  That
-// costs about 4 us, a block of 64 about 0.2: 64 x 2048 over 4096 (four parts) 19.6 -> 11.8 us, 256 x 2048 over 4096 (two) 20.1 -> 17.5, but
-// 128 x 4096 over 2048 (two) 12.5 -> 13.9 and 64 x 1024 over 1024 7.6 -> 8.4; so as many blocks have to be saved:
+// costs about 4 us, a block of 64 about 0.2: 64 x 2048 over 4096 (four parts) 18.6 -> 10.6 us, 256 x 2048 over 4096 (two) 19.0 -> 16.0, but
+// 128 x 4096 over 2048 (two) 11.5 -> 12.5 and 64 x 1024 over 1024 6.7 -> 7.0; so as many blocks have to be saved:
 constexpr int64_t kWorthSplit = 24;
 // float32 results: contractions longer than kLong are added up in registers every kSegment indices.
 constexpr int64_t kSegment = 512, kLong = 1024;

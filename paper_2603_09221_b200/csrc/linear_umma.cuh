@@ -10,10 +10,10 @@
 // gradients') is staged in boxes of 64 contiguous rows by 64 contraction indices and described to the instruction as MN-major;
 // nothing is transposed.  Rows, columns and contraction indices past the end are filled with zeros by TMA.
 //
-// bfloat16, 8192 x 8192 over 8192: 692 us, 1589 TFLOP/s (torch.mm in the same loop 682 to 728); 8192 x 2048 over 4096 93 us alone and 97
-// back to back (92, 93), where power bounds both.  512 x 4096 over 2048 13.7 us (9.1): one round of tiles, whose start and end
+// bfloat16, 8192 x 8192 over 8192: 692 to 738 us by the clock, 1589 TFLOP/s (torch.mm in the same loops 682 to 787); 8192 x 2048 over 4096 93 us alone
+// and 97 back to back (92, 94), where power bounds both.  512 x 4096 over 2048 13.7 us (9.9): one round of tiles, whose start and end
 // nothing hides.  Float32 results with softplus, 4096 x 2304 over 1024: 26.8 us, of which the end of a tile, 9 us, comes twice.
-// Sums in segments: 4096 x 2048 over 2048 38 us (30 without).
+// Sums in segments: 4096 x 2048 over 2048 36 us (30 without).
 #pragma once
 
 #include <cuda.h>

@@ -1,7 +1,7 @@
 """What selective scans and their gradients keep over long sequences in float32: every output within a bound that is carried along
 with the recurrences (scan_bounds.py: it forgets what the state forgets), and small in the 2-norm.
 
-The 2-norm.  The exponentials' mean error, at most 1.2e-8, adds up over a memory of 200 tokens to 2.4e-6; what is random in a token's
+The 2-norm.  The mean error of the exponentials of decays that last, at most 1.2e-8, adds up over a memory of 200 tokens to 2.4e-6; what is random in a token's
 decay, product and sums is below 2^-22 and adds up in squares, 14 times that, 3.4e-6; sums over states and channels by less.  1e-5 is
 allowed to what holds a state or a co-state, twice that to what holds both."""
 import numpy as np
