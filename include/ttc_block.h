@@ -8,6 +8,7 @@
  *   ttc_causal_conv             short depthwise causal convolution of token rows
  *   ttc_selective_scan          state space recurrence with a diagonal, token-dependent transition: the memory layer that a
  *                               hybrid model runs beside the control layer
+ *   ttc_decay_attention         linear attention with a decay for each head: the same with a matrix for a state, in chunks
  * each with its gradients (.._grad) and, for decoding, a form for single tokens (.._step; ttc_linear takes few rows itself).
  *
  * TOKEN ROWS.  A ttc_rows names a matrix of token rows: channel c of token t of sequence b is element
@@ -18,7 +19,7 @@
  *            seq_offsets[b + 1] of ONE matrix of `tokens` rows (bstride is ignored).  Sequences may be empty.  Rows outside
  *            every sequence are neither used nor written.  Offsets are clamped to [0, tokens] on the device, so wrong
  *            ones give wrong results but no access out of range.
- * Element types: TTC_F32, TTC_BF16, TTC_F16; all row operands of a call have the same one (ttc_linear: see there).
+ * Element types: TTC_F32, TTC_BF16, TTC_F16; all row operands of a call have the same one (ttc_linear, ttc_decay_attention: see there).
  * Arithmetic, sums and states are float32.  Parameter vectors (A, D, bias, convolution taps) and their gradients are float32.
  *
  * CALLS.  Every pointer is device memory of `device` and owned by the caller, aligned to its element.  A call is
@@ -140,6 +141,54 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
                             int64_t workspace_bytes, void* cuda_stream);
 
 /*
+ * Linear attention with a decay for each head.  Per head h of `heads`, with the group g(h) = h / (heads / groups) of its queries and keys:
+ *     D_t = delta_t + delta_bias;  with softplus: D_t = log(1 + exp(delta_t + delta_bias));  delta missing: D_t = 1
+ *     S_t = exp(A D_t) S_{t-1} + k_t[g] v_t'              [dk][dv]
+ *     y_t = scale q_t[g] S_t
+ * q and k rows hold groups * dk elements, v and y rows heads * dv, delta rows `heads`; dk, dv 1 .. 128.  Rows are bfloat16 or float16.
+ * A [heads], delta_bias [heads] (NULL: 0; not used without delta).  state [batch][heads][dk][dv] float32 is S in front of every sequence
+ * (NULL: zero), state_out receives the last one; it may be state itself.  y may be v (the same pointer and strides).
+ * Exponents A D_t are expected to be <= 0; minus infinity forgets everything.  Tokens go through the tensor cores in chunks of 128, counted from their
+ * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, and of those behind it.  float16: products scale q . k, and in the
+ * gradients dy . v, have to stay below 65504.  Scratch: 6 bytes for each element of a state (dk, dv rounded up to 64 or 128) of every chunk.
+ */
+typedef struct ttc_decay_args {
+    int64_t batch, tokens;
+    const int32_t* seq_offsets;
+    int32_t heads, groups, dk, dv, dtype, softplus;
+    float scale;
+    int32_t reserved;
+    ttc_rows q, k, v, delta, y;
+    const float *A, *delta_bias;
+    const float* state;
+    float* state_out;
+} ttc_decay_args;
+
+int64_t ttc_decay_attention_workspace(int32_t device, const ttc_decay_args* a);
+int ttc_decay_attention(int32_t device, const ttc_decay_args* a, void* workspace, int64_t workspace_bytes, void* cuda_stream);
+
+/* One token of each of `batch` sequences (as ttc_causal_conv_step): S in `state_out` is moved on in place, `state` is not used. */
+int ttc_decay_attention_step(int32_t device, const ttc_decay_args* a, void* cuda_stream);
+
+/*
+ * Gradients of ttc_decay_attention given dy and, optionally, the gradient dstate_out of the last states (NULL: zero).  `a` as in
+ * the forward call (y and state_out are ignored).  With Z_t = scale q_t dy_t' + exp(A D_{t+1}) Z_{t+1}:
+ *     dq_t = scale S_t dy_t    dk_t = Z_t v_t    dv_t = Z_t' k_t    (dq, dk summed over the heads of a group)
+ *     dD_t = A exp(A D_t) <Z_t, S_{t-1}>         dA = sum_t D_t exp(A D_t) <Z_t, S_{t-1}>
+ * ddelta from dD_t through the softplus, ddelta_bias its sum over all tokens; dA, ddelta_bias [heads], dstate [batch][heads][dk][dv] float32; the row
+ * gradients in the rows' type.  Scratch: 12 bytes for each element of a state of every chunk, and, where heads share queries and keys, 8 dk for every token and head.
+ */
+typedef struct ttc_decay_grads {
+    ttc_rows dy, dq, dk, dv, ddelta;
+    const float* dstate_out;
+    float *dA, *ddelta_bias, *dstate;
+} ttc_decay_grads;
+
+int64_t ttc_decay_attention_grad_workspace(int32_t device, const ttc_decay_args* a, const ttc_decay_grads* g);
+int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_decay_grads* g, void* workspace,
+                             int64_t workspace_bytes, void* cuda_stream);
+
+/*
  * Projection of `rows` token rows:  z = x W' + bias,  y = act(z) + r.
  * x [rows][k] and W [m][k] are bfloat16 or float16 (`dtype`), row strides ldx, ldw; bias [m] float32 (NULL: none); residual r
  * [rows][m] (NULL: none) and y have the type `out_dtype`: dtype, or TTC_F32; pre (NULL: not wanted) receives z in `dtype`, which
@@ -179,7 +228,7 @@ int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_g
                     int64_t workspace_bytes, void* cuda_stream);
 
 /*
- * Every wait inside the matrix-product kernels is bounded.  *value receives 1 if one of them has given up on `device` since
+ * Every wait inside the kernels on the tensor cores is bounded.  *value receives 1 if one of them has given up on `device` since
  * the library was loaded (the results of that call are not valid), else 0.  Synchronous.
  */
 int ttc_block_device_error(int32_t device, int32_t* value);

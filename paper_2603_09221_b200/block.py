@@ -3,6 +3,7 @@
     linear, linear_grad                                            projections with bias, activation and residual
     causal_conv, causal_conv_step, causal_conv_grad                short depthwise causal convolution
     selective_scan, selective_scan_step, selective_scan_grad       state space scan with a diagonal transition
+    decay_attention, decay_attention_step, decay_attention_grad    linear attention with a decay for each head
 
 As :mod:`.lqr`, it only marshals arguments: everything runs in the CUDA kernels of ``libttc_lqr.so`` and there is no CPU
 fallback.  Calls are enqueued on ``stream`` (a ``torch.cuda.Stream``; default: the current one of the tensors' device) and
@@ -35,7 +36,8 @@ EXPORTS = (
     "ttc_linear", "ttc_linear_workspace", "ttc_linear_grad", "ttc_linear_grad_workspace",
     "ttc_causal_conv", "ttc_causal_conv_step", "ttc_causal_conv_grad", "ttc_causal_conv_grad_workspace",
     "ttc_selective_scan", "ttc_selective_scan_workspace", "ttc_selective_scan_step", "ttc_selective_scan_grad",
-    "ttc_selective_scan_grad_workspace", "ttc_block_device_error",
+    "ttc_selective_scan_grad_workspace", "ttc_decay_attention", "ttc_decay_attention_workspace", "ttc_decay_attention_step",
+    "ttc_decay_attention_grad", "ttc_decay_attention_grad_workspace", "ttc_block_device_error",
 )
 
 _F32 = torch.float32
@@ -47,6 +49,8 @@ _CONV_ARGS = struct.Struct("qqP4i" + 2 * "Pqq" + "PPPP")
 _CONV_GRADS = struct.Struct(2 * "Pqq" + "PPPP")
 _SCAN_ARGS = struct.Struct("qqP6i" + 6 * "Pqq" + "PPPPP")
 _SCAN_GRADS = struct.Struct(6 * "Pqq" + "PPPPP")
+_DECAY_ARGS = struct.Struct("qqP6ifi" + 5 * "Pqq" + "PPPP")
+_DECAY_GRADS = struct.Struct(5 * "Pqq" + "PPPP")
 _LINEAR_ARGS = struct.Struct("q6i" + "PPPPPP" + "qqqqq")
 _LINEAR_GRADS = struct.Struct("PPPP" + "qqq")
 _NO_ROWS = (0, 0, 0)
@@ -71,7 +75,7 @@ def _load():
             elif name.endswith("_workspace"):
                 f.restype = i64
                 f.argtypes = [i32, p] + grads
-            elif name in ("ttc_causal_conv", "ttc_causal_conv_step", "ttc_selective_scan_step"):
+            elif name in ("ttc_causal_conv", "ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_decay_attention_step"):
                 f.argtypes = [i32, p, p]
             else:
                 f.argtypes = [i32, p] + grads + [p, i64, p]
@@ -427,6 +431,99 @@ def selective_scan_grad(dy, x, delta, A, B, C, D=None, z=None, delta_bias=None, 
     need = lib.ttc_selective_scan_grad_workspace(index, record, grads)
     ws, at = _workspace(need, x, stream)
     _check(lib.ttc_selective_scan_grad(index, record, grads, at, need, _raw(index, stream)))
+    return got
+
+
+# ---- linear attention ---------------------------------------------------------------------------------------------------
+
+def _head_widths(q, v, offsets, lead):
+    """Groups, dk, heads, dv."""
+    if v.dim() != lead + 2 or q.dim() != lead + 2:
+        raise ValueError("q and v must be %s" % ("[batch, heads, channels]" if lead == 1 and offsets is None else
+                                                 "[rows, heads, channels]" if lead == 1 else "[batch, tokens, heads, channels] (or [rows, heads, channels] with offsets)"))
+    return q.shape[-2], q.shape[-1], v.shape[-2], v.shape[-1]
+
+
+def _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, y, state_out, step=False):
+    code, t, dev = _type_of(v, False), v.dtype, v.get_device()
+    lead = 1 if step or offsets is not None else 2
+    groups, dk, heads, dv = _head_widths(q, v, offsets, lead)
+    if step:
+        batch, tokens, off, rows = v.shape[0], 1, 0, _rows1
+    else:
+        batch, tokens, off, rows = _sequences(v[..., 0], offsets)
+    lead = tuple(v.shape[:lead])
+    if delta is None and delta_bias is not None:
+        raise ValueError("delta_bias without delta")
+    states = (batch, heads, dk, dv)
+    scale = dk ** -0.5 if scale is None and dk else scale or 0.0
+    return _DECAY_ARGS.pack(batch, tokens, off, heads, groups, dk, dv, code, 1 if softplus else 0, scale, 0,
+                            *_shared(q, "q", lead, dev, t, dk, groups, rows), *_shared(k, "k", lead, dev, t, dk, groups, rows),
+                            *_shared(v, "v", lead, dev, t, dv, heads, rows), *rows(delta, "delta", (*lead, heads), dev, t),
+                            *_shared(y, "y", lead, dev, t, dv, heads, rows), _dense(A, "A", (heads,), dev),
+                            _dense(delta_bias, "delta_bias", (heads,), dev), _dense(state, "state", states, dev),
+                            _dense(state_out, "state_out", states, dev)), states, rows, lead
+
+
+def decay_attention(q, k, v, A, delta=None, delta_bias=None, softplus=False, scale=None, state=None, offsets=None, y=None, state_out=None,
+                    stream=None):
+    """``S_t = exp(A D_t) S_{t-1} + k_t v_t'``, ``y_t = scale q_t S_t`` per head (``ttc_decay_attention``), where ``D_t = delta_t + delta_bias``, or
+    its softplus, or 1 where there is no ``delta``.
+
+    ``q, k [.., groups, dk]`` and ``v [.., heads, dv]`` bfloat16 or float16, the heads one behind the other (1 to 128 channels each; ``heads / groups``
+    neighbouring heads share queries and keys); ``delta [.., heads]`` of the same type; ``A, delta_bias [heads]`` and ``state, state_out [batch, heads, dk, dv]``
+    float32.  ``scale`` is ``dk ** -0.5`` by default.  ``state`` is S in front of the sequences (default: zero), ``state_out``
+    receives the last ones and may be ``state``.  Returns ``y``, which may be ``v``."""
+    if y is None:
+        y = _empty(v.shape, v.dtype, v, stream)
+    record = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, y, state_out)[0]
+    index = _device_of(v)
+    lib = _load()
+    need = lib.ttc_decay_attention_workspace(index, record)
+    ws, at = _workspace(need, v, stream)
+    status = lib.ttc_decay_attention(index, record, at, need, _raw(index, stream))
+    if status:
+        _check(status)
+    return y
+
+
+def decay_attention_step(q, k, v, A, state, delta=None, delta_bias=None, softplus=False, scale=None, y=None, stream=None):
+    """One token of each sequence, ``v [batch, heads, dv]``: as :func:`decay_attention`; ``state`` moves on in place."""
+    if y is None:
+        y = _empty(v.shape, v.dtype, v, stream)
+    record = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, None, None, y, state, step=True)[0]
+    index = _device_of(v)
+    status = (_lib or _load()).ttc_decay_attention_step(index, record, _raw(index, stream))
+    if status:
+        _check(status)
+    return y
+
+
+DECAY_GRAD_KEYS = ("dq", "dk", "dv", "ddelta", "dA", "ddelta_bias", "dstate")
+
+
+def decay_attention_grad(dy, q, k, v, A, delta=None, delta_bias=None, softplus=False, scale=None, state=None, offsets=None, dstate_out=None,
+                         want=None, out=None, stream=None):
+    """Gradients of :func:`decay_attention` given ``dy`` and that of ``state_out`` (``dstate_out``; default: zero).  Returns a dict with the wanted
+    of ``dq, dk, dv, ddelta, dA, ddelta_bias, dstate`` (default: all, without ``ddelta`` and ``ddelta_bias`` where there is no ``delta``); ``out`` may hold
+    tensors to write them to."""
+    record, states, rows, lead = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, None, None)
+    index, t = _device_of(v), v.dtype
+    groups, dk, heads, dv = q.shape[-2], q.shape[-1], v.shape[-2], v.shape[-1]
+    if want is None:
+        want = DECAY_GRAD_KEYS if delta is not None else ("dq", "dk", "dv", "dA", "dstate")
+    shapes = {"dq": (q.shape, t), "dk": (k.shape, t), "dv": (v.shape, t), "ddelta": ((*lead, heads), t), "dA": ((heads,), _F32),
+              "ddelta_bias": ((heads,), _F32), "dstate": (states, _F32)}
+    got = _outputs(want, out, shapes, v, stream)
+    grads = _DECAY_GRADS.pack(*_shared(dy, "dy", lead, index, t, dv, heads, rows), *_shared(got.get("dq"), "dq", lead, index, t, dk, groups, rows),
+                              *_shared(got.get("dk"), "dk", lead, index, t, dk, groups, rows), *_shared(got.get("dv"), "dv", lead, index, t, dv, heads, rows),
+                              *rows(got.get("ddelta"), "ddelta", (*lead, heads), index, t), _dense(dstate_out, "dstate_out", states, index),
+                              _dense(got.get("dA"), "dA", (heads,), index), _dense(got.get("ddelta_bias"), "ddelta_bias", (heads,), index),
+                              _dense(got.get("dstate"), "dstate", states, index))
+    lib = _load()
+    need = lib.ttc_decay_attention_grad_workspace(index, record, grads)
+    ws, at = _workspace(need, v, stream)
+    _check(lib.ttc_decay_attention_grad(index, record, grads, at, need, _raw(index, stream)))
     return got
 
 

@@ -4,6 +4,7 @@
 #include <initializer_list>
 
 #include "block_host.h"
+#include "device_error.h"
 #include "linear_rows.cuh"
 
 using namespace ttc;
@@ -520,8 +521,10 @@ int ttc_block_device_error(int32_t device, int32_t* value)
     DeviceScope scope;
     TTC_TRY(scope.enter(device));
     int v = 0;
+    int w = 0;
     TTC_CUDA(cudaMemcpyFromSymbol(&v, g_error, sizeof(v)));
-    *value = v;
+    TTC_TRY(attention_device_error(&w));
+    *value = v | w;
     return TTC_OK;
 }
 
