@@ -9,7 +9,8 @@
  *   ttc_selective_scan          state space recurrence with a diagonal, token-dependent transition: the memory layer that a
  *                               hybrid model runs beside the control layer
  *   ttc_decay_attention         linear attention with a decay for each head: the same with a matrix for a state, in chunks
- * each with its gradients (.._grad) and, for decoding, a form for single tokens (.._step; ttc_linear takes few rows itself).
+ *   ttc_block_norm              the norms behind and in front of a block, with its gate, residual scale and residual
+ * each with its gradients (.._grad) and, for decoding, a form for single tokens (.._step; ttc_linear and ttc_block_norm take few rows themselves).
  *
  * TOKEN ROWS.  A ttc_rows names a matrix of token rows: channel c of token t of sequence b is element
  * b * bstride + t * tstride + c, so that slices of wider rows (a projection that gives several operands at once) are
@@ -226,6 +227,44 @@ typedef struct ttc_linear_grads {
 int64_t ttc_linear_grad_workspace(int32_t device, const ttc_linear_args* a, const ttc_linear_grads* g);
 int ttc_linear_grad(int32_t device, const ttc_linear_args* a, const ttc_linear_grads* g, void* workspace,
                     int64_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Norms behind and in front of a block, with its gate, residual scale and residual:
+ *     u = x rms_g(x) w_post      (w_post [d]; NULL: u = x)             rms_g(v) = 1 / sqrt(mean of v^2 over the channels of a group + eps)
+ *     u = u silu(z)              (z missing: no gate)
+ *     h = residual + scale u     (scale [d], NULL: 1; residual missing: 0)
+ *     y = h rms(h) w_pre         (w_pre [d]; the mean over all channels)
+ * Rows [rows][d] of one type (1 .. 16384 channels), each with its row stride; w_post, scale, w_pre float32.  `groups` equal groups of neighbouring
+ * channels (a head's, say) for w_post.  y is given with w_pre and only then; h may be missing.  h and y may each be x, z or residual (the same pointer and stride).
+ * y is taken from h before that is rounded.
+ */
+typedef struct ttc_norm_args {
+    int64_t rows;
+    int32_t d, groups, dtype;
+    float eps;
+    const void *x, *z, *residual;
+    void *h, *y;
+    int64_t ldx, ldz, ldr, ldh, ldy;
+    const float *w_post, *scale, *w_pre;
+} ttc_norm_args;
+
+int ttc_block_norm(int32_t device, const ttc_norm_args* a, void* cuda_stream);
+
+/*
+ * Gradients of ttc_block_norm given dy (with w_pre) and dh (the gradient of h by what else reads it; NULL: zero).  `a` as in the forward call, but h is an input, as
+ * the forward call wrote it (needed with w_pre; NULL where nothing changes x: h is x then), and residual and y are not used.  dresidual receives the whole gradient of h, and may be dh;
+ * dx, dz in the rows' type, dw_post, dscale, dw_pre [d] float32.
+ */
+typedef struct ttc_norm_grads {
+    const void *dy, *dh;
+    void *dx, *dz, *dresidual;
+    int64_t lddy, lddh, lddx, lddz, lddr;
+    float *dw_post, *dscale, *dw_pre;
+} ttc_norm_grads;
+
+int64_t ttc_block_norm_grad_workspace(int32_t device, const ttc_norm_args* a, const ttc_norm_grads* g);
+int ttc_block_norm_grad(int32_t device, const ttc_norm_args* a, const ttc_norm_grads* g, void* workspace,
+                        int64_t workspace_bytes, void* cuda_stream);
 
 /*
  * Every wait inside the kernels on the tensor cores is bounded.  *value receives 1 if one of them has given up on `device` since

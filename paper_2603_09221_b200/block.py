@@ -4,6 +4,7 @@
     causal_conv, causal_conv_step, causal_conv_grad                short depthwise causal convolution
     selective_scan, selective_scan_step, selective_scan_grad       state space scan with a diagonal transition
     decay_attention, decay_attention_step, decay_attention_grad    linear attention with a decay for each head
+    block_norm, block_norm_grad                                    norms around a block with its gate, scale and residual
 
 As :mod:`.lqr`, it only marshals arguments: everything runs in the CUDA kernels of ``libttc_lqr.so`` and there is no CPU
 fallback.  Calls are enqueued on ``stream`` (a ``torch.cuda.Stream``; default: the current one of the tensors' device) and
@@ -37,7 +38,8 @@ EXPORTS = (
     "ttc_causal_conv", "ttc_causal_conv_step", "ttc_causal_conv_grad", "ttc_causal_conv_grad_workspace",
     "ttc_selective_scan", "ttc_selective_scan_workspace", "ttc_selective_scan_step", "ttc_selective_scan_grad",
     "ttc_selective_scan_grad_workspace", "ttc_decay_attention", "ttc_decay_attention_workspace", "ttc_decay_attention_step",
-    "ttc_decay_attention_grad", "ttc_decay_attention_grad_workspace", "ttc_block_device_error",
+    "ttc_decay_attention_grad", "ttc_decay_attention_grad_workspace", "ttc_block_norm", "ttc_block_norm_grad", "ttc_block_norm_grad_workspace",
+    "ttc_block_device_error",
 )
 
 _F32 = torch.float32
@@ -53,6 +55,8 @@ _DECAY_ARGS = struct.Struct("qqP6ifi" + 5 * "Pqq" + "PPPP")
 _DECAY_GRADS = struct.Struct(5 * "Pqq" + "PPPP")
 _LINEAR_ARGS = struct.Struct("q6i" + "PPPPPP" + "qqqqq")
 _LINEAR_GRADS = struct.Struct("PPPP" + "qqq")
+_NORM_ARGS = struct.Struct("q3if" + "PPPPP" + "qqqqq" + "PPP")
+_NORM_GRADS = struct.Struct("PPPPP" + "qqqqq" + "PPP")
 _NO_ROWS = (0, 0, 0)
 
 _lib = None
@@ -75,7 +79,7 @@ def _load():
             elif name.endswith("_workspace"):
                 f.restype = i64
                 f.argtypes = [i32, p] + grads
-            elif name in ("ttc_causal_conv", "ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_decay_attention_step"):
+            elif name in ("ttc_causal_conv", "ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_decay_attention_step", "ttc_block_norm"):
                 f.argtypes = [i32, p, p]
             else:
                 f.argtypes = [i32, p] + grads + [p, i64, p]
@@ -635,6 +639,87 @@ def linear_grad(dy, x, w, act="none", pre=None, want=LINEAR_GRAD_KEYS, out=None,
     need = lib.ttc_linear_grad_workspace(dev, record, grads)
     ws, at = _workspace(need, x, stream)
     _check(lib.ttc_linear_grad(dev, record, grads, at, need, _raw(dev, stream)))
+    return got
+
+
+# ---- norms --------------------------------------------------------------------------------------------------------------
+
+def _norm_operands(x, w_post, z, scale, w_pre, groups, stream):
+    code, dtype, dev = _type_of(x), x.dtype, x.get_device()
+    if x.dim() < 1:
+        raise ValueError("x must be [.., channels]")
+    d = x.shape[-1]
+    x2, px, rows, ldx = _matrix(x, "x", d, dtype, dev, None, stream)
+    if z is not None and z.shape != x.shape:
+        _explain(z, "z", x.shape, dtype, dev)
+    z2, pz, _, ldz = _matrix(z, "z", d, dtype, dev, rows, stream)
+    vectors = tuple(_dense(w, name, (d,), dev) for w, name in ((w_post, "w_post"), (scale, "scale"), (w_pre, "w_pre")))
+    return code, dtype, dev, d, rows, (x2, z2), px, pz, ldx, ldz, vectors
+
+
+def block_norm(x, w_post=None, z=None, scale=None, residual=None, w_pre=None, eps=1e-6, groups=1, h=None, y=None, stream=None):
+    """``u = x rms(x) w_post`` (in ``groups`` groups of channels), ``u = u silu(z)``, ``h = residual + scale u``, ``y = h rms(h) w_pre``
+    (``ttc_block_norm``), each part where its operand is given; ``rms(v) = 1 / sqrt(mean(v^2) + eps)``.
+
+    ``x, z, residual [.., channels]`` of one type; ``w_post, scale, w_pre [channels]`` float32.  Returns ``(h, y)``: ``h`` is ``x`` itself where
+    nothing changes it (unless a tensor for it is handed in), ``y`` is None without ``w_pre``.  ``h`` and ``y`` may each be one of the inputs."""
+    code, dtype, dev, d, rows, kept, px, pz, ldx, ldz, vectors = _norm_operands(x, w_post, z, scale, w_pre, groups, stream)
+    if residual is not None and residual.shape != x.shape:
+        _explain(residual, "residual", x.shape, dtype, dev)
+    r2, pr, _, ldr = _matrix(residual, "residual", d, dtype, dev, rows, stream)
+    changed = w_post is not None or z is not None or scale is not None or residual is not None
+    for t, name in ((h, "h"), (y, "y")):
+        if t is not None and t.shape != x.shape:
+            _explain(t, name, x.shape, dtype, dev)
+    if y is not None and w_pre is None:
+        raise ValueError("y without w_pre")
+    if dev < 0:
+        _device_of(x)
+    if not changed and w_pre is None and h is None:
+        return x, None
+    if h is None and changed:
+        h = _empty(x.shape, dtype, x, stream)
+    if y is None and w_pre is not None:
+        y = _empty(x.shape, dtype, x, stream)
+    _, ph, _, ldh = _matrix(h, "h", d, dtype, dev, rows, None, True)
+    _, py, _, ldy = _matrix(y, "y", d, dtype, dev, rows, None, True)
+    record = _NORM_ARGS.pack(rows, d, groups, code, eps, px, pz, pr, ph, py, ldx, ldz, ldr, ldh, ldy, *vectors)
+    status = (_lib or _load()).ttc_block_norm(dev, record, _raw(dev, stream))
+    if status:
+        _check(status)
+    return (x if h is None else h), y
+
+
+def block_norm_grad(x, h=None, dy=None, dh=None, w_post=None, z=None, scale=None, w_pre=None, eps=1e-6, groups=1, residual=False, want=None, out=None,
+                    stream=None):
+    """Gradients of :func:`block_norm` given ``dy`` (with ``w_pre``) and ``dh``, the gradient of ``h`` by what else reads it (default: zero).  ``h`` as the
+    forward call returned it (needed with ``w_pre``, unless ``h`` is ``x``); ``residual``: whether there was one.  Returns a dict with the wanted of ``dx, dz, dresidual,
+    dw_post, dscale, dw_pre`` (default: all whose operand is there); ``out`` may hold tensors to write them to, ``dresidual`` may be ``dh``."""
+    code, dtype, dev, d, rows, kept, px, pz, ldx, ldz, vectors = _norm_operands(x, w_post, z, scale, w_pre, groups, stream)
+    more = []
+    for t, name in ((h, "h"), (dy, "dy"), (dh, "dh")):
+        if t is not None and t.shape != x.shape:
+            _explain(t, name, x.shape, dtype, dev)
+        more.append(_matrix(t, name, d, dtype, dev, rows, stream))
+    _device_of(x)
+    if want is None:
+        want = [k for k, have in (("dx", True), ("dz", z is not None), ("dresidual", residual), ("dw_post", w_post is not None), ("dscale", scale is not None),
+                                  ("dw_pre", w_pre is not None)) if have]
+    shapes = {"dx": (x.shape, dtype), "dz": (x.shape, dtype), "dresidual": (x.shape, dtype), "dw_post": ((d,), _F32), "dscale": ((d,), _F32), "dw_pre": ((d,), _F32)}
+    got = _outputs(want, out, shapes, x, stream)
+    to = []
+    for k in ("dx", "dz", "dresidual"):
+        t = got.get(k)
+        if t is not None and t.shape != x.shape:
+            _explain(t, k, x.shape, dtype, dev)
+        to.append(_matrix(t, k, d, dtype, dev, rows, None, True))
+    (_, ph, _, ldh), (_, pdy, _, lddy), (_, pdh, _, lddh) = more
+    record = _NORM_ARGS.pack(rows, d, groups, code, eps, px, pz, 0, ph, 0, ldx, ldz, 0, ldh, 0, *vectors)
+    grads = _NORM_GRADS.pack(pdy, pdh, *(v[1] for v in to), lddy, lddh, *(v[3] for v in to), *(_dense(got.get(k), k, (d,), dev) for k in ("dw_post", "dscale", "dw_pre")))
+    lib = _load()
+    need = lib.ttc_block_norm_grad_workspace(dev, record, grads)
+    ws, at = _workspace(need, x, stream)
+    _check(lib.ttc_block_norm_grad(dev, record, grads, at, need, _raw(dev, stream)))
     return got
 
 
