@@ -4,6 +4,7 @@
 #include "block_host.h"
 #include "decay_attention_grad.cuh"
 #include "device_error.h"
+#include "tensor_map.h"
 
 using namespace ttc;
 using namespace ttc::blk;
@@ -104,40 +105,94 @@ AttnDev to_dev(const ttc_decay_args* a, bool step)
     return p;
 }
 
-// Scratch that the states of the chunks take, for `p` to keep.
-int take_states(const ttc_decay_args* a, AttnDev& p, Scratch& s)
+struct Plan {
+    AttnDev p;
+    States q;
+    int splits;
+    size_t bytes;
+};
+
+int map_pieces(const AttnDev& p, int64_t piece, int at_least, int64_t bound, cudaStream_t st)
 {
-    if (p.chunks > INT32_MAX)
-        return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks", (long long)p.chunks);
-    const size_t each = (size_t)p.chunks * a->heads, elements = (size_t)padded(a->dk) * padded(a->dv);
-    if (a->seq_offsets) {
-        p.piece_map = s.take<int2>(p.chunks);
-        p.seq_first = s.take<int>(a->batch + 1);
+    if (!p.piece_map)
+        return TTC_OK;
+    return launch_early("decay attention, pieces", piece_map_kernel, dim3(1), 1024, 0, 1, st, p.seqs, (long long)piece, at_least, (long long)bound,
+                        const_cast<int2*>(p.piece_map), const_cast<int*>(p.seq_first));
+}
+
+// Rows of heads as [batch][tokens][heads][width], in boxes of 64 channels (128 bytes, swizzled) of 128 tokens.
+int describe(CUtensorMap& map, const Rows& r, int heads, int width, const Seqs& s, bool is_bf16)
+{
+    EncodeTiled f;
+    TTC_TRY(encoder(f));
+    const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)heads, (cuuint64_t)s.tokens, (cuuint64_t)(s.offsets ? 1 : s.batch)};
+    // (the copy engine takes no stride of nothing, which is what a dimension of one may have)
+    const cuuint64_t head = width * 2, token = r.ts ? r.ts * 2 : head, seq = !s.offsets && r.bs ? r.bs * 2 : token;
+    const cuuint64_t strides[3] = {head, token, seq};
+    const cuuint32_t box[4] = {64, 1, kChunk, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult e = f(&map, is_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, r.ptr, dims, strides, box, steps,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return e == CUDA_SUCCESS ? TTC_OK : fail(TTC_STATUS_CUDA_ERROR, "cuTensorMapEncodeTiled: error %d", (int)e);
+}
+bool can_describe(const Rows& r, bool by_16_bytes, const Seqs& s)
+{
+    const long long most = 1ll << 38;            // of strides in elements
+    return by_16_bytes && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most;
+}
+
+// (q may be missing)
+int describe_all(const AttnDev& p, const Rows* q, bool vec_q, const Rows& k, bool vec_k, const Rows& v, bool vec_v, bool is_bf16, Maps& m)
+{
+    m.there = (!q || can_describe(*q, vec_q, p.seqs)) && can_describe(k, vec_k, p.seqs) && can_describe(v, vec_v, p.seqs) && p.seqs.tokens && p.seqs.batch;
+    if (!m.there)
+        return TTC_OK;
+    if (q)
+        TTC_TRY(describe(m.q, *q, p.heads / p.share, p.dk, p.seqs, is_bf16));
+    TTC_TRY(describe(m.k, k, p.heads / p.share, p.dk, p.seqs, is_bf16));
+    return describe(m.v, v, p.heads, p.dv, p.seqs, is_bf16);
+}
+
+// One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each piece of a sequence, behind a walk for what the pieces add to the state.
+int take_pieces(int device, const ttc_decay_args* a, int splits, int columns, AttnDev& p, States& q, int ways, Scratch& s)
+{
+    const int64_t sms = sm_count(device), walks = (int64_t)a->heads * splits * ways, rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
+    int64_t want = a->batch;                                         // pieces in all
+    if (walks * a->batch && sms / (walks * a->batch) >= (a->seq_offsets ? 1 : 3))
+        want = sms / walks;
+    p.piece = a->tokens ? a->tokens : 1;
+    p.pieces_per_seq = 1;
+    p.pieces = a->batch;
+    if (a->batch && rows) {
+        const int64_t each = want / a->batch;                        // of equal sequences, as many to each
+        int64_t piece = a->seq_offsets ? (rows + want - 1) / want : (a->tokens + each - 1) / each;
+        piece = (piece + kChunk - 1) / kChunk * kChunk;
+        if (want > a->batch && piece < a->tokens) {
+            p.piece = piece;
+            p.pieces_per_seq = (a->tokens + piece - 1) / piece;
+            p.pieces = a->seq_offsets ? a->tokens / piece + a->batch : a->batch * p.pieces_per_seq;
+        }
     }
-    p.added = s.take<float>(each * elements);
-    p.whole = s.take<float>(each);
-    if (a->dtype == TTC_F16) {
-        p.most = s.take<float>(each);
-        p.most_given = s.take<float>((size_t)a->batch * a->heads);
+    if (p.pieces > INT32_MAX)
+        return fail(TTC_STATUS_UNSUPPORTED, "%lld pieces of sequences", (long long)p.pieces);
+    if (p.piece < a->tokens) {
+        for (int i = 0; i < ways; ++i) {
+            q.way[i].piece_state = s.take<float>((size_t)p.pieces * a->heads * splits * kWalkThreads * (columns / 4));
+            q.way[i].piece_decay = s.take<float>((size_t)p.pieces * a->heads);
+        }
+        p.piece_state = q.way[0].piece_state;
     }
     return TTC_OK;
 }
 
-struct Plan {
-    AttnDev p;
-    size_t bytes;
-};
-
-int plan_forward(const ttc_decay_args* a, void* ws, Plan& o)
+int plan_forward(int device, const ttc_decay_args* a, void* ws, Plan& o)
 {
     TTC_TRY(check(a, false));
-    o.p = to_dev(a, false);
+    AttnDev& p = o.p;
+    p = to_dev(a, false);
+    o.splits = (a->dv + kCols - 1) / kCols;
     Scratch s(ws);
-    TTC_TRY(take_states(a, o.p, s));
-    const size_t each = (size_t)o.p.chunks * a->heads;
-    o.p.image = s.take<char>(each * padded(a->dk) * padded(a->dv) * 2);
-    if (a->dtype == TTC_F16)
-        o.p.unit = s.take<float>(each);
+    o.q = States{};
+    TTC_TRY(take_pieces(device, a, o.splits, kCols, p, o.q, 1, s));
     o.bytes = s.used;
     return TTC_OK;
 }
@@ -148,37 +203,38 @@ template <typename K> int allow_smem(K* kernel, int bytes)
     return TTC_OK;
 }
 
-int map_chunks(const AttnDev& p, cudaStream_t st)
+// What the pieces add to the state, and from that the states in front of them (back: behind); `ways` walks in one launch.
+template <typename T, int DK, int COLS> int piece_states(const Maps (&maps)[2], const AttnDev& p, States q, int ways, int splits, cudaStream_t st)
 {
-    if (!p.piece_map)
-        return TTC_OK;
-    return launch_early("decay attention, chunks", piece_map_kernel, dim3(1), 1024, 0, 1, st, p.seqs, (long long)kChunk, 0, p.chunks,
-                        const_cast<int2*>(p.piece_map), const_cast<int*>(p.seq_first));
+    q.way[0].image = q.way[1].image = nullptr;
+    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)(splits * ways));
+    constexpr int smem = StateShape<T, DK, COLS>::SMEM;
+    TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
+    TTC_TRY((launch_early("decay attention, what the pieces add", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[1], p, q, splits)));
+    return launch_early("decay attention, states of the pieces", join_kernel, dim3(grid.x, grid.y, grid.z * (COLS / 16)), kWalkThreads, 0, 1, st, p, q, COLS / 4, splits);
 }
 
-// Images of the states in front of every chunk (BACK: of the gradients of those behind), and the last ones.
-template <typename T, int DK, int DV, bool BACK, bool SPLIT>
-int chunk_states(const AttnDev& p, const Rows& a, const Rows& b, int vec_a, int vec_b, float factor, char* image, const float* given, float* last, float* unit,
-                 cudaStream_t st)
+// The states in front of all chunks, and the gradients of those behind them.
+template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], const AttnDev& p, const States& q, int splits, cudaStream_t st)
 {
-    const dim3 grid((unsigned)p.chunks, (unsigned)p.heads);
-    if (p.chunks) {
-        constexpr int smem = StateShape<T, DK, DV>::SMEM;
-        TTC_TRY((allow_smem(chunk_state_kernel<T, DK, DV, BACK>, smem)));
-        TTC_TRY((launch_early("decay attention, what the chunks add", chunk_state_kernel<T, DK, DV, BACK>, grid, kThreads, smem, 1, st, p, a, b, vec_a, vec_b, factor, given)));
-    }
-    if (p.seqs.batch && (p.chunks || last))
-        TTC_TRY((launch_early("decay attention, states", state_scan_kernel<T, DK, DV, BACK, SPLIT>, dim3((unsigned)(p.seqs.batch * p.heads), DK * DV / 8 / kThreads), kThreads,
-                              0, 1, st, p, (const float*)p.added, image, given, last, (const float*)p.most, unit)));
-    return TTC_OK;
+    if (p.pieces == 0)
+        return TTC_OK;
+    if (q.way[0].piece_state)
+        TTC_TRY((piece_states<T, DK, COLS>(maps, p, q, 2, splits, st)));
+    constexpr int smem = StateShape<T, DK, COLS>::SMEM;
+    TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
+    return launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, dim3((unsigned)p.pieces, (unsigned)p.heads, 2 * splits), kWalkBlock, smem, 1, st, maps[0], maps[1], p,
+                        q, splits);
 }
 
 struct GradPlan {
     GradDev g;
+    States q;
+    int splits;
     size_t bytes;
 };
 
-int plan_grad(const ttc_decay_args* a, const ttc_decay_grads* g, void* ws, GradPlan& o)
+int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, void* ws, GradPlan& o)
 {
     TTC_TRY(check(a, false));
     if (!g)
@@ -231,7 +287,17 @@ int plan_grad(const ttc_decay_args* a, const ttc_decay_grads* g, void* ws, GradP
     p.want_q = p.want_l || g->dq.ptr;
     p.want_kv = p.want_l || g->dk.ptr || g->dv.ptr;
     Scratch s(ws);
-    TTC_TRY(take_states(a, p.f, s));
+    // float16: a power of two goes with each image of a state, so that it is one walk's
+    o.splits = a->dtype == TTC_BF16 ? padded(a->dv) / kCols : 1;
+    States& q = o.q;
+    q = States{};
+    TTC_TRY(take_pieces(device, a, o.splits, padded(a->dv) / o.splits, p.f, q, 2, s));
+    if (p.f.chunks > INT32_MAX)
+        return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks", (long long)p.f.chunks);
+    if (packed) {
+        p.f.piece_map = s.take<int2>(p.f.chunks);
+        p.f.seq_first = s.take<int>(a->batch + 1);
+    }
     const size_t each = (size_t)p.f.chunks * a->heads, image = (size_t)padded(a->dk) * padded(a->dv) * 4;
     p.image_S = s.take<char>(each * image);
     p.image_Z = s.take<char>(each * image);
@@ -239,6 +305,22 @@ int plan_grad(const ttc_decay_args* a, const ttc_decay_grads* g, void* ws, GradP
         p.unit_S = s.take<float>(each);
         p.unit_Z = s.take<float>(each);
     }
+    q.seq_first = p.f.seq_first;
+    q.way[0].k = p.f.k, q.way[0].vec_k = p.f.vec_k;
+    q.way[0].v = p.f.v, q.way[0].vec_v = p.f.vec_v;
+    q.way[0].given = a->state;
+    q.way[0].factor = 1.f;
+    q.way[0].image = p.image_S;
+    q.way[0].unit = p.unit_S;
+    q.way[1].back = 1;                           // with queries for keys and dy for values
+    q.way[1].k = p.f.q, q.way[1].vec_k = p.f.vec_q;
+    q.way[1].v = p.dy, q.way[1].vec_v = p.vec_dy;
+    q.way[1].given = p.dstate_out;
+    q.way[1].last = p.dstate;
+    q.way[1].factor = a->scale;
+    q.way[1].image = p.image_Z;
+    q.way[1].unit = p.unit_Z;
+    q.way[0].image_bytes = q.way[1].image_bytes = padded(a->dk) * padded(a->dv) * 2;
     if (p.want_l) {
         p.tokens = s.take<float>(5 * each * kChunk);
         p.across = s.take<float>(each);
@@ -270,35 +352,48 @@ int attention_device_error(int* value)
 
 extern "C" {
 
-int64_t ttc_decay_attention_workspace(int32_t, const ttc_decay_args* a)
+int64_t ttc_decay_attention_workspace(int32_t device, const ttc_decay_args* a)
 {
     Plan o;
-    TTC_TRY(plan_forward(a, nullptr, o));
+    TTC_TRY(plan_forward(device, a, nullptr, o));
     return (int64_t)o.bytes;
 }
 
 int ttc_decay_attention(int32_t device, const ttc_decay_args* a, void* workspace, int64_t workspace_bytes, void* cuda_stream)
 {
     Plan o;
-    TTC_TRY(plan_forward(a, workspace, o));
+    TTC_TRY(plan_forward(device, a, workspace, o));
     TTC_TRY(check_output(a, false));
     TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
     DeviceScope scope;
     TTC_TRY(scope.enter(device));
     const AttnDev& p = o.p;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    TTC_TRY(map_chunks(p, st));
-    return by_widths(a, [&](auto t, auto kc, auto vc) {
+    if (p.pieces == 0)
+        return TTC_OK;
+    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)o.splits);
+    Maps maps[2] = {};
+    TTC_TRY(describe_all(p, &p.q, p.vec_q, p.k, p.vec_k, p.v, p.vec_v, a->dtype == TTC_BF16, maps[0]));
+    auto go = [&](auto t, auto kc) {
         using T = decltype(t);
-        constexpr int DK = decltype(kc)::value, DV = decltype(vc)::value;
-        TTC_TRY((chunk_states<T, DK, DV, false, false>(p, p.k, p.v, p.vec_k, p.vec_v, 1.f, p.image, p.state, p.state_out, p.unit, st)));
-        if (p.chunks) {
-            constexpr int smem = OutShape<DK, DV>::SMEM;
-            TTC_TRY((allow_smem(chunk_out_kernel<T, DK, DV>, smem)));
-            TTC_TRY((launch_early("decay attention", chunk_out_kernel<T, DK, DV>, dim3((unsigned)p.chunks, (unsigned)p.heads), kThreads, smem, 1, st, p)));
+        constexpr int DK = decltype(kc)::value;
+        if (p.piece_state) {
+            States q = o.q;
+            q.way[0].k = p.k, q.way[0].vec_k = p.vec_k;
+            q.way[0].v = p.v, q.way[0].vec_v = p.vec_v;
+            q.way[0].given = p.state;
+            q.way[0].factor = 1.f;
+            TTC_TRY((piece_states<T, DK, kCols>(maps, p, q, 1, o.splits, st)));
         }
-        return (int)TTC_OK;
-    });
+        constexpr int smem = WalkShape<T, DK>::SMEM;
+        TTC_TRY((allow_smem(walk_kernel<T, DK>, smem)));
+        return launch_early("decay attention", walk_kernel<T, DK>, grid, kWalkBlock, smem, 1, st, maps[0], p);
+    };
+    constexpr std::integral_constant<int, 64> small;
+    constexpr std::integral_constant<int, 128> large;
+    if (a->dtype == TTC_BF16)
+        return a->dk > 64 ? go(bf16(), large) : go(bf16(), small);
+    return a->dk > 64 ? go(__half(), large) : go(__half(), small);
 }
 
 int ttc_decay_attention_step(int32_t device, const ttc_decay_args* a, void* cuda_stream)
@@ -326,38 +421,38 @@ int ttc_decay_attention_step(int32_t device, const ttc_decay_args* a, void* cuda
     return a->dtype == TTC_BF16 ? go(bf16()) : go(__half());
 }
 
-int64_t ttc_decay_attention_grad_workspace(int32_t, const ttc_decay_args* a, const ttc_decay_grads* g)
+int64_t ttc_decay_attention_grad_workspace(int32_t device, const ttc_decay_args* a, const ttc_decay_grads* g)
 {
     GradPlan o;
-    TTC_TRY(plan_grad(a, g, nullptr, o));
+    TTC_TRY(plan_grad(device, a, g, nullptr, o));
     return (int64_t)o.bytes;
 }
 
 int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_decay_grads* g, void* workspace, int64_t workspace_bytes, void* cuda_stream)
 {
     GradPlan o;
-    TTC_TRY(plan_grad(a, g, workspace, o));
+    TTC_TRY(plan_grad(device, a, g, workspace, o));
     TTC_TRY(check_workspace(workspace, workspace_bytes, o.bytes));
     DeviceScope scope;
     TTC_TRY(scope.enter(device));
     const GradDev& p = o.g;
     const AttnDev& f = p.f;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    TTC_TRY(map_chunks(f, st));
+    TTC_TRY(map_pieces(f, kChunk, 0, f.chunks, st));
+    Maps maps[2] = {};
+    const bool is_bf16 = a->dtype == TTC_BF16;
+    TTC_TRY(describe_all(f, nullptr, false, f.k, f.vec_k, f.v, f.vec_v, is_bf16, maps[0]));
+    TTC_TRY(describe_all(f, nullptr, false, f.q, f.vec_q, p.dy, p.vec_dy, is_bf16, maps[1]));
     return by_widths(a, [&](auto t, auto kc, auto vc) {
         using T = decltype(t);
         constexpr int DK = decltype(kc)::value, DV = decltype(vc)::value;
-        TTC_TRY((chunk_states<T, DK, DV, false, true>(f, f.k, f.v, f.vec_k, f.vec_v, 1.f, p.image_S, f.state, nullptr, p.unit_S, st)));
-        TTC_TRY((chunk_states<T, DK, DV, true, true>(f, f.q, p.dy, f.vec_q, p.vec_dy, f.scale, p.image_Z, p.dstate_out, p.dstate, p.unit_Z, st)));
-        const dim3 grid((unsigned)f.chunks, (unsigned)f.heads);
-        constexpr int smem = GradShape<DK, DV>::SMEM;
-        if (f.chunks && p.want_q) {
-            TTC_TRY((allow_smem(grad_q_kernel<T, DK, DV>, smem)));
-            TTC_TRY((launch_early("gradients of decay attention, q", grad_q_kernel<T, DK, DV>, grid, kThreads, smem, 1, st, p)));
-        }
-        if (f.chunks && p.want_kv) {
-            TTC_TRY((allow_smem(grad_kv_kernel<T, DK, DV>, smem)));
-            TTC_TRY((launch_early("gradients of decay attention, k and v", grad_kv_kernel<T, DK, DV>, grid, kThreads, smem, 1, st, p)));
+        constexpr int COLS = std::is_same<T, bf16>::value ? kCols : DV;
+        TTC_TRY((chunk_states<T, DK, COLS>(maps, f, o.q, o.splits, st)));
+        if (f.chunks && (p.want_q || p.want_kv)) {
+            constexpr int smem = GradShape<DK, DV>::SMEM;
+            TTC_TRY((allow_smem(grad_kernel<T, DK, DV>, smem)));
+            TTC_TRY((launch_early("gradients of decay attention", grad_kernel<T, DK, DV>, dim3((unsigned)f.chunks, (unsigned)f.heads, p.want_q && p.want_kv ? 2 : 1), kThreads, smem, 1,
+                                  st, p)));
         }
         if (f.chunks && (p.part_q || p.part_k))
             TTC_TRY((launch_early("gradients of decay attention, groups", grad_group_kernel<T>, dim3((unsigned)f.chunks, 16), kThreads, 0, 1, st, p)));

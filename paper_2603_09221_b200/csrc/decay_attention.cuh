@@ -22,6 +22,8 @@
 // and the states were off by 2.4e-6 in the 2-norm).
 #pragma once
 
+#include <cuda.h>
+
 #include <type_traits>
 
 #include "pieces.cuh"
@@ -39,9 +41,10 @@ constexpr float kFloor = -192.f;                 // of exponents to the base 2: 
 
 struct AttnDev {
     Seqs seqs;
-    const int2* piece_map;                       // packed sequences: sequence and first token of each chunk
+    const int2* piece_map;                       // packed sequences, gradients: sequence and first token of each chunk
     const int* seq_first;                        // and the first chunk of each sequence
     long long chunks_per_seq, chunks;            // equal sequences; chunks in all (packed: room for them)
+    long long piece, pieces_per_seq, pieces;     // tokens of a piece; the same for pieces
     int heads, share, dk, dv;                    // share: heads of a group
     int softplus;
     float scale;
@@ -50,13 +53,7 @@ struct AttnDev {
     int vec_state;                               // and the states
     const float *A, *delta_bias, *state;
     float* state_out;
-    // scratch
-    float* added;                                // U: [chunks][heads][DV / 4][DK][4]
-    float* whole;                                // exp(G_C): [chunks][heads]
-    float* most;                                 // largest |U|: [chunks][heads] (float16)
-    float* most_given;                           // and of the states that are given: [batch][heads] (float16)
-    float* unit;                                 // what the image of S_0 has to be multiplied by: [chunks][heads] (float16)
-    char* image;                                 // S_0 in 16 bits: [chunks][heads][1 or 2][DV / 8][DK][8]
+    const float* piece_state;                    // scratch: the states in front of the pieces of a sequence
 };
 
 struct Chunk {
@@ -102,20 +99,22 @@ template <typename T> __device__ __forceinline__ float raw_step(const AttnDev& p
     return to_f(row_ptr<T>(p.delta, seq, row)[head]) + (p.delta_bias ? p.delta_bias[head] : 0.f);
 }
 
-template <typename T> __device__ __forceinline__ float log_decay(const AttnDev& p, const Chunk& c, int head, int t)
+__device__ __forceinline__ float log_decay(const AttnDev& p, float A, float raw)
+{
+    const float l = A * step_of(p, raw) * kLog2e;
+    return l < kFloor ? kFloor : l;              // NaN stays
+}
+template <typename T> __device__ __forceinline__ float log_decay_at(const AttnDev& p, const Chunk& c, int head, int t)
 {
     if (t >= c.len)
         return 0.f;
-    const float d = p.delta.ptr ? step_of(p, raw_step<T>(p, c.seq, c.row0 + t, head)) : 1.f;
-    const float l = p.A[head] * d * kLog2e;
-    return l < kFloor ? kFloor : l;              // NaN stays
+    return p.delta.ptr ? log_decay(p, p.A[head], raw_step<T>(p, c.seq, c.row0 + t, head)) : p.A[head] * kLog2e < kFloor ? kFloor : p.A[head] * kLog2e;
 }
 
-// By the first four warps.
-template <typename T> __device__ __forceinline__ void find_decays(const AttnDev& p, const Chunk& c, int head, Decays& o)
+// By one warp for the 32 tokens of a block, from the log decay of each lane's token: the sum from the block's begin, and behind the token to its end.
+__device__ __forceinline__ float block_sums(float l, float& behind)
 {
-    const int t = threadIdx.x, lane = t % 32;
-    const float l = log_decay<T>(p, c, head, t);
+    const int lane = threadIdx.x % 32;
     float g = l, s = l;
 #pragma unroll
     for (int i = 1; i < 32; i *= 2) {
@@ -123,11 +122,15 @@ template <typename T> __device__ __forceinline__ void find_decays(const AttnDev&
         g += lane >= i ? a : 0.f;
         s += lane + i < 32 ? b : 0.f;
     }
-    const float behind = __shfl_down_sync(0xffffffffu, s, 1);
-    o.g[t] = g;
-    o.s[t] = lane < 31 ? behind : 0.f;
-    if (lane == 31)
-        o.block[t / 32] = g;
+    s = __shfl_down_sync(0xffffffffu, s, 1);
+    behind = lane < 31 ? s : 0.f;
+    return g;
+}
+__device__ __forceinline__ void block_decays(float l, int t, Decays& o)
+{
+    o.g[t] = block_sums(l, o.s[t]);
+    if (t % 32 == 31)
+        o.block[t / 32] = o.g[t];
 }
 
 // exp of the sum from the chunk's begin to token t, and from behind t to the chunk's end
@@ -171,19 +174,20 @@ template <int N> __device__ __forceinline__ void copies_done() { asm volatile("c
 // what threads have written becomes visible to the tensor cores (before the barrier that they are issued behind)
 __device__ __forceinline__ void to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Thread t sees to the vectors t, t + 256, ..: the same ones wherever a tile is gone through.
-template <typename T, int COLS> __device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chunk& c, int head, int width, bool vec)
+// `width` channels from channel col0 of the rows.  Thread t sees to the vectors t, t + THREADS, ..: the same ones wherever a tile is gone through.
+template <typename T, int COLS, int THREADS>
+__device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chunk& c, int col0, int width, bool vec, int thread)
 {
-    const T* base = row_ptr<T>(r, c.seq, c.row0) + (long long)head * width;
+    const T* base = row_ptr<T>(r, c.seq, c.row0) + col0;
     if (vec) {
-#pragma unroll
-        for (int i = 0; i < kChunk * COLS / 8; i += kThreads) {
-            const int e = i + threadIdx.x, row = e / (COLS / 8), c8 = e % (COLS / 8);
+#pragma unroll 8
+        for (int i = 0; i < kChunk * COLS / 8; i += THREADS) {
+            const int e = i + thread, row = e / (COLS / 8), c8 = e % (COLS / 8);
             const bool ok = row < c.len && c8 * 8 < width;
             copy16(to + tile_at(row, c8), ok ? base + row * r.ts + c8 * 8 : base, ok);
         }
     } else {
-        for (int e = threadIdx.x; e < kChunk * COLS / 8; e += kThreads) {
+        for (int e = thread; e < kChunk * COLS / 8; e += THREADS) {
             const int row = e / (COLS / 8), c8 = e % (COLS / 8);
             Vec<T, 8> u;
 #pragma unroll
@@ -233,6 +237,17 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n"
                  :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16])
+{
+    uint32_t r[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                   "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        v[i] = __uint_as_float(r[i]);
+}
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -270,6 +285,30 @@ template <> __device__ __forceinline__ float2 unpack16<bf16>(uint32_t v) { retur
 template <> __device__ __forceinline__ float2 unpack16<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 template <typename T> constexpr bool kIsBf16 = std::is_same<T, bf16>::value;
+
+// A pair of numbers times w as a sum of TERMS pairs of 16 bits, each what those before it left.  bfloat16 cuts off instead of rounding: three times 8 bits are
+// all of the product's 24, and take no conversions.
+template <typename T, int TERMS, typename F> __device__ __forceinline__ void split_terms(uint32_t pair, float w, F&& put)
+{
+    const float2 in = unpack16<T>(pair);
+    f2 x = mul2(pack2(in.x, in.y), pack2(w, w));
+#pragma unroll
+    for (int n = 0; n < TERMS; ++n) {
+        float a, b;
+        unpack2(x, a, b);
+        float2 f;
+        if (kIsBf16<T>) {
+            put(n, __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632));
+            f = make_float2(__uint_as_float(__float_as_uint(a) & 0xffff0000u), __uint_as_float(__float_as_uint(b) & 0xffff0000u));
+        } else {
+            const uint32_t u = pack16<T>(a, b);
+            put(n, u);
+            f = unpack16<T>(u);
+        }
+        if (n + 1 < TERMS)
+            x = fma2(pack2(f.x, f.y), pack2(-1.f, -1.f), x);
+    }
+}
 
 // Barriers and tensor memory of a block.
 struct Control {
@@ -313,407 +352,1028 @@ __device__ __forceinline__ void products_done(Control& c, int i, uint32_t parity
 extern __shared__ char dattn_smem[];
 __device__ __forceinline__ char* aligned_smem() { return reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(dattn_smem) + 1023) / 1024 * 1024); }
 
-// ---- what a chunk adds to the state ---------------------------------------------------------------------------------------
+// Decay of the pairs of a row and 32 earlier tokens (a block), in a row's lane: on the diagonal from the sums `g` of the block's tokens and the row's own, else e_row, the
+// row's decay from the earlier block's end, times each token's decay to that end.
+__device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const float* to_end)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 t = *reinterpret_cast<const float4*>(to_end + j);
+        unpack2(mul2(pack2(v[j], v[j + 1]), mul2(pack2(e_row, e_row), pack2(t.x, t.y))), v[j], v[j + 1]);
+        unpack2(mul2(pack2(v[j + 2], v[j + 3]), mul2(pack2(e_row, e_row), pack2(t.z, t.w))), v[j + 2], v[j + 3]);
+    }
+}
+// (later tokens' results are of no use: they may be infinite)
+__device__ __forceinline__ void decay_own(float (&v)[32], const float* g, float own)
+{
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 h = *reinterpret_cast<const float4*>(g + j);
+        float a, b, c, d;
+        unpack2(add2(pack2(own, own), pack2(-h.x, -h.y)), a, b);
+        unpack2(add2(pack2(own, own), pack2(-h.z, -h.w)), c, d);
+        unpack2(mul2(pack2(v[j], v[j + 1]), pack2(ex2(a), ex2(b))), v[j], v[j + 1]);
+        unpack2(mul2(pack2(v[j + 2], v[j + 3]), pack2(ex2(c), ex2(d))), v[j + 2], v[j + 3]);
+    }
+}
+// Pairs in 16 bits without the tokens behind the lane's.
+__device__ __forceinline__ void cut_later(uint32_t (&packed)[16], int lane)
+{
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        packed[j] = lane > 2 * j ? packed[j] : lane == 2 * j ? packed[j] & 0xffffu : 0u;
+}
+__device__ __forceinline__ void decay_row(float (&v)[32], const float* g, bool diagonal, int lane, float own, float e_row, const float* to_end)
+{
+    if (diagonal) {
+        decay_own(v, g, own);
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            v[j] = j <= lane ? v[j] : 0.f;
+    } else {
+        decay_earlier(v, e_row, to_end);
+    }
+}
 
-template <typename T, int DK, int DV> struct StateShape {
-    static constexpr int TERMS = kIsBf16<T> ? 3 : 2;                 // numbers of 16 bits that a weighted key is split into
-    static constexpr int A_BYTES = DK / 64 * kBox, B_BYTES = DV / 64 * kBox;
-    static constexpr int HALF_BYTES = A_BYTES / 2;                   // of 64 tokens
-    static constexpr int SMEM = 1024 + A_BYTES + (TERMS - 1) * HALF_BYTES + B_BYTES;
+// ---- a walk along the chunks ----------------------------------------------------------------------------------------------
+
+constexpr int kWalkThreads = 512;
+constexpr int kCols = 64;                        // value channels of a walk: heads of more are walked along twice
+
+// A piece of a sequence (all of it, where there are enough sequences and heads), and the state in registers: of kWalkThreads threads, each has 16 neighbouring columns of
+// a row of dk.
+struct Piece {
+    long long seq, row0, owner;                  // as a Chunk's; owner: the sequence
+    long long t0, len;                           // its first token in the sequence, and its tokens
+    bool first, last;                            // of its sequence
 };
 
-// the largest of a block's values, for every thread
-__device__ __forceinline__ float largest(float v, float (&parts)[8])
+// Piece i, found by a whole warp: of packed sequences, which have one piece at least, by going along their lengths 32 at a time.  (`first_of_sequence`: number of its sequence's
+// first piece.)  Offsets that decrease leave lengths of nothing.
+__device__ __forceinline__ Piece piece_at(const AttnDev& p, long long i, long long* first_of_sequence = nullptr)
+{
+    Piece r = {0, 0, -1, 0, 0, false, false};
+    if (p.seqs.offsets) {
+        const int lane = threadIdx.x % 32;
+        long long base = 0;
+        for (long long b0 = 0; b0 < p.seqs.batch; b0 += 32) {
+            const long long b = b0 + lane;
+            const Span s = b < p.seqs.batch ? span_of(p.seqs, b) : Span{0, 0};
+            const int own = b < p.seqs.batch ? (int)max((s.len + p.piece - 1) / p.piece, 1ll) : 0;
+            int sum = own;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int v = __shfl_up_sync(0xffffffffu, sum, o);
+                sum += lane >= o ? v : 0;
+            }
+            const unsigned here = __ballot_sync(0xffffffffu, i < base + sum);
+            if (here) {
+                const int at = __ffs(here) - 1;
+                const long long row0 = __shfl_sync(0xffffffffu, s.row0, at), len = __shfl_sync(0xffffffffu, s.len, at);
+                const long long first = base + __shfl_sync(0xffffffffu, sum - own, at), t0 = (i - first) * p.piece;
+                if (first_of_sequence)
+                    *first_of_sequence = first;
+                r.owner = b0 + at;
+                r.row0 = row0 + t0;
+                r.t0 = t0;
+                r.len = min(len - t0, p.piece);
+                r.first = t0 == 0;
+                r.last = t0 + p.piece >= len;
+                return r;
+            }
+            base += __shfl_sync(0xffffffffu, sum, 31);
+        }
+    } else {
+        r.seq = r.owner = i / p.pieces_per_seq;
+        r.row0 = r.t0 = i % p.pieces_per_seq * p.piece;
+        r.len = min(p.seqs.tokens - r.row0, p.piece);
+        r.first = r.row0 == 0;
+        r.last = r.row0 + p.piece >= p.seqs.tokens;
+    }
+    return r;
+}
+__device__ __forceinline__ Chunk chunk_of(const Piece& q, int i)
+{
+    return Chunk{q.seq, q.row0 + (long long)i * kChunk, -1, (int)min(q.len - (long long)i * kChunk, (long long)kChunk)};
+}
+
+// The columns of a row of a float32 state that a thread has, from or to [batch][heads][dk][dv].
+template <int N> __device__ __forceinline__ void load_state(float (&S)[N], const AttnDev& p, const float* from, long long owner, int head, int row, int c0)
+{
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        S[j] = 0.f;
+    if (!from || row >= p.dk)
+        return;
+    from += ((owner * p.heads + head) * p.dk + row) * (long long)p.dv;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        if (p.vec_state && c0 + j < p.dv) {
+            *reinterpret_cast<float4*>(S + j) = *reinterpret_cast<const float4*>(from + c0 + j);
+        } else {
+#pragma unroll
+            for (int i = j; i < j + 4; ++i)
+                if (c0 + i < p.dv)
+                    S[i] = from[c0 + i];
+        }
+    }
+}
+template <int N> __device__ __forceinline__ void store_state(const float (&S)[N], const AttnDev& p, float* to, long long owner, int head, int row, int c0)
+{
+    if (!to || row >= p.dk)
+        return;
+    to += ((owner * p.heads + head) * p.dk + row) * (long long)p.dv;
+#pragma unroll
+    for (int j = 0; j < N; j += 4) {
+        if (p.vec_state && c0 + j < p.dv) {
+            *reinterpret_cast<float4*>(to + c0 + j) = *reinterpret_cast<const float4*>(S + j);
+        } else {
+#pragma unroll
+            for (int i = j; i < j + 4; ++i)
+                if (c0 + i < p.dv)
+                    to[c0 + i] = S[i];
+        }
+    }
+}
+
+constexpr int kFrontWarps = 2;                   // that load, and find the decays of two blocks of 32 tokens each (with a third, threads would have 80 registers)
+constexpr int kWalkBlock = kWalkThreads + 32 * (kFrontWarps + 1);
+constexpr int kWalkWarps = kWalkThreads / 32;
+
+// What a walk needs of a chunk's decays: exponentials within blocks of 32 tokens and over whole blocks, to be multiplied.
+struct alignas(16) Table {
+    float g[kChunk];                             // sums to the base 2 from the begin of the token's block, the token's own included
+    float to_end[kChunk];                        // exp from behind the token to its block's end
+    float block[4];                              // sums over the blocks
+    float before[4], behind[4];                  // exp over all blocks before and behind one
+    float skipped[4];                            // over blocks 1, 1 and 2, 2: between two that are not neighbours (index a + b - 2)
+    float whole;
+};
+__device__ __forceinline__ float between(const Table& t, int a, int b) { return b - a < 2 ? 1.f : t.skipped[a + b - 2]; }
+
+template <typename T, int DK> struct WalkShape {
+    static constexpr int TERMS = kIsBf16<T> ? 3 : 2;                 // numbers of 16 bits that a weighted value is split into
+    static constexpr int K_BYTES = DK / 64 * kBox, V_BYTES = kBox, STAGE = 2 * K_BYTES + V_BYTES;
+    static constexpr int IMAGE = DK * kCols * 2;
+    struct Small {
+        uint64_t loaded[2], freed[2];            // of the two stages
+        uint64_t scores, state, added, out;      // products that are done
+        uint64_t weighted, weighed, imaged;      // operands that are there: weighted values, weighted scores (and q S_0 times its decays), the image of the state
+        uint64_t drained;
+        uint32_t tmem;
+        int dead;
+        Table dec[2];
+        float most[kIsBf16<T> ? 1 : 32];
+    };
+    static constexpr int TILES = 2 * STAGE + TERMS * V_BYTES + IMAGE;
+    static constexpr int SMEM = TILES + sizeof(Small);
+    static constexpr int COLUMNS = 512;                              // of tensor memory
+};
+static_assert(WalkShape<bf16, 128>::SMEM <= 232448 && WalkShape<__half, 128>::SMEM <= 232448, "shared memory of a block");
+
+extern __shared__ __align__(1024) char dattn_tiles[];
+
+// a power of two that takes `most` to 2^13 .. 2^14, and its inverse
+__device__ __forceinline__ float power_for(float most, float& inverse)
+{
+    const int x = (int)((__float_as_uint(most) >> 23) & 255) - 127, k = min(max(13 - x, -100), 100);
+    inverse = __uint_as_float((uint32_t)(127 - k) << 23);
+    return __uint_as_float((uint32_t)(127 + k) << 23);
+}
+// the largest of the walking threads' values; `parts` may be written again behind the threads' next barrier
+__device__ __forceinline__ float walk_largest(float v, float* parts)
 {
 #pragma unroll
     for (int o = 16; o; o /= 2)
         v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-    __syncthreads();
     if (threadIdx.x % 32 == 0)
         parts[threadIdx.x / 32] = v;
-    __syncthreads();
-    for (int i = 0; i < 8; ++i)
+    asm volatile("bar.sync 1, %0;" :: "n"(kWalkThreads) : "memory");
+    for (int i = 0; i < kWalkWarps; ++i)
         v = fmaxf(v, parts[i]);
     return v;
 }
 
-// U = sum_t w_t a_t b_t' of one chunk and head, w_t in [0, 1]: keys and values with w = exp(R_t), or, BACK, queries and gradients of y with
-// w = exp(G_t) (there a step of the first token is taken out, so that the largest weight is 1, and put back into the sums).
-// One block: rows of 16 bytes are weighted and split where they lie, the further terms beside them for 64 tokens at a time, so that two blocks fit
-// into an SM.
-template <typename T, int DK, int DV, bool BACK>
-__global__ void __launch_bounds__(kThreads, 2) chunk_state_kernel(const AttnDev p, const Rows a, const Rows b, int vec_a, int vec_b, float factor, const float* given)
+// Rows as [batch][tokens][heads][channels] for the copy engines.
+struct Maps {
+    CUtensorMap q, k, v;
+    int there;                                   // whether the rows can be described so
+};
+__device__ __forceinline__ void fetch_box(uint32_t to, const CUtensorMap* map, int col, int head, int row, int seq, uint32_t bar)
 {
-    using S = StateShape<T, DK, DV>;
-    __shared__ Control ctl;
-    __shared__ Decays dec;
-    __shared__ float s_most[8];
-    const long long ci = blockIdx.x;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+                 :: "r"(to), "l"(map), "r"(col), "r"(head), "r"(row), "r"(seq), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fetch_to_l2(const CUtensorMap* map, int col, int head, int row, int seq)
+{
+    asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" :: "l"(map), "r"(col), "r"(head), "r"(row), "r"(seq) : "memory");
+}
+
+// As umma::wait, but asleep for up to 20 us at a time: many warps wait at once here, and what they would issue meanwhile slows the others down.
+__device__ __forceinline__ void await(uint32_t bar, uint32_t parity, volatile int* dead)
+{
+    for (int i = 0; i < (1 << 16); ++i) {
+        uint32_t ok;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                     : "=r"(ok) : "r"(bar), "r"(parity), "r"(20000u) : "memory");
+        if (ok)
+            return;
+        if ((i & 15) == 15 && *dead)
+            return;
+    }
+    *dead = 1;
+    g_error = 1;
+}
+
+// A warp's part in a barrier of all walking warps, behind what its lanes have written.
+__device__ __forceinline__ void warp_arrives(uint32_t bar)
+{
+    __syncwarp();
+    if (threadIdx.x % 32 == 0)
+        arrive(bar);
+}
+
+// One piece and 64 value channels of one head, chunk by chunk.
+//
+// Every operand is read once from memory (queries and keys once for each 64 value channels), and nothing but the results is written: with the states of all chunks in memory
+// between kernels for what a chunk adds, the states and the outputs, 4 x 2048 tokens of 16 heads of 128 x 128 took 97 us for three times the bytes.  Two warps load the
+// next chunk's tiles and find its decays, one issues products, sixteen (512 threads) do the rest, each at its own pace:
+//
+//     values times exp(R_j), split        [U = k' (weighted values)]
+//     scores times decays, q S_0 times exp(G_i)      [+ scores v]
+//     S = exp(G_C) S + U, its image in 16 bits       [next q S_0]
+//     (the next chunk's values), the results
+//
+// Tensor memory: scores of two chunks in turn, results of two chunks in turn, what the chunk adds to the state, and the weighted scores as an operand.
+template <typename T, int DK>
+__global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_constant__ Maps maps, const AttnDev p)
+{
+    using S_ = WalkShape<T, DK>;
+    using Small = typename S_::Small;
+    constexpr int TERMS = S_::TERMS;
+    char* smem = dattn_tiles;
+    Small& sm = *reinterpret_cast<Small*>(smem + S_::TILES);
+    const int head = blockIdx.y, group = head / p.share, col0 = blockIdx.z * kCols;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const int cols = min(kCols, p.dv - col0);
     wait_for_previous();
-    const Chunk c = chunk_at(p, ci);
-    if (c.len <= 0)
+    const Piece piece = piece_at(p, blockIdx.x);
+    if (piece.owner < 0)
         return;
-    char* smem = aligned_smem();
-    const uint32_t first = smem_u32(smem), rest = first + S::A_BYTES, values = rest + (S::TERMS - 1) * S::HALF_BYTES;
-    load_tile<T, DK>(first, a, c, head / p.share, p.dk, vec_a);
-    copies_begun();
-    load_tile<T, DV>(values, b, c, head, p.dv, vec_b);
-    copies_begun();
-    if (warp < 4)
-        find_decays<T>(p, c, head, dec);
-    const uint32_t tmem = set_up(ctl, DV);
-    copies_done<1>();
-    const float begin = BACK ? dec.g[0] : 0.f;
-#pragma unroll
-    for (int phase = 0; phase < 2; ++phase) {
-#pragma unroll
-        for (int i = phase * kChunk * DK / 16; i < (phase + 1) * kChunk * DK / 16; i += kThreads) {
-            const int e = i + threadIdx.x, row = e / (DK / 8), c8 = e % (DK / 8);
-            float w;
-            if (BACK) {
-                float sum = dec.g[row] - begin;
-                for (int q = 0; q < row / 32; ++q)
-                    sum += dec.block[q];
-                w = row < c.len ? ex2(sum) : 0.f;
-            } else {
-                w = to_end(dec, row);
-            }
-            uint4* at = reinterpret_cast<uint4*>(smem + tile_at(row, c8));
-            uint4 term[S::TERMS];
-            const uint4 v = *at;
-            const uint32_t* in = &v.x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float2 x = unpack16<T>(in[j]);
-                x.x *= w, x.y *= w;
-#pragma unroll
-                for (int n = 0; n < S::TERMS; ++n) {
-                    const uint32_t u = pack16<T>(x.x, x.y);
-                    (&term[n].x)[j] = u;
-                    const float2 f = unpack16<T>(u);
-                    x.x -= f.x, x.y -= f.y;
-                }
-            }
-            *at = term[0];
-            const int low = (c8 / 8) * (kBox / 2) + row % 64 * 128 + (((c8 % 8) ^ (row & 7)) << 4);
-#pragma unroll
-            for (int n = 1; n < S::TERMS; ++n)
-                *reinterpret_cast<uint4*>(smem + S::A_BYTES + (n - 1) * S::HALF_BYTES + low) = term[n];
+    const int n = __shfl_sync(0xffffffffu, (int)((piece.len + kChunk - 1) / kChunk), 0);
+    if (threadIdx.x == 0) {
+        auto init = [](uint64_t& bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(&bar)), "r"(count) : "memory"); };
+        for (int i = 0; i < 2; ++i) {
+            init(sm.loaded[i], 32 * kFrontWarps);
+            init(sm.freed[i], kWalkWarps);
         }
-        if (phase == 0)
-            copies_done<0>();
-        to_tensor_cores();
-        __syncthreads();
-        if (warp == 0) {
-            constexpr uint32_t id = instruction(kIsBf16<T>, true, true, 128, DV);
+        init(sm.scores, 1), init(sm.state, 1), init(sm.added, 1), init(sm.out, 1), init(sm.drained, 1);
+        init(sm.weighted, kWalkWarps), init(sm.weighed, kWalkWarps), init(sm.imaged, kWalkWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        sm.dead = 0;
+    }
+    if (warp == kWalkWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sm.tmem)), "r"(S_::COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    before_barrier();
+    __syncthreads();
+    behind_barrier();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
+    const uint32_t tiles = __shfl_sync(0xffffffffu, smem_u32(smem), 0), weighted = tiles + 2 * S_::STAGE, image = weighted + TERMS * S_::V_BYTES;
+    // tensor memory: what the chunk adds to the state (64 columns for each term), the weighted scores as an operand, results of two chunks in turn, scores
+    const uint32_t added = tmem, operand = tmem + 192, scores = tmem + 384;
+    auto keys_at = [&](int i) { return tiles + (i & 1) * S_::STAGE; };
+    auto values_at = [&](int i) { return tiles + (i & 1) * S_::STAGE + S_::K_BYTES; };
+    auto queries_at = [&](int i) { return tiles + (i & 1) * S_::STAGE + S_::K_BYTES + S_::V_BYTES; };
+    auto results_at = [&](int i) { return tmem + 256 + (i & 1) * 64; };
+    auto until = [&](uint64_t& bar, int phase) {
+        await(smem_u32(&bar), phase & 1, &sm.dead);
+        __syncwarp();
+    };
+
+    if (warp > kWalkWarps) {                     // ---- tiles and decays
+        const int thread = threadIdx.x - 32 * (kWalkWarps + 1);
+        const float A = p.A[head], bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
+        T raw[4 / kFrontWarps];
+        auto ask = [&](int i) {
+            const Chunk c = chunk_of(piece, i);
+#pragma unroll
+            for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                const int t = b * 32 * kFrontWarps + thread;
+                raw[b] = load_if(row_ptr<T>(p.delta, c.seq, c.row0 + t) + head, p.delta.ptr && t < c.len);
+            }
+        };
+        if (n > 0)
+            ask(0);
+        for (int i = 0; i < n; ++i) {
+            const Chunk c = chunk_of(piece, i);
+            // by the copy engine, which fills up with zeros behind the matrix; the last chunk of a packed sequence, which others' rows follow, and rows that no
+            // map describes by the threads
+            const bool engine = maps.there && (!p.seqs.offsets || c.len == kChunk);
+            const uint32_t bar = smem_u32(&sm.loaded[i & 1]);
+            bool arrived = false;
+            auto fetch = [&]() {
+                until(sm.freed[i & 1], i / 2 + 1);                   // passes at once for the first two
+                if (engine) {
+                    if (warp == kWalkWarps + 1) {
+                        arrived = elect_one();
+                        if (arrived) {
+                            expect_bytes(bar, S_::STAGE);
+                            const int row0 = (int)c.row0, seq = (int)c.seq;
+                            fetch_box(values_at(i), &maps.v, col0, head, row0, seq, bar);
+#pragma unroll
+                            for (int b = 0; b < DK / 64; ++b)
+                                fetch_box(keys_at(i) + b * kBox, &maps.k, b * 64, group, row0, seq, bar);
+#pragma unroll
+                            for (int b = 0; b < DK / 64; ++b)
+                                fetch_box(queries_at(i) + b * kBox, &maps.q, b * 64, group, row0, seq, bar);
+                            if (i + 2 < n) {                         // stages are free late: by then their next tiles have come half of the way
+                                const int next = row0 + 2 * kChunk;
+                                fetch_to_l2(&maps.v, col0, head, next, seq);
+#pragma unroll
+                                for (int b = 0; b < DK / 64; ++b) {
+                                    fetch_to_l2(&maps.k, b * 64, group, next, seq);
+                                    fetch_to_l2(&maps.q, b * 64, group, next, seq);
+                                }
+                            }
+                        }
+                        __syncwarp();
+                    }
+                } else {
+                    load_tile<T, kCols, 32 * kFrontWarps>(values_at(i), p.v, c, head * p.dv + col0, cols, p.vec_v, thread);
+                    load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), p.k, c, group * p.dk, p.dk, p.vec_k, thread);
+                    load_tile<T, DK, 32 * kFrontWarps>(queries_at(i), p.q, c, group * p.dk, p.dk, p.vec_q, thread);
+                    copies_begun();
+                }
+            };
+            if (i < 2)                           // nothing to wait for
+                fetch();
+            float sum[4 / kFrontWarps], behind[4 / kFrontWarps];
+#pragma unroll
+            for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
+                sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind[b]);
+                behind[b] = ex2(behind[b]);
+            }
+            if (i + 1 < n)
+                ask(i + 1);
+            if (i >= 2)
+                fetch();
+            Table& dec = sm.dec[i & 1];
+#pragma unroll
+            for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                const int t = b * 32 * kFrontWarps + thread;
+                dec.g[t] = sum[b];
+                dec.to_end[t] = behind[b];
+                if (lane == 31)
+                    dec.block[t / 32] = sum[b];
+            }
+            asm volatile("bar.sync 2, %0;" :: "n"(32 * kFrontWarps) : "memory");
+            if (thread < 12) {                   // before, behind, skipped, whole
+                const float b0 = dec.block[0], b1 = dec.block[1], b2 = dec.block[2], b3 = dec.block[3];
+                const int k = thread % 4;
+                float e;
+                if (thread < 4)
+                    e = k == 0 ? 0.f : k == 1 ? b0 : k == 2 ? b0 + b1 : b0 + b1 + b2;
+                else if (thread < 8)
+                    e = k == 0 ? b1 + b2 + b3 : k == 1 ? b2 + b3 : k == 2 ? b3 : 0.f;
+                else
+                    e = k == 0 ? b1 : k == 1 ? b1 + b2 : k == 2 ? b2 : (b0 + b1) + (b2 + b3);
+                (thread < 4 ? dec.before[k] : thread < 8 ? dec.behind[k] : k < 3 ? dec.skipped[k] : dec.whole) = ex2(e);
+            }
+            if (!engine) {
+                copies_done<0>();
+                to_tensor_cores();
+            }
+            if (!arrived)
+                arrive(bar);
+        }
+        if (sm.dead) {                           // copies under way end before the block does
+            for (int i = n > 2 ? n - 2 : 0; i < n; ++i)
+                drain(smem_u32(&sm.loaded[i & 1]), i / 2 & 1);
+        }
+    } else if (warp == kWalkWarps) {             // ---- products
+        auto score_products = [&](int i) {
+            behind_barrier();
+            constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128);
+            const uint64_t a = over_columns(queries_at(i), 0), b = over_columns(keys_at(i), 0);
             if (elect_one()) {
 #pragma unroll
-                for (int s = 0; s < 4; ++s) {
-                    mma(tmem, over_tokens(first, phase * 4 + s), over_tokens(values, phase * 4 + s), id, phase > 0 || s > 0);
+                for (int s = 0; s < DK / 16; ++s)
+                    mma(scores, a + (s / 4 * kBox + s % 4 * 32 >> 4), b + (s / 4 * kBox + s % 4 * 32 >> 4), id, s > 0);
+                commit(smem_u32(&sm.scores));
+            }
+            __syncwarp();
+        };
+        if (n > 0) {
+            until(sm.loaded[0], 0);
+            score_products(0);
+        }
+        for (int i = 0; i < n; ++i) {
+            until(sm.imaged, i);
+            behind_barrier();
+            constexpr uint32_t id = instruction(kIsBf16<T>, false, true, 128, kCols);
+            const uint64_t a = over_columns(queries_at(i), 0), state = image_over_dk<DK>(image, 0), values = over_tokens(values_at(i), 0);
+            const uint32_t to = results_at(i);
+            if (elect_one()) {
 #pragma unroll
-                    for (int n = 1; n < S::TERMS; ++n)
-                        mma(tmem, desc(rest + (n - 1) * S::HALF_BYTES + s * 2048, kBox / 2, 1024, 2), over_tokens(values, phase * 4 + s), id, 1);
+                for (int s = 0; s < DK / 16; ++s)
+                    mma(to, a + (s / 4 * kBox + s % 4 * 32 >> 4), state + (s * 256 >> 4), id, s > 0);
+                commit(smem_u32(&sm.state));
+            }
+            __syncwarp();
+            until(sm.weighted, i);
+            behind_barrier();
+            {
+                constexpr uint32_t id_added = instruction(kIsBf16<T>, true, true, 128, TERMS * kCols); // all terms beside one another: the keys are read once
+                const uint64_t keys = over_tokens(keys_at(i), 0), terms = over_tokens(weighted, 0);
+                if (elect_one()) {
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        mma(added, keys + (s * 2048 >> 4), terms + (s * 2048 >> 4), id_added, s > 0);
+                    commit(smem_u32(&sm.added));
                 }
-                commit(smem_u32(&ctl.bar[phase]));
+                __syncwarp();
+            }
+            until(sm.weighed, i);
+            behind_barrier();
+            if (elect_one()) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    mma_tmem(to, operand + s * 8, values + (s * 2048 >> 4), id, 1);
+                commit(smem_u32(&sm.out));
+            }
+            __syncwarp();
+            if (i + 1 < n) {
+                until(sm.loaded[(i + 1) & 1], (i + 1) / 2);
+                score_products(i + 1);
+            }
+        }
+        if (sm.dead) {                           // products under way end before tensor memory is given back
+            if (elect_one())
+                commit(smem_u32(&sm.drained));
+            __syncwarp();
+            drain(smem_u32(&sm.drained), 0);
+        }
+    } else {                                     // ---- everything else
+        const int quarter = warp % 4, sub = warp / 4, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const long long place = (((long long)blockIdx.x * p.heads + head) * gridDim.z + blockIdx.z) * (kWalkThreads * 16);
+        float S[16];
+        if (!piece.first) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                *reinterpret_cast<float4*>(S + 4 * j) = *reinterpret_cast<const float4*>(p.piece_state + place + (j * kWalkThreads + threadIdx.x) * 4);
+        } else {
+            load_state(S, p, p.state, piece.owner, head, row, col0 + sub * 16);
+        }
+        float unit = 1.f, unit_v = 1.f;
+        // the image of the state in 16 bits, [8 groups of 8 columns][DK rows]; float16: times a power of two, so that it neither overflows nor vanishes
+        auto put_image = [&]() {
+            float up = 1.f;
+            if (!kIsBf16<T>) {
+                float most = 0.f;
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    most = fmaxf(most, fabsf(S[j]));
+                up = power_for(walk_largest(quarter * 32 < DK ? most : 0.f, sm.most), unit);
+            }
+            if (quarter * 32 < DK) {
+#pragma unroll
+                for (int j = 0; j < 16; j += 8) {
+                    const uint4 w = make_uint4(pack16<T>(S[j] * up, S[j + 1] * up), pack16<T>(S[j + 2] * up, S[j + 3] * up), pack16<T>(S[j + 4] * up, S[j + 5] * up),
+                                               pack16<T>(S[j + 6] * up, S[j + 7] * up));
+                    *reinterpret_cast<uint4*>(smem + (image - tiles) + ((sub * 2 + j / 8) * DK + row) * 16) = w;
+                }
+            }
+            to_tensor_cores();
+            before_barrier();
+            warp_arrives(smem_u32(&sm.imaged));
+        };
+        // values times their decays to the chunk's end, split
+        auto put_values = [&](int i) {
+            until(sm.loaded[i & 1], i / 2);
+            uint4 v[2];
+            float up = 1.f, most = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = h * kWalkThreads + threadIdx.x;
+                v[h] = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + tile_at(e / 8, e % 8));
+                if (!kIsBf16<T>) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 x = unpack16<T>((&v[h].x)[j]);
+                        most = fmaxf(most, fmaxf(fabsf(x.x), fabsf(x.y)));
+                    }
+                }
+            }
+            if (!kIsBf16<T>)
+                up = power_for(walk_largest(most, sm.most + kWalkWarps), unit_v);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int e = h * kWalkThreads + threadIdx.x;
+                const Table& dec = sm.dec[i & 1];
+                const float w = dec.to_end[e / 8] * (dec.behind[e / 256] * up);
+                uint4 term[TERMS];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    split_terms<T, TERMS>((&v[h].x)[j], w, [&](int t, uint32_t u) { (&term[t].x)[j] = u; });
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t)
+                    *reinterpret_cast<uint4*>(smem + (weighted - tiles) + t * S_::V_BYTES + tile_at(e / 8, e % 8)) = term[t];
+            }
+            to_tensor_cores();
+            before_barrier();
+            warp_arrives(smem_u32(&sm.weighted));
+        };
+        if (n > 0) {
+            put_image();
+            put_values(0);
+        }
+        for (int i = 0; i < n; ++i) {
+            const Chunk c = chunk_of(piece, i);
+            const Table& dec = sm.dec[i & 1];
+            const float across = dec.whole;
+            const float mine = dec.g[row], own = ex2(mine), f = own * dec.before[quarter] * unit;
+            until(sm.scores, i);
+            behind_barrier();
+            uint32_t packed[16];
+            if (sub <= quarter) {
+                float v[32];
+                tmem_ld32(scores + sub * 32 + lanes, v);
+                if (sub == quarter)
+                    decay_own(v, dec.g + sub * 32, mine);
+                else
+                    decay_earlier(v, own * between(dec, sub, quarter), dec.to_end + sub * 32);
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+                if (sub == quarter)
+                    cut_later(packed, lane);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    packed[j] = 0;
+            }
+            tmem_st16(operand + sub * 16 + lanes, packed);
+            until(sm.state, i);
+            behind_barrier();
+            float v[16];
+            tmem_ld16(results_at(i) + sub * 16 + lanes, v);
+            uint32_t u[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                u[j] = __float_as_uint(v[j] * f);
+            tmem_st16(results_at(i) + sub * 16 + lanes, u);
+            tmem_st_done();
+            before_barrier();
+            warp_arrives(smem_u32(&sm.weighed));
+            until(sm.added, i);
+            behind_barrier();
+            if (quarter * 32 < DK) {
+                float u[16];
+                tmem_ld16(added + (TERMS - 1) * kCols + sub * 16 + lanes, u);
+#pragma unroll
+                for (int t = TERMS - 2; t >= 0; --t) {
+                    float v[16];
+                    tmem_ld16(added + t * kCols + sub * 16 + lanes, v);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        u[j] += v[j];
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    S[j] = fmaf(across, S[j], u[j] * unit_v);
+            }
+            if (i + 1 < n) {
+                put_image();
+                put_values(i + 1);
+            }
+            until(sm.out, i);
+            behind_barrier();
+            tmem_ld16(results_at(i) + sub * 16 + lanes, v);
+            // through the place of the values, which are done with, so that rows are written as a whole
+            char* stage = smem + (values_at(i) - tiles);
+#pragma unroll
+            for (int j = 0; j < 16; j += 8) {
+                const uint4 w = make_uint4(pack16<T>(v[j] * p.scale, v[j + 1] * p.scale), pack16<T>(v[j + 2] * p.scale, v[j + 3] * p.scale),
+                                           pack16<T>(v[j + 4] * p.scale, v[j + 5] * p.scale), pack16<T>(v[j + 6] * p.scale, v[j + 7] * p.scale));
+                *reinterpret_cast<uint4*>(stage + tile_at(row, sub * 2 + j / 8)) = w;
+            }
+            asm volatile("bar.sync %0, 128;" :: "r"(3 + quarter) : "memory");          // the four warps of these rows
+            T* to = row_ptr<T>(p.y, c.seq, c.row0 + quarter * 32) + (long long)head * p.dv + col0;
+            if (p.vec_y) {
+                uint4 w[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int e = h * 128 + sub * 32 + lane;
+                    w[h] = *reinterpret_cast<const uint4*>(stage + tile_at(quarter * 32 + e / 8, e % 8));
+                }
+                to_tensor_cores();           // (with stores to memory under way this would wait for them)
+                before_barrier();
+                warp_arrives(smem_u32(&sm.freed[i & 1]));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int e = h * 128 + sub * 32 + lane, r = e / 8, c8 = e % 8;
+                    if (quarter * 32 + r < c.len && c8 * 8 < cols)
+                        *reinterpret_cast<uint4*>(to + r * p.y.ts + c8 * 8) = w[h];
+                }
+            } else {
+                for (int e = sub * 32 + lane; e < 32 * kCols; e += 128) {
+                    const int r = e / kCols, k = e % kCols;
+                    if (quarter * 32 + r < c.len && k < cols)
+                        to[r * p.y.ts + k] = reinterpret_cast<const T*>(stage + tile_at(quarter * 32 + r, k / 8))[k % 8];
+                }
+                to_tensor_cores();
+                before_barrier();
+                warp_arrives(smem_u32(&sm.freed[i & 1]));
+            }
+        }
+        if (piece.last)
+            store_state(S, p, p.state_out, piece.owner, head, row, col0 + sub * 16);
+    }
+    before_barrier();
+    __syncthreads();
+    if (warp == kWalkWarps)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(S_::COLUMNS) : "memory");
+}
+
+// ---- states alone ---------------------------------------------------------------------------------------------------------
+
+// What a state walk does: along a sequence or, `back`, from its end (with queries for keys and the gradients of y for values: the gradients of the states), for what a piece adds,
+// from zero, or for the states in front of all chunks.
+struct StateDev {
+    Rows k, v;
+    int vec_k, vec_v, back;
+    const float* given;                          // in front of the sequences (back: behind them)
+    float* last;                                 // behind them (in front)
+    float factor;                                // of what is added
+    float *piece_state, *piece_decay;            // of the pieces of a sequence, as the threads of a walk have them: what each adds, then the state in front of it; [pieces][heads]
+    // the states in front of the chunks in 16 bits, [chunks][heads][2][DV / 8][DK][8], as two numbers (2^-17 of the value, float16 2^-22); float16: what they have to be multiplied by
+    char* image;
+    float* unit;
+    int image_bytes;
+};
+// Walks of one launch: one along the sequences, or one each way.
+struct States {
+    StateDev way[2];
+    const int* seq_first;                        // packed sequences: the first chunk of each
+};
+
+template <typename T, int DK, int COLS> struct StateShape {
+    static constexpr int TERMS = kIsBf16<T> ? 3 : 2;
+    static constexpr int K_BYTES = DK / 64 * kBox, V_BYTES = COLS / 64 * kBox, STAGE = K_BYTES + V_BYTES;
+    struct alignas(16) Weights {
+        float own[kChunk];                       // of each token, within its block of 32
+        float block[4], of_block[4];             // sums over the blocks; weights of whole blocks
+        float whole;
+    };
+    struct Small {
+        uint64_t loaded[2], freed[2], weighted, added, drained;
+        uint32_t tmem;
+        int dead;
+        Weights dec[2];
+        float most[32];
+    };
+    static constexpr int TILES = 2 * STAGE + TERMS * V_BYTES;
+    static constexpr int SMEM = TILES + sizeof(Small);
+    static constexpr int COLUMNS = TERMS * COLS > 256 ? 512 : 256;
+};
+static_assert(StateShape<bf16, 128, 128>::SMEM <= 232448, "shared memory of a block");
+
+// One piece of one head (COLS value channels of it), chunk by chunk: values times their weights, split into TERMS numbers of 16 bits, all terms beside one another as one operand of the
+// product with the keys; the state in registers, COLS / 4 neighbouring columns of a row of dk to a thread.  Warps have the roles of walk_kernel's.
+template <typename T, int DK, int COLS>
+__global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_constant__ Maps maps_there, const __grid_constant__ Maps maps_back, const AttnDev p, const States states,
+                                                                   int splits)
+{
+    const StateDev& q = states.way[blockIdx.z / splits];
+    const Maps& maps = blockIdx.z / splits ? maps_back : maps_there;
+    const int z = blockIdx.z % splits;
+    const bool BACK = q.back;
+    using S_ = StateShape<T, DK, COLS>;
+    using Small = typename S_::Small;
+    constexpr int TERMS = S_::TERMS, OWN = COLS / 4;
+    char* smem = dattn_tiles;
+    Small& sm = *reinterpret_cast<Small*>(smem + S_::TILES);
+    const int head = blockIdx.y, group = head / p.share, col0 = z * COLS;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
+    const int cols = min(COLS, p.dv - col0);
+    wait_for_previous();
+    const Piece piece = piece_at(p, blockIdx.x);
+    if (piece.owner < 0 || (!q.image && (BACK ? piece.first : piece.last)))
+        return;
+    const int n = __shfl_sync(0xffffffffu, (int)((piece.len + kChunk - 1) / kChunk), 0);
+    if (threadIdx.x == 0) {
+        auto init = [](uint64_t& bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(&bar)), "r"(count) : "memory"); };
+        for (int i = 0; i < 2; ++i) {
+            init(sm.loaded[i], 32 * kFrontWarps);
+            init(sm.freed[i], kWalkWarps);
+        }
+        init(sm.added, 1), init(sm.drained, 1), init(sm.weighted, kWalkWarps);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        sm.dead = 0;
+    }
+    if (warp == kWalkWarps) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(smem_u32(&sm.tmem)), "r"(S_::COLUMNS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    before_barrier();
+    __syncthreads();
+    behind_barrier();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sm.tmem, 0);
+    const uint32_t tiles = __shfl_sync(0xffffffffu, smem_u32(smem), 0), weighted = tiles + 2 * S_::STAGE;
+    auto keys_at = [&](int i) { return tiles + (i & 1) * S_::STAGE; };
+    auto values_at = [&](int i) { return tiles + (i & 1) * S_::STAGE + S_::K_BYTES; };
+    auto until = [&](uint64_t& bar, int phase) {
+        await(smem_u32(&bar), phase & 1, &sm.dead);
+        __syncwarp();
+    };
+    auto chunk = [&](int i) { return BACK ? n - 1 - i : i; };
+
+    if (warp > kWalkWarps) {                     // ---- tiles and decays
+        const int thread = threadIdx.x - 32 * (kWalkWarps + 1);
+        const float A = p.A[head], bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
+        T raw[4 / kFrontWarps];
+        auto ask = [&](int i) {
+            const Chunk c = chunk_of(piece, chunk(i));
+#pragma unroll
+            for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                const int t = b * 32 * kFrontWarps + thread;
+                raw[b] = load_if(row_ptr<T>(p.delta, c.seq, c.row0 + t) + head, p.delta.ptr && t < c.len);
+            }
+        };
+        if (n > 0)
+            ask(0);
+        for (int i = 0; i < n; ++i) {
+            const Chunk c = chunk_of(piece, chunk(i));
+            const bool engine = maps.there && (!p.seqs.offsets || c.len == kChunk);
+            const uint32_t bar = smem_u32(&sm.loaded[i & 1]);
+            bool arrived = false;
+            until(sm.freed[i & 1], i / 2 + 1);
+            if (engine) {
+                if (warp == kWalkWarps + 1) {
+                    arrived = elect_one();
+                    if (arrived) {
+                        expect_bytes(bar, S_::STAGE);
+                        const int row0 = (int)c.row0, seq = (int)c.seq;
+#pragma unroll
+                        for (int b = 0; b < COLS / 64; ++b)
+                            fetch_box(values_at(i) + b * kBox, &maps.v, col0 + b * 64, head, row0, seq, bar);
+#pragma unroll
+                        for (int b = 0; b < DK / 64; ++b)
+                            fetch_box(keys_at(i) + b * kBox, &maps.k, b * 64, group, row0, seq, bar);
+                        if (i + 2 < n) {
+                            const int next = BACK ? row0 - 2 * kChunk : row0 + 2 * kChunk;
+#pragma unroll
+                            for (int b = 0; b < COLS / 64; ++b)
+                                fetch_to_l2(&maps.v, col0 + b * 64, head, next, seq);
+#pragma unroll
+                            for (int b = 0; b < DK / 64; ++b)
+                                fetch_to_l2(&maps.k, b * 64, group, next, seq);
+                        }
+                    }
+                    __syncwarp();
+                }
+            } else {
+                load_tile<T, COLS, 32 * kFrontWarps>(values_at(i), q.v, c, head * p.dv + col0, cols, q.vec_v, thread);
+                load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), q.k, c, group * p.dk, p.dk, q.vec_k, thread);
+                copies_begun();
+            }
+            typename S_::Weights& dec = sm.dec[i & 1];
+#pragma unroll
+            for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                const int t = b * 32 * kFrontWarps + thread;
+                const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
+                float behind;
+                const float sum = block_sums(t < c.len ? l : 0.f, behind);
+                dec.own[t] = ex2(BACK ? sum : behind);
+                if (lane == 31)
+                    dec.block[t / 32] = sum;
+            }
+            if (i + 1 < n)
+                ask(i + 1);
+            asm volatile("bar.sync 2, %0;" :: "n"(32 * kFrontWarps) : "memory");
+            if (thread < 5) {
+                const float b0 = dec.block[0], b1 = dec.block[1], b2 = dec.block[2], b3 = dec.block[3];
+                const int k = BACK ? thread : 3 - thread;
+                float e;
+                if (BACK)
+                    e = k == 0 ? 0.f : k == 1 ? b0 : k == 2 ? b0 + b1 : b0 + b1 + b2;
+                else
+                    e = k == 0 ? 0.f : k == 1 ? b3 : k == 2 ? b2 + b3 : b1 + b2 + b3;
+                if (thread < 4)
+                    dec.of_block[thread] = ex2(e);
+                else
+                    dec.whole = ex2((b0 + b1) + (b2 + b3));
+            }
+            if (!engine) {
+                copies_done<0>();
+                to_tensor_cores();
+            }
+            if (!arrived)
+                arrive(bar);
+        }
+        if (sm.dead) {                           // copies under way end before the block does
+            for (int i = n > 2 ? n - 2 : 0; i < n; ++i)
+                drain(smem_u32(&sm.loaded[i & 1]), i / 2 & 1);
+        }
+    } else if (warp == kWalkWarps) {             // ---- products
+        for (int i = 0; i < n; ++i) {
+            until(sm.weighted, i);
+            behind_barrier();
+            constexpr int N = TERMS * COLS < 256 ? TERMS * COLS : 256, REST = TERMS * COLS - N;
+            constexpr uint32_t id = instruction(kIsBf16<T>, true, true, 128, N);
+            const uint64_t a = over_tokens(keys_at(i), 0), b = over_tokens(weighted, 0);
+            if (elect_one()) {
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    mma(tmem, a + (s * 2048 >> 4), b + (s * 2048 >> 4), id, s > 0);
+                    if constexpr (REST > 0)
+                        mma(tmem + N, a + (s * 2048 >> 4), b + (N / 64 * kBox + s * 2048 >> 4), instruction(kIsBf16<T>, true, true, 128, REST), s > 0);
+                }
+                commit(smem_u32(&sm.added));
             }
             __syncwarp();
         }
-        products_done(ctl, phase);
-    }
-    const int quarter = warp % 4, half = warp / 4, r = quarter * 32 + lane;
-    float most = 0.f;
-    if (quarter * 32 < DK) {
-        const float f = BACK ? factor * ex2(begin) : factor;
-        float4* out = reinterpret_cast<float4*>(p.added) + (ci * p.heads + head) * (long long)(DK * DV / 4) + r;
-#pragma unroll
-        for (int c0 = 0; c0 < DV / 2; c0 += 32) {
-            float v[32];
-            tmem_ld32(tmem + half * (DV / 2) + c0 + ((uint32_t)(quarter * 32) << 16), v);
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const float4 u = make_float4(v[i] * f, v[i + 1] * f, v[i + 2] * f, v[i + 3] * f);
-                most = fmaxf(most, fmaxf(fmaxf(fabsf(u.x), fabsf(u.y)), fmaxf(fabsf(u.z), fabsf(u.w))));
-                out[(half * (DV / 2) + c0 + i) / 4 * DK] = u;
-            }
+        if (sm.dead) {                           // products under way end before tensor memory is given back
+            if (elect_one())
+                commit(smem_u32(&sm.drained));
+            __syncwarp();
+            drain(smem_u32(&sm.drained), 0);
         }
-    }
-    if (!kIsBf16<T>) {
-        most = largest(most, s_most);
-        if (threadIdx.x == 0)
-            p.most[ci * p.heads + head] = most;
-        if (given && c.owner >= 0) {
-            const long long n = (long long)p.dk * p.dv, at = c.owner * p.heads + head;
-            most = 0.f;
-            for (long long i = threadIdx.x; i < n; i += kThreads)
-                most = fmaxf(most, fabsf(given[at * n + i]));
-            most = largest(most, s_most);
-            if (threadIdx.x == 0)
-                p.most_given[at] = most;
-        }
-    }
-    if (!BACK && threadIdx.x == 0)
-        p.whole[ci * p.heads + head] = over_chunk(dec);
-    give_back(tmem, DV);
-}
-
-// ---- the states in front of the chunks ------------------------------------------------------------------------------------
-
-// S_{c+1} = exp(G_C) S_c + U_c, or, BACK, from the last chunk to the first.  A thread has 8 neighbouring columns of one row of dk; the
-// loads of four chunks are under way together.  float16 images are taken times a power of two that a bound on the states' size gives (largest
-// |S| so far, decayed, plus the largest |U|), so that they neither overflow nor vanish; `unit` undoes it.
-// SPLIT: images of two numbers of 16 bits.
-template <typename T, int DK, int DV, bool BACK, bool SPLIT>
-__global__ void __launch_bounds__(kThreads) state_scan_kernel(const AttnDev p, const float* added, char* image, const float* given, float* last,
-                                                             const float* most, float* unit)
-{
-    constexpr int IMAGE = DK * DV * 2 * (SPLIT ? 2 : 1), AHEAD = 4;
-    wait_for_previous();
-    const long long b = blockIdx.x / p.heads;
-    const int head = blockIdx.x % p.heads, e = blockIdx.y * kThreads + threadIdx.x, r = e % DK, c0 = e / DK * 8;
-    long long first, n;
-    if (p.piece_map) {
-        first = p.seq_first[b];
-        n = p.seq_first[b + 1] - first;
-    } else {
-        first = b * p.chunks_per_seq;
-        n = p.chunks_per_seq;
-    }
-    const long long place = (b * p.heads + head) * (long long)p.dk * p.dv;
-    const long long own = place + (long long)r * p.dv + c0;
-    float S[8];
+    } else {                                     // ---- everything else
+        const int quarter = warp % 4, sub = warp / 4, row = quarter * 32 + lane;
+        const bool mine = quarter * 32 < DK;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const long long place = (((long long)blockIdx.x * p.heads + head) * splits + z) * (kWalkThreads * OWN);
+        const long long first = q.image ? (p.seqs.offsets ? states.seq_first[piece.owner] : piece.owner * p.chunks_per_seq) + piece.t0 / kChunk : 0;
+        float S[OWN];
+        if (q.image && !(BACK ? piece.last : piece.first)) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-        S[j] = 0.f;
-    if (given && r < p.dk) {
-        if (p.vec_state && c0 < p.dv) {
-            *reinterpret_cast<float4*>(S) = *reinterpret_cast<const float4*>(given + own);
-            *reinterpret_cast<float4*>(S + 4) = *reinterpret_cast<const float4*>(given + own + 4);
+            for (int j = 0; j < OWN / 4; ++j)
+                *reinterpret_cast<float4*>(S + 4 * j) = *reinterpret_cast<const float4*>(q.piece_state + place + (j * kWalkThreads + threadIdx.x) * 4);
         } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c0 + j < p.dv)
-                    S[j] = given[own + j];
+            load_state(S, p, q.image ? q.given : nullptr, piece.owner, head, row, col0 + sub * OWN);
         }
-    }
-    float bound = !kIsBf16<T> && given && n > 0 ? p.most_given[b * p.heads + head] : 0.f;
-    for (long long i0 = 0; i0 < n; i0 += AHEAD) {
-        float4 u[AHEAD][2];
-        float w[AHEAD], m[AHEAD];
+        float whole = 1.f;
+        for (int i = 0; i < n; ++i) {
+            const typename S_::Weights& dec = sm.dec[i & 1];
+            until(sm.loaded[i & 1], i / 2);
+            float unit_v = 1.f;
+            {                                    // values times their weights, split
+                constexpr int VECTORS = COLS / 32;
+                float up = 1.f;
+                if (!kIsBf16<T>) {
+                    float most = 0.f;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const long long c = BACK ? first + n - 1 - (i0 + i) : first + i0 + i, at = c * p.heads + head;
-            const bool ok = i0 + i < n;
-            const float4* from = reinterpret_cast<const float4*>(added) + (ok ? at : 0) * (long long)(DK * DV / 4) + (long long)(c0 / 4) * DK + r;
-            u[i][0] = load_if(from, ok);
-            u[i][1] = load_if(from + DK, ok);
-            w[i] = load_if(p.whole + (ok ? at : 0), ok);
-            m[i] = kIsBf16<T> ? 0.f : load_if(most + (ok ? at : 0), ok);
-        }
+                    for (int h = 0; h < VECTORS; ++h) {
+                        const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
+                        const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + tile_at(t, e % (COLS / 8)));
+                        float here = 0.f;
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            if (i0 + i >= n)
-                break;
-            const long long c = BACK ? first + n - 1 - (i0 + i) : first + i0 + i, at = c * p.heads + head;
-            float up = 1.f;
-            if (!kIsBf16<T>) {                   // 2^(13 - floor(log2(bound))): results below 2^14
-                const int x = ((__float_as_uint(bound) >> 23) & 255) - 127;
-                const int k = min(max(13 - x, -100), 100);
-                up = __uint_as_float((uint32_t)(k + 127) << 23);
-                if (blockIdx.y == 0 && threadIdx.x == 0)
-                    unit[at] = __uint_as_float((uint32_t)(127 - k) << 23);
-                bound = fmaf(w[i], bound, m[i]);
-            }
-            uint4 hi, lo;
-            uint32_t *h = &hi.x, *l = &lo.x;
+                        for (int j = 0; j < 4; ++j) {
+                            const float2 x = unpack16<T>((&v.x)[j]);
+                            here = fmaxf(here, fmaxf(fabsf(x.x), fabsf(x.y)));
+                        }
+                        most = fmaxf(most, here * (dec.own[t] * dec.of_block[t / 32]));
+                    }
+                    up = power_for(walk_largest(most, sm.most), unit_v);
+                }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float x = S[2 * j] * up, y = S[2 * j + 1] * up;
-                h[j] = pack16<T>(x, y);
-                if (SPLIT) {
-                    const float2 f = unpack16<T>(h[j]);
-                    l[j] = pack16<T>(x - f.x, y - f.y);
+                for (int h = 0; h < VECTORS; ++h) {
+                    const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
+                    const uint32_t at = tile_at(t, e % (COLS / 8));
+                    const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + at);
+                    const float w = dec.own[t] * (dec.of_block[t / 32] * up);
+                    uint4 term[TERMS];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        split_terms<T, TERMS>((&v.x)[j], w, [&](int n, uint32_t u) { (&term[n].x)[j] = u; });
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n)
+                        *reinterpret_cast<uint4*>(smem + (weighted - tiles) + n * S_::V_BYTES + at) = term[n];
                 }
             }
-            char* to = image + at * IMAGE + ((c0 / 8) * DK + r) * 16;
-            *reinterpret_cast<uint4*>(to) = hi;
-            if (SPLIT)
-                *reinterpret_cast<uint4*>(to + DK * DV * 2) = lo;
-            const float* f = &u[i][0].x;
+            to_tensor_cores();
+            before_barrier();
+            warp_arrives(smem_u32(&sm.weighted));
+            const float over = dec.whole;
+            if (q.image) {                       // the state in front of the chunk, while the products run
+                const long long at = (first + chunk(i)) * p.heads + head;
+                float up = 1.f;
+                if (!kIsBf16<T>) {
+                    float most = 0.f, unit;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                S[j] = fmaf(w[i], S[j], f[j]);
+                    for (int j = 0; j < OWN; ++j)
+                        most = fmaxf(most, fabsf(S[j]));
+                    up = power_for(walk_largest(mine ? most : 0.f, sm.most + kWalkWarps), unit);
+                    if (threadIdx.x == 0)
+                        q.unit[at] = unit;
+                }
+                if (mine) {
+#pragma unroll
+                    for (int j = 0; j < OWN; j += 8) {
+                        uint4 hi, lo;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const float x = S[j + 2 * k] * up, y = S[j + 2 * k + 1] * up;
+                            const uint32_t h = pack16<T>(x, y);
+                            const float2 f = unpack16<T>(h);
+                            (&hi.x)[k] = h;
+                            (&lo.x)[k] = pack16<T>(x - f.x, y - f.y);
+                        }
+                        char* to = q.image + at * (2 * q.image_bytes) + (((col0 + sub * OWN + j) / 8 * DK + row) * 16);
+                        *reinterpret_cast<uint4*>(to) = hi;
+                        *reinterpret_cast<uint4*>(to + q.image_bytes) = lo;
+                    }
+                }
+            }
+            until(sm.added, i);
+            behind_barrier();
+            if (mine) {
+#pragma unroll
+                for (int j = 0; j < OWN; j += 16) {
+                    float u[16];
+                    tmem_ld16(tmem + (TERMS - 1) * COLS + sub * OWN + j + lanes, u);
+#pragma unroll
+                    for (int t = TERMS - 2; t >= 0; --t) {
+                        float v[16];
+                        tmem_ld16(tmem + t * COLS + sub * OWN + j + lanes, v);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            u[k] += v[k];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 16; ++k)
+                        S[j + k] = fmaf(over, S[j + k], u[k] * (unit_v * q.factor));
+                }
+            }
+            whole *= over;
+            before_barrier();
+            warp_arrives(smem_u32(&sm.freed[i & 1]));
         }
-    }
-    if (last && r < p.dk) {
-        if (p.vec_state && c0 < p.dv) {
-            *reinterpret_cast<float4*>(last + own) = *reinterpret_cast<const float4*>(S);
-            *reinterpret_cast<float4*>(last + own + 4) = *reinterpret_cast<const float4*>(S + 4);
+        if (q.image) {
+            if (BACK ? piece.first : piece.last)
+                store_state(S, p, q.last, piece.owner, head, row, col0 + sub * OWN);
         } else {
+            if (mine) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (c0 + j < p.dv)
-                    last[own + j] = S[j];
+                for (int j = 0; j < OWN / 4; ++j)
+                    *reinterpret_cast<float4*>(q.piece_state + place + (j * kWalkThreads + threadIdx.x) * 4) = *reinterpret_cast<const float4*>(S + 4 * j);
+            }
+            if (threadIdx.x == 0 && z == 0)
+                q.piece_decay[blockIdx.x * (long long)p.heads + head] = whole;
         }
     }
+    before_barrier();
+    __syncthreads();
+    if (warp == kWalkWarps)
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(S_::COLUMNS) : "memory");
 }
 
-// ---- outputs --------------------------------------------------------------------------------------------------------------
-
-// Decay of the pairs (row, 32 columns of block b) of the lower triangle times f: a row's lane has `mine` = its sum from its block's begin.
-// `to_here` [32]: exp from each column to the begin of the row's block.
-__device__ __forceinline__ void decay_row(float (&v)[32], const Decays& d, bool diagonal, int b, int lane, float mine, float e_mine, const float* to_here)
+// The states in front of the pieces (BACK: behind them), from what each adds: S = exp(..) S + U along a sequence, eight pieces' loads under way together.  A block works for the
+// sequence whose last piece its number is, and for four of the `own` columns that a thread has in a state walk.
+static __global__ void __launch_bounds__(kWalkThreads) join_kernel(const AttnDev p, const States states, int own, int splits)
 {
-    if (diagonal) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const float4 g = *reinterpret_cast<const float4*>(d.g + b * 32 + j);
-            v[j] = j <= lane ? v[j] * ex2(mine - g.x) : 0.f;
-            v[j + 1] = j + 1 <= lane ? v[j + 1] * ex2(mine - g.y) : 0.f;
-            v[j + 2] = j + 2 <= lane ? v[j + 2] * ex2(mine - g.z) : 0.f;
-            v[j + 3] = j + 3 <= lane ? v[j + 3] * ex2(mine - g.w) : 0.f;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const float4 t = *reinterpret_cast<const float4*>(to_here + j);
-            v[j] *= e_mine * t.x;
-            v[j + 1] *= e_mine * t.y;
-            v[j + 2] *= e_mine * t.z;
-            v[j + 3] *= e_mine * t.w;
-        }
-    }
-}
-
-template <int DK, int DV> struct OutShape {
-    static constexpr int Q_BYTES = DK / 64 * kBox, V_BYTES = DV / 64 * kBox, KV_BYTES = Q_BYTES > V_BYTES ? Q_BYTES : V_BYTES;
-    static constexpr int QY_BYTES = KV_BYTES;    // queries, then the staged results
-    static constexpr int IMAGE = DK * DV * 2;
-    static constexpr int SMEM = 1024 + QY_BYTES + KV_BYTES + IMAGE;
-};
-
-__device__ __forceinline__ void load_image(uint32_t to, const char* from, int bytes)
-{
-    for (int i = threadIdx.x * 16; i < bytes; i += kThreads * 16)
-        copy16(to + i, from + i, true);
-}
-
-// One chunk of one head: scores and q S_0 into tensor memory; the scores, times their decays, go back there in 16 bits as an operand, and
-// the values take the keys' place in shared memory meanwhile.  Two blocks to an SM, so that one's loads run beside the other's products.
-template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads, 2) chunk_out_kernel(const AttnDev p)
-{
-    using S = OutShape<DK, DV>;
-    __shared__ Control ctl;
-    __shared__ Decays dec;
-    __shared__ alignas(16) float s_to[4][96];                // [block][earlier token]: decay from it to the block's begin
-    const long long ci = blockIdx.x;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, half = warp / 4;
+    constexpr int AHEAD = 8;
     wait_for_previous();
-    const Chunk c = chunk_at(p, ci);
-    if (c.len <= 0)
+    const int parts = own / 4, head = blockIdx.y, z = blockIdx.z / parts % splits, part = blockIdx.z % parts;
+    const StateDev& q = states.way[blockIdx.z / parts / splits];
+    const bool back = q.back;
+    long long first = p.seqs.offsets ? 0 : blockIdx.x / p.pieces_per_seq * p.pieces_per_seq;
+    const Piece piece = piece_at(p, blockIdx.x, &first);
+    const int lane = threadIdx.x % 32, quarter = threadIdx.x / 32 % 4, sub = threadIdx.x / 128, row = quarter * 32 + lane;
+    if (piece.owner < 0 || !piece.last || piece.first || row >= p.dk)
         return;
-    char* smem = aligned_smem();
-    const uint32_t queries = smem_u32(smem), keys = queries + S::QY_BYTES, image = keys + S::KV_BYTES;
-    load_tile<T, DK>(queries, p.q, c, head / p.share, p.dk, p.vec_q);
-    load_tile<T, DK>(keys, p.k, c, head / p.share, p.dk, p.vec_k);
-    load_image(image, p.image + (ci * p.heads + head) * (long long)S::IMAGE, S::IMAGE);
-    copies_begun();
-    if (warp < 4)
-        find_decays<T>(p, c, head, dec);
-    const uint32_t tmem = set_up(ctl, 256);      // scores: columns 0 .. 127, results behind them
-    const uint32_t scores = tmem, results = tmem + 128, lanes = (uint32_t)(quarter * 32) << 16;
-    for (int i = threadIdx.x; i < 4 * 96; i += kThreads)
-        s_to[i / 96][i % 96] = i % 96 < i / 96 * 32 ? to_block(dec, i % 96, i / 96) : 0.f;
-    copies_done<0>();
-    to_tensor_cores();
-    __syncthreads();
-    if (warp == 0) {
-        constexpr uint32_t id_scores = instruction(kIsBf16<T>, false, false, 128, 128), id_state = instruction(kIsBf16<T>, false, true, 128, DV);
-        if (elect_one()) {
+    const long long n = blockIdx.x - first + 1;
+    float four[4];
+    load_state(four, p, q.given, piece.owner, head, row, z * 4 * own + sub * own + part * 4);
+    float4 S = make_float4(four[0], four[1], four[2], four[3]);
+    auto which = [&](long long i) { return back ? first + n - 1 - i : first + i; };
+    auto at = [&](long long i) {
+        return reinterpret_cast<float4*>(q.piece_state + ((which(i) * p.heads + head) * splits + z) * (long long)(kWalkThreads * own)) + part * kWalkThreads + threadIdx.x;
+    };
+    for (long long i0 = 0; i0 < n - 1; i0 += AHEAD) {
+        float4 u[AHEAD];
+        float w[AHEAD];
 #pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                mma(scores, over_columns(queries, s), over_columns(keys, s), id_scores, s > 0);
-            commit(smem_u32(&ctl.bar[0]));
-#pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                mma(results, over_columns(queries, s), image_over_dk<DK>(image, s), id_state, s > 0);
-            commit(smem_u32(&ctl.bar[1]));
+        for (int i = 0; i < AHEAD; ++i) {
+            const bool ok = i0 + i < n - 1;
+            u[i] = load_if(at(ok ? i0 + i : 0), ok);
+            w[i] = load_if(q.piece_decay + which(ok ? i0 + i : 0) * p.heads + head, ok);
         }
-        __syncwarp();
-    }
-    products_done(ctl, 0);
-    load_tile<T, DV>(keys, p.v, c, head, p.dv, p.vec_v);
-    copies_begun();
-    const int row = quarter * 32 + lane;
-    const float mine = dec.g[row], e_mine = ex2(mine);
-    uint32_t packed[2][16];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int b = half + 2 * i;
-        if (b <= quarter) {
-            float v[32];
-            tmem_ld32(scores + b * 32 + lanes, v);
-            decay_row(v, dec, b == quarter, b, lane, mine, e_mine, &s_to[quarter][b < quarter ? b * 32 : 0]);
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                packed[i][j] = pack16<T>(v[2 * j] * p.scale, v[2 * j + 1] * p.scale);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                packed[i][j] = 0;
+        for (int i = 0; i < AHEAD; ++i) {
+            if (i0 + i < n - 1) {
+                if (i0 + i > 0)
+                    *at(i0 + i) = S;
+                S.x = fmaf(w[i], S.x, u[i].x), S.y = fmaf(w[i], S.y, u[i].y), S.z = fmaf(w[i], S.z, u[i].z), S.w = fmaf(w[i], S.w, u[i].w);
+            }
         }
     }
-    // both warps of these rows have read what is overwritten now
-    before_barrier();
-    asm volatile("bar.sync %0, 64;" :: "r"(1 + quarter) : "memory");
-    behind_barrier();
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        tmem_st16(scores + (half + 2 * i) * 16 + lanes, packed[i]);
-    products_done(ctl, 1);
-    {
-        const float f = from_begin(dec, row) * p.scale * (kIsBf16<T> ? 1.f : p.unit[ci * p.heads + head]);
-#pragma unroll
-        for (int c0 = 0; c0 < DV / 2; c0 += 32) {
-            float v[32];
-            const uint32_t at = results + half * (DV / 2) + c0 + lanes;
-            tmem_ld32(at, v);
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                v[j] *= f;
-            tmem_st32(at, v);
-        }
-    }
-    tmem_st_done();
-    copies_done<0>();
-    to_tensor_cores();
-    before_barrier();
-    __syncthreads();
-    if (warp == 0) {
-        behind_barrier();
-        constexpr uint32_t id = instruction(kIsBf16<T>, false, true, 128, DV);
-        if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                mma_tmem(results, scores + s * 8, over_tokens(keys, s), id, 1);
-            commit(smem_u32(&ctl.bar[2]));
-        }
-        __syncwarp();
-    }
-    products_done(ctl, 2);
-#pragma unroll
-    for (int c0 = 0; c0 < DV / 2; c0 += 32) {
-        float v[32];
-        tmem_ld32(results + half * (DV / 2) + c0 + lanes, v);
-#pragma unroll
-        for (int j = 0; j < 32; j += 8) {
-            const uint4 w = make_uint4(pack16<T>(v[j], v[j + 1]), pack16<T>(v[j + 2], v[j + 3]), pack16<T>(v[j + 4], v[j + 5]), pack16<T>(v[j + 6], v[j + 7]));
-            *reinterpret_cast<uint4*>(smem + tile_at(row, (half * (DV / 2) + c0 + j) / 8)) = w;
-        }
-    }
-    give_back(tmem, 256);
-    store_tile<T, DV>(smem, p.y, c, head, p.dv, p.vec_y);
+    *at(n - 1) = S;
 }
 
 // ---- one token of each sequence -------------------------------------------------------------------------------------------

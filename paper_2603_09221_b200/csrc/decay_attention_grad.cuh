@@ -14,7 +14,7 @@
 // dl goes into float32 sums over all tokens (dA, ddelta_bias): M is taken from the float32 scores, and S_0 and Z go into e and f as two numbers of 16 bits
 // (2^-18 of the value).
 //
-// The states in front of the chunks come from the kernels of the forward pass, the Z from the same ones with queries and dy, backwards; then one
+// The states in front of the chunks come from a state walk, the Z from one that goes backwards along queries and dy; then one
 // kernel finds dq, e and row, one dk, dv, f and col, and a small one dl.
 #pragma once
 
@@ -22,6 +22,12 @@
 
 namespace ttc {
 namespace dattn {
+
+__device__ __forceinline__ void load_image(uint32_t to, const char* from, int bytes)
+{
+    for (int i = threadIdx.x * 16; i < bytes; i += kThreads * 16)
+        copy16(to + i, from + i, true);
+}
 
 struct GradDev {
     AttnDev f;
@@ -110,15 +116,14 @@ __device__ __forceinline__ long long packed_row(const AttnDev& p, const Chunk& c
 
 // dq of one chunk and head, lanes for the tokens i: scores and dy v' into tensor memory beside S_0 dy; M's row sums from both; dy v' with its decays goes
 // back in 16 bits and is multiplied with the keys.
-template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const GradDev g)
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(const GradDev& g)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
     __shared__ Control ctl;
     __shared__ Decays dec;
     __shared__ alignas(16) float s_to[4][96];
-    __shared__ float s_half[kChunk], s_rows[kChunk], s_within[kChunk], s_pairs[4][4];
+    __shared__ float s_half[kChunk], s_rows[kChunk], s_within[kChunk], s_pairs[4][4], s_dot[8];
     const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
     const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, half = warp / 4;
     wait_for_previous();
@@ -127,14 +132,25 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const GradDev g)
         return;
     char* smem = aligned_smem();
     const uint32_t queries = smem_u32(smem), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
-    load_tile<T, DK>(queries, p.q, c, head / p.share, p.dk, p.vec_q);
-    load_tile<T, DK>(keys, p.k, c, head / p.share, p.dk, p.vec_k);
-    load_tile<T, DV>(values, p.v, c, head, p.dv, p.vec_v);
-    load_tile<T, DV>(dys, g.dy, c, head, p.dv, g.vec_dy);
+    load_tile<T, DK, kThreads>(queries, p.q, c, head / p.share * p.dk, p.dk, p.vec_q, threadIdx.x);
+    load_tile<T, DK, kThreads>(keys, p.k, c, head / p.share * p.dk, p.dk, p.vec_k, threadIdx.x);
+    load_tile<T, DV, kThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
+    load_tile<T, DV, kThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
     load_image(image, g.image_S + at * (2 * S::IMAGE), 2 * S::IMAGE);
     copies_begun();
+    // for <Z, S_0>: the image of Z comes into registers beside the tiles' copies
+    constexpr int VECTORS = S::IMAGE / 16 / kThreads;
+    uint4 other[2][VECTORS];
+    if (g.want_l) {
+        const uint4* from = reinterpret_cast<const uint4*>(g.image_Z + at * (2 * S::IMAGE)) + threadIdx.x;
+#pragma unroll
+        for (int i = 0; i < VECTORS; ++i) {
+            other[0][i] = from[i * kThreads];
+            other[1][i] = from[S::IMAGE / 16 + i * kThreads];
+        }
+    }
     if (warp < 4)
-        find_decays<T>(p, c, head, dec);
+        block_decays(log_decay_at<T>(p, c, head, threadIdx.x), threadIdx.x, dec);
     const uint32_t tmem = set_up(ctl, 512);      // scores, dy v', results: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, results = tmem + 256, lanes = (uint32_t)(quarter * 32) << 16;
     for (int i = threadIdx.x; i < 4 * 96; i += kThreads)
@@ -162,6 +178,25 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const GradDev g)
         }
         __syncwarp();
     }
+    if (g.want_l) {                              // <Z, S_0>, while the products run
+        const uint4* have = reinterpret_cast<const uint4*>(smem + 2 * S::K_BYTES + 2 * S::V_BYTES) + threadIdx.x;
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < VECTORS; ++i) {
+            const uint4 x = have[i * kThreads], y = have[S::IMAGE / 16 + i * kThreads];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 a = unpack16<T>((&other[0][i].x)[j]), b = unpack16<T>((&other[1][i].x)[j]), c = unpack16<T>((&x.x)[j]), d = unpack16<T>((&y.x)[j]);
+                dot = fmaf(a.x + b.x, c.x + d.x, dot);
+                dot = fmaf(a.y + b.y, c.y + d.y, dot);
+            }
+        }
+#pragma unroll
+        for (int o = 16; o; o /= 2)
+            dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        if (lane == 0)
+            s_dot[warp] = dot;
+    }
     products_done(ctl, 0);
     const int row = quarter * 32 + lane;
     const float mine = dec.g[row], e_mine = ex2(mine);
@@ -173,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const GradDev g)
         if (b <= quarter) {
             float v[32];
             tmem_ld32(slopes + b * 32 + lanes, v);
-            decay_row(v, dec, b == quarter, b, lane, mine, e_mine, &s_to[quarter][b < quarter ? b * 32 : 0]);
+            decay_row(v, dec.g + b * 32, b == quarter, lane, mine, e_mine, &s_to[quarter][b < quarter ? b * 32 : 0]);
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 packed[i][j] = pack16<T>(v[2 * j], v[2 * j + 1]);
@@ -240,6 +275,12 @@ __global__ void __launch_bounds__(kThreads, 1) grad_q_kernel(const GradDev g)
         to[0] = (e + s_half[row]) * p.scale;
         to[plane] = (row_sum + s_rows[row]) * p.scale;
         to[4 * plane] = s_within[row] * p.scale;
+        if (row == 0) {
+            float dot = 0.f;
+            for (int i = 0; i < 8; ++i)
+                dot += s_dot[i];
+            g.across[at] = dot * over_chunk(dec) * (kIsBf16<T> ? 1.f : g.unit_S[at] * g.unit_Z[at]);
+        }
         if (row < 2)
             g.bridges[2 * at + row] = (s_pairs[3][0] + s_pairs[2 + row][row]) * p.scale;
     }
@@ -279,15 +320,14 @@ __device__ __forceinline__ void decay_column(float (&v)[32], const Decays& d, bo
 }
 
 // dk and dv of one chunk and head, lanes for the tokens j.
-template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const GradDev g)
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(const GradDev& g)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
     __shared__ Control ctl;
     __shared__ Decays dec;
     __shared__ alignas(16) float s_from[kChunk];
-    __shared__ float s_f[kChunk], s_col[kChunk], s_dot[8];
+    __shared__ float s_f[kChunk], s_col[kChunk];
     const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
     const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, half = warp / 4;
     wait_for_previous();
@@ -298,15 +338,14 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const GradDev g)
     const uint32_t queries = smem_u32(smem), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
     char* s_keys = smem + S::K_BYTES;
     char* s_values = s_keys + S::K_BYTES;
-    char* s_image = s_values + 2 * S::V_BYTES;
-    load_tile<T, DK>(queries, p.q, c, head / p.share, p.dk, p.vec_q);
-    load_tile<T, DK>(keys, p.k, c, head / p.share, p.dk, p.vec_k);
-    load_tile<T, DV>(values, p.v, c, head, p.dv, p.vec_v);
-    load_tile<T, DV>(dys, g.dy, c, head, p.dv, g.vec_dy);
+    load_tile<T, DK, kThreads>(queries, p.q, c, head / p.share * p.dk, p.dk, p.vec_q, threadIdx.x);
+    load_tile<T, DK, kThreads>(keys, p.k, c, head / p.share * p.dk, p.dk, p.vec_k, threadIdx.x);
+    load_tile<T, DV, kThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
+    load_tile<T, DV, kThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
     load_image(image, g.image_Z + at * (2 * S::IMAGE), 2 * S::IMAGE);
     copies_begun();
     if (warp < 4)
-        find_decays<T>(p, c, head, dec);
+        block_decays(log_decay_at<T>(p, c, head, threadIdx.x), threadIdx.x, dec);
     const uint32_t tmem = set_up(ctl, 512);      // scores, v dy', dk, dv: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, dks = tmem + 256, dvs = tmem + 384, lanes = (uint32_t)(quarter * 32) << 16;
     if (warp < 4)
@@ -337,26 +376,6 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const GradDev g)
             commit(smem_u32(&ctl.bar[1]));
         }
         __syncwarp();
-    }
-    if (g.want_l) {                              // exp(G_C) <Z, S_0>, while the products run
-        const uint4* from = reinterpret_cast<const uint4*>(g.image_S + at * (2 * S::IMAGE));
-        const uint4* have = reinterpret_cast<const uint4*>(s_image);
-        float dot = 0.f;
-        for (int i = threadIdx.x; i < S::IMAGE / 16; i += kThreads) {
-            const uint4 a = from[i], b = from[i + S::IMAGE / 16], x = have[i], y = have[i + S::IMAGE / 16];
-            const uint32_t *pa = &a.x, *pb = &b.x, *px = &x.x, *py = &y.x;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 fa = unpack16<T>(pa[j]), fb = unpack16<T>(pb[j]), fx = unpack16<T>(px[j]), fy = unpack16<T>(py[j]);
-                dot = fmaf(fa.x + fb.x, fx.x + fy.x, dot);
-                dot = fmaf(fa.y + fb.y, fx.y + fy.y, dot);
-            }
-        }
-#pragma unroll
-        for (int o = 16; o; o /= 2)
-            dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        if (lane == 0)
-            s_dot[warp] = dot;
     }
     products_done(ctl, 0);
     const int row = quarter * 32 + lane;
@@ -440,14 +459,6 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const GradDev g)
         float* to = g.tokens + ((long long)head * p.chunks + ci) * kChunk + row;
         to[2 * plane] = fj + s_f[row];
         to[3 * plane] = col + s_col[row];
-        if (threadIdx.x == 0) {
-            float dot = 0.f;
-            for (int i = 0; i < 8; ++i)
-                dot += s_dot[i];
-            if (!kIsBf16<T>)
-                dot = dot * g.unit_S[at] * g.unit_Z[at];
-            g.across[at] = dot * over_chunk(dec);
-        }
     }
     products_done(ctl, 2);
     if (g.part_k)
@@ -461,6 +472,16 @@ __global__ void __launch_bounds__(kThreads, 1) grad_kv_kernel(const GradDev g)
         store_tile<T, DK>(s_keys, g.dk, c, head, p.dk, g.vec_dk);
     if (g.dv.ptr)
         store_tile<T, DV>(s_values, g.dv, c, head, p.dv, g.vec_dv);
+}
+
+// Both in one launch (blockIdx.z), whose last round of blocks is then half as long.
+template <typename T, int DK, int DV>
+__global__ void __launch_bounds__(kThreads, 1) grad_kernel(const GradDev g)
+{
+    if (blockIdx.z == 0 && g.want_kv)
+        grad_kv<T, DK, DV>(g);
+    else
+        grad_q<T, DK, DV>(g);
 }
 
 // Sums of dq and dk over the heads of a group, one block per token row, in the order of the heads.
@@ -532,7 +553,8 @@ __global__ void __launch_bounds__(128) grad_decay_kernel(const GradDev g)
         float behind = (lane < 31 ? x : 0.f) + (lane % 8 < 7 ? z : 0.f), front = (lane ? y : 0.f) + (lane % 8 ? w : 0.f);
         const int block = lane / 8;
         const long long ch = ci * p.heads + head;
-        const float over = g.across[ch] + (block == 1 || block == 2 ? g.bridges[2 * ch + block - 1] : 0.f), A = p.A[head];
+        const float over = g.across[ch] + (block == 1 || block == 2 ? g.bridges[2 * ch + block - 1] : 0.f);
+        const float A = p.A[head];
 #pragma unroll
         for (int i = 3; i >= 0; --i) {
             behind += e[i] + rows[i];

@@ -5,6 +5,7 @@
 
 #include "block_host.h"
 #include "device_error.h"
+#include "tensor_map.h"
 #include "linear_rows.cuh"
 
 using namespace ttc;
@@ -28,24 +29,6 @@ int few_parts(int64_t blocks, int64_t k, int sms)
     while (parts < 8 && 2 * parts * blocks <= 2 * sms && k >= parts * 2 * 1024)
         parts *= 2;
     return parts;
-}
-
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-int encoder(EncodeTiled& f)
-{
-    static std::atomic<void*> known;
-    void* p = known.load(std::memory_order_relaxed);
-    if (!p) {
-        cudaDriverEntryPointQueryResult found;
-        TTC_CUDA(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &found));
-        if (found != cudaDriverEntryPointSuccess || !p)
-            return fail(TTC_STATUS_CUDA_ERROR, "the driver has no cuTensorMapEncodeTiled");
-        known.store(p, std::memory_order_relaxed);
-    }
-    f = reinterpret_cast<EncodeTiled>(p);
-    return TTC_OK;
 }
 
 // Matrix of `rows` rows of `cols` 16-bit elements, fetched in boxes of 64 columns (128 bytes, swizzled) by `box` rows.
