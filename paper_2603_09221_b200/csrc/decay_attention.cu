@@ -155,9 +155,9 @@ int describe_all(const AttnDev& p, const Rows* q, bool vec_q, const Rows& k, boo
 // One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each piece of a sequence, behind a walk for what the pieces add to the state.
 int take_pieces(int device, const ttc_decay_args* a, int splits, int columns, AttnDev& p, States& q, int ways, Scratch& s)
 {
-    const int64_t sms = sm_count(device), walks = (int64_t)a->heads * splits * ways, rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
+    const int64_t sms = sm_count(device), walks = (int64_t)a->heads * splits, rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
     int64_t want = a->batch;                                         // pieces in all
-    if (walks * a->batch && sms / (walks * a->batch) >= (a->seq_offsets ? 1 : 3))
+    if (walks * a->batch && sms / (walks * a->batch) >= (a->seq_offsets ? 2 : 3))
         want = sms / walks;
     p.piece = a->tokens ? a->tokens : 1;
     p.pieces_per_seq = 1;
@@ -214,7 +214,7 @@ template <typename T, int DK, int COLS> int piece_states(const Maps (&maps)[2], 
     return launch_early("decay attention, states of the pieces", join_kernel, dim3(grid.x, grid.y, grid.z * (COLS / 16)), kWalkThreads, 0, 1, st, p, q, COLS / 4, splits);
 }
 
-// The states in front of all chunks, and the gradients of those behind them.
+// The states in front of all chunks, then the gradients of those behind them.
 template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], const AttnDev& p, const States& q, int splits, cudaStream_t st)
 {
     if (p.pieces == 0)
@@ -223,8 +223,11 @@ template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], 
         TTC_TRY((piece_states<T, DK, COLS>(maps, p, q, 2, splits, st)));
     constexpr int smem = StateShape<T, DK, COLS>::SMEM;
     TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
-    return launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, dim3((unsigned)p.pieces, (unsigned)p.heads, 2 * splits), kWalkBlock, smem, 1, st, maps[0], maps[1], p,
-                        q, splits);
+    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)splits);
+    TTC_TRY((launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[0], p, q, splits)));
+    States back = q;
+    back.way[0] = q.way[1];
+    return launch_early("decay attention, gradients of states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[1], maps[1], p, back, splits);
 }
 
 struct GradPlan {
@@ -283,6 +286,7 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     p.dA = g->dA;
     p.dbias = g->ddelta_bias;
     p.dstate = g->dstate;
+    p.resident = sm_count(device);
     p.want_l = g->ddelta.ptr || g->dA || g->ddelta_bias;
     p.want_q = p.want_l || g->dq.ptr;
     p.want_kv = p.want_l || g->dk.ptr || g->dv.ptr;
@@ -298,7 +302,7 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
         p.f.piece_map = s.take<int2>(p.f.chunks);
         p.f.seq_first = s.take<int>(a->batch + 1);
     }
-    const size_t each = (size_t)p.f.chunks * a->heads, image = (size_t)padded(a->dk) * padded(a->dv) * 4;
+    const size_t each = (size_t)p.f.chunks * a->heads, image = (size_t)padded(a->dk) * padded(a->dv) * 2 * (p.terms = a->dtype == TTC_BF16 && p.want_l ? 3 : 2);
     p.image_S = s.take<char>(each * image);
     p.image_Z = s.take<char>(each * image);
     if (a->dtype == TTC_F16) {
@@ -320,10 +324,15 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     q.way[1].factor = a->scale;
     q.way[1].image = p.image_Z;
     q.way[1].unit = p.unit_Z;
+    q.way[0].terms = q.way[1].terms = p.terms;
     q.way[0].image_bytes = q.way[1].image_bytes = padded(a->dk) * padded(a->dv) * 2;
     if (p.want_l) {
         p.tokens = s.take<float>(5 * each * kChunk);
-        p.across = s.take<float>(each);
+        p.across_of = o.splits * kWalkWarps;
+        p.across = s.take<float>(each * p.across_of);
+        q.way[1].other = p.image_S;
+        q.way[1].other_unit = p.unit_S;
+        q.way[1].across = p.across;
         p.bridges = s.take<float>(2 * each);
         p.sums = s.take<float>(2 * each);
     }
@@ -451,8 +460,8 @@ int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_
         if (f.chunks && (p.want_q || p.want_kv)) {
             constexpr int smem = GradShape<DK, DV>::SMEM;
             TTC_TRY((allow_smem(grad_kernel<T, DK, DV>, smem)));
-            TTC_TRY((launch_early("gradients of decay attention", grad_kernel<T, DK, DV>, dim3((unsigned)f.chunks, (unsigned)f.heads, p.want_q && p.want_kv ? 2 : 1), kThreads, smem, 1,
-                                  st, p)));
+            TTC_TRY((launch_early("gradients of decay attention", grad_kernel<T, DK, DV>, dim3((unsigned)f.chunks, (unsigned)f.heads, p.want_q && p.want_kv ? 2 : 1), kGradThreads, smem,
+                                  1, st, maps[0], maps[1], p)));
         }
         if (f.chunks && (p.part_q || p.part_k))
             TTC_TRY((launch_early("gradients of decay attention, groups", grad_group_kernel<T>, dim3((unsigned)f.chunks, 16), kThreads, 0, 1, st, p)));

@@ -200,10 +200,10 @@ __device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chun
 }
 
 // The tile of results staged in shared memory, to its rows.
-template <typename T, int COLS> __device__ __forceinline__ void store_tile(const char* from, const Rows& r, const Chunk& c, int head, int width, bool vec)
+template <typename T, int COLS, int THREADS> __device__ __forceinline__ void store_tile(const char* from, const Rows& r, const Chunk& c, int head, int width, bool vec)
 {
     T* base = row_ptr<T>(r, c.seq, c.row0) + (long long)head * width;
-    for (int e = threadIdx.x; e < kChunk * COLS / 8; e += kThreads) {
+    for (int e = threadIdx.x; e < kChunk * COLS / 8; e += THREADS) {
         const int row = e / (COLS / 8), c8 = e % (COLS / 8);
         if (row >= c.len || c8 * 8 >= width)
             continue;
@@ -310,6 +310,8 @@ template <typename T, int TERMS, typename F> __device__ __forceinline__ void spl
     }
 }
 
+extern __shared__ __align__(1024) char dattn_tiles[];
+
 // Barriers and tensor memory of a block.
 struct Control {
     uint64_t bar[4];
@@ -334,24 +336,6 @@ __device__ __forceinline__ uint32_t set_up(Control& c, int columns)
     behind_barrier();
     return __shfl_sync(0xffffffffu, c.tmem, 0);
 }
-__device__ __forceinline__ void give_back(uint32_t tmem, int columns)
-{
-    before_barrier();
-    __syncthreads();
-    if (threadIdx.x / 32 == 4)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(columns) : "memory");
-}
-// Products are waited for by everybody; where that takes too long, everybody goes on (the error is noted), so that barriers stay in step.
-__device__ __forceinline__ void products_done(Control& c, int i, uint32_t parity = 0)
-{
-    wait(smem_u32(&c.bar[i]), parity, &c.dead);
-    __syncwarp();
-    behind_barrier();
-}
-
-extern __shared__ char dattn_smem[];
-__device__ __forceinline__ char* aligned_smem() { return reinterpret_cast<char*>((reinterpret_cast<uintptr_t>(dattn_smem) + 1023) / 1024 * 1024); }
-
 // Decay of the pairs of a row and 32 earlier tokens (a block), in a row's lane: on the diagonal from the sums `g` of the block's tokens and the row's own, else e_row, the
 // row's decay from the earlier block's end, times each token's decay to that end.
 __device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const float* to_end)
@@ -530,8 +514,6 @@ template <typename T, int DK> struct WalkShape {
     static constexpr int COLUMNS = 512;                              // of tensor memory
 };
 static_assert(WalkShape<bf16, 128>::SMEM <= 232448 && WalkShape<__half, 128>::SMEM <= 232448, "shared memory of a block");
-
-extern __shared__ __align__(1024) char dattn_tiles[];
 
 // a power of two that takes `most` to 2^13 .. 2^14, and its inverse
 __device__ __forceinline__ float power_for(float most, float& inverse)
@@ -1010,10 +992,14 @@ struct StateDev {
     float* last;                                 // behind them (in front)
     float factor;                                // of what is added
     float *piece_state, *piece_decay;            // of the pieces of a sequence, as the threads of a walk have them: what each adds, then the state in front of it; [pieces][heads]
-    // the states in front of the chunks in 16 bits, [chunks][heads][2][DV / 8][DK][8], as two numbers (2^-17 of the value, float16 2^-22); float16: what they have to be multiplied by
+    // the states in front of the chunks in 16 bits, [chunks][heads][terms][DV / 8][DK][8], as sums of two numbers or three; float16: what they have to be multiplied by
     char* image;
     float* unit;
-    int image_bytes;
+    int image_bytes, terms;
+    // back: <Z, S_0> exp(G_C) of every chunk from the images of S_0: the shares of the warps of its walks, [chunks][heads][splits][16]
+    const char* other;
+    const float* other_unit;
+    float* across;
 };
 // Walks of one launch: one along the sequences, or one each way.
 struct States {
@@ -1222,6 +1208,16 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             const typename S_::Weights& dec = sm.dec[i & 1];
             until(sm.loaded[i & 1], i / 2);
             float unit_v = 1.f;
+            uint4 other[OWN / 8][TERMS];         // asked for early
+            const long long at = (first + chunk(i)) * p.heads + head;
+            const long long place_of = at * ((long long)q.terms * q.image_bytes) + ((col0 + sub * OWN) / 8 * DK + row) * 16;
+            if (q.other) {
+#pragma unroll
+                for (int j = 0; j < OWN / 8; ++j)
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t)
+                        other[j][t] = load_if(reinterpret_cast<const uint4*>(q.other + place_of + j * DK * 16 + t * q.image_bytes), mine && t < q.terms);
+            }
             {                                    // values times their weights, split
                 constexpr int VECTORS = COLS / 32;
                 float up = 1.f;
@@ -1261,7 +1257,6 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             warp_arrives(smem_u32(&sm.weighted));
             const float over = dec.whole;
             if (q.image) {                       // the state in front of the chunk, while the products run
-                const long long at = (first + chunk(i)) * p.heads + head;
                 float up = 1.f;
                 if (!kIsBf16<T>) {
                     float most = 0.f, unit;
@@ -1275,19 +1270,44 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                 if (mine) {
 #pragma unroll
                     for (int j = 0; j < OWN; j += 8) {
-                        uint4 hi, lo;
+                        uint4 term[TERMS];
 #pragma unroll
                         for (int k = 0; k < 4; ++k) {
-                            const float x = S[j + 2 * k] * up, y = S[j + 2 * k + 1] * up;
-                            const uint32_t h = pack16<T>(x, y);
-                            const float2 f = unpack16<T>(h);
-                            (&hi.x)[k] = h;
-                            (&lo.x)[k] = pack16<T>(x - f.x, y - f.y);
+                            float x = S[j + 2 * k] * up, y = S[j + 2 * k + 1] * up;
+#pragma unroll
+                            for (int t = 0; t < TERMS; ++t) {
+                                const uint32_t u = pack16<T>(x, y);
+                                const float2 f = unpack16<T>(u);
+                                (&term[t].x)[k] = u;
+                                x -= f.x, y -= f.y;
+                            }
                         }
-                        char* to = q.image + at * (2 * q.image_bytes) + (((col0 + sub * OWN + j) / 8 * DK + row) * 16);
-                        *reinterpret_cast<uint4*>(to) = hi;
-                        *reinterpret_cast<uint4*>(to + q.image_bytes) = lo;
+                        char* to = q.image + place_of + j / 8 * DK * 16;
+#pragma unroll
+                        for (int t = 0; t < TERMS; ++t)
+                            if (t < q.terms)
+                                *reinterpret_cast<uint4*>(to + t * q.image_bytes) = term[t];
                     }
+                }
+                if (q.other) {
+                    float dot = 0.f;
+#pragma unroll
+                    for (int j = 0; j < OWN; j += 2) {
+                        float2 f = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int t = TERMS - 1; t >= 0; --t) {
+                            const float2 x = unpack16<T>((&other[j / 8][t].x)[j % 8 / 2]);
+                            f.x += x.x, f.y += x.y;
+                        }
+                        dot = fmaf(S[j], f.x, dot);
+                        dot = fmaf(S[j + 1], f.y, dot);
+                    }
+                    dot = mine ? dot : 0.f;
+#pragma unroll
+                    for (int o = 16; o; o /= 2)
+                        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                    if (lane == 0)
+                        q.across[(at * splits + z) * kWalkWarps + warp] = dot * over * (kIsBf16<T> ? 1.f : q.other_unit[at]);
                 }
             }
             until(sm.added, i);

@@ -11,8 +11,8 @@
 // behind t, of which only the few that span t count where decays are strong (dA was off by 4e-6 of its norm).  Instead, with the chunk in four blocks of 32: pairs within t's block
 // one by one (prefix sums of M's rows, added up over the rows from t on); pairs of t's block and an earlier one by row sums, with a later one by column
 // sums, and pairs of blocks on both sides of t's by their totals.
-// dl goes into float32 sums over all tokens (dA, ddelta_bias): M is taken from the float32 scores, and S_0 and Z go into e and f as two numbers of 16 bits
-// (2^-18 of the value).
+// dl goes into float32 sums over all tokens (dA, ddelta_bias): M is taken from the float32 scores, and S_0 and Z go into e and f as sums of numbers of 16 bits, three
+// bfloat16 (2^-27 of the value; with two, 2^-18, dA was off by up to 7e-6 of its norm) or two float16 (2^-23).  dq, dk and dv alone make do with two.
 //
 // The states in front of the chunks come from a state walk, the Z from one that goes backwards along queries and dy; then one
 // kernel finds dq, e and row, one dk, dv, f and col, and a small one dl.
@@ -23,12 +23,6 @@
 namespace ttc {
 namespace dattn {
 
-__device__ __forceinline__ void load_image(uint32_t to, const char* from, int bytes)
-{
-    for (int i = threadIdx.x * 16; i < bytes; i += kThreads * 16)
-        copy16(to + i, from + i, true);
-}
-
 struct GradDev {
     AttnDev f;
     Rows dy, dq, dk, dv, ddelta;
@@ -37,127 +31,241 @@ struct GradDev {
     float *dA, *dbias, *dstate;
     // scratch
     float *part_q, *part_k;                      // dq, dk of every head, where heads share them: [rows][heads][dk]
-    char *image_S, *image_Z;                     // [chunks][heads][2][DV / 8][DK][8]
+    char *image_S, *image_Z;                     // [chunks][heads][terms][DV / 8][DK][8]
+    int terms;
     float *unit_S, *unit_Z;
     float* tokens;                               // [5][heads][chunks][128]: e, row sums, f, column sums (both without the blocks on the diagonal), pairs within t's block
     float* bridges;                              // [chunks][heads][2]: of pairs on both sides of the second and the third block
-    float* across;                               // exp(G_C) <Z, S_0>: [chunks][heads]
+    float* across;                               // exp(G_C) <Z, S_0>: shares, [chunks][heads][across_of]
+    int across_of;
     float* sums;                                 // of dA and of ddelta_bias: [2][heads][chunks]
     int want_q, want_kv, want_l;
+    int resident;                                // blocks that run at once
 };
+
+constexpr int kGradThreads = 512;
 
 template <int DK, int DV> struct GradShape {
     static constexpr int K_BYTES = DK / 64 * kBox, V_BYTES = DV / 64 * kBox, IMAGE = DK * DV * 2;
-    static constexpr int SMEM = 1024 + 2 * K_BYTES + 2 * V_BYTES + 2 * IMAGE;
+    static constexpr int TILES = 2 * K_BYTES + 2 * V_BYTES + 2 * IMAGE;
+    struct Small {
+        Control ctl;
+        uint64_t second_product, third, third_product;               // of the images' terms: products that are done, the third term is there
+        Decays dec;
+        alignas(16) float to[4][96];             // [block][earlier token]: decay from it to the block's begin
+        alignas(16) float from[kChunk];          // exp from each token's block's begin
+        float sums[4][kChunk], dots[4][kChunk], within[kChunk], pairs[4][4];
+    };
+    static constexpr int SMEM = TILES + sizeof(Small);
 };
 
-// Half of a row of results (COLS / 2 of tensor memory's columns), times f, staged in a tile.
-template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32_t from, char* tile, int row, int half, float f)
+// A quarter of a row of results (COLS / 4 of tensor memory's columns), times f, staged in a tile.
+template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32_t from, char* tile, int row, int sub, float f)
 {
 #pragma unroll
-    for (int c0 = 0; c0 < COLS / 2; c0 += 32) {
-        float v[32];
-        tmem_ld32(from + half * (COLS / 2) + c0, v);
+    for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
+        float v[16];
+        tmem_ld16(from + sub * (COLS / 4) + c0, v);
 #pragma unroll
-        for (int j = 0; j < 32; j += 8) {
+        for (int j = 0; j < 16; j += 8) {
             const uint4 w = make_uint4(pack16<T>(v[j] * f, v[j + 1] * f), pack16<T>(v[j + 2] * f, v[j + 3] * f), pack16<T>(v[j + 4] * f, v[j + 5] * f),
                                        pack16<T>(v[j + 6] * f, v[j + 7] * f));
-            *reinterpret_cast<uint4*>(tile + tile_at(row, (half * (COLS / 2) + c0 + j) / 8)) = w;
+            *reinterpret_cast<uint4*>(tile + tile_at(row, (sub * (COLS / 4) + c0 + j) / 8)) = w;
         }
     }
 }
-// The same in float32, to the head's part of a sum over the heads of a group.
-template <int COLS> __device__ __forceinline__ void part_row(uint32_t from, float* to, int width, bool ok, int half, float f)
+// The same in float32, [128][COLS], 16 bytes in another place of their 128 in each of eight rows.
+template <int COLS> __device__ __forceinline__ float4* part_at(char* area, int row, int c4) { return reinterpret_cast<float4*>(area) + row * (COLS / 4) + (c4 ^ (row & 7)); }
+template <int COLS> __device__ __forceinline__ void stage_part(uint32_t from, char* area, int row, int sub, float f)
 {
 #pragma unroll
-    for (int c0 = 0; c0 < COLS / 2; c0 += 32) {
-        float v[32];
-        const int at = half * (COLS / 2) + c0;
-        tmem_ld32(from + at, v);
-        if (ok) {
+    for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
+        float v[16];
+        tmem_ld16(from + sub * (COLS / 4) + c0, v);
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (at + j < width)
-                    to[at + j] = v[j] * f;
+        for (int j = 0; j < 16; j += 4)
+            *part_at<COLS>(area, row, (sub * (COLS / 4) + c0 + j) / 4) = make_float4(v[j] * f, v[j + 1] * f, v[j + 2] * f, v[j + 3] * f);
+    }
+}
+// From there to a head's part of a sum over the heads of a group.
+template <int COLS> __device__ __forceinline__ void store_part(char* area, float* to, long long stride, int rows, int width)
+{
+    for (int e = threadIdx.x; e < kChunk * COLS / 4; e += kGradThreads) {
+        const int row = e / (COLS / 4), c4 = e % (COLS / 4);
+        if (row >= rows || c4 * 4 >= width)
+            continue;
+        const float4 v = *part_at<COLS>(area, row, c4);
+        float* at = to + row * stride + c4 * 4;
+        if (width % 4 == 0) {
+            *reinterpret_cast<float4*>(at) = v;
+        } else {
+            at[0] = v.x;
+            if (c4 * 4 + 1 < width)
+                at[1] = v.y;
+            if (c4 * 4 + 2 < width)
+                at[2] = v.z;
+            if (c4 * 4 + 3 < width)
+                at[3] = v.w;
         }
     }
 }
-// Half of a row of results, times f, back to where it was; returns its product with the same half of row `row` of a tile.
-template <typename T, int COLS> __device__ __forceinline__ float weigh_row(uint32_t at, const char* tile, int row, int half, float f)
+// A quarter of a row of results, times f, back to where it was; returns its product with the same quarter of row `row` of a tile.
+template <typename T, int COLS> __device__ __forceinline__ float weigh_row(uint32_t at, const char* tile, int row, int sub, float f)
 {
     float dot = 0.f;
 #pragma unroll
-    for (int c0 = 0; c0 < COLS / 2; c0 += 32) {
-        float v[32];
-        const uint32_t here = at + half * (COLS / 2) + c0;
-        tmem_ld32(here, v);
+    for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
+        float v[16];
+        const uint32_t here = at + sub * (COLS / 4) + c0;
+        tmem_ld16(here, v);
+        uint32_t r[16];
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 16; ++j) {
             v[j] *= f;
+            r[j] = __float_as_uint(v[j]);
+        }
         if (tile) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-                const uint4 w = *reinterpret_cast<const uint4*>(tile + tile_at(row, (half * (COLS / 2) + c0 + j) / 8));
-                const uint32_t* u = &w.x;
+            for (int j = 0; j < 16; j += 8) {
+                const uint4 w = *reinterpret_cast<const uint4*>(tile + tile_at(row, (sub * (COLS / 4) + c0 + j) / 8));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float2 x = unpack16<T>(u[i]);
+                    const float2 x = unpack16<T>((&w.x)[i]);
                     dot = fmaf(x.x, v[j + 2 * i], dot);
                     dot = fmaf(x.y, v[j + 2 * i + 1], dot);
                 }
             }
         }
-        tmem_st32(here, v);
+        tmem_st16(here, r);
     }
     return dot;
 }
 
 __device__ __forceinline__ long long packed_row(const AttnDev& p, const Chunk& c, int t) { return c.seq * p.seqs.tokens + c.row0 + t; }
 
-// dq of one chunk and head, lanes for the tokens i: scores and dy v' into tensor memory beside S_0 dy; M's row sums from both; dy v' with its decays goes
-// back in 16 bits and is multiplied with the keys.
-template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(const GradDev& g)
+__device__ __forceinline__ void fetch_bytes(uint32_t to, const char* from, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" :: "r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void fetch_bytes_to_l2(const char* from, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" :: "l"(from), "r"(bytes) : "memory");
+}
+
+// The tiles and the image of a chunk and head, and its decays.  What the block that will run behind this one needs is asked for into L2, so that memory is at work while this
+// one computes.
+template <typename T, int DK, int DV, bool KV>
+__device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& there, const Maps& back, const Chunk& c, typename GradShape<DK, DV>::Small& sm, uint32_t tiles)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    __shared__ Control ctl;
-    __shared__ Decays dec;
-    __shared__ alignas(16) float s_to[4][96];
-    __shared__ float s_half[kChunk], s_rows[kChunk], s_within[kChunk], s_pairs[4][4], s_dot[8];
+    const int head = blockIdx.y, group = head / p.share, warp = threadIdx.x / 32;
+    const uint32_t queries = tiles, keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
+    const char* from = (KV ? g.image_Z : g.image_S) + ((long long)blockIdx.x * p.heads + head) * ((long long)g.terms * S::IMAGE);
+    float l = 0.f;
+    if (warp < 4)
+        l = log_decay_at<T>(p, c, head, threadIdx.x);
+    if (threadIdx.x == 0) {
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.second_product)) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.third)) : "memory");
+        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.third_product)) : "memory");
+    }
+    const uint32_t tmem = set_up(sm.ctl, 512);
+    const uint32_t bar = smem_u32(&sm.ctl.bar[3]);
+    const bool engine = there.there && back.there && (!p.seqs.offsets || c.len == kChunk);
+    if (threadIdx.x == 32 * 15) {
+        expect_bytes(bar, 2 * S::IMAGE + (engine ? 2 * S::K_BYTES + 2 * S::V_BYTES : 0));
+        if (engine) {
+            const int row0 = (int)c.row0, seq = (int)c.seq;
+            for (int b = 0; b < DV / 64; ++b) {
+                fetch_box(values + b * kBox, &there.v, b * 64, head, row0, seq, bar);
+                fetch_box(dys + b * kBox, &back.v, b * 64, head, row0, seq, bar);
+            }
+            for (int b = 0; b < DK / 64; ++b) {
+                fetch_box(keys + b * kBox, &there.k, b * 64, group, row0, seq, bar);
+                fetch_box(queries + b * kBox, &back.k, b * 64, group, row0, seq, bar);
+            }
+        }
+        fetch_bytes(image, from, 2 * S::IMAGE, bar);
+        const long long next = blockIdx.x + (long long)gridDim.x * (blockIdx.y + (long long)gridDim.y * blockIdx.z) + g.resident;
+        const long long ci = next % gridDim.x, h = next / gridDim.x % gridDim.y, z = next / gridDim.x / gridDim.y;
+        if (engine && z < gridDim.z) {
+            const Chunk n = chunk_at(p, ci);
+            if (n.len > 0) {
+                const int row0 = (int)n.row0, seq = (int)n.seq;
+                for (int b = 0; b < DV / 64; ++b) {
+                    fetch_to_l2(&there.v, b * 64, (int)h, row0, seq);
+                    fetch_to_l2(&back.v, b * 64, (int)h, row0, seq);
+                }
+                for (int b = 0; b < DK / 64; ++b) {
+                    fetch_to_l2(&there.k, b * 64, (int)h / p.share, row0, seq);
+                    fetch_to_l2(&back.k, b * 64, (int)h / p.share, row0, seq);
+                }
+                fetch_bytes_to_l2((z == 0 && g.want_kv ? g.image_Z : g.image_S) + (ci * p.heads + h) * ((long long)g.terms * S::IMAGE), g.terms * S::IMAGE);
+            }
+        }
+    }
+    if (!engine) {
+        load_tile<T, DK, kGradThreads>(queries, p.q, c, group * p.dk, p.dk, p.vec_q, threadIdx.x);
+        load_tile<T, DK, kGradThreads>(keys, p.k, c, group * p.dk, p.dk, p.vec_k, threadIdx.x);
+        load_tile<T, DV, kGradThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
+        load_tile<T, DV, kGradThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
+        copies_begun();
+    }
+    if (warp < 4) {
+        block_decays(l, threadIdx.x, sm.dec);
+        sm.from[threadIdx.x] = ex2(sm.dec.g[threadIdx.x]);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 4 * 96; i += kGradThreads)
+        sm.to[i / 96][i % 96] = i % 96 < i / 96 * 32 ? to_block(sm.dec, i % 96, i / 96) : 0.f;
+    copies_done<0>();
+    await(bar, 0, &sm.ctl.dead);
+    to_tensor_cores();
+    __syncthreads();
+    behind_barrier();
+    return tmem;
+}
+__device__ __forceinline__ void grad_products_done(Control& c, int i)
+{
+    await(smem_u32(&c.bar[i]), 0, &c.dead);
+    __syncwarp();
+    behind_barrier();
+}
+// (products under way end before tensor memory is given back)
+__device__ __forceinline__ void end_grad(Control& c, uint32_t tmem)
+{
+    before_barrier();
+    __syncthreads();
+    if (threadIdx.x / 32 == 4) {
+        if (c.dead) {
+            if (threadIdx.x % 32 == 0)
+                for (int i = 0; i < 1000; ++i)
+                    __nanosleep(1000);
+            __syncwarp();
+        }
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// dq of one chunk and head, lanes for the tokens i, a block of 32 tokens j to each of a row's four warps: scores and dy v' into tensor memory beside S_0 dy; M's row sums from both;
+// dy v' with its decays goes back in 16 bits and is multiplied with the keys.
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(const GradDev& g, const Maps& there, const Maps& back)
+{
+    using S = GradShape<DK, DV>;
+    const AttnDev& p = g.f;
     const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, half = warp / 4;
-    wait_for_previous();
+    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
         return;
-    char* smem = aligned_smem();
-    const uint32_t queries = smem_u32(smem), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
-    load_tile<T, DK, kThreads>(queries, p.q, c, head / p.share * p.dk, p.dk, p.vec_q, threadIdx.x);
-    load_tile<T, DK, kThreads>(keys, p.k, c, head / p.share * p.dk, p.dk, p.vec_k, threadIdx.x);
-    load_tile<T, DV, kThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
-    load_tile<T, DV, kThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
-    load_image(image, g.image_S + at * (2 * S::IMAGE), 2 * S::IMAGE);
-    copies_begun();
-    // for <Z, S_0>: the image of Z comes into registers beside the tiles' copies
-    constexpr int VECTORS = S::IMAGE / 16 / kThreads;
-    uint4 other[2][VECTORS];
-    if (g.want_l) {
-        const uint4* from = reinterpret_cast<const uint4*>(g.image_Z + at * (2 * S::IMAGE)) + threadIdx.x;
-#pragma unroll
-        for (int i = 0; i < VECTORS; ++i) {
-            other[0][i] = from[i * kThreads];
-            other[1][i] = from[S::IMAGE / 16 + i * kThreads];
-        }
-    }
-    if (warp < 4)
-        block_decays(log_decay_at<T>(p, c, head, threadIdx.x), threadIdx.x, dec);
-    const uint32_t tmem = set_up(ctl, 512);      // scores, dy v', results: 128 columns each
+    char* smem = dattn_tiles;
+    typename S::Small& sm = *reinterpret_cast<typename S::Small*>(smem + S::TILES);
+    const Decays& dec = sm.dec;
+    const uint32_t queries = __shfl_sync(0xffffffffu, smem_u32(smem), 0), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES,
+                   image = dys + S::V_BYTES;
+    const uint32_t tmem = begin_grad<T, DK, DV, false>(g, there, back, c, sm, queries);        // scores, dy v', results: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, results = tmem + 256, lanes = (uint32_t)(quarter * 32) << 16;
-    for (int i = threadIdx.x; i < 4 * 96; i += kThreads)
-        s_to[i / 96][i % 96] = i % 96 < i / 96 * 32 ? to_block(dec, i % 96, i / 96) : 0.f;
-    copies_done<0>();
-    to_tensor_cores();
-    __syncthreads();
     if (warp == 0) {
         constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_state = instruction(kIsBf16<T>, false, false, 128, DK);
         if (elect_one()) {
@@ -167,94 +275,88 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
 #pragma unroll
             for (int s = 0; s < DK / 16; ++s)
                 mma(scores, over_columns(queries, s), over_columns(keys, s), id, s > 0);
-            commit(smem_u32(&ctl.bar[0]));
+            commit(smem_u32(&sm.ctl.bar[0]));
+#pragma unroll
+            for (int s = 0; s < DV / 16; ++s)    // the small ones first: the tensor cores cut sums off
+                mma(results, over_columns(dys, s), image_over_dv<DK>(image + S::IMAGE, s), id_state, s > 0);
 #pragma unroll
             for (int s = 0; s < DV / 16; ++s)
-                mma(results, over_columns(dys, s), image_over_dv<DK>(image, s), id_state, s > 0);
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(results, over_columns(dys, s), image_over_dv<DK>(image + S::IMAGE, s), id_state, 1);
-            commit(smem_u32(&ctl.bar[1]));
+                mma(results, over_columns(dys, s), image_over_dv<DK>(image, s), id_state, 1);
+            commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
     }
-    if (g.want_l) {                              // <Z, S_0>, while the products run
-        const uint4* have = reinterpret_cast<const uint4*>(smem + 2 * S::K_BYTES + 2 * S::V_BYTES) + threadIdx.x;
-        float dot = 0.f;
-#pragma unroll
-        for (int i = 0; i < VECTORS; ++i) {
-            const uint4 x = have[i * kThreads], y = have[S::IMAGE / 16 + i * kThreads];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 a = unpack16<T>((&other[0][i].x)[j]), b = unpack16<T>((&other[1][i].x)[j]), c = unpack16<T>((&x.x)[j]), d = unpack16<T>((&y.x)[j]);
-                dot = fmaf(a.x + b.x, c.x + d.x, dot);
-                dot = fmaf(a.y + b.y, c.y + d.y, dot);
-            }
+    grad_products_done(sm.ctl, 0);
+    if (g.terms == 3 && warp == 12) {            // the third term takes the values' place (this warp has nothing else to do)
+        if (elect_one()) {
+            expect_bytes(smem_u32(&sm.third), S::IMAGE);
+            fetch_bytes(values, g.image_S + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
         }
+        __syncwarp();
+        await(smem_u32(&sm.third), 0, &sm.ctl.dead);
+        __syncwarp();
+        constexpr uint32_t id_state = instruction(kIsBf16<T>, false, false, 128, DK);
+        if (elect_one()) {
 #pragma unroll
-        for (int o = 16; o; o /= 2)
-            dot += __shfl_xor_sync(0xffffffffu, dot, o);
-        if (lane == 0)
-            s_dot[warp] = dot;
+            for (int s = 0; s < DV / 16; ++s)
+                mma(results, over_columns(dys, s), image_over_dv<DK>(values, s), id_state, 1);
+            commit(smem_u32(&sm.third_product));
+        }
+        __syncwarp();
     }
-    products_done(ctl, 0);
     const int row = quarter * 32 + lane;
-    const float mine = dec.g[row], e_mine = ex2(mine);
-    uint32_t packed[2][16];
+    uint32_t packed[16];
     float row_sum = 0.f;
+    if (sub <= quarter) {
+        float v[32];
+        tmem_ld32(slopes + sub * 32 + lanes, v);
+        decay_row(v, dec.g + sub * 32, sub == quarter, lane, dec.g[row], sm.from[row], &sm.to[quarter][sub < quarter ? sub * 32 : 0]);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int b = half + 2 * i;
-        if (b <= quarter) {
-            float v[32];
-            tmem_ld32(slopes + b * 32 + lanes, v);
-            decay_row(v, dec.g + b * 32, b == quarter, lane, mine, e_mine, &s_to[quarter][b < quarter ? b * 32 : 0]);
+        for (int j = 0; j < 16; ++j)
+            packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+        if (g.want_l) {
+            float w[32];
+            tmem_ld32(scores + sub * 32 + lanes, w);
+            if (sub < quarter) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                packed[i][j] = pack16<T>(v[2 * j], v[2 * j + 1]);
-            if (g.want_l) {
-                float w[32];
-                tmem_ld32(scores + b * 32 + lanes, w);
-                if (b < quarter) {
-                    float part = 0.f;
+                for (int j = 0; j < 32; ++j)
+                    row_sum = fmaf(v[j], w[j], row_sum);
+                float part = row_sum;
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        part = fmaf(v[j], w[j], part);
-                    row_sum += part;
+                for (int o = 16; o; o /= 2)
+                    part += __shfl_xor_sync(0xffffffffu, part, o);
+                if (lane == 0)
+                    sm.pairs[quarter][sub] = part;
+            } else {
+                float sum = 0.f;
 #pragma unroll
-                    for (int o = 16; o; o /= 2)
-                        part += __shfl_xor_sync(0xffffffffu, part, o);
-                    if (lane == 0)
-                        s_pairs[quarter][b] = part;
-                } else {
-                    float x[32], sum = 0.f;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j) {
-                        x[j] = j <= lane ? sum : 0.f;
-                        sum = fmaf(v[j], w[j], sum);
-                    }
-                    group_sums<32, 32, 1>(x, lane);
-                    s_within[b * 32 + first_value<32, 32>(lane)] = x[0];
+                for (int j = 0; j < 32; ++j) {
+                    const float m = v[j] * w[j];
+                    v[j] = j <= lane ? sum : 0.f;
+                    sum += m;
                 }
+                group_sums<32, 32, 1>(v, lane);
+                sm.within[sub * 32 + first_value<32, 32>(lane)] = v[0];
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                packed[i][j] = 0;
         }
-    }
-    before_barrier();
-    asm volatile("bar.sync %0, 64;" :: "r"(1 + quarter) : "memory");
-    behind_barrier();
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        tmem_st16(slopes + (half + 2 * i) * 16 + lanes, packed[i]);
-    products_done(ctl, 1);
-    const float e = weigh_row<T, DK>(results + lanes, smem, row, half, from_begin(dec, row) * (kIsBf16<T> ? 1.f : g.unit_S[at]));
-    if (half == 1) {
-        s_half[row] = e;
-        s_rows[row] = row_sum;
+        for (int j = 0; j < 16; ++j)
+            packed[j] = 0;
     }
+    // the four warps of these rows have read what is overwritten now
+    before_barrier();
+    asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
+    behind_barrier();
+    tmem_st16(slopes + sub * 16 + lanes, packed);
+    grad_products_done(sm.ctl, 1);
+    if (g.terms == 3) {
+        await(smem_u32(&sm.third_product), 0, &sm.ctl.dead);
+        __syncwarp();
+        behind_barrier();
+    }
+    sm.dots[sub][row] = weigh_row<T, DK>(results + lanes, smem, row, sub, from_begin(dec, row) * (kIsBf16<T> ? 1.f : g.unit_S[at]));
+    sm.sums[sub][row] = row_sum;
     tmem_st_done();
     before_barrier();
     __syncthreads();
@@ -265,94 +367,80 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
 #pragma unroll
             for (int s = 0; s < 8; ++s)
                 mma_tmem(results, slopes + s * 8, over_tokens(keys, s), id, 1);
-            commit(smem_u32(&ctl.bar[2]));
+            commit(smem_u32(&sm.ctl.bar[2]));
         }
         __syncwarp();
     }
-    if (half == 0 && g.want_l) {
+    if (sub == 0 && g.want_l) {
         const long long plane = (long long)p.heads * p.chunks * kChunk;
         float* to = g.tokens + ((long long)head * p.chunks + ci) * kChunk + row;
-        to[0] = (e + s_half[row]) * p.scale;
-        to[plane] = (row_sum + s_rows[row]) * p.scale;
-        to[4 * plane] = s_within[row] * p.scale;
-        if (row == 0) {
-            float dot = 0.f;
-            for (int i = 0; i < 8; ++i)
-                dot += s_dot[i];
-            g.across[at] = dot * over_chunk(dec) * (kIsBf16<T> ? 1.f : g.unit_S[at] * g.unit_Z[at]);
-        }
+        to[0] = ((sm.dots[0][row] + sm.dots[1][row]) + (sm.dots[2][row] + sm.dots[3][row])) * p.scale;
+        to[plane] = ((sm.sums[0][row] + sm.sums[1][row]) + (sm.sums[2][row] + sm.sums[3][row])) * p.scale;
+        to[4 * plane] = sm.within[row] * p.scale;
         if (row < 2)
-            g.bridges[2 * at + row] = (s_pairs[3][0] + s_pairs[2 + row][row]) * p.scale;
+            g.bridges[2 * at + row] = (sm.pairs[3][0] + sm.pairs[2 + row][row]) * p.scale;
     }
-    products_done(ctl, 2);
-    if (g.part_q)
-        part_row<DK>(results + lanes, g.part_q + (packed_row(p, c, row) * p.heads + head) * p.dk, p.dk, row < c.len, half, p.scale);
+    grad_products_done(sm.ctl, 2);
+    if (g.part_q)                                // (in the place of queries and keys)
+        stage_part<DK>(results + lanes, smem, row, sub, p.scale);
     else if (g.dq.ptr)
-        stage_row<T, DK>(results + lanes, smem, row, half, p.scale);
-    give_back(tmem, 512);
-    if (!g.part_q && g.dq.ptr)
-        store_tile<T, DK>(smem, g.dq, c, head, p.dk, g.vec_dq);
+        stage_row<T, DK>(results + lanes, smem, row, sub, p.scale);
+    end_grad(sm.ctl, tmem);
+    if (g.part_q)
+        store_part<DK>(smem, g.part_q + (packed_row(p, c, 0) * p.heads + head) * p.dk, (long long)p.heads * p.dk, c.len, p.dk);
+    else if (g.dq.ptr)
+        store_tile<T, DK, kGradThreads>(smem, g.dq, c, head, p.dk, g.vec_dq);
 }
 
 // Decay of the pairs (32 rows of block b, column) of the lower triangle, a lane for the column j: `mine` its sum from its block's begin, `to_there` the decay from it
 // to block b's begin; from [32]: the rows' decays from there.
-__device__ __forceinline__ void decay_column(float (&v)[32], const Decays& d, bool diagonal, int b, int lane, float mine, float to_there, const float* from)
+__device__ __forceinline__ void decay_column(float (&v)[32], float (&w)[32], const float* sums, bool diagonal, int lane, float mine, float to_there, float scale, const float* from)
 {
     if (diagonal) {
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-            const float4 h = *reinterpret_cast<const float4*>(d.g + b * 32 + i);
-            v[i] = i >= lane ? v[i] * ex2(h.x - mine) : 0.f;
-            v[i + 1] = i + 1 >= lane ? v[i + 1] * ex2(h.y - mine) : 0.f;
-            v[i + 2] = i + 2 >= lane ? v[i + 2] * ex2(h.z - mine) : 0.f;
-            v[i + 3] = i + 3 >= lane ? v[i + 3] * ex2(h.w - mine) : 0.f;
+            const float4 h = *reinterpret_cast<const float4*>(sums + i);
+            const float d[4] = {i >= lane ? ex2(h.x - mine) * scale : 0.f, i + 1 >= lane ? ex2(h.y - mine) * scale : 0.f, i + 2 >= lane ? ex2(h.z - mine) * scale : 0.f,
+                                i + 3 >= lane ? ex2(h.w - mine) * scale : 0.f};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[i + j] = i + j >= lane ? v[i + j] * d[j] : 0.f;
+                w[i + j] = i + j >= lane ? w[i + j] * d[j] : 0.f;
+            }
         }
     } else {
+        const f2 both = pack2(to_there * scale, to_there * scale);
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
             const float4 h = *reinterpret_cast<const float4*>(from + i);
-            v[i] *= to_there * h.x;
-            v[i + 1] *= to_there * h.y;
-            v[i + 2] *= to_there * h.z;
-            v[i + 3] *= to_there * h.w;
+            const f2 a = mul2(both, pack2(h.x, h.y)), b = mul2(both, pack2(h.z, h.w));
+            unpack2(mul2(pack2(v[i], v[i + 1]), a), v[i], v[i + 1]);
+            unpack2(mul2(pack2(v[i + 2], v[i + 3]), b), v[i + 2], v[i + 3]);
+            unpack2(mul2(pack2(w[i], w[i + 1]), a), w[i], w[i + 1]);
+            unpack2(mul2(pack2(w[i + 2], w[i + 3]), b), w[i + 2], w[i + 3]);
         }
     }
 }
 
-// dk and dv of one chunk and head, lanes for the tokens j.
-template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(const GradDev& g)
+// dk and dv of one chunk and head, lanes for the tokens j, a block of 32 tokens i to each of a row's four warps.
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(const GradDev& g, const Maps& there, const Maps& back)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    __shared__ Control ctl;
-    __shared__ Decays dec;
-    __shared__ alignas(16) float s_from[kChunk];
-    __shared__ float s_f[kChunk], s_col[kChunk];
     const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, half = warp / 4;
-    wait_for_previous();
+    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
         return;
-    char* smem = aligned_smem();
-    const uint32_t queries = smem_u32(smem), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
+    char* smem = dattn_tiles;
+    typename S::Small& sm = *reinterpret_cast<typename S::Small*>(smem + S::TILES);
+    const Decays& dec = sm.dec;
     char* s_keys = smem + S::K_BYTES;
     char* s_values = s_keys + S::K_BYTES;
-    load_tile<T, DK, kThreads>(queries, p.q, c, head / p.share * p.dk, p.dk, p.vec_q, threadIdx.x);
-    load_tile<T, DK, kThreads>(keys, p.k, c, head / p.share * p.dk, p.dk, p.vec_k, threadIdx.x);
-    load_tile<T, DV, kThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
-    load_tile<T, DV, kThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
-    load_image(image, g.image_Z + at * (2 * S::IMAGE), 2 * S::IMAGE);
-    copies_begun();
-    if (warp < 4)
-        block_decays(log_decay_at<T>(p, c, head, threadIdx.x), threadIdx.x, dec);
-    const uint32_t tmem = set_up(ctl, 512);      // scores, v dy', dk, dv: 128 columns each
+    const uint32_t queries = __shfl_sync(0xffffffffu, smem_u32(smem), 0), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES,
+                   image = dys + S::V_BYTES;
+    const uint32_t tmem = begin_grad<T, DK, DV, true>(g, there, back, c, sm, queries);         // scores, v dy', dk, dv: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, dks = tmem + 256, dvs = tmem + 384, lanes = (uint32_t)(quarter * 32) << 16;
-    if (warp < 4)
-        s_from[threadIdx.x] = ex2(dec.g[threadIdx.x]);
-    copies_done<0>();
-    to_tensor_cores();
-    __syncthreads();
     if (warp == 0) {
         constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_k = instruction(kIsBf16<T>, false, false, 128, DK),
                            id_v = instruction(kIsBf16<T>, false, true, 128, DV);
@@ -363,80 +451,87 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
 #pragma unroll
             for (int s = 0; s < DK / 16; ++s)
                 mma(scores, over_columns(keys, s), over_columns(queries, s), id, s > 0);
-            commit(smem_u32(&ctl.bar[0]));
+            commit(smem_u32(&sm.ctl.bar[0]));
 #pragma unroll
             for (int s = 0; s < DV / 16; ++s)
-                mma(dks, over_columns(values, s), image_over_dv<DK>(image, s), id_k, s > 0);
+                mma(dks, over_columns(values, s), image_over_dv<DK>(image + S::IMAGE, s), id_k, s > 0);
+            commit(smem_u32(&sm.second_product));
 #pragma unroll
             for (int s = 0; s < DV / 16; ++s)
-                mma(dks, over_columns(values, s), image_over_dv<DK>(image + S::IMAGE, s), id_k, 1);
+                mma(dks, over_columns(values, s), image_over_dv<DK>(image, s), id_k, 1);
 #pragma unroll
             for (int s = 0; s < DK / 16; ++s)
                 mma(dvs, over_columns(keys, s), image_over_dk<DK>(image, s), id_v, s > 0);
-            commit(smem_u32(&ctl.bar[1]));
+            commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
     }
-    products_done(ctl, 0);
-    const int row = quarter * 32 + lane;
-    const float mine = dec.g[row];
-    uint32_t packed_v[2][16], packed_k[2][16];
-    float col = 0.f;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int b = half + 2 * i;
-        if (b >= quarter) {
-            const float to_there = b > quarter ? to_block(dec, row, b) * p.scale : 0.f;
-            float v[32], w[32];
-            tmem_ld32(scores + b * 32 + lanes, v);
-            tmem_ld32(slopes + b * 32 + lanes, w);
-            // M = decay scale (q . k) (dy . v): the decay goes into the scores first, then into the slopes
-            decay_column(v, dec, b == quarter, b, lane, mine, to_there, s_from + b * 32);
-            if (b == quarter) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    v[j] *= p.scale;
-            }
-            if (b > quarter) {
-                float part = 0.f;
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    part = fmaf(v[j], w[j], part);
-                col += part;
-            }
-            decay_column(w, dec, b == quarter, b, lane, mine, to_there, s_from + b * 32);
-            if (b == quarter) {
-#pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    w[j] *= p.scale;
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                packed_v[i][j] = pack16<T>(v[2 * j], v[2 * j + 1]);
-                packed_k[i][j] = pack16<T>(w[2 * j], w[2 * j + 1]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                packed_v[i][j] = packed_k[i][j] = 0;
+    if (g.terms == 3 && warp == 3) {             // the third term takes the second one's place (this warp has nothing else to do)
+        await(smem_u32(&sm.second_product), 0, &sm.ctl.dead);
+        __syncwarp();
+        behind_barrier();
+        if (elect_one()) {
+            expect_bytes(smem_u32(&sm.third), S::IMAGE);
+            fetch_bytes(image + S::IMAGE, g.image_Z + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
         }
+        __syncwarp();
+        await(smem_u32(&sm.third), 0, &sm.ctl.dead);
+        __syncwarp();
+        constexpr uint32_t id_k = instruction(kIsBf16<T>, false, false, 128, DK);
+        if (elect_one()) {
+#pragma unroll
+            for (int s = 0; s < DV / 16; ++s)
+                mma(dks, over_columns(values, s), image_over_dv<DK>(image + S::IMAGE, s), id_k, 1);
+            commit(smem_u32(&sm.third_product));
+        }
+        __syncwarp();
+    }
+    grad_products_done(sm.ctl, 0);
+    const int row = quarter * 32 + lane;
+    uint32_t packed_v[16], packed_k[16];
+    float col = 0.f;
+    if (sub >= quarter) {
+        float v[32], w[32];
+        tmem_ld32(scores + sub * 32 + lanes, v);
+        tmem_ld32(slopes + sub * 32 + lanes, w);
+        if (sub > quarter) {                     // M's column sums: the decay once, in front of the products' operands, which have it each
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                const float4 h = *reinterpret_cast<const float4*>(sm.from + sub * 32 + j);
+                col = fmaf(v[j] * w[j], h.x, col);
+                col = fmaf(v[j + 1] * w[j + 1], h.y, col);
+                col = fmaf(v[j + 2] * w[j + 2], h.z, col);
+                col = fmaf(v[j + 3] * w[j + 3], h.w, col);
+            }
+        }
+        const float to_there = sub > quarter ? to_block(dec, row, sub) : 0.f;
+        col *= to_there * p.scale;
+        decay_column(v, w, dec.g + sub * 32, sub == quarter, lane, dec.g[row], to_there, p.scale, sm.from + sub * 32);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            packed_v[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+            packed_k[j] = pack16<T>(w[2 * j], w[2 * j + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            packed_v[j] = packed_k[j] = 0;
     }
     before_barrier();
-    asm volatile("bar.sync %0, 64;" :: "r"(1 + quarter) : "memory");
+    asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
     behind_barrier();
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        tmem_st16(scores + (half + 2 * i) * 16 + lanes, packed_v[i]);
-        tmem_st16(slopes + (half + 2 * i) * 16 + lanes, packed_k[i]);
+    tmem_st16(scores + sub * 16 + lanes, packed_v);
+    tmem_st16(slopes + sub * 16 + lanes, packed_k);
+    grad_products_done(sm.ctl, 1);
+    if (g.terms == 3) {
+        await(smem_u32(&sm.third_product), 0, &sm.ctl.dead);
+        __syncwarp();
+        behind_barrier();
     }
-    products_done(ctl, 1);
     const float f = to_end(dec, row) * (kIsBf16<T> ? 1.f : g.unit_Z[at]);
-    const float fj = weigh_row<T, DK>(dks + lanes, s_keys, row, half, f);
-    weigh_row<T, DV>(dvs + lanes, nullptr, row, half, f);
-    if (half == 1) {
-        s_f[row] = fj;
-        s_col[row] = col;
-    }
+    sm.dots[sub][row] = weigh_row<T, DK>(dks + lanes, s_keys, row, sub, f);
+    weigh_row<T, DV>(dvs + lanes, nullptr, row, sub, f);
+    sm.sums[sub][row] = col;
     tmem_st_done();
     before_barrier();
     __syncthreads();
@@ -450,38 +545,42 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
 #pragma unroll
             for (int s = 0; s < 8; ++s)
                 mma_tmem(dks, slopes + s * 8, over_tokens(queries, s), id_k, 1);
-            commit(smem_u32(&ctl.bar[2]));
+            commit(smem_u32(&sm.ctl.bar[2]));
         }
         __syncwarp();
     }
-    if (half == 0 && g.want_l) {
+    if (sub == 0 && g.want_l) {
         const long long plane = (long long)p.heads * p.chunks * kChunk;
         float* to = g.tokens + ((long long)head * p.chunks + ci) * kChunk + row;
-        to[2 * plane] = fj + s_f[row];
-        to[3 * plane] = col + s_col[row];
+        to[2 * plane] = (sm.dots[0][row] + sm.dots[1][row]) + (sm.dots[2][row] + sm.dots[3][row]);
+        to[3 * plane] = (sm.sums[0][row] + sm.sums[1][row]) + (sm.sums[2][row] + sm.sums[3][row]);
     }
-    products_done(ctl, 2);
+    grad_products_done(sm.ctl, 2);
+    // (results in float32 take the place of queries and keys; all tiles are done with)
     if (g.part_k)
-        part_row<DK>(dks + lanes, g.part_k + (packed_row(p, c, row) * p.heads + head) * p.dk, p.dk, row < c.len, half, 1.f);
+        stage_part<DK>(dks + lanes, smem, row, sub, 1.f);
     else if (g.dk.ptr)
-        stage_row<T, DK>(dks + lanes, s_keys, row, half, 1.f);
+        stage_row<T, DK>(dks + lanes, s_keys, row, sub, 1.f);
     if (g.dv.ptr)
-        stage_row<T, DV>(dvs + lanes, s_values, row, half, 1.f);
-    give_back(tmem, 512);
-    if (!g.part_k && g.dk.ptr)
-        store_tile<T, DK>(s_keys, g.dk, c, head, p.dk, g.vec_dk);
+        stage_row<T, DV>(dvs + lanes, s_values, row, sub, 1.f);
+    end_grad(sm.ctl, tmem);
+    if (g.part_k)
+        store_part<DK>(smem, g.part_k + (packed_row(p, c, 0) * p.heads + head) * p.dk, (long long)p.heads * p.dk, c.len, p.dk);
+    else if (g.dk.ptr)
+        store_tile<T, DK, kGradThreads>(s_keys, g.dk, c, head, p.dk, g.vec_dk);
     if (g.dv.ptr)
-        store_tile<T, DV>(s_values, g.dv, c, head, p.dv, g.vec_dv);
+        store_tile<T, DV, kGradThreads>(s_values, g.dv, c, head, p.dv, g.vec_dv);
 }
 
 // Both in one launch (blockIdx.z), whose last round of blocks is then half as long.
 template <typename T, int DK, int DV>
-__global__ void __launch_bounds__(kThreads, 1) grad_kernel(const GradDev g)
+__global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Maps there, const __grid_constant__ Maps back, const GradDev g)
 {
+    wait_for_previous();
     if (blockIdx.z == 0 && g.want_kv)
-        grad_kv<T, DK, DV>(g);
+        grad_kv<T, DK, DV>(g, there, back);
     else
-        grad_q<T, DK, DV>(g);
+        grad_q<T, DK, DV>(g, there, back);
 }
 
 // Sums of dq and dk over the heads of a group, one block per token row, in the order of the heads.
@@ -553,7 +652,11 @@ __global__ void __launch_bounds__(128) grad_decay_kernel(const GradDev g)
         float behind = (lane < 31 ? x : 0.f) + (lane % 8 < 7 ? z : 0.f), front = (lane ? y : 0.f) + (lane % 8 ? w : 0.f);
         const int block = lane / 8;
         const long long ch = ci * p.heads + head;
-        const float over = g.across[ch] + (block == 1 || block == 2 ? g.bridges[2 * ch + block - 1] : 0.f);
+        float over = lane < g.across_of ? g.across[ch * g.across_of + lane] : 0.f;
+#pragma unroll
+        for (int o = 16; o; o /= 2)
+            over += __shfl_xor_sync(0xffffffffu, over, o);
+        over += block == 1 || block == 2 ? g.bridges[2 * ch + block - 1] : 0.f;
         const float A = p.A[head];
 #pragma unroll
         for (int i = 3; i >= 0; --i) {
