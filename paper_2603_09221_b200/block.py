@@ -89,7 +89,7 @@ def _load():
 
 class _LongWay:
     """Stands in for the compiled module where it cannot be built: every call is marshalled here."""
-    conv_step = scan_step = linear = staticmethod(lambda *args: None)
+    conv_step = scan_step = linear = attention = norm = staticmethod(lambda *args: None)
 
 
 def _short_way(lib):
@@ -101,7 +101,10 @@ def _short_way(lib):
         step.bind(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
                     for k in ("ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_linear", "ttc_linear_workspace")),
                   _CONV_ARGS.size, _SCAN_ARGS.size, _LINEAR_ARGS.size)
-    except (ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:
+        step.bind_more(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
+                         for k in ("ttc_decay_attention", "ttc_decay_attention_workspace", "ttc_decay_attention_step", "ttc_block_norm")),
+                       _DECAY_ARGS.size, _NORM_ARGS.size)
+    except (AttributeError, ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:
         warnings.warn("single-token calls take the slower way through Python: %s" % e)
         return _LongWay
     return step
@@ -478,6 +481,12 @@ def decay_attention(q, k, v, A, delta=None, delta_bias=None, softplus=False, sca
     neighbouring heads share queries and keys); ``delta [.., heads]`` of the same type; ``A, delta_bias [heads]`` and ``state, state_out [batch, heads, dk, dv]``
     float32.  ``scale`` is ``dk ** -0.5`` by default.  ``state`` is S in front of the sequences (default: zero), ``state_out``
     receives the last ones and may be ``state``.  Returns ``y``, which may be ``v``."""
+    if stream is None:
+        if _step is None:
+            _load()
+        got = _step.attention(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, y, state_out, False)
+        if got is not None:
+            return got
     if y is None:
         y = _empty(v.shape, v.dtype, v, stream)
     record = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, y, state_out)[0]
@@ -493,6 +502,12 @@ def decay_attention(q, k, v, A, delta=None, delta_bias=None, softplus=False, sca
 
 def decay_attention_step(q, k, v, A, state, delta=None, delta_bias=None, softplus=False, scale=None, y=None, stream=None):
     """One token of each sequence, ``v [batch, heads, dv]``: as :func:`decay_attention`; ``state`` moves on in place."""
+    if stream is None:
+        if _step is None:
+            _load()
+        got = _step.attention(q, k, v, A, delta, delta_bias, softplus, scale, None, None, y, state, True)
+        if got is not None:
+            return got
     if y is None:
         y = _empty(v.shape, v.dtype, v, stream)
     record = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, None, None, y, state, step=True)[0]
@@ -663,6 +678,12 @@ def block_norm(x, w_post=None, z=None, scale=None, residual=None, w_pre=None, ep
 
     ``x, z, residual [.., channels]`` of one type; ``w_post, scale, w_pre [channels]`` float32.  Returns ``(h, y)``: ``h`` is ``x`` itself where
     nothing changes it (unless a tensor for it is handed in), ``y`` is None without ``w_pre``.  ``h`` and ``y`` may each be one of the inputs."""
+    if stream is None:
+        if _step is None:
+            _load()
+        got = _step.norm(x, w_post, z, scale, residual, w_pre, eps, groups, h, y)
+        if got is not None:
+            return got
     code, dtype, dev, d, rows, kept, px, pz, ldx, ldz, vectors = _norm_operands(x, w_post, z, scale, w_pre, groups, stream)
     if residual is not None and residual.shape != x.shape:
         _explain(residual, "residual", x.shape, dtype, dev)

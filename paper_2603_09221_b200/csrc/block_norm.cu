@@ -67,6 +67,7 @@ int check_overlap(const ttc_norm_args* a, const Operand& out, const Operand& in,
 
 struct Way {
     int v, k, threads, rows_per_block;
+    bool mixed;                                  // groups of channels whose sums go through shared memory
     size_t smem;
 };
 
@@ -78,12 +79,12 @@ int ceil_pow2(int v)
     return r;
 }
 
-// Vectors of 16 bytes where every row and parameter can be accessed so and no vector lies across two groups; else single elements.  Then as many
+// Vectors of 16 bytes where every row and parameter can be accessed so; else single elements.  Then as many
 // threads as give each at most `most` vectors, with more for rows that would need over 512 of them.
 Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> rows, int most)
 {
-    const int size = (int)element_size(a->dtype), v = 16 / size;
-    bool vec = a->d / a->groups % v == 0;
+    const int v = 16 / (int)element_size(a->dtype);
+    bool vec = a->d % v == 0;
     for (auto& o : rows)
         vec = vec && (!o.ptr || (reinterpret_cast<uintptr_t>(o.ptr) % 16 == 0 && (o.ld % v == 0 || a->rows <= 1)));
     for (const float* w : {a->w_post, a->scale, a->w_pre})
@@ -99,9 +100,10 @@ Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> ro
     o.threads = threads;
     o.k = k <= 1 ? 1 : k <= 2 ? 2 : k <= 4 ? 4 : 16;
     o.rows_per_block = threads == 32 ? kRowsOfWarps : 1;
-    const int lanes = a->d / a->groups / o.v;
-    p.lanes = lanes <= 32 && (lanes & (lanes - 1)) == 0 ? lanes : 0;
-    o.smem = a->groups > 1 && !p.lanes ? (size_t)o.rows_per_block * (vectors + a->groups) * sizeof(float) : 0;
+    const int size = a->d / a->groups, lanes = size / o.v;
+    p.lanes = lanes;
+    o.mixed = a->groups > 1 && (size % o.v || lanes > 32 || (lanes & (lanes - 1)));
+    o.smem = o.mixed ? (size_t)o.rows_per_block * (a->d + a->groups) * sizeof(float) : 0;
     return o;
 }
 
@@ -111,16 +113,17 @@ template <typename F> int by_way(int dtype, const Way& w, F&& f)
         constexpr int V = 16 / sizeof(t);
         constexpr std::integral_constant<int, V> wide;
         constexpr std::integral_constant<int, 1> single;
-        auto of = [&](auto v) {
+        auto of = [&](auto v, auto k) { return w.mixed ? f(t, v, k, std::true_type()) : f(t, v, k, std::false_type()); };
+        auto by_k = [&](auto v) {
             switch (w.k) {
-            case 1: return f(t, v, std::integral_constant<int, 1>());
-            case 2: return f(t, v, std::integral_constant<int, 2>());
-            default: return f(t, v, std::integral_constant<int, 4>());
+            case 1: return of(v, std::integral_constant<int, 1>());
+            case 2: return of(v, std::integral_constant<int, 2>());
+            default: return of(v, std::integral_constant<int, 4>());
             }
         };
         if (w.v > 1)
-            return of(wide);
-        return w.k == 16 ? f(t, single, std::integral_constant<int, 16>()) : of(single);
+            return by_k(wide);
+        return w.k == 16 ? of(single, std::integral_constant<int, 16>()) : by_k(single);
     });
 }
 
@@ -212,7 +215,11 @@ int plan_grad(int device, const ttc_norm_args* a, const ttc_norm_grads* g, void*
     p.dscale = g->dscale;
     p.dw_pre = g->dw_pre;
     o.w = way_of(a, p, {ins[0], ins[1], ins[2], ins[3], ins[4], outs[0], outs[1], outs[2]}, 1);
-    const int64_t most = (int64_t)sm_count(device) * (o.w.threads <= 512 ? 1024 / (o.w.threads * o.w.rows_per_block) : 1);
+    if (o.w.v > 1 && o.w.k == 1)
+        o.w.smem += (size_t)kAhead * 5 * o.w.threads * o.w.rows_per_block * 16;
+    // as many workers as are resident: 512 threads to an SM by their registers, 1024 where a thread has single elements
+    const int resident = (o.w.v > 1 ? 512 : 1024) / (o.w.threads * o.w.rows_per_block);
+    const int64_t most = (int64_t)sm_count(device) * (resident > 1 ? resident : 1);
     const int64_t all = (a->rows + o.w.rows_per_block - 1) / o.w.rows_per_block;
     o.blocks = (int)(all < most ? all : most);
     p.workers = o.blocks * o.w.rows_per_block;
@@ -250,8 +257,8 @@ int ttc_block_norm(int32_t device, const ttc_norm_args* a, void* cuda_stream)
     p.y = a->y, p.ldy = a->ldy;
     const Way w = way_of(a, p, {x, z, r, h, y}, 2);
     const dim3 grid((unsigned)((a->rows + w.rows_per_block - 1) / w.rows_per_block));
-    return by_way(a->dtype, w, [&](auto t, auto v, auto k) {
-        return launch("block norm", norm_kernel<decltype(t), decltype(v)::value, decltype(k)::value>, grid, w, sm_count(device), static_cast<cudaStream_t>(cuda_stream), p);
+    return by_way(a->dtype, w, [&](auto t, auto v, auto k, auto m) {
+        return launch("block norm", norm_kernel<decltype(t), decltype(v)::value, decltype(k)::value, decltype(m)::value>, grid, w, sm_count(device), static_cast<cudaStream_t>(cuda_stream), p);
     });
 }
 
@@ -272,8 +279,8 @@ int ttc_block_norm_grad(int32_t device, const ttc_norm_args* a, const ttc_norm_g
     const NormDev& p = o.p;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (o.blocks)
-        TTC_TRY(by_way(a->dtype, o.w, [&](auto t, auto v, auto k) {
-            return launch("gradients of the block norm", norm_grad_kernel<decltype(t), decltype(v)::value, decltype(k)::value>, dim3(o.blocks), o.w, sm_count(device), st, p);
+        TTC_TRY(by_way(a->dtype, o.w, [&](auto t, auto v, auto k, auto m) {
+            return launch("gradients of the block norm", norm_grad_kernel<decltype(t), decltype(v)::value, decltype(k)::value, decltype(m)::value>, dim3(o.blocks), o.w, sm_count(device), st, p);
         }));
     if (p.dw_post || p.dscale || p.dw_pre)
         TTC_TRY((launch_early("gradients of the block norm, parameters", norm_sum_kernel, dim3((unsigned)((a->d + 31) / 32), 3), 256, 0, 1, st, p)));

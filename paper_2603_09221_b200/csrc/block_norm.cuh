@@ -22,6 +22,7 @@ namespace bnorm {
 using namespace blk;
 
 constexpr int kRowsOfWarps = 4;                  // rows of a block in which a row is one warp's
+constexpr int kAhead = 3;                        // rows whose operands are on their way, gradients
 
 struct NormDev {
     long long rows;
@@ -38,7 +39,7 @@ struct NormDev {
     int plain;                                   // h is x
 };
 
-extern __shared__ float bnorm_smem[];
+extern __shared__ __align__(16) float bnorm_smem[];
 
 // Sums of N values over the threads of a row.  `buffer` [2][32 N]: two take turns, so that one barrier is enough.
 template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* buffer, int& turn)
@@ -67,72 +68,74 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
     }
 }
 
-// Sums over the groups of channels, of N values for each of a thread's K vectors.  Where a group is a few neighbouring threads, among them; else
-// through shared memory, group by group.
-template <int N, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, float (&v)[K][N], float* buffer, int& turn)
+// Sums over the groups of channels: in, the values of a thread's K vectors, one for each element; out, the sum of the element's group.  MIXED: groups that vectors lie across, or of
+// more than a warp's vectors, through shared memory, group by group.  Else all elements of a vector have the same sum, and only the first is set: a group is the row, or a few
+// neighbouring threads.
+template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, float (&v)[K][V], float* area, float* buffer, int& turn)
 {
-    if (p.groups == 1) {
-        float all[N];
+    if constexpr (MIXED) {
+        const int warps = blockDim.x / 32;
+        float* s = area + threadIdx.y * (p.d + p.groups);
+        float* sums = s + p.d;
+        __syncthreads();                         // earlier sums have been read
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            all[i] = 0.f;
+        for (int k = 0; k < K; ++k) {
+            const int at = (k * blockDim.x + threadIdx.x) * V;
+            if (at < p.d)
 #pragma unroll
-            for (int k = 0; k < K; ++k)
-                all[i] += v[k][i];
+                for (int j = 0; j < V; ++j)
+                    s[at + j] = v[k][j];
         }
-        row_sums<N>(all, buffer, turn);
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[k][i] = all[i];
-        return;
-    }
-    if (p.lanes) {
-#pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-#pragma unroll
-                for (int o = 1; o < 32; o *= 2)
-                    if (o < p.lanes)
-                        v[k][i] += __shfl_xor_sync(0xffffffffu, v[k][i], o);
-        return;
-    }
-    // one area for each row of the block: [N][vectors], then [N][groups]
-    const int vectors = p.d / V, each = vectors + p.groups, warps = blockDim.x / 32, per_group = p.size / V;
-    float* s = bnorm_smem + threadIdx.y * N * each;
-    float* sums = s + N * vectors;
-    __syncthreads();                             // earlier sums have been read
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int at = k * blockDim.x + threadIdx.x;
-        if (at < vectors)
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                s[i * vectors + at] = v[k][i];
-    }
-    __syncthreads();
-    for (int g = threadIdx.x / 32; g < p.groups; g += warps)
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
+        __syncthreads();
+        for (int g = threadIdx.x / 32; g < p.groups; g += warps) {
             float sum = 0.f;
-            for (int j = threadIdx.x % 32; j < per_group; j += 32)
-                sum += s[i * vectors + g * per_group + j];
+            for (int j = threadIdx.x % 32; j < p.size; j += 32)
+                sum += s[g * p.size + j];
 #pragma unroll
             for (int o = 16; o; o /= 2)
                 sum += __shfl_xor_sync(0xffffffffu, sum, o);
             if (threadIdx.x % 32 == 0)
-                sums[i * p.groups + g] = sum;
+                sums[g] = sum;
         }
-    __syncthreads();
+        __syncthreads();
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-        const int at = k * blockDim.x + threadIdx.x;
-        if (at < vectors)
+        for (int k = 0; k < K; ++k) {
+            const int at = (k * blockDim.x + threadIdx.x) * V;
+            if (at < p.d) {
+                int g = at / p.size, left = (g + 1) * p.size - at;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                v[k][i] = sums[i * p.groups + at / per_group];
+                for (int j = 0; j < V; ++j) {
+                    if (left == 0) {
+                        ++g;
+                        left = p.size;
+                    }
+                    v[k][j] = sums[g];
+                    --left;
+                }
+            }
+        }
+    } else {
+        float all[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+#pragma unroll
+            for (int j = 1; j < V; ++j)
+                v[k][0] += v[k][j];
+            all[0] += v[k][0];
+        }
+        if (p.groups == 1) {
+            row_sums<1>(all, buffer, turn);
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                v[k][0] = all[0];
+        } else {
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2)
+                    if (o < p.lanes)
+                        v[k][0] += __shfl_xor_sync(0xffffffffu, v[k][0], o);
+        }
     }
 }
 
@@ -175,7 +178,7 @@ template <int V> __device__ __forceinline__ void keep(float* to, const float (&f
 }
 
 // K vectors of V elements to a thread; blockDim.x threads to a row, blockDim.y rows to a block (more than one only where a row is a warp's).
-template <typename T, int V, int K>
+template <typename T, int V, int K, bool MIXED>
 __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev p)
 {
     __shared__ float buffer[2 * 32];
@@ -202,23 +205,23 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev 
     for (int k = 0; k < K; ++k)
         widen(x[k], u[k]);
     if (p.w_post) {
-        float sum[K][1];
+        float sum[K][V];
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            sum[k][0] = 0.f;
+        for (int k = 0; k < K; ++k)
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                sum[k][0] = fmaf(u[k][j], u[k][j], sum[k][0]);
-        }
-        group_sums_of<1, K, V>(p, sum, buffer, turn);
+                sum[k][j] = u[k][j] * u[k][j];
+        group_sums_of<MIXED, K, V>(p, sum, bnorm_smem, buffer, turn);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            const float rms = rsqrtf(fmaf(sum[k][0], p.per_group, p.eps));
             float w[V];
             params(p.w_post, c[k], true, w);
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                u[k][j] *= rms * w[j];
+                sum[k][j] = MIXED || j == 0 ? rsqrtf(fmaf(sum[k][j], p.per_group, p.eps)) : sum[k][0];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                u[k][j] *= sum[k][j] * w[j];
         }
     }
     if (p.z) {
@@ -271,9 +274,13 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev 
 }
 
 // Workers (a block, or a warp of one) take every workers-th row and keep their shares of the parameters' gradients in registers.
-template <typename T, int V, int K>
+//
+// Where a thread has one vector of each operand of a row, copies of the next rows' vectors into its own places of shared memory are under way (kAhead rows; no other thread looks at
+// them), so that memory is at work while the sums of a row are waited for.
+template <typename T, int V, int K, bool MIXED>
 __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const NormDev p)
 {
+    constexpr bool RING = K == 1 && V > 1;
     __shared__ float buffer[2 * 32 * 2];
     wait_for_previous();
     const int worker = blockIdx.x * blockDim.y + threadIdx.y, vectors = p.d / V;
@@ -291,19 +298,54 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
             s_post[k][j] = s_scale[k][j] = s_pre[k][j] = 0.f;
     }
     const long long rounds = (p.rows + p.workers - 1) / p.workers;               // the same number for all rows of a block: they share barriers
+    const int threads = blockDim.x * blockDim.y;
+    uint4* ring = reinterpret_cast<uint4*>(bnorm_smem) + threadIdx.y * blockDim.x + threadIdx.x;
+    float* area = bnorm_smem + (RING ? kAhead * 5 * threads * 4 : 0);
+    auto ask = [&](long long round) {            // (vectors of nothing where an operand is missing or the row lies behind the last)
+        const long long row = round * p.workers + worker;
+        const bool ok = in[0] && row < p.rows;
+        auto copy = [&](int i, const void* ptr, long long ld, bool there) {
+            const bool have = ok && there;
+            const T* from = have ? static_cast<const T*>(ptr) + row * ld + c[0] : static_cast<const T*>(p.x);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(ring + ((round % kAhead) * 5 + i) * threads)), "l"(from),
+                         "r"(have ? 16 : 0) : "memory");
+        };
+        copy(0, p.x, p.ldx, true);
+        copy(1, p.z, p.ldz, p.z);
+        copy(2, p.h_in, p.ldh, p.w_pre);
+        copy(3, p.dy, p.lddy, p.w_pre);
+        copy(4, p.dh, p.lddh, p.dh);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if constexpr (RING) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            ask(i);
+    }
     for (long long round = 0; round < rounds; ++round) {
         const long long row = round * p.workers + worker;
         const bool here = row < p.rows;
         const long long lead = here ? row : 0;
         Vec<T, V> x[K], z[K], h[K], dy[K], dh[K];
+        if constexpr (RING) {
+            asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
+            const uint4* from = ring + (round % kAhead) * 5 * threads;
+            x[0] = *reinterpret_cast<const Vec<T, V>*>(from);
+            z[0] = *reinterpret_cast<const Vec<T, V>*>(from + threads);
+            h[0] = *reinterpret_cast<const Vec<T, V>*>(from + 2 * threads);
+            dy[0] = *reinterpret_cast<const Vec<T, V>*>(from + 3 * threads);
+            dh[0] = *reinterpret_cast<const Vec<T, V>*>(from + 4 * threads);
+            ask(round + kAhead);
+        } else {
 #pragma unroll
-        for (int k = 0; k < K; ++k) {
-            const bool ok = in[k] && here;
-            x[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.x) + lead * p.ldx + c[k]), ok);
-            z[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.z) + lead * p.ldz + c[k]), ok && p.z);
-            h[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.h_in) + lead * p.ldh + c[k]), ok && p.w_pre);
-            dy[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dy) + lead * p.lddy + c[k]), ok && p.w_pre);
-            dh[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dh) + lead * p.lddh + c[k]), ok && p.dh);
+            for (int k = 0; k < K; ++k) {
+                const bool ok = in[k] && here;
+                x[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.x) + lead * p.ldx + c[k]), ok);
+                z[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.z) + lead * p.ldz + c[k]), ok && p.z);
+                h[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.h_in) + lead * p.ldh + c[k]), ok && p.w_pre);
+                dy[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dy) + lead * p.lddy + c[k]), ok && p.w_pre);
+                dh[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dh) + lead * p.lddh + c[k]), ok && p.dh);
+            }
         }
         float g[K][V];
 #pragma unroll
@@ -344,22 +386,22 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                 if (in[k] && here)
                     store<T, V>(static_cast<T*>(p.dr) + row * p.lddr + c[k], g[k]);
         }
-        float inverse[K];
+        float inverse[K][V];
         if (p.w_post) {
-            float sum[K][1];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float a[V];
                 widen(x[k], a);
-                sum[k][0] = 0.f;
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    sum[k][0] = fmaf(a[j], a[j], sum[k][0]);
+                    inverse[k][j] = a[j] * a[j];
             }
-            group_sums_of<1, K, V>(p, sum, buffer, turn);
+            group_sums_of<MIXED, K, V>(p, inverse, area, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                inverse[k] = rsqrtf(fmaf(sum[k][0], p.per_group, p.eps));
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    inverse[k][j] = MIXED || j == 0 ? rsqrtf(fmaf(inverse[k][j], p.per_group, p.eps)) : inverse[k][0];
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
@@ -373,7 +415,7 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                 widen(z[k], slope);
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                u[j] = p.w_post ? a[j] * inverse[k] * u[j] : a[j];
+                u[j] = p.w_post ? a[j] * inverse[k][j] * u[j] : a[j];
                 gate[j] = 1.f;
                 if (p.z) {
                     const float f = slope[j], q = sigmoid(f);
@@ -393,29 +435,29 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                 store<T, V>(static_cast<T*>(p.dz) + row * p.lddz + c[k], slope);
         }
         if (p.w_post) {
-            float sum[K][1];
+            float sum[K][V];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float a[V], w[V];
                 widen(x[k], a);
                 params(p.w_post, c[k], true, w);
-                sum[k][0] = 0.f;
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    s_post[k][j] = fmaf(g[k][j], a[j] * inverse[k], s_post[k][j]);
+                    s_post[k][j] = fmaf(g[k][j], a[j] * inverse[k][j], s_post[k][j]);
                     g[k][j] *= w[j];
-                    sum[k][0] = fmaf(a[j], g[k][j], sum[k][0]);
+                    sum[k][j] = a[j] * g[k][j];
                 }
             }
-            group_sums_of<1, K, V>(p, sum, buffer, turn);
+            group_sums_of<MIXED, K, V>(p, sum, area, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 float a[V];
                 widen(x[k], a);
-                const float mean = sum[k][0] * p.per_group * inverse[k] * inverse[k];
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    g[k][j] = inverse[k] * fmaf(-a[j], mean, g[k][j]);
+                for (int j = 0; j < V; ++j) {
+                    const float mean = sum[k][MIXED ? j : 0] * p.per_group * inverse[k][j] * inverse[k][j];
+                    g[k][j] = inverse[k][j] * fmaf(-a[j], mean, g[k][j]);
+                }
             }
         }
         if (p.dx) {
@@ -425,6 +467,8 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                     store<T, V>(static_cast<T*>(p.dx) + row * p.lddx + c[k], g[k]);
         }
     }
+    if constexpr (RING)
+        asm volatile("cp.async.wait_all;" ::: "memory");
     if (p.parts) {
         float* to = p.parts + (long long)worker * 3 * p.d;
 #pragma unroll

@@ -1,5 +1,5 @@
 // Short way into the calls of block.py whose kernels take less time than Python takes to describe their arguments: a single
-// token's convolution and scan, and the projections.  Each function checks what block.py checks and, where everything is in its ordinary
+// token's convolution, scan and linear attention, linear attention itself, the norms and the projections.  Each function checks what block.py checks and, where everything is in its ordinary
 // place (the arguments' types, shapes, contiguity, one CUDA device, the current stream), fills the record, makes the call and
 // returns the output; otherwise it returns None and block.py goes its own way, which also says what is wrong.
 #define PY_SSIZE_T_CLEAN
@@ -9,6 +9,8 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+
 #include "../../include/ttc_block.h"
 
 namespace {
@@ -17,6 +19,10 @@ decltype(&ttc_causal_conv_step) conv_step_call;
 decltype(&ttc_selective_scan_step) scan_step_call;
 decltype(&ttc_linear) linear_call;
 decltype(&ttc_linear_workspace) linear_workspace_call;
+decltype(&ttc_decay_attention) attention_call;
+decltype(&ttc_decay_attention_workspace) attention_workspace_call;
+decltype(&ttc_decay_attention_step) attention_step_call;
+decltype(&ttc_block_norm) norm_call;
 
 // A tensor argument: absent (None), present, or something else.
 struct Arg {
@@ -68,6 +74,19 @@ bool shared_rows(const at::Tensor& t, int64_t batch, int64_t groups, int64_t n, 
     if (k == 2 ? groups != 1 : t.size(1) != groups || (groups > 1 && t.stride(1) != n))
         return false;
     r = ttc_rows{t.data_ptr(), t.stride(0), 0};
+    return true;
+}
+
+// rows of heads [lead..][heads][width], the heads one behind the other; `lead` is the number of dimensions in front (2: batch and tokens)
+bool head_rows(const at::Tensor& t, const at::Tensor& like, int lead, int64_t heads, int64_t width, bool packed, ttc_rows& r)
+{
+    if (!here(t, like.scalar_type(), like.device()) || t.dim() != lead + 2 || t.size(lead) != heads || t.size(lead + 1) != width ||
+        (width > 1 && t.stride(lead + 1) != 1) || (heads > 1 && t.stride(lead) != width))
+        return false;
+    for (int i = 0; i < lead; ++i)
+        if (t.size(i) != like.size(i))
+            return false;
+    r = lead == 2 ? ttc_rows{t.data_ptr(), t.stride(0), t.stride(1)} : packed ? ttc_rows{t.data_ptr(), 0, t.stride(0)} : ttc_rows{t.data_ptr(), t.stride(0), 0};
     return true;
 }
 
@@ -232,6 +251,169 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t count)
     }
 }
 
+// (q, k, v, A, delta, delta_bias, softplus, scale or None, state, offsets, y, state_out, step)
+PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 13 || !attention_call)
+        Py_RETURN_NONE;
+    try {
+        const Arg q(args[0]), k(args[1]), v(args[2]), A(args[3]), delta(args[4]), bias(args[5]), state(args[8]), offsets(args[9]), y_arg(args[10]), state_out(args[11]);
+        const int softplus = PyObject_IsTrue(args[6]), step = PyObject_IsTrue(args[12]);
+        if (!q.t || !k.t || !v.t || !A.t || !delta.ok || !bias.ok || !state.ok || !offsets.ok || !y_arg.ok || !state_out.ok || softplus < 0 || step < 0 || (bias.t && !delta.t))
+            return PyErr_Clear(), Py_NewRef(Py_None);
+        const at::Tensor& vt = *v.t;
+        const auto type = vt.scalar_type();
+        const auto device = vt.device();
+        const bool packed = offsets.t;
+        const int lead = step || packed ? 1 : 2;
+        if (!vt.is_cuda() || (type != at::kBFloat16 && type != at::kHalf) || vt.dim() != lead + 2 || q.t->dim() != lead + 2 || (step && packed))
+            Py_RETURN_NONE;
+        const int64_t heads = vt.size(lead), dv = vt.size(lead + 1), groups = q.t->size(lead), dk = q.t->size(lead + 1);
+        int64_t batch = vt.size(0);
+        const int64_t tokens = step ? 1 : packed ? vt.size(0) : vt.size(1);
+        if (packed) {
+            if (!here(*offsets.t, at::kInt, device) || offsets.t->dim() != 1 || offsets.t->size(0) < 1 || !offsets.t->is_contiguous())
+                Py_RETURN_NONE;
+            batch = offsets.t->size(0) - 1;
+        }
+        ttc_decay_args a = {};
+        if (batch == 0 || tokens == 0 || heads >= INT32_MAX || groups >= INT32_MAX || dk < 1 || dk > 128 || dv > 128 || !dense(A, {heads}, at::kFloat, device) ||
+            !dense(bias, {heads}, at::kFloat, device) || !dense(state, {batch, heads, dk, dv}, at::kFloat, device) ||
+            !dense(state_out, {batch, heads, dk, dv}, at::kFloat, device) || !head_rows(*q.t, vt, lead, groups, dk, packed, a.q) ||
+            !head_rows(*k.t, vt, lead, groups, dk, packed, a.k) || !head_rows(vt, vt, lead, heads, dv, packed, a.v))
+            Py_RETURN_NONE;
+        if (delta.t) {                           // [lead..][heads]
+            const at::Tensor& t = *delta.t;
+            if (!here(t, type, device) || t.dim() != lead + 1 || t.size(lead) != heads || (heads > 1 && t.stride(lead) != 1) || t.size(0) != vt.size(0) ||
+                (lead == 2 && t.size(1) != vt.size(1)))
+                Py_RETURN_NONE;
+            a.delta = lead == 2 ? ttc_rows{t.data_ptr(), t.stride(0), t.stride(1)} : packed ? ttc_rows{t.data_ptr(), 0, t.stride(0)} : ttc_rows{t.data_ptr(), t.stride(0), 0};
+        }
+        double scale = 1.0 / std::sqrt((double)dk);
+        if (args[7] != Py_None) {
+            scale = PyFloat_AsDouble(args[7]);
+            if (PyErr_Occurred())
+                return PyErr_Clear(), Py_NewRef(Py_None);
+        }
+        at::Tensor y;
+        if (y_arg.t) {
+            if (!head_rows(*y_arg.t, vt, lead, heads, dv, packed, a.y))
+                Py_RETURN_NONE;
+        } else {
+            y = at::empty(vt.sizes(), vt.options());
+            head_rows(y, vt, lead, heads, dv, packed, a.y);
+        }
+        a.batch = batch;
+        a.tokens = tokens;
+        a.seq_offsets = packed ? static_cast<const int32_t*>(offsets.ptr()) : nullptr;
+        a.heads = (int32_t)heads;
+        a.groups = (int32_t)groups;
+        a.dk = (int32_t)dk;
+        a.dv = (int32_t)dv;
+        a.dtype = type_code(type);
+        a.softplus = softplus;
+        a.scale = (float)scale;
+        a.A = static_cast<const float*>(A.ptr());
+        a.delta_bias = static_cast<const float*>(bias.ptr());
+        a.state = static_cast<const float*>(state.ptr());
+        a.state_out = static_cast<float*>(state_out.ptr());
+        void* stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
+        if (step) {
+            if (attention_step_call(device.index(), &a, stream) != TTC_OK)
+                Py_RETURN_NONE;
+            return give(args[10], y);
+        }
+        const int64_t need = attention_workspace_call(device.index(), &a);
+        if (need < 0)
+            Py_RETURN_NONE;
+        at::Tensor ws;
+        if (need > 0)
+            ws = at::empty({need}, vt.options().dtype(at::kByte));
+        if (attention_call(device.index(), &a, need ? ws.data_ptr() : nullptr, need, stream) != TTC_OK)
+            Py_RETURN_NONE;
+        return give(args[10], y);
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
+// rows of d channels with one stride, whatever their leading dimensions (contiguous ones are taken together), or none
+bool flat_rows(const Arg& a, const at::Tensor& like, const void*& ptr, int64_t& ld)
+{
+    ptr = nullptr, ld = 0;
+    if (!a.ok || !a.t)
+        return a.ok;
+    const at::Tensor& t = *a.t;
+    if (!here(t, like.scalar_type(), like.device()) || t.sizes() != like.sizes())
+        return false;
+    const int64_t d = t.size(t.dim() - 1);
+    if (t.is_contiguous())
+        ld = d;
+    else if (t.dim() == 2 && (d <= 1 || t.stride(1) == 1) && t.stride(0) >= d)
+        ld = t.stride(0);
+    else
+        return false;
+    ptr = t.data_ptr();
+    return true;
+}
+
+// (x, w_post, z, scale, residual, w_pre, eps, groups, h, y): the pair (h, y)
+PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 10 || !norm_call)
+        Py_RETURN_NONE;
+    try {
+        const Arg x(args[0]), w_post(args[1]), z(args[2]), scale(args[3]), residual(args[4]), w_pre(args[5]), h_arg(args[8]), y_arg(args[9]);
+        const double eps = PyFloat_AsDouble(args[6]);
+        const long groups = PyErr_Occurred() ? -1 : PyLong_AsLong(args[7]);
+        if (PyErr_Occurred() || !x.t || !z.ok || !residual.ok || !h_arg.ok || !y_arg.ok || groups < 1 || groups >= INT32_MAX)
+            return PyErr_Clear(), Py_NewRef(Py_None);
+        const at::Tensor& xt = *x.t;
+        const bool changed = w_post.t || z.t || scale.t || residual.t;
+        if (!xt.is_cuda() || xt.dim() < 1 || type_code(xt.scalar_type()) < 0 || xt.numel() == 0 || (!changed && !w_pre.t) || (y_arg.t && !w_pre.t))
+            Py_RETURN_NONE;
+        const int64_t d = xt.size(xt.dim() - 1);
+        const auto device = xt.device();
+        ttc_norm_args a = {};
+        const void *h_ptr, *y_ptr;
+        if (d >= INT32_MAX || !dense(w_post, {d}, at::kFloat, device) || !dense(scale, {d}, at::kFloat, device) || !dense(w_pre, {d}, at::kFloat, device) ||
+            !flat_rows(x, xt, a.x, a.ldx) || !flat_rows(z, xt, a.z, a.ldz) || !flat_rows(residual, xt, a.residual, a.ldr) || !flat_rows(h_arg, xt, h_ptr, a.ldh) ||
+            !flat_rows(y_arg, xt, y_ptr, a.ldy))
+            Py_RETURN_NONE;
+        at::Tensor h, y;
+        if (changed && !h_arg.t) {
+            h = at::empty(xt.sizes(), xt.options());
+            h_ptr = h.data_ptr(), a.ldh = d;
+        }
+        if (w_pre.t && !y_arg.t) {
+            y = at::empty(xt.sizes(), xt.options());
+            y_ptr = y.data_ptr(), a.ldy = d;
+        }
+        a.rows = xt.numel() / d;
+        a.d = (int32_t)d;
+        a.groups = (int32_t)groups;
+        a.dtype = type_code(xt.scalar_type());
+        a.eps = (float)eps;
+        a.h = const_cast<void*>(h_ptr);
+        a.y = const_cast<void*>(y_ptr);
+        a.w_post = static_cast<const float*>(w_post.ptr());
+        a.scale = static_cast<const float*>(scale.ptr());
+        a.w_pre = static_cast<const float*>(w_pre.ptr());
+        if (norm_call(device.index(), &a, c10::cuda::getCurrentCUDAStream(device.index()).stream()) != TTC_OK)
+            Py_RETURN_NONE;
+        PyObject* first = h_arg.t || changed ? give(args[8], h) : Py_NewRef(args[0]);
+        PyObject* second = w_pre.t ? give(args[9], y) : Py_NewRef(Py_None);
+        PyObject* both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
+        Py_XDECREF(first);
+        Py_XDECREF(second);
+        return both;
+    } catch (...) {
+        PyErr_Clear();
+        Py_RETURN_NONE;
+    }
+}
+
 // Addresses of the library's functions, in the order of the declarations above, and the sizes of the records that they take (a module
 // that was compiled with another header than the library must not fill them).
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
@@ -263,8 +445,38 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
     Py_RETURN_NONE;
 }
 
+// The same for linear attention and the norms.
+PyObject* bind_more(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 6) {
+        PyErr_SetString(PyExc_TypeError, "bind_more takes four addresses and two sizes");
+        return nullptr;
+    }
+    void* at[4];
+    for (int i = 0; i < 4; ++i) {
+        at[i] = PyLong_AsVoidPtr(args[i]);
+        if (PyErr_Occurred())
+            return nullptr;
+    }
+    const long sizes[2] = {(long)sizeof(ttc_decay_args), (long)sizeof(ttc_norm_args)};
+    for (int i = 0; i < 2; ++i) {
+        const long size = PyLong_AsLong(args[4 + i]);
+        if (PyErr_Occurred())
+            return nullptr;
+        if (size != sizes[i]) {
+            PyErr_Format(PyExc_ImportError, "_step.so was built for records of %ld bytes, not %ld: build it again", sizes[i], size);
+            return nullptr;
+        }
+    }
+    attention_call = reinterpret_cast<decltype(attention_call)>(at[0]);
+    attention_workspace_call = reinterpret_cast<decltype(attention_workspace_call)>(at[1]);
+    attention_step_call = reinterpret_cast<decltype(attention_step_call)>(at[2]);
+    norm_call = reinterpret_cast<decltype(norm_call)>(at[3]);
+    Py_RETURN_NONE;
+}
+
 #define TTC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TTC_METHOD(bind), TTC_METHOD(conv_step), TTC_METHOD(scan_step), TTC_METHOD(linear), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {TTC_METHOD(bind), TTC_METHOD(conv_step), TTC_METHOD(scan_step), TTC_METHOD(linear), TTC_METHOD(bind_more), TTC_METHOD(attention), TTC_METHOD(norm), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace
