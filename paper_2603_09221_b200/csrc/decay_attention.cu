@@ -172,8 +172,8 @@ int take_pieces(int device, const ttc_decay_args* a, int splits, int columns, At
             p.pieces = a->seq_offsets ? a->tokens / piece + a->batch : a->batch * p.pieces_per_seq;
         }
     }
-    if (p.pieces > INT32_MAX)
-        return fail(TTC_STATUS_UNSUPPORTED, "%lld pieces of sequences", (long long)p.pieces);
+    if (p.pieces > INT32_MAX / (2 * walks))      // blocks are counted in 32 bits
+        return fail(TTC_STATUS_UNSUPPORTED, "%lld pieces of sequences, %d heads", (long long)p.pieces, a->heads);
     if (p.piece < a->tokens) {
         for (int i = 0; i < ways; ++i) {
             q.way[i].piece_state = s.take<float>((size_t)p.pieces * a->heads * splits * kWalkThreads * (columns / 4));
@@ -207,11 +207,12 @@ template <typename K> int allow_smem(K* kernel, int bytes)
 template <typename T, int DK, int COLS> int piece_states(const Maps (&maps)[2], const AttnDev& p, States q, int ways, int splits, cudaStream_t st)
 {
     q.way[0].image = q.way[1].image = nullptr;
-    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)(splits * ways));
+    q.ways = ways;
+    const dim3 grid((unsigned)(p.pieces * p.heads * splits * ways));
     constexpr int smem = StateShape<T, DK, COLS>::SMEM;
     TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
     TTC_TRY((launch_early("decay attention, what the pieces add", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[1], p, q, splits)));
-    return launch_early("decay attention, states of the pieces", join_kernel, dim3(grid.x, grid.y, grid.z * (COLS / 16)), kWalkThreads, 0, 1, st, p, q, COLS / 4, splits);
+    return launch_early("decay attention, states of the pieces", join_kernel, dim3((unsigned)p.pieces, (unsigned)p.heads, (unsigned)(splits * ways * (COLS / 16))), kWalkThreads, 0, 1, st, p, q, COLS / 4, splits);
 }
 
 // The states in front of all chunks, then the gradients of those behind them.
@@ -223,9 +224,11 @@ template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], 
         TTC_TRY((piece_states<T, DK, COLS>(maps, p, q, 2, splits, st)));
     constexpr int smem = StateShape<T, DK, COLS>::SMEM;
     TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
-    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)splits);
-    TTC_TRY((launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[0], p, q, splits)));
-    States back = q;
+    const dim3 grid((unsigned)(p.pieces * p.heads * splits));
+    States there = q;
+    there.ways = 1;
+    TTC_TRY((launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[0], p, there, splits)));
+    States back = there;
     back.way[0] = q.way[1];
     return launch_early("decay attention, gradients of states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[1], maps[1], p, back, splits);
 }
@@ -296,8 +299,8 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     States& q = o.q;
     q = States{};
     TTC_TRY(take_pieces(device, a, o.splits, padded(a->dv) / o.splits, p.f, q, 2, s));
-    if (p.f.chunks > INT32_MAX)
-        return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks", (long long)p.f.chunks);
+    if (p.f.chunks > INT32_MAX / (2 * a->heads))
+        return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks, %d heads", (long long)p.f.chunks, a->heads);
     if (packed) {
         p.f.piece_map = s.take<int2>(p.f.chunks);
         p.f.seq_first = s.take<int>(a->batch + 1);
@@ -380,7 +383,7 @@ int ttc_decay_attention(int32_t device, const ttc_decay_args* a, void* workspace
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (p.pieces == 0)
         return TTC_OK;
-    const dim3 grid((unsigned)p.pieces, (unsigned)p.heads, (unsigned)o.splits);
+    const dim3 grid((unsigned)(p.pieces * p.heads * o.splits));
     Maps maps[2] = {};
     TTC_TRY(describe_all(p, &p.q, p.vec_q, p.k, p.vec_k, p.v, p.vec_v, a->dtype == TTC_BF16, maps[0]));
     auto go = [&](auto t, auto kc) {
@@ -460,11 +463,12 @@ int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_
         if (f.chunks && (p.want_q || p.want_kv)) {
             constexpr int smem = GradShape<DK, DV>::SMEM;
             TTC_TRY((allow_smem(grad_kernel<T, DK, DV>, smem)));
-            TTC_TRY((launch_early("gradients of decay attention", grad_kernel<T, DK, DV>, dim3((unsigned)f.chunks, (unsigned)f.heads, p.want_q && p.want_kv ? 2 : 1), kGradThreads, smem,
+            TTC_TRY((launch_early("gradients of decay attention", grad_kernel<T, DK, DV>, dim3((unsigned)(f.chunks * f.heads * (p.want_q && p.want_kv ? 2 : 1))), kGradThreads, smem,
                                   1, st, maps[0], maps[1], p)));
         }
         if (f.chunks && (p.part_q || p.part_k))
-            TTC_TRY((launch_early("gradients of decay attention, groups", grad_group_kernel<T>, dim3((unsigned)f.chunks, 16), kThreads, 0, 1, st, p)));
+            TTC_TRY((launch_early("gradients of decay attention, groups", a->dk % 4 ? grad_group_kernel<T, 1> : grad_group_kernel<T, 4>, dim3((unsigned)f.chunks, 8, 2), kThreads, 0, 1,
+                                  st, p)));
         if (p.want_l) {
             if (f.chunks)
                 TTC_TRY((launch_early("gradients of decay attention, decays", grad_decay_kernel<T>, dim3((unsigned)f.chunks, (unsigned)((f.heads + 3) / 4)), 128, 0, 1, st, p)));

@@ -392,6 +392,17 @@ struct Piece {
     bool first, last;                            // of its sequence
 };
 
+// What a block of a walk works for: pieces one after the other, the heads and columns of each together.
+struct Place {
+    long long piece;
+    int head, part;                              // part of `parts`: columns, or the way
+};
+__device__ __forceinline__ Place place_of(const AttnDev& p, int parts)
+{
+    const unsigned id = blockIdx.x, each = p.heads * parts;
+    return Place{id / each, (int)(id % each / parts), (int)(id % parts)};
+}
+
 // Piece i, found by a whole warp: of packed sequences, which have one piece at least, by going along their lengths 32 at a time.  (`first_of_sequence`: number of its sequence's
 // first piece.)  Offsets that decrease leave lengths of nothing.
 __device__ __forceinline__ Piece piece_at(const AttnDev& p, long long i, long long* first_of_sequence = nullptr)
@@ -399,6 +410,22 @@ __device__ __forceinline__ Piece piece_at(const AttnDev& p, long long i, long lo
     Piece r = {0, 0, -1, 0, 0, false, false};
     if (p.seqs.offsets) {
         const int lane = threadIdx.x % 32;
+        if (p.pieces == p.seqs.batch && p.seqs.batch <= 32) {
+            // uncut: the longest first, so that no long one is left for the end (7 sequences of 4093 tokens, 32 walks each: 60 -> 35 us)
+            const Span s = lane < p.seqs.batch ? span_of(p.seqs, lane) : Span{0, -1};
+            int rank = 0;
+#pragma unroll
+            for (int o = 0; o < 32; ++o) {
+                const long long v = __shfl_sync(0xffffffffu, s.len, o);
+                rank += v > s.len || (v == s.len && o < lane);
+            }
+            const int at = __ffs(__ballot_sync(0xffffffffu, rank == i)) - 1;
+            r.owner = at;
+            r.row0 = __shfl_sync(0xffffffffu, s.row0, at);
+            r.len = __shfl_sync(0xffffffffu, s.len, at);
+            r.first = r.last = true;
+            return r;
+        }
         long long base = 0;
         for (long long b0 = 0; b0 < p.seqs.batch; b0 += 32) {
             const long long b = b0 + lane;
@@ -595,11 +622,13 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
     constexpr int TERMS = S_::TERMS;
     char* smem = dattn_tiles;
     Small& sm = *reinterpret_cast<Small*>(smem + S_::TILES);
-    const int head = blockIdx.y, group = head / p.share, col0 = blockIdx.z * kCols;
+    const int splits = (p.dv + kCols - 1) / kCols;
+    const Place where = place_of(p, splits);
+    const int head = where.head, group = head / p.share, col0 = where.part * kCols;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int cols = min(kCols, p.dv - col0);
     wait_for_previous();
-    const Piece piece = piece_at(p, blockIdx.x);
+    const Piece piece = piece_at(p, where.piece);
     if (piece.owner < 0)
         return;
     const int n = __shfl_sync(0xffffffffu, (int)((piece.len + kChunk - 1) / kChunk), 0);
@@ -801,7 +830,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
     } else {                                     // ---- everything else
         const int quarter = warp % 4, sub = warp / 4, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const long long place = (((long long)blockIdx.x * p.heads + head) * gridDim.z + blockIdx.z) * (kWalkThreads * 16);
+        const long long place = ((where.piece * p.heads + head) * splits + where.part) * (kWalkThreads * 16);
         float S[16];
         if (!piece.first) {
 #pragma unroll
@@ -1004,6 +1033,7 @@ struct StateDev {
 // Walks of one launch: one along the sequences, or one each way.
 struct States {
     StateDev way[2];
+    int ways;
     const int* seq_first;                        // packed sequences: the first chunk of each
 };
 
@@ -1016,15 +1046,17 @@ template <typename T, int DK, int COLS> struct StateShape {
         float whole;
     };
     struct Small {
-        uint64_t loaded[2], freed[2], weighted, added, drained;
+        uint64_t loaded[2], freed[2], weighted[2], added[2], drained;                // of chunks in turn
         uint32_t tmem;
         int dead;
         Weights dec[2];
         float most[32];
     };
-    static constexpr int TILES = 2 * STAGE + TERMS * V_BYTES;
+    // weighted values of two chunks, where there is room, and their products: the next ones are made while a chunk's products run
+    static constexpr int TURNS = 2 * STAGE + 2 * TERMS * V_BYTES <= 225 * 1024 ? 2 : 1;
+    static constexpr int TILES = 2 * STAGE + TURNS * TERMS * V_BYTES;
     static constexpr int SMEM = TILES + sizeof(Small);
-    static constexpr int COLUMNS = TERMS * COLS > 256 ? 512 : 256;
+    static constexpr int COLUMNS = TURNS * TERMS * COLS > 256 ? 512 : 256;
 };
 static_assert(StateShape<bf16, 128, 128>::SMEM <= 232448, "shared memory of a block");
 
@@ -1034,20 +1066,21 @@ template <typename T, int DK, int COLS>
 __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_constant__ Maps maps_there, const __grid_constant__ Maps maps_back, const AttnDev p, const States states,
                                                                    int splits)
 {
-    const StateDev& q = states.way[blockIdx.z / splits];
-    const Maps& maps = blockIdx.z / splits ? maps_back : maps_there;
-    const int z = blockIdx.z % splits;
+    const Place where = place_of(p, splits * states.ways);
+    const StateDev& q = states.way[where.part / splits];
+    const Maps& maps = where.part / splits ? maps_back : maps_there;
+    const int z = where.part % splits;
     const bool BACK = q.back;
     using S_ = StateShape<T, DK, COLS>;
     using Small = typename S_::Small;
     constexpr int TERMS = S_::TERMS, OWN = COLS / 4;
     char* smem = dattn_tiles;
     Small& sm = *reinterpret_cast<Small*>(smem + S_::TILES);
-    const int head = blockIdx.y, group = head / p.share, col0 = z * COLS;
+    const int head = where.head, group = head / p.share, col0 = z * COLS;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32;
     const int cols = min(COLS, p.dv - col0);
     wait_for_previous();
-    const Piece piece = piece_at(p, blockIdx.x);
+    const Piece piece = piece_at(p, where.piece);
     if (piece.owner < 0 || (!q.image && (BACK ? piece.first : piece.last)))
         return;
     const int n = __shfl_sync(0xffffffffu, (int)((piece.len + kChunk - 1) / kChunk), 0);
@@ -1056,8 +1089,10 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
         for (int i = 0; i < 2; ++i) {
             init(sm.loaded[i], 32 * kFrontWarps);
             init(sm.freed[i], kWalkWarps);
+            init(sm.weighted[i], kWalkWarps);
+            init(sm.added[i], 1);
         }
-        init(sm.added, 1), init(sm.drained, 1), init(sm.weighted, kWalkWarps);
+        init(sm.drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         sm.dead = 0;
     }
@@ -1167,19 +1202,20 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
         }
     } else if (warp == kWalkWarps) {             // ---- products
         for (int i = 0; i < n; ++i) {
-            until(sm.weighted, i);
+            until(sm.weighted[i & 1], i / 2);
             behind_barrier();
             constexpr int N = TERMS * COLS < 256 ? TERMS * COLS : 256, REST = TERMS * COLS - N;
             constexpr uint32_t id = instruction(kIsBf16<T>, true, true, 128, N);
-            const uint64_t a = over_tokens(keys_at(i), 0), b = over_tokens(weighted, 0);
+            const uint64_t a = over_tokens(keys_at(i), 0), b = over_tokens(weighted + i % S_::TURNS * (TERMS * S_::V_BYTES), 0);
+            const uint32_t to = tmem + i % S_::TURNS * (TERMS * COLS);
             if (elect_one()) {
 #pragma unroll
                 for (int s = 0; s < 8; ++s) {
-                    mma(tmem, a + (s * 2048 >> 4), b + (s * 2048 >> 4), id, s > 0);
+                    mma(to, a + (s * 2048 >> 4), b + (s * 2048 >> 4), id, s > 0);
                     if constexpr (REST > 0)
-                        mma(tmem + N, a + (s * 2048 >> 4), b + (N / 64 * kBox + s * 2048 >> 4), instruction(kIsBf16<T>, true, true, 128, REST), s > 0);
+                        mma(to + N, a + (s * 2048 >> 4), b + (N / 64 * kBox + s * 2048 >> 4), instruction(kIsBf16<T>, true, true, 128, REST), s > 0);
                 }
-                commit(smem_u32(&sm.added));
+                commit(smem_u32(&sm.added[i & 1]));
             }
             __syncwarp();
         }
@@ -1193,7 +1229,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
         const int quarter = warp % 4, sub = warp / 4, row = quarter * 32 + lane;
         const bool mine = quarter * 32 < DK;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        const long long place = (((long long)blockIdx.x * p.heads + head) * splits + z) * (kWalkThreads * OWN);
+        const long long place = ((where.piece * p.heads + head) * splits + z) * (kWalkThreads * OWN);
         const long long first = q.image ? (p.seqs.offsets ? states.seq_first[piece.owner] : piece.owner * p.chunks_per_seq) + piece.t0 / kChunk : 0;
         float S[OWN];
         if (q.image && !(BACK ? piece.last : piece.first)) {
@@ -1204,10 +1240,53 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             load_state(S, p, q.image ? q.given : nullptr, piece.owner, head, row, col0 + sub * OWN);
         }
         float whole = 1.f;
-        for (int i = 0; i < n; ++i) {
+        float unit_of[2] = {1.f, 1.f};
+        // values times their weights, split
+        auto put_values = [&](int i) {
             const typename S_::Weights& dec = sm.dec[i & 1];
             until(sm.loaded[i & 1], i / 2);
             float unit_v = 1.f;
+            constexpr int VECTORS = COLS / 32;
+            float up = 1.f;
+            if (!kIsBf16<T>) {
+                float most = 0.f;
+#pragma unroll
+                for (int h = 0; h < VECTORS; ++h) {
+                    const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
+                    const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + tile_at(t, e % (COLS / 8)));
+                    float here = 0.f;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float2 x = unpack16<T>((&v.x)[j]);
+                        here = fmaxf(here, fmaxf(fabsf(x.x), fabsf(x.y)));
+                    }
+                    most = fmaxf(most, here * (dec.own[t] * dec.of_block[t / 32]));
+                }
+                up = power_for(walk_largest(most, sm.most), unit_v);
+            }
+#pragma unroll
+            for (int h = 0; h < VECTORS; ++h) {
+                const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
+                const uint32_t at = tile_at(t, e % (COLS / 8));
+                const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + at);
+                const float w = dec.own[t] * (dec.of_block[t / 32] * up);
+                uint4 term[TERMS];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    split_terms<T, TERMS>((&v.x)[j], w, [&](int n, uint32_t u) { (&term[n].x)[j] = u; });
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n)
+                    *reinterpret_cast<uint4*>(smem + (weighted - tiles) + (i % S_::TURNS * TERMS + n) * S_::V_BYTES + at) = term[n];
+            }
+            to_tensor_cores();
+            before_barrier();
+            warp_arrives(smem_u32(&sm.weighted[i & 1]));
+            unit_of[i & 1] = unit_v;
+        };
+        if (n > 0)
+            put_values(0);
+        for (int i = 0; i < n; ++i) {
+            const typename S_::Weights& dec = sm.dec[i & 1];
             uint4 other[OWN / 8][TERMS];         // asked for early
             const long long at = (first + chunk(i)) * p.heads + head;
             const long long place_of = at * ((long long)q.terms * q.image_bytes) + ((col0 + sub * OWN) / 8 * DK + row) * 16;
@@ -1218,43 +1297,6 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                     for (int t = 0; t < TERMS; ++t)
                         other[j][t] = load_if(reinterpret_cast<const uint4*>(q.other + place_of + j * DK * 16 + t * q.image_bytes), mine && t < q.terms);
             }
-            {                                    // values times their weights, split
-                constexpr int VECTORS = COLS / 32;
-                float up = 1.f;
-                if (!kIsBf16<T>) {
-                    float most = 0.f;
-#pragma unroll
-                    for (int h = 0; h < VECTORS; ++h) {
-                        const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
-                        const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + tile_at(t, e % (COLS / 8)));
-                        float here = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float2 x = unpack16<T>((&v.x)[j]);
-                            here = fmaxf(here, fmaxf(fabsf(x.x), fabsf(x.y)));
-                        }
-                        most = fmaxf(most, here * (dec.own[t] * dec.of_block[t / 32]));
-                    }
-                    up = power_for(walk_largest(most, sm.most), unit_v);
-                }
-#pragma unroll
-                for (int h = 0; h < VECTORS; ++h) {
-                    const int e = h * kWalkThreads + threadIdx.x, t = e / (COLS / 8);
-                    const uint32_t at = tile_at(t, e % (COLS / 8));
-                    const uint4 v = *reinterpret_cast<const uint4*>(smem + (values_at(i) - tiles) + at);
-                    const float w = dec.own[t] * (dec.of_block[t / 32] * up);
-                    uint4 term[TERMS];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        split_terms<T, TERMS>((&v.x)[j], w, [&](int n, uint32_t u) { (&term[n].x)[j] = u; });
-#pragma unroll
-                    for (int n = 0; n < TERMS; ++n)
-                        *reinterpret_cast<uint4*>(smem + (weighted - tiles) + n * S_::V_BYTES + at) = term[n];
-                }
-            }
-            to_tensor_cores();
-            before_barrier();
-            warp_arrives(smem_u32(&sm.weighted));
             const float over = dec.whole;
             if (q.image) {                       // the state in front of the chunk, while the products run
                 float up = 1.f;
@@ -1310,17 +1352,21 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                         q.across[(at * splits + z) * kWalkWarps + warp] = dot * over * (kIsBf16<T> ? 1.f : q.other_unit[at]);
                 }
             }
-            until(sm.added, i);
+            if (S_::TURNS == 2 && i + 1 < n)
+                put_values(i + 1);
+            until(sm.added[i & 1], i / 2);
             behind_barrier();
+            const uint32_t from = tmem + i % S_::TURNS * (TERMS * COLS);
+            const float unit_v = kIsBf16<T> ? 1.f : i & 1 ? unit_of[1] : unit_of[0];
             if (mine) {
 #pragma unroll
                 for (int j = 0; j < OWN; j += 16) {
                     float u[16];
-                    tmem_ld16(tmem + (TERMS - 1) * COLS + sub * OWN + j + lanes, u);
+                    tmem_ld16(from + (TERMS - 1) * COLS + sub * OWN + j + lanes, u);
 #pragma unroll
                     for (int t = TERMS - 2; t >= 0; --t) {
                         float v[16];
-                        tmem_ld16(tmem + t * COLS + sub * OWN + j + lanes, v);
+                        tmem_ld16(from + t * COLS + sub * OWN + j + lanes, v);
 #pragma unroll
                         for (int k = 0; k < 16; ++k)
                             u[k] += v[k];
@@ -1333,6 +1379,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             whole *= over;
             before_barrier();
             warp_arrives(smem_u32(&sm.freed[i & 1]));
+            if (S_::TURNS == 1 && i + 1 < n)
+                put_values(i + 1);
         }
         if (q.image) {
             if (BACK ? piece.first : piece.last)
@@ -1344,7 +1392,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                     *reinterpret_cast<float4*>(q.piece_state + place + (j * kWalkThreads + threadIdx.x) * 4) = *reinterpret_cast<const float4*>(S + 4 * j);
             }
             if (threadIdx.x == 0 && z == 0)
-                q.piece_decay[blockIdx.x * (long long)p.heads + head] = whole;
+                q.piece_decay[where.piece * p.heads + head] = whole;
         }
     }
     before_barrier();

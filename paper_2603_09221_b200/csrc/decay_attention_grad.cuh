@@ -155,13 +155,14 @@ __device__ __forceinline__ void fetch_bytes_to_l2(const char* from, uint32_t byt
 // The tiles and the image of a chunk and head, and its decays.  What the block that will run behind this one needs is asked for into L2, so that memory is at work while this
 // one computes.
 template <typename T, int DK, int DV, bool KV>
-__device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& there, const Maps& back, const Chunk& c, typename GradShape<DK, DV>::Small& sm, uint32_t tiles)
+__device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& there, const Maps& back, const Chunk& c, long long at, int head, typename GradShape<DK, DV>::Small& sm,
+                                               uint32_t tiles)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    const int head = blockIdx.y, group = head / p.share, warp = threadIdx.x / 32;
+    const int group = head / p.share, warp = threadIdx.x / 32;
     const uint32_t queries = tiles, keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
-    const char* from = (KV ? g.image_Z : g.image_S) + ((long long)blockIdx.x * p.heads + head) * ((long long)g.terms * S::IMAGE);
+    const char* from = (KV ? g.image_Z : g.image_S) + at * ((long long)g.terms * S::IMAGE);
     float l = 0.f;
     if (warp < 4)
         l = log_decay_at<T>(p, c, head, threadIdx.x);
@@ -187,9 +188,9 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
             }
         }
         fetch_bytes(image, from, 2 * S::IMAGE, bar);
-        const long long next = blockIdx.x + (long long)gridDim.x * (blockIdx.y + (long long)gridDim.y * blockIdx.z) + g.resident;
-        const long long ci = next % gridDim.x, h = next / gridDim.x % gridDim.y, z = next / gridDim.x / gridDim.y;
-        if (engine && z < gridDim.z) {
+        const int ways = g.want_q && g.want_kv ? 2 : 1;
+        const long long next = (long long)blockIdx.x + g.resident, ci = next / ways % p.chunks, h = next / ways / p.chunks;
+        if (engine && next < gridDim.x) {
             const Chunk n = chunk_at(p, ci);
             if (n.len > 0) {
                 const int row0 = (int)n.row0, seq = (int)n.seq;
@@ -201,7 +202,7 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
                     fetch_to_l2(&there.k, b * 64, (int)h / p.share, row0, seq);
                     fetch_to_l2(&back.k, b * 64, (int)h / p.share, row0, seq);
                 }
-                fetch_bytes_to_l2((z == 0 && g.want_kv ? g.image_Z : g.image_S) + (ci * p.heads + h) * ((long long)g.terms * S::IMAGE), g.terms * S::IMAGE);
+                fetch_bytes_to_l2((g.want_kv && (ways == 1 || next % 2 == 0) ? g.image_Z : g.image_S) + (ci * p.heads + h) * ((long long)g.terms * S::IMAGE), g.terms * S::IMAGE);
             }
         }
     }
@@ -254,8 +255,11 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
+    const int ways = g.want_q && g.want_kv ? 2 : 1;
+    const long long ci = blockIdx.x / ways % p.chunks;
+    const int head = (int)(blockIdx.x / ways / p.chunks);
+    const long long at = ci * p.heads + head;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
         return;
@@ -264,7 +268,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
     const Decays& dec = sm.dec;
     const uint32_t queries = __shfl_sync(0xffffffffu, smem_u32(smem), 0), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES,
                    image = dys + S::V_BYTES;
-    const uint32_t tmem = begin_grad<T, DK, DV, false>(g, there, back, c, sm, queries);        // scores, dy v', results: 128 columns each
+    const uint32_t tmem = begin_grad<T, DK, DV, false>(g, there, back, c, at, head, sm, queries);        // scores, dy v', results: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, results = tmem + 256, lanes = (uint32_t)(quarter * 32) << 16;
     if (warp == 0) {
         constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_state = instruction(kIsBf16<T>, false, false, 128, DK);
@@ -427,8 +431,11 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    const long long ci = blockIdx.x, at = ci * p.heads + blockIdx.y;
-    const int head = blockIdx.y, warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
+    const int ways = g.want_q && g.want_kv ? 2 : 1;
+    const long long ci = blockIdx.x / ways % p.chunks;
+    const int head = (int)(blockIdx.x / ways / p.chunks);
+    const long long at = ci * p.heads + head;
+    const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
         return;
@@ -439,7 +446,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
     char* s_values = s_keys + S::K_BYTES;
     const uint32_t queries = __shfl_sync(0xffffffffu, smem_u32(smem), 0), keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES,
                    image = dys + S::V_BYTES;
-    const uint32_t tmem = begin_grad<T, DK, DV, true>(g, there, back, c, sm, queries);         // scores, v dy', dk, dv: 128 columns each
+    const uint32_t tmem = begin_grad<T, DK, DV, true>(g, there, back, c, at, head, sm, queries);         // scores, v dy', dk, dv: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, dks = tmem + 256, dvs = tmem + 384, lanes = (uint32_t)(quarter * 32) << 16;
     if (warp == 0) {
         constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_k = instruction(kIsBf16<T>, false, false, 128, DK),
@@ -572,41 +579,43 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         store_tile<T, DV, kGradThreads>(s_values, g.dv, c, head, p.dv, g.vec_dv);
 }
 
-// Both in one launch (blockIdx.z), whose last round of blocks is then half as long.
+// Both in one launch, side by side: the second one finds the tiles in L2.
 template <typename T, int DK, int DV>
 __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Maps there, const __grid_constant__ Maps back, const GradDev g)
 {
     wait_for_previous();
-    if (blockIdx.z == 0 && g.want_kv)
+    if (g.want_kv && !(g.want_q && blockIdx.x % 2))
         grad_kv<T, DK, DV>(g, there, back);
     else
         grad_q<T, DK, DV>(g, there, back);
 }
 
-// Sums of dq and dk over the heads of a group, one block per token row, in the order of the heads.
-template <typename T>
+// Sums of dq and dk over the heads of a group, in the order of the heads; V channels to a thread.
+template <typename T, int V>
 __global__ void __launch_bounds__(kThreads) grad_group_kernel(const GradDev g)
 {
     wait_for_previous();
     const AttnDev& p = g.f;
     const Chunk c = chunk_at(p, blockIdx.x);
-    const int n = p.heads / p.share * p.dk;
-    for (int t = blockIdx.y; t < c.len; t += gridDim.y) {
-        const long long row = packed_row(p, c, t) * p.heads * p.dk;
-        for (int i = threadIdx.x; i < n; i += kThreads) {
-            const long long from = row + (long long)(i / p.dk) * p.share * p.dk + i % p.dk;
-            float q = 0.f, k = 0.f;
-            for (int h = 0; h < p.share; ++h) {
-                if (g.part_q)
-                    q += g.part_q[from + (long long)h * p.dk];
-                if (g.part_k)
-                    k += g.part_k[from + (long long)h * p.dk];
-            }
-            if (g.part_q)
-                row_ptr<T>(g.dq, c.seq, c.row0 + t)[i] = from_f<T>(q);
-            if (g.part_k)
-                row_ptr<T>(g.dk, c.seq, c.row0 + t)[i] = from_f<T>(k);
+    const int each = p.dk / V, n = p.heads / p.share * each;
+    const float* part = blockIdx.z ? g.part_k : g.part_q;
+    if (!part)
+        return;
+    for (int e = blockIdx.y * kThreads + threadIdx.x; e < c.len * n; e += gridDim.y * kThreads) {
+        const int t = e / n, i = e % n;
+        const float* from = part + packed_row(p, c, t) * p.heads * p.dk + (long long)(i / each) * p.share * p.dk + i % each * V;
+        float sum[V] = {};
+#pragma unroll 4
+        for (int h = 0; h < p.share; ++h) {
+            const Vec<float, V> v = *reinterpret_cast<const Vec<float, V>*>(from + (long long)h * p.dk);
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                sum[j] += v.v[j];
         }
+        T* to = row_ptr<T>(blockIdx.z ? g.dk : g.dq, c.seq, c.row0 + t) + (long long)(i / each) * p.dk + i % each * V;
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            to[j] = from_f<T>(sum[j]);
     }
 }
 
