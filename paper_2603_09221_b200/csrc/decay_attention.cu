@@ -215,8 +215,8 @@ template <typename T, int DK, int COLS> int piece_states(const Maps (&maps)[2], 
     return launch_early("decay attention, states of the pieces", join_kernel, dim3((unsigned)p.pieces, (unsigned)p.heads, (unsigned)(splits * ways * (COLS / 16))), kWalkThreads, 0, 1, st, p, q, COLS / 4, splits);
 }
 
-// The states in front of all chunks, then the gradients of those behind them.
-template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], const AttnDev& p, const States& q, int splits, cudaStream_t st)
+// The states in front of all chunks, and the gradients of those behind them, side by side or one after the other.
+template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], const AttnDev& p, const States& q, int splits, bool together, cudaStream_t st)
 {
     if (p.pieces == 0)
         return TTC_OK;
@@ -224,19 +224,24 @@ template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], 
         TTC_TRY((piece_states<T, DK, COLS>(maps, p, q, 2, splits, st)));
     constexpr int smem = StateShape<T, DK, COLS>::SMEM;
     TTC_TRY((allow_smem(state_walk_kernel<T, DK, COLS>, smem)));
-    const dim3 grid((unsigned)(p.pieces * p.heads * splits));
+    const unsigned walks = (unsigned)(p.pieces * p.heads * splits);
     States there = q;
+    if (together) {
+        there.ways = 2;
+        return launch_early("decay attention, states and their gradients", state_walk_kernel<T, DK, COLS>, dim3(2 * walks), kWalkBlock, smem, 1, st, maps[0], maps[1], p, there, splits);
+    }
     there.ways = 1;
-    TTC_TRY((launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[0], maps[0], p, there, splits)));
+    TTC_TRY((launch_early("decay attention, states", state_walk_kernel<T, DK, COLS>, dim3(walks), kWalkBlock, smem, 1, st, maps[0], maps[0], p, there, splits)));
     States back = there;
     back.way[0] = q.way[1];
-    return launch_early("decay attention, gradients of states", state_walk_kernel<T, DK, COLS>, grid, kWalkBlock, smem, 1, st, maps[1], maps[1], p, back, splits);
+    return launch_early("decay attention, gradients of states", state_walk_kernel<T, DK, COLS>, dim3(walks), kWalkBlock, smem, 1, st, maps[1], maps[1], p, back, splits);
 }
 
 struct GradPlan {
     GradDev g;
     States q;
     int splits;
+    bool together;
     size_t bytes;
 };
 
@@ -299,6 +304,9 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     States& q = o.q;
     q = States{};
     TTC_TRY(take_pieces(device, a, o.splits, padded(a->dv) / o.splits, p.f, q, 2, s));
+    // Walks both ways side by side, where one way leaves SMs idle (of packed sequences, the shorter ones'): <Z, S_0> takes a kernel of its own then, which reads
+    // both images again (11 documents of 8191 tokens, 8 heads of 64 x 64: 187 -> 150 us; 4 x 1024 tokens, 16 heads of 128 x 128, whose walks fill the SMs: 159, side by side 170).
+    o.together = 2 * p.f.pieces * a->heads * o.splits <= (packed ? 3 : 2) * sm_count(device) / 2;
     if (p.f.chunks > INT32_MAX / (2 * a->heads))
         return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks, %d heads", (long long)p.f.chunks, a->heads);
     if (packed) {
@@ -331,11 +339,15 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     q.way[0].image_bytes = q.way[1].image_bytes = padded(a->dk) * padded(a->dv) * 2;
     if (p.want_l) {
         p.tokens = s.take<float>(5 * each * kChunk);
-        p.across_of = o.splits * kWalkWarps;
+        p.across_of = o.together ? 1 : o.splits * kWalkWarps;
         p.across = s.take<float>(each * p.across_of);
-        q.way[1].other = p.image_S;
-        q.way[1].other_unit = p.unit_S;
-        q.way[1].across = p.across;
+        if (o.together) {
+            p.whole = q.way[0].whole = s.take<float>(each);
+        } else {
+            q.way[1].other = p.image_S;
+            q.way[1].other_unit = p.unit_S;
+            q.way[1].across = p.across;
+        }
         p.bridges = s.take<float>(2 * each);
         p.sums = s.take<float>(2 * each);
     }
@@ -459,7 +471,7 @@ int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_
         using T = decltype(t);
         constexpr int DK = decltype(kc)::value, DV = decltype(vc)::value;
         constexpr int COLS = std::is_same<T, bf16>::value ? kCols : DV;
-        TTC_TRY((chunk_states<T, DK, COLS>(maps, f, o.q, o.splits, st)));
+        TTC_TRY((chunk_states<T, DK, COLS>(maps, f, o.q, o.splits, o.together, st)));
         if (f.chunks && (p.want_q || p.want_kv)) {
             constexpr int smem = GradShape<DK, DV>::SMEM;
             TTC_TRY((allow_smem(grad_kernel<T, DK, DV>, smem)));
@@ -470,6 +482,8 @@ int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_
             TTC_TRY((launch_early("gradients of decay attention, groups", a->dk % 4 ? grad_group_kernel<T, 1> : grad_group_kernel<T, 4>, dim3((unsigned)f.chunks, 8, 2), kThreads, 0, 1,
                                   st, p)));
         if (p.want_l) {
+            if (f.chunks && o.together)
+                TTC_TRY((launch_early("gradients of decay attention, across chunks", grad_across_kernel<T>, dim3((unsigned)(f.chunks * f.heads)), kThreads, 0, 1, st, p, DK * DV * 2)));
             if (f.chunks)
                 TTC_TRY((launch_early("gradients of decay attention, decays", grad_decay_kernel<T>, dim3((unsigned)f.chunks, (unsigned)((f.heads + 3) / 4)), 128, 0, 1, st, p)));
             if (p.dA || p.dbias)

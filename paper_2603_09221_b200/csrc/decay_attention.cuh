@@ -1029,6 +1029,7 @@ struct StateDev {
     const char* other;
     const float* other_unit;
     float* across;
+    float* whole;                                // or exp(G_C) alone, for a kernel of its own, [chunks][heads]
 };
 // Walks of one launch: one along the sequences, or one each way.
 struct States {
@@ -1132,6 +1133,20 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             const bool engine = maps.there && (!p.seqs.offsets || c.len == kChunk);
             const uint32_t bar = smem_u32(&sm.loaded[i & 1]);
             bool arrived = false;
+            float sum[4 / kFrontWarps], own[4 / kFrontWarps];
+            auto find = [&]() {
+#pragma unroll
+                for (int b = 0; b < 4 / kFrontWarps; ++b) {
+                    const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
+                    float behind;
+                    sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind);
+                    own[b] = ex2(BACK ? sum[b] : behind);
+                }
+                if (i + 1 < n)
+                    ask(i + 1);
+            };
+            if (i >= 2)                          // while there is no room for the tiles
+                find();
             until(sm.freed[i & 1], i / 2 + 1);
             if (engine) {
                 if (warp == kWalkWarps + 1) {
@@ -1162,19 +1177,16 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                 load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), q.k, c, group * p.dk, p.dk, q.vec_k, thread);
                 copies_begun();
             }
+            if (i < 2)
+                find();
             typename S_::Weights& dec = sm.dec[i & 1];
 #pragma unroll
             for (int b = 0; b < 4 / kFrontWarps; ++b) {
                 const int t = b * 32 * kFrontWarps + thread;
-                const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
-                float behind;
-                const float sum = block_sums(t < c.len ? l : 0.f, behind);
-                dec.own[t] = ex2(BACK ? sum : behind);
+                dec.own[t] = own[b];
                 if (lane == 31)
-                    dec.block[t / 32] = sum;
+                    dec.block[t / 32] = sum[b];
             }
-            if (i + 1 < n)
-                ask(i + 1);
             asm volatile("bar.sync 2, %0;" :: "n"(32 * kFrontWarps) : "memory");
             if (thread < 5) {
                 const float b0 = dec.block[0], b1 = dec.block[1], b2 = dec.block[2], b3 = dec.block[3];
@@ -1331,6 +1343,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                                 *reinterpret_cast<uint4*>(to + t * q.image_bytes) = term[t];
                     }
                 }
+                if (q.whole && threadIdx.x == 0 && z == 0)
+                    q.whole[at] = over;
                 if (q.other) {
                     float dot = 0.f;
 #pragma unroll

@@ -38,6 +38,7 @@ struct GradDev {
     float* bridges;                              // [chunks][heads][2]: of pairs on both sides of the second and the third block
     float* across;                               // exp(G_C) <Z, S_0>: shares, [chunks][heads][across_of]
     int across_of;
+    float* whole;                                // exp(G_C), [chunks][heads], where <Z, S_0> has a kernel of its own
     float* sums;                                 // of dA and of ddelta_bias: [2][heads][chunks]
     int want_q, want_kv, want_l;
     int resident;                                // blocks that run at once
@@ -588,6 +589,50 @@ __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_cons
         grad_kv<T, DK, DV>(g, there, back);
     else
         grad_q<T, DK, DV>(g, there, back);
+}
+
+// exp(G_C) <Z, S_0> of each chunk and head from the images of both, where the walks ran side by side.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) grad_across_kernel(const GradDev g, int image_bytes)
+{
+    wait_for_previous();
+    __shared__ float s_sum[8];
+    const AttnDev& p = g.f;
+    const long long at = blockIdx.x;
+    if (chunk_at(p, at / p.heads).len <= 0)
+        return;
+    const uint4* S = reinterpret_cast<const uint4*>(g.image_S + at * ((long long)g.terms * image_bytes));
+    const uint4* Z = reinterpret_cast<const uint4*>(g.image_Z + at * ((long long)g.terms * image_bytes));
+    float dot = 0.f;
+#pragma unroll 2
+    for (int i = threadIdx.x; i < image_bytes / 16; i += kThreads) {
+        float a[8] = {}, b[8] = {};
+#pragma unroll
+        for (int t = 2; t >= 0; --t) {
+            const uint4 x = load_if(S + t * (image_bytes / 16) + i, t < g.terms), y = load_if(Z + t * (image_bytes / 16) + i, t < g.terms);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 u = unpack16<T>((&x.x)[j]), v = unpack16<T>((&y.x)[j]);
+                a[2 * j] += u.x, a[2 * j + 1] += u.y;
+                b[2 * j] += v.x, b[2 * j + 1] += v.y;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            dot = fmaf(a[j], b[j], dot);
+    }
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    if (threadIdx.x % 32 == 0)
+        s_sum[threadIdx.x / 32] = dot;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        dot = 0.f;
+        for (int i = 0; i < 8; ++i)
+            dot += s_sum[i];
+        g.across[at] = dot * g.whole[at] * (kIsBf16<T> ? 1.f : g.unit_S[at] * g.unit_Z[at]);
+    }
 }
 
 // Sums of dq and dk over the heads of a group, in the order of the heads; V channels to a thread.
