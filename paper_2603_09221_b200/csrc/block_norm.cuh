@@ -14,6 +14,8 @@
 // it (a warp, or a block of up to 1024), in vectors of 16 bytes, where its sums are formed in float32.
 #pragma once
 
+#include <type_traits>
+
 #include "block_common.cuh"
 
 namespace ttc {
@@ -45,27 +47,28 @@ extern __shared__ __align__(16) float bnorm_smem[];
 template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* buffer, int& turn)
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int o = 16; o; o /= 2)
 #pragma unroll
-        for (int o = 16; o; o /= 2)
+        for (int i = 0; i < N; ++i)
             v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     if (blockDim.x == 32)
         return;
     float* s = buffer + turn * 32 * N;
     turn ^= 1;
-    const int warps = blockDim.x / 32;
-    if (threadIdx.x % 32 == 0) {
+    const int warps = blockDim.x / 32, lane = threadIdx.x % 32;
+    if (lane == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            s[threadIdx.x / 32 * N + i] = v[i];
+            s[i * 32 + threadIdx.x / 32] = v[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = 0.f;
-        for (int w = 0; w < warps; ++w)
-            v[i] += s[w * N + i];
-    }
+    for (int i = 0; i < N; ++i)
+        v[i] = s[i * 32 + lane % warps];         // (a power of two)
+    for (int o = warps / 2; o; o /= 2)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
 // Sums over the groups of channels: in, the values of a thread's K vectors, one for each element; out, the sum of the element's group.  MIXED: groups that vectors lie across, or of
@@ -141,16 +144,39 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
 
 template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V>& a, float (&f)[V])
 {
+    if constexpr (std::is_same<T, bf16>::value && V % 2 == 0) {
+        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(&a);
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        f[j] = to_f(a.v[j]);
+        for (int j = 0; j < V; j += 2) {
+            f[j] = __uint_as_float(pairs[j / 2] << 16);
+            f[j + 1] = __uint_as_float(pairs[j / 2] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            f[j] = to_f(a.v[j]);
+    }
 }
 template <typename T, int V> __device__ __forceinline__ void store(T* to, const float (&f)[V])
 {
     Vec<T, V> u;
+    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
+        uint32_t* pairs = reinterpret_cast<uint32_t*>(&u);
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-        u.v[j] = from_f<T>(f[j]);
+        for (int j = 0; j < V; j += 2) {
+            if constexpr (std::is_same<T, bf16>::value) {
+                const __nv_bfloat162 r = __floats2bfloat162_rn(f[j], f[j + 1]);
+                pairs[j / 2] = *reinterpret_cast<const uint32_t*>(&r);
+            } else {
+                const __half2 r = __floats2half2_rn(f[j], f[j + 1]);
+                pairs[j / 2] = *reinterpret_cast<const uint32_t*>(&r);
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            u.v[j] = from_f<T>(f[j]);
+    }
     *reinterpret_cast<Vec<T, V>*>(to) = u;
 }
 // Parameters of a vector's channels.
@@ -301,14 +327,17 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
     const int threads = blockDim.x * blockDim.y;
     uint4* ring = reinterpret_cast<uint4*>(bnorm_smem) + threadIdx.y * blockDim.x + threadIdx.x;
     float* area = bnorm_smem + (RING ? kAhead * 5 * threads * 4 : 0);
+    int slot = 0;                                // of the ring
     auto ask = [&](long long round) {            // (vectors of nothing where an operand is missing or the row lies behind the last)
         const long long row = round * p.workers + worker;
         const bool ok = in[0] && row < p.rows;
+        const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring) + slot * (5 * 16 * threads);
         auto copy = [&](int i, const void* ptr, long long ld, bool there) {
+            if (!there && round >= kAhead)       // nothing is there already
+                return;
             const bool have = ok && there;
             const T* from = have ? static_cast<const T*>(ptr) + row * ld + c[0] : static_cast<const T*>(p.x);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"((uint32_t)__cvta_generic_to_shared(ring + ((round % kAhead) * 5 + i) * threads)), "l"(from),
-                         "r"(have ? 16 : 0) : "memory");
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" :: "r"(to + i * (16 * threads)), "l"(from), "r"(have ? 16 : 0) : "memory");
         };
         copy(0, p.x, p.ldx, true);
         copy(1, p.z, p.ldz, p.z);
@@ -319,8 +348,10 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
     };
     if constexpr (RING) {
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
+        for (int i = 0; i < kAhead; ++i) {
             ask(i);
+            slot = slot + 1 < kAhead ? slot + 1 : 0;
+        }
     }
     for (long long round = 0; round < rounds; ++round) {
         const long long row = round * p.workers + worker;
@@ -329,13 +360,14 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
         Vec<T, V> x[K], z[K], h[K], dy[K], dh[K];
         if constexpr (RING) {
             asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
-            const uint4* from = ring + (round % kAhead) * 5 * threads;
+            const uint4* from = ring + slot * 5 * threads;
             x[0] = *reinterpret_cast<const Vec<T, V>*>(from);
             z[0] = *reinterpret_cast<const Vec<T, V>*>(from + threads);
             h[0] = *reinterpret_cast<const Vec<T, V>*>(from + 2 * threads);
             dy[0] = *reinterpret_cast<const Vec<T, V>*>(from + 3 * threads);
             dh[0] = *reinterpret_cast<const Vec<T, V>*>(from + 4 * threads);
             ask(round + kAhead);
+            slot = slot + 1 < kAhead ? slot + 1 : 0;
         } else {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
