@@ -1051,7 +1051,7 @@ template <typename T, int DK, int COLS> struct StateShape {
         uint32_t tmem;
         int dead;
         Weights dec[2];
-        float most[32];
+        float most[3][kWalkWarps];               // of values of chunks in turn, of the state
     };
     // weighted values of two chunks, where there is room, and their products: the next ones are made while a chunk's products run
     static constexpr int TURNS = 2 * STAGE + 2 * TERMS * V_BYTES <= 225 * 1024 ? 2 : 1;
@@ -1274,7 +1274,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                     }
                     most = fmaxf(most, here * (dec.own[t] * dec.of_block[t / 32]));
                 }
-                up = power_for(walk_largest(most, sm.most), unit_v);
+                up = power_for(walk_largest(most, sm.most[i & 1]), unit_v);
             }
 #pragma unroll
             for (int h = 0; h < VECTORS; ++h) {
@@ -1317,7 +1317,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
 #pragma unroll
                     for (int j = 0; j < OWN; ++j)
                         most = fmaxf(most, fabsf(S[j]));
-                    up = power_for(walk_largest(mine ? most : 0.f, sm.most + kWalkWarps), unit);
+                    up = power_for(walk_largest(mine ? most : 0.f, sm.most[2]), unit);
                     if (threadIdx.x == 0)
                         q.unit[at] = unit;
                 }
@@ -1427,7 +1427,7 @@ static __global__ void __launch_bounds__(kWalkThreads) join_kernel(const AttnDev
     long long first = p.seqs.offsets ? 0 : blockIdx.x / p.pieces_per_seq * p.pieces_per_seq;
     const Piece piece = piece_at(p, blockIdx.x, &first);
     const int lane = threadIdx.x % 32, quarter = threadIdx.x / 32 % 4, sub = threadIdx.x / 128, row = quarter * 32 + lane;
-    if (piece.owner < 0 || !piece.last || piece.first || row >= p.dk)
+    if (piece.owner < 0 || !piece.last || piece.first || row >= (p.dk > 64 ? 128 : 64))        // (rows behind dk are zeros)
         return;
     const long long n = blockIdx.x - first + 1;
     float four[4];

@@ -1,0 +1,335 @@
+"""Linear attention with a decay for each head against its 64-bit form, token by token."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2603_09221_b200 import block
+from tests import attention_util as au
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+B, H, F = torch.bfloat16, torch.float16, torch.float32
+
+
+def _inputs(lead, batch, heads, groups, dk, dv, dtype, seed, decay="token", strength=1.0, state=True, offsets=None, grad=False):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    r = lambda *s, t=dtype, a=1.0: (torch.randn(s, generator=g, device=DEV) * a).to(t)  # noqa: E731
+    i = dict(q=r(*lead, groups, dk), k=r(*lead, groups, dk), v=r(*lead, heads, dv), A=-torch.rand(heads, generator=g, device=DEV) * strength - 1e-3,
+             delta=r(*lead, heads, a=0.5) if decay == "token" else None, delta_bias=r(heads, t=F, a=0.5) if decay == "token" else None,
+             softplus=decay == "token", state=r(batch, heads, dk, dv, t=F, a=0.3) if state else None,
+             offsets=torch.tensor(offsets, dtype=torch.int32, device=DEV) if offsets is not None else None)
+    if grad:
+        i.update(dy=r(*lead, heads, dv), dlast=r(batch, heads, dk, dv, t=F) if state else None)
+    return i
+
+
+def _flat(t, lead):
+    return None if t is None else au.f64(t).reshape(int(np.prod(lead)), *t.shape[len(lead):])
+
+
+def _args(i, lead, scale):
+    f = lambda n: _flat(i[n], lead)  # noqa: E731
+    seqs = au.spans(lead, i["offsets"].tolist() if i["offsets"] is not None else None)
+    return (f("q"), f("k"), f("v"), au.f64(i["A"]), f("delta"), au.f64(i["delta_bias"]), i["softplus"], scale, au.f64(i["state"]), seqs)
+
+
+def _bounds(i, args, lead):
+    heads, dk, dv = i["v"].shape[-2], i["q"].shape[-1], i["v"].shape[-1]
+    longest = max((hi - lo for lo, hi in args[-1]), default=0)
+    return au.roundings(dk, dv, longest, args[3], args[4], args[5], args[6], args[2].shape[0], heads) * au.U, -(-longest // au.CHUNK)
+
+
+def _call(i, scale=None, **kw):
+    return block.decay_attention(i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], i["softplus"], scale, i["state"], i["offsets"], **kw)
+
+
+def _check_forward(i, lead, scale=None, y=None, state_out=None):
+    s = i["q"].shape[-1] ** -0.5 if scale is None else scale
+    args = _args(i, lead, s)
+    want, last, _, _ = au.attend(*args)
+    mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
+    rel, _ = _bounds(i, args, lead)
+    batch = len(args[-1])
+    if state_out is None:
+        state_out = torch.full((batch, i["v"].shape[-2], i["q"].shape[-1], i["v"].shape[-1]), float("nan"), device=DEV)
+    if y is None:
+        y = torch.full_like(i["v"], float("nan"))
+    assert _call(i, scale, y=y, state_out=state_out) is y
+    inside = np.zeros(want.shape[0], bool)
+    for lo, hi in args[-1]:
+        inside[lo:hi] = True
+    got = y.reshape(want.shape)[torch.from_numpy(inside).to(DEV)]
+    au.within(got, want[inside], ((au.half_step(y.dtype) + rel) * mag)[inside], y.dtype, "y")
+    assert bool(torch.isnan(y.reshape(want.shape)[torch.from_numpy(~inside).to(DEV)]).all())           # rows of no sequence
+    au.within(state_out, last, rel * mag_last, F, "state_out")
+    assert block.device_error(0) == 0
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 31, 32, 33, 127, 128, 129, 257, 600])
+@pytest.mark.parametrize("dk, dv, dtype", [(64, 64, B), (128, 128, B), (128, 64, H), (64, 128, H), (16, 128, B)])
+def test_lengths(tokens, dk, dv, dtype):
+    lead = (2, tokens)
+    _check_forward(_inputs(lead, 2, 2, 1, dk, dv, dtype, tokens), lead)
+
+
+@pytest.mark.parametrize("dk, dv", [(1, 1), (7, 3), (8, 72), (36, 20), (72, 8), (65, 127), (127, 65), (100, 100)])
+@pytest.mark.parametrize("dtype", [B, H])
+def test_widths_of_heads(dk, dv, dtype):
+    lead = (2, 150)
+    _check_forward(_inputs(lead, 2, 3, 3, dk, dv, dtype, dk), lead)
+
+
+@pytest.mark.parametrize("heads, groups", [(1, 1), (6, 2), (8, 1), (4, 4)])
+@pytest.mark.parametrize("decay", ["token", "head"])
+def test_heads_and_decays(heads, groups, decay):
+    lead = (1, 200)
+    _check_forward(_inputs(lead, 1, heads, groups, 32, 48, B, heads, decay, state=False), lead, scale=-1.5)
+
+
+@pytest.mark.parametrize("offsets, rows", [([0, 0, 130, 130, 131, 400], 400), ([3, 60, 60, 64, 199], 210), ([0, 300], 300), ([5], 9), ([0, 1, 2, 3, 4], 4),
+                                           ([0] + [7 * i for i in range(1, 41)], 280)])
+@pytest.mark.parametrize("dk, dtype", [(64, B), (40, H), (20, B)])
+def test_packed_sequences_some_empty_and_rows_of_none(offsets, rows, dk, dtype):
+    _check_forward(_inputs((rows,), len(offsets) - 1, 4, 2, dk, 64, dtype, rows, offsets=offsets), (rows,))
+
+
+def test_few_heads_are_cut_into_pieces():
+    """One sequence of one head is walked along in as many pieces as there are SMs."""
+    lead = (1, 3000)
+    i = _inputs(lead, 1, 1, 1, 64, 32, B, 7, strength=0.05)
+    _check_forward(i, lead)
+    i["offsets"], flat = torch.tensor([0, 10, 10, 2600, 3000], dtype=torch.int32, device=DEV), {n: i[n][0] for n in ("q", "k", "v", "delta")}
+    i.update(flat, state=i["state"].expand(4, -1, -1, -1).contiguous())
+    _check_forward(i, (3000,))
+
+
+@pytest.mark.parametrize("strength", [0.0, 1e-3, 30.0, 1e4])
+def test_decays_from_none_to_all(strength):
+    lead = (2, 260)
+    i = _inputs(lead, 2, 2, 2, 32, 32, B, 9, strength=strength)
+    if strength == 0.0:
+        i["A"].zero_()
+    _check_forward(i, lead)
+
+
+@pytest.mark.parametrize("dtype", [B, H])
+def test_a_decay_of_minus_infinity_forgets_everything(dtype):
+    lead = (1, 300)
+    i = _inputs(lead, 1, 2, 1, 32, 64, dtype, 11, "head")
+    i["delta"] = torch.zeros((*lead, 2), device=DEV, dtype=dtype)
+    i["A"] = -torch.ones(2, device=DEV)
+    for t in (0, 5, 6, 130, 200, 299):
+        i["delta"][:, t, 1] = float("inf")
+    _check_forward(i, lead)
+
+
+def test_states_far_from_one_in_float16():
+    """What queries meet is held in 16 bits: it is taken times a power of two."""
+    lead = (1, 400)
+    for a in (3e4, 1e-4):
+        i = _inputs(lead, 1, 2, 2, 64, 96, H, 13, strength=1e-4)
+        i["state"] *= a
+        i["v"] = (i["v"].float() * min(a, 100.0)).to(H)
+        i["q"] = (i["q"].float() * min(1.0, 1 / a)).to(H)
+        lead_scale = 0.125
+        _check_forward(i, lead, scale=lead_scale)
+
+
+def test_slices_of_wider_rows_and_state_in_place():
+    g = torch.Generator(device=DEV).manual_seed(3)
+    for pad in (0, 8, 3):                                                           # aligned to 16 bytes, or not
+        wide = torch.randn((2, 140, 2 * 64 + 2 * 64 + 4 * 32 + 4 + pad), generator=g, device=DEV).to(B)
+        q, k, v, delta = wide[..., :128].unflatten(-1, (2, 64)), wide[..., 128:256].unflatten(-1, (2, 64)), wide[..., 256:384].unflatten(-1, (4, 32)), wide[..., 384:388]
+        i = dict(q=q, k=k, v=v, A=-torch.rand(4, generator=g, device=DEV), delta=delta, delta_bias=None, softplus=True, offsets=None,
+                 state=torch.randn((2, 4, 64, 32), generator=g, device=DEV))
+        args = _args(i, (2, 140), 0.125)
+        want, last, _, _ = au.attend(*args)
+        mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
+        rel, _ = _bounds(i, args, (2, 140))
+        before = wide.clone()
+        S = i["state"].clone()
+        i["state"] = S
+        y = _call(i, state_out=S, y=v if pad == 3 else None)                        # over v, and over the state
+        au.within(y.reshape(want.shape), want, (au.half_step(B) + rel) * mag, B, "y")
+        au.within(S, last, rel * mag_last, F, "state")
+        if pad == 3:
+            before[..., 256:384] = y.flatten(-2)
+        assert torch.equal(wide, before)
+
+
+def test_other_sequences_infinities_stay_there():
+    i = _inputs((300,), 3, 2, 2, 64, 64, B, 17, offsets=[0, 100, 180, 300])
+    clean = _call(i).clone()
+    for n in ("q", "k", "v"):
+        i[n][100:180] = float("nan")
+        i[n][140] = float("inf")
+    got = _call(i)
+    assert torch.equal(got[:100], clean[:100]) and torch.equal(got[180:], clean[180:])
+
+
+@pytest.mark.parametrize("dk, dv, dtype", [(64, 64, B), (128, 128, H), (36, 20, B), (7, 3, H), (100, 128, B)])
+@pytest.mark.parametrize("decay", ["token", "head"])
+def test_single_tokens(dk, dv, dtype, decay):
+    i = _inputs((3,), 3, 4, 2, dk, dv, dtype, 19, decay)
+    s = dk ** -0.5
+    f = lambda n: au.f64(i[n])  # noqa: E731
+    args = (f("q"), f("k"), f("v"), f("A"), f("delta"), f("delta_bias"), i["softplus"], s, f("state"), [(b, b + 1) for b in range(3)])
+    want, last, _, _ = au.attend(*args)
+    mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
+    S = i["state"].clone()
+    y = block.decay_attention_step(i["q"], i["k"], i["v"], i["A"], S, i["delta"], i["delta_bias"], i["softplus"])
+    R = dk + 8 * 200 + 16                                                           # exponents up to 200, one token: no 16-bit operands
+    au.within(y, want, R * au.U * mag, dtype, "y")
+    au.within(S, last, R * au.U * mag_last, F, "state")
+
+
+def test_a_prompt_is_its_tokens_one_by_one():
+    lead = (2, 40)
+    i = _inputs(lead, 2, 3, 1, 48, 64, B, 23)
+    S = i["state"].clone()
+    steps = [block.decay_attention_step(i["q"][:, t], i["k"][:, t], i["v"][:, t], i["A"], S, i["delta"][:, t], i["delta_bias"], True) for t in range(40)]
+    last = torch.empty_like(S)
+    y = _call(i, state_out=last)
+    args = _args(i, lead, 48 ** -0.5)
+    mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
+    rel, _ = _bounds(i, args, lead)
+    h = au.half_step(B)
+    off = np.abs(au.f64(y) - au.f64(torch.stack(steps, 1))).reshape(mag.shape)
+    assert (off <= (3 * h + 2 * rel) * mag).all()                                   # scores or states, and both results rounded
+    assert (np.abs(au.f64(last) - au.f64(S)) <= 2 * rel * mag_last).all()
+
+
+# ---- gradients ------------------------------------------------------------------------------------------------------------
+
+def _check_gradients(i, lead, scale=None, want=None, **kw):
+    s = i["q"].shape[-1] ** -0.5 if scale is None else scale
+    args = _args(i, lead, s)
+    dy, dlast = _flat(i["dy"], lead), au.f64(i["dlast"])
+    ref = au.attend_grad(dy, *args, dlast)
+    mag = au.attend_grad(dy, *args, dlast, magnitudes=True)
+    rel, chunks = _bounds(i, args, lead)
+    got = block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], i["softplus"], scale, i["state"], i["offsets"], i["dlast"],
+                                     want=want, **kw)
+    assert set(got) == set(want or ref)
+    inside = np.zeros(dy.shape[0], bool)
+    for lo, hi in args[-1]:
+        inside[lo:hi] = True
+    at = torch.from_numpy(inside).to(DEV)
+    h = au.half_step(i["q"].dtype)
+    for n in got:
+        if n in ("dq", "dk", "dv", "ddelta"):
+            t = got[n].reshape(ref[n].shape)[at]
+            au.within(t, ref[n][inside], ((0 if n == "ddelta" else h) + 2 * rel + 256 * au.U) * mag[n][inside], got[n].dtype, n)
+        else:
+            au.within(got[n], ref[n], (2 * rel + (256 + dy.shape[0]) * au.U) * mag[n], F, n)
+    assert block.device_error(0) == 0
+    return got
+
+
+@pytest.mark.parametrize("tokens", [1, 31, 33, 128, 129, 390])
+@pytest.mark.parametrize("dk, dv, dtype", [(64, 64, B), (128, 128, B), (128, 64, H), (64, 128, H), (128, 128, H)])
+def test_gradients_lengths(tokens, dk, dv, dtype):
+    lead = (2, tokens)
+    _check_gradients(_inputs(lead, 2, 2, 2, dk, dv, dtype, tokens + 1, grad=True), lead)
+
+
+@pytest.mark.parametrize("heads, groups, dk, dv, decay", [(6, 2, 36, 20, "token"), (4, 1, 7, 66, "token"), (3, 3, 72, 8, "head"), (4, 1, 128, 64, "head"), (8, 4, 64, 64, "token")])
+@pytest.mark.parametrize("dtype", [B, H])
+def test_gradients_of_shared_heads_and_odd_widths(heads, groups, dk, dv, decay, dtype):
+    lead = (2, 140)
+    _check_gradients(_inputs(lead, 2, heads, groups, dk, dv, dtype, dk, decay, grad=True), lead, scale=0.3)
+
+
+@pytest.mark.parametrize("offsets, rows", [([0, 0, 130, 130, 131, 400], 400), ([3, 60, 60, 64, 199], 210), ([0, 1, 2], 2)])
+@pytest.mark.parametrize("dk, dtype, groups", [(64, B, 2), (40, H, 4)])
+def test_gradients_of_packed_sequences(offsets, rows, dk, dtype, groups):
+    _check_gradients(_inputs((rows,), len(offsets) - 1, 4, groups, dk, 64, dtype, rows, offsets=offsets, grad=True), (rows,))
+
+
+def test_gradients_of_a_long_sequence_in_pieces_and_of_none():
+    _check_gradients(_inputs((1, 1500), 1, 1, 1, 64, 32, B, 29, strength=0.05, grad=True), (1, 1500))
+    got = block.decay_attention_grad(*(torch.zeros((0, 2, 8), device=DEV, dtype=B) for _ in range(4)), -torch.ones(2, device=DEV),
+                                     offsets=torch.zeros(3, dtype=torch.int32, device=DEV), dstate_out=torch.ones((2, 2, 8, 8), device=DEV))
+    assert bool((got["dA"] == 0).all()) and bool((got["dstate"] == 1).all())
+
+
+def test_gradients_without_states_some_wanted_and_outputs_handed_in():
+    lead = (1, 200)
+    i = _inputs(lead, 1, 2, 2, 64, 64, B, 31, state=False, grad=True)
+    every = _check_gradients(i, lead)
+    for want in (["dq"], ["dk"], ["dv", "dstate"], ["dA"], ["ddelta"], ["dq", "dk", "dv"]):
+        some = _check_gradients(i, lead, want=want, out={n: torch.full_like(every[n], float("nan")) for n in want})
+        for n in want:
+            if n in ("dstate", "dA", "ddelta"):                                     # (dq, dk, dv alone make do with states in two terms)
+                assert torch.equal(some[n], every[n]), n
+
+
+def test_gradients_with_strong_and_infinite_decays():
+    lead = (1, 260)
+    for strength in (0.0, 1e-3, 50.0):
+        i = _inputs(lead, 1, 2, 2, 32, 32, B, 37, strength=strength, grad=True)
+        if strength == 0.0:
+            i["A"].zero_()
+        _check_gradients(i, lead)
+
+
+def test_the_same_call_gives_the_same_bits():
+    i = _inputs((2, 300), 2, 4, 2, 64, 64, H, 41, grad=True)
+    call = lambda: block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], None, i["dlast"])  # noqa: E731
+    one, two = call(), call()
+    assert all(torch.equal(one[n], two[n]) for n in one)
+    assert torch.equal(_call(i), _call(i))
+
+
+@pytest.mark.parametrize("dk, dv, dtype, rows, offsets", [(40, 64, H, 400, [0, 0, 130, 130, 131, 400]), (7, 66, H, 140, [0, 140]), (100, 30, B, 600, [0, 600]), (64, 64, H, 700, [0, 700])])
+def test_what_scratch_held_before_does_not_matter(dk, dv, dtype, rows, offsets):
+    i = _inputs((rows,), len(offsets) - 1, 2, 1, dk, dv, dtype, 47, offsets=offsets, grad=True)
+
+    def both():
+        last = torch.empty_like(i["state"])
+        got = block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], i["offsets"], i["dlast"])
+        return dict(got, y=_call(i, state_out=last), last=last)
+
+    first = both()
+    for fill in (0, 255, 0x7e):
+        for size in (1 << 16, 1 << 20, 1 << 24, 1 << 26):                           # of all sizes that the allocator keeps apart
+            torch.full((size,), fill, dtype=torch.uint8, device=DEV)
+        got = both()
+        assert all(torch.equal(got[n], first[n]) for n in first), fill
+
+
+# ---- streams, graphs, many calls ------------------------------------------------------------------------------------------
+
+def test_another_stream_and_a_captured_call():
+    i = _inputs((2, 300), 2, 4, 2, 64, 64, B, 43, grad=True)
+    want, last = torch.empty_like(i["v"]), torch.empty_like(i["state"])
+    _call(i, y=want, state_out=last)
+    grads = block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"])
+    s = torch.cuda.Stream(device=DEV)
+    torch.cuda.synchronize()
+    y = _call(i, stream=s)
+    s.synchronize()
+    assert torch.equal(y, want)
+    g = torch.cuda.CUDAGraph()
+    S = i["state"].clone()
+    with torch.cuda.graph(g):
+        y = _call(i)
+        got = block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"])
+        one = block.decay_attention_step(i["q"][:, 0], i["k"][:, 0], i["v"][:, 0], i["A"], S, i["delta"][:, 0], i["delta_bias"], True)
+    y.zero_()
+    for _ in range(3):
+        S.copy_(i["state"])
+        g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(y, want) and all(torch.equal(got[n], grads[n]) for n in got)
+    S.copy_(i["state"])
+    assert torch.equal(one, block.decay_attention_step(i["q"][:, 0], i["k"][:, 0], i["v"][:, 0], i["A"], S, i["delta"][:, 0], i["delta_bias"], True))
+
+
+def test_many_calls_one_behind_another():
+    """Waits of one call do not see signals of another: four hundred of them, of different sizes."""
+    some = [_inputs((b, n), b, h, h, dk, 64, B, n) for b, n, h, dk in ((1, 1500, 4, 64), (4, 513, 8, 128), (2, 100, 2, 64))]
+    want = [_call(i).clone() for i in some]
+    for _ in range(130):
+        got = [_call(i) for i in some]
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and block.device_error(0) == 0
