@@ -89,7 +89,7 @@ def _load():
 
 class _LongWay:
     """Stands in for the compiled module where it cannot be built: every call is marshalled here."""
-    conv_step = scan_step = linear = attention = norm = staticmethod(lambda *args: None)
+    conv_step = scan_step = linear = attention = attention_grad = norm = norm_grad = staticmethod(lambda *args: None)
 
 
 def _short_way(lib):
@@ -102,8 +102,9 @@ def _short_way(lib):
                     for k in ("ttc_causal_conv_step", "ttc_selective_scan_step", "ttc_linear", "ttc_linear_workspace")),
                   _CONV_ARGS.size, _SCAN_ARGS.size, _LINEAR_ARGS.size)
         step.bind_more(*(ctypes.cast(getattr(lib, k), ctypes.c_void_p).value
-                         for k in ("ttc_decay_attention", "ttc_decay_attention_workspace", "ttc_decay_attention_step", "ttc_block_norm")),
-                       _DECAY_ARGS.size, _NORM_ARGS.size)
+                         for k in ("ttc_decay_attention", "ttc_decay_attention_workspace", "ttc_decay_attention_step", "ttc_decay_attention_grad",
+                                   "ttc_decay_attention_grad_workspace", "ttc_block_norm", "ttc_block_norm_grad", "ttc_block_norm_grad_workspace")),
+                       _DECAY_ARGS.size, _DECAY_GRADS.size, _NORM_ARGS.size, _NORM_GRADS.size)
     except (AttributeError, ImportError, OSError, TypeError, subprocess.CalledProcessError) as e:
         warnings.warn("single-token calls take the slower way through Python: %s" % e)
         return _LongWay
@@ -526,6 +527,12 @@ def decay_attention_grad(dy, q, k, v, A, delta=None, delta_bias=None, softplus=F
     """Gradients of :func:`decay_attention` given ``dy`` and that of ``state_out`` (``dstate_out``; default: zero).  Returns a dict with the wanted
     of ``dq, dk, dv, ddelta, dA, ddelta_bias, dstate`` (default: all, without ``ddelta`` and ``ddelta_bias`` where there is no ``delta``); ``out`` may hold
     tensors to write them to."""
+    if stream is None and want is None and out is None:
+        if _step is None:
+            _load()
+        got = _step.attention_grad(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, dy, dstate_out)
+        if got is not None:
+            return got
     record, states, rows, lead = _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets, None, None)
     index, t = _device_of(v), v.dtype
     groups, dk, heads, dv = q.shape[-2], q.shape[-1], v.shape[-2], v.shape[-1]
@@ -716,6 +723,12 @@ def block_norm_grad(x, h=None, dy=None, dh=None, w_post=None, z=None, scale=None
     """Gradients of :func:`block_norm` given ``dy`` (with ``w_pre``) and ``dh``, the gradient of ``h`` by what else reads it (default: zero).  ``h`` as the
     forward call returned it (needed with ``w_pre``, unless ``h`` is ``x``); ``residual``: whether there was one.  Returns a dict with the wanted of ``dx, dz, dresidual,
     dw_post, dscale, dw_pre`` (default: all whose operand is there); ``out`` may hold tensors to write them to, ``dresidual`` may be ``dh``."""
+    if stream is None and want is None and out is None:
+        if _step is None:
+            _load()
+        got = _step.norm_grad(x, h, dy, dh, w_post, z, scale, w_pre, eps, groups, residual)
+        if got is not None:
+            return got
     code, dtype, dev, d, rows, kept, px, pz, ldx, ldz, vectors = _norm_operands(x, w_post, z, scale, w_pre, groups, stream)
     more = []
     for t, name in ((h, "h"), (dy, "dy"), (dh, "dh")):

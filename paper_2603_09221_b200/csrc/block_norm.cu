@@ -217,8 +217,8 @@ int plan_grad(int device, const ttc_norm_args* a, const ttc_norm_grads* g, void*
     o.w = way_of(a, p, {ins[0], ins[1], ins[2], ins[3], ins[4], outs[0], outs[1], outs[2]}, 1);
     if (o.w.v > 1 && o.w.k == 1)
         o.w.smem += (size_t)kAhead * 5 * o.w.threads * o.w.rows_per_block * 16;
-    // as many workers as are resident: 512 threads to an SM by their registers, 1024 where a thread has few elements
-    const int resident = (o.w.v > 4 ? 512 : o.w.v > 1 ? 768 : 1024) / (o.w.threads * o.w.rows_per_block);
+    // as many workers as are resident by their registers
+    const int resident = (o.w.k == 1 && o.w.v < 8 ? 768 : 512) / (o.w.threads * o.w.rows_per_block);
     const int64_t most = (int64_t)sm_count(device) * (resident > 1 ? resident : 1);
     const int64_t all = (a->rows + o.w.rows_per_block - 1) / o.w.rows_per_block;
     o.blocks = (int)(all < most ? all : most);

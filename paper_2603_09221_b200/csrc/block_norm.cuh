@@ -71,10 +71,74 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
             v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
-// Sums over the groups of channels: in, the values of a thread's K vectors, one for each element; out, the sum of the element's group.  MIXED: groups that vectors lie across, or of
-// more than a warp's vectors, through shared memory, group by group.  Else all elements of a vector have the same sum, and only the first is set: a group is the row, or a few
+// ---- the vectors of a thread as pairs of floats (one instruction for two lanes of arithmetic; a single element's partner is nothing) ----
+
+template <int V> constexpr int kPairs = (V + 1) / 2;
+
+__device__ __forceinline__ f2 both(float v) { return pack2(v, v); }
+__device__ __forceinline__ float sum_of(f2 v)
+{
+    float a, b;
+    unpack2(v, a, b);
+    return a + b;
+}
+
+template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V>& a, f2 (&f)[kPairs<V>])
+{
+    if constexpr (V == 1) {
+        f[0] = pack2(to_f(a.v[0]), 0.f);
+    } else if constexpr (std::is_same<T, bf16>::value) {
+        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(&a);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j)
+            f[j] = pack2(__uint_as_float(pairs[j] << 16), __uint_as_float(pairs[j] & 0xffff0000u));
+    } else {
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j)
+            f[j] = pack2(to_f(a.v[2 * j]), to_f(a.v[2 * j + 1]));
+    }
+}
+template <typename T, int V> __device__ __forceinline__ void store(T* to, const f2 (&f)[kPairs<V>])
+{
+    Vec<T, V> u;
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j) {
+        float a, b;
+        unpack2(f[j], a, b);
+        if constexpr (V == 1) {
+            u.v[0] = from_f<T>(a);
+        } else if constexpr (std::is_same<T, bf16>::value) {
+            const __nv_bfloat162 r = __floats2bfloat162_rn(a, b);
+            reinterpret_cast<uint32_t*>(&u)[j] = *reinterpret_cast<const uint32_t*>(&r);
+        } else if constexpr (std::is_same<T, __half>::value) {
+            const __half2 r = __floats2half2_rn(a, b);
+            reinterpret_cast<uint32_t*>(&u)[j] = *reinterpret_cast<const uint32_t*>(&r);
+        } else {
+            u.v[2 * j] = a;
+            u.v[2 * j + 1] = b;
+        }
+    }
+    *reinterpret_cast<Vec<T, V>*>(to) = u;
+}
+// Parameters of a vector's channels.
+template <int V> __device__ __forceinline__ void params(const float* w, int c, f2 (&f)[kPairs<V>])
+{
+    if constexpr (V == 1) {
+        f[0] = pack2(w[c], 0.f);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; j += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(w + c + j);
+            f[j / 2] = pack2(u.x, u.y);
+            f[j / 2 + 1] = pack2(u.z, u.w);
+        }
+    }
+}
+
+// Sums over the groups of channels: in, the values of a thread's K vectors; out, the sum of each element's group.  MIXED: groups that vectors lie across, or of
+// more than a warp's vectors, through shared memory, group by group.  Else all elements of a vector have the same sum, and only the first pair is set: a group is the row, or a few
 // neighbouring threads.
-template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, float (&v)[K][V], float* area, float* buffer, int& turn)
+template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, f2 (&v)[K][kPairs<V>], float* area, float* buffer, int& turn)
 {
     if constexpr (MIXED) {
         const int warps = blockDim.x / 32;
@@ -84,10 +148,16 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int at = (k * blockDim.x + threadIdx.x) * V;
-            if (at < p.d)
+            if (at < p.d) {
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    s[at + j] = v[k][j];
+                for (int j = 0; j < V; j += 2) {
+                    float a, b;
+                    unpack2(v[k][j / 2], a, b);
+                    s[at + j] = a;
+                    if (V > 1)
+                        s[at + j + (V > 1)] = b;
+                }
+            }
         }
         __syncthreads();
         for (int g = threadIdx.x / 32; g < p.groups; g += warps) {
@@ -106,93 +176,69 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
             const int at = (k * blockDim.x + threadIdx.x) * V;
             if (at < p.d) {
                 int g = at / p.size, left = (g + 1) * p.size - at;
+                float e[2];
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     if (left == 0) {
                         ++g;
                         left = p.size;
                     }
-                    v[k][j] = sums[g];
+                    e[j & 1] = sums[g];
                     --left;
+                    if ((j & 1) || V == 1)
+                        v[k][j / 2] = pack2(e[0], V == 1 ? e[0] : e[1]);
                 }
             }
         }
     } else {
-        float all[1] = {0.f};
+        float one[K], all[1] = {0.f};
 #pragma unroll
         for (int k = 0; k < K; ++k) {
+            f2 sum = v[k][0];
 #pragma unroll
-            for (int j = 1; j < V; ++j)
-                v[k][0] += v[k][j];
-            all[0] += v[k][0];
+            for (int j = 1; j < kPairs<V>; ++j)
+                sum = add2(sum, v[k][j]);
+            one[k] = sum_of(sum);
+            all[0] += one[k];
         }
         if (p.groups == 1) {
             row_sums<1>(all, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                v[k][0] = all[0];
+                v[k][0] = both(all[0]);
         } else {
 #pragma unroll
-            for (int k = 0; k < K; ++k)
+            for (int k = 0; k < K; ++k) {
 #pragma unroll
                 for (int o = 1; o < 32; o *= 2)
                     if (o < p.lanes)
-                        v[k][0] += __shfl_xor_sync(0xffffffffu, v[k][0], o);
-        }
-    }
-}
-
-template <typename T, int V> __device__ __forceinline__ void widen(const Vec<T, V>& a, float (&f)[V])
-{
-    if constexpr (std::is_same<T, bf16>::value && V % 2 == 0) {
-        const uint32_t* pairs = reinterpret_cast<const uint32_t*>(&a);
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-            f[j] = __uint_as_float(pairs[j / 2] << 16);
-            f[j + 1] = __uint_as_float(pairs[j / 2] & 0xffff0000u);
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            f[j] = to_f(a.v[j]);
-    }
-}
-template <typename T, int V> __device__ __forceinline__ void store(T* to, const float (&f)[V])
-{
-    Vec<T, V> u;
-    if constexpr (sizeof(T) == 2 && V % 2 == 0) {
-        uint32_t* pairs = reinterpret_cast<uint32_t*>(&u);
-#pragma unroll
-        for (int j = 0; j < V; j += 2) {
-            if constexpr (std::is_same<T, bf16>::value) {
-                const __nv_bfloat162 r = __floats2bfloat162_rn(f[j], f[j + 1]);
-                pairs[j / 2] = *reinterpret_cast<const uint32_t*>(&r);
-            } else {
-                const __half2 r = __floats2half2_rn(f[j], f[j + 1]);
-                pairs[j / 2] = *reinterpret_cast<const uint32_t*>(&r);
+                        one[k] += __shfl_xor_sync(0xffffffffu, one[k], o);
+                v[k][0] = both(one[k]);
             }
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j)
-            u.v[j] = from_f<T>(f[j]);
     }
-    *reinterpret_cast<Vec<T, V>*>(to) = u;
 }
-// Parameters of a vector's channels.
-template <int V> __device__ __forceinline__ void params(const float* w, int c, bool ok, float (&f)[V])
+// 1 / sqrt(sum / size + eps), from what group_sums_of leaves.
+template <bool MIXED, int V> __device__ __forceinline__ void inverse_roots(f2 (&v)[kPairs<V>], float per_group, float eps)
 {
 #pragma unroll
-    for (int j = 0; j < V; j += V < 4 ? V : 4) {
-        const Vec<float, V < 4 ? V : 4> u = load_if(reinterpret_cast<const Vec<float, V < 4 ? V : 4>*>(w + c + j), ok);
-#pragma unroll
-        for (int i = 0; i < (V < 4 ? V : 4); ++i)
-            f[j + i] = u.v[i];
+    for (int j = 0; j < (MIXED ? kPairs<V> : 1); ++j) {
+        float a, b;
+        unpack2(v[j], a, b);
+        a = rsqrtf(fmaf(a, per_group, eps));
+        v[j] = MIXED ? pack2(a, rsqrtf(fmaf(b, per_group, eps))) : both(a);
     }
+#pragma unroll
+    for (int j = 1; j < kPairs<V>; ++j)
+        v[j] = MIXED ? v[j] : v[0];
 }
 
-template <int V> __device__ __forceinline__ void keep(float* to, const float (&f)[V])
+template <int V> __device__ __forceinline__ void keep(float* to, const f2 (&v)[kPairs<V>])
 {
+    float f[2 * kPairs<V>];
+#pragma unroll
+    for (int j = 0; j < kPairs<V>; ++j)
+        unpack2(v[j], f[2 * j], f[2 * j + 1]);
 #pragma unroll
     for (int j = 0; j < V; j += V < 4 ? V : 4) {
         Vec<float, V < 4 ? V : 4> u;
@@ -205,7 +251,7 @@ template <int V> __device__ __forceinline__ void keep(float* to, const float (&f
 
 // K vectors of V elements to a thread; blockDim.x threads to a row, blockDim.y rows to a block (more than one only where a row is a warp's).
 template <typename T, int V, int K, bool MIXED>
-__global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev p)
+__global__ void __launch_bounds__(K < 4 || V == 8 ? 512 : 1024) norm_kernel(const NormDev p)
 {
     __shared__ float buffer[2 * 32];
     wait_for_previous();
@@ -226,74 +272,71 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev 
         z[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.z) + lead * p.ldz + c[k]), ok[k] && p.z);
         r[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.r) + lead * p.ldr + c[k]), ok[k] && p.r);
     }
-    float u[K][V];
+    constexpr int P = kPairs<V>;
+    f2 u[K][P];
 #pragma unroll
     for (int k = 0; k < K; ++k)
         widen(x[k], u[k]);
     if (p.w_post) {
-        float sum[K][V];
+        f2 sum[K][P];
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                sum[k][j] = u[k][j] * u[k][j];
+            for (int j = 0; j < P; ++j)
+                sum[k][j] = mul2(u[k][j], u[k][j]);
         group_sums_of<MIXED, K, V>(p, sum, bnorm_smem, buffer, turn);
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float w[V];
-            params(p.w_post, c[k], true, w);
+            f2 w[P];
+            params<V>(p.w_post, c[k], w);
+            inverse_roots<MIXED, V>(sum[k], p.per_group, p.eps);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                sum[k][j] = MIXED || j == 0 ? rsqrtf(fmaf(sum[k][j], p.per_group, p.eps)) : sum[k][0];
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                u[k][j] *= sum[k][j] * w[j];
+            for (int j = 0; j < P; ++j)
+                u[k][j] = mul2(u[k][j], mul2(sum[k][j], w[j]));
         }
     }
-    if (p.z) {
-#pragma unroll
-        for (int k = 0; k < K; ++k) {
-            float f[V];
-            widen(z[k], f);
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                u[k][j] *= silu(f[j]);
-        }
-    }
-    float square[1] = {0.f};
+    f2 square = both(0.f);
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        if (p.scale) {
-            float s[V];
-            params(p.scale, c[k], true, s);
+        f2 f[P];
+        if (p.z) {
+            widen(z[k], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                u[k][j] *= s[j];
+            for (int j = 0; j < P; ++j)
+                u[k][j] = mul2(u[k][j], silu2(f[j]));
+        }
+        if (p.scale) {
+            params<V>(p.scale, c[k], f);
+#pragma unroll
+            for (int j = 0; j < P; ++j)
+                u[k][j] = mul2(u[k][j], f[j]);
         }
         if (p.r) {
-            float f[V];
             widen(r[k], f);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                u[k][j] += f[j];
+            for (int j = 0; j < P; ++j)
+                u[k][j] = add2(u[k][j], f[j]);
         }
         if (p.h && ok[k])
             store<T, V>(static_cast<T*>(p.h) + row * p.ldh + c[k], u[k]);
+        if (ok[k]) {
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            square[0] = ok[k] ? fmaf(u[k][j], u[k][j], square[0]) : square[0];
+            for (int j = 0; j < P; ++j)
+                square = fma2(u[k][j], u[k][j], square);
+        }
     }
     if (!p.w_pre)
         return;
-    row_sums<1>(square, buffer, turn);
-    const float rms = rsqrtf(fmaf(square[0], p.per_row, p.eps));
+    float all[1] = {sum_of(square)};
+    row_sums<1>(all, buffer, turn);
+    const f2 rms = both(rsqrtf(fmaf(all[0], p.per_row, p.eps)));
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-        float w[V];
-        params(p.w_pre, c[k], true, w);
+        f2 w[P];
+        params<V>(p.w_pre, c[k], w);
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            u[k][j] *= rms * w[j];
+        for (int j = 0; j < P; ++j)
+            u[k][j] = mul2(u[k][j], mul2(rms, w[j]));
         if (ok[k])
             store<T, V>(static_cast<T*>(p.y) + row * p.ldy + c[k], u[k]);
     }
@@ -304,24 +347,25 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_kernel(const NormDev 
 // Where a thread has one vector of each operand of a row, copies of the next rows' vectors into its own places of shared memory are under way (kAhead rows; no other thread looks at
 // them), so that memory is at work while the sums of a row are waited for.
 template <typename T, int V, int K, bool MIXED>
-__global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const NormDev p)
+__global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) norm_grad_kernel(const NormDev p)
 {
     constexpr bool RING = K == 1 && V > 1;
+    constexpr int P = kPairs<V>;
     __shared__ float buffer[2 * 32 * 2];
     wait_for_previous();
     const int worker = blockIdx.x * blockDim.y + threadIdx.y, vectors = p.d / V;
     int turn = 0;
     bool in[K];
     int c[K];
-    float s_post[K][V], s_scale[K][V], s_pre[K][V];
+    f2 s_post[K][P], s_scale[K][P], s_pre[K][P];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
         const int at = k * blockDim.x + threadIdx.x;
         in[k] = at < vectors;
         c[k] = in[k] ? at * V : 0;
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            s_post[k][j] = s_scale[k][j] = s_pre[k][j] = 0.f;
+        for (int j = 0; j < P; ++j)
+            s_post[k][j] = s_scale[k][j] = s_pre[k][j] = both(0.f);
     }
     const long long rounds = (p.rows + p.workers - 1) / p.workers;               // the same number for all rows of a block: they share barriers
     const int threads = blockDim.x * blockDim.y;
@@ -379,36 +423,38 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                 dh[k] = load_if(reinterpret_cast<const Vec<T, V>*>(static_cast<const T*>(p.dh) + lead * p.lddh + c[k]), ok && p.dh);
             }
         }
-        float g[K][V];
+        f2 g[K][P];
 #pragma unroll
         for (int k = 0; k < K; ++k)
             widen(dh[k], g[k]);
         if (p.w_pre) {
-            float sums[2] = {0.f, 0.f};
+            f2 square = both(0.f), product = both(0.f);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a[V], b[V], w[V];
+                f2 a[P], b[P], w[P];
                 widen(h[k], a);
                 widen(dy[k], b);
-                params(p.w_pre, c[k], true, w);
+                params<V>(p.w_pre, c[k], w);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    sums[0] = fmaf(a[j], a[j], sums[0]);
-                    sums[1] = fmaf(a[j], w[j] * b[j], sums[1]);
+                for (int j = 0; j < P; ++j) {
+                    square = fma2(a[j], a[j], square);
+                    product = fma2(a[j], mul2(w[j], b[j]), product);
                 }
             }
+            float sums[2] = {sum_of(square), sum_of(product)};
             row_sums<2>(sums, buffer, turn);
-            const float rms = rsqrtf(fmaf(sums[0], p.per_row, p.eps)), mean = sums[1] * p.per_row * rms * rms;
+            const float rms = rsqrtf(fmaf(sums[0], p.per_row, p.eps));
+            const f2 rms2 = both(rms), mean = both(-sums[1] * p.per_row * rms * rms);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a[V], b[V], w[V];
+                f2 a[P], b[P], w[P];
                 widen(h[k], a);
                 widen(dy[k], b);
-                params(p.w_pre, c[k], true, w);
+                params<V>(p.w_pre, c[k], w);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    s_pre[k][j] = fmaf(a[j] * rms, b[j], s_pre[k][j]);
-                    g[k][j] = fmaf(rms, fmaf(w[j], b[j], -a[j] * mean), g[k][j]);
+                for (int j = 0; j < P; ++j) {
+                    s_pre[k][j] = fma2(mul2(a[j], rms2), b[j], s_pre[k][j]);
+                    g[k][j] = fma2(rms2, fma2(a[j], mean, mul2(w[j], b[j])), g[k][j]);
                 }
             }
         }
@@ -418,77 +464,83 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
                 if (in[k] && here)
                     store<T, V>(static_cast<T*>(p.dr) + row * p.lddr + c[k], g[k]);
         }
-        float inverse[K][V];
+        f2 inverse[K][P];
         if (p.w_post) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a[V];
+                f2 a[P];
                 widen(x[k], a);
 #pragma unroll
-                for (int j = 0; j < V; ++j)
-                    inverse[k][j] = a[j] * a[j];
+                for (int j = 0; j < P; ++j)
+                    inverse[k][j] = mul2(a[j], a[j]);
             }
             group_sums_of<MIXED, K, V>(p, inverse, area, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k)
-#pragma unroll
-                for (int j = 0; j < V; ++j)
-                    inverse[k][j] = MIXED || j == 0 ? rsqrtf(fmaf(inverse[k][j], p.per_group, p.eps)) : inverse[k][0];
+                inverse_roots<MIXED, V>(inverse[k], p.per_group, p.eps);
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            float a[V], u[V], gate[V], slope[V], s[V];
-            widen(x[k], a);
-            if (p.w_post)
-                params(p.w_post, c[k], true, u);
-            if (p.scale)
-                params(p.scale, c[k], true, s);
-            if (p.z)
-                widen(z[k], slope);
+            f2 u[P], w[P];
+            widen(x[k], u);
+            if (p.w_post) {
+                params<V>(p.w_post, c[k], w);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                u[j] = p.w_post ? a[j] * inverse[k][j] * u[j] : a[j];
-                gate[j] = 1.f;
-                if (p.z) {
-                    const float f = slope[j], q = sigmoid(f);
-                    gate[j] = f * q;
-                    slope[j] = fmaf(q * f, 1.f - q, q);
-                }
-                if (p.scale) {
-                    s_scale[k][j] = fmaf(g[k][j], u[j] * gate[j], s_scale[k][j]);
-                    g[k][j] *= s[j];
-                }
-                if (p.z) {
-                    slope[j] *= g[k][j] * u[j];
-                    g[k][j] *= gate[j];
+                for (int j = 0; j < P; ++j)
+                    u[j] = mul2(mul2(u[j], inverse[k][j]), w[j]);
+            }
+            f2 gate[P], slope[P];
+            if (p.z) {
+                f2 f[P];
+                widen(z[k], f);
+#pragma unroll
+                for (int j = 0; j < P; ++j) {    // silu, and its slope q + f q (1 - q)
+                    const f2 q = sigmoid2(f[j]);
+                    gate[j] = mul2(f[j], q);
+                    slope[j] = fma2(gate[j], fma2(q, both(-1.f), both(1.f)), q);
                 }
             }
-            if (p.dz && in[k] && here)
-                store<T, V>(static_cast<T*>(p.dz) + row * p.lddz + c[k], slope);
+            if (p.scale) {
+                params<V>(p.scale, c[k], w);
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    s_scale[k][j] = fma2(g[k][j], p.z ? mul2(u[j], gate[j]) : u[j], s_scale[k][j]);
+                    g[k][j] = mul2(g[k][j], w[j]);
+                }
+            }
+            if (p.z) {
+#pragma unroll
+                for (int j = 0; j < P; ++j) {
+                    slope[j] = mul2(slope[j], mul2(g[k][j], u[j]));
+                    g[k][j] = mul2(g[k][j], gate[j]);
+                }
+                if (p.dz && in[k] && here)
+                    store<T, V>(static_cast<T*>(p.dz) + row * p.lddz + c[k], slope);
+            }
         }
         if (p.w_post) {
-            float sum[K][V];
+            f2 sum[K][P];
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a[V], w[V];
+                f2 a[P], w[P];
                 widen(x[k], a);
-                params(p.w_post, c[k], true, w);
+                params<V>(p.w_post, c[k], w);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    s_post[k][j] = fmaf(g[k][j], a[j] * inverse[k][j], s_post[k][j]);
-                    g[k][j] *= w[j];
-                    sum[k][j] = a[j] * g[k][j];
+                for (int j = 0; j < P; ++j) {
+                    s_post[k][j] = fma2(g[k][j], mul2(a[j], inverse[k][j]), s_post[k][j]);
+                    g[k][j] = mul2(g[k][j], w[j]);
+                    sum[k][j] = mul2(a[j], g[k][j]);
                 }
             }
             group_sums_of<MIXED, K, V>(p, sum, area, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                float a[V];
+                f2 a[P];
                 widen(x[k], a);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float mean = sum[k][MIXED ? j : 0] * p.per_group * inverse[k][j] * inverse[k][j];
-                    g[k][j] = inverse[k][j] * fmaf(-a[j], mean, g[k][j]);
+                for (int j = 0; j < P; ++j) {
+                    const f2 mean = mul2(mul2(sum[k][MIXED ? j : 0], both(-p.per_group)), mul2(inverse[k][j], inverse[k][j]));
+                    g[k][j] = mul2(inverse[k][j], fma2(a[j], mean, g[k][j]));
                 }
             }
         }
@@ -507,11 +559,11 @@ __global__ void __launch_bounds__(K < 4 ? 512 : 1024) norm_grad_kernel(const Nor
         for (int k = 0; k < K; ++k)
             if (in[k]) {
                 if (p.dw_post)
-                    keep(to + c[k], s_post[k]);
+                    keep<V>(to + c[k], s_post[k]);
                 if (p.dscale)
-                    keep(to + p.d + c[k], s_scale[k]);
+                    keep<V>(to + p.d + c[k], s_scale[k]);
                 if (p.dw_pre)
-                    keep(to + 2 * p.d + c[k], s_pre[k]);
+                    keep<V>(to + 2 * p.d + c[k], s_pre[k]);
             }
     }
 }

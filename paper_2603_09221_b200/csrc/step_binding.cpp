@@ -1,5 +1,5 @@
 // Short way into the calls of block.py whose kernels take less time than Python takes to describe their arguments: a single
-// token's convolution, scan and linear attention, linear attention itself, the norms and the projections.  Each function checks what block.py checks and, where everything is in its ordinary
+// token's convolution, scan and linear attention, linear attention and the norms with their gradients, and the projections.  Each function checks what block.py checks and, where everything is in its ordinary
 // place (the arguments' types, shapes, contiguity, one CUDA device, the current stream), fills the record, makes the call and
 // returns the output; otherwise it returns None and block.py goes its own way, which also says what is wrong.
 #define PY_SSIZE_T_CLEAN
@@ -23,6 +23,10 @@ decltype(&ttc_decay_attention) attention_call;
 decltype(&ttc_decay_attention_workspace) attention_workspace_call;
 decltype(&ttc_decay_attention_step) attention_step_call;
 decltype(&ttc_block_norm) norm_call;
+decltype(&ttc_decay_attention_grad) attention_grad_call;
+decltype(&ttc_decay_attention_grad_workspace) attention_grad_workspace_call;
+decltype(&ttc_block_norm_grad) norm_grad_call;
+decltype(&ttc_block_norm_grad_workspace) norm_grad_workspace_call;
 
 // A tensor argument: absent (None), present, or something else.
 struct Arg {
@@ -251,57 +255,50 @@ PyObject* linear(PyObject*, PyObject* const* args, Py_ssize_t count)
     }
 }
 
-// (q, k, v, A, delta, delta_bias, softplus, scale or None, state, offsets, y, state_out, step)
-PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count)
-{
-    if (count != 13 || !attention_call)
-        Py_RETURN_NONE;
-    try {
-        const Arg q(args[0]), k(args[1]), v(args[2]), A(args[3]), delta(args[4]), bias(args[5]), state(args[8]), offsets(args[9]), y_arg(args[10]), state_out(args[11]);
-        const int softplus = PyObject_IsTrue(args[6]), step = PyObject_IsTrue(args[12]);
-        if (!q.t || !k.t || !v.t || !A.t || !delta.ok || !bias.ok || !state.ok || !offsets.ok || !y_arg.ok || !state_out.ok || softplus < 0 || step < 0 || (bias.t && !delta.t))
-            return PyErr_Clear(), Py_NewRef(Py_None);
+// What a call of linear attention is given, checked; the record without y and state_out.
+struct Attention {
+    Arg q, k, v, A, delta, bias, state, offsets;
+    ttc_decay_args a = {};
+    int lead = 0;
+    bool packed = false, ok = false;
+    // args: (q, k, v, A, delta, delta_bias, softplus, scale or None, state, offsets)
+    Attention(PyObject* const* args, bool step)
+        : q(args[0]), k(args[1]), v(args[2]), A(args[3]), delta(args[4]), bias(args[5]), state(args[8]), offsets(args[9])
+    {
+        const int softplus = PyObject_IsTrue(args[6]);
+        if (!q.t || !k.t || !v.t || !A.t || !delta.ok || !bias.ok || !state.ok || !offsets.ok || softplus < 0 || (bias.t && !delta.t))
+            return;
         const at::Tensor& vt = *v.t;
         const auto type = vt.scalar_type();
         const auto device = vt.device();
-        const bool packed = offsets.t;
-        const int lead = step || packed ? 1 : 2;
+        packed = offsets.t;
+        lead = step || packed ? 1 : 2;
         if (!vt.is_cuda() || (type != at::kBFloat16 && type != at::kHalf) || vt.dim() != lead + 2 || q.t->dim() != lead + 2 || (step && packed))
-            Py_RETURN_NONE;
+            return;
         const int64_t heads = vt.size(lead), dv = vt.size(lead + 1), groups = q.t->size(lead), dk = q.t->size(lead + 1);
         int64_t batch = vt.size(0);
         const int64_t tokens = step ? 1 : packed ? vt.size(0) : vt.size(1);
         if (packed) {
             if (!here(*offsets.t, at::kInt, device) || offsets.t->dim() != 1 || offsets.t->size(0) < 1 || !offsets.t->is_contiguous())
-                Py_RETURN_NONE;
+                return;
             batch = offsets.t->size(0) - 1;
         }
-        ttc_decay_args a = {};
         if (batch == 0 || tokens == 0 || heads >= INT32_MAX || groups >= INT32_MAX || dk < 1 || dk > 128 || dv > 128 || !dense(A, {heads}, at::kFloat, device) ||
-            !dense(bias, {heads}, at::kFloat, device) || !dense(state, {batch, heads, dk, dv}, at::kFloat, device) ||
-            !dense(state_out, {batch, heads, dk, dv}, at::kFloat, device) || !head_rows(*q.t, vt, lead, groups, dk, packed, a.q) ||
+            !dense(bias, {heads}, at::kFloat, device) || !dense(state, {batch, heads, dk, dv}, at::kFloat, device) || !head_rows(*q.t, vt, lead, groups, dk, packed, a.q) ||
             !head_rows(*k.t, vt, lead, groups, dk, packed, a.k) || !head_rows(vt, vt, lead, heads, dv, packed, a.v))
-            Py_RETURN_NONE;
+            return;
         if (delta.t) {                           // [lead..][heads]
             const at::Tensor& t = *delta.t;
             if (!here(t, type, device) || t.dim() != lead + 1 || t.size(lead) != heads || (heads > 1 && t.stride(lead) != 1) || t.size(0) != vt.size(0) ||
                 (lead == 2 && t.size(1) != vt.size(1)))
-                Py_RETURN_NONE;
-            a.delta = lead == 2 ? ttc_rows{t.data_ptr(), t.stride(0), t.stride(1)} : packed ? ttc_rows{t.data_ptr(), 0, t.stride(0)} : ttc_rows{t.data_ptr(), t.stride(0), 0};
+                return;
+            a.delta = token_rows(t);
         }
         double scale = 1.0 / std::sqrt((double)dk);
         if (args[7] != Py_None) {
             scale = PyFloat_AsDouble(args[7]);
             if (PyErr_Occurred())
-                return PyErr_Clear(), Py_NewRef(Py_None);
-        }
-        at::Tensor y;
-        if (y_arg.t) {
-            if (!head_rows(*y_arg.t, vt, lead, heads, dv, packed, a.y))
-                Py_RETURN_NONE;
-        } else {
-            y = at::empty(vt.sizes(), vt.options());
-            head_rows(y, vt, lead, heads, dv, packed, a.y);
+                return;
         }
         a.batch = batch;
         a.tokens = tokens;
@@ -316,25 +313,122 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count)
         a.A = static_cast<const float*>(A.ptr());
         a.delta_bias = static_cast<const float*>(bias.ptr());
         a.state = static_cast<const float*>(state.ptr());
+        ok = true;
+    }
+    ttc_rows token_rows(const at::Tensor& t) const
+    {
+        return lead == 2 ? ttc_rows{t.data_ptr(), t.stride(0), t.stride(1)} : packed ? ttc_rows{t.data_ptr(), 0, t.stride(0)} : ttc_rows{t.data_ptr(), t.stride(0), 0};
+    }
+};
+
+PyObject* none()
+{
+    PyErr_Clear();
+    return Py_NewRef(Py_None);
+}
+
+// (q, k, v, A, delta, delta_bias, softplus, scale or None, state, offsets, y, state_out, step)
+PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 13 || !attention_call)
+        Py_RETURN_NONE;
+    try {
+        const int step = PyObject_IsTrue(args[12]);
+        if (step < 0)
+            return none();
+        Attention c(args, step);
+        const Arg y_arg(args[10]), state_out(args[11]);
+        if (!c.ok || !y_arg.ok)
+            return none();
+        const at::Tensor& vt = *c.v.t;
+        ttc_decay_args& a = c.a;
+        const auto device = vt.device();
+        if (!dense(state_out, {a.batch, a.heads, a.dk, a.dv}, at::kFloat, device))
+            return none();
+        at::Tensor y;
+        if (!y_arg.t)
+            y = at::empty(vt.sizes(), vt.options());
+        if (!head_rows(y_arg.t ? *y_arg.t : y, vt, c.lead, a.heads, a.dv, c.packed, a.y))
+            return none();
         a.state_out = static_cast<float*>(state_out.ptr());
         void* stream = c10::cuda::getCurrentCUDAStream(device.index()).stream();
         if (step) {
             if (attention_step_call(device.index(), &a, stream) != TTC_OK)
-                Py_RETURN_NONE;
+                return none();
             return give(args[10], y);
         }
         const int64_t need = attention_workspace_call(device.index(), &a);
         if (need < 0)
-            Py_RETURN_NONE;
+            return none();
         at::Tensor ws;
         if (need > 0)
             ws = at::empty({need}, vt.options().dtype(at::kByte));
         if (attention_call(device.index(), &a, need ? ws.data_ptr() : nullptr, need, stream) != TTC_OK)
-            Py_RETURN_NONE;
+            return none();
         return give(args[10], y);
     } catch (...) {
-        PyErr_Clear();
+        return none();
+    }
+}
+
+// Puts a tensor into a dict; false on failure.
+bool put(PyObject* d, const char* name, const at::Tensor& t)
+{
+    PyObject* o = THPVariable_Wrap(t);
+    const bool ok = o && PyDict_SetItemString(d, name, o) == 0;
+    Py_XDECREF(o);
+    return ok;
+}
+
+// (q, k, v, A, delta, delta_bias, softplus, scale or None, state, offsets, dy, dstate_out): a dict of all gradients
+PyObject* attention_grad(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 12 || !attention_grad_call)
         Py_RETURN_NONE;
+    try {
+        Attention c(args, false);
+        const Arg dy(args[10]), dlast(args[11]);
+        if (!c.ok || !dy.t)
+            return none();
+        const at::Tensor &vt = *c.v.t, &qt = *c.q.t;
+        const ttc_decay_args& a = c.a;
+        const auto device = vt.device();
+        ttc_decay_grads g = {};
+        if (!dense(dlast, {a.batch, a.heads, a.dk, a.dv}, at::kFloat, device) || !head_rows(*dy.t, vt, c.lead, a.heads, a.dv, c.packed, g.dy))
+            return none();
+        const auto f32 = vt.options().dtype(at::kFloat);
+        const at::Tensor dq = at::empty(qt.sizes(), vt.options()), dk = at::empty(qt.sizes(), vt.options()), dv = at::empty(vt.sizes(), vt.options()), dA = at::empty({a.heads}, f32),
+                         dstate = at::empty({a.batch, a.heads, a.dk, a.dv}, f32);
+        at::Tensor ddelta, dbias;
+        head_rows(dq, vt, c.lead, a.groups, a.dk, c.packed, g.dq);
+        head_rows(dk, vt, c.lead, a.groups, a.dk, c.packed, g.dk);
+        head_rows(dv, vt, c.lead, a.heads, a.dv, c.packed, g.dv);
+        g.dA = static_cast<float*>(dA.data_ptr());
+        g.dstate = static_cast<float*>(dstate.data_ptr());
+        g.dstate_out = static_cast<const float*>(dlast.ptr());
+        if (c.delta.t) {
+            ddelta = at::empty(c.delta.t->sizes(), vt.options());
+            dbias = at::empty({a.heads}, f32);
+            g.ddelta = c.token_rows(ddelta);
+            g.ddelta_bias = static_cast<float*>(dbias.data_ptr());
+        }
+        const int64_t need = attention_grad_workspace_call(device.index(), &a, &g);
+        if (need < 0)
+            return none();
+        at::Tensor ws;
+        if (need > 0)
+            ws = at::empty({need}, vt.options().dtype(at::kByte));
+        if (attention_grad_call(device.index(), &a, &g, need ? ws.data_ptr() : nullptr, need, c10::cuda::getCurrentCUDAStream(device.index()).stream()) != TTC_OK)
+            return none();
+        PyObject* d = PyDict_New();
+        if (!d || !put(d, "dq", dq) || !put(d, "dk", dk) || !put(d, "dv", dv) || (c.delta.t && !put(d, "ddelta", ddelta)) || !put(d, "dA", dA) ||
+            (c.delta.t && !put(d, "ddelta_bias", dbias)) || !put(d, "dstate", dstate)) {
+            Py_XDECREF(d);
+            return none();
+        }
+        return d;
+    } catch (...) {
+        return none();
     }
 }
 
@@ -414,6 +508,78 @@ PyObject* norm(PyObject*, PyObject* const* args, Py_ssize_t count)
     }
 }
 
+// (x, h, dy, dh, w_post, z, scale, w_pre, eps, groups, residual): a dict of all gradients
+PyObject* norm_grad(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    if (count != 11 || !norm_grad_call)
+        Py_RETURN_NONE;
+    try {
+        const Arg x(args[0]), h(args[1]), dy(args[2]), dh(args[3]), w_post(args[4]), z(args[5]), scale(args[6]), w_pre(args[7]);
+        const double eps = PyFloat_AsDouble(args[8]);
+        const long groups = PyErr_Occurred() ? -1 : PyLong_AsLong(args[9]);
+        const int residual = PyObject_IsTrue(args[10]);
+        if (PyErr_Occurred() || !x.t || residual < 0 || groups < 1 || groups >= INT32_MAX)
+            return none();
+        const at::Tensor& xt = *x.t;
+        if (!xt.is_cuda() || xt.dim() < 1 || type_code(xt.scalar_type()) < 0 || xt.numel() == 0)
+            return none();
+        const int64_t d = xt.size(xt.dim() - 1);
+        const auto device = xt.device();
+        ttc_norm_args a = {};
+        ttc_norm_grads g = {};
+        const void* h_ptr;
+        if (d >= INT32_MAX || !dense(w_post, {d}, at::kFloat, device) || !dense(scale, {d}, at::kFloat, device) || !dense(w_pre, {d}, at::kFloat, device) ||
+            !flat_rows(x, xt, a.x, a.ldx) || !flat_rows(z, xt, a.z, a.ldz) || !flat_rows(h, xt, h_ptr, a.ldh) || !flat_rows(dy, xt, g.dy, g.lddy) || !flat_rows(dh, xt, g.dh, g.lddh))
+            return none();
+        a.h = const_cast<void*>(h_ptr);
+        a.rows = xt.numel() / d;
+        a.d = (int32_t)d;
+        a.groups = (int32_t)groups;
+        a.dtype = type_code(xt.scalar_type());
+        a.eps = (float)eps;
+        a.w_post = static_cast<const float*>(w_post.ptr());
+        a.scale = static_cast<const float*>(scale.ptr());
+        a.w_pre = static_cast<const float*>(w_pre.ptr());
+        const auto f32 = xt.options().dtype(at::kFloat);
+        at::Tensor dx = at::empty(xt.sizes(), xt.options()), dz, dr, dwp, ds, dw;
+        g.dx = dx.data_ptr(), g.lddx = d;
+        if (z.t) {
+            dz = at::empty(xt.sizes(), xt.options());
+            g.dz = dz.data_ptr(), g.lddz = d;
+        }
+        if (residual) {
+            dr = at::empty(xt.sizes(), xt.options());
+            g.dresidual = dr.data_ptr(), g.lddr = d;
+        }
+        auto vector = [&](const Arg& w, at::Tensor& t, float*& to) {
+            if (w.t) {
+                t = at::empty({d}, f32);
+                to = static_cast<float*>(t.data_ptr());
+            }
+        };
+        vector(w_post, dwp, g.dw_post);
+        vector(scale, ds, g.dscale);
+        vector(w_pre, dw, g.dw_pre);
+        const int64_t need = norm_grad_workspace_call(device.index(), &a, &g);
+        if (need < 0)
+            return none();
+        at::Tensor ws;
+        if (need > 0)
+            ws = at::empty({need}, xt.options().dtype(at::kByte));
+        if (norm_grad_call(device.index(), &a, &g, need ? ws.data_ptr() : nullptr, need, c10::cuda::getCurrentCUDAStream(device.index()).stream()) != TTC_OK)
+            return none();
+        PyObject* o = PyDict_New();
+        if (!o || !put(o, "dx", dx) || (z.t && !put(o, "dz", dz)) || (residual && !put(o, "dresidual", dr)) || (w_post.t && !put(o, "dw_post", dwp)) ||
+            (scale.t && !put(o, "dscale", ds)) || (w_pre.t && !put(o, "dw_pre", dw))) {
+            Py_XDECREF(o);
+            return none();
+        }
+        return o;
+    } catch (...) {
+        return none();
+    }
+}
+
 // Addresses of the library's functions, in the order of the declarations above, and the sizes of the records that they take (a module
 // that was compiled with another header than the library must not fill them).
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
@@ -448,19 +614,19 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t count)
 // The same for linear attention and the norms.
 PyObject* bind_more(PyObject*, PyObject* const* args, Py_ssize_t count)
 {
-    if (count != 6) {
-        PyErr_SetString(PyExc_TypeError, "bind_more takes four addresses and two sizes");
+    if (count != 12) {
+        PyErr_SetString(PyExc_TypeError, "bind_more takes eight addresses and four sizes");
         return nullptr;
     }
-    void* at[4];
-    for (int i = 0; i < 4; ++i) {
+    void* at[8];
+    for (int i = 0; i < 8; ++i) {
         at[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred())
             return nullptr;
     }
-    const long sizes[2] = {(long)sizeof(ttc_decay_args), (long)sizeof(ttc_norm_args)};
-    for (int i = 0; i < 2; ++i) {
-        const long size = PyLong_AsLong(args[4 + i]);
+    const long sizes[4] = {(long)sizeof(ttc_decay_args), (long)sizeof(ttc_decay_grads), (long)sizeof(ttc_norm_args), (long)sizeof(ttc_norm_grads)};
+    for (int i = 0; i < 4; ++i) {
+        const long size = PyLong_AsLong(args[8 + i]);
         if (PyErr_Occurred())
             return nullptr;
         if (size != sizes[i]) {
@@ -471,12 +637,16 @@ PyObject* bind_more(PyObject*, PyObject* const* args, Py_ssize_t count)
     attention_call = reinterpret_cast<decltype(attention_call)>(at[0]);
     attention_workspace_call = reinterpret_cast<decltype(attention_workspace_call)>(at[1]);
     attention_step_call = reinterpret_cast<decltype(attention_step_call)>(at[2]);
-    norm_call = reinterpret_cast<decltype(norm_call)>(at[3]);
+    attention_grad_call = reinterpret_cast<decltype(attention_grad_call)>(at[3]);
+    attention_grad_workspace_call = reinterpret_cast<decltype(attention_grad_workspace_call)>(at[4]);
+    norm_call = reinterpret_cast<decltype(norm_call)>(at[5]);
+    norm_grad_call = reinterpret_cast<decltype(norm_grad_call)>(at[6]);
+    norm_grad_workspace_call = reinterpret_cast<decltype(norm_grad_workspace_call)>(at[7]);
     Py_RETURN_NONE;
 }
 
 #define TTC_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TTC_METHOD(bind), TTC_METHOD(conv_step), TTC_METHOD(scan_step), TTC_METHOD(linear), TTC_METHOD(bind_more), TTC_METHOD(attention), TTC_METHOD(norm), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {TTC_METHOD(bind), TTC_METHOD(conv_step), TTC_METHOD(scan_step), TTC_METHOD(linear), TTC_METHOD(bind_more), TTC_METHOD(attention), TTC_METHOD(attention_grad), TTC_METHOD(norm), TTC_METHOD(norm_grad), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_step", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 } // namespace

@@ -123,7 +123,7 @@ def test_python_says_what_is_wrong():
         block.block_norm_grad(x, dy=x, w_pre=w)
 
 
-@pytest.mark.parametrize("record", ["_DECAY_ARGS", "_NORM_ARGS"])
+@pytest.mark.parametrize("record", ["_DECAY_ARGS", "_DECAY_GRADS", "_NORM_ARGS", "_NORM_GRADS"])
 def test_a_module_built_for_other_records_is_not_used(monkeypatch, record):
     lib = block._load()
     assert block._short_way(lib) is not block._LongWay
