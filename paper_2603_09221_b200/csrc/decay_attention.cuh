@@ -248,6 +248,20 @@ __device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16])
     for (int i = 0; i < 16; ++i)
         v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t at, float (&v)[8])
+{
+    uint32_t r[8];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void tmem_st4(uint32_t at, const uint32_t (&r)[4])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16])
 {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
@@ -347,33 +361,17 @@ __device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const
         unpack2(mul2(pack2(v[j + 2], v[j + 3]), mul2(pack2(e_row, e_row), pack2(t.z, t.w))), v[j + 2], v[j + 3]);
     }
 }
-// (later tokens' results are of no use: they may be infinite)
-__device__ __forceinline__ void decay_own(float (&v)[32], const float* g, float own)
-{
-#pragma unroll
-    for (int j = 0; j < 32; j += 4) {
-        const float4 h = *reinterpret_cast<const float4*>(g + j);
-        float a, b, c, d;
-        unpack2(add2(pack2(own, own), pack2(-h.x, -h.y)), a, b);
-        unpack2(add2(pack2(own, own), pack2(-h.z, -h.w)), c, d);
-        unpack2(mul2(pack2(v[j], v[j + 1]), pack2(ex2(a), ex2(b))), v[j], v[j + 1]);
-        unpack2(mul2(pack2(v[j + 2], v[j + 3]), pack2(ex2(c), ex2(d))), v[j + 2], v[j + 3]);
-    }
-}
-// Pairs in 16 bits without the tokens behind the lane's.
-__device__ __forceinline__ void cut_later(uint32_t (&packed)[16], int lane)
-{
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        packed[j] = lane > 2 * j ? packed[j] : lane == 2 * j ? packed[j] & 0xffffu : 0u;
-}
 __device__ __forceinline__ void decay_row(float (&v)[32], const float* g, bool diagonal, int lane, float own, float e_row, const float* to_end)
 {
     if (diagonal) {
-        decay_own(v, g, own);
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            v[j] = j <= lane ? v[j] : 0.f;
+        for (int j = 0; j < 32; j += 4) {
+            const float4 h = *reinterpret_cast<const float4*>(g + j);
+            v[j] = j <= lane ? v[j] * ex2(own - h.x) : 0.f;
+            v[j + 1] = j + 1 <= lane ? v[j + 1] * ex2(own - h.y) : 0.f;
+            v[j + 2] = j + 2 <= lane ? v[j + 2] * ex2(own - h.z) : 0.f;
+            v[j + 3] = j + 3 <= lane ? v[j + 3] * ex2(own - h.w) : 0.f;
+        }
     } else {
         decay_earlier(v, e_row, to_end);
     }
@@ -909,25 +907,36 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             const float mine = dec.g[row], own = ex2(mine), f = own * dec.before[quarter] * unit;
             until(sm.scores, i);
             behind_barrier();
+            // a warp has one of the earlier blocks of 32 tokens and a quarter of its rows' own block, where the exponentials are (all of that in one warp took
+            // 1700 clocks of a chunk's 4600; the later blocks are zeros)
             uint32_t packed[16];
-            if (sub <= quarter) {
+            if (sub < quarter) {
                 float v[32];
                 tmem_ld32(scores + sub * 32 + lanes, v);
-                if (sub == quarter)
-                    decay_own(v, dec.g + sub * 32, mine);
-                else
-                    decay_earlier(v, own * between(dec, sub, quarter), dec.to_end + sub * 32);
+                decay_earlier(v, own * between(dec, sub, quarter), dec.to_end + sub * 32);
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
-                if (sub == quarter)
-                    cut_later(packed, lane);
             } else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     packed[j] = 0;
             }
-            tmem_st16(operand + sub * 16 + lanes, packed);
+            if (sub != quarter)
+                tmem_st16(operand + sub * 16 + lanes, packed);
+            {
+                const int at = quarter * 32 + sub * 8;
+                float v[8];
+                tmem_ld8(scores + at + lanes, v);
+                uint32_t r[4];
+#pragma unroll
+                for (int j = 0; j < 8; j += 2) {                     // (of later tokens it may be infinite: they are taken out behind it)
+                    const float2 h = *reinterpret_cast<const float2*>(dec.g + at + j);
+                    const uint32_t w = pack16<T>(v[j] * ex2(mine - h.x), v[j + 1] * ex2(mine - h.y));
+                    r[j / 2] = lane > sub * 8 + j ? w : lane == sub * 8 + j ? w & 0xffffu : 0u;
+                }
+                tmem_st4(operand + at / 2 + lanes, r);
+            }
             until(sm.state, i);
             behind_barrier();
             float v[16];
