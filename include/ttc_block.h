@@ -150,8 +150,9 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
  * A [heads], delta_bias [heads] (NULL: 0; not used without delta).  state [batch][heads][dk][dv] float32 is S in front of every sequence
  * (NULL: zero), state_out receives the last one; it may be state itself.  y may be v (the same pointer and strides).
  * Exponents A D_t are expected to be <= 0; minus infinity forgets everything.  Tokens go through the tensor cores in chunks of 128, counted from their
- * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, and of those behind it.  float16: products scale q . k, and in the
- * gradients dy . v, have to stay below 65504.  Scratch: 6 bytes for each element of a state (dk, dv rounded up to 64 or 128) of every chunk.
+ * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, earlier tokens' too, and of those behind it.  float16: products scale q . k,
+ * and in the gradients dy . v, have to stay below 65504.  Scratch: none where sequences, heads and columns fill the SMs; else sequences are walked along in pieces, with
+ * 512 bytes for each value channel (dv rounded up to 64 or 128) of a piece and head, of which there are as many as SMs, and one more for each packed sequence.
  */
 typedef struct ttc_decay_args {
     int64_t batch, tokens;
@@ -177,7 +178,8 @@ int ttc_decay_attention_step(int32_t device, const ttc_decay_args* a, void* cuda
  *     dq_t = scale S_t dy_t    dk_t = Z_t v_t    dv_t = Z_t' k_t    (dq, dk summed over the heads of a group)
  *     dD_t = A exp(A D_t) <Z_t, S_{t-1}>         dA = sum_t D_t exp(A D_t) <Z_t, S_{t-1}>
  * ddelta from dD_t through the softplus, ddelta_bias its sum over all tokens; dA, ddelta_bias [heads], dstate [batch][heads][dk][dv] float32; the row
- * gradients in the rows' type.  Scratch: 12 bytes for each element of a state of every chunk, and, where heads share queries and keys, 8 dk for every token and head.
+ * gradients in the rows' type.  Scratch: for each element of a state (dk, dv rounded up to 64 or 128) of every chunk of 128 tokens 8 bytes, or 12 of bfloat16 rows where ddelta, dA
+ * or ddelta_bias are wanted; with these 20 bytes for every token and head; where heads share queries and keys, 8 dk for every token and head; and twice the forward call's.
  */
 typedef struct ttc_decay_grads {
     ttc_rows dy, dq, dk, dv, ddelta;

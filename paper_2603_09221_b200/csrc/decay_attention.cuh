@@ -904,7 +904,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             const Chunk c = chunk_of(piece, i);
             const Table& dec = sm.dec[i & 1];
             const float across = dec.whole;
-            const float mine = dec.g[row], own = ex2(mine), f = own * dec.before[quarter] * unit;
+            const float mine = dec.g[row], own = ex2(mine) * p.scale, f = own * dec.before[quarter] * unit;
             until(sm.scores, i);
             behind_barrier();
             // a warp has one of the earlier blocks of 32 tokens and a quarter of its rows' own block, where the exponentials are (all of that in one warp took
@@ -932,7 +932,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {                     // (of later tokens it may be infinite: they are taken out behind it)
                     const float2 h = *reinterpret_cast<const float2*>(dec.g + at + j);
-                    const uint32_t w = pack16<T>(v[j] * ex2(mine - h.x), v[j + 1] * ex2(mine - h.y));
+                    const uint32_t w = pack16<T>(v[j] * (p.scale * ex2(mine - h.x)), v[j + 1] * (p.scale * ex2(mine - h.y)));
                     r[j / 2] = lane > sub * 8 + j ? w : lane == sub * 8 + j ? w & 0xffffu : 0u;
                 }
                 tmem_st4(operand + at / 2 + lanes, r);
@@ -977,8 +977,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             char* stage = smem + (values_at(i) - tiles);
 #pragma unroll
             for (int j = 0; j < 16; j += 8) {
-                const uint4 w = make_uint4(pack16<T>(v[j] * p.scale, v[j + 1] * p.scale), pack16<T>(v[j + 2] * p.scale, v[j + 3] * p.scale),
-                                           pack16<T>(v[j + 4] * p.scale, v[j + 5] * p.scale), pack16<T>(v[j + 6] * p.scale, v[j + 7] * p.scale));
+                const uint4 w = make_uint4(pack16<T>(v[j], v[j + 1]), pack16<T>(v[j + 2], v[j + 3]), pack16<T>(v[j + 4], v[j + 5]), pack16<T>(v[j + 6], v[j + 7]));
                 *reinterpret_cast<uint4*>(stage + tile_at(row, sub * 2 + j / 8)) = w;
             }
             asm volatile("bar.sync %0, 128;" :: "r"(3 + quarter) : "memory");          // the four warps of these rows

@@ -135,6 +135,15 @@ def test_states_far_from_one_in_float16():
         _check_forward(i, lead, scale=lead_scale)
 
 
+def test_large_products_in_float16():
+    """The scale goes into the scores before they are rounded: q . k may pass the largest float16 as long as scale q . k does not."""
+    lead = (1, 200)
+    i = _inputs(lead, 1, 2, 2, 64, 64, H, 14, strength=0.01)
+    i["q"], i["k"] = i["q"] * 100, i["k"] * 100                                     # q . k up to 4e5
+    i["state"] *= 100
+    _check_forward(i, lead, scale=1e-3)
+
+
 def test_slices_of_wider_rows_and_state_in_place():
     g = torch.Generator(device=DEV).manual_seed(3)
     for pad in (0, 8, 3):                                                           # aligned to 16 bytes, or not
@@ -333,3 +342,56 @@ def test_many_calls_one_behind_another():
     for _ in range(130):
         got = [_call(i) for i in some]
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and block.device_error(0) == 0
+
+
+def test_two_streams_at_once():
+    some = [_inputs((2, 700), 2, 8, 4, 64, 64, B, n, grad=True) for n in (1, 2)]
+    grads = lambda i, **kw: block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], None, i["dlast"], **kw)  # noqa: E731
+    want = [(_call(i), grads(i)) for i in some]
+    streams = [torch.cuda.Stream(device=DEV) for _ in some]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(10):
+        for i, s in zip(some, streams):
+            with torch.cuda.stream(s):
+                got.append((_call(i), grads(i)))
+    torch.cuda.synchronize()
+    for n, (y, g) in enumerate(got):
+        assert torch.equal(y, want[n % 2][0]) and all(torch.equal(g[m], want[n % 2][1][m]) for m in g)
+
+
+def test_two_captured_calls_replayed_in_turn():
+    """Each graph has its own scratch: neither finds what the other left wrong."""
+    some = [_inputs((1, n), 1, 2, 1, 64, 64, B, n, grad=True) for n in (1500, 900)]  # cut into pieces: states in scratch
+    grads = lambda i: block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], None, i["dlast"])  # noqa: E731
+    want = [(_call(i).clone(), {n: t.clone() for n, t in grads(i).items()}) for i in some]
+    graphs, got = [torch.cuda.CUDAGraph() for _ in some], []
+    torch.cuda.synchronize()
+    for g, i in zip(graphs, some):
+        with torch.cuda.graph(g):
+            got.append((_call(i), grads(i)))
+    for n in (0, 1, 1, 0, 1, 0):
+        graphs[n].replay()
+        assert torch.equal(got[n][0], want[n][0]) and all(torch.equal(got[n][1][m], want[n][1][m]) for m in want[n][1])
+
+
+def test_rows_past_32_bits():
+    """Rows of 2.4e9 elements in all: operands and results are slices of them."""
+    tokens, heads, d = 60000, 2, 64
+    g = torch.Generator(device=DEV).manual_seed(3)
+    wide = torch.zeros((tokens, 40000), device=DEV, dtype=B)
+    slices = [wide[:, at:at + heads * d].unflatten(-1, (heads, d)) for at in (0, 8000, 16000, 24000, 32000)]
+    q, k, v, dy, y = slices
+    for t in (q, k, v, dy):
+        t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+    A = torch.tensor([-0.01, -0.2], device=DEV)
+    offsets = torch.tensor([0, 100, 59000, 59990], dtype=torch.int32, device=DEV)
+    c = lambda t: t.contiguous()  # noqa: E731
+    want = block.decay_attention(c(q), c(k), c(v), A, offsets=offsets, y=torch.zeros_like(c(v)))
+    block.decay_attention(q, k, v, A, offsets=offsets, y=y)
+    assert torch.equal(y, want) and bool((y[59990:] == 0).all()) and bool(y[59000:59990].any())
+    some = ["dq", "dk", "dv"]
+    new = lambda: {n: torch.zeros((tokens, heads, d), device=DEV, dtype=B) for n in some}  # noqa: E731
+    want = block.decay_attention_grad(c(dy), c(q), c(k), c(v), A, offsets=offsets, want=some, out=new())
+    got = block.decay_attention_grad(dy, q, k, v, A, offsets=offsets, want=some, out=new())
+    assert all(torch.equal(got[n], want[n]) and bool(got[n][59000:59990].any()) for n in some)
