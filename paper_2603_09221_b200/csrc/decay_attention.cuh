@@ -148,7 +148,6 @@ __device__ __forceinline__ float to_end(const Decays& d, int t)
         e += d.block[b];
     return ex2(e);
 }
-__device__ __forceinline__ float over_chunk(const Decays& d) { return ex2((d.block[0] + d.block[1]) + (d.block[2] + d.block[3])); }
 // from behind token t of an earlier block to the begin of block b
 __device__ __forceinline__ float to_block(const Decays& d, int t, int b)
 {
@@ -203,16 +202,24 @@ __device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chun
 template <typename T, int COLS, int THREADS> __device__ __forceinline__ void store_tile(const char* from, const Rows& r, const Chunk& c, int head, int width, bool vec)
 {
     T* base = row_ptr<T>(r, c.seq, c.row0) + (long long)head * width;
-    for (int e = threadIdx.x; e < kChunk * COLS / 8; e += THREADS) {
-        const int row = e / (COLS / 8), c8 = e % (COLS / 8);
-        if (row >= c.len || c8 * 8 >= width)
-            continue;
-        const uint4 w = *reinterpret_cast<const uint4*>(from + tile_at(row, c8));
+    constexpr int N = kChunk * COLS / 8 / THREADS;                   // vectors of a thread: of one place in every THREADS / (COLS / 8)-th row
+    const int c8 = threadIdx.x % (COLS / 8), row0 = threadIdx.x / (COLS / 8);
+    if (c8 * 8 >= width)
+        return;
+    uint4 w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        w[i] = *reinterpret_cast<const uint4*>(from + tile_at(row0 + i * (THREADS / (COLS / 8)), c8));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int row = row0 + i * (THREADS / (COLS / 8));
         T* at = base + row * r.ts + c8 * 8;
+        if (row >= c.len)
+            break;
         if (vec) {
-            *reinterpret_cast<uint4*>(at) = w;
+            *reinterpret_cast<uint4*>(at) = w[i];
         } else {
-            const Vec<T, 8> u = *reinterpret_cast<const Vec<T, 8>*>(&w);
+            const Vec<T, 8> u = *reinterpret_cast<const Vec<T, 8>*>(&w[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (c8 * 8 + j < width)
@@ -268,17 +275,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16])
                  :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
                     "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const float (&v)[32])
-{
-    uint32_t r[16];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-            r[i] = __float_as_uint(v[h * 16 + i]);
-        tmem_st16(at + h * 16, r);
-    }
-}
 __device__ __forceinline__ void tmem_st_done() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void before_barrier() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void behind_barrier() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -328,7 +324,7 @@ extern __shared__ __align__(1024) char dattn_tiles[];
 
 // Barriers and tensor memory of a block.
 struct Control {
-    uint64_t bar[4];
+    uint64_t bar[3];
     uint32_t tmem;
     int dead;
 };
@@ -336,7 +332,7 @@ struct Control {
 __device__ __forceinline__ uint32_t set_up(Control& c, int columns)
 {
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 3; ++i)
             asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&c.bar[i])) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         c.dead = 0;

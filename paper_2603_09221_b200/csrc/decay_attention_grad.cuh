@@ -51,6 +51,7 @@ template <int DK, int DV> struct GradShape {
     static constexpr int TILES = 2 * K_BYTES + 2 * V_BYTES + 2 * IMAGE;
     struct Small {
         Control ctl;
+        uint64_t tiles, image;                                       // what has come: the tiles, two terms of the image
         uint64_t second_product, third, third_product;               // of the images' terms: products that are done, the third term is there
         Decays dec;
         alignas(16) float to[4][96];             // [block][earlier token]: decay from it to the block's begin
@@ -60,10 +61,27 @@ template <int DK, int DV> struct GradShape {
     static constexpr int SMEM = TILES + sizeof(Small);
 };
 
+// N products of 16 indices each, one behind the other; STEP: 16 bytes from an operand's 16 indices to the next ones.  Rolled up, as whatever need not lie in registers here: a block goes
+// through its code once, and waited for instructions more than for anything else (the tensor cores take 64 clocks for one of these).
+constexpr int kColumns = 0, kTokens = 128;                           // (over columns: 2, and from box to box)
+template <int STEP> __device__ __forceinline__ uint64_t step_to(int s) { return STEP == kColumns ? (s / 4) * (kBox >> 4) + (s % 4) * 2 : s * STEP; }
+template <int N, int A, int B> __device__ __forceinline__ void products(uint32_t d, uint64_t a, uint64_t b, uint32_t id, bool add)
+{
+#pragma unroll 1
+    for (int s = 0; s < N; ++s)
+        mma(d, a + step_to<A>(s), b + step_to<B>(s), id, add || s > 0);
+}
+template <int N, int B> __device__ __forceinline__ void products_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t id)
+{
+#pragma unroll 1
+    for (int s = 0; s < N; ++s)
+        mma_tmem(d, a + s * 8, b + step_to<B>(s), id, 1);
+}
+
 // A quarter of a row of results (COLS / 4 of tensor memory's columns), times f, staged in a tile.
 template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32_t from, char* tile, int row, int sub, float f)
 {
-#pragma unroll
+#pragma unroll 1
     for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
         float v[16];
         tmem_ld16(from + sub * (COLS / 4) + c0, v);
@@ -79,7 +97,7 @@ template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32
 template <int COLS> __device__ __forceinline__ float4* part_at(char* area, int row, int c4) { return reinterpret_cast<float4*>(area) + row * (COLS / 4) + (c4 ^ (row & 7)); }
 template <int COLS> __device__ __forceinline__ void stage_part(uint32_t from, char* area, int row, int sub, float f)
 {
-#pragma unroll
+#pragma unroll 1
     for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
         float v[16];
         tmem_ld16(from + sub * (COLS / 4) + c0, v);
@@ -114,7 +132,7 @@ template <int COLS> __device__ __forceinline__ void store_part(char* area, float
 template <typename T, int COLS> __device__ __forceinline__ float weigh_row(uint32_t at, const char* tile, int row, int sub, float f)
 {
     float dot = 0.f;
-#pragma unroll
+#pragma unroll 1
     for (int c0 = 0; c0 < COLS / 4; c0 += 16) {
         float v[16];
         const uint32_t here = at + sub * (COLS / 4) + c0;
@@ -153,8 +171,18 @@ __device__ __forceinline__ void fetch_bytes_to_l2(const char* from, uint32_t byt
     asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" :: "l"(from), "r"(bytes) : "memory");
 }
 
-// The tiles and the image of a chunk and head, and its decays.  What the block that will run behind this one needs is asked for into L2, so that memory is at work while this
-// one computes.
+// Chunk and head of a block: those of one head one behind the other, both ways (dk and dv, dq) of a chunk together.
+struct GradPlace {
+    int chunk, head;
+    bool kv;
+};
+__device__ __forceinline__ GradPlace grad_place(const GradDev& g, unsigned id)
+{
+    const unsigned ways = g.want_q && g.want_kv ? 2 : 1, job = id / ways, chunks = (unsigned)g.f.chunks;
+    return GradPlace{(int)(job % chunks), (int)(job / chunks), g.want_kv && (ways == 1 || id % 2 == 0)};
+}
+
+// The tiles of a chunk and head and its decays; its image is asked for.  The copies are under way before tensor memory is taken.
 template <typename T, int DK, int DV, bool KV>
 __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& there, const Maps& back, const Chunk& c, long long at, int head, typename GradShape<DK, DV>::Small& sm,
                                                uint32_t tiles)
@@ -163,20 +191,13 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
     const AttnDev& p = g.f;
     const int group = head / p.share, warp = threadIdx.x / 32;
     const uint32_t queries = tiles, keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
-    const char* from = (KV ? g.image_Z : g.image_S) + at * ((long long)g.terms * S::IMAGE);
-    float l = 0.f;
-    if (warp < 4)
-        l = log_decay_at<T>(p, c, head, threadIdx.x);
-    if (threadIdx.x == 0) {
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.second_product)) : "memory");
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.third)) : "memory");
-        asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(&sm.third_product)) : "memory");
-    }
-    const uint32_t tmem = set_up(sm.ctl, 512);
-    const uint32_t bar = smem_u32(&sm.ctl.bar[3]);
     const bool engine = there.there && back.there && (!p.seqs.offsets || c.len == kChunk);
-    if (threadIdx.x == 32 * 15) {
-        expect_bytes(bar, 2 * S::IMAGE + (engine ? 2 * S::K_BYTES + 2 * S::V_BYTES : 0));
+    const uint32_t bar = smem_u32(&sm.tiles);
+    if (threadIdx.x == kGradThreads - 32) {
+        for (uint64_t* b : {&sm.tiles, &sm.image, &sm.second_product, &sm.third, &sm.third_product})
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" :: "r"(smem_u32(b)) : "memory");
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        expect_bytes(bar, engine ? 2 * S::K_BYTES + 2 * S::V_BYTES : 0);
         if (engine) {
             const int row0 = (int)c.row0, seq = (int)c.seq;
             for (int b = 0; b < DV / 64; ++b) {
@@ -188,25 +209,13 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
                 fetch_box(queries + b * kBox, &back.k, b * 64, group, row0, seq, bar);
             }
         }
-        fetch_bytes(image, from, 2 * S::IMAGE, bar);
-        const int ways = g.want_q && g.want_kv ? 2 : 1;
-        const long long next = (long long)blockIdx.x + g.resident, ci = next / ways % p.chunks, h = next / ways / p.chunks;
-        if (engine && next < gridDim.x) {
-            const Chunk n = chunk_at(p, ci);
-            if (n.len > 0) {
-                const int row0 = (int)n.row0, seq = (int)n.seq;
-                for (int b = 0; b < DV / 64; ++b) {
-                    fetch_to_l2(&there.v, b * 64, (int)h, row0, seq);
-                    fetch_to_l2(&back.v, b * 64, (int)h, row0, seq);
-                }
-                for (int b = 0; b < DK / 64; ++b) {
-                    fetch_to_l2(&there.k, b * 64, (int)h / p.share, row0, seq);
-                    fetch_to_l2(&back.k, b * 64, (int)h / p.share, row0, seq);
-                }
-                fetch_bytes_to_l2((g.want_kv && (ways == 1 || next % 2 == 0) ? g.image_Z : g.image_S) + (ci * p.heads + h) * ((long long)g.terms * S::IMAGE), g.terms * S::IMAGE);
-            }
-        }
+        expect_bytes(smem_u32(&sm.image), 2 * S::IMAGE);
+        fetch_bytes(image, (KV ? g.image_Z : g.image_S) + at * ((long long)g.terms * S::IMAGE), 2 * S::IMAGE, smem_u32(&sm.image));
     }
+    float l = 0.f;
+    if (warp < 4)
+        l = log_decay_at<T>(p, c, head, threadIdx.x);
+    const uint32_t tmem = set_up(sm.ctl, 512);
     if (!engine) {
         load_tile<T, DK, kGradThreads>(queries, p.q, c, group * p.dk, p.dk, p.vec_q, threadIdx.x);
         load_tile<T, DK, kGradThreads>(keys, p.k, c, group * p.dk, p.dk, p.vec_k, threadIdx.x);
@@ -227,6 +236,29 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
     __syncthreads();
     behind_barrier();
     return tmem;
+}
+// What the block that will run behind this one needs is asked for into L2, so that memory is at work while this one computes.  By a thread that has nothing else to do.
+template <int DK, int DV> __device__ __forceinline__ void fetch_next(const GradDev& g, const Maps& there, const Maps& back)
+{
+    const AttnDev& p = g.f;
+    const unsigned next = blockIdx.x + g.resident;
+    if (!there.there || !back.there || next >= gridDim.x)
+        return;
+    const GradPlace where = grad_place(g, next);
+    const Chunk n = chunk_at(p, where.chunk);
+    if (n.len <= 0)
+        return;
+    const int row0 = (int)n.row0, seq = (int)n.seq, group = where.head / p.share;
+    for (int b = 0; b < DV / 64; ++b) {
+        fetch_to_l2(&there.v, b * 64, where.head, row0, seq);
+        fetch_to_l2(&back.v, b * 64, where.head, row0, seq);
+    }
+    for (int b = 0; b < DK / 64; ++b) {
+        fetch_to_l2(&there.k, b * 64, group, row0, seq);
+        fetch_to_l2(&back.k, b * 64, group, row0, seq);
+    }
+    const int bytes = g.terms * GradShape<DK, DV>::IMAGE;
+    fetch_bytes_to_l2((where.kv ? g.image_Z : g.image_S) + ((long long)where.chunk * p.heads + where.head) * bytes, bytes);
 }
 __device__ __forceinline__ void grad_products_done(Control& c, int i)
 {
@@ -252,14 +284,12 @@ __device__ __forceinline__ void end_grad(Control& c, uint32_t tmem)
 
 // dq of one chunk and head, lanes for the tokens i, a block of 32 tokens j to each of a row's four warps: scores and dy v' into tensor memory beside S_0 dy; M's row sums from both;
 // dy v' with its decays goes back in 16 bits and is multiplied with the keys.
-template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(const GradDev& g, const Maps& there, const Maps& back)
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(const GradDev& g, const Maps& there, const Maps& back, const GradPlace& where)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    const int ways = g.want_q && g.want_kv ? 2 : 1;
-    const long long ci = blockIdx.x / ways % p.chunks;
-    const int head = (int)(blockIdx.x / ways / p.chunks);
-    const long long at = ci * p.heads + head;
+    const long long ci = where.chunk, at = ci * p.heads + where.head;
+    const int head = where.head;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
@@ -272,43 +302,45 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
     const uint32_t tmem = begin_grad<T, DK, DV, false>(g, there, back, c, at, head, sm, queries);        // scores, dy v', results: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, results = tmem + 256, lanes = (uint32_t)(quarter * 32) << 16;
     if (warp == 0) {
-        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_state = instruction(kIsBf16<T>, false, false, 128, DK);
+        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128);
         if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(slopes, over_columns(dys, s), over_columns(values, s), id, s > 0);
-#pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                mma(scores, over_columns(queries, s), over_columns(keys, s), id, s > 0);
+            products<DV / 16, kColumns, kColumns>(slopes, over_columns(dys, 0), over_columns(values, 0), id, false);
+            products<DK / 16, kColumns, kColumns>(scores, over_columns(queries, 0), over_columns(keys, 0), id, false);
             commit(smem_u32(&sm.ctl.bar[0]));
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)    // the small ones first: the tensor cores cut sums off
-                mma(results, over_columns(dys, s), image_over_dv<DK>(image + S::IMAGE, s), id_state, s > 0);
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(results, over_columns(dys, s), image_over_dv<DK>(image, s), id_state, 1);
+        }
+        __syncwarp();
+    }
+    if (warp == 12) {                            // (which has no pairs to weigh, as warp 8)
+        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, DK);
+        await(smem_u32(&sm.image), 0, &sm.ctl.dead);
+        __syncwarp();
+        if (elect_one()) {
+            products<DV / 16, kColumns, 2 * DK>(results, over_columns(dys, 0), image_over_dv<DK>(image + S::IMAGE, 0), id, false); // the small ones first: the tensor cores cut sums off
+            products<DV / 16, kColumns, 2 * DK>(results, over_columns(dys, 0), image_over_dv<DK>(image, 0), id, true);
             commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
+        if (g.terms == 3) {                      // the third term takes the values' place
+            grad_products_done(sm.ctl, 0);
+            if (elect_one()) {
+                expect_bytes(smem_u32(&sm.third), S::IMAGE);
+                fetch_bytes(values, g.image_S + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
+            }
+            __syncwarp();
+            await(smem_u32(&sm.third), 0, &sm.ctl.dead);
+            __syncwarp();
+            if (elect_one()) {
+                products<DV / 16, kColumns, 2 * DK>(results, over_columns(dys, 0), image_over_dv<DK>(values, 0), id, true);
+                commit(smem_u32(&sm.third_product));
+            }
+            __syncwarp();
+        }
+    } else if (warp == 8) {
+        if (elect_one())
+            fetch_next<DK, DV>(g, there, back);
+        __syncwarp();
     }
     grad_products_done(sm.ctl, 0);
-    if (g.terms == 3 && warp == 12) {            // the third term takes the values' place (this warp has nothing else to do)
-        if (elect_one()) {
-            expect_bytes(smem_u32(&sm.third), S::IMAGE);
-            fetch_bytes(values, g.image_S + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
-        }
-        __syncwarp();
-        await(smem_u32(&sm.third), 0, &sm.ctl.dead);
-        __syncwarp();
-        constexpr uint32_t id_state = instruction(kIsBf16<T>, false, false, 128, DK);
-        if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(results, over_columns(dys, s), image_over_dv<DK>(values, s), id_state, 1);
-            commit(smem_u32(&sm.third_product));
-        }
-        __syncwarp();
-    }
     const int row = quarter * 32 + lane;
     uint32_t packed[16];
     float row_sum = 0.f;
@@ -369,9 +401,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
         behind_barrier();
         constexpr uint32_t id = instruction(kIsBf16<T>, false, true, 128, DK);
         if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                mma_tmem(results, slopes + s * 8, over_tokens(keys, s), id, 1);
+            products_tmem<8, kTokens>(results, slopes, over_tokens(keys, 0), id);
             commit(smem_u32(&sm.ctl.bar[2]));
         }
         __syncwarp();
@@ -428,14 +458,12 @@ __device__ __forceinline__ void decay_column(float (&v)[32], float (&w)[32], con
 }
 
 // dk and dv of one chunk and head, lanes for the tokens j, a block of 32 tokens i to each of a row's four warps.
-template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(const GradDev& g, const Maps& there, const Maps& back)
+template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(const GradDev& g, const Maps& there, const Maps& back, const GradPlace& where)
 {
     using S = GradShape<DK, DV>;
     const AttnDev& p = g.f;
-    const int ways = g.want_q && g.want_kv ? 2 : 1;
-    const long long ci = blockIdx.x / ways % p.chunks;
-    const int head = (int)(blockIdx.x / ways / p.chunks);
-    const long long at = ci * p.heads + head;
+    const long long ci = where.chunk, at = ci * p.heads + where.head;
+    const int head = where.head;
     const int warp = __shfl_sync(0xffffffffu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, quarter = warp % 4, sub = warp / 4;
     const Chunk c = chunk_at(p, ci);
     if (c.len <= 0)
@@ -450,48 +478,46 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
     const uint32_t tmem = begin_grad<T, DK, DV, true>(g, there, back, c, at, head, sm, queries);         // scores, v dy', dk, dv: 128 columns each
     const uint32_t scores = tmem, slopes = tmem + 128, dks = tmem + 256, dvs = tmem + 384, lanes = (uint32_t)(quarter * 32) << 16;
     if (warp == 0) {
-        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128), id_k = instruction(kIsBf16<T>, false, false, 128, DK),
-                           id_v = instruction(kIsBf16<T>, false, true, 128, DV);
+        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128);
         if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(slopes, over_columns(values, s), over_columns(dys, s), id, s > 0);
-#pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                mma(scores, over_columns(keys, s), over_columns(queries, s), id, s > 0);
+            products<DV / 16, kColumns, kColumns>(slopes, over_columns(values, 0), over_columns(dys, 0), id, false);
+            products<DK / 16, kColumns, kColumns>(scores, over_columns(keys, 0), over_columns(queries, 0), id, false);
             commit(smem_u32(&sm.ctl.bar[0]));
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(dks, over_columns(values, s), image_over_dv<DK>(image + S::IMAGE, s), id_k, s > 0);
-            commit(smem_u32(&sm.second_product));
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(dks, over_columns(values, s), image_over_dv<DK>(image, s), id_k, 1);
-#pragma unroll
-            for (int s = 0; s < DK / 16; ++s)
-                mma(dvs, over_columns(keys, s), image_over_dk<DK>(image, s), id_v, s > 0);
-            commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
     }
-    if (g.terms == 3 && warp == 3) {             // the third term takes the second one's place (this warp has nothing else to do)
-        await(smem_u32(&sm.second_product), 0, &sm.ctl.dead);
+    if (warp == 3) {                             // (which has no pairs to weigh, as warp 2)
+        constexpr uint32_t id_k = instruction(kIsBf16<T>, false, false, 128, DK), id_v = instruction(kIsBf16<T>, false, true, 128, DV);
+        await(smem_u32(&sm.image), 0, &sm.ctl.dead);
         __syncwarp();
-        behind_barrier();
         if (elect_one()) {
-            expect_bytes(smem_u32(&sm.third), S::IMAGE);
-            fetch_bytes(image + S::IMAGE, g.image_Z + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
+            products<DV / 16, kColumns, 2 * DK>(dks, over_columns(values, 0), image_over_dv<DK>(image + S::IMAGE, 0), id_k, false);
+            commit(smem_u32(&sm.second_product));
+            products<DV / 16, kColumns, 2 * DK>(dks, over_columns(values, 0), image_over_dv<DK>(image, 0), id_k, true);
+            products<DK / 16, kColumns, 16>(dvs, over_columns(keys, 0), image_over_dk<DK>(image, 0), id_v, false);
+            commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
-        await(smem_u32(&sm.third), 0, &sm.ctl.dead);
-        __syncwarp();
-        constexpr uint32_t id_k = instruction(kIsBf16<T>, false, false, 128, DK);
-        if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < DV / 16; ++s)
-                mma(dks, over_columns(values, s), image_over_dv<DK>(image + S::IMAGE, s), id_k, 1);
-            commit(smem_u32(&sm.third_product));
+        if (g.terms == 3) {                      // the third term takes the second one's place
+            await(smem_u32(&sm.second_product), 0, &sm.ctl.dead);
+            __syncwarp();
+            behind_barrier();
+            if (elect_one()) {
+                expect_bytes(smem_u32(&sm.third), S::IMAGE);
+                fetch_bytes(image + S::IMAGE, g.image_Z + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
+            }
+            __syncwarp();
+            await(smem_u32(&sm.third), 0, &sm.ctl.dead);
+            __syncwarp();
+            if (elect_one()) {
+                products<DV / 16, kColumns, 2 * DK>(dks, over_columns(values, 0), image_over_dv<DK>(image + S::IMAGE, 0), id_k, true);
+                commit(smem_u32(&sm.third_product));
+            }
+            __syncwarp();
         }
+    } else if (warp == 2) {
+        if (elect_one())
+            fetch_next<DK, DV>(g, there, back);
         __syncwarp();
     }
     grad_products_done(sm.ctl, 0);
@@ -547,12 +573,8 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         behind_barrier();
         constexpr uint32_t id_k = instruction(kIsBf16<T>, false, true, 128, DK), id_v = instruction(kIsBf16<T>, false, true, 128, DV);
         if (elect_one()) {
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                mma_tmem(dvs, scores + s * 8, over_tokens(dys, s), id_v, 1);
-#pragma unroll
-            for (int s = 0; s < 8; ++s)
-                mma_tmem(dks, slopes + s * 8, over_tokens(queries, s), id_k, 1);
+            products_tmem<8, kTokens>(dvs, scores, over_tokens(dys, 0), id_v);
+            products_tmem<8, kTokens>(dks, slopes, over_tokens(queries, 0), id_k);
             commit(smem_u32(&sm.ctl.bar[2]));
         }
         __syncwarp();
@@ -585,10 +607,11 @@ template <typename T, int DK, int DV>
 __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Maps there, const __grid_constant__ Maps back, const GradDev g)
 {
     wait_for_previous();
-    if (g.want_kv && !(g.want_q && blockIdx.x % 2))
-        grad_kv<T, DK, DV>(g, there, back);
+    const GradPlace where = grad_place(g, blockIdx.x);
+    if (where.kv)
+        grad_kv<T, DK, DV>(g, there, back, where);
     else
-        grad_q<T, DK, DV>(g, there, back);
+        grad_q<T, DK, DV>(g, there, back, where);
 }
 
 // exp(G_C) <Z, S_0> of each chunk and head from the images of both, where the walks ran side by side.
