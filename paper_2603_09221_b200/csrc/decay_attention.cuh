@@ -244,6 +244,22 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint64_t b, uin
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n"
                  :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
+// N products of 16 indices each, one behind the other; STEP: 16 bytes from an operand's 16 indices to the next ones.  Rolled up, as whatever need not lie in registers here: a block goes
+// through its code once, and waited for instructions more than for anything else (the tensor cores take 64 clocks for one of these).
+constexpr int kColumns = 0, kTokens = 128;                           // (over columns: 2, and from box to box)
+template <int STEP> __device__ __forceinline__ uint64_t step_to(int s) { return STEP == kColumns ? (s / 4) * (kBox >> 4) + (s % 4) * 2 : s * STEP; }
+template <int N, int A, int B> __device__ __forceinline__ void products(uint32_t d, uint64_t a, uint64_t b, uint32_t id, bool add)
+{
+#pragma unroll 1
+    for (int s = 0; s < N; ++s)
+        mma(d, a + step_to<A>(s), b + step_to<B>(s), id, add || s > 0);
+}
+template <int N, int B> __device__ __forceinline__ void products_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t id)
+{
+#pragma unroll 1
+    for (int s = 0; s < N; ++s)
+        mma_tmem(d, a + s * 8, b + step_to<B>(s), id, 1);
+}
 __device__ __forceinline__ void tmem_ld16(uint32_t at, float (&v)[16])
 {
     uint32_t r[16];
@@ -293,6 +309,27 @@ template <> __device__ __forceinline__ uint32_t pack16<__half>(float a, float b)
 template <typename T> __device__ __forceinline__ float2 unpack16(uint32_t v);
 template <> __device__ __forceinline__ float2 unpack16<bf16>(uint32_t v) { return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u)); }
 template <> __device__ __forceinline__ float2 unpack16<__half>(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+
+// In pairs: half the instructions of a loop over the numbers.
+template <int N> __device__ __forceinline__ void scale_all(float (&v)[N], float f)
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2)
+        unpack2(mul2(pack2(v[j], v[j + 1]), pack2(f, f)), v[j], v[j + 1]);
+}
+template <int N> __device__ __forceinline__ void add_all(float (&v)[N], const float (&w)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2)
+        unpack2(add2(pack2(v[j], v[j + 1]), pack2(w[j], w[j + 1])), v[j], v[j + 1]);
+}
+// S = over S + u
+template <int N> __device__ __forceinline__ void carry_all(float (&S)[N], float over, const float (&u)[N])
+{
+#pragma unroll
+    for (int j = 0; j < N; j += 2)
+        unpack2(fma2(pack2(over, over), pack2(S[j], S[j + 1]), pack2(u[j], u[j + 1])), S[j], S[j + 1]);
+}
 
 template <typename T> constexpr bool kIsBf16 = std::is_same<T, bf16>::value;
 
@@ -762,11 +799,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
         auto score_products = [&](int i) {
             behind_barrier();
             constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, 128);
-            const uint64_t a = over_columns(queries_at(i), 0), b = over_columns(keys_at(i), 0);
             if (elect_one()) {
-#pragma unroll
-                for (int s = 0; s < DK / 16; ++s)
-                    mma(scores, a + (s / 4 * kBox + s % 4 * 32 >> 4), b + (s / 4 * kBox + s % 4 * 32 >> 4), id, s > 0);
+                products<DK / 16, kColumns, kColumns>(scores, over_columns(queries_at(i), 0), over_columns(keys_at(i), 0), id, false);
                 commit(smem_u32(&sm.scores));
             }
             __syncwarp();
@@ -779,12 +813,9 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             until(sm.imaged, i);
             behind_barrier();
             constexpr uint32_t id = instruction(kIsBf16<T>, false, true, 128, kCols);
-            const uint64_t a = over_columns(queries_at(i), 0), state = image_over_dk<DK>(image, 0), values = over_tokens(values_at(i), 0);
             const uint32_t to = results_at(i);
             if (elect_one()) {
-#pragma unroll
-                for (int s = 0; s < DK / 16; ++s)
-                    mma(to, a + (s / 4 * kBox + s % 4 * 32 >> 4), state + (s * 256 >> 4), id, s > 0);
+                products<DK / 16, kColumns, 16>(to, over_columns(queries_at(i), 0), image_over_dk<DK>(image, 0), id, false);
                 commit(smem_u32(&sm.state));
             }
             __syncwarp();
@@ -792,11 +823,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             behind_barrier();
             {
                 constexpr uint32_t id_added = instruction(kIsBf16<T>, true, true, 128, TERMS * kCols); // all terms beside one another: the keys are read once
-                const uint64_t keys = over_tokens(keys_at(i), 0), terms = over_tokens(weighted, 0);
                 if (elect_one()) {
-#pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        mma(added, keys + (s * 2048 >> 4), terms + (s * 2048 >> 4), id_added, s > 0);
+                    products<8, kTokens, kTokens>(added, over_tokens(keys_at(i), 0), over_tokens(weighted, 0), id_added, false);
                     commit(smem_u32(&sm.added));
                 }
                 __syncwarp();
@@ -804,9 +832,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             until(sm.weighed, i);
             behind_barrier();
             if (elect_one()) {
-#pragma unroll
-                for (int s = 0; s < 8; ++s)
-                    mma_tmem(to, operand + s * 8, values + (s * 2048 >> 4), id, 1);
+                products_tmem<8, kTokens>(to, operand, over_tokens(values_at(i), 0), id);
                 commit(smem_u32(&sm.out));
             }
             __syncwarp();
@@ -892,12 +918,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             before_barrier();
             warp_arrives(smem_u32(&sm.weighted));
         };
-        if (n > 0) {
-            put_image();
-            put_values(0);
-        }
-        for (int i = 0; i < n; ++i) {
-            const Chunk c = chunk_of(piece, i);
+        // scores times decays, q S_0 times exp(G_i), the state behind the chunk
+        auto weigh = [&](int i) {
             const Table& dec = sm.dec[i & 1];
             const float across = dec.whole;
             const float mine = dec.g[row], own = ex2(mine) * p.scale, f = own * dec.before[quarter] * unit;
@@ -937,11 +959,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             behind_barrier();
             float v[16];
             tmem_ld16(results_at(i) + sub * 16 + lanes, v);
-            uint32_t u[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                u[j] = __float_as_uint(v[j] * f);
-            tmem_st16(results_at(i) + sub * 16 + lanes, u);
+            scale_all(v, f);
+            tmem_st16(results_at(i) + sub * 16 + lanes, reinterpret_cast<const uint32_t(&)[16]>(v));
             tmem_st_done();
             before_barrier();
             warp_arrives(smem_u32(&sm.weighed));
@@ -954,18 +973,17 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                 for (int t = TERMS - 2; t >= 0; --t) {
                     float v[16];
                     tmem_ld16(added + t * kCols + sub * 16 + lanes, v);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        u[j] += v[j];
+                    add_all(u, v);
                 }
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    S[j] = fmaf(across, S[j], u[j] * unit_v);
+                if (!kIsBf16<T>)
+                    scale_all(u, unit_v);
+                carry_all(S, across, u);
             }
-            if (i + 1 < n) {
-                put_image();
-                put_values(i + 1);
-            }
+        };
+        // (the products' sum) to memory
+        auto put_results = [&](int i) {
+            const Chunk c = chunk_of(piece, i);
+            float v[16];
             until(sm.out, i);
             behind_barrier();
             tmem_ld16(results_at(i) + sub * 16 + lanes, v);
@@ -1004,6 +1022,16 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                 before_barrier();
                 warp_arrives(smem_u32(&sm.freed[i & 1]));
             }
+        };
+        for (int i = -1; i < n; ++i) {           // (what is made for the next chunk has its code once: the first passes through it wait for instructions)
+            if (i >= 0)
+                weigh(i);
+            if (i + 1 < n) {
+                put_image();
+                put_values(i + 1);
+            }
+            if (i >= 0)
+                put_results(i);
         }
         if (piece.last)
             store_state(S, p, p.state_out, piece.owner, head, row, col0 + sub * 16);
@@ -1225,7 +1253,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             const uint64_t a = over_tokens(keys_at(i), 0), b = over_tokens(weighted + i % S_::TURNS * (TERMS * S_::V_BYTES), 0);
             const uint32_t to = tmem + i % S_::TURNS * (TERMS * COLS);
             if (elect_one()) {
-#pragma unroll
+#pragma unroll 1
                 for (int s = 0; s < 8; ++s) {
                     mma(to, a + (s * 2048 >> 4), b + (s * 2048 >> 4), id, s > 0);
                     if constexpr (REST > 0)
@@ -1299,9 +1327,12 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             warp_arrives(smem_u32(&sm.weighted[i & 1]));
             unit_of[i & 1] = unit_v;
         };
-        if (n > 0)
-            put_values(0);
-        for (int i = 0; i < n; ++i) {
+        for (int i = -1; i < n; ++i) {           // (what is made for the next chunk has its code once)
+            if (i < 0) {
+                if (n > 0)
+                    put_values(0);
+                continue;
+            }
             const typename S_::Weights& dec = sm.dec[i & 1];
             uint4 other[OWN / 8][TERMS];         // asked for early
             const long long at = (first + chunk(i)) * p.heads + head;
@@ -1385,13 +1416,10 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                     for (int t = TERMS - 2; t >= 0; --t) {
                         float v[16];
                         tmem_ld16(from + t * COLS + sub * OWN + j + lanes, v);
-#pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            u[k] += v[k];
+                        add_all(u, v);
                     }
-#pragma unroll
-                    for (int k = 0; k < 16; ++k)
-                        S[j + k] = fmaf(over, S[j + k], u[k] * (unit_v * q.factor));
+                    scale_all(u, unit_v * q.factor);
+                    carry_all(reinterpret_cast<float(&)[16]>(S[j]), over, u);
                 }
             }
             whole *= over;

@@ -61,23 +61,6 @@ template <int DK, int DV> struct GradShape {
     static constexpr int SMEM = TILES + sizeof(Small);
 };
 
-// N products of 16 indices each, one behind the other; STEP: 16 bytes from an operand's 16 indices to the next ones.  Rolled up, as whatever need not lie in registers here: a block goes
-// through its code once, and waited for instructions more than for anything else (the tensor cores take 64 clocks for one of these).
-constexpr int kColumns = 0, kTokens = 128;                           // (over columns: 2, and from box to box)
-template <int STEP> __device__ __forceinline__ uint64_t step_to(int s) { return STEP == kColumns ? (s / 4) * (kBox >> 4) + (s % 4) * 2 : s * STEP; }
-template <int N, int A, int B> __device__ __forceinline__ void products(uint32_t d, uint64_t a, uint64_t b, uint32_t id, bool add)
-{
-#pragma unroll 1
-    for (int s = 0; s < N; ++s)
-        mma(d, a + step_to<A>(s), b + step_to<B>(s), id, add || s > 0);
-}
-template <int N, int B> __device__ __forceinline__ void products_tmem(uint32_t d, uint32_t a, uint64_t b, uint32_t id)
-{
-#pragma unroll 1
-    for (int s = 0; s < N; ++s)
-        mma_tmem(d, a + s * 8, b + step_to<B>(s), id, 1);
-}
-
 // A quarter of a row of results (COLS / 4 of tensor memory's columns), times f, staged in a tile.
 template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32_t from, char* tile, int row, int sub, float f)
 {
