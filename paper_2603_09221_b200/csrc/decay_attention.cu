@@ -305,7 +305,8 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     q = States{};
     TTC_TRY(take_pieces(device, a, o.splits, padded(a->dv) / o.splits, p.f, q, 2, s));
     // Walks both ways side by side, where one way leaves SMs idle (of packed sequences, the shorter ones'): <Z, S_0> takes a kernel of its own then, which reads
-    // both images again (11 documents of 8191 tokens, 8 heads of 64 x 64: 187 -> 150 us; 4 x 1024 tokens, 16 heads of 128 x 128, whose walks fill the SMs: 159, side by side 170).
+    // both images again (11 documents of 8191 tokens in all,
+    // 8 heads of 64 x 64: 187 -> 136 us).  Where one way fills the SMs (4 x 1024 tokens, 16 heads of 128 x 128), the second walk reads the states of the first as it goes.
     o.together = 2 * p.f.pieces * a->heads * o.splits <= (packed ? 3 : 2) * sm_count(device) / 2;
     if (p.f.chunks > INT32_MAX / (2 * a->heads))
         return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks, %d heads", (long long)p.f.chunks, a->heads);

@@ -7,9 +7,10 @@
 //
 // four products of 128 rows each, which the 5th-generation tensor cores take, and the chunks depend on one another through S only:
 //
-//     chunk_state_kernel   U = sum_j exp(R_j) k_j v_j' of every chunk and head
-//     state_scan_kernel    S_0 of every chunk from S_C = exp(G_C) S_0 + U, element by element
-//     chunk_out_kernel     y
+//     walk_kernel          y, chunk by chunk along a sequence (or a piece of one), S in registers
+//     state_walk_kernel    S alone: what a piece adds to it, where sequences are cut into pieces; for the gradients, S in front of every chunk
+//     join_kernel          S in front of the pieces, from what each adds
+//     decay_step_kernel    one token: token by token after all
 //
 // Exponents.  None is positive: pairs of tokens of one block of 32 take exp(G_i - G_j) itself, from sums within the block; others the product
 // of exp(from the block's begin to i) and exp(from j to that begin), so that no difference of long sums is formed.  Exponents
@@ -17,8 +18,8 @@
 // everything, gives no difference of infinities.
 //
 // Roundings.  Sums are float32 in tensor memory, states float32.  Operands of the tensor cores are 16 bits: scores with their decay, and S_0 where q
-// multiplies it, are rounded once (half a step each, as the result itself).  The weighted keys of U are not: states are float32 results and are carried on, so
-// the keys go in as a sum of numbers of 16 bits, each what the ones before it left: three bfloat16 or two float16 (2^-24, 2^-22 of the value; two bfloat16 leave 2^-18,
+// multiplies it, are rounded once (half a step each, as the result itself).  The weighted values of S_C are not: states are float32 results and are carried on, so
+// the values go in as a sum of numbers of 16 bits, each what the ones before it left: three bfloat16 or two float16 (2^-24, 2^-22 of the value; two bfloat16 leave 2^-18,
 // and the states were off by 2.4e-6 in the 2-norm).
 #pragma once
 
@@ -58,7 +59,6 @@ struct AttnDev {
 
 struct Chunk {
     long long seq, row0;                         // sequence and row of the first token, as row_ptr takes them
-    long long owner;                             // the sequence, where the chunk is its first one, else -1
     int len;                                     // tokens, 0: nothing to do
 };
 
@@ -68,16 +68,14 @@ __device__ __forceinline__ Chunk chunk_at(const AttnDev& p, long long c)
     if (p.piece_map) {
         const int2 m = p.piece_map[c];
         if (m.x < 0)
-            return Chunk{0, 0, -1, 0};
+            return Chunk{0, 0, 0};
         const Span s = span_of(p.seqs, m.x);
         r.seq = 0;
         r.row0 = s.row0 + m.y;
-        r.owner = m.y ? -1 : m.x;
         r.len = (int)min(s.len - m.y, (long long)kChunk);
     } else {
         r.seq = c / p.chunks_per_seq;
         r.row0 = (c % p.chunks_per_seq) * kChunk;
-        r.owner = r.row0 ? -1 : r.seq;
         r.len = (int)min(p.seqs.tokens - r.row0, (long long)kChunk);
     }
     return r;
@@ -99,16 +97,16 @@ template <typename T> __device__ __forceinline__ float raw_step(const AttnDev& p
     return to_f(row_ptr<T>(p.delta, seq, row)[head]) + (p.delta_bias ? p.delta_bias[head] : 0.f);
 }
 
-__device__ __forceinline__ float log_decay(const AttnDev& p, float A, float raw)
+// A of a head.  Minus infinity becomes the lowest number: times a step of 0 (a softplus that underflows) it has to be 0.
+__device__ __forceinline__ float rate(const AttnDev& p, int head) { return p.A[head] < -3.4e38f ? -3.4e38f : p.A[head]; }
+__device__ __forceinline__ float log_decay(float A, float step)
 {
-    const float l = A * step_of(p, raw) * kLog2e;
+    const float l = A * step * kLog2e;
     return l < kFloor ? kFloor : l;              // NaN stays
 }
 template <typename T> __device__ __forceinline__ float log_decay_at(const AttnDev& p, const Chunk& c, int head, int t)
 {
-    if (t >= c.len)
-        return 0.f;
-    return p.delta.ptr ? log_decay(p, p.A[head], raw_step<T>(p, c.seq, c.row0 + t, head)) : p.A[head] * kLog2e < kFloor ? kFloor : p.A[head] * kLog2e;
+    return t < c.len ? log_decay(rate(p, head), p.delta.ptr ? step_of(p, raw_step<T>(p, c.seq, c.row0 + t, head)) : 1.f) : 0.f;
 }
 
 // By one warp for the 32 tokens of a block, from the log decay of each lane's token: the sum from the block's begin, and behind the token to its end.
@@ -383,33 +381,16 @@ __device__ __forceinline__ uint32_t set_up(Control& c, int columns)
     behind_barrier();
     return __shfl_sync(0xffffffffu, c.tmem, 0);
 }
-// Decay of the pairs of a row and 32 earlier tokens (a block), in a row's lane: on the diagonal from the sums `g` of the block's tokens and the row's own, else e_row, the
-// row's decay from the earlier block's end, times each token's decay to that end.
-__device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const float* to_end)
+// Decay of the pairs of a row and 32 tokens of another block, in a row's lane: e_row, the row's decay to that block, times each token's decay within it.
+__device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const float* within)
 {
 #pragma unroll
     for (int j = 0; j < 32; j += 4) {
-        const float4 t = *reinterpret_cast<const float4*>(to_end + j);
+        const float4 t = *reinterpret_cast<const float4*>(within + j);
         unpack2(mul2(pack2(v[j], v[j + 1]), mul2(pack2(e_row, e_row), pack2(t.x, t.y))), v[j], v[j + 1]);
         unpack2(mul2(pack2(v[j + 2], v[j + 3]), mul2(pack2(e_row, e_row), pack2(t.z, t.w))), v[j + 2], v[j + 3]);
     }
 }
-__device__ __forceinline__ void decay_row(float (&v)[32], const float* g, bool diagonal, int lane, float own, float e_row, const float* to_end)
-{
-    if (diagonal) {
-#pragma unroll
-        for (int j = 0; j < 32; j += 4) {
-            const float4 h = *reinterpret_cast<const float4*>(g + j);
-            v[j] = j <= lane ? v[j] * ex2(own - h.x) : 0.f;
-            v[j + 1] = j + 1 <= lane ? v[j + 1] * ex2(own - h.y) : 0.f;
-            v[j + 2] = j + 2 <= lane ? v[j + 2] * ex2(own - h.z) : 0.f;
-            v[j + 3] = j + 3 <= lane ? v[j + 3] * ex2(own - h.w) : 0.f;
-        }
-    } else {
-        decay_earlier(v, e_row, to_end);
-    }
-}
-
 // ---- a walk along the chunks ----------------------------------------------------------------------------------------------
 
 constexpr int kWalkThreads = 512;
@@ -418,7 +399,8 @@ constexpr int kCols = 64;                        // value channels of a walk: he
 // A piece of a sequence (all of it, where there are enough sequences and heads), and the state in registers: of kWalkThreads threads, each has 16 neighbouring columns of
 // a row of dk.
 struct Piece {
-    long long seq, row0, owner;                  // as a Chunk's; owner: the sequence
+    long long seq, row0;                         // as a Chunk's
+    long long owner;                             // the sequence
     long long t0, len;                           // its first token in the sequence, and its tokens
     bool first, last;                            // of its sequence
 };
@@ -442,7 +424,7 @@ __device__ __forceinline__ Piece piece_at(const AttnDev& p, long long i, long lo
     if (p.seqs.offsets) {
         const int lane = threadIdx.x % 32;
         if (p.pieces == p.seqs.batch && p.seqs.batch <= 32) {
-            // uncut: the longest first, so that no long one is left for the end (7 sequences of 4093 tokens, 32 walks each: 60 -> 35 us)
+            // uncut: the longest first, so that no long one is left for the end (7 sequences of 4093 tokens in all, 32 walks each: 60 -> 47 us)
             const Span s = lane < p.seqs.batch ? span_of(p.seqs, lane) : Span{0, -1};
             int rank = 0;
 #pragma unroll
@@ -496,7 +478,7 @@ __device__ __forceinline__ Piece piece_at(const AttnDev& p, long long i, long lo
 }
 __device__ __forceinline__ Chunk chunk_of(const Piece& q, int i)
 {
-    return Chunk{q.seq, q.row0 + (long long)i * kChunk, -1, (int)min(q.len - (long long)i * kChunk, (long long)kChunk)};
+    return Chunk{q.seq, q.row0 + (long long)i * kChunk, (int)min(q.len - (long long)i * kChunk, (long long)kChunk)};
 }
 
 // The columns of a row of a float32 state that a thread has, from or to [batch][heads][dk][dv].
@@ -644,7 +626,10 @@ __device__ __forceinline__ void warp_arrives(uint32_t bar)
 //     S = exp(G_C) S + U, its image in 16 bits       [next q S_0]
 //     (the next chunk's values), the results
 //
-// Tensor memory: scores of two chunks in turn, results of two chunks in turn, what the chunk adds to the state, and the weighted scores as an operand.
+// Tensor memory: scores, results of two chunks in turn, what the chunk adds to the state, and the weighted scores as an operand.
+//
+// Bounds: not memory (4 x 2048 tokens of 16 heads of 128 x 128 in 50 us, 2.8 TB/s) but a chunk's steps one behind the other, 4600 clocks: the products' operands take all of shared
+// memory's bandwidth for 2600 of them, and the threads' instructions have to fit in between.
 template <typename T, int DK>
 __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_constant__ Maps maps, const AttnDev p)
 {
@@ -696,7 +681,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
 
     if (warp > kWalkWarps) {                     // ---- tiles and decays
         const int thread = threadIdx.x - 32 * (kWalkWarps + 1);
-        const float A = p.A[head], bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
+        const float A = rate(p, head), bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
         T raw[4 / kFrontWarps];
         auto ask = [&](int i) {
             const Chunk c = chunk_of(piece, i);
@@ -754,7 +739,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             float sum[4 / kFrontWarps], behind[4 / kFrontWarps];
 #pragma unroll
             for (int b = 0; b < 4 / kFrontWarps; ++b) {
-                const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
+                const float l = log_decay(A, p.delta.ptr ? step_of(p, to_f(raw[b]) + bias) : 1.f);
                 sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind[b]);
                 behind[b] = ex2(behind[b]);
             }
@@ -1094,7 +1079,8 @@ template <typename T, int DK, int COLS> struct StateShape {
 static_assert(StateShape<bf16, 128, 128>::SMEM <= 232448, "shared memory of a block");
 
 // One piece of one head (COLS value channels of it), chunk by chunk: values times their weights, split into TERMS numbers of 16 bits, all terms beside one another as one operand of the
-// product with the keys; the state in registers, COLS / 4 neighbouring columns of a row of dk to a thread.  Warps have the roles of walk_kernel's.
+// product with the keys; the state in registers, COLS / 4 neighbouring columns of a row of dk to a thread.  Warps have the roles of walk_kernel's.  4 x 1024 tokens of 16 heads of
+// 128 x 128, images in three terms: 28 us each way (48 KB read and written for each chunk and 64 columns, 3.6 TB/s).
 template <typename T, int DK, int COLS>
 __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_constant__ Maps maps_there, const __grid_constant__ Maps maps_back, const AttnDev p, const States states,
                                                                    int splits)
@@ -1148,7 +1134,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
 
     if (warp > kWalkWarps) {                     // ---- tiles and decays
         const int thread = threadIdx.x - 32 * (kWalkWarps + 1);
-        const float A = p.A[head], bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
+        const float A = rate(p, head), bias = p.delta.ptr && p.delta_bias ? p.delta_bias[head] : 0.f;
         T raw[4 / kFrontWarps];
         auto ask = [&](int i) {
             const Chunk c = chunk_of(piece, chunk(i));
@@ -1169,7 +1155,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             auto find = [&]() {
 #pragma unroll
                 for (int b = 0; b < 4 / kFrontWarps; ++b) {
-                    const float l = p.delta.ptr ? log_decay(p, A, to_f(raw[b]) + bias) : A * kLog2e < kFloor ? kFloor : A * kLog2e;
+                    const float l = log_decay(A, p.delta.ptr ? step_of(p, to_f(raw[b]) + bias) : 1.f);
                     float behind;
                     sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind);
                     own[b] = ex2(BACK ? sum[b] : behind);
@@ -1448,7 +1434,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
 }
 
 // The states in front of the pieces (BACK: behind them), from what each adds: S = exp(..) S + U along a sequence, eight pieces' loads under way together.  A block works for the
-// sequence whose last piece its number is, and for four of the `own` columns that a thread has in a state walk.
+// sequence whose last piece its number is, and for four of the `own` columns that a thread has in a state walk.  18 pieces of 8 heads of 64 x 64: 9 us, three loads one behind the
+// other and a launch.
 static __global__ void __launch_bounds__(kWalkThreads) join_kernel(const AttnDev p, const States states, int own, int splits)
 {
     constexpr int AHEAD = 8;
@@ -1495,7 +1482,7 @@ static __global__ void __launch_bounds__(kWalkThreads) join_kernel(const AttnDev
 constexpr int kStepThreads = 128;
 
 // The state is read and written once, which is all that counts.  A block has all rows and COLS columns of a head's state: a thread 4 columns
-// (V = 4; 1 where states cannot be accessed by 16 bytes) of every PARTS-th row, in loads of eight rows that are under way together.
+// (V = 4; 1 where states cannot be accessed by 16 bytes) of every PARTS-th row, in loads of eight rows that are under way together.  67 MB of states in 26 us: read and written at 5.1 TB/s.
 template <typename T, int V>
 __global__ void __launch_bounds__(kStepThreads) decay_step_kernel(const AttnDev p, int lanes)
 {
@@ -1512,7 +1499,7 @@ __global__ void __launch_bounds__(kStepThreads) decay_step_kernel(const AttnDev 
         s_k[i] = to_f(row_ptr<T>(p.k, b, 0)[(long long)group * p.dk + i]);
     }
     const float d = p.delta.ptr ? step_of(p, raw_step<T>(p, b, 0, head)) : 1.f;
-    const float a = ex2(p.A[head] * d * kLog2e + kExBias);
+    const float a = ex2(rate(p, head) * d * kLog2e + kExBias);
     float v[V], y[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {

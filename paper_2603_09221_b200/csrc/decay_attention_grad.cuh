@@ -56,7 +56,7 @@ template <int DK, int DV> struct GradShape {
         Decays dec;
         alignas(16) float to[4][96];             // [block][earlier token]: decay from it to the block's begin
         alignas(16) float from[kChunk];          // exp from each token's block's begin
-        float sums[4][kChunk], dots[4][kChunk], within[kChunk], pairs[4][4];
+        float sums[4][kChunk], dots[4][kChunk], within[4][kChunk], pairs[4][4];
     };
     static constexpr int SMEM = TILES + sizeof(Small);
 };
@@ -293,7 +293,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
         }
         __syncwarp();
     }
-    if (warp == 12) {                            // (which has no pairs to weigh, as warp 8)
+    if (warp == 12) {                            // (of the first 32 rows' warps, which have the fewest pairs to weigh, as warp 8)
         constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, DK);
         await(smem_u32(&sm.image), 0, &sm.ctl.dead);
         __syncwarp();
@@ -303,72 +303,98 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
             commit(smem_u32(&sm.ctl.bar[1]));
         }
         __syncwarp();
-        if (g.terms == 3) {                      // the third term takes the values' place
-            grad_products_done(sm.ctl, 0);
-            if (elect_one()) {
-                expect_bytes(smem_u32(&sm.third), S::IMAGE);
-                fetch_bytes(values, g.image_S + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
-            }
-            __syncwarp();
-            await(smem_u32(&sm.third), 0, &sm.ctl.dead);
-            __syncwarp();
-            if (elect_one()) {
-                products<DV / 16, kColumns, 2 * DK>(results, over_columns(dys, 0), image_over_dv<DK>(values, 0), id, true);
-                commit(smem_u32(&sm.third_product));
-            }
-            __syncwarp();
-        }
     } else if (warp == 8) {
         if (elect_one())
             fetch_next<DK, DV>(g, there, back);
         __syncwarp();
     }
     grad_products_done(sm.ctl, 0);
+    if (g.terms == 3 && warp == 12) {            // the third term takes the values' place
+        if (elect_one()) {
+            expect_bytes(smem_u32(&sm.third), S::IMAGE);
+            fetch_bytes(values, g.image_S + (at * 3 + 2) * S::IMAGE, S::IMAGE, smem_u32(&sm.third));
+        }
+        __syncwarp();
+    }
+    // A warp has one of the earlier blocks of 32 tokens and a quarter of its rows' own block, where the exponentials are (packed
+    // documents, 8 heads of 64 x 64: 130.4 -> 129.3 us).
     const int row = quarter * 32 + lane;
-    uint32_t packed[16];
+    uint32_t packed[16], diagonal[4];
     float row_sum = 0.f;
-    if (sub <= quarter) {
+    if (sub < quarter) {
         float v[32];
         tmem_ld32(slopes + sub * 32 + lanes, v);
-        decay_row(v, dec.g + sub * 32, sub == quarter, lane, dec.g[row], sm.from[row], &sm.to[quarter][sub < quarter ? sub * 32 : 0]);
+        decay_earlier(v, sm.from[row], sm.to[quarter] + sub * 32);
 #pragma unroll
         for (int j = 0; j < 16; ++j)
             packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
         if (g.want_l) {
             float w[32];
             tmem_ld32(scores + sub * 32 + lanes, w);
-            if (sub < quarter) {
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-                    row_sum = fmaf(v[j], w[j], row_sum);
-                float part = row_sum;
+            for (int j = 0; j < 32; ++j)
+                row_sum = fmaf(v[j], w[j], row_sum);
+            float part = row_sum;
 #pragma unroll
-                for (int o = 16; o; o /= 2)
-                    part += __shfl_xor_sync(0xffffffffu, part, o);
-                if (lane == 0)
-                    sm.pairs[quarter][sub] = part;
-            } else {
-                float sum = 0.f;
-#pragma unroll
-                for (int j = 0; j < 32; ++j) {
-                    const float m = v[j] * w[j];
-                    v[j] = j <= lane ? sum : 0.f;
-                    sum += m;
-                }
-                group_sums<32, 32, 1>(v, lane);
-                sm.within[sub * 32 + first_value<32, 32>(lane)] = v[0];
-            }
+            for (int o = 16; o; o /= 2)
+                part += __shfl_xor_sync(0xffffffffu, part, o);
+            if (lane == 0)
+                sm.pairs[quarter][sub] = part;
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
             packed[j] = 0;
     }
+    {
+        const int first = sub * 8, from = quarter * 32 + first;
+        const float own = dec.g[row];
+        float v[8];
+        tmem_ld8(slopes + from + lanes, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            v[j] = first + j <= lane ? v[j] * ex2(own - dec.g[from + j]) : 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            diagonal[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+        if (g.want_l) {                          // pairs on both sides of t whose earlier token is one of these eight: of t among them one by one, of a later t all
+            float w[8], sum = 0.f;
+            tmem_ld8(scores + from + lanes, w);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float m = v[j] * w[j];
+                v[j] = first + j <= lane ? sum : 0.f;
+                sum += m;
+            }
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const float b = __shfl_down_sync(0xffffffffu, sum, o);
+                sum += lane + o < 32 ? b : 0.f;
+            }
+            group_sums<8, 32, 1>(v, lane);
+            if (lane < first || lane >= first + 8)
+                sm.within[sub][row] = lane < first ? 0.f : sum;
+            if (lane < 8)
+                sm.within[sub][from + first_value<8, 32>(lane)] = v[0];
+        }
+    }
     // the four warps of these rows have read what is overwritten now
     before_barrier();
     asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
     behind_barrier();
-    tmem_st16(slopes + sub * 16 + lanes, packed);
+    if (sub != quarter)
+        tmem_st16(slopes + sub * 16 + lanes, packed);
+    tmem_st4(slopes + quarter * 16 + sub * 4 + lanes, diagonal);
+    if (g.terms == 3 && warp == 12) {
+        constexpr uint32_t id = instruction(kIsBf16<T>, false, false, 128, DK);
+        await(smem_u32(&sm.third), 0, &sm.ctl.dead);
+        __syncwarp();
+        if (elect_one()) {
+            products<DV / 16, kColumns, 2 * DK>(results, over_columns(dys, 0), image_over_dv<DK>(values, 0), id, true);
+            commit(smem_u32(&sm.third_product));
+        }
+        __syncwarp();
+    }
     grad_products_done(sm.ctl, 1);
     if (g.terms == 3) {
         await(smem_u32(&sm.third_product), 0, &sm.ctl.dead);
@@ -394,7 +420,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
         float* to = g.tokens + ((long long)head * p.chunks + ci) * kChunk + row;
         to[0] = ((sm.dots[0][row] + sm.dots[1][row]) + (sm.dots[2][row] + sm.dots[3][row])) * p.scale;
         to[plane] = ((sm.sums[0][row] + sm.sums[1][row]) + (sm.sums[2][row] + sm.sums[3][row])) * p.scale;
-        to[4 * plane] = sm.within[row] * p.scale;
+        to[4 * plane] = ((sm.within[0][row] + sm.within[1][row]) + (sm.within[2][row] + sm.within[3][row])) * p.scale;
         if (row < 2)
             g.bridges[2 * at + row] = (sm.pairs[3][0] + sm.pairs[2 + row][row]) * p.scale;
     }
@@ -408,36 +434,6 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
         store_part<DK>(smem, g.part_q + (packed_row(p, c, 0) * p.heads + head) * p.dk, (long long)p.heads * p.dk, c.len, p.dk);
     else if (g.dq.ptr)
         store_tile<T, DK, kGradThreads>(smem, g.dq, c, head, p.dk, g.vec_dq);
-}
-
-// Decay of the pairs (32 rows of block b, column) of the lower triangle, a lane for the column j: `mine` its sum from its block's begin, `to_there` the decay from it
-// to block b's begin; from [32]: the rows' decays from there.
-__device__ __forceinline__ void decay_column(float (&v)[32], float (&w)[32], const float* sums, bool diagonal, int lane, float mine, float to_there, float scale, const float* from)
-{
-    if (diagonal) {
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const float4 h = *reinterpret_cast<const float4*>(sums + i);
-            const float d[4] = {i >= lane ? ex2(h.x - mine) * scale : 0.f, i + 1 >= lane ? ex2(h.y - mine) * scale : 0.f, i + 2 >= lane ? ex2(h.z - mine) * scale : 0.f,
-                                i + 3 >= lane ? ex2(h.w - mine) * scale : 0.f};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[i + j] = i + j >= lane ? v[i + j] * d[j] : 0.f;
-                w[i + j] = i + j >= lane ? w[i + j] * d[j] : 0.f;
-            }
-        }
-    } else {
-        const f2 both = pack2(to_there * scale, to_there * scale);
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const float4 h = *reinterpret_cast<const float4*>(from + i);
-            const f2 a = mul2(both, pack2(h.x, h.y)), b = mul2(both, pack2(h.z, h.w));
-            unpack2(mul2(pack2(v[i], v[i + 1]), a), v[i], v[i + 1]);
-            unpack2(mul2(pack2(v[i + 2], v[i + 3]), b), v[i + 2], v[i + 3]);
-            unpack2(mul2(pack2(w[i], w[i + 1]), a), w[i], w[i + 1]);
-            unpack2(mul2(pack2(w[i + 2], w[i + 3]), b), w[i + 2], w[i + 3]);
-        }
-    }
 }
 
 // dk and dv of one chunk and head, lanes for the tokens j, a block of 32 tokens i to each of a row's four warps.
@@ -469,7 +465,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         }
         __syncwarp();
     }
-    if (warp == 3) {                             // (which has no pairs to weigh, as warp 2)
+    if (warp == 3) {                             // (of the last 32 tokens' warps, which have the fewest pairs to weigh, as warp 7)
         constexpr uint32_t id_k = instruction(kIsBf16<T>, false, false, 128, DK), id_v = instruction(kIsBf16<T>, false, true, 128, DV);
         await(smem_u32(&sm.image), 0, &sm.ctl.dead);
         __syncwarp();
@@ -498,32 +494,31 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
             }
             __syncwarp();
         }
-    } else if (warp == 2) {
+    } else if (warp == 7) {
         if (elect_one())
             fetch_next<DK, DV>(g, there, back);
         __syncwarp();
     }
     grad_products_done(sm.ctl, 0);
     const int row = quarter * 32 + lane;
-    uint32_t packed_v[16], packed_k[16];
+    uint32_t packed_v[16], packed_k[16], diagonal_v[4], diagonal_k[4];
     float col = 0.f;
-    if (sub >= quarter) {
+    if (sub > quarter) {
         float v[32], w[32];
         tmem_ld32(scores + sub * 32 + lanes, v);
         tmem_ld32(slopes + sub * 32 + lanes, w);
-        if (sub > quarter) {                     // M's column sums: the decay once, in front of the products' operands, which have it each
+        const float to_there = to_block(dec, row, sub) * p.scale;
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                const float4 h = *reinterpret_cast<const float4*>(sm.from + sub * 32 + j);
-                col = fmaf(v[j] * w[j], h.x, col);
-                col = fmaf(v[j + 1] * w[j + 1], h.y, col);
-                col = fmaf(v[j + 2] * w[j + 2], h.z, col);
-                col = fmaf(v[j + 3] * w[j + 3], h.w, col);
-            }
+        for (int j = 0; j < 32; j += 4) {        // M's column sums: the decay once, in front of the products' operands, which have it each
+            const float4 h = *reinterpret_cast<const float4*>(sm.from + sub * 32 + j);
+            col = fmaf(v[j] * w[j], h.x, col);
+            col = fmaf(v[j + 1] * w[j + 1], h.y, col);
+            col = fmaf(v[j + 2] * w[j + 2], h.z, col);
+            col = fmaf(v[j + 3] * w[j + 3], h.w, col);
         }
-        const float to_there = sub > quarter ? to_block(dec, row, sub) : 0.f;
-        col *= to_there * p.scale;
-        decay_column(v, w, dec.g + sub * 32, sub == quarter, lane, dec.g[row], to_there, p.scale, sm.from + sub * 32);
+        col *= to_there;
+        decay_earlier(v, to_there, sm.from + sub * 32);
+        decay_earlier(w, to_there, sm.from + sub * 32);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             packed_v[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
@@ -534,11 +529,34 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         for (int j = 0; j < 16; ++j)
             packed_v[j] = packed_k[j] = 0;
     }
+    {
+        const int first = sub * 8, from = quarter * 32 + first;
+        const float own = dec.g[row];
+        float v[8], w[8];
+        tmem_ld8(scores + from + lanes, v);
+        tmem_ld8(slopes + from + lanes, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool later = first + j >= lane;
+            const float d = ex2(dec.g[from + j] - own) * p.scale;
+            v[j] = later ? v[j] * d : 0.f;
+            w[j] = later ? w[j] * d : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            diagonal_v[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+            diagonal_k[j] = pack16<T>(w[2 * j], w[2 * j + 1]);
+        }
+    }
     before_barrier();
     asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
     behind_barrier();
-    tmem_st16(scores + sub * 16 + lanes, packed_v);
-    tmem_st16(slopes + sub * 16 + lanes, packed_k);
+    if (sub != quarter) {
+        tmem_st16(scores + sub * 16 + lanes, packed_v);
+        tmem_st16(slopes + sub * 16 + lanes, packed_k);
+    }
+    tmem_st4(scores + quarter * 16 + sub * 4 + lanes, diagonal_v);
+    tmem_st4(slopes + quarter * 16 + sub * 4 + lanes, diagonal_k);
     grad_products_done(sm.ctl, 1);
     if (g.terms == 3) {
         await(smem_u32(&sm.third_product), 0, &sm.ctl.dead);
@@ -585,7 +603,8 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         store_tile<T, DV, kGradThreads>(s_values, g.dv, c, head, p.dv, g.vec_dv);
 }
 
-// Both in one launch, side by side: the second one finds the tiles in L2.
+// Both in one launch, side by side: the second one finds the tiles in L2.  4 x 1024 tokens of 16 heads of 128 x 128 take 76 us: a block has an SM's shared memory to itself and goes through
+// loads (2200 clocks), products, weights, products and stores one behind the other, 12000 clocks for dq and 14000 for dk and dv.
 template <typename T, int DK, int DV>
 __global__ void __launch_bounds__(kGradThreads, 1) grad_kernel(const __grid_constant__ Maps there, const __grid_constant__ Maps back, const GradDev g)
 {
@@ -717,7 +736,7 @@ __global__ void __launch_bounds__(128) grad_decay_kernel(const GradDev g)
         for (int o = 16; o; o /= 2)
             over += __shfl_xor_sync(0xffffffffu, over, o);
         over += block == 1 || block == 2 ? g.bridges[2 * ch + block - 1] : 0.f;
-        const float A = p.A[head];
+        const float A = rate(p, head);
 #pragma unroll
         for (int i = 3; i >= 0; --i) {
             behind += e[i] + rows[i];
@@ -739,8 +758,9 @@ __global__ void __launch_bounds__(128) grad_decay_kernel(const GradDev g)
                 step = step_of(p, raw);
                 slope = p.softplus ? sigmoid(raw) : 1.f;
             }
-            const float d = dl[i] * A * slope;
-            sum_A = fmaf(dl[i], step, sum_A);
+            const bool none = dl[i] == 0.f;      // what is forgotten has no share, whatever forgets it (a step of infinity)
+            const float d = none ? 0.f : dl[i] * A * slope;
+            sum_A = none ? sum_A : fmaf(dl[i], step, sum_A);
             sum_bias += d;
             if (g.ddelta.ptr)
                 row_ptr<T>(g.ddelta, c.seq, c.row0 + t)[head] = from_f<T>(d);

@@ -282,6 +282,39 @@ def test_gradients_with_strong_and_infinite_decays():
         _check_gradients(i, lead)
 
 
+@pytest.mark.parametrize("softplus", [True, False])
+def test_steps_of_infinity_and_decays_of_minus_infinity(softplus):
+    """A step of infinity forgets as any other does whose decay is zero in float32, and has no share in the gradients of A and delta; a decay of minus
+    infinity forgets everything, but keeps the state over a step of nothing (of zero, or a softplus below the numbers there are)."""
+    lead = (1, 200)
+    i = _inputs(lead, 1, 3, 1, 32, 40, B, 39, grad=True)
+    i["softplus"], i["delta_bias"], i["delta"] = softplus, None, i["delta"].abs()
+    i["A"] = torch.tensor([-1.0, -0.5, -1.0], device=DEV)
+
+    def all_of():
+        last, S = torch.empty_like(i["state"]), i["state"].clone()
+        got = block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], None, softplus, None, i["state"], None, i["dlast"])
+        got.update(y=_call(i, state_out=last), last=last)
+        got["one"] = block.decay_attention_step(i["q"][:, 5], i["k"][:, 5], i["v"][:, 5], i["A"], S, i["delta"][:, 5], None, softplus)
+        got["S"] = S
+        return got
+
+    i["delta"][:, 0::3, 2], i["delta"][:, 1::3, 2] = 1.0, 2.0
+    i["delta"][:, 2::3, 2] = -200.0 if softplus else 0.0                            # a step of nothing
+    results = []
+    for large, lowest in ((1e4, -1e4), (float("inf"), float("-inf"))):
+        for t in (0, 5, 6, 130, 199):
+            i["delta"][:, t, 1] = large
+        i["A"][2] = lowest
+        results.append(all_of())
+    for n in results[0]:
+        one, two = results[0][n], results[1][n]
+        if n in ("ddelta", "ddelta_bias"):                                          # (A times what passes through a decay: not finite where A is not)
+            one, two = one[..., :2], two[..., :2]
+        assert torch.isfinite(two).all(), n
+        assert torch.equal(one, two), n
+
+
 def test_the_same_call_gives_the_same_bits():
     i = _inputs((2, 300), 2, 4, 2, 64, 64, H, 41, grad=True)
     call = lambda: block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], None, i["dlast"])  # noqa: E731
