@@ -1,4 +1,5 @@
 // Host side of ttc_decay_attention, ttc_decay_attention_step and ttc_decay_attention_grad.
+#include <algorithm>
 #include <type_traits>
 
 #include "block_host.h"
@@ -152,21 +153,23 @@ int describe_all(const AttnDev& p, const Rows* q, bool vec_q, const Rows& k, boo
     return describe(m.v, v, p.heads, p.dv, p.seqs, is_bf16);
 }
 
-// One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each piece of a sequence, behind a walk for what the pieces add to the state.
+// One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each of a sequence's pieces, behind a walk for what the pieces add to the state.  Uncut,
+// n chunks take 2.65 n + 7 us; cut, the longest piece's m take 4.6 m + 25, so that n has to be above 7 m / 4 + 6.5.  (One sequence of 32 chunks, 128 x 128, uncut and cut: 64 walks, m = 16, 90 and 99 us;
+// 48 walks, m = 11, 90 and 79; of 64 x 64, 36 walks, m = 8, 86 and 63; three of 8 chunks, 48 walks, m = 3, 29 and 38.)  Lengths of packed sequences are not known here: the longest is taken for
+// one and a half times the mean (four in 32 chunks, 64 walks, m = 4: the longest of 15 chunks 49 and 48 us, of 9 chunks 35 and 50).
 int take_pieces(int device, const ttc_decay_args* a, int splits, int columns, AttnDev& p, States& q, int ways, Scratch& s)
 {
     const int64_t sms = sm_count(device), walks = (int64_t)a->heads * splits, rows = a->seq_offsets ? a->tokens : a->tokens * a->batch;
-    int64_t want = a->batch;                                         // pieces in all
-    if (walks * a->batch && sms / (walks * a->batch) >= (a->seq_offsets ? 2 : 3))
-        want = sms / walks;
+    const int64_t want = sms / walks;                                // pieces in all
     p.piece = a->tokens ? a->tokens : 1;
     p.pieces_per_seq = 1;
     p.pieces = a->batch;
-    if (a->batch && rows) {
+    if (want > a->batch && a->batch && rows) {
         const int64_t each = want / a->batch;                        // of equal sequences, as many to each
         int64_t piece = a->seq_offsets ? (rows + want - 1) / want : (a->tokens + each - 1) / each;
         piece = (piece + kChunk - 1) / kChunk * kChunk;
-        if (want > a->batch && piece < a->tokens) {
+        const int64_t longest = a->seq_offsets ? std::min(a->tokens, 3 * rows / (2 * a->batch)) : a->tokens;
+        if (piece < a->tokens && 4 * longest > 7 * piece + 26 * kChunk) {
             p.piece = piece;
             p.pieces_per_seq = (a->tokens + piece - 1) / piece;
             p.pieces = a->seq_offsets ? a->tokens / piece + a->batch : a->batch * p.pieces_per_seq;
@@ -304,10 +307,10 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     States& q = o.q;
     q = States{};
     TTC_TRY(take_pieces(device, a, o.splits, padded(a->dv) / o.splits, p.f, q, 2, s));
-    // Walks both ways side by side, where one way leaves SMs idle (of packed sequences, the shorter ones'): <Z, S_0> takes a kernel of its own then, which reads
-    // both images again (11 documents of 8191 tokens in all,
-    // 8 heads of 64 x 64: 187 -> 136 us).  Where one way fills the SMs (4 x 1024 tokens, 16 heads of 128 x 128), the second walk reads the states of the first as it goes.
-    o.together = 2 * p.f.pieces * a->heads * o.splits <= (packed ? 3 : 2) * sm_count(device) / 2;
+    // Walks both ways side by side, where one way leaves SMs idle (of packed sequences, whose shorter walks end early, where it fills them once): <Z, S_0> takes a kernel of its own
+    // then, which reads both images again; else the second walk reads the states of the first as it goes.  One after the other and side by side: 4 x 1024 tokens, 96 walks of 64 x 64
+    // 135 and 139 us, 72 walks 115 and 104; 11 documents of 8191 tokens in all, 88 walks 134 and 106 us, 132 walks 163 and 144, 176 walks of 128 x 64 177 and 183.
+    o.together = p.f.pieces * a->heads * o.splits <= (packed ? sm_count(device) : sm_count(device) / 2);
     if (p.f.chunks > INT32_MAX / (2 * a->heads))
         return fail(TTC_STATUS_UNSUPPORTED, "%lld chunks, %d heads", (long long)p.f.chunks, a->heads);
     if (packed) {
