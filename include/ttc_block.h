@@ -152,7 +152,8 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
  * Exponents A D_t are expected to be <= 0; minus infinity forgets everything.  Tokens go through the tensor cores in chunks of 128, counted from their
  * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, earlier tokens' too, and of those behind it.  float16: products scale q . k,
  * and in the gradients dy . v, have to stay below 65504.  Scratch: none where sequences, heads and columns fill the SMs; else sequences are walked along in pieces, with
- * 512 bytes for each value channel (dv rounded up to 64 or 128) of a piece and head, of which there are as many as SMs, and one more for each packed sequence.
+ * 512 bytes for each value channel (dv rounded up to 64 or 128) of a piece and head, of which there are as many as SMs, and one more for each packed sequence.  Rows of q, k, v (and
+ * dy of the gradients) that do not begin on 16 bytes, whose heads do not (dk, dv not a multiple of 8) or that are one row for many tokens are copied there too, 2 bytes for each channel.
  */
 typedef struct ttc_decay_args {
     int64_t batch, tokens;

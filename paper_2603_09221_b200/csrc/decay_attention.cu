@@ -92,9 +92,8 @@ AttnDev to_dev(const ttc_decay_args* a, bool step)
     p.v = dev_rows(a->v, off);
     p.delta = dev_rows(a->delta, off);
     p.y = dev_rows(a->y, off);
-    p.vec_q = by_16_bytes(a->q, a->dk, off);
-    p.vec_k = by_16_bytes(a->k, a->dk, off);
-    p.vec_v = by_16_bytes(a->v, a->dv, off);
+    p.head_q = p.head_k = a->dk;
+    p.head_v = a->dv;
     p.vec_y = by_16_bytes(a->y, a->dv, off);
     p.vec_state = a->dv % 8 == 0 && floats_by_16_bytes(a->state) && floats_by_16_bytes(a->state_out);
     p.A = a->A;
@@ -108,6 +107,7 @@ AttnDev to_dev(const ttc_decay_args* a, bool step)
 
 struct Plan {
     AttnDev p;
+    Operands o;
     States q;
     int splits;
     size_t bytes;
@@ -122,35 +122,44 @@ int map_pieces(const AttnDev& p, int64_t piece, int at_least, int64_t bound, cud
 }
 
 // Rows of heads as [batch][tokens][heads][width], in boxes of 64 channels (128 bytes, swizzled) of 128 tokens.
-int describe(CUtensorMap& map, const Rows& r, int heads, int width, const Seqs& s, bool is_bf16)
+int describe(CUtensorMap& map, const Rows& r, int heads, int width, int head, const Seqs& s, bool is_bf16)
 {
+    if (!s.tokens || !s.batch)                   // nothing is read
+        return TTC_OK;
     EncodeTiled f;
     TTC_TRY(encoder(f));
     const cuuint64_t dims[4] = {(cuuint64_t)width, (cuuint64_t)heads, (cuuint64_t)s.tokens, (cuuint64_t)(s.offsets ? 1 : s.batch)};
     // (the copy engine takes no stride of nothing, which is what a dimension of one may have)
-    const cuuint64_t head = width * 2, token = r.ts ? r.ts * 2 : head, seq = !s.offsets && r.bs ? r.bs * 2 : token;
-    const cuuint64_t strides[3] = {head, token, seq};
+    const cuuint64_t next = (cuuint64_t)head * 2, token = r.ts ? r.ts * 2 : next, seq = !s.offsets && r.bs ? r.bs * 2 : token;
+    const cuuint64_t strides[3] = {next, token, seq};
     const cuuint32_t box[4] = {64, 1, kChunk, 1}, steps[4] = {1, 1, 1, 1};
     const CUresult e = f(&map, is_bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, r.ptr, dims, strides, box, steps,
                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return e == CUDA_SUCCESS ? TTC_OK : fail(TTC_STATUS_CUDA_ERROR, "cuTensorMapEncodeTiled: error %d", (int)e);
 }
-bool can_describe(const Rows& r, bool by_16_bytes, const Seqs& s)
+
+// Rows that no map describes are laid out anew in scratch.
+void align(const Seqs& s, int heads, int width, Rows& r, int& head, Operands& o, Scratch& scratch)
 {
     const long long most = 1ll << 38;            // of strides in elements
-    return by_16_bytes && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most;
+    const bool by_16_bytes = width % 8 == 0 && reinterpret_cast<uintptr_t>(r.ptr) % 16 == 0 && r.ts % 8 == 0 && (s.offsets || r.bs % 8 == 0);
+    if (!s.tokens || !s.batch || (by_16_bytes && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most))
+        return;
+    const int padded = (width + 7) / 8 * 8;
+    const long long row = (long long)heads * padded;
+    unsigned short* to = scratch.take<unsigned short>((size_t)(s.offsets ? s.tokens : s.batch * s.tokens) * row);
+    auto& q = o.of[o.n++];
+    q.from = r;
+    q.to = to;
+    q.heads = heads, q.width = width, q.padded = head = padded;
+    r = Rows{to, s.offsets ? 0 : s.tokens * row, row};
 }
-
-// (q may be missing)
-int describe_all(const AttnDev& p, const Rows* q, bool vec_q, const Rows& k, bool vec_k, const Rows& v, bool vec_v, bool is_bf16, Maps& m)
+int align_all(const Seqs& s, const Operands& o, cudaStream_t st)
 {
-    m.there = (!q || can_describe(*q, vec_q, p.seqs)) && can_describe(k, vec_k, p.seqs) && can_describe(v, vec_v, p.seqs) && p.seqs.tokens && p.seqs.batch;
-    if (!m.there)
+    if (!o.n)
         return TTC_OK;
-    if (q)
-        TTC_TRY(describe(m.q, *q, p.heads / p.share, p.dk, p.seqs, is_bf16));
-    TTC_TRY(describe(m.k, k, p.heads / p.share, p.dk, p.seqs, is_bf16));
-    return describe(m.v, v, p.heads, p.dv, p.seqs, is_bf16);
+    const long long rows = s.offsets ? s.tokens : s.batch * s.tokens;
+    return launch_early("decay attention, rows laid out anew", align_kernel, dim3((unsigned)std::min(rows, (long long)kMaxGridY), o.n), 256, 0, 1, st, s, o);
 }
 
 // One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each of a sequence's pieces, behind a walk for what the pieces add to the state.  Uncut,
@@ -194,6 +203,10 @@ int plan_forward(int device, const ttc_decay_args* a, void* ws, Plan& o)
     p = to_dev(a, false);
     o.splits = (a->dv + kCols - 1) / kCols;
     Scratch s(ws);
+    o.o.n = 0;
+    align(p.seqs, a->groups, a->dk, p.q, p.head_q, o.o, s);
+    align(p.seqs, a->groups, a->dk, p.k, p.head_k, o.o, s);
+    align(p.seqs, a->heads, a->dv, p.v, p.head_v, o.o, s);
     o.q = States{};
     TTC_TRY(take_pieces(device, a, o.splits, kCols, p, o.q, 1, s));
     o.bytes = s.used;
@@ -242,6 +255,7 @@ template <typename T, int DK, int COLS> int chunk_states(const Maps (&maps)[2], 
 
 struct GradPlan {
     GradDev g;
+    Operands o;
     States q;
     int splits;
     bool together;
@@ -288,7 +302,7 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     p.dk = dev_rows(g->dk, a->seq_offsets);
     p.dv = dev_rows(g->dv, a->seq_offsets);
     p.ddelta = dev_rows(g->ddelta, a->seq_offsets);
-    p.vec_dy = by_16_bytes(g->dy, a->dv, packed);
+    p.head_dy = a->dv;
     p.vec_dq = by_16_bytes(g->dq, a->dk, packed);
     p.vec_dk = by_16_bytes(g->dk, a->dk, packed);
     p.vec_dv = by_16_bytes(g->dv, a->dv, packed);
@@ -302,6 +316,11 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     p.want_q = p.want_l || g->dq.ptr;
     p.want_kv = p.want_l || g->dk.ptr || g->dv.ptr;
     Scratch s(ws);
+    o.o.n = 0;
+    align(p.f.seqs, a->groups, a->dk, p.f.q, p.f.head_q, o.o, s);
+    align(p.f.seqs, a->groups, a->dk, p.f.k, p.f.head_k, o.o, s);
+    align(p.f.seqs, a->heads, a->dv, p.f.v, p.f.head_v, o.o, s);
+    align(p.f.seqs, a->heads, a->dv, p.dy, p.head_dy, o.o, s);
     // float16: a power of two goes with each image of a state, so that it is one walk's
     o.splits = a->dtype == TTC_BF16 ? padded(a->dv) / kCols : 1;
     States& q = o.q;
@@ -325,15 +344,15 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
         p.unit_Z = s.take<float>(each);
     }
     q.seq_first = p.f.seq_first;
-    q.way[0].k = p.f.k, q.way[0].vec_k = p.f.vec_k;
-    q.way[0].v = p.f.v, q.way[0].vec_v = p.f.vec_v;
+    q.way[0].k = p.f.k, q.way[0].head_k = p.f.head_k;
+    q.way[0].v = p.f.v, q.way[0].head_v = p.f.head_v;
     q.way[0].given = a->state;
     q.way[0].factor = 1.f;
     q.way[0].image = p.image_S;
     q.way[0].unit = p.unit_S;
     q.way[1].back = 1;                           // with queries for keys and dy for values
-    q.way[1].k = p.f.q, q.way[1].vec_k = p.f.vec_q;
-    q.way[1].v = p.dy, q.way[1].vec_v = p.vec_dy;
+    q.way[1].k = p.f.q, q.way[1].head_k = p.f.head_q;
+    q.way[1].v = p.dy, q.way[1].head_v = p.head_dy;
     q.way[1].given = p.dstate_out;
     q.way[1].last = p.dstate;
     q.way[1].factor = a->scale;
@@ -401,14 +420,18 @@ int ttc_decay_attention(int32_t device, const ttc_decay_args* a, void* workspace
         return TTC_OK;
     const dim3 grid((unsigned)(p.pieces * p.heads * o.splits));
     Maps maps[2] = {};
-    TTC_TRY(describe_all(p, &p.q, p.vec_q, p.k, p.vec_k, p.v, p.vec_v, a->dtype == TTC_BF16, maps[0]));
+    const bool is_bf16 = a->dtype == TTC_BF16;
+    TTC_TRY(describe(maps[0].q, p.q, a->groups, a->dk, p.head_q, p.seqs, is_bf16));
+    TTC_TRY(describe(maps[0].k, p.k, a->groups, a->dk, p.head_k, p.seqs, is_bf16));
+    TTC_TRY(describe(maps[0].v, p.v, a->heads, a->dv, p.head_v, p.seqs, is_bf16));
+    TTC_TRY(align_all(p.seqs, o.o, st));
     auto go = [&](auto t, auto kc) {
         using T = decltype(t);
         constexpr int DK = decltype(kc)::value;
         if (p.piece_state) {
             States q = o.q;
-            q.way[0].k = p.k, q.way[0].vec_k = p.vec_k;
-            q.way[0].v = p.v, q.way[0].vec_v = p.vec_v;
+            q.way[0].k = p.k, q.way[0].head_k = p.head_k;
+            q.way[0].v = p.v, q.way[0].head_v = p.head_v;
             q.way[0].given = p.state;
             q.way[0].factor = 1.f;
             TTC_TRY((piece_states<T, DK, kCols>(maps, p, q, 1, o.splits, st)));
@@ -469,8 +492,11 @@ int ttc_decay_attention_grad(int32_t device, const ttc_decay_args* a, const ttc_
     TTC_TRY(map_pieces(f, kChunk, 0, f.chunks, st));
     Maps maps[2] = {};
     const bool is_bf16 = a->dtype == TTC_BF16;
-    TTC_TRY(describe_all(f, nullptr, false, f.k, f.vec_k, f.v, f.vec_v, is_bf16, maps[0]));
-    TTC_TRY(describe_all(f, nullptr, false, f.q, f.vec_q, p.dy, p.vec_dy, is_bf16, maps[1]));
+    TTC_TRY(describe(maps[0].k, f.k, a->groups, a->dk, f.head_k, f.seqs, is_bf16));
+    TTC_TRY(describe(maps[0].v, f.v, a->heads, a->dv, f.head_v, f.seqs, is_bf16));
+    TTC_TRY(describe(maps[1].k, f.q, a->groups, a->dk, f.head_q, f.seqs, is_bf16));
+    TTC_TRY(describe(maps[1].v, p.dy, a->heads, a->dv, p.head_dy, f.seqs, is_bf16));
+    TTC_TRY(align_all(f.seqs, o.o, st));
     return by_widths(a, [&](auto t, auto kc, auto vc) {
         using T = decltype(t);
         constexpr int DK = decltype(kc)::value, DV = decltype(vc)::value;

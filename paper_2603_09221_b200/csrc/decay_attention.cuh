@@ -50,8 +50,8 @@ struct AttnDev {
     int softplus;
     float scale;
     Rows q, k, v, delta, y;
-    int vec_q, vec_k, vec_v, vec_y;              // rows can be accessed by 16 bytes
-    int vec_state;                               // and the states
+    int head_q, head_k, head_v;                  // elements from a head to the next one: its channels, or those rounded up, of rows laid out anew
+    int vec_y, vec_state;                        // can be accessed by 16 bytes
     const float *A, *delta_bias, *state;
     float* state_out;
     const float* piece_state;                    // scratch: the states in front of the pieces of a sequence
@@ -171,28 +171,17 @@ template <int N> __device__ __forceinline__ void copies_done() { asm volatile("c
 // what threads have written becomes visible to the tensor cores (before the barrier that they are issued behind)
 __device__ __forceinline__ void to_tensor_cores() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// `width` channels from channel col0 of the rows.  Thread t sees to the vectors t, t + THREADS, ..: the same ones wherever a tile is gone through.
+// `width` channels from channel col0 of the rows, for the last chunk of a packed sequence, which others' rows follow: the copy engine fills the others.  (Channels behind a head's up to
+// eight are zeros, as align_kernel lays them out.)
 template <typename T, int COLS, int THREADS>
-__device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chunk& c, int col0, int width, bool vec, int thread)
+__device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chunk& c, int col0, int width, int thread)
 {
     const T* base = row_ptr<T>(r, c.seq, c.row0) + col0;
-    if (vec) {
 #pragma unroll 8
-        for (int i = 0; i < kChunk * COLS / 8; i += THREADS) {
-            const int e = i + thread, row = e / (COLS / 8), c8 = e % (COLS / 8);
-            const bool ok = row < c.len && c8 * 8 < width;
-            copy16(to + tile_at(row, c8), ok ? base + row * r.ts + c8 * 8 : base, ok);
-        }
-    } else {
-        for (int e = thread; e < kChunk * COLS / 8; e += THREADS) {
-            const int row = e / (COLS / 8), c8 = e % (COLS / 8);
-            Vec<T, 8> u;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                u.v[j] = row < c.len && c8 * 8 + j < width ? base[row * r.ts + c8 * 8 + j] : from_f<T>(0.f);
-            const uint4 w = *reinterpret_cast<const uint4*>(&u);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to + tile_at(row, c8)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w) : "memory");
-        }
+    for (int i = 0; i < kChunk * COLS / 8; i += THREADS) {
+        const int e = i + thread, row = e / (COLS / 8), c8 = e % (COLS / 8);
+        const bool ok = row < c.len && c8 * 8 < width;
+        copy16(to + tile_at(row, c8), ok ? base + row * r.ts + c8 * 8 : base, ok);
     }
 }
 
@@ -391,6 +380,39 @@ __device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const
         unpack2(mul2(pack2(v[j + 2], v[j + 3]), mul2(pack2(e_row, e_row), pack2(t.z, t.w))), v[j + 2], v[j + 3]);
     }
 }
+// ---- rows laid out anew ---------------------------------------------------------------------------------------------------
+
+// Operands that the copy engines cannot take (heads that do not begin on 16 bytes, one row for all tokens) are copied first, the heads' channels rounded up to eight with zeros behind them.
+// Two bytes at a time and 64 threads for a chunk's tiles were the other way: 4 x 1024 tokens of 16 heads of 100 x 100 took 421 us and of 36 x 36 263.
+struct Operands {
+    struct {
+        Rows from;
+        unsigned short* to;
+        int heads, width, padded;
+    } of[4];
+    int n;
+};
+static __global__ void __launch_bounds__(256) align_kernel(const Seqs s, const Operands o)
+{
+    wait_for_previous();
+    const auto& q = o.of[blockIdx.y];
+    const unsigned each = q.padded / 8, per_row = q.heads * each;
+    const long long rows = s.offsets ? s.tokens : s.batch * s.tokens;
+    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
+        const long long seq = s.offsets ? 0 : row / s.tokens;
+        const unsigned short* from = row_ptr<unsigned short>(q.from, seq, row - seq * s.tokens);
+        uint4* to = reinterpret_cast<uint4*>(q.to + row * q.heads * q.padded);
+        for (unsigned e = threadIdx.x; e < per_row; e += 256) {
+            const unsigned head = e / each, c = e % each * 8;
+            Vec<unsigned short, 8> u;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                u.v[j] = load_if(from + (long long)head * q.width + c + j, c + j < q.width);
+            to[e] = *reinterpret_cast<const uint4*>(&u);
+        }
+    }
+}
+
 // ---- a walk along the chunks ----------------------------------------------------------------------------------------------
 
 constexpr int kWalkThreads = 512;
@@ -579,7 +601,6 @@ __device__ __forceinline__ float walk_largest(float v, float* parts)
 // Rows as [batch][tokens][heads][channels] for the copy engines.
 struct Maps {
     CUtensorMap q, k, v;
-    int there;                                   // whether the rows can be described so
 };
 __device__ __forceinline__ void fetch_box(uint32_t to, const CUtensorMap* map, int col, int head, int row, int seq, uint32_t bar)
 {
@@ -695,9 +716,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             ask(0);
         for (int i = 0; i < n; ++i) {
             const Chunk c = chunk_of(piece, i);
-            // by the copy engine, which fills up with zeros behind the matrix; the last chunk of a packed sequence, which others' rows follow, and rows that no
-            // map describes by the threads
-            const bool engine = maps.there && (!p.seqs.offsets || c.len == kChunk);
+            // by the copy engine, which fills up with zeros behind the matrix; the last chunk of a packed sequence, which others' rows follow, by the threads
+            const bool engine = !p.seqs.offsets || c.len == kChunk;
             const uint32_t bar = smem_u32(&sm.loaded[i & 1]);
             bool arrived = false;
             auto fetch = [&]() {
@@ -728,9 +748,9 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                         __syncwarp();
                     }
                 } else {
-                    load_tile<T, kCols, 32 * kFrontWarps>(values_at(i), p.v, c, head * p.dv + col0, cols, p.vec_v, thread);
-                    load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), p.k, c, group * p.dk, p.dk, p.vec_k, thread);
-                    load_tile<T, DK, 32 * kFrontWarps>(queries_at(i), p.q, c, group * p.dk, p.dk, p.vec_q, thread);
+                    load_tile<T, kCols, 32 * kFrontWarps>(values_at(i), p.v, c, head * p.head_v + col0, cols, thread);
+                    load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), p.k, c, group * p.head_k, p.dk, thread);
+                    load_tile<T, DK, 32 * kFrontWarps>(queries_at(i), p.q, c, group * p.head_q, p.dk, thread);
                     copies_begun();
                 }
             };
@@ -1033,7 +1053,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
 // from zero, or for the states in front of all chunks.
 struct StateDev {
     Rows k, v;
-    int vec_k, vec_v, back;
+    int head_k, head_v, back;
     const float* given;                          // in front of the sequences (back: behind them)
     float* last;                                 // behind them (in front)
     float factor;                                // of what is added
@@ -1148,7 +1168,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
             ask(0);
         for (int i = 0; i < n; ++i) {
             const Chunk c = chunk_of(piece, chunk(i));
-            const bool engine = maps.there && (!p.seqs.offsets || c.len == kChunk);
+            const bool engine = !p.seqs.offsets || c.len == kChunk;
             const uint32_t bar = smem_u32(&sm.loaded[i & 1]);
             bool arrived = false;
             float sum[4 / kFrontWarps], own[4 / kFrontWarps];
@@ -1191,8 +1211,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                     __syncwarp();
                 }
             } else {
-                load_tile<T, COLS, 32 * kFrontWarps>(values_at(i), q.v, c, head * p.dv + col0, cols, q.vec_v, thread);
-                load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), q.k, c, group * p.dk, p.dk, q.vec_k, thread);
+                load_tile<T, COLS, 32 * kFrontWarps>(values_at(i), q.v, c, head * q.head_v + col0, cols, thread);
+                load_tile<T, DK, 32 * kFrontWarps>(keys_at(i), q.k, c, group * q.head_k, p.dk, thread);
                 copies_begun();
             }
             if (i < 2)

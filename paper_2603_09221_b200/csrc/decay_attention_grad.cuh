@@ -26,7 +26,8 @@ namespace dattn {
 struct GradDev {
     AttnDev f;
     Rows dy, dq, dk, dv, ddelta;
-    int vec_dy, vec_dq, vec_dk, vec_dv;
+    int head_dy;                                 // as f.head_v
+    int vec_dq, vec_dk, vec_dv;
     const float* dstate_out;
     float *dA, *dbias, *dstate;
     // scratch
@@ -174,7 +175,7 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
     const AttnDev& p = g.f;
     const int group = head / p.share, warp = threadIdx.x / 32;
     const uint32_t queries = tiles, keys = queries + S::K_BYTES, values = keys + S::K_BYTES, dys = values + S::V_BYTES, image = dys + S::V_BYTES;
-    const bool engine = there.there && back.there && (!p.seqs.offsets || c.len == kChunk);
+    const bool engine = !p.seqs.offsets || c.len == kChunk;
     const uint32_t bar = smem_u32(&sm.tiles);
     if (threadIdx.x == kGradThreads - 32) {
         for (uint64_t* b : {&sm.tiles, &sm.image, &sm.second_product, &sm.third, &sm.third_product})
@@ -200,10 +201,10 @@ __device__ __forceinline__ uint32_t begin_grad(const GradDev& g, const Maps& the
         l = log_decay_at<T>(p, c, head, threadIdx.x);
     const uint32_t tmem = set_up(sm.ctl, 512);
     if (!engine) {
-        load_tile<T, DK, kGradThreads>(queries, p.q, c, group * p.dk, p.dk, p.vec_q, threadIdx.x);
-        load_tile<T, DK, kGradThreads>(keys, p.k, c, group * p.dk, p.dk, p.vec_k, threadIdx.x);
-        load_tile<T, DV, kGradThreads>(values, p.v, c, head * p.dv, p.dv, p.vec_v, threadIdx.x);
-        load_tile<T, DV, kGradThreads>(dys, g.dy, c, head * p.dv, p.dv, g.vec_dy, threadIdx.x);
+        load_tile<T, DK, kGradThreads>(queries, p.q, c, group * p.head_q, p.dk, threadIdx.x);
+        load_tile<T, DK, kGradThreads>(keys, p.k, c, group * p.head_k, p.dk, threadIdx.x);
+        load_tile<T, DV, kGradThreads>(values, p.v, c, head * p.head_v, p.dv, threadIdx.x);
+        load_tile<T, DV, kGradThreads>(dys, g.dy, c, head * g.head_dy, p.dv, threadIdx.x);
         copies_begun();
     }
     if (warp < 4) {
@@ -225,7 +226,7 @@ template <int DK, int DV> __device__ __forceinline__ void fetch_next(const GradD
 {
     const AttnDev& p = g.f;
     const unsigned next = blockIdx.x + g.resident;
-    if (!there.there || !back.there || next >= gridDim.x)
+    if (next >= gridDim.x)
         return;
     const GradPlace where = grad_place(g, next);
     const Chunk n = chunk_at(p, where.chunk);

@@ -166,6 +166,16 @@ def test_slices_of_wider_rows_and_state_in_place():
         assert torch.equal(wide, before)
 
 
+@pytest.mark.parametrize("dk, dv", [(64, 64), (20, 33)])
+def test_one_row_for_all_tokens_and_one_sequence_for_all(dk, dv):
+    """Operands of stride zero, by expand: what their copies give."""
+    i = _inputs((3, 150), 3, 4, 2, dk, dv, B, 15, grad=True)
+    i["q"], i["v"], i["dy"] = i["q"][:, :1].expand(3, 150, 2, dk), i["v"][:1].expand(3, 150, 4, dv), i["dy"][:1, :1].expand(3, 150, 4, dv)
+    call = lambda j: dict(block.decay_attention_grad(j["dy"], j["q"], j["k"], j["v"], j["A"], j["delta"], j["delta_bias"], True, None, j["state"], None, j["dlast"]), y=_call(j))  # noqa: E731
+    got, want = call(i), call({n: t.contiguous() if torch.is_tensor(t) else t for n, t in i.items()})
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
 def test_other_sequences_infinities_stay_there():
     i = _inputs((300,), 3, 2, 2, 64, 64, B, 17, offsets=[0, 100, 180, 300])
     clean = _call(i).clone()
