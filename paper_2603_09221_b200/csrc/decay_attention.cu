@@ -55,10 +55,13 @@ int check_output(const ttc_decay_args* a, bool step)
     return TTC_OK;
 }
 
-// Whether rows of heads of `width` elements can be accessed by 16 bytes (8 elements).
-bool by_16_bytes(const ttc_rows& r, int width, bool packed)
+// Bytes that rows of heads of `width` elements can be accessed by.  (4 x 1024 tokens, 16 heads of 36 x 36, results written by 8 and by 2: 48 and 60 us; gradients 121 and 141.)
+int bytes_at_once(const Rows& r, int width)
 {
-    return width % 8 == 0 && reinterpret_cast<uintptr_t>(r.ptr) % 16 == 0 && r.tstride % 8 == 0 && (packed || r.bstride % 8 == 0);
+    for (int n : {8, 4})
+        if (width % n == 0 && reinterpret_cast<uintptr_t>(r.ptr) % (2 * n) == 0 && r.ts % n == 0 && r.bs % n == 0)
+            return 2 * n;
+    return 2;
 }
 bool floats_by_16_bytes(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
@@ -94,7 +97,7 @@ AttnDev to_dev(const ttc_decay_args* a, bool step)
     p.y = dev_rows(a->y, off);
     p.head_q = p.head_k = a->dk;
     p.head_v = a->dv;
-    p.vec_y = by_16_bytes(a->y, a->dv, off);
+    p.vec_y = bytes_at_once(p.y, a->dv);
     p.vec_state = a->dv % 8 == 0 && floats_by_16_bytes(a->state) && floats_by_16_bytes(a->state_out);
     p.A = a->A;
     p.delta_bias = a->delta_bias;
@@ -142,8 +145,8 @@ int describe(CUtensorMap& map, const Rows& r, int heads, int width, int head, co
 void align(const Seqs& s, int heads, int width, Rows& r, int& head, Operands& o, Scratch& scratch)
 {
     const long long most = 1ll << 38;            // of strides in elements
-    const bool by_16_bytes = width % 8 == 0 && reinterpret_cast<uintptr_t>(r.ptr) % 16 == 0 && r.ts % 8 == 0 && (s.offsets || r.bs % 8 == 0);
-    if (!s.tokens || !s.batch || (by_16_bytes && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most))
+    const int vec = bytes_at_once(r, width);
+    if (!s.tokens || !s.batch || (vec == 16 && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most))
         return;
     const int padded = (width + 7) / 8 * 8;
     const long long row = (long long)heads * padded;
@@ -152,6 +155,7 @@ void align(const Seqs& s, int heads, int width, Rows& r, int& head, Operands& o,
     q.from = r;
     q.to = to;
     q.heads = heads, q.width = width, q.padded = head = padded;
+    q.vec = vec == 2 ? 2 : 8;
     r = Rows{to, s.offsets ? 0 : s.tokens * row, row};
 }
 int align_all(const Seqs& s, const Operands& o, cudaStream_t st)
@@ -159,7 +163,7 @@ int align_all(const Seqs& s, const Operands& o, cudaStream_t st)
     if (!o.n)
         return TTC_OK;
     const long long rows = s.offsets ? s.tokens : s.batch * s.tokens;
-    return launch_early("decay attention, rows laid out anew", align_kernel, dim3((unsigned)std::min(rows, (long long)kMaxGridY), o.n), 256, 0, 1, st, s, o);
+    return launch_early("decay attention, rows laid out anew", align_kernel, dim3((unsigned)std::min((rows + kAlignRows - 1) / kAlignRows, (long long)kMaxGridY), o.n), 256, 0, 1, st, s, o);
 }
 
 // One walk to each sequence, head and `columns` value channels, or, where those leave SMs idle, to each of a sequence's pieces, behind a walk for what the pieces add to the state.  Uncut,
@@ -303,9 +307,9 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
     p.dv = dev_rows(g->dv, a->seq_offsets);
     p.ddelta = dev_rows(g->ddelta, a->seq_offsets);
     p.head_dy = a->dv;
-    p.vec_dq = by_16_bytes(g->dq, a->dk, packed);
-    p.vec_dk = by_16_bytes(g->dk, a->dk, packed);
-    p.vec_dv = by_16_bytes(g->dv, a->dv, packed);
+    p.vec_dq = bytes_at_once(p.dq, a->dk);
+    p.vec_dk = bytes_at_once(p.dk, a->dk);
+    p.vec_dv = bytes_at_once(p.dv, a->dv);
     p.f.vec_state = a->dv % 8 == 0 && floats_by_16_bytes(a->state) && floats_by_16_bytes(g->dstate_out) && floats_by_16_bytes(g->dstate);
     p.dstate_out = g->dstate_out;
     p.dA = g->dA;

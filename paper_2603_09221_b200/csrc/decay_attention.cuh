@@ -51,7 +51,8 @@ struct AttnDev {
     float scale;
     Rows q, k, v, delta, y;
     int head_q, head_k, head_v;                  // elements from a head to the next one: its channels, or those rounded up, of rows laid out anew
-    int vec_y, vec_state;                        // can be accessed by 16 bytes
+    int vec_y;                                   // bytes that results can be accessed by: 16, 8 or 2
+    int vec_state;                               // states can be accessed by 16 bytes
     const float *A, *delta_bias, *state;
     float* state_out;
     const float* piece_state;                    // scratch: the states in front of the pieces of a sequence
@@ -186,7 +187,7 @@ __device__ __forceinline__ void load_tile(uint32_t to, const Rows& r, const Chun
 }
 
 // The tile of results staged in shared memory, to its rows.
-template <typename T, int COLS, int THREADS> __device__ __forceinline__ void store_tile(const char* from, const Rows& r, const Chunk& c, int head, int width, bool vec)
+template <typename T, int COLS, int THREADS> __device__ __forceinline__ void store_tile(const char* from, const Rows& r, const Chunk& c, int head, int width, int vec)
 {
     T* base = row_ptr<T>(r, c.seq, c.row0) + (long long)head * width;
     constexpr int N = kChunk * COLS / 8 / THREADS;                   // vectors of a thread: of one place in every THREADS / (COLS / 8)-th row
@@ -203,8 +204,12 @@ template <typename T, int COLS, int THREADS> __device__ __forceinline__ void sto
         T* at = base + row * r.ts + c8 * 8;
         if (row >= c.len)
             break;
-        if (vec) {
+        if (vec == 16) {
             *reinterpret_cast<uint4*>(at) = w[i];
+        } else if (vec == 8) {
+            *reinterpret_cast<uint2*>(at) = make_uint2(w[i].x, w[i].y);
+            if (c8 * 8 + 4 < width)
+                *reinterpret_cast<uint2*>(at + 4) = make_uint2(w[i].z, w[i].w);
         } else {
             const Vec<T, 8> u = *reinterpret_cast<const Vec<T, 8>*>(&w[i]);
 #pragma unroll
@@ -383,32 +388,40 @@ __device__ __forceinline__ void decay_earlier(float (&v)[32], float e_row, const
 // ---- rows laid out anew ---------------------------------------------------------------------------------------------------
 
 // Operands that the copy engines cannot take (heads that do not begin on 16 bytes, one row for all tokens) are copied first, the heads' channels rounded up to eight with zeros behind them.
-// Two bytes at a time and 64 threads for a chunk's tiles were the other way: 4 x 1024 tokens of 16 heads of 100 x 100 took 421 us and of 36 x 36 263.
+// 64 threads that read a chunk's tiles by elements were the other way: 4 x 1024 tokens of 16 heads of 36 x 36 took 263 us, now 42, of 37 x 37 259 and 56, of 100 x 100 421 and 60; 3 x 29 tokens
+// of 6 heads of 36 x 20 13.7 and 10.6.
 struct Operands {
     struct {
         Rows from;
         unsigned short* to;
-        int heads, width, padded;
+        int heads, width, padded, vec;           // vec: bytes that rows can be read by: 8 or 2
     } of[4];
     int n;
 };
+constexpr int kAlignRows = 8;                    // of a block
 static __global__ void __launch_bounds__(256) align_kernel(const Seqs s, const Operands o)
 {
     wait_for_previous();
     const auto& q = o.of[blockIdx.y];
     const unsigned each = q.padded / 8, per_row = q.heads * each;
     const long long rows = s.offsets ? s.tokens : s.batch * s.tokens;
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        const long long seq = s.offsets ? 0 : row / s.tokens;
-        const unsigned short* from = row_ptr<unsigned short>(q.from, seq, row - seq * s.tokens);
-        uint4* to = reinterpret_cast<uint4*>(q.to + row * q.heads * q.padded);
-        for (unsigned e = threadIdx.x; e < per_row; e += 256) {
-            const unsigned head = e / each, c = e % each * 8;
-            Vec<unsigned short, 8> u;
+    for (long long row0 = (long long)blockIdx.x * kAlignRows; row0 < rows; row0 += (long long)gridDim.x * kAlignRows) {
+        uint4* to = reinterpret_cast<uint4*>(q.to + row0 * q.heads * q.padded);
+        const unsigned n = per_row * (unsigned)min((long long)kAlignRows, rows - row0);
+        for (unsigned e = threadIdx.x; e < n; e += 256) {
+            const long long row = row0 + e / per_row, seq = s.offsets ? 0 : row / s.tokens;
+            const unsigned head = e % per_row / each, c = e % each * 8;
+            const unsigned short* from = row_ptr<unsigned short>(q.from, seq, row - seq * s.tokens) + (long long)head * q.width + c;
+            if (q.vec == 8) {
+                const uint2 a = *reinterpret_cast<const uint2*>(from), b = load_if(reinterpret_cast<const uint2*>(from + 4), c + 4 < q.width);
+                to[e] = make_uint4(a.x, a.y, b.x, b.y);
+            } else {
+                Vec<unsigned short, 8> u;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                u.v[j] = load_if(from + (long long)head * q.width + c + j, c + j < q.width);
-            to[e] = *reinterpret_cast<const uint4*>(&u);
+                for (int j = 0; j < 8; ++j)
+                    u.v[j] = load_if(from + j, c + j < q.width);
+                to[e] = *reinterpret_cast<const uint4*>(&u);
+            }
         }
     }
 }
@@ -1001,7 +1014,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             }
             asm volatile("bar.sync %0, 128;" :: "r"(3 + quarter) : "memory");          // the four warps of these rows
             T* to = row_ptr<T>(p.y, c.seq, c.row0 + quarter * 32) + (long long)head * p.dv + col0;
-            if (p.vec_y) {
+            if (p.vec_y == 16) {
                 uint4 w[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -1018,10 +1031,19 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                         *reinterpret_cast<uint4*>(to + r * p.y.ts + c8 * 8) = w[h];
                 }
             } else {
-                for (int e = sub * 32 + lane; e < 32 * kCols; e += 128) {
-                    const int r = e / kCols, k = e % kCols;
-                    if (quarter * 32 + r < c.len && k < cols)
-                        to[r * p.y.ts + k] = reinterpret_cast<const T*>(stage + tile_at(quarter * 32 + r, k / 8))[k % 8];
+                if (p.vec_y == 8) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const int e = h * 128 + sub * 32 + lane, r = e / 16, c4 = e % 16;
+                        if (quarter * 32 + r < c.len && c4 * 4 < cols)
+                            *reinterpret_cast<uint2*>(to + r * p.y.ts + c4 * 4) = *reinterpret_cast<const uint2*>(stage + tile_at(quarter * 32 + r, c4 / 2) + c4 % 2 * 8);
+                    }
+                } else {
+                    for (int e = sub * 32 + lane; e < 32 * kCols; e += 128) {
+                        const int r = e / kCols, k = e % kCols;
+                        if (quarter * 32 + r < c.len && k < cols)
+                            to[r * p.y.ts + k] = reinterpret_cast<const T*>(stage + tile_at(quarter * 32 + r, k / 8))[k % 8];
+                    }
                 }
                 to_tensor_cores();
                 before_barrier();
