@@ -67,7 +67,7 @@ int check_overlap(const ttc_norm_args* a, const Operand& out, const Operand& in,
 
 struct Way {
     int v, k, threads, rows_per_block;
-    bool mixed;                                  // groups of channels whose sums go through shared memory
+    int mixed;                                   // how groups of channels lie
     size_t smem;
 };
 
@@ -102,7 +102,7 @@ Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> ro
     o.rows_per_block = threads == 32 ? kRowsOfWarps : 1;
     const int size = a->d / a->groups, lanes = size / o.v;
     p.lanes = lanes;
-    o.mixed = a->groups > 1 && (size % o.v || lanes > 32 || (lanes & (lanes - 1)));
+    o.mixed = a->groups == 1 ? kNear : size % o.v ? kAcross : lanes <= 32 && !(lanes & (lanes - 1)) ? kNear : o.v > 1 ? kWhole : kAcross;
     o.smem = o.mixed ? (size_t)o.rows_per_block * (a->d + a->groups) * sizeof(float) : 0;
     return o;
 }
@@ -113,7 +113,12 @@ template <typename F> int by_way(int dtype, const Way& w, F&& f)
         constexpr int V = 16 / sizeof(t);
         constexpr std::integral_constant<int, V> wide;
         constexpr std::integral_constant<int, 1> single;
-        auto of = [&](auto v, auto k) { return w.mixed ? f(t, v, k, std::true_type()) : f(t, v, k, std::false_type()); };
+        auto of = [&](auto v, auto k) {
+            if constexpr (decltype(v)::value > 1)
+                if (w.mixed == kWhole)
+                    return f(t, v, k, std::integral_constant<int, kWhole>());
+            return w.mixed ? f(t, v, k, std::integral_constant<int, kAcross>()) : f(t, v, k, std::integral_constant<int, kNear>());
+        };
         auto by_k = [&](auto v) {
             switch (w.k) {
             case 1: return of(v, std::integral_constant<int, 1>());
@@ -283,7 +288,7 @@ int ttc_block_norm_grad(int32_t device, const ttc_norm_args* a, const ttc_norm_g
             return launch("gradients of the block norm", norm_grad_kernel<decltype(t), decltype(v)::value, decltype(k)::value, decltype(m)::value>, dim3(o.blocks), o.w, sm_count(device), st, p);
         }));
     if (p.dw_post || p.dscale || p.dw_pre)
-        TTC_TRY((launch_early("gradients of the block norm, parameters", norm_sum_kernel, dim3((unsigned)((a->d + 31) / 32), 3), 256, 0, 1, st, p)));
+        TTC_TRY((launch_early("gradients of the block norm, parameters", norm_sum_kernel, dim3((unsigned)((a->d + 31) / 32), 3), 32 * kRuns, 0, 1, st, p)));
     return TTC_OK;
 }
 

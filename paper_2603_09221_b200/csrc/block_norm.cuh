@@ -136,20 +136,32 @@ template <int V> __device__ __forceinline__ void params(const float* w, int c, f
     }
 }
 
+// How groups of channels lie: a group is the row or neighbouring threads' vectors, a power of two of them up to 32; vectors lie across groups; vectors lie in one each, of which the
+// sums alone go through shared memory (gradients of 13541 x 1216 in two groups 170 -> 145 us).
+enum { kNear = 0, kAcross = 1, kWhole = 2 };
+
 // Sums over the groups of channels: in, the values of a thread's K vectors; out, the sum of each element's group.  MIXED: groups that vectors lie across, or of
 // more than a warp's vectors, through shared memory, group by group.  Else all elements of a vector have the same sum, and only the first pair is set: a group is the row, or a few
 // neighbouring threads.
-template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, f2 (&v)[K][kPairs<V>], float* area, float* buffer, int& turn)
+template <int MIXED, int K, int V> __device__ __forceinline__ void group_sums_of(const NormDev& p, f2 (&v)[K][kPairs<V>], float* area, float* buffer, int& turn)
 {
     if constexpr (MIXED) {
         const int warps = blockDim.x / 32;
         float* s = area + threadIdx.y * (p.d + p.groups);
         float* sums = s + p.d;
+        constexpr bool whole = MIXED == kWhole;
+        const int size = whole ? p.size / V : p.size;
         __syncthreads();                         // earlier sums have been read
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int at = (k * blockDim.x + threadIdx.x) * V;
-            if (at < p.d) {
+            if (whole && at < p.d) {
+                f2 sum = v[k][0];
+#pragma unroll
+                for (int j = 1; j < kPairs<V>; ++j)
+                    sum = add2(sum, v[k][j]);
+                s[at / V] = sum_of(sum);
+            } else if (at < p.d) {
 #pragma unroll
                 for (int j = 0; j < V; j += 2) {
                     float a, b;
@@ -163,8 +175,8 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
         __syncthreads();
         for (int g = threadIdx.x / 32; g < p.groups; g += warps) {
             float sum = 0.f;
-            for (int j = threadIdx.x % 32; j < p.size; j += 32)
-                sum += s[g * p.size + j];
+            for (int j = threadIdx.x % 32; j < size; j += 32)
+                sum += s[g * size + j];
 #pragma unroll
             for (int o = 16; o; o /= 2)
                 sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -175,7 +187,12 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int at = (k * blockDim.x + threadIdx.x) * V;
-            if (at < p.d) {
+            if (whole && at < p.d) {
+                const f2 sum = both(sums[at / p.size]);
+#pragma unroll
+                for (int j = 0; j < kPairs<V>; ++j)
+                    v[k][j] = sum;
+            } else if (at < p.d) {
                 int g = at / p.size, left = (g + 1) * p.size - at;
                 float e[2];
 #pragma unroll
@@ -220,7 +237,7 @@ template <bool MIXED, int K, int V> __device__ __forceinline__ void group_sums_o
     }
 }
 // 1 / sqrt(sum / size + eps), from what group_sums_of leaves.
-template <bool MIXED, int V> __device__ __forceinline__ void inverse_roots(f2 (&v)[kPairs<V>], float per_group, float eps)
+template <int MIXED, int V> __device__ __forceinline__ void inverse_roots(f2 (&v)[kPairs<V>], float per_group, float eps)
 {
 #pragma unroll
     for (int j = 0; j < (MIXED ? kPairs<V> : 1); ++j) {
@@ -251,7 +268,7 @@ template <int V> __device__ __forceinline__ void keep(float* to, const f2 (&v)[k
 }
 
 // K vectors of V elements to a thread; blockDim.x threads to a row, blockDim.y rows to a block (more than one only where a row is a warp's).  Pairs of floats: 68 -> 60 us with every part.
-template <typename T, int V, int K, bool MIXED>
+template <typename T, int V, int K, int MIXED>
 __global__ void __launch_bounds__(K < 4 || V == 8 ? 512 : 1024) norm_kernel(const NormDev p)
 {
     __shared__ float buffer[2 * 32];
@@ -348,7 +365,7 @@ __global__ void __launch_bounds__(K < 4 || V == 8 ? 512 : 1024) norm_kernel(cons
 // Where a thread has one vector of each operand of a row, copies of the next rows' vectors into its own places of shared memory are under way (kAhead rows; no other thread looks at
 // them), so that memory is at work while the sums of a row are waited for (8192 x 2048: 106 -> 88 us; pairs of floats 88 -> 80).  80 registers for vectors of up to four elements, for more
 // blocks on an SM; eight do not fit there (81 -> 99 us, spilled).
-template <typename T, int V, int K, bool MIXED>
+template <typename T, int V, int K, int MIXED>
 __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) norm_grad_kernel(const NormDev p)
 {
     constexpr bool RING = K == 1 && V > 1;
@@ -570,11 +587,12 @@ __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) n
     }
 }
 
-// The workers' shares added up in their order: 32 channels to a block, eight runs of workers side by side.
-static __global__ void __launch_bounds__(256) norm_sum_kernel(const NormDev p)
+// The workers' shares added up in their order: 32 channels to a block, kRuns runs of workers side by side (2368 workers of 128 channels: with eight runs 22 us).
+constexpr int kRuns = 32;
+static __global__ void __launch_bounds__(32 * kRuns) norm_sum_kernel(const NormDev p)
 {
     wait_for_previous();
-    __shared__ float s[8][32];
+    __shared__ float s[kRuns][33];
     const int lane = threadIdx.x % 32, run = threadIdx.x / 32, which = blockIdx.y, c = blockIdx.x * 32 + lane;
     float* to = which == 0 ? p.dw_post : which == 1 ? p.dscale : p.dw_pre;
     if (!to)
@@ -582,18 +600,26 @@ static __global__ void __launch_bounds__(256) norm_sum_kernel(const NormDev p)
     float sum = 0.f;
     if (c < p.d) {
         const float* from = p.parts + (long long)which * p.d + c;
-        const int lo = (int)((long long)p.workers * run / 8), hi = (int)((long long)p.workers * (run + 1) / 8);
-#pragma unroll 8
-        for (int w = lo; w < hi; ++w)
-            sum += from[(long long)w * 3 * p.d];
+        const int lo = (int)((long long)p.workers * run / kRuns), hi = (int)((long long)p.workers * (run + 1) / kRuns);
+        for (int w = lo; w < hi; w += 16) {      // sixteen loads under way together
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                v[i] = load_if(from + (long long)(w + i) * 3 * p.d, w + i < hi);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                sum += v[i];
+        }
     }
     s[run][lane] = sum;
     __syncthreads();
-    if (run == 0 && c < p.d) {
-        for (int i = 1; i < 8; ++i)
-            sum += s[i][lane];
-        to[c] = sum;
-    }
+    sum = s[lane][run];                          // a warp for each channel
+#pragma unroll
+    for (int o = 16; o; o /= 2)
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    const int mine = blockIdx.x * 32 + run;
+    if (lane == 0 && mine < p.d)
+        to[mine] = sum;
 }
 
 } // namespace bnorm
