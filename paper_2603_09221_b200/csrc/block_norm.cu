@@ -1,4 +1,5 @@
 // Host side of ttc_block_norm and ttc_block_norm_grad.
+#include <algorithm>
 #include <type_traits>
 
 #include "block_host.h"
@@ -80,7 +81,7 @@ int ceil_pow2(int v)
 }
 
 // Vectors of 16 bytes where every row and parameter can be accessed so; else single elements.  Then as many
-// threads as give each at most `most` vectors, with more for rows that would need over 512 of them.
+// threads as give each at most `most` vectors, with more for rows that would need over 512 of them, in whole warps.
 Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> rows, int most)
 {
     const int v = 16 / (int)element_size(a->dtype);
@@ -97,8 +98,9 @@ Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> ro
     if (vectors > 2 * threads)
         threads = vectors > 4096 ? 1024 : ceil_pow2((vectors + 3) / 4) < 32 ? 32 : ceil_pow2((vectors + 3) / 4);
     const int k = (vectors + threads - 1) / threads;
-    o.threads = threads;
     o.k = k <= 1 ? 1 : k <= 2 ? 2 : k <= 4 ? 4 : 16;
+    // (160 threads for 152 vectors instead of 256: gradients of 13541 x 1216 134 -> 91 us, of 14563 x 1152 86 -> 58)
+    o.threads = threads = std::min(threads, ((vectors + o.k - 1) / o.k + 31) / 32 * 32);
     o.rows_per_block = threads == 32 ? kRowsOfWarps : 1;
     const int size = a->d / a->groups, lanes = size / o.v;
     p.lanes = lanes;

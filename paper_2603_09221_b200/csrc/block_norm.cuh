@@ -12,7 +12,8 @@
 //
 // Memory bounds both: every operand is read once and every result written once.  A row stays in the registers of the threads that share
 // it (a warp, or a block of up to 1024), in vectors of 16 bytes, where its sums are formed in float32.  Measured, and at the rate that copies reach: forward, 8192 x 4096 bfloat16 with every
-// part 60 us, 51; gradients, 8192 x 2048 of all of them 80, 41 (instructions: 56 % of the issue slots), groups of 64 channels in float32 43; 8 rows 2.6 us, two rounds of loads.
+// part 61 us, 51; gradients, 8192 x 2048 of all of them 77, 41 (instructions: 56 % of the issue slots), 4093 x 1000 in groups of 125 channels in float32 41, 13; 8 rows 2.6 us, two rounds
+// of loads.
 #pragma once
 
 #include <type_traits>
@@ -56,7 +57,7 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
         return;
     float* s = buffer + turn * 32 * N;
     turn ^= 1;
-    const int warps = blockDim.x / 32, lane = threadIdx.x % 32;
+    const int warps = blockDim.x / 32, lane = threadIdx.x % 32, span = 1 << (32 - __clz(warps - 1));       // (warps: two at least)
     if (lane == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -65,8 +66,8 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < N; ++i)
-        v[i] = s[i * 32 + lane % warps];         // (a power of two)
-    for (int o = warps / 2; o; o /= 2)
+        v[i] = (lane & (span - 1)) < warps ? s[i * 32 + (lane & (span - 1))] : 0.f;
+    for (int o = span / 2; o; o /= 2)
 #pragma unroll
         for (int i = 0; i < N; ++i)
             v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(K < 4 || V == 8 ? 512 : 1024) norm_kernel(cons
 // Workers (a block, or a warp of one) take every workers-th row and keep their shares of the parameters' gradients in registers.
 //
 // Where a thread has one vector of each operand of a row, copies of the next rows' vectors into its own places of shared memory are under way (kAhead rows; no other thread looks at
-// them), so that memory is at work while the sums of a row are waited for (8192 x 2048: 106 -> 88 us; pairs of floats 88 -> 80).  80 registers for vectors of up to four elements, for more
+// them), so that memory is at work while the sums of a row are waited for (8192 x 2048: 106 -> 88 us; pairs of floats 88 -> 81).  80 registers for vectors of up to four elements, for more
 // blocks on an SM; eight do not fit there (81 -> 99 us, spilled).
 template <typename T, int V, int K, int MIXED>
 __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) norm_grad_kernel(const NormDev p)
