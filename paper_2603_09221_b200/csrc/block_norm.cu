@@ -100,7 +100,8 @@ Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> ro
     const int k = (vectors + threads - 1) / threads;
     o.k = k <= 1 ? 1 : k <= 2 ? 2 : k <= 4 ? 4 : 16;
     // (160 threads for 152 vectors instead of 256: gradients of 13541 x 1216 134 -> 91 us, of 14563 x 1152 86 -> 58)
-    o.threads = threads = std::min(threads, ((vectors + o.k - 1) / o.k + 31) / 32 * 32);
+    const int each = o.k == 16 ? k : o.k;
+    o.threads = threads = std::min(threads, ((vectors + each - 1) / each + 31) / 32 * 32);
     o.rows_per_block = threads == 32 ? kRowsOfWarps : 1;
     const int size = a->d / a->groups, lanes = size / o.v;
     p.lanes = lanes;

@@ -145,8 +145,8 @@ int describe(CUtensorMap& map, const Rows& r, int heads, int width, int head, co
 void align(const Seqs& s, int heads, int width, Rows& r, int& head, Operands& o, Scratch& scratch)
 {
     const long long most = 1ll << 38;            // of strides in elements
-    const int vec = bytes_at_once(r, width);
-    if (!s.tokens || !s.batch || (vec == 16 && (r.ts || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most))
+    const int vec = bytes_at_once(r, width);             // (rows that lie over one another are not asked of the copy engine either)
+    if (!s.tokens || !s.batch || (vec == 16 && (r.ts >= (long long)heads * width || s.tokens <= 1) && (s.offsets || r.bs || s.batch <= 1) && r.ts < most && r.bs < most))
         return;
     const int padded = (width + 7) / 8 * 8;
     const long long row = (long long)heads * padded;

@@ -176,6 +176,18 @@ def test_one_row_for_all_tokens_and_one_sequence_for_all(dk, dv):
     assert all(torch.equal(got[n], want[n]) for n in want)
 
 
+def test_tokens_of_all_sequences_beside_one_another_and_rows_over_one_another():
+    """Strides in another order ([tokens, batch, ..]), and windows that overlap: what their copies give."""
+    i = _inputs((3, 150), 3, 4, 2, 64, 64, B, 16, grad=True)
+    for n in ("q", "v", "dy", "delta"):
+        i[n] = i[n].transpose(0, 1).contiguous().transpose(0, 1)
+    line = i["k"].flatten()
+    i["k"] = line.as_strided((3, 150, 2, 64), (4096, 8, 64, 1))
+    call = lambda j: dict(block.decay_attention_grad(j["dy"], j["q"], j["k"], j["v"], j["A"], j["delta"], j["delta_bias"], True, None, j["state"], None, j["dlast"]), y=_call(j))  # noqa: E731
+    got, want = call(i), call({n: t.contiguous() if torch.is_tensor(t) else t for n, t in i.items()})
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
 def test_other_sequences_infinities_stay_there():
     i = _inputs((300,), 3, 2, 2, 64, 64, B, 17, offsets=[0, 100, 180, 300])
     clean = _call(i).clone()
