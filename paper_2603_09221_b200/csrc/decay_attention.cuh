@@ -358,6 +358,7 @@ struct Control {
     int dead;
 };
 
+// Behind wait_for_previous, as in every kernel here: blocks that held tensor memory while they wait would keep it from those of the kernel in front on the same SM.
 __device__ __forceinline__ uint32_t set_up(Control& c, int columns)
 {
     if (threadIdx.x == 0) {
