@@ -341,8 +341,8 @@ int plan_grad(int device, const ttc_decay_args* a, const ttc_decay_grads* g, voi
         p.f.seq_first = s.take<int>(a->batch + 1);
     }
     const size_t each = (size_t)p.f.chunks * a->heads, image = (size_t)padded(a->dk) * padded(a->dv) * 2 * (p.terms = a->dtype == TTC_BF16 && p.want_l ? 3 : 2);
-    p.image_S = s.take<char>(each * image);
-    p.image_Z = s.take<char>(each * image);
+    p.image_S = s.take<char>(std::max(each * image, (size_t)1));     // (there even for no chunks: a walk without images is one for what a piece adds)
+    p.image_Z = s.take<char>(std::max(each * image, (size_t)1));
     if (a->dtype == TTC_F16) {
         p.unit_S = s.take<float>(each);
         p.unit_Z = s.take<float>(each);

@@ -450,3 +450,42 @@ def test_rows_past_32_bits():
     want = block.decay_attention_grad(c(dy), c(q), c(k), c(v), A, offsets=offsets, want=some, out=new())
     got = block.decay_attention_grad(dy, q, k, v, A, offsets=offsets, want=some, out=new())
     assert all(torch.equal(got[n], want[n]) and bool(got[n][59000:59990].any()) for n in some)
+
+
+def test_no_tokens_and_no_sequences():
+    g = torch.Generator(device=DEV).manual_seed(5)
+    S, A = torch.randn((2, 3, 16, 24), generator=g, device=DEV), -torch.ones(3, device=DEV)
+    q, v = torch.zeros((2, 0, 1, 16), device=DEV, dtype=B), torch.zeros((2, 0, 3, 24), device=DEV, dtype=B)
+    last = torch.full_like(S, float("nan"))
+    assert block.decay_attention(q, q, v, A, state=S, state_out=last).shape == v.shape
+    got = block.decay_attention_grad(v, q, q, v, A, state=S, dstate_out=2 * S)
+    assert torch.equal(last, S) and torch.equal(got["dstate"], 2 * S) and bool((got["dA"] == 0).all()) and got["dq"].shape == q.shape
+    none = block.decay_attention(q[:0], q[:0], v[:0], A)
+    assert none.shape == (0, 0, 3, 24)
+    one = block.decay_attention_step(q[:0, 0:0].reshape(0, 1, 16), q[:0].reshape(0, 1, 16), v[:0].reshape(0, 3, 24), A, S[:0])
+    assert one.shape == (0, 3, 24)
+
+
+def test_calls_from_several_threads():
+    import threading
+
+    some = [_inputs((2, n), 2, 4, 2, 64, 64, B, n, grad=True) for n in (200, 300, 500, 1400)]
+    both = lambda i: (_call(i), block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"])["dk"],  # noqa: E731
+                      block.block_norm(i["v"].flatten(-2), w_pre=torch.ones(256, device=DEV))[1])
+    want, wrong = [both(i) for i in some], []
+    torch.cuda.synchronize()
+
+    def work(i, w):
+        s = torch.cuda.Stream(device=DEV)
+        with torch.cuda.stream(s):
+            for _ in range(20):
+                got = both(i)
+                s.synchronize()
+                wrong.extend(n for n in range(3) if not torch.equal(got[n], w[n]))
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(some, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and block.device_error(0) == 0
