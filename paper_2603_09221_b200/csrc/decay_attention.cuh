@@ -1153,7 +1153,10 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
     const Piece piece = piece_at(p, where.piece);
     if (piece.owner < 0 || (!q.image && (BACK ? piece.first : piece.last)))
         return;
-    const int n = __shfl_sync(0xffffffffu, (int)((piece.len + kChunk - 1) / kChunk), 0);
+    // its first chunk's number; offsets that decrease could ask for more chunks than there is room for: those behind are left out
+    const long long first = q.image ? (p.seqs.offsets ? states.seq_first[piece.owner] : piece.owner * p.chunks_per_seq) + piece.t0 / kChunk : 0;
+    const long long chunks = (piece.len + kChunk - 1) / kChunk;
+    const int n = __shfl_sync(0xffffffffu, (int)(q.image ? min(chunks, max(p.chunks - first, 0ll)) : chunks), 0);
     if (threadIdx.x == 0) {
         auto init = [](uint64_t& bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(smem_u32(&bar)), "r"(count) : "memory"); };
         for (int i = 0; i < 2; ++i) {
@@ -1311,7 +1314,6 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
         const bool mine = quarter * 32 < DK;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const long long place = ((where.piece * p.heads + head) * splits + z) * (kWalkThreads * OWN);
-        const long long first = q.image ? (p.seqs.offsets ? states.seq_first[piece.owner] : piece.owner * p.chunks_per_seq) + piece.t0 / kChunk : 0;
         float S[OWN];
         if (q.image && !(BACK ? piece.last : piece.first)) {
 #pragma unroll

@@ -489,3 +489,28 @@ def test_calls_from_several_threads():
     for t in threads:
         t.join()
     assert not wrong and block.device_error(0) == 0
+
+
+@pytest.mark.parametrize("dtype", [B, H])
+@pytest.mark.parametrize("heads, offsets", [(2, [-50, 200, 100, 1 << 30, 250]), (2, [0, 300] * 10 + [0]), (40, [0, 300] * 10 + [0]), (2, [0, 300] * 40)])
+def test_offsets_that_make_no_sense_stay_in_range(monkeypatch, heads, offsets, dtype):
+    """Offsets beyond the rows and ones that jump back, which ask for more chunks than there is room for: nothing outside of scratch and results is touched."""
+    kept = []
+
+    def guarded(need, x, stream):
+        block._check(min(need, 0))
+        kept.append((torch.full((need + 512,), 0x5a, dtype=torch.uint8, device=DEV), need))
+        return kept[-1][0], kept[-1][0].data_ptr() + 256
+
+    monkeypatch.setattr(block, "_workspace", guarded)
+    block._load()
+    monkeypatch.setattr(block, "_step", block._LongWay)                           # (the short way has scratch of its own)
+    i = _inputs((300,), len(offsets) - 1, heads, heads, 64, 64, dtype, 51, offsets=offsets, grad=True)
+    guard = torch.full((500, heads, 64), 3.0, device=DEV, dtype=dtype)
+    last = torch.empty_like(i["state"])
+    _call(i, y=guard[100:400], state_out=last)
+    block.decay_attention_grad(i["dy"], i["q"], i["k"], i["v"], i["A"], i["delta"], i["delta_bias"], True, None, i["state"], i["offsets"], i["dlast"])
+    torch.cuda.synchronize()
+    assert len(kept) == 2 and bool((guard[:100] == 3).all()) and bool((guard[400:] == 3).all()) and block.device_error(0) == 0
+    for ws, need in kept:
+        assert bool((ws[:256] == 0x5a).all()) and bool((ws[256 + need:] == 0x5a).all())
