@@ -879,7 +879,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const long long place = ((where.piece * p.heads + head) * splits + where.part) * (kWalkThreads * 16);
         float S[16];
-        if (!piece.first) {
+        if (!piece.first || !piece.last) {       // (the first piece too: the last one may write over the states in front of the sequences)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 *reinterpret_cast<float4*>(S + 4 * j) = *reinterpret_cast<const float4*>(p.piece_state + place + (j * kWalkThreads + threadIdx.x) * 4);
@@ -1521,8 +1521,7 @@ static __global__ void __launch_bounds__(kWalkThreads) join_kernel(const AttnDev
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             if (i0 + i < n - 1) {
-                if (i0 + i > 0)
-                    *at(i0 + i) = S;
+                *at(i0 + i) = S;
                 S.x = fmaf(w[i], S.x, u[i].x), S.y = fmaf(w[i], S.y, u[i].y), S.z = fmaf(w[i], S.z, u[i].z), S.w = fmaf(w[i], S.w, u[i].w);
             }
         }

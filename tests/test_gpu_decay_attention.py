@@ -188,6 +188,19 @@ def test_tokens_of_all_sequences_beside_one_another_and_rows_over_one_another():
     assert all(torch.equal(got[n], want[n]) for n in want)
 
 
+@pytest.mark.parametrize("offsets", [None, [0, 1, 2000, 3000]])
+def test_state_in_place_where_sequences_are_cut(offsets):
+    """The first piece does not find what the last one leaves."""
+    lead = (1, 3000) if offsets is None else (3000,)
+    i = _inputs(lead, 1 if offsets is None else 3, 2, 1, 64, 64, B, 18, strength=0.01, offsets=offsets)
+    last = torch.empty_like(i["state"])
+    want, given = _call(i, state_out=last), i["state"].clone()
+    for _ in range(20):
+        i["state"].copy_(given)
+        y = _call(i, state_out=i["state"])
+        assert torch.equal(y, want) and torch.equal(i["state"], last)
+
+
 def test_other_sequences_infinities_stay_there():
     i = _inputs((300,), 3, 2, 2, 64, 64, B, 17, offsets=[0, 100, 180, 300])
     clean = _call(i).clone()
