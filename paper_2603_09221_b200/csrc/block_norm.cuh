@@ -45,9 +45,13 @@ struct NormDev {
 
 extern __shared__ __align__(16) float bnorm_smem[];
 
-// Sums of N values over the threads of a row.  `buffer` [2][32 N]: two take turns, so that one barrier is enough.
+constexpr int kSlot = 2 * 32;                    // of two values over 32 warps
+
+// Sums of N values (one or two) over the threads of a row.  `buffer` [2][kSlot]: two take turns, so that one barrier is enough.  They lie apart whatever N is: calls
+// of one and of two values take turns on the same buffer.
 template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* buffer, int& turn)
 {
+    static_assert(32 * N <= kSlot, "");
 #pragma unroll
     for (int o = 16; o; o /= 2)
 #pragma unroll
@@ -55,7 +59,7 @@ template <int N> __device__ __forceinline__ void row_sums(float (&v)[N], float* 
             v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
     if (blockDim.x == 32)
         return;
-    float* s = buffer + turn * 32 * N;
+    float* s = buffer + turn * kSlot;
     turn ^= 1;
     const int warps = blockDim.x / 32, lane = threadIdx.x % 32, span = 1 << (32 - __clz(warps - 1));       // (warps: two at least)
     if (lane == 0) {
@@ -272,7 +276,7 @@ template <int V> __device__ __forceinline__ void keep(float* to, const f2 (&v)[k
 template <typename T, int V, int K, int MIXED>
 __global__ void __launch_bounds__(K < 4 || V == 8 ? 512 : 1024) norm_kernel(const NormDev p)
 {
-    __shared__ float buffer[2 * 32];
+    __shared__ float buffer[2 * kSlot];
     wait_for_previous();
     const long long row = (long long)blockIdx.x * blockDim.y + threadIdx.y;
     const bool here = row < p.rows;
@@ -371,7 +375,7 @@ __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) n
 {
     constexpr bool RING = K == 1 && V > 1;
     constexpr int P = kPairs<V>;
-    __shared__ float buffer[2 * 32 * 2];
+    __shared__ float buffer[2 * kSlot];
     wait_for_previous();
     const int worker = blockIdx.x * blockDim.y + threadIdx.y, vectors = p.d / V;
     int turn = 0;
