@@ -815,6 +815,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                 copies_done<0>();
                 to_tensor_cores();
             }
+            __syncwarp();                        // what the elected lane wrote of the table, whose arrival came with its copies, is there before the others arrive
             if (!arrived)
                 arrive(bar);
         }
@@ -1277,6 +1278,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
                 copies_done<0>();
                 to_tensor_cores();
             }
+            __syncwarp();                        // what the elected lane wrote of the table, whose arrival came with its copies, is there before the others arrive
             if (!arrived)
                 arrive(bar);
         }
