@@ -425,6 +425,7 @@ __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) n
         const long long row = round * p.workers + worker;
         const bool here = row < p.rows;
         const long long lead = here ? row : 0;
+        const float eps = here ? p.eps : 1.f;    // (a row behind the last, of zeros, has finite roots whatever eps is: it adds zeros to the parameters' gradients)
         Vec<T, V> x[K], z[K], h[K], dy[K], dh[K];
         if constexpr (RING) {
             asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
@@ -467,7 +468,7 @@ __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) n
             }
             float sums[2] = {sum_of(square), sum_of(product)};
             row_sums<2>(sums, buffer, turn);
-            const float rms = rsqrtf(fmaf(sums[0], p.per_row, p.eps));
+            const float rms = rsqrtf(fmaf(sums[0], p.per_row, eps));
             const f2 rms2 = both(rms), mean = both(-sums[1] * p.per_row * rms * rms);
 #pragma unroll
             for (int k = 0; k < K; ++k) {
@@ -501,7 +502,7 @@ __global__ void __maxnreg__(K == 1 && V < 8 ? 80 : K < 4 || V == 8 ? 128 : 64) n
             group_sums_of<MIXED, K, V>(p, inverse, area, buffer, turn);
 #pragma unroll
             for (int k = 0; k < K; ++k)
-                inverse_roots<MIXED, V>(inverse[k], p.per_group, p.eps);
+                inverse_roots<MIXED, V>(inverse[k], p.per_group, eps);
         }
 #pragma unroll
         for (int k = 0; k < K; ++k) {

@@ -37,3 +37,11 @@ def test_one_group_and_the_next_norm_over_many_warps(rows, d, dtype):
     for _ in range(30):
         got = block.block_norm_grad(**i, eps=1e-5, residual=True)
         assert all(torch.equal(got[n], first[n]) for n in first)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 149, 600, 1187])
+@pytest.mark.parametrize("d, groups, dtype", [(64, 1, F), (96, 4, B), (1000, 8, F), (257, 1, H), (2048, 16, B), (2048, 1, B)])
+def test_no_eps(rows, d, groups, dtype):
+    """With an eps of nothing, rows that are not there (the last round of a kernel's workers) leave the parameters' gradients alone."""
+    i = _inputs(rows, d, dtype, rows)
+    _check(i, groups, 0.0, block.block_norm_grad(**i, eps=0.0, groups=groups, residual=True))
