@@ -135,10 +135,13 @@ template <typename F> int by_way(int dtype, const Way& w, F&& f)
     });
 }
 
+// The most that a call asks for: gradients of 512 threads (a ring of 240 bytes each) in groups of one channel (4096 of them, 8 bytes each), 152 KB; rows of 16384 without a ring, 128 KB.  A
+// kernel's limit is set to this by every call that needs it set, and never to less: what one thread sets has to serve another's launch.
+constexpr int kMostShared = 160 * 1024;
 template <typename K> int allow_smem(K* kernel, size_t bytes)
 {
     if (bytes > 40 * 1024)
-        TTC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes));
+        TTC_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared));
     return TTC_OK;
 }
 

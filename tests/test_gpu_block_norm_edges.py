@@ -45,3 +45,39 @@ def test_no_eps(rows, d, groups, dtype):
     """With an eps of nothing, rows that are not there (the last round of a kernel's workers) leave the parameters' gradients alone."""
     i = _inputs(rows, d, dtype, rows)
     _check(i, groups, 0.0, block.block_norm_grad(**i, eps=0.0, groups=groups, residual=True))
+
+
+def test_several_threads_with_rows_of_different_widths():
+    """Calls of one kernel that need more and less shared memory (123 and 61 KB), from threads that do not wait for one another: none takes the other's."""
+    import threading
+
+    lib, calls = block._load(), []
+    for d in (2048, 4096) * 4:
+        i = _inputs(4, d, B, d)
+        out = {n: torch.empty_like(i["x"]) for n in ("dx", "dz", "dr")}
+        w = {n: torch.empty_like(i["w_pre"]) for n in ("post", "scale", "pre")}
+        at = lambda t: t.data_ptr()  # noqa: E731
+        record = block._NORM_ARGS.pack(4, d, 16, block._type_of(i["x"]), 1e-5, at(i["x"]), at(i["z"]), 0, at(i["h"]), 0, d, d, 0, d, 0, *(at(i[n]) for n in ("w_post", "scale", "w_pre")))
+        grads = block._NORM_GRADS.pack(at(i["dy"]), at(i["dh"]), *(at(t) for t in out.values()), *[d] * 5, *(at(t) for t in w.values()))
+        need = lib.ttc_block_norm_grad_workspace(0, record, grads)
+        calls.append((record, grads, torch.empty(need, dtype=torch.uint8, device=DEV), need, torch.cuda.Stream(device=DEV), (i, out, w)))
+    torch.cuda.synchronize()
+    statuses, go = [], threading.Barrier(len(calls))
+
+    def work(record, grads, ws, need, stream, kept):
+        go.wait()
+        for _ in range(3000):
+            status = lib.ttc_block_norm_grad(0, record, grads, ws.data_ptr(), need, stream.cuda_stream)
+            if status:
+                statuses.append(status)
+                return
+
+    threads = [threading.Thread(target=work, args=c) for c in calls]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not statuses
+    i, out, w = calls[1][-1]
+    _check(i, 16, 1e-5, dict(dx=out["dx"], dz=out["dz"], dresidual=out["dr"], dw_post=w["post"], dscale=w["scale"], dw_pre=w["pre"]))
