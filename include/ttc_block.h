@@ -255,7 +255,7 @@ int ttc_block_norm(int32_t device, const ttc_norm_args* a, void* cuda_stream);
 
 /*
  * Gradients of ttc_block_norm given dy (with w_pre) and dh (the gradient of h by what else reads it; NULL: zero).  `a` as in the forward call, but h is an input, as
- * the forward call wrote it (needed with w_pre; NULL where nothing changes x: h is x then), and residual and y are not used.  dresidual receives the whole gradient of h, and may be dh;
+ * the forward call wrote it (needed with w_pre; NULL where nothing changes x, no residual either: h is x then), and y is not used, nor what residual points to.  dresidual receives the whole gradient of h, and may be dh;
  * dx, dz in the rows' type, dw_post, dscale, dw_pre [d] float32.
  */
 typedef struct ttc_norm_grads {

@@ -721,7 +721,7 @@ def block_norm(x, w_post=None, z=None, scale=None, residual=None, w_pre=None, ep
 def block_norm_grad(x, h=None, dy=None, dh=None, w_post=None, z=None, scale=None, w_pre=None, eps=1e-6, groups=1, residual=False, want=None, out=None,
                     stream=None):
     """Gradients of :func:`block_norm` given ``dy`` (with ``w_pre``) and ``dh``, the gradient of ``h`` by what else reads it (default: zero).  ``h`` as the
-    forward call returned it (needed with ``w_pre``, unless ``h`` is ``x``); ``residual``: whether there was one.  Returns a dict with the wanted of ``dx, dz, dresidual,
+    forward call returned it (needed with ``w_pre``, unless nothing changed ``x``); ``residual``: whether there was one.  Returns a dict with the wanted of ``dx, dz, dresidual,
     dw_post, dscale, dw_pre`` (default: all whose operand is there); ``out`` may hold tensors to write them to, ``dresidual`` may be ``dh``."""
     if stream is None and want is None and out is None:
         if _step is None:
@@ -730,6 +730,8 @@ def block_norm_grad(x, h=None, dy=None, dh=None, w_post=None, z=None, scale=None
         if got is not None:
             return got
     code, dtype, dev, d, rows, kept, px, pz, ldx, ldz, vectors = _norm_operands(x, w_post, z, scale, w_pre, groups, stream)
+    if residual and h is None and w_pre is not None and rows:
+        raise ValueError("w_pre behind a residual wants h, as block_norm returned it")
     more = []
     for t, name in ((h, "h"), (dy, "dy"), (dh, "dh")):
         if t is not None and t.shape != x.shape:

@@ -204,7 +204,7 @@ int plan_grad(int device, const ttc_norm_args* a, const ttc_norm_grads* g, void*
         for (int j = 0; j < i; ++j)
             TTC_TRY(check_overlap(a, outs[i], outs[j], false));
     }
-    if (a->rows && a->w_pre && (!g->dy || (!a->h && changes(a))))
+    if (a->rows && a->w_pre && (!g->dy || (!a->h && (changes(a) || g->dresidual))))
         return fail(TTC_STATUS_INVALID_ARGUMENT, "w_pre without dy or h");
     if (g->dy && !a->w_pre)
         return fail(TTC_STATUS_INVALID_ARGUMENT, "dy without w_pre");
