@@ -459,7 +459,7 @@ def _decay_record(q, k, v, A, delta, delta_bias, softplus, scale, state, offsets
     if step:
         batch, tokens, off, rows = v.shape[0], 1, 0, _rows1
     else:
-        batch, tokens, off, rows = _sequences(v[..., 0], offsets)
+        batch, tokens, off, rows = _sequences(v[..., :0].flatten(-2), offsets)
     lead = tuple(v.shape[:lead])
     if delta is None and delta_bias is not None:
         raise ValueError("delta_bias without delta")

@@ -27,3 +27,12 @@ def test_the_norm_behind_a_residual_wants_h():
     for want in (None, ["dx"], ["dw_pre"]):
         with pytest.raises(ValueError, match="residual wants h"):
             block.block_norm_grad(x, dy=x, w_pre=w, residual=True, want=want)
+
+
+@pytest.mark.parametrize("heads, dv", [(0, 32), (4, 0)])
+def test_no_heads_or_no_channels(heads, dv):
+    q, v = torch.zeros((2, 8, 2, 16), dtype=torch.bfloat16), torch.zeros((2, 8, heads, dv), dtype=torch.bfloat16)
+    A, state = torch.zeros(heads), torch.zeros((2, heads, 16, dv))
+    for call in (lambda: block.decay_attention(q, q, v, A), lambda: block.decay_attention_grad(v, q, q, v, A), lambda: block.decay_attention_step(q[:, 0], q[:, 0], v[:, 0], A, state)):
+        with pytest.raises(ValueError):
+            call()
