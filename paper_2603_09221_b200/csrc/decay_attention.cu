@@ -227,6 +227,7 @@ template <typename K> int allow_smem(K* kernel, int bytes)
 template <typename T, int DK, int COLS> int piece_states(const Maps (&maps)[2], const AttnDev& p, States q, int ways, int splits, cudaStream_t st)
 {
     q.way[0].image = q.way[1].image = nullptr;
+    q.way[0].other = q.way[1].other = nullptr;   // (which nobody has written yet)
     q.ways = ways;
     const dim3 grid((unsigned)(p.pieces * p.heads * splits * ways));
     constexpr int smem = StateShape<T, DK, COLS>::SMEM;
