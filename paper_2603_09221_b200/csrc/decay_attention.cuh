@@ -15,7 +15,9 @@
 // Exponents.  None is positive: pairs of tokens of one block of 32 take exp(G_i - G_j) itself, from sums within the block; others the product
 // of exp(from the block's begin to i) and exp(from j to that begin), so that no difference of long sums is formed.  Exponents
 // below -192 / log2(e) count as that (their exponentials are zero), so that a decay of minus infinity, which forgets
-// everything, gives no difference of infinities.
+// everything, gives no difference of infinities.  The sums within a block reach 32 times that, where float32's steps are 5e-4: what their additions round off is
+// carried along in a second number, so that a difference of two of them is off by its own rounding alone, whatever stands in front of both tokens (with one number 25 tokens that
+// forget, in front of seven that do not, put dA off by 1.2e-5 of the sum of its terms' magnitudes).
 //
 // Roundings.  Sums are float32 in tensor memory, states float32.  Operands of the tensor cores are 16 bits: scores with their decay, and S_0 where q
 // multiplies it, are rounded once (half a step each, as the result itself).  The weighted values of S_C are not: states are float32 results and are carried on, so
@@ -86,6 +88,7 @@ __device__ __forceinline__ Chunk chunk_at(const AttnDev& p, long long c)
 
 struct alignas(16) Decays {
     float g[kChunk];                             // sums to the base 2 from the begin of the token's block of 32, the token's own included
+    float low[kChunk];                           // what their additions rounded off
     float s[kChunk];                             // behind the token, to the end of its block
     float block[4];                              // of whole blocks
 };
@@ -110,15 +113,22 @@ template <typename T> __device__ __forceinline__ float log_decay_at(const AttnDe
     return t < c.len ? log_decay(rate(p, head), p.delta.ptr ? step_of(p, raw_step<T>(p, c.seq, c.row0 + t, head)) : 1.f) : 0.f;
 }
 
-// By one warp for the 32 tokens of a block, from the log decay of each lane's token: the sum from the block's begin, and behind the token to its end.
-__device__ __forceinline__ float block_sums(float l, float& behind)
+// By one warp for the 32 tokens of a block, from the log decay of each lane's token: the sum from the block's begin, and behind the token to its end.  LOW: what the additions of the
+// first one rounded off, too (by Knuth's sum of two numbers with its rounding error).
+template <bool LOW> __device__ __forceinline__ float block_sums(float l, float& behind, float& low)
 {
     const int lane = threadIdx.x % 32;
     float g = l, s = l;
+    low = 0.f;
 #pragma unroll
     for (int i = 1; i < 32; i *= 2) {
-        const float a = __shfl_up_sync(0xffffffffu, g, i), b = __shfl_down_sync(0xffffffffu, s, i);
-        g += lane >= i ? a : 0.f;
+        const float up = __shfl_up_sync(0xffffffffu, g, i), b = __shfl_down_sync(0xffffffffu, s, i);
+        const float a = lane >= i ? up : 0.f, sum = g + a;
+        if (LOW) {
+            const float up_low = __shfl_up_sync(0xffffffffu, low, i), part = sum - g;
+            low += (lane >= i ? up_low : 0.f) + ((g - (sum - part)) + (a - part));
+        }
+        g = sum;
         s += lane + i < 32 ? b : 0.f;
     }
     s = __shfl_down_sync(0xffffffffu, s, 1);
@@ -127,7 +137,7 @@ __device__ __forceinline__ float block_sums(float l, float& behind)
 }
 __device__ __forceinline__ void block_decays(float l, int t, Decays& o)
 {
-    o.g[t] = block_sums(l, o.s[t]);
+    o.g[t] = block_sums<true>(l, o.s[t], o.low[t]);
     if (t % 32 == 31)
         o.block[t / 32] = o.g[t];
 }
@@ -591,6 +601,7 @@ template <typename T, int DK> struct WalkShape {
         uint32_t tmem;
         int dead;
         Table dec[2];
+        alignas(8) float low[2][kIsBf16<T> ? 2 : kChunk];            // of the sums within blocks: what their additions rounded off (up to 2e-4, of weights that bfloat16 rounds by 2e-3)
         float most[kIsBf16<T> ? 1 : 32];
     };
     static constexpr int TILES = 2 * STAGE + TERMS * V_BYTES + IMAGE;
@@ -778,11 +789,11 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             };
             if (i < 2)                           // nothing to wait for
                 fetch();
-            float sum[4 / kFrontWarps], behind[4 / kFrontWarps];
+            float sum[4 / kFrontWarps], behind[4 / kFrontWarps], low[4 / kFrontWarps];
 #pragma unroll
             for (int b = 0; b < 4 / kFrontWarps; ++b) {
                 const float l = log_decay(A, p.delta.ptr ? step_of(p, to_f(raw[b]) + bias) : 1.f);
-                sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind[b]);
+                sum[b] = block_sums<!kIsBf16<T>>(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind[b], low[b]);
                 behind[b] = ex2(behind[b]);
             }
             if (i + 1 < n)
@@ -794,6 +805,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             for (int b = 0; b < 4 / kFrontWarps; ++b) {
                 const int t = b * 32 * kFrontWarps + thread;
                 dec.g[t] = sum[b];
+                if (!kIsBf16<T>)
+                    sm.low[i & 1][t] = low[b];
                 dec.to_end[t] = behind[b];
                 if (lane == 31)
                     dec.block[t / 32] = sum[b];
@@ -975,10 +988,17 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                 float v[8];
                 tmem_ld8(scores + at + lanes, v);
                 uint32_t r[4];
+                const float* low = sm.low[i & 1];
+                const float mine_low = kIsBf16<T> ? 0.f : low[row];
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {                     // (of later tokens it may be infinite: they are taken out behind it)
                     const float2 h = *reinterpret_cast<const float2*>(dec.g + at + j);
-                    const uint32_t w = pack16<T>(v[j] * (p.scale * ex2(mine - h.x)), v[j + 1] * (p.scale * ex2(mine - h.y)));
+                    float d0 = mine - h.x, d1 = mine - h.y;
+                    if (!kIsBf16<T>) {
+                        const float2 l = *reinterpret_cast<const float2*>(low + at + j);
+                        d0 += mine_low - l.x, d1 += mine_low - l.y;
+                    }
+                    const uint32_t w = pack16<T>(v[j] * (p.scale * ex2(d0)), v[j + 1] * (p.scale * ex2(d1)));
                     r[j / 2] = lane > sub * 8 + j ? w : lane == sub * 8 + j ? w & 0xffffu : 0u;
                 }
                 tmem_st4(operand + at / 2 + lanes, r);
@@ -1211,8 +1231,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) state_walk_kernel(const __grid_
 #pragma unroll
                 for (int b = 0; b < 4 / kFrontWarps; ++b) {
                     const float l = log_decay(A, p.delta.ptr ? step_of(p, to_f(raw[b]) + bias) : 1.f);
-                    float behind;
-                    sum[b] = block_sums(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind);
+                    float behind, low;           // (no differences here)
+                    sum[b] = block_sums<false>(b * 32 * kFrontWarps + thread < c.len ? l : 0.f, behind, low);
                     own[b] = ex2(BACK ? sum[b] : behind);
                 }
                 if (i + 1 < n)

@@ -349,12 +349,12 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
     }
     {
         const int first = sub * 8, from = quarter * 32 + first;
-        const float own = dec.g[row];
+        const float own = dec.g[row], own_low = dec.low[row];
         float v[8];
         tmem_ld8(slopes + from + lanes, v);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            v[j] = first + j <= lane ? v[j] * ex2(own - dec.g[from + j]) : 0.f;
+            v[j] = first + j <= lane ? v[j] * ex2((own - dec.g[from + j]) + (own_low - dec.low[from + j])) : 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             diagonal[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
@@ -532,14 +532,14 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
     }
     {
         const int first = sub * 8, from = quarter * 32 + first;
-        const float own = dec.g[row];
+        const float own = dec.g[row], own_low = dec.low[row];
         float v[8], w[8];
         tmem_ld8(scores + from + lanes, v);
         tmem_ld8(slopes + from + lanes, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool later = first + j >= lane;
-            const float d = ex2(dec.g[from + j] - own) * p.scale;
+            const float d = ex2((dec.g[from + j] - own) + (dec.low[from + j] - own_low)) * p.scale;
             v[j] = later ? v[j] * d : 0.f;
             w[j] = later ? w[j] * d : 0.f;
         }

@@ -37,3 +37,69 @@ def test_tables_of_many_chunks_are_whole(dtype):
         (y2, last2), got = _forward(i), _grads(i)
         assert torch.equal(y, y2) and torch.equal(last, last2) and all(torch.equal(got[n], grads[n]) for n in grads)
     assert block.device_error(0) == 0
+
+
+def _args(i, scale):
+    f = lambda n: None if i[n] is None else au.f64(i[n])[0]  # noqa: E731
+    state = None if i["state"] is None else au.f64(i["state"])
+    return f("q"), f("k"), f("v"), au.f64(i["A"]), f("delta"), None, False, scale, state, [(0, i["q"].shape[1])]
+
+
+def _roundings(i, args):
+    """As the other tests of linear attention count them, but for the arguments of exponentials: weights are zero where the sum of log2 decays between two tokens is below
+    -126 (2^-126 of a product at most, which `within` leaves room for), so that no sum of more than that, with what rounding it costs, is behind a result."""
+    dk, dv, tokens = args[0].shape[-1], args[2].shape[-1], args[2].shape[0]
+    L = min(128 * float(np.abs(args[3] * args[4]).max()) * np.log2(np.e), 128.0)
+    return 2 * (dk + dv + 3 * 128) + 8 * L + 16 * -(-tokens // 128) + 64
+
+
+def _check(i, scale=None):
+    """y and the gradients of the rows are off by the half step of each operand of 16 bits besides float32's operations; states, dstate, dA and ddelta_bias by these alone."""
+    args = _args(i, i["q"].shape[-1] ** -0.5 if scale is None else scale)
+    R = _roundings(i, args) * au.U
+    h = au.half_step(i["q"].dtype)
+    y, last = _forward(i, scale)
+    want, want_last, _, _ = au.attend(*args)
+    mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
+    au.within(y[0], want, (h + R) * mag, y.dtype, "y")
+    au.within(last, want_last, R * mag_last, F, "state_out")
+    dlast = au.f64(i["dlast"])
+    ref, mag = (au.attend_grad(au.f64(i["dy"])[0], *args, dlast, magnitudes=m) for m in (False, True))
+    for n, t in _grads(i, scale).items():
+        rows = n in ("dq", "dk", "dv", "ddelta")
+        more = 256 + (0 if rows else args[2].shape[0])
+        au.within(t[0] if rows else t, ref[n], (h * (n in ("dq", "dk", "dv")) + 2 * R + more * au.U) * mag[n], t.dtype, n)
+    assert block.device_error(0) == 0
+
+
+@pytest.mark.parametrize("strength", [1.0, 30.0, 1e4])
+@pytest.mark.parametrize("dtype", [B, H])
+def test_strong_decays_among_weak_ones(strength, dtype):
+    i = _inputs(260, 4, 32, 32, dtype, 5)
+    strong = torch.rand(1, 260, 4, generator=torch.Generator(device=DEV).manual_seed(6), device=DEV) < 0.3
+    i["delta"] = torch.where(strong, i["delta"].float() * strength * 50, i["delta"].float() * 0.01).clamp(max=3e4).to(dtype)
+    _check(i)
+
+
+@pytest.mark.parametrize("dtype", [B, H])
+@pytest.mark.parametrize("large", [100.0, 1e4, float("inf")])
+@pytest.mark.parametrize("at", [0, 32, 96])
+def test_weak_decays_behind_many_that_forget_everything(dtype, large, at):
+    """What passes through decays is a sum over pairs of tokens, each exp of the decays between the two whatever stands in front of them in their block: 25 tokens that forget, and
+    seven that do not.  Operands are -1, 0 and 1 (keys 0 in front of the block), so that products are exact; a pair's weight is off by some 16 u (its exponential, its argument
+    below 1) and passes fewer than 150 additions and products."""
+    i = _inputs(at + 32, 16, 16, 16, dtype, 7)
+    for n in ("q", "k", "v", "dy"):
+        i[n] = i[n].round().clamp(-1, 1)
+    i["k"][:, :at] = 0
+    i["A"].fill_(-1.0)
+    i["delta"] = i["delta"] * 0.02 + 0.01
+    i["delta"][:, at:at + 25] = large
+    i["state"] = i["dlast"] = None
+    args = _args(i, 1.0)
+    args = (*args[:4], np.minimum(args[4], 1e4), *args[5:])                       # (1e4 and infinity are the same decay)
+    ref, mag = (au.attend_grad(au.f64(i["dy"])[0], *args, None, magnitudes=m) for m in (False, True))
+    got = _grads(i, 1.0, want=["ddelta", "dA", "ddelta_bias"])
+    for n in ("dA", "ddelta_bias"):
+        au.within(got[n], ref[n], 200 * au.U * mag[n], F, n)
+    au.within(got["ddelta"][0], ref["ddelta"], 200 * au.U * mag["ddelta"], dtype, "ddelta")
