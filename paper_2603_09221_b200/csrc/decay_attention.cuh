@@ -20,7 +20,8 @@
 // forget, in front of seven that do not, put dA off by 1.2e-5 of the sum of its terms' magnitudes).
 //
 // Roundings.  Sums are float32 in tensor memory, states float32.  Operands of the tensor cores are 16 bits: scores with their decay, and S_0 where q
-// multiplies it, are rounded once (half a step each, as the result itself).  The weighted values of S_C are not: states are float32 results and are carried on, so
+// multiplies it, are rounded once (half a step each, as the result itself; float16: times a power of two, of a row of scores or of the state, so that neither small nor large ones
+// lose more; for the rows' 16381 tokens of 8 heads of 64 x 64 took 63.6 us, now 66.5).  The weighted values of S_C are not: states are float32 results and are carried on, so
 // the values go in as a sum of numbers of 16 bits, each what the ones before it left: three bfloat16 or two float16 (2^-24, 2^-22 of the value; two bfloat16 leave 2^-18,
 // and the states were off by 2.4e-6 in the 2-norm).
 #pragma once
@@ -602,7 +603,7 @@ template <typename T, int DK> struct WalkShape {
         int dead;
         Table dec[2];
         alignas(8) float low[2][kIsBf16<T> ? 2 : kChunk];            // of the sums within blocks: what their additions rounded off (up to 2e-4, of weights that bfloat16 rounds by 2e-3)
-        float most[kIsBf16<T> ? 1 : 32];
+        float most[kIsBf16<T> ? 1 : 32], row_most[4][kIsBf16<T> ? 1 : kChunk];
     };
     static constexpr int TILES = 2 * STAGE + TERMS * V_BYTES + IMAGE;
     static constexpr int SMEM = TILES + sizeof(Small);
@@ -629,6 +630,47 @@ __device__ __forceinline__ float walk_largest(float v, float* parts)
     for (int i = 0; i < kWalkWarps; ++i)
         v = fmaxf(v, parts[i]);
     return v;
+}
+
+// float16: weights of a row (scores times decays) go into their product times a power of two, the row's, so that they neither overflow nor vanish: `most`, the largest
+// of them, is taken to 2^13 .. 2^14, or towards there by `highest` at most.  A product of the smallest numbers, 2^-48, is held to 11 bits that way.
+constexpr int kHighest = 60;
+__device__ __forceinline__ float row_power(float most, int highest, float& inverse)
+{
+    const int x = (int)((__float_as_uint(most) >> 23) & 255) - 127, k = min(max(13 - x, -100), highest);
+    inverse = __uint_as_float((uint32_t)(127 - k) << 23);
+    return __uint_as_float((uint32_t)(127 + k) << 23);
+}
+// (together with `unit`, the state's power of two, it stays below 2^100)
+__device__ __forceinline__ int highest_with(float unit) { return min(kHighest, 100 - ((int)(__float_as_uint(unit) >> 23) - 127)); }
+template <int N> __device__ __forceinline__ float largest(const float (&v)[N])
+{
+    float m = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        m = fmaxf(m, fabsf(v[j]));
+    return m;
+}
+// Weights as 16-bit numbers.  float16: times a power of two of their own, of which `inverse` is left, until the row's is known (`change`: that one over theirs, 1 at most).
+template <typename T, int N> __device__ __forceinline__ void pack_weights(const float (&v)[N], uint32_t (&to)[N / 2], float& most, float& inverse)
+{
+    float up = 1.f;
+    if (!kIsBf16<T>) {
+        most = largest(v);
+        up = row_power(most, kHighest, inverse);
+    }
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j)
+        to[j] = kIsBf16<T> ? pack16<T>(v[2 * j], v[2 * j + 1]) : pack16<T>(v[2 * j] * up, v[2 * j + 1] * up);
+}
+template <int N> __device__ __forceinline__ void change_power(uint32_t (&v)[N], float change)
+{
+    const __half2 f = __float2half2_rn(change);  // (2^-24 at least, or nothing)
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v[j]), f);
+        v[j] = *reinterpret_cast<const uint32_t*>(&r);
+    }
 }
 
 // Rows as [batch][tokens][heads][channels] for the copy engines.
@@ -900,7 +942,7 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
         } else {
             load_state(S, p, p.state, piece.owner, head, row, col0 + sub * 16);
         }
-        float unit = 1.f, unit_v = 1.f;
+        float unit = 1.f, unit_v = 1.f, unit_row = 1.f;
         // the image of the state in 16 bits, [8 groups of 8 columns][DK rows]; float16: times a power of two, so that it neither overflows nor vanishes
         auto put_image = [&]() {
             float up = 1.f;
@@ -963,31 +1005,28 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
         auto weigh = [&](int i) {
             const Table& dec = sm.dec[i & 1];
             const float across = dec.whole;
-            const float mine = dec.g[row], own = ex2(mine) * p.scale, f = own * dec.before[quarter] * unit;
+            const float mine = dec.g[row], own = ex2(mine) * p.scale;
+            float f = own * dec.before[quarter];
             until(sm.scores, i);
             behind_barrier();
             // a warp has one of the earlier blocks of 32 tokens and a quarter of its rows' own block, where the exponentials are (all of that in one warp took
             // 1700 clocks of a chunk's 4600; the later blocks are zeros)
-            uint32_t packed[16];
+            uint32_t packed[16], own_block[4];
+            float most = 0.f, most_own = 0.f, over = 0.f, over_own = 0.f;           // (nothing is changed into nothing)
             if (sub < quarter) {
                 float v[32];
                 tmem_ld32(scores + sub * 32 + lanes, v);
                 decay_earlier(v, own * between(dec, sub, quarter), dec.to_end + sub * 32);
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+                pack_weights<T>(v, packed, most, over);
             } else {
 #pragma unroll
                 for (int j = 0; j < 16; ++j)
                     packed[j] = 0;
             }
-            if (sub != quarter)
-                tmem_st16(operand + sub * 16 + lanes, packed);
             {
                 const int at = quarter * 32 + sub * 8;
                 float v[8];
                 tmem_ld8(scores + at + lanes, v);
-                uint32_t r[4];
                 const float* low = sm.low[i & 1];
                 const float mine_low = kIsBf16<T> ? 0.f : low[row];
 #pragma unroll
@@ -998,11 +1037,32 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
                         const float2 l = *reinterpret_cast<const float2*>(low + at + j);
                         d0 += mine_low - l.x, d1 += mine_low - l.y;
                     }
-                    const uint32_t w = pack16<T>(v[j] * (p.scale * ex2(d0)), v[j + 1] * (p.scale * ex2(d1)));
-                    r[j / 2] = lane > sub * 8 + j ? w : lane == sub * 8 + j ? w & 0xffffu : 0u;
+                    v[j] *= p.scale * ex2(d0), v[j + 1] *= p.scale * ex2(d1);
+                    if (!kIsBf16<T>) {
+                        v[j] = lane >= sub * 8 + j ? v[j] : 0.f;
+                        v[j + 1] = lane > sub * 8 + j ? v[j + 1] : 0.f;
+                    }
                 }
-                tmem_st4(operand + at / 2 + lanes, r);
+                pack_weights<T>(v, own_block, most_own, over_own);
+                if (kIsBf16<T>) {
+#pragma unroll
+                    for (int j = 0; j < 8; j += 2)
+                        own_block[j / 2] = lane > sub * 8 + j ? own_block[j / 2] : lane == sub * 8 + j ? own_block[j / 2] & 0xffffu : 0u;
+                }
             }
+            if (kIsBf16<T>) {
+                f *= unit;
+            } else {                             // the power of the four warps that share the row
+                sm.row_most[sub][row] = fmaxf(most, most_own);
+                asm volatile("bar.sync %0, 128;" :: "r"(3 + quarter) : "memory");
+                const float up = row_power(fmaxf(fmaxf(sm.row_most[0][row], sm.row_most[1][row]), fmaxf(sm.row_most[2][row], sm.row_most[3][row])), highest_with(unit), unit_row);
+                change_power(packed, up * over);
+                change_power(own_block, up * over_own);
+                f *= unit * up;
+            }
+            if (sub != quarter)
+                tmem_st16(operand + sub * 16 + lanes, packed);
+            tmem_st4(operand + quarter * 16 + sub * 4 + lanes, own_block);
             until(sm.state, i);
             behind_barrier();
             float v[16];
@@ -1035,6 +1095,8 @@ __global__ void __launch_bounds__(kWalkBlock, 1) walk_kernel(const __grid_consta
             until(sm.out, i);
             behind_barrier();
             tmem_ld16(results_at(i) + sub * 16 + lanes, v);
+            if (!kIsBf16<T>)
+                scale_all(v, unit_row);
             // through the place of the values, which are done with, so that rows are written as a whole
             char* stage = smem + (values_at(i) - tiles);
 #pragma unroll

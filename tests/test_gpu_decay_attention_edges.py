@@ -53,22 +53,29 @@ def _roundings(i, args):
     return 2 * (dk + dv + 3 * 128) + 8 * L + 16 * -(-tokens // 128) + 64
 
 
-def _check(i, scale=None):
-    """y and the gradients of the rows are off by the half step of each operand of 16 bits besides float32's operations; states, dstate, dA and ddelta_bias by these alone."""
+def _check_forward(i, scale=None):
+    """y is off by the half step of each operand of 16 bits besides float32's operations, the last state by these alone."""
     args = _args(i, i["q"].shape[-1] ** -0.5 if scale is None else scale)
     R = _roundings(i, args) * au.U
-    h = au.half_step(i["q"].dtype)
     y, last = _forward(i, scale)
     want, want_last, _, _ = au.attend(*args)
     mag, mag_last, _, _ = au.attend(*args, magnitudes=True)
-    au.within(y[0], want, (h + R) * mag, y.dtype, "y")
+    au.within(y[0], want, (au.half_step(y.dtype) + R) * mag, y.dtype, "y")
     au.within(last, want_last, R * mag_last, F, "state_out")
+    assert block.device_error(0) == 0
+
+
+def _check_grads(i, scale=None):
+    """The same of the rows' gradients, and of dstate, dA and ddelta_bias."""
+    args = _args(i, i["q"].shape[-1] ** -0.5 if scale is None else scale)
+    R = _roundings(i, args) * au.U
     dlast = au.f64(i["dlast"])
     ref, mag = (au.attend_grad(au.f64(i["dy"])[0], *args, dlast, magnitudes=m) for m in (False, True))
     for n, t in _grads(i, scale).items():
         rows = n in ("dq", "dk", "dv", "ddelta")
         more = 256 + (0 if rows else args[2].shape[0])
-        au.within(t[0] if rows else t, ref[n], (h * (n in ("dq", "dk", "dv")) + 2 * R + more * au.U) * mag[n], t.dtype, n)
+        half = au.half_step(t.dtype) if n in ("dq", "dk", "dv") else 0.0
+        au.within(t[0] if rows else t, ref[n], (half + 2 * R + more * au.U) * mag[n], t.dtype, n)
     assert block.device_error(0) == 0
 
 
@@ -78,7 +85,8 @@ def test_strong_decays_among_weak_ones(strength, dtype):
     i = _inputs(260, 4, 32, 32, dtype, 5)
     strong = torch.rand(1, 260, 4, generator=torch.Generator(device=DEV).manual_seed(6), device=DEV) < 0.3
     i["delta"] = torch.where(strong, i["delta"].float() * strength * 50, i["delta"].float() * 0.01).clamp(max=3e4).to(dtype)
-    _check(i)
+    _check_forward(i)
+    _check_grads(i)
 
 
 @pytest.mark.parametrize("dtype", [B, H])
@@ -103,3 +111,32 @@ def test_weak_decays_behind_many_that_forget_everything(dtype, large, at):
     for n in ("dA", "ddelta_bias"):
         au.within(got[n], ref[n], 200 * au.U * mag[n], F, n)
     au.within(got["ddelta"][0], ref["ddelta"], 200 * au.U * mag["ddelta"], dtype, "ddelta")
+
+
+def _scaled(q=1.0, k=1.0, v=1.0, dy=1.0, state=0.0):
+    i = _inputs(200, 2, 64, 64, H, 9)
+    i.update(q=i["q"] * q, k=i["k"] * k, v=i["v"] * v, dy=i["dy"] * dy, state=i["state"] * state, dlast=i["dlast"] * state)
+    return i
+
+
+def _names(sizes):
+    return "-".join("%s%g" % i for i in sizes.items())
+
+
+@pytest.mark.parametrize("sizes", [dict(q=1e-3, k=1e-3, v=1e3), dict(q=1e-4, k=1e-4, v=3e3), dict(q=300.0, k=300.0, v=1e-3), dict(q=1e-3, k=1e3), dict(q=3e3, k=3e3, v=1e-4, scale=1e-2)],
+                         ids=_names)
+@pytest.mark.parametrize("state", [0.0, 1e-3, 10.0])
+def test_small_and_large_products_in_float16(sizes, state):
+    """Scores far below the smallest normal float16 (6e-5) and above the largest (65504), between operands and results that are neither."""
+    sizes = dict(sizes)
+    scale = sizes.pop("scale", None)
+    i = _scaled(**sizes, state=state / sizes["q"])
+    _check_forward(i, scale)
+
+
+@pytest.mark.parametrize("q, state", [(1.0, 0.0), (1.0, 1e-20), (1.0, 1.0), (0.0, 1e20)])
+def test_rows_that_meet_nothing_in_float16(q, state):
+    """Queries and keys of zero beside others, or all queries, with states far from one."""
+    i = _scaled(q=q, state=state)
+    i["q"][:, 3::5], i["k"][:, :40] = 0, 0
+    _check_forward(i)
