@@ -150,8 +150,7 @@ int ttc_selective_scan_grad(int32_t device, const ttc_scan_args* a, const ttc_sc
  * A [heads], delta_bias [heads] (NULL: 0; not used without delta).  state [batch][heads][dk][dv] float32 is S in front of every sequence
  * (NULL: zero), state_out receives the last one; it may be state itself.  y may be v (the same pointer and strides).
  * Exponents A D_t are expected to be <= 0; minus infinity forgets everything.  Tokens go through the tensor cores in chunks of 128, counted from their
- * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, earlier tokens' too, and of those behind it.  float16: in the gradients,
- * products scale q . k and dy . v have to stay below 65504 and are rounded as float16 where they are small.  Scratch: none where sequences, heads and columns fill the SMs; else sequences are walked along in pieces, with
+ * sequence's begin: an infinity or NaN reaches the results of the whole chunk that it stands in, earlier tokens' too, and of those behind it.  Scratch: none where sequences, heads and columns fill the SMs; else sequences are walked along in pieces, with
  * 512 bytes for each value channel (dv rounded up to 64 or 128) of a piece and head, of which there are as many as SMs, and one more for each packed sequence.  Rows of q, k, v (and
  * dy of the gradients) that do not begin on 16 bytes, whose heads do not (dk, dv not a multiple of 8) or that are one row for many tokens are copied there too, 2 bytes for each channel.
  */

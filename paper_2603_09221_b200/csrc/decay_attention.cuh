@@ -21,7 +21,7 @@
 //
 // Roundings.  Sums are float32 in tensor memory, states float32.  Operands of the tensor cores are 16 bits: scores with their decay, and S_0 where q
 // multiplies it, are rounded once (half a step each, as the result itself; float16: times a power of two, of a row of scores or of the state, so that neither small nor large ones
-// lose more; for the rows' 16381 tokens of 8 heads of 64 x 64 took 63.6 us, now 66.5).  The weighted values of S_C are not: states are float32 results and are carried on, so
+// lose more: 16381 tokens of 8 heads of 64 x 64 took 63.6 us without the rows', 66.5 with them).  The weighted values of S_C are not: states are float32 results and are carried on, so
 // the values go in as a sum of numbers of 16 bits, each what the ones before it left: three bfloat16 or two float16 (2^-24, 2^-22 of the value; two bfloat16 leave 2^-18,
 // and the states were off by 2.4e-6 in the 2-norm).
 #pragma once
@@ -641,8 +641,8 @@ __device__ __forceinline__ float row_power(float most, int highest, float& inver
     inverse = __uint_as_float((uint32_t)(127 - k) << 23);
     return __uint_as_float((uint32_t)(127 + k) << 23);
 }
-// (together with `unit`, the state's power of two, it stays below 2^100)
-__device__ __forceinline__ int highest_with(float unit) { return min(kHighest, 100 - ((int)(__float_as_uint(unit) >> 23) - 127)); }
+// (times the state's power of two, `unit`, it stays below 2^60, so that what the state gives to the row, and its product with another in the gradients, stays in float32)
+__device__ __forceinline__ int highest_with(float unit) { return min(kHighest, kHighest - ((int)(__float_as_uint(unit) >> 23) - 127)); }
 template <int N> __device__ __forceinline__ float largest(const float (&v)[N])
 {
     float m = 0.f;

@@ -58,6 +58,7 @@ template <int DK, int DV> struct GradShape {
         alignas(16) float to[4][96];             // [block][earlier token]: decay from it to the block's begin
         alignas(16) float from[kChunk];          // exp from each token's block's begin
         float sums[4][kChunk], dots[4][kChunk], within[4][kChunk], pairs[4][4];
+        float most[2][4][kChunk];                // float16: the largest weights of a row's warps
     };
     static constexpr int SMEM = TILES + sizeof(Small);
 };
@@ -142,6 +143,12 @@ template <typename T, int COLS> __device__ __forceinline__ float weigh_row(uint3
         tmem_st16(here, r);
     }
     return dot;
+}
+
+// float16: the power of two that a row's weights are taken times, from what its four warps have left in `most`; `inverse` of it.
+__device__ __forceinline__ float power_of_row(const float (&most)[4][kChunk], int row, float unit, float& inverse)
+{
+    return row_power(fmaxf(fmaxf(most[0][row], most[1][row]), fmaxf(most[2][row], most[3][row])), highest_with(unit), inverse);
 }
 
 __device__ __forceinline__ long long packed_row(const AttnDev& p, const Chunk& c, int t) { return c.seq * p.seqs.tokens + c.row0 + t; }
@@ -321,14 +328,13 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
     // documents, 8 heads of 64 x 64: 130.4 -> 129.3 us).
     const int row = quarter * 32 + lane;
     uint32_t packed[16], diagonal[4];
+    float most = 0.f, most_own = 0.f, over = 0.f, over_own = 0.f;
     float row_sum = 0.f;
     if (sub < quarter) {
         float v[32];
         tmem_ld32(slopes + sub * 32 + lanes, v);
         decay_earlier(v, sm.from[row], sm.to[quarter] + sub * 32);
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            packed[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+        pack_weights<T>(v, packed, most, over);
         if (g.want_l) {
             float w[32];
             tmem_ld32(scores + sub * 32 + lanes, w);
@@ -355,9 +361,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             v[j] = first + j <= lane ? v[j] * ex2((own - dec.g[from + j]) + (own_low - dec.low[from + j])) : 0.f;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            diagonal[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
+        pack_weights<T>(v, diagonal, most_own, over_own);
         if (g.want_l) {                          // pairs on both sides of t whose earlier token is one of these eight: of t among them one by one, of a later t all
             float w[8], sum = 0.f;
             tmem_ld8(scores + from + lanes, w);
@@ -379,10 +383,20 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
                 sm.within[sub][from + first_value<8, 32>(lane)] = v[0];
         }
     }
+    if (!kIsBf16<T>)
+        sm.most[0][sub][row] = fmaxf(most, most_own);
     // the four warps of these rows have read what is overwritten now
     before_barrier();
     asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
     behind_barrier();
+    float up = 1.f, down = 1.f;
+    if (!kIsBf16<T>) {
+        const float unit = g.unit_S[at];
+        up = power_of_row(sm.most[0], row, unit, down);
+        change_power(packed, up * over);
+        change_power(diagonal, up * over_own);
+        up *= unit;
+    }
     if (sub != quarter)
         tmem_st16(slopes + sub * 16 + lanes, packed);
     tmem_st4(slopes + quarter * 16 + sub * 4 + lanes, diagonal);
@@ -402,7 +416,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
         __syncwarp();
         behind_barrier();
     }
-    sm.dots[sub][row] = weigh_row<T, DK>(results + lanes, smem, row, sub, from_begin(dec, row) * (kIsBf16<T> ? 1.f : g.unit_S[at]));
+    sm.dots[sub][row] = weigh_row<T, DK>(results + lanes, smem, row, sub, from_begin(dec, row) * up) * down;
     sm.sums[sub][row] = row_sum;
     tmem_st_done();
     before_barrier();
@@ -427,9 +441,9 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_q(con
     }
     grad_products_done(sm.ctl, 2);
     if (g.part_q)                                // (in the place of queries and keys)
-        stage_part<DK>(results + lanes, smem, row, sub, p.scale);
+        stage_part<DK>(results + lanes, smem, row, sub, p.scale * down);
     else if (g.dq.ptr)
-        stage_row<T, DK>(results + lanes, smem, row, sub, p.scale);
+        stage_row<T, DK>(results + lanes, smem, row, sub, p.scale * down);
     end_grad(sm.ctl, tmem);
     if (g.part_q)
         store_part<DK>(smem, g.part_q + (packed_row(p, c, 0) * p.heads + head) * p.dk, (long long)p.heads * p.dk, c.len, p.dk);
@@ -503,6 +517,7 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
     grad_products_done(sm.ctl, 0);
     const int row = quarter * 32 + lane;
     uint32_t packed_v[16], packed_k[16], diagonal_v[4], diagonal_k[4];
+    float most_v = 0.f, most_k = 0.f, own_v = 0.f, own_k = 0.f, over_v = 0.f, over_k = 0.f, over_own_v = 0.f, over_own_k = 0.f;
     float col = 0.f;
     if (sub > quarter) {
         float v[32], w[32];
@@ -520,11 +535,8 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         col *= to_there;
         decay_earlier(v, to_there, sm.from + sub * 32);
         decay_earlier(w, to_there, sm.from + sub * 32);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            packed_v[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
-            packed_k[j] = pack16<T>(w[2 * j], w[2 * j + 1]);
-        }
+        pack_weights<T>(v, packed_v, most_v, over_v);
+        pack_weights<T>(w, packed_k, most_k, over_k);
     } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
@@ -543,15 +555,27 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
             v[j] = later ? v[j] * d : 0.f;
             w[j] = later ? w[j] * d : 0.f;
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            diagonal_v[j] = pack16<T>(v[2 * j], v[2 * j + 1]);
-            diagonal_k[j] = pack16<T>(w[2 * j], w[2 * j + 1]);
-        }
+        pack_weights<T>(v, diagonal_v, own_v, over_own_v);
+        pack_weights<T>(w, diagonal_k, own_k, over_own_k);
+    }
+    if (!kIsBf16<T>) {
+        sm.most[0][sub][row] = fmaxf(most_v, own_v);
+        sm.most[1][sub][row] = fmaxf(most_k, own_k);
     }
     before_barrier();
     asm volatile("bar.sync %0, 128;" :: "r"(1 + quarter) : "memory");
     behind_barrier();
+    float up_v = 1.f, up_k = 1.f, down_v = 1.f, down_k = 1.f;
+    if (!kIsBf16<T>) {
+        const float unit = g.unit_Z[at];
+        up_v = power_of_row(sm.most[0], row, unit, down_v);
+        up_k = power_of_row(sm.most[1], row, unit, down_k);
+        change_power(packed_v, up_v * over_v);
+        change_power(packed_k, up_k * over_k);
+        change_power(diagonal_v, up_v * over_own_v);
+        change_power(diagonal_k, up_k * over_own_k);
+        up_v *= unit, up_k *= unit;
+    }
     if (sub != quarter) {
         tmem_st16(scores + sub * 16 + lanes, packed_v);
         tmem_st16(slopes + sub * 16 + lanes, packed_k);
@@ -564,9 +588,9 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
         __syncwarp();
         behind_barrier();
     }
-    const float f = to_end(dec, row) * (kIsBf16<T> ? 1.f : g.unit_Z[at]);
-    sm.dots[sub][row] = weigh_row<T, DK>(dks + lanes, s_keys, row, sub, f);
-    weigh_row<T, DV>(dvs + lanes, nullptr, row, sub, f);
+    const float f = to_end(dec, row);
+    sm.dots[sub][row] = weigh_row<T, DK>(dks + lanes, s_keys, row, sub, f * up_k) * down_k;
+    weigh_row<T, DV>(dvs + lanes, nullptr, row, sub, f * up_v);
     sm.sums[sub][row] = col;
     tmem_st_done();
     before_barrier();
@@ -590,11 +614,11 @@ template <typename T, int DK, int DV> __device__ __forceinline__ void grad_kv(co
     grad_products_done(sm.ctl, 2);
     // (results in float32 take the place of queries and keys; all tiles are done with)
     if (g.part_k)
-        stage_part<DK>(dks + lanes, smem, row, sub, 1.f);
+        stage_part<DK>(dks + lanes, smem, row, sub, down_k);
     else if (g.dk.ptr)
-        stage_row<T, DK>(dks + lanes, s_keys, row, sub, 1.f);
+        stage_row<T, DK>(dks + lanes, s_keys, row, sub, down_k);
     if (g.dv.ptr)
-        stage_row<T, DV>(dvs + lanes, s_values, row, sub, 1.f);
+        stage_row<T, DV>(dvs + lanes, s_values, row, sub, down_v);
     end_grad(sm.ctl, tmem);
     if (g.part_k)
         store_part<DK>(smem, g.part_k + (packed_row(p, c, 0) * p.heads + head) * p.dk, (long long)p.heads * p.dk, c.len, p.dk);

@@ -140,3 +140,19 @@ def test_rows_that_meet_nothing_in_float16(q, state):
     i = _scaled(q=q, state=state)
     i["q"][:, 3::5], i["k"][:, :40] = 0, 0
     _check_forward(i)
+
+
+@pytest.mark.parametrize("sizes", [dict(q=1e-3, k=1e-3, dy=1e3), dict(v=1e-3, dy=1e-3, q=1e-3, k=1e3), dict(v=1e-3, dy=1e-3, q=1e3, k=1e-3), dict(v=1e-4, dy=1e-3, q=1e-3, k=3e3),
+                                   dict(v=300.0, dy=300.0, q=1e-3, k=1e-3), dict(q=300.0, k=300.0, v=1e-3, dy=1e-3)], ids=_names)
+@pytest.mark.parametrize("state", [0.0, 1e-3, 1.0])
+def test_gradients_of_small_and_large_products_in_float16(sizes, state):
+    """The same of scores and of dy . v."""
+    _check_grads(_scaled(**sizes, state=state))
+
+
+@pytest.mark.parametrize("q, dy, state", [(1.0, 1.0, 0.0), (1.0, 1.0, 1e-20), (1.0, 1.0, 1.0), (0.0, 0.0, 1e15)])
+def test_gradients_of_rows_that_meet_nothing_in_float16(q, dy, state):
+    """Queries, keys, values and gradients of zero beside others, or all queries and gradients, with states far from one."""
+    i = _scaled(q=q, dy=dy, state=state)
+    i["q"][:, 3::5], i["dy"][:, 4::5], i["k"][:, :40], i["v"][:, 60:120], i["dlast"] = 0, 0, 0, 0, i["dlast"] * min(1.0, 1 / max(state, 1.0))
+    _check_grads(i)
