@@ -103,9 +103,9 @@ Way way_of(const ttc_norm_args* a, NormDev& p, std::initializer_list<Operand> ro
     const int each = o.k == 16 ? k : o.k;
     o.threads = threads = std::min(threads, ((vectors + each - 1) / each + 31) / 32 * 32);
     o.rows_per_block = threads == 32 ? kRowsOfWarps : 1;
-    const int size = a->d / a->groups, lanes = size / o.v;
-    p.lanes = lanes;
-    o.mixed = a->groups == 1 ? kNear : size % o.v ? kAcross : lanes <= 32 && !(lanes & (lanes - 1)) ? kNear : o.v > 1 ? kWhole : kAcross;
+    const int size = a->d / a->groups, vectors_of_group = size / o.v;
+    p.lanes = size % o.v == 0 && vectors_of_group <= 32 && !(vectors_of_group & (vectors_of_group - 1)) ? vectors_of_group : 0;
+    o.mixed = a->groups == 1 || p.lanes ? kNear : size % o.v || o.v == 1 ? kAcross : kWhole;
     o.smem = o.mixed ? (size_t)o.rows_per_block * (a->d + a->groups) * sizeof(float) : 0;
     return o;
 }

@@ -40,7 +40,6 @@ struct NormDev {
     float *dw_post, *dscale, *dw_pre;
     float* parts;                                // [count of row workers][3][d]: shares of dw_post, dscale, dw_pre
     int workers;
-    int plain;                                   // h is x
 };
 
 extern __shared__ __align__(16) float bnorm_smem[];
